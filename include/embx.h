@@ -45,7 +45,8 @@ typedef enum {
   EMB_ERR_BUFFER_TOO_SMALL = 7    /* serialization buffer too small (len_out is set)  */
 } emb_status_t;
 
-typedef enum { EMB_DTYPE_F32 = 0, EMB_DTYPE_F16 = 1 } emb_dtype_t;
+/* Tables are f32 or f16; the dense layers (embx_dense.h) take all three. */
+typedef enum { EMB_DTYPE_F32 = 0, EMB_DTYPE_F16 = 1, EMB_DTYPE_BF16 = 2 } emb_dtype_t;
 
 /* Reduction of a table's bags (Sec. II-B): the sum, or the sum over the bag length
  * (an empty bag gives +0.0 either way; an out-of-range index adds nothing but counts

@@ -31,7 +31,7 @@ _lib = ctypes.CDLL(LIB_PATH)
 # ---------------------------------------------------------------- constants (include/embx.h)
 OK, ERR_INVALID_ARGUMENT, ERR_UNSUPPORTED, ERR_OUT_OF_MEMORY, ERR_DEVICE, ERR_NOT_BOUND, \
     ERR_INDEX_OUT_OF_RANGE, ERR_BUFFER_TOO_SMALL = range(8)
-DTYPE_F32, DTYPE_F16 = 0, 1
+DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2   # tables: the first two; dense layers: all
 STRAT_AUTO, STRAT_LDS, STRAT_HOT, STRAT_DEDUP, STRAT_GATHER = -1, 0, 1, 2, 3
 STRATEGY_NAMES = {0: "LDS", 1: "HOT", 2: "DEDUP", 3: "GATHER", 4: "STREAM"}
 POOL_SUM, POOL_MEAN = 0, 1
@@ -430,3 +430,7 @@ def dedup_tile(idx, stream=None):
                                      _stream_ptr(stream)), "emb_debug_dedup_tile")
     k = int(nu.item())
     return uniq[:k], inv[:n]
+
+
+if torch is not None:
+    from .dense import ACTIVATIONS, gated_ffn, gated_ffn_backward, linear, linear_backward  # noqa: E402,F401

@@ -56,6 +56,8 @@ LOOKUP_UNIFORM_PARTS = (5, 6, 11)
 # of row loads in flight per step a plan may choose (kGatherStepChoices in device_types.hpp)
 GATHER_PARTS = 4
 GATHER_STEPS = (12, 13, 16)
+# dense.hip: one part per element type (f32, f16, bf16)
+DENSE_PARTS = 3
 
 
 def _run_all(cmds, verbose):
@@ -96,11 +98,15 @@ def build(verbose: bool = False) -> str:
         cmds.append([hipcc, *HIP_FLAGS, *UNIFORM_FLAGS, f"-DEMBX_GPART={part}", "-DEMBX_GKS=12", f"-DEMBX_FAR={FAR}",
                      "-c", os.path.join(CSRC, "gather.hip"), "-o", o])
         far[os.path.join(BUILD, f"gather_{part}_k12.o")] = o
+    for part in range(DENSE_PARTS):
+        o = os.path.join(BUILD, f"dense_{part}.o")
+        cmds.append([hipcc, *HIP_FLAGS, f"-DEMBX_DPART={part}", "-c", os.path.join(CSRC, "dense.hip"), "-o", o])
+        objs.append(o)
     o = os.path.join(BUILD, "api.o")
     cmds.append([hipcc, *HIP_FLAGS, "-x", "hip", "-c", os.path.join(CSRC, "api.cpp"), "-o", o])
     objs.append(o)
     # the planner is plain host C++: every binary64 operation rounds as written
-    for name in ("planner", "queues"):
+    for name in ("planner", "queues", "dense_api"):
         o = os.path.join(BUILD, f"{name}.o")
         cmds.append(["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, f"{name}.cpp"), "-o", o])
         objs.append(o)

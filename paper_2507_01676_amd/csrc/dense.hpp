@@ -1,0 +1,57 @@
+// What the dense layers' entry points (dense_api.cpp) and kernels (dense.hip) share.
+#ifndef EMBX_DENSE_HPP
+#define EMBX_DENSE_HPP
+
+#include <cstddef>
+#include <cstdint>
+
+namespace embx {
+
+enum DenseType { kDenseF32 = 0, kDenseF16 = 1, kDenseBF16 = 2 };
+
+// The three products of a layer.  A matrix is "reduction-major" (R) where consecutive
+// elements in memory step along the outputs, and "along the reduction" (K) otherwise.
+enum DenseKind {
+  kForward = 0,      // C[i][j] = sum_r A[i][r] B[j][r]   A = x, B = W        (K, K)
+  kGated = 1,        // the same with two B's, joined by the gate
+  kInputGrad = 2,    // C[i][j] = sum_r A[i][r] B[r][j]   A = dz, B = W       (K, R)
+  kWeightGrad = 3    // C[i][j] = sum_r A[r][i] B[r][j]   A = dz, B = x       (R, R)
+};
+
+// One matrix product.  Arrays of two: kGated's two weights and results; kInputGrad's two
+// products summed into one result (parts = 2); kWeightGrad's two results (parts = 2).
+struct DenseGemm {
+  const void* a[2];
+  const void* b[2];
+  void* c[2];
+  void* z[2];              // forward kinds: sums before the activation, or NULL
+  const void* bias[2];     // forward kinds, or NULL
+  const void* res;         // kForward, or NULL
+  float* partial;          // [parts of the result][splits][ni][nj], with splits > 1
+  int64_t lda, ldb[2], ldc[2], ldz[2], ldr;
+  int32_t ni, nj, nr;      // C is [ni][nj], the sum over nr (in each part)
+  int32_t parts, splits, act;
+};
+
+// dz = dy * act'(z), or dg, du; and partial column sums of them
+struct DenseSlope {
+  const void* dy;
+  const void* z[2];        // z, or g and u; NULL z[0]: dz = dy (only column sums)
+  void* dz[2];             // NULL: not written
+  float* colsum[2];        // [row blocks][n], or NULL
+  int64_t lddy, ldz[2], lddz;
+  int32_t m, n, act, gated, row_blocks;
+};
+
+// launches of the kernels of one type (dense.hip is compiled once per type); 0 or a hipError_t
+#define EMBX_DENSE_DECLARE(NAME)                                                        \
+  int dense_gemm_##NAME(int kind, const DenseGemm& g, void* stream);                    \
+  int dense_slope_##NAME(const DenseSlope& s, void* stream);                            \
+  int dense_colsum_##NAME(const float* p, int32_t blocks, int32_t n, void* out, void* stream);
+EMBX_DENSE_DECLARE(f32)
+EMBX_DENSE_DECLARE(f16)
+EMBX_DENSE_DECLARE(bf16)
+#undef EMBX_DENSE_DECLARE
+
+}  // namespace embx
+#endif
