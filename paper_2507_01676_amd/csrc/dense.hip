@@ -51,6 +51,29 @@ __device__ inline float slope_f(float z, int act) {
   }
 }
 
+// the same of eight values: one branch
+__device__ inline void act8(float* z, int act) {
+  switch (act) {
+    case EMB_ACT_RELU:
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = z[e] < 0.0f ? 0.0f : z[e];
+      break;
+    case EMB_ACT_SIGMOID:
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] = sigmoid_f(z[e]);
+      break;
+    case EMB_ACT_SILU:
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] *= sigmoid_f(z[e]);
+      break;
+    case EMB_ACT_GELU:
+#pragma unroll
+      for (int e = 0; e < 8; ++e) z[e] *= phi_f(z[e]);
+      break;
+    default: break;
+  }
+}
+
 // ---------------------------------------------------------------- epilogue
 
 // Stores one element of the result from its sums (s1: the up projection's).
@@ -76,18 +99,18 @@ __device__ inline void finish(const DenseGemm& g, int part, int i, int j, float 
 
 // ---------------------------------------------------------------- matrix products
 
-constexpr int kBM = 64, kBN = 64, kBK = 32, kPad = 8;
+constexpr int kSM = 64, kSN = 64, kSK = 32, kPad = 8;
 
 // A tile of 64 x 64 results, four wavefronts of 32 x 32 each.
 template <int TYPE, int KIND>
 __global__ __launch_bounds__(256) void dense_tile(DenseGemm g) {
   using T = typename Elem<TYPE>::T;
-  __shared__ T sa[kBM][kBK + kPad], sb[kBN][kBK + kPad];
+  __shared__ T sa[kSM][kSK + kPad], sb[kSN][kSK + kPad];
   constexpr bool kGate = KIND == kGated;
-  constexpr int kCols = kGate ? kBN / 2 : kBN;   // result columns of a tile
+  constexpr int kCols = kGate ? kSN / 2 : kSN;   // result columns of a tile
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int tiles_j = (g.nj + kCols - 1) / kCols;
-  const int i0 = static_cast<int>(blockIdx.x / tiles_j) * kBM, j0 = static_cast<int>(blockIdx.x % tiles_j) * kCols;
+  const int i0 = static_cast<int>(blockIdx.x / tiles_j) * kSM, j0 = static_cast<int>(blockIdx.x % tiles_j) * kCols;
   const int wi = (wave >> 1) * 32, wj = (wave & 1) * 32;
   const int q = lane >> 4, c = lane & 15;
   const int bpart = KIND == kWeightGrad ? blockIdx.z : 0;
@@ -95,25 +118,25 @@ __global__ __launch_bounds__(256) void dense_tile(DenseGemm g) {
   const int parts = KIND == kInputGrad ? g.parts : 1;
   for (int part = 0; part < parts; ++part) {
     const T* a = static_cast<const T*>(g.a[KIND == kWeightGrad ? bpart : part]);
-    for (int r0 = 0; r0 < g.nr; r0 += kBK) {
+    for (int r0 = 0; r0 < g.nr; r0 += kSK) {
       __syncthreads();
-      for (int e = tid; e < kBM * kBK; e += 256) {
+      for (int e = tid; e < kSM * kSK; e += 256) {
         if constexpr (KIND == kWeightGrad) {
-          const int r = e / kBM, i = e % kBM;
+          const int r = e / kSM, i = e % kSM;
           sa[i][r] = r0 + r < g.nr && i0 + i < g.ni ? a[(r0 + r) * g.lda + i0 + i] : T(0.0f);
         } else {
-          const int i = e / kBK, r = e % kBK;
+          const int i = e / kSK, r = e % kSK;
           sa[i][r] = r0 + r < g.nr && i0 + i < g.ni ? a[(i0 + i) * g.lda + r0 + r] : T(0.0f);
         }
       }
-      for (int e = tid; e < kBN * kBK; e += 256) {
+      for (int e = tid; e < kSN * kSK; e += 256) {
         if constexpr (KIND == kForward || KIND == kGated) {
-          const int row = e / kBK, r = e % kBK;
+          const int row = e / kSK, r = e % kSK;
           const int mat = kGate ? row / kCols : 0, j = row - mat * kCols;
           const T* b = static_cast<const T*>(g.b[mat]);
           sb[row][r] = r0 + r < g.nr && j0 + j < g.nj ? b[(j0 + j) * g.ldb[mat] + r0 + r] : T(0.0f);
         } else {
-          const int r = e / kBN, j = e % kBN;
+          const int r = e / kSN, j = e % kSN;
           const int mat = KIND == kInputGrad ? part : 0;
           const T* b = static_cast<const T*>(g.b[mat]);
           sb[j][r] = r0 + r < g.nr && j0 + j < g.nj ? b[(r0 + r) * g.ldb[mat] + j0 + j] : T(0.0f);
@@ -129,7 +152,7 @@ __global__ __launch_bounds__(256) void dense_tile(DenseGemm g) {
           const T* pb = kGate ? sb[fj * kCols + (wave & 1) * 16 + c] : sb[wj + fj * 16 + c];
           if constexpr (TYPE == kDenseF32) {
 #pragma unroll
-            for (int s = 0; s < kBK / 4; ++s)
+            for (int s = 0; s < kSK / 4; ++s)
               acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x4f32(pb[4 * s + q], pa[4 * s + q], acc[fi][fj], 0, 0, 0);
           } else {
             using V = typename Elem<TYPE>::V;
@@ -153,6 +176,584 @@ __global__ __launch_bounds__(256) void dense_tile(DenseGemm g) {
         const int j = j0 + (kGate ? (wave & 1) * 16 : wj + fj * 16) + 4 * q + e;
         if (i < g.ni && j < g.nj) finish<TYPE, KIND>(g, bpart, i, j, acc[fi][fj][e], kGate ? acc[fi][1][e] : 0.0f);
       }
+}
+
+// ---------------------------------------------------------------- tiles of 16-bit types
+//
+// A workgroup computes BM x BN sums (kGated: BN / 2 columns of each projection) in WI x WJ
+// wavefronts.  Each step takes kBK of the reduction of both operands from LDS, while later steps are
+// on their way there.  A tile lies in LDS as in memory: rows of kBK elements
+// (operand along the reduction) or kBK rows of BM or BN elements (reduction-major), with the
+// 16-byte chunks of a row permuted so that what a wavefront reads at once lies in different
+// banks.  Chunks go from memory to LDS without registers, so their order within a wavefront's
+// 1 KB is fixed in LDS, and the permutation is applied to the address each lane loads from.
+constexpr int kBK = 64;
+constexpr int kOutOfRange = static_cast<int>(0x80000000u);   // past every descriptor: reads zeros
+
+#define LDS_PTR(T) __attribute__((address_space(3))) T*
+
+__device__ inline uint32_t lds_address(const void* p) {
+  return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((LDS_PTR(const void))p));
+}
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+__device__ inline i32x4 descriptor(const void* base) {
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  i32x4 r;
+  r[0] = __builtin_amdgcn_readfirstlane(static_cast<int>(p));
+  r[1] = __builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32) & 0xffff);
+  r[2] = 0x7fffffff;
+  r[3] = 0x00027000;
+  return r;
+}
+
+// 16 bytes a lane from descriptor + voffset to LDS at lds + 16 * lane.  The wait for it is
+// written out where the tile is needed (stage_done): the compiler, told of the write, would
+// wait at the next LDS read of any kind.
+__device__ inline void load_to_lds(i32x4 rsrc, int voffset, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+               :: "s"(lds), "v"(voffset), "s"(rsrc) : "memory");
+}
+
+// Waits until all but this wavefront's last LOADS loads are in LDS and every LDS read of it is done,
+// then for the other wavefronts.
+template <int LOADS>
+__device__ inline void stage_done() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LOADS) : "memory");
+}
+
+template <int TYPE>
+__device__ inline f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
+  using V = typename Elem<TYPE>::V;
+  if constexpr (TYPE == kDenseF16)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
+}
+
+// One operand's tile of ROWS results (rows of x or dz, columns of the result) by kBK.
+// RM: reduction-major in memory.
+template <int ROWS, bool RM, int WAVES>
+struct Tile {
+  static constexpr int kBytes = ROWS * kBK * 2;
+  static constexpr int kLoads = kBytes / 1024 / WAVES;     // 1 KB pieces a wavefront loads
+  static constexpr int kRowBytes = RM ? ROWS * 2 : kBK * 2;
+  static constexpr int kChunks = kRowBytes / 16;
+  static constexpr int kRowsPerLoad = 1024 / kRowBytes;
+  static_assert(kBytes % (1024 * WAVES) == 0, "every wavefront loads alike");
+
+  // the permutation of a row's chunks
+  __device__ static int swizzle(int row) {
+    if (RM) return (kChunks >= 16 ? (row & 3) | ((row >> 1) & 4) : row & 3) << 1;
+    return (row >> 1) & 7;
+  }
+
+  // row and chunk in memory that this lane loads with piece n
+  __device__ static int load_row(int n, int wave, int lane) { return (n * WAVES + wave) * kRowsPerLoad + lane / kChunks; }
+  __device__ static int load_chunk(int row, int lane) { return (lane % kChunks) ^ swizzle(row); }
+
+  int voff[kLoads];
+
+  // rows: valid rows (RM: valid columns, a multiple of 8) from the tile's origin on
+  __device__ void init(int wave, int lane, int64_t ld, int rows) {
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int row = load_row(n, wave, lane), chunk = load_chunk(row, lane);
+      const bool in = RM ? chunk * 8 < rows : row < rows;
+      voff[n] = in ? static_cast<int>(row * ld * 2) + chunk * 16 : kOutOfRange;
+    }
+  }
+
+  // The same piece of a matrix whose rows start anywhere: elements of a chunk one by one where it is not
+  // whole, else all at once, at any alignment.
+  template <class T>
+  __device__ static s16x8 fetch(const T* base, int64_t ld, int rows, int valid, int wave, int lane, int n) {
+    const int row = load_row(n, wave, lane), at = load_chunk(row, lane) * 8;
+    const int count = (RM ? row < valid : row < rows) ? (RM ? rows : valid) - at : 0;
+    const T* p = base + row * ld + at;
+    s16x8 v = {};
+    if (count >= 8) {
+      __builtin_memcpy(&v, p, 16);
+    } else if (count > 0) {
+#pragma unroll
+      for (int e = 0; e < 7; ++e)
+        if (e < count) v[e] = __builtin_bit_cast(short, p[e]);
+    }
+    return v;
+  }
+  __device__ static void put(char* tile, s16x8 v, int wave, int lane, int n) {
+    *reinterpret_cast<s16x8*>(tile + (n * WAVES + wave) * 1024 + lane * 16) = v;
+  }
+
+  // valid: how many of this step's kBK are inside
+  __device__ void load(i32x4 rsrc, uint32_t lds, int wave, int lane, int valid, int n) const {
+    int v = voff[n];
+    if (valid < kBK) {
+      const int row = load_row(n, wave, lane), chunk = load_chunk(row, lane);
+      v = (RM ? row < valid : chunk * 8 < valid) ? v : kOutOfRange;
+    }
+    load_to_lds(rsrc, v, lds + (n * WAVES + wave) * 1024);
+  }
+
+  // fragment of 16 results (from `first` on, a multiple of 16) by 32 of the reduction (half ks):
+  // lane: result lane % 16, reduction 8 (lane / 16) .. + 7
+  __device__ static s16x8 fragment(const char* tile, int first, int ks, int lane) {
+    const int q = lane >> 4, c = lane & 15;
+    if constexpr (RM) {
+      const int r = ks * 32 + 8 * q + (c >> 2);
+      const int unit = (first >> 4) ^ (swizzle(r) >> 1);     // (r + 4 has the same permutation)
+      const char* p = tile + r * kRowBytes + unit * 32 + (c & 3) * 8;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(p + 4 * kRowBytes));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      const int row = first + c;
+      return *reinterpret_cast<const s16x8*>(tile + row * kRowBytes + (((ks * 4 + q) ^ swizzle(row)) << 4));
+    }
+  }
+};
+
+// Which tile a workgroup computes.  Workgroups go round-robin over the 8 XCDs, each with an L2 of its
+// own: XCD x takes the x-th eighth of the tiles, in bands of kBand tile rows walked column by column,
+// so that the tiles in flight on one XCD share few rows of A and of B.
+constexpr int kXcds = 8, kBand = 4;
+
+__device__ inline void tile_of(uint32_t id, uint32_t tiles_i, uint32_t tiles_j, int* ti, int* tj) {
+  const uint32_t tiles = tiles_i * tiles_j;
+  const uint32_t per = tiles / kXcds, more = tiles % kXcds;
+  const uint32_t x = id % kXcds, at = id / kXcds;
+  const uint32_t t = x * per + min(x, more) + at;
+  const uint32_t band = t / (kBand * tiles_j), in = t % (kBand * tiles_j);
+  const uint32_t rows = min(static_cast<uint32_t>(kBand), tiles_i - band * kBand);
+  *ti = band * kBand + in % rows;
+  *tj = in / rows;
+}
+
+template <int TYPE> struct Pack8 { using V = typename Elem<TYPE>::V; };
+
+// eight consecutive elements at p (which of them are inside: n; vec: 16-byte aligned and whole)
+template <int TYPE>
+__device__ inline void load8(const void* p, bool vec, int n, float* v) {
+  using T = typename Elem<TYPE>::T;
+  using V = typename Elem<TYPE>::V;
+  if (vec) {
+    const V x = *static_cast<const V*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = float(x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < n ? float(static_cast<const T*>(p)[e]) : 0.0f;
+  }
+}
+
+template <int TYPE>
+__device__ inline void store8(void* p, bool vec, int n, const float* v) {
+  using T = typename Elem<TYPE>::T;
+  using V = typename Elem<TYPE>::V;
+  if (vec) {
+    V x;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = T(v[e]);
+    *static_cast<V*>(p) = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) static_cast<T*>(p)[e] = T(v[e]);
+  }
+}
+
+// Eight sums of a row become results.
+template <int TYPE, int KIND, bool JOINED = false>
+__device__ inline void finish8(const DenseGemm& g, int part, int split, int64_t i, int j, float* s0, float* s1) {
+  using T = typename Elem<TYPE>::T;
+  const int n = min(8, g.nj - j);
+  const bool vec = g.vec && n == 8;
+  if (!JOINED && g.splits > 1) {
+    constexpr int kMats = KIND == kGated ? 2 : 1;
+    for (int mat = 0; mat < kMats; ++mat) {
+      float* p = g.partial + ((int64_t(kMats == 2 ? mat : part) * g.splits + split) * g.ni + i) * g.nj + j;
+      const float* s = mat ? s1 : s0;
+      if (n == 8 && g.nj % 4 == 0) {
+        reinterpret_cast<f32x4*>(p)[0] = f32x4{s[0], s[1], s[2], s[3]};
+        reinterpret_cast<f32x4*>(p)[1] = f32x4{s[4], s[5], s[6], s[7]};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < n) p[e] = s[e];
+      }
+    }
+    return;
+  }
+  if constexpr (KIND == kForward || KIND == kGated) {
+    float b[8];
+    if (g.bias[0]) {
+      load8<TYPE>(static_cast<const T*>(g.bias[0]) + j, vec, n, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s0[e] += b[e];
+    }
+    if (g.z[0]) store8<TYPE>(static_cast<T*>(g.z[0]) + i * g.ldz[0] + j, vec, n, s0);
+    act8(s0, g.act);
+    if constexpr (KIND == kGated) {
+      if (g.bias[1]) {
+        load8<TYPE>(static_cast<const T*>(g.bias[1]) + j, vec, n, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s1[e] += b[e];
+      }
+      if (g.z[1]) store8<TYPE>(static_cast<T*>(g.z[1]) + i * g.ldz[1] + j, vec, n, s1);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s0[e] *= s1[e];
+    } else if (g.res) {
+      load8<TYPE>(static_cast<const T*>(g.res) + i * g.ldr + j, vec, n, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s0[e] += b[e];
+    }
+    store8<TYPE>(static_cast<T*>(g.c[0]) + i * g.ldc[0] + j, vec, n, s0);
+  } else {
+    store8<TYPE>(static_cast<T*>(g.c[part]) + i * g.ldc[part] + j, vec, n, s0);
+  }
+}
+
+template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU, bool ALIGNED>
+__global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile16(DenseGemm g) {
+  constexpr bool kGate = KIND == kGated;
+  constexpr bool kRmA = KIND == kWeightGrad, kRmB = KIND == kWeightGrad || KIND == kInputGrad;
+  constexpr int kWaves = WI * WJ;
+  constexpr bool kTurns = kWaves == 8;                     // see the main loop
+  constexpr int kSlotsA = kTurns ? 3 : 2, kSlotsB = 2;     // tiles of steps in LDS
+  constexpr int kCols = kGate ? BN / 2 : BN;               // result columns of a tile
+  constexpr int kWI = BM / WI, kWJ = kCols / WJ;           // results of a wavefront
+  constexpr int kFI = kWI / 16, kFJ = BN / WJ / 16;        // its fragments
+  using TileA = Tile<BM, kRmA, kWaves>;
+  using TileB = Tile<BN, kRmB, kWaves>;
+  using TileH = Tile<kCols, kRmB, kWaves>;                // one projection's half of B
+  constexpr int kStages = kSlotsA * TileA::kBytes + kSlotsB * TileB::kBytes;
+  constexpr int kLds = kStages > kWaves * 16384 ? kStages : kWaves * 16384;   // (16 KB: epilogue)
+  __shared__ __align__(1024) char lds[kLds];
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int ti, tj;
+  tile_of(blockIdx.x, (g.ni + BM - 1) / BM, (g.nj + kCols - 1) / kCols, &ti, &tj);
+  const int i0 = ti * BM, j0 = tj * kCols;
+  const int split = blockIdx.y, wpart = KIND == kWeightGrad ? blockIdx.z : 0;
+  const int per_part = (g.nr + kBK - 1) / kBK;
+  const int steps = per_part * (KIND == kInputGrad ? g.parts : 1);
+  const int begin = static_cast<int>(int64_t(steps) * split / g.splits);
+  const int end = static_cast<int>(int64_t(steps) * (split + 1) / g.splits);
+
+  TileA ta;
+  ta.init(wave, lane, g.lda, g.ni - i0);
+  // kGated: two halves with the rows of each projection; kInputGrad: strides may differ by part
+  TileB tb;
+  TileH th[2];
+  if constexpr (kGate) {
+    th[0].init(wave, lane, g.ldb[0], g.nj - j0);
+    th[1].init(wave, lane, g.ldb[1], g.nj - j0);
+  } else {
+    tb.init(wave, lane, g.ldb[0], g.nj - j0);
+  }
+  int tb_part = 0;
+
+  const uint32_t lds0 = lds_address(lds);
+  constexpr int kIssues = TileA::kLoads + TileB::kLoads;
+  // LDS: kSlotsA tiles of A, then kSlotsB tiles of B.  set_a, set_b: the step that issue_a, issue_b load
+  // next and where to; steps past the last are loaded too, as zeros, so that the count of loads under
+  // way is always the same.
+  constexpr int kAreaB = kSlotsA * TileA::kBytes;
+  struct Next { i32x4 a, b0, b1; int valid_a, valid_b; uint32_t at_a, at_b; } next;
+  auto set_a = [&](int step, int slot) {
+    const int part = KIND == kInputGrad && step >= per_part && g.parts > 1 ? 1 : 0;
+    const int r0 = (step - part * per_part) * kBK;
+    next.valid_a = step < end ? g.nr - r0 : 0;
+    const char* a = static_cast<const char*>(g.a[KIND == kWeightGrad ? wpart : part]);
+    next.a = descriptor(a + (kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0) * 2);
+    next.at_a = lds0 + slot * TileA::kBytes;
+  };
+  auto set_b = [&](int step, int slot) {
+    const int part = KIND == kInputGrad && step >= per_part && g.parts > 1 ? 1 : 0;
+    const int r0 = (step - part * per_part) * kBK;
+    next.valid_b = step < end ? g.nr - r0 : 0;
+    const char* b = static_cast<const char*>(g.b[part]);
+    next.b0 = descriptor(b + (kRmB ? int64_t(r0) * g.ldb[part] + j0 : int64_t(j0) * g.ldb[part] + r0) * 2);
+    if constexpr (kGate) next.b1 = descriptor(static_cast<const char*>(g.b[1]) + (int64_t(j0) * g.ldb[1] + r0) * 2);
+    if constexpr (KIND == kInputGrad) {
+      if (part != tb_part) {
+        tb.init(wave, lane, g.ldb[part], g.nj - j0);
+        tb_part = part;
+      }
+    }
+    next.at_b = lds0 + kAreaB + slot * TileB::kBytes;
+  };
+  auto issue_a = [&](int n) { ta.load(next.a, next.at_a, wave, lane, next.valid_a, n); };
+  auto issue_b = [&](int n) {
+    if constexpr (kGate) {
+      if (n < TileH::kLoads) th[0].load(next.b0, next.at_b, wave, lane, next.valid_b, n);
+      else th[1].load(next.b1, next.at_b + TileH::kBytes, wave, lane, next.valid_b, n - TileH::kLoads);
+    } else {
+      tb.load(next.b0, next.at_b, wave, lane, next.valid_b, n);
+    }
+  };
+  auto issue = [&](int n) {   // B first: stage_done<kLoads of A> leaves A's under way
+    if (n < TileB::kLoads) issue_b(n);
+    else issue_a(n - TileB::kLoads);
+  };
+
+  const int wi = (wave / WJ) * kWI, wj = (wave % WJ) * kWJ;
+  f32x4 acc[kFI][kFJ] = {};
+  auto fragments_a = [&](const char* sa, int ks, s16x8* f) {
+#pragma unroll
+    for (int n = 0; n < kFI; ++n) f[n] = TileA::fragment(sa, wi + n * 16, ks, lane);
+  };
+  auto fragments_b = [&](const char* sb, int ks, s16x8* f) {
+#pragma unroll
+    for (int n = 0; n < kFJ; ++n) {
+      if constexpr (kGate)
+        f[n] = TileH::fragment(sb + (n >= kFJ / 2) * TileH::kBytes, wj + (n % (kFJ / 2)) * 16, ks, lane);
+      else
+        f[n] = TileB::fragment(sb, wj + n * 16, ks, lane);
+    }
+  };
+  int at_a = 0, at_b = 0;   // slots of the step that is multiplied
+  if constexpr (!ALIGNED) {
+    using T = typename Elem<TYPE>::T;
+    static_assert(!kTurns);
+    s16x8 held[kIssues];
+    auto fetch = [&](int step) {
+      const int part = KIND == kInputGrad && step >= per_part && g.parts > 1 ? 1 : 0;
+      const int r0 = (step - part * per_part) * kBK, valid = g.nr - r0;
+      const T* a = static_cast<const T*>(g.a[KIND == kWeightGrad ? wpart : part]);
+      a += kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0;
+      const T* b = static_cast<const T*>(g.b[part]);
+      b += kRmB ? int64_t(r0) * g.ldb[part] + j0 : int64_t(j0) * g.ldb[part] + r0;
+#pragma unroll
+      for (int n = 0; n < TileA::kLoads; ++n) held[n] = TileA::fetch(a, g.lda, g.ni - i0, valid, wave, lane, n);
+      if constexpr (kGate) {
+        const T* b1 = static_cast<const T*>(g.b[1]) + int64_t(j0) * g.ldb[1] + r0;
+#pragma unroll
+        for (int n = 0; n < TileH::kLoads; ++n) {
+          held[TileA::kLoads + n] = TileH::fetch(b, g.ldb[0], g.nj - j0, valid, wave, lane, n);
+          held[TileA::kLoads + TileH::kLoads + n] = TileH::fetch(b1, g.ldb[1], g.nj - j0, valid, wave, lane, n);
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < TileB::kLoads; ++n)
+          held[TileA::kLoads + n] = TileB::fetch(b, g.ldb[part], g.nj - j0, valid, wave, lane, n);
+      }
+    };
+    auto put = [&](int slot) {
+      char* sa = lds + slot * TileA::kBytes;
+      char* sb = lds + kAreaB + slot * TileB::kBytes;
+#pragma unroll
+      for (int n = 0; n < TileA::kLoads; ++n) TileA::put(sa, held[n], wave, lane, n);
+#pragma unroll
+      for (int n = 0; n < TileB::kLoads; ++n) {
+        if constexpr (kGate)
+          TileH::put(sb + (n >= TileH::kLoads) * TileH::kBytes, held[TileA::kLoads + n], wave, lane, n % TileH::kLoads);
+        else
+          TileB::put(sb, held[TileA::kLoads + n], wave, lane, n);
+      }
+    };
+    if (begin < end) {
+      fetch(begin);
+      put(0);
+    }
+    for (int step = begin; step < end; ++step) {
+      stage_done<0>();
+      if (step + 1 < end) fetch(step + 1);
+      const char* sa = lds + at_a * TileA::kBytes;
+      const char* sb = lds + kAreaB + at_a * TileB::kBytes;
+#pragma unroll
+      for (int ks = 0; ks < kBK / 32; ++ks) {
+        s16x8 fa[kFI], fb[kFJ];
+        fragments_b(sb, ks, fb);
+        fragments_a(sa, ks, fa);
+#pragma unroll
+        for (int fi = 0; fi < kFI; ++fi)
+#pragma unroll
+          for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[fj], fa[fi], acc[fi][fj]);
+      }
+      at_a ^= 1;
+      if (step + 1 < end) put(at_a);
+    }
+  } else if constexpr (!kTurns) {
+    // Two workgroups a CU: one reads while the other multiplies.
+    set_a(begin, 0);
+    set_b(begin, 0);
+#pragma unroll
+    for (int n = 0; n < kIssues; ++n) issue(n);
+    for (int step = begin; step < end; ++step) {
+      stage_done<0>();
+      const char* sa = lds + at_a * TileA::kBytes;
+      const char* sb = lds + kAreaB + at_a * TileB::kBytes;
+      at_a ^= 1;
+      set_a(step + 1, at_a);
+      set_b(step + 1, at_a);
+#pragma unroll
+      for (int n = 0; n < kIssues; ++n) issue(n);
+#pragma unroll
+      for (int ks = 0; ks < kBK / 32; ++ks) {
+        s16x8 fa[kFI], fb[kFJ];
+        fragments_b(sb, ks, fb);
+        fragments_a(sa, ks, fa);
+#pragma unroll
+        for (int fi = 0; fi < kFI; ++fi)
+#pragma unroll
+          for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[fj], fa[fi], acc[fi][fj]);
+      }
+    }
+  } else {
+    // The two wavefronts of a SIMD take turns: while one multiplies a step, the other reads its fragments of a
+    // step into registers (wavefronts 0-3 are one to a SIMD, and so are 4-7, which run a turn behind).  B has two
+    // slots, A three: a step of A, whose rows come from memory, is asked for four turns before it is read, one of
+    // B, which other tiles share in L2, two.  A slot is loaded again after the turn in which the late wavefronts
+    // have read it.
+    constexpr int kUnderWay = TileA::kLoads;
+    const bool late = wave >= 4;
+    s16x8 fa[kBK / 32][kFI], fb[kBK / 32][kFJ];
+    auto read = [&]() {
+      const char* sa = lds + at_a * TileA::kBytes;
+      const char* sb = lds + kAreaB + at_b * TileB::kBytes;
+#pragma unroll
+      for (int ks = 0; ks < kBK / 32; ++ks) {
+        fragments_b(sb, ks, fb[ks]);
+        fragments_a(sa, ks, fa[ks]);
+      }
+    };
+    auto after = [](int slot) { return slot == 2 ? 0 : slot + 1; };
+    set_a(begin, 0);
+    set_b(begin, 0);
+#pragma unroll
+    for (int n = 0; n < kIssues; ++n) issue(n);
+    set_a(begin + 1, 1);
+#pragma unroll
+    for (int n = 0; n < TileA::kLoads; ++n) issue_a(n);
+    stage_done<kUnderWay>();
+    if (!late) {
+      for (int step = begin; step < end; ++step) {
+        read();
+        set_b(step + 1, at_b ^ 1);
+        set_a(step + 2, after(after(at_a)));
+        at_b ^= 1;
+        at_a = after(at_a);
+#pragma unroll
+        for (int n = 0; n < kIssues; ++n) issue(n);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int ks = 0; ks < kBK / 32; ++ks)
+#pragma unroll
+          for (int fi = 0; fi < kFI; ++fi)
+#pragma unroll
+            for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[ks][fj], fa[ks][fi], acc[fi][fj]);
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        stage_done<kUnderWay>();
+      }
+      asm volatile("s_barrier" ::: "memory");
+    } else {
+      set_b(begin + 1, 1);
+      set_a(begin + 2, 2);
+#pragma unroll
+      for (int n = 0; n < kIssues; ++n) issue(n);
+      asm volatile("s_barrier" ::: "memory");
+      for (int step = begin; step < end; ++step) {
+        read();
+        set_b(step + 2, at_b);
+        set_a(step + 3, at_a);
+        at_b ^= 1;
+        at_a = after(at_a);
+        __builtin_amdgcn_sched_barrier(0);
+        stage_done<kUnderWay>();
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int ks = 0; ks < kBK / 32; ++ks)
+#pragma unroll
+          for (int fi = 0; fi < kFI; ++fi) {
+#pragma unroll
+            for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[ks][fj], fa[ks][fi], acc[fi][fj]);
+            if (ks * kFI + fi < kIssues) issue(ks * kFI + fi);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+      }
+    }
+  }
+
+  // Results through LDS, 64 x 64 sums of a wavefront at a time, so that a lane has eight consecutive
+  // columns and the activation's code is there once: lane (q, c) has rows c and columns 4 q .. + 3 of
+  // each fragment.  Rows of 256 bytes, their 16-byte chunks permuted by the row.
+  stage_done<0>();
+  char* own = lds + wave * 16384;
+  const int q = lane >> 4, c = lane & 15;
+#pragma unroll
+  for (int h = 0; h < (kFI / 4) * (kFJ / 4); ++h) {
+    const int hi = h / (kFJ / 4), hj = h % (kFJ / 4);
+#pragma unroll
+    for (int fi = 0; fi < 4; ++fi)
+#pragma unroll
+      for (int fj = 0; fj < 4; ++fj) {
+        // kGated: two fragments of the gate, two of the up projection
+        const int f = kGate ? (fj / 2) * (kFJ / 2) + hj * 2 + fj % 2 : hj * 4 + fj;
+        *reinterpret_cast<f32x4*>(own + (fi * 16 + c) * 256 + (((fj * 4 + q) ^ c) << 4)) = acc[hi * 4 + fi][f];
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int kLanes = kGate ? 4 : 8;      // of a row
+#pragma unroll 1
+    for (int row0 = 0; row0 < 64; row0 += 64 / kLanes) {
+      const int row = row0 + lane / kLanes, e = (lane % kLanes) * 2;   // e: the row's first chunk
+      const int64_t i = i0 + wi + hi * 64 + row;
+      const int j = j0 + wj + hj * (kGate ? 32 : 64) + e * 4;
+      float s0[8], s1[8];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(own + row * 256 + (((e + x) ^ (row & 15)) << 4));
+        s0[4 * x] = v[0], s0[4 * x + 1] = v[1], s0[4 * x + 2] = v[2], s0[4 * x + 3] = v[3];
+        if constexpr (kGate) {
+          const f32x4 w = *reinterpret_cast<const f32x4*>(own + row * 256 + (((8 + e + x) ^ (row & 15)) << 4));
+          s1[4 * x] = w[0], s1[4 * x + 1] = w[1], s1[4 * x + 2] = w[2], s1[4 * x + 3] = w[3];
+        }
+      }
+      if (i < g.ni && j < g.nj) finish8<TYPE, KIND>(g, wpart, split, i, j, s0, s1);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
+// Results of a product whose reduction was split: the splits' sums are added in order.  A thread has eight columns.
+template <int TYPE, int KIND>
+__global__ __launch_bounds__(256) void dense_join(DenseGemm g) {
+  const int groups = (g.nj + 7) / 8;
+  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  if (at >= int64_t(groups) * g.ni) return;
+  const int64_t i = at / groups;
+  const int j = static_cast<int>(at % groups) * 8, n = min(8, g.nj - j), part = blockIdx.y;
+  const int64_t slice = int64_t(g.ni) * g.nj;
+  float s[2][8];
+#pragma unroll
+  for (int mat = 0; mat < (KIND == kGated ? 2 : 1); ++mat) {
+    const float* p = g.partial + int64_t(KIND == kGated ? mat : part) * g.splits * slice + i * g.nj + j;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[mat][e] = 0.0f;
+    for (int split = 0; split < g.splits; ++split, p += slice) {
+      if (n == 8 && g.nj % 4 == 0) {
+        const f32x4 lo = reinterpret_cast<const f32x4*>(p)[0], hi = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[mat][e] += lo[e], s[mat][4 + e] += hi[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < n) s[mat][e] += p[e];
+      }
+    }
+  }
+  finish8<TYPE, KIND, true>(g, part, 0, i, j, s[0], s[1]);
 }
 
 // ---------------------------------------------------------------- elementwise parts of the gradients
@@ -198,18 +799,58 @@ __global__ __launch_bounds__(256) void dense_colsum(const float* partial, int32_
   static_cast<T*>(out)[j] = T(sum);
 }
 
+template <int TYPE, int KIND>
+int simple_launch(const DenseGemm& g, hipStream_t stream) {
+  const int cols = KIND == kGated ? kSN / 2 : kSN;
+  const int64_t tiles = int64_t((g.ni + kSM - 1) / kSM) * ((g.nj + cols - 1) / cols);
+  const dim3 grid(static_cast<uint32_t>(tiles), 1, KIND == kWeightGrad ? g.parts : 1);
+  dense_tile<TYPE, KIND><<<grid, 256, 0, stream>>>(g);
+  return hipGetLastError();
+}
+
+template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU, bool ALIGNED>
+int tile16_launch(const DenseGemm& g, hipStream_t stream) {
+  const int cols = KIND == kGated ? BN / 2 : BN;
+  const int64_t tiles = int64_t((g.ni + BM - 1) / BM) * ((g.nj + cols - 1) / cols);
+  const dim3 grid(static_cast<uint32_t>(tiles), g.splits, KIND == kWeightGrad ? g.parts : 1);
+  dense_tile16<TYPE, KIND, BM, BN, WI, WJ, PER_CU, ALIGNED><<<grid, 64 * WI * WJ, 0, stream>>>(g);
+  return hipGetLastError();
+}
+
+template <int TYPE, int KIND>
+int join_launch(const DenseGemm& g, hipStream_t stream) {
+  const int64_t threads = int64_t((g.nj + 7) / 8) * g.ni;
+  const dim3 grid(static_cast<uint32_t>((threads + 255) / 256), KIND == kWeightGrad ? g.parts : 1);
+  dense_join<TYPE, KIND><<<grid, 256, 0, stream>>>(g);
+  return hipGetLastError();
+}
+
+template <int TYPE, int KIND>
+int kind_launch(const DenseGemm& g, hipStream_t stream) {
+  if constexpr (TYPE != kDenseF32) {
+    if (g.variant == kTile256) return tile16_launch<TYPE, KIND, 256, 256, 2, 4, 1, true>(g, stream);
+    if (g.aligned) return tile16_launch<TYPE, KIND, 128, 128, 2, 2, 2, true>(g, stream);
+    return tile16_launch<TYPE, KIND, 128, 128, 2, 2, 2, false>(g, stream);
+  }
+  return simple_launch<TYPE, KIND>(g, stream);
+}
+
+template <int TYPE, int KIND>
+int product_launch(const DenseGemm& g, hipStream_t stream) {
+  const int rc = kind_launch<TYPE, KIND>(g, stream);
+  if (rc != 0 || g.splits == 1) return rc;
+  if constexpr (TYPE != kDenseF32) return join_launch<TYPE, KIND>(g, stream);
+  return rc;
+}
+
 template <int TYPE>
 int gemm_launch(int kind, const DenseGemm& g, hipStream_t stream) {
-  const int cols = kind == kGated ? kBN / 2 : kBN;
-  const int64_t tiles = int64_t((g.ni + kBM - 1) / kBM) * ((g.nj + cols - 1) / cols);
-  const dim3 grid(static_cast<uint32_t>(tiles), 1, kind == kWeightGrad ? g.parts : 1);
   switch (kind) {
-    case kForward: dense_tile<TYPE, kForward><<<grid, 256, 0, stream>>>(g); break;
-    case kGated: dense_tile<TYPE, kGated><<<grid, 256, 0, stream>>>(g); break;
-    case kInputGrad: dense_tile<TYPE, kInputGrad><<<grid, 256, 0, stream>>>(g); break;
-    default: dense_tile<TYPE, kWeightGrad><<<grid, 256, 0, stream>>>(g); break;
+    case kForward: return product_launch<TYPE, kForward>(g, stream);
+    case kGated: return product_launch<TYPE, kGated>(g, stream);
+    case kInputGrad: return product_launch<TYPE, kInputGrad>(g, stream);
+    default: return product_launch<TYPE, kWeightGrad>(g, stream);
   }
-  return hipGetLastError();
 }
 
 template <int TYPE>

@@ -18,6 +18,8 @@ enum DenseKind {
   kWeightGrad = 3    // C[i][j] = sum_r A[r][i] B[r][j]   A = dz, B = x       (R, R)
 };
 
+enum DenseVariant { kSimple = 0, kTile128 = 1, kTile256 = 2 };
+
 // One matrix product.  Arrays of two: kGated's two weights and results; kInputGrad's two
 // products summed into one result (parts = 2); kWeightGrad's two results (parts = 2).
 struct DenseGemm {
@@ -31,6 +33,9 @@ struct DenseGemm {
   int64_t lda, ldb[2], ldc[2], ldz[2], ldr;
   int32_t ni, nj, nr;      // C is [ni][nj], the sum over nr (in each part)
   int32_t parts, splits, act;
+  int32_t variant;         // DenseVariant
+  int32_t aligned;         // operands' rows start at multiples of 16 bytes and hold whole chunks
+  int32_t vec;             // results, residual and bias may be read and written 16 bytes at a time
 };
 
 // dz = dy * act'(z), or dg, du; and partial column sums of them

@@ -2,6 +2,7 @@
 // launches.  See include/embx_dense.h for the contract.
 #include <algorithm>
 #include <cstdint>
+#include <cmath>
 
 #include "../../include/embx_dense.h"
 #include "dense.hpp"
@@ -57,7 +58,99 @@ emb_status_t check_workspace(const void* ws, size_t have, size_t need) {
 
 emb_status_t run(int rc) { return rc == 0 ? EMB_OK : EMB_ERR_DEVICE; }
 
-emb_status_t gemm(int32_t dtype, int kind, const DenseGemm& g, void* stream) {
+// (a tile's offsets, 256 rows at most, are 32-bit)
+bool whole(const void* p, int64_t ld) { return !misaligned(p, 16) && ld % 8 == 0 && ld <= (int64_t(1) << 22); }
+
+// Whether rows of every operand and result start at multiples of 16 bytes and hold whole chunks of
+// eight elements (16-bit types).
+bool aligned16(int kind, const DenseGemm& g) {
+  const int parts = g.parts;
+  bool ok = g.nj % 8 == 0;
+  for (int p = 0; p < (kind == kGated ? 1 : parts); ++p) ok = ok && whole(g.a[p], g.lda);
+  for (int p = 0; p < (kind == kGated ? 2 : parts); ++p) ok = ok && whole(g.b[p], g.ldb[p]);
+  // along the reduction: whole chunks of it; reduction-major: whole chunks of results
+  if (kind != kWeightGrad) ok = ok && g.nr % 8 == 0;
+  if (kind == kWeightGrad) ok = ok && g.ni % 8 == 0;
+  return ok;
+}
+
+bool aligned_results(int kind, const DenseGemm& g) {
+  bool ok = g.nj % 8 == 0;
+  for (int p = 0; p < (kind == kWeightGrad ? g.parts : 1); ++p) ok = ok && whole(g.c[p], g.ldc[p]);
+  for (int p = 0; p < 2; ++p) {
+    if (g.z[p]) ok = ok && whole(g.z[p], g.ldz[p]);
+    if (g.bias[p]) ok = ok && !misaligned(g.bias[p], 16);
+  }
+  if (g.res) ok = ok && whole(g.res, g.ldr);
+  return ok;
+}
+
+// Which tile a product takes and over how many workgroups its reduction is split.
+struct Choice { int32_t variant, splits; };
+
+constexpr int kCus = 256;
+constexpr int kStep = 64;   // of the reduction
+
+// Microseconds of a product by tiles of 256 x 256 or 128 x 128 over `steps` steps, split s ways.  Measured on bf16
+// products of 256 to 8192 rows: a step of the large tile takes 0.97 us on a GPU that is otherwise idle and 1.50 us
+// with a workgroup on every CU (the clock drops, and L2 is shared); one of the small tile 0.62 us alone on its CU, 1.03
+// us where two share it.  A round starts and ends in 3 us.  Split products write their sums and read them back.
+double tile_us(int variant, double tiles, int steps, int s, double result_bytes) {
+  const double groups = tiles * s, each = (steps + s - 1) / s;
+  double us;
+  if (variant == kTile256) {
+    const double rounds = std::ceil(groups / kCus);
+    us = rounds * (each * (0.97 + 0.53 * std::min(1.0, groups / kCus)) + 3.0);
+  } else {
+    const double whole = std::floor(groups / (2 * kCus)), rest = groups - whole * 2 * kCus;
+    us = whole * (each * 1.03 + 3.0);
+    if (rest > 0) us += each * (rest <= kCus ? 0.62 + 0.1 * rest / kCus : 1.03) + 3.0;
+  }
+  if (s > 1) us += 3.0 + result_bytes * s / 2.0e6;
+  return us;
+}
+
+Choice choose(int kind, int64_t ni, int64_t nj, int64_t nr, int parts, bool large_tiles) {
+  const int64_t steps = (nr + kStep - 1) / kStep * (kind == kInputGrad ? parts : 1);
+  const int results = kind == kWeightGrad ? parts : kind == kGated ? 2 : 1;
+  const double result_bytes = 4.0 * ni * nj * results;
+  Choice best = {kTile128, 1};
+  double least = 0.0;
+  for (int variant = kTile256; variant >= kTile128; --variant) {
+    if (variant == kTile256 && !large_tiles) continue;
+    const int64_t side = variant == kTile256 ? 256 : 128;
+    const double tiles = double((ni + side - 1) / side) * ((nj * (kind == kGated ? 2 : 1) + side - 1) / side) *
+                         (kind == kWeightGrad ? parts : 1);
+    for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= (256 << 20))); ++s) {
+      const double us = tile_us(variant, tiles, static_cast<int>(std::min<int64_t>(steps, 1 << 30)), s, result_bytes);
+      if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, s};
+    }
+  }
+  return best;
+}
+
+// Bytes of partial sums of a product, whatever its operands' alignment.
+size_t partial_bytes(int32_t dtype, int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
+  if (dtype == EMB_DTYPE_F32) return 0;
+  const int results = kind == kWeightGrad ? parts : kind == kGated ? 2 : 1;
+  size_t most = 0;
+  for (bool large : {false, true}) {
+    const int s = choose(kind, ni, nj, nr, parts, large).splits;
+    if (s > 1) most = std::max(most, size_t(s) * ni * nj * results * 4);
+  }
+  return most;
+}
+
+emb_status_t gemm(int32_t dtype, int kind, const DenseGemm& given, float* partial, void* stream) {
+  DenseGemm g = given;
+  g.splits = 1;
+  g.partial = partial;
+  if (dtype != EMB_DTYPE_F32) {
+    g.aligned = aligned16(kind, g);
+    g.vec = aligned_results(kind, g);
+    const Choice c = choose(kind, g.ni, g.nj, g.nr, g.parts, g.aligned);
+    g.variant = c.variant, g.splits = c.splits;
+  }
   switch (dtype) {
     case EMB_DTYPE_F32: return run(dense_gemm_f32(kind, g, stream));
     case EMB_DTYPE_F16: return run(dense_gemm_f16(kind, g, stream));
@@ -99,6 +192,7 @@ int32_t slope_blocks(int64_t m) { return static_cast<int32_t>(std::max<int64_t>(
 struct GradSpace {
   void* dz[2] = {nullptr, nullptr};
   float* colsum[2] = {nullptr, nullptr};
+  float* partial = nullptr;   // of one product after the other
   int64_t lddz = 0;
   int32_t blocks = 1;
 };
@@ -117,12 +211,19 @@ GradSpace grad_space(Arena& ar, int64_t m, int64_t n, int32_t dtype, int mats, b
 
 GradSpace linear_grad_space(Arena& ar, const emb_linear_grad_t& a) {
   const bool sums[2] = {a.dbias != nullptr, false};
-  return grad_space(ar, a.m, a.n, a.dtype, 1, a.activation != EMB_ACT_NONE && (a.dx || a.dweight), sums);
+  GradSpace g = grad_space(ar, a.m, a.n, a.dtype, 1, a.activation != EMB_ACT_NONE && (a.dx || a.dweight), sums);
+  g.partial = ar.take<float>(std::max(a.dx ? partial_bytes(a.dtype, kInputGrad, a.m, a.k, a.n, 1) : 0,
+                                      a.dweight ? partial_bytes(a.dtype, kWeightGrad, a.n, a.k, a.m, 1) : 0));
+  return g;
 }
 
 GradSpace gated_grad_space(Arena& ar, const emb_gated_grad_t& a) {
   const bool sums[2] = {a.db_gate != nullptr, a.db_up != nullptr};
-  return grad_space(ar, a.m, a.n, a.dtype, 2, a.dx || a.dw_gate || a.dw_up, sums);
+  GradSpace g = grad_space(ar, a.m, a.n, a.dtype, 2, a.dx || a.dw_gate || a.dw_up, sums);
+  const int weights = (a.dw_gate != nullptr) + (a.dw_up != nullptr);
+  g.partial = ar.take<float>(std::max(a.dx ? partial_bytes(a.dtype, kInputGrad, a.m, a.k, a.n, 2) : 0,
+                                      weights ? partial_bytes(a.dtype, kWeightGrad, a.n, a.k, a.m, weights) : 0));
+  return g;
 }
 
 }  // namespace
@@ -132,7 +233,7 @@ extern "C" {
 emb_status_t emb_linear_workspace(const emb_linear_t* a, size_t* bytes) {
   if (!a || !bytes) return EMB_ERR_INVALID_ARGUMENT;
   EMBX_TRY(check_shape(a->m, a->n, a->k, a->dtype, a->activation));
-  *bytes = 0;
+  *bytes = partial_bytes(a->dtype, kForward, a->m, a->n, a->k, 1);
   return EMB_OK;
 }
 
@@ -156,7 +257,7 @@ emb_status_t emb_linear(const emb_linear_t* a, void* workspace, size_t workspace
   g.res = a->residual, g.ldr = a->ldr;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
   g.parts = 1, g.splits = 1, g.act = a->activation;
-  return gemm(a->dtype, kForward, g, stream);
+  return gemm(a->dtype, kForward, g, static_cast<float*>(workspace), stream);
 }
 
 emb_status_t emb_linear_backward_workspace(const emb_linear_grad_t* a, size_t* bytes) {
@@ -200,13 +301,13 @@ emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, si
     g.b[0] = a->weight, g.ldb[0] = a->ldw;
     g.c[0] = a->dx, g.ldc[0] = a->lddx;
     g.ni = a->m, g.nj = a->k, g.nr = a->n;
-    EMBX_TRY(gemm(a->dtype, kInputGrad, g, stream));
+    EMBX_TRY(gemm(a->dtype, kInputGrad, g, sp.partial, stream));
   }
   if (a->dweight) {
     g.b[0] = a->x, g.ldb[0] = a->ldx;
     g.c[0] = a->dweight, g.ldc[0] = a->lddw;
     g.ni = a->n, g.nj = a->k, g.nr = a->m;
-    EMBX_TRY(gemm(a->dtype, kWeightGrad, g, stream));
+    EMBX_TRY(gemm(a->dtype, kWeightGrad, g, sp.partial, stream));
   }
   return EMB_OK;
 }
@@ -214,7 +315,7 @@ emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, si
 emb_status_t emb_gated_workspace(const emb_gated_t* a, size_t* bytes) {
   if (!a || !bytes) return EMB_ERR_INVALID_ARGUMENT;
   EMBX_TRY(check_shape(a->m, a->n, a->k, a->dtype, a->activation));
-  *bytes = 0;
+  *bytes = partial_bytes(a->dtype, kGated, a->m, a->n, a->k, 1);
   return EMB_OK;
 }
 
@@ -241,7 +342,7 @@ emb_status_t emb_gated(const emb_gated_t* a, void* workspace, size_t workspace_b
   g.bias[0] = a->b_gate, g.bias[1] = a->b_up;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
   g.parts = 1, g.splits = 1, g.act = a->activation;
-  return gemm(a->dtype, kGated, g, stream);
+  return gemm(a->dtype, kGated, g, static_cast<float*>(workspace), stream);
 }
 
 emb_status_t emb_gated_backward_workspace(const emb_gated_grad_t* a, size_t* bytes) {
@@ -295,7 +396,7 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
     g.b[1] = a->w_up, g.ldb[1] = a->ld_up;
     g.c[0] = a->dx, g.ldc[0] = a->lddx;
     g.ni = a->m, g.nj = a->k, g.nr = a->n, g.parts = 2;
-    EMBX_TRY(gemm(a->dtype, kInputGrad, g, stream));
+    EMBX_TRY(gemm(a->dtype, kInputGrad, g, sp.partial, stream));
   }
   if (weights) {
     g.parts = 0;
@@ -308,7 +409,7 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
     }
     g.b[0] = g.b[1] = a->x, g.ldb[0] = g.ldb[1] = a->ldx;
     g.ni = a->n, g.nj = a->k, g.nr = a->m;
-    EMBX_TRY(gemm(a->dtype, kWeightGrad, g, stream));
+    EMBX_TRY(gemm(a->dtype, kWeightGrad, g, sp.partial, stream));
   }
   return EMB_OK;
 }
