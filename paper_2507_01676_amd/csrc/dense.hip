@@ -22,37 +22,86 @@ template <> struct Elem<kDenseF32> { using T = float; };
 template <> struct Elem<kDenseF16> { using T = _Float16; using V = f16x8; };
 template <> struct Elem<kDenseBF16> { using T = __bf16; using V = bf16x8; };
 
-__device__ inline float sigmoid_f(float z) { return 1.0f / (1.0f + expf(-z)); }
-__device__ inline float phi_f(float z) { return 0.5f * (1.0f + erff(z * 0.70710678f)); }
+// Activations in 32 bits.  The 16-bit types take the hardware's exp2 and reciprocal (an ulp each; the product
+// with log2 e costs |z| / 2^24 more) and the normal distribution function by formula 7.1.26 of Abramowitz and
+// Stegun, Handbook of Mathematical Functions (off by less than 1e-7): all far below what their results are rounded
+// to.  f32 takes the library's.
+template <int TYPE>
+__device__ inline float exp_f(float z) {
+  if constexpr (TYPE == kDenseF32) return expf(z);
+  else return __builtin_amdgcn_exp2f(z * 1.44269504f);
+}
 
+template <int TYPE>
+__device__ inline float rcp_f(float z) {
+  if constexpr (TYPE == kDenseF32) return 1.0f / z;
+  else return __builtin_amdgcn_rcpf(z);
+}
+
+template <int TYPE>
+__device__ inline float sigmoid_f(float z) { return rcp_f<TYPE>(1.0f + exp_f<TYPE>(-z)); }
+
+// the normal distribution function, and exp(-z^2 / 2) on the way
+template <int TYPE>
+__device__ inline float phi_f(float z, float* bell) {
+  const float e = exp_f<TYPE>(-0.5f * z * z);
+  *bell = e;
+  if constexpr (TYPE == kDenseF32) {
+    return 0.5f * (1.0f + erff(z * 0.70710678f));
+  } else {
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f) * t;
+    const float tail = 0.5f * p * e;   // of |z|
+    return z < 0.0f ? tail : 1.0f - tail;
+  }
+}
+
+template <int TYPE>
 __device__ inline float act_f(float z, int act) {
+  float bell;
   switch (act) {
     case EMB_ACT_RELU: return z < 0.0f ? 0.0f : z;   // NaN passes
-    case EMB_ACT_SIGMOID: return sigmoid_f(z);
-    case EMB_ACT_SILU: return z * sigmoid_f(z);
-    case EMB_ACT_GELU: return z * phi_f(z);
+    case EMB_ACT_SIGMOID: return sigmoid_f<TYPE>(z);
+    case EMB_ACT_SILU: return z * sigmoid_f<TYPE>(z);
+    case EMB_ACT_GELU: return z * phi_f<TYPE>(z, &bell);
     default: return z;
   }
 }
 
-// The sigmoid's slope is s(z) s(-z), with both from exp(-|z|): 1 - s(z) would lose all its digits
-// where z is large.
-__device__ inline float slope_f(float z, int act) {
+// dy act'(z); *value = act(z).  The sigmoid's slope is s(z) s(-z), with both from exp(-|z|): 1 - s(z) would
+// lose all its digits where z is large.
+template <int TYPE>
+__device__ inline float slope_f(float dy, float z, int act, float* value) {
   switch (act) {
-    case EMB_ACT_RELU: return z <= 0.0f ? 0.0f : 1.0f;
+    case EMB_ACT_RELU:
+      *value = z < 0.0f ? 0.0f : z;
+      return z <= 0.0f ? 0.0f : dy;   // an infinite dy is not multiplied by 0
     case EMB_ACT_SIGMOID:
     case EMB_ACT_SILU: {
-      const float t = expf(-fabsf(z)), r = 1.0f / (1.0f + t), w = t * r;
+      const float t = exp_f<TYPE>(-fabsf(z)), r = rcp_f<TYPE>(1.0f + t), w = t * r;
       const float s = z >= 0.0f ? r : w, c = z >= 0.0f ? w : r;
-      return act == EMB_ACT_SIGMOID ? s * c : s * (1.0f + z * c);
+      *value = act == EMB_ACT_SIGMOID ? s : z * s;
+      return dy * (act == EMB_ACT_SIGMOID ? s * c : s * (1.0f + z * c));
     }
-    case EMB_ACT_GELU: return phi_f(z) + z * 0.39894228f * expf(-0.5f * z * z);
-    default: return 1.0f;
+    case EMB_ACT_GELU: {
+      float bell;
+      const float p = phi_f<TYPE>(z, &bell);
+      *value = z * p;
+      return dy * (p + z * 0.39894228f * bell);
+    }
+    default:
+      *value = z;
+      return dy;
   }
 }
 
-// the same of eight values: one branch
+// act of eight values: one branch
+template <int TYPE>
 __device__ inline void act8(float* z, int act) {
+  float bell;
   switch (act) {
     case EMB_ACT_RELU:
 #pragma unroll
@@ -60,15 +109,15 @@ __device__ inline void act8(float* z, int act) {
       break;
     case EMB_ACT_SIGMOID:
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = sigmoid_f(z[e]);
+      for (int e = 0; e < 8; ++e) z[e] = sigmoid_f<TYPE>(z[e]);
       break;
     case EMB_ACT_SILU:
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] *= sigmoid_f(z[e]);
+      for (int e = 0; e < 8; ++e) z[e] *= sigmoid_f<TYPE>(z[e]);
       break;
     case EMB_ACT_GELU:
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] *= phi_f(z[e]);
+      for (int e = 0; e < 8; ++e) z[e] *= phi_f<TYPE>(z[e], &bell);
       break;
     default: break;
   }
@@ -83,7 +132,7 @@ __device__ inline void finish(const DenseGemm& g, int part, int i, int j, float 
   if constexpr (KIND == kForward || KIND == kGated) {
     if (g.bias[0]) s0 += float(static_cast<const T*>(g.bias[0])[j]);
     if (g.z[0]) static_cast<T*>(g.z[0])[i * g.ldz[0] + j] = T(s0);
-    float y = act_f(s0, g.act);
+    float y = act_f<TYPE>(s0, g.act);
     if constexpr (KIND == kGated) {
       if (g.bias[1]) s1 += float(static_cast<const T*>(g.bias[1])[j]);
       if (g.z[1]) static_cast<T*>(g.z[1])[i * g.ldz[1] + j] = T(s1);
@@ -267,27 +316,6 @@ struct Tile {
     }
   }
 
-  // The same piece of a matrix whose rows start anywhere: elements of a chunk one by one where it is not
-  // whole, else all at once, at any alignment.
-  template <class T>
-  __device__ static s16x8 fetch(const T* base, int64_t ld, int rows, int valid, int wave, int lane, int n) {
-    const int row = load_row(n, wave, lane), at = load_chunk(row, lane) * 8;
-    const int count = (RM ? row < valid : row < rows) ? (RM ? rows : valid) - at : 0;
-    const T* p = base + row * ld + at;
-    s16x8 v = {};
-    if (count >= 8) {
-      __builtin_memcpy(&v, p, 16);
-    } else if (count > 0) {
-#pragma unroll
-      for (int e = 0; e < 7; ++e)
-        if (e < count) v[e] = __builtin_bit_cast(short, p[e]);
-    }
-    return v;
-  }
-  __device__ static void put(char* tile, s16x8 v, int wave, int lane, int n) {
-    *reinterpret_cast<s16x8*>(tile + (n * WAVES + wave) * 1024 + lane * 16) = v;
-  }
-
   // valid: how many of this step's kBK are inside
   __device__ void load(i32x4 rsrc, uint32_t lds, int wave, int lane, int valid, int n) const {
     int v = voff[n];
@@ -332,36 +360,34 @@ __device__ inline void tile_of(uint32_t id, uint32_t tiles_i, uint32_t tiles_j, 
   *tj = in / rows;
 }
 
-template <int TYPE> struct Pack8 { using V = typename Elem<TYPE>::V; };
-
-// eight consecutive elements at p (which of them are inside: n; vec: 16-byte aligned and whole)
+// Eight consecutive elements at p, of which n >= 1 are inside (the last one stands for the others); whole eights are read and written 16 bytes at a time at
+// any alignment.
 template <int TYPE>
-__device__ inline void load8(const void* p, bool vec, int n, float* v) {
+__device__ inline void load8(const void* p, int n, float* v) {
   using T = typename Elem<TYPE>::T;
-  using V = typename Elem<TYPE>::V;
-  if (vec) {
-    const V x = *static_cast<const V*>(p);
+  T x[8];
+  if (n == 8) {
+    __builtin_memcpy(x, p, sizeof(x));
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = float(x[e]);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < n ? float(static_cast<const T*>(p)[e]) : 0.0f;
+    for (int e = 0; e < 8; ++e) v[e] = float(static_cast<const T*>(p)[min(e, n - 1)]);
   }
 }
 
 template <int TYPE>
-__device__ inline void store8(void* p, bool vec, int n, const float* v) {
+__device__ inline void store8(void* p, int n, const float* v) {
   using T = typename Elem<TYPE>::T;
-  using V = typename Elem<TYPE>::V;
-  if (vec) {
-    V x;
+  T x[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = T(v[e]);
-    *static_cast<V*>(p) = x;
+  for (int e = 0; e < 8; ++e) x[e] = T(v[e]);
+  if (n == 8) {
+    __builtin_memcpy(p, x, sizeof(x));
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      if (e < n) static_cast<T*>(p)[e] = T(v[e]);
+      if (e < n) static_cast<T*>(p)[e] = x[e];
   }
 }
 
@@ -370,53 +396,47 @@ template <int TYPE, int KIND, bool JOINED = false>
 __device__ inline void finish8(const DenseGemm& g, int part, int split, int64_t i, int j, float* s0, float* s1) {
   using T = typename Elem<TYPE>::T;
   const int n = min(8, g.nj - j);
-  const bool vec = g.vec && n == 8;
   if (!JOINED && g.splits > 1) {
     constexpr int kMats = KIND == kGated ? 2 : 1;
     for (int mat = 0; mat < kMats; ++mat) {
-      float* p = g.partial + ((int64_t(kMats == 2 ? mat : part) * g.splits + split) * g.ni + i) * g.nj + j;
+      // rows of partial sums are padded to whole eights
+      float* p = g.partial + ((int64_t(kMats == 2 ? mat : part) * g.splits + split) * g.ni + i) * ((g.nj + 7) / 8 * 8) + j;
       const float* s = mat ? s1 : s0;
-      if (n == 8 && g.nj % 4 == 0) {
-        reinterpret_cast<f32x4*>(p)[0] = f32x4{s[0], s[1], s[2], s[3]};
-        reinterpret_cast<f32x4*>(p)[1] = f32x4{s[4], s[5], s[6], s[7]};
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < n) p[e] = s[e];
-      }
+      reinterpret_cast<f32x4*>(p)[0] = f32x4{s[0], s[1], s[2], s[3]};
+      reinterpret_cast<f32x4*>(p)[1] = f32x4{s[4], s[5], s[6], s[7]};
     }
     return;
   }
   if constexpr (KIND == kForward || KIND == kGated) {
     float b[8];
     if (g.bias[0]) {
-      load8<TYPE>(static_cast<const T*>(g.bias[0]) + j, vec, n, b);
+      load8<TYPE>(static_cast<const T*>(g.bias[0]) + j, n, b);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s0[e] += b[e];
     }
-    if (g.z[0]) store8<TYPE>(static_cast<T*>(g.z[0]) + i * g.ldz[0] + j, vec, n, s0);
-    act8(s0, g.act);
+    if (g.z[0]) store8<TYPE>(static_cast<T*>(g.z[0]) + i * g.ldz[0] + j, n, s0);
+    act8<TYPE>(s0, g.act);
     if constexpr (KIND == kGated) {
       if (g.bias[1]) {
-        load8<TYPE>(static_cast<const T*>(g.bias[1]) + j, vec, n, b);
+        load8<TYPE>(static_cast<const T*>(g.bias[1]) + j, n, b);
 #pragma unroll
         for (int e = 0; e < 8; ++e) s1[e] += b[e];
       }
-      if (g.z[1]) store8<TYPE>(static_cast<T*>(g.z[1]) + i * g.ldz[1] + j, vec, n, s1);
+      if (g.z[1]) store8<TYPE>(static_cast<T*>(g.z[1]) + i * g.ldz[1] + j, n, s1);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s0[e] *= s1[e];
     } else if (g.res) {
-      load8<TYPE>(static_cast<const T*>(g.res) + i * g.ldr + j, vec, n, b);
+      load8<TYPE>(static_cast<const T*>(g.res) + i * g.ldr + j, n, b);
 #pragma unroll
       for (int e = 0; e < 8; ++e) s0[e] += b[e];
     }
-    store8<TYPE>(static_cast<T*>(g.c[0]) + i * g.ldc[0] + j, vec, n, s0);
+    store8<TYPE>(static_cast<T*>(g.c[0]) + i * g.ldc[0] + j, n, s0);
   } else {
-    store8<TYPE>(static_cast<T*>(g.c[part]) + i * g.ldc[part] + j, vec, n, s0);
+    store8<TYPE>(static_cast<T*>(g.c[part]) + i * g.ldc[part] + j, n, s0);
   }
 }
 
-template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU, bool ALIGNED>
+template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
 __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile16(DenseGemm g) {
   constexpr bool kGate = KIND == kGated;
   constexpr bool kRmA = KIND == kWeightGrad, kRmB = KIND == kWeightGrad || KIND == kInputGrad;
@@ -516,68 +536,7 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
     }
   };
   int at_a = 0, at_b = 0;   // slots of the step that is multiplied
-  if constexpr (!ALIGNED) {
-    using T = typename Elem<TYPE>::T;
-    static_assert(!kTurns);
-    s16x8 held[kIssues];
-    auto fetch = [&](int step) {
-      const int part = KIND == kInputGrad && step >= per_part && g.parts > 1 ? 1 : 0;
-      const int r0 = (step - part * per_part) * kBK, valid = g.nr - r0;
-      const T* a = static_cast<const T*>(g.a[KIND == kWeightGrad ? wpart : part]);
-      a += kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0;
-      const T* b = static_cast<const T*>(g.b[part]);
-      b += kRmB ? int64_t(r0) * g.ldb[part] + j0 : int64_t(j0) * g.ldb[part] + r0;
-#pragma unroll
-      for (int n = 0; n < TileA::kLoads; ++n) held[n] = TileA::fetch(a, g.lda, g.ni - i0, valid, wave, lane, n);
-      if constexpr (kGate) {
-        const T* b1 = static_cast<const T*>(g.b[1]) + int64_t(j0) * g.ldb[1] + r0;
-#pragma unroll
-        for (int n = 0; n < TileH::kLoads; ++n) {
-          held[TileA::kLoads + n] = TileH::fetch(b, g.ldb[0], g.nj - j0, valid, wave, lane, n);
-          held[TileA::kLoads + TileH::kLoads + n] = TileH::fetch(b1, g.ldb[1], g.nj - j0, valid, wave, lane, n);
-        }
-      } else {
-#pragma unroll
-        for (int n = 0; n < TileB::kLoads; ++n)
-          held[TileA::kLoads + n] = TileB::fetch(b, g.ldb[part], g.nj - j0, valid, wave, lane, n);
-      }
-    };
-    auto put = [&](int slot) {
-      char* sa = lds + slot * TileA::kBytes;
-      char* sb = lds + kAreaB + slot * TileB::kBytes;
-#pragma unroll
-      for (int n = 0; n < TileA::kLoads; ++n) TileA::put(sa, held[n], wave, lane, n);
-#pragma unroll
-      for (int n = 0; n < TileB::kLoads; ++n) {
-        if constexpr (kGate)
-          TileH::put(sb + (n >= TileH::kLoads) * TileH::kBytes, held[TileA::kLoads + n], wave, lane, n % TileH::kLoads);
-        else
-          TileB::put(sb, held[TileA::kLoads + n], wave, lane, n);
-      }
-    };
-    if (begin < end) {
-      fetch(begin);
-      put(0);
-    }
-    for (int step = begin; step < end; ++step) {
-      stage_done<0>();
-      if (step + 1 < end) fetch(step + 1);
-      const char* sa = lds + at_a * TileA::kBytes;
-      const char* sb = lds + kAreaB + at_a * TileB::kBytes;
-#pragma unroll
-      for (int ks = 0; ks < kBK / 32; ++ks) {
-        s16x8 fa[kFI], fb[kFJ];
-        fragments_b(sb, ks, fb);
-        fragments_a(sa, ks, fa);
-#pragma unroll
-        for (int fi = 0; fi < kFI; ++fi)
-#pragma unroll
-          for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[fj], fa[fi], acc[fi][fj]);
-      }
-      at_a ^= 1;
-      if (step + 1 < end) put(at_a);
-    }
-  } else if constexpr (!kTurns) {
+  if constexpr (!kTurns) {
     // Two workgroups a CU: one reads while the other multiplies.
     set_a(begin, 0);
     set_b(begin, 0);
@@ -733,24 +692,19 @@ __global__ __launch_bounds__(256) void dense_join(DenseGemm g) {
   const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (at >= int64_t(groups) * g.ni) return;
   const int64_t i = at / groups;
-  const int j = static_cast<int>(at % groups) * 8, n = min(8, g.nj - j), part = blockIdx.y;
-  const int64_t slice = int64_t(g.ni) * g.nj;
+  const int j = static_cast<int>(at % groups) * 8, part = blockIdx.y;
+  const int64_t slice = int64_t(g.ni) * groups * 8;
   float s[2][8];
 #pragma unroll
   for (int mat = 0; mat < (KIND == kGated ? 2 : 1); ++mat) {
-    const float* p = g.partial + int64_t(KIND == kGated ? mat : part) * g.splits * slice + i * g.nj + j;
+    const float* p = g.partial + int64_t(KIND == kGated ? mat : part) * g.splits * slice + at * 8;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[mat][e] = 0.0f;
+#pragma unroll 4
     for (int split = 0; split < g.splits; ++split, p += slice) {
-      if (n == 8 && g.nj % 4 == 0) {
-        const f32x4 lo = reinterpret_cast<const f32x4*>(p)[0], hi = reinterpret_cast<const f32x4*>(p)[1];
+      const f32x4 lo = reinterpret_cast<const f32x4*>(p)[0], hi = reinterpret_cast<const f32x4*>(p)[1];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[mat][e] += lo[e], s[mat][4 + e] += hi[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (e < n) s[mat][e] += p[e];
-      }
+      for (int e = 0; e < 4; ++e) s[mat][e] += lo[e], s[mat][4 + e] += hi[e];
     }
   }
   finish8<TYPE, KIND, true>(g, part, 0, i, j, s[0], s[1]);
@@ -758,45 +712,135 @@ __global__ __launch_bounds__(256) void dense_join(DenseGemm g) {
 
 // ---------------------------------------------------------------- elementwise parts of the gradients
 
-// dz (or dg and du) and sums of their columns over a block of rows: a thread per column
-template <int TYPE>
+// dz (or dg and du), and the sums of their columns over a block of rows.  A thread has eight columns and every
+// lanes_y-th row of its block: 256 threads are lanes_x eights of columns by lanes_y rows.  One pass over the data.
+// Where all rows start at multiples of 16 bytes and hold whole eights (WHOLE), a thread's columns are consecutive and
+// read and written 16 bytes at a time (8192 x 4096 gated: 335 MB in 67 us, 5.0 TB/s); else they are lanes_x apart, and a
+// wavefront reads consecutive elements.  The column sums are of the 32-bit values, not of the rounded ones.
+template <int TYPE, bool GATED, bool WHOLE>
 __global__ __launch_bounds__(256) void dense_slope(DenseSlope s) {
   using T = typename Elem<TYPE>::T;
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= s.n) return;
+  constexpr int kMats = GATED ? 2 : 1;
+  __shared__ float sums[256][kMats * 8 + 1];
+  const int lanes_x = 1 << s.log_x, x = threadIdx.x & (lanes_x - 1), y = threadIdx.x >> s.log_x;
+  const int lanes_y = 256 >> s.log_x;
+  const int j = blockIdx.x * lanes_x * 8 + (WHOLE ? x * 8 : x), n8 = (s.n + 7) / 8 * 8;
   const int rows = (s.m + s.row_blocks - 1) / s.row_blocks;
-  const int first = blockIdx.y * rows, end = min(s.m, first + rows);
-  float sum0 = 0.0f, sum1 = 0.0f;
-  for (int i = first; i < end; ++i) {
-    const float dy = float(static_cast<const T*>(s.dy)[i * s.lddy + j]);
-    float d0 = dy, d1 = 0.0f;
-    if (s.z[0]) {
-      const float z = float(static_cast<const T*>(s.z[0])[i * s.ldz[0] + j]);
-      if (s.gated) {
-        const float u = float(static_cast<const T*>(s.z[1])[i * s.ldz[1] + j]);
-        d1 = dy * act_f(z, s.act);
-        d0 = dy * u * slope_f(z, s.act);
+  const int64_t first = int64_t(blockIdx.y) * rows, end = min(int64_t(s.m), first + rows);
+  float sum[kMats][8] = {};
+  auto load = [&](const void* base, int64_t row, float* v) {
+    const T* p = static_cast<const T*>(base) + row + j;
+    if constexpr (WHOLE) {
+      load8<TYPE>(p, 8, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = float(p[min(e * lanes_x, s.n - 1 - j)]);   // no branches between loads
+    }
+  };
+  auto store = [&](void* base, int64_t row, const float* v) {   // rows of dz are padded to whole eights, with zeros
+    T* p = static_cast<T*>(base) + row + j;
+    if constexpr (WHOLE) {
+      store8<TYPE>(p, 8, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (j + e * lanes_x < n8) p[e * lanes_x] = T(v[e]);
+    }
+  };
+  if (j < n8) {
+#pragma unroll 2
+    for (int64_t i = first + y; i < end; i += lanes_y) {
+      float dy[8], z[8], u[8], d0[8], d1[8];
+      load(s.dy, i * s.lddy, dy);
+      if (s.z[0]) {
+        load(s.z[0], i * s.ldz[0], z);
+        if constexpr (GATED) load(s.z[1], i * s.ldz[1], u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float value;
+          if constexpr (GATED) {
+            d0[e] = slope_f<TYPE>(dy[e] * u[e], z[e], s.act, &value);
+            d1[e] = dy[e] * value;
+          } else {
+            d0[e] = slope_f<TYPE>(dy[e], z[e], s.act, &value);
+          }
+        }
       } else {
-        d0 = s.act == EMB_ACT_RELU ? (z <= 0.0f ? 0.0f : dy) : dy * slope_f(z, s.act);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d0[e] = dy[e];
+      }
+      if constexpr (!WHOLE) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (j + e * lanes_x < s.n) continue;
+          d0[e] = 0.0f;
+          if constexpr (GATED) d1[e] = 0.0f;
+        }
+      }
+      if (s.dz[0]) store(s.dz[0], i * s.lddz, d0);
+      if constexpr (GATED)
+        if (s.dz[1]) store(s.dz[1], i * s.lddz, d1);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sum[0][e] += d0[e];
+        if constexpr (GATED) sum[1][e] += d1[e];
       }
     }
-    if (s.dz[0]) static_cast<T*>(s.dz[0])[i * s.lddz + j] = T(d0);
-    if (s.dz[1]) static_cast<T*>(s.dz[1])[i * s.lddz + j] = T(d1);
-    sum0 += d0;
-    sum1 += d1;
   }
-  if (s.colsum[0]) s.colsum[0][int64_t(blockIdx.y) * s.n + j] = sum0;
-  if (s.colsum[1]) s.colsum[1][int64_t(blockIdx.y) * s.n + j] = sum1;
+  if (!s.colsum[0] && !s.colsum[1]) return;
+#pragma unroll
+  for (int e = 0; e < kMats * 8; ++e) sums[threadIdx.x][e] = sum[e / 8][e % 8];
+  __syncthreads();
+  // the rows' sums are added in order, a column a thread
+  for (int c = threadIdx.x; c < lanes_x * 8 * kMats; c += 256) {
+    const int mat = c / (lanes_x * 8), column = c % (lanes_x * 8);
+    const int thread = WHOLE ? column / 8 : column % lanes_x, e = WHOLE ? column % 8 : column / lanes_x;
+    float total = 0.0f;
+    for (int r = 0; r < lanes_y; ++r) total += sums[r * lanes_x + thread][mat * 8 + e];
+    const int at = blockIdx.x * lanes_x * 8 + column;
+    if (at < s.n && s.colsum[mat]) s.colsum[mat][int64_t(blockIdx.y) * s.n + at] = total;
+  }
 }
 
+// sums of the blocks' column sums: 32 columns a workgroup, eight threads a column
 template <int TYPE>
-__global__ __launch_bounds__(256) void dense_colsum(const float* partial, int32_t blocks, int32_t n, void* out) {
+__global__ __launch_bounds__(256) void dense_colsum(DenseColsum s) {
   using T = typename Elem<TYPE>::T;
-  const int j = blockIdx.x * 256 + threadIdx.x;
-  if (j >= n) return;
+  __shared__ float sums[8][32];
+  const int c = threadIdx.x & 31, y = threadIdx.x >> 5, j = blockIdx.x * 32 + c;
+  const float* p = s.partial[blockIdx.y];
+  if (!p) return;
   float sum = 0.0f;
-  for (int b = 0; b < blocks; ++b) sum += partial[int64_t(b) * n + j];
-  static_cast<T*>(out)[j] = T(sum);
+  if (j < s.n) {
+#pragma unroll 8
+    for (int b = y; b < s.blocks; b += 8) sum += p[int64_t(b) * s.n + j];
+  }
+  sums[y][c] = sum;
+  __syncthreads();
+  if (y == 0 && j < s.n) {
+#pragma unroll
+    for (int r = 1; r < 8; ++r) sum += sums[r][c];
+    static_cast<T*>(s.out[blockIdx.y])[j] = T(sum);
+  }
+}
+
+// Copies up to three matrices to rows that start at multiples of 16 bytes and end in zeros up to a whole chunk: the
+// tiles above read nothing else.  A wavefront takes 64 consecutive elements at a time, as rows that start anywhere
+// are read fastest (16-byte loads at odd addresses measured 1.1 TB/s).
+__global__ __launch_bounds__(256) void dense_pack(DensePack p) {
+  const int mat = blockIdx.y;
+  const uint32_t cols = p.cols[mat], padded = (cols + 7) / 8 * 8;
+  const uint32_t rows = p.rows[mat];
+  const uint16_t* src = static_cast<const uint16_t*>(p.src[mat]);
+  uint16_t* dst = static_cast<uint16_t*>(p.dst[mat]);
+  // as many rows side by side as 256 threads hold
+  const uint32_t wide = p.wide[mat], x = threadIdx.x % wide, y = threadIdx.x / wide, side = 256 / wide;
+  for (uint64_t i = uint64_t(blockIdx.x) * side + y; i < rows; i += uint64_t(gridDim.x) * side)
+#pragma unroll 4
+    for (uint32_t j = x; j < padded; j += wide) {
+      const uint16_t v = src[i * p.lds[mat] + min(j, cols - 1)];
+      dst[i * p.ldd[mat] + j] = j < cols ? v : 0;
+    }
 }
 
 template <int TYPE, int KIND>
@@ -808,12 +852,12 @@ int simple_launch(const DenseGemm& g, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU, bool ALIGNED>
+template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
 int tile16_launch(const DenseGemm& g, hipStream_t stream) {
   const int cols = KIND == kGated ? BN / 2 : BN;
   const int64_t tiles = int64_t((g.ni + BM - 1) / BM) * ((g.nj + cols - 1) / cols);
   const dim3 grid(static_cast<uint32_t>(tiles), g.splits, KIND == kWeightGrad ? g.parts : 1);
-  dense_tile16<TYPE, KIND, BM, BN, WI, WJ, PER_CU, ALIGNED><<<grid, 64 * WI * WJ, 0, stream>>>(g);
+  dense_tile16<TYPE, KIND, BM, BN, WI, WJ, PER_CU><<<grid, 64 * WI * WJ, 0, stream>>>(g);
   return hipGetLastError();
 }
 
@@ -828,9 +872,8 @@ int join_launch(const DenseGemm& g, hipStream_t stream) {
 template <int TYPE, int KIND>
 int kind_launch(const DenseGemm& g, hipStream_t stream) {
   if constexpr (TYPE != kDenseF32) {
-    if (g.variant == kTile256) return tile16_launch<TYPE, KIND, 256, 256, 2, 4, 1, true>(g, stream);
-    if (g.aligned) return tile16_launch<TYPE, KIND, 128, 128, 2, 2, 2, true>(g, stream);
-    return tile16_launch<TYPE, KIND, 128, 128, 2, 2, 2, false>(g, stream);
+    if (g.variant == kTile256) return tile16_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
+    return tile16_launch<TYPE, KIND, 128, 128, 2, 2, 2>(g, stream);
   }
   return simple_launch<TYPE, KIND>(g, stream);
 }
@@ -855,13 +898,18 @@ int gemm_launch(int kind, const DenseGemm& g, hipStream_t stream) {
 
 template <int TYPE>
 int slope_launch(const DenseSlope& s, hipStream_t stream) {
-  dense_slope<TYPE><<<dim3((s.n + 255) / 256, s.row_blocks), 256, 0, stream>>>(s);
+  const int eights = (s.n + 7) / 8, x = 1 << s.log_x;
+  const dim3 grid((eights + x - 1) / x, s.row_blocks);
+  if (s.gated && s.whole) dense_slope<TYPE, true, true><<<grid, 256, 0, stream>>>(s);
+  else if (s.gated) dense_slope<TYPE, true, false><<<grid, 256, 0, stream>>>(s);
+  else if (s.whole) dense_slope<TYPE, false, true><<<grid, 256, 0, stream>>>(s);
+  else dense_slope<TYPE, false, false><<<grid, 256, 0, stream>>>(s);
   return hipGetLastError();
 }
 
 template <int TYPE>
-int colsum_launch(const float* partial, int32_t blocks, int32_t n, void* out, hipStream_t stream) {
-  dense_colsum<TYPE><<<(n + 255) / 256, 256, 0, stream>>>(partial, blocks, n, out);
+int colsum_launch(const DenseColsum& s, hipStream_t stream) {
+  dense_colsum<TYPE><<<dim3((s.n + 31) / 32, 2), 256, 0, stream>>>(s);
   return hipGetLastError();
 }
 
@@ -874,9 +922,16 @@ int colsum_launch(const float* partial, int32_t blocks, int32_t n, void* out, hi
   int dense_slope_##NAME(const DenseSlope& s, void* stream) {                                           \
     return slope_launch<TYPE>(s, static_cast<hipStream_t>(stream));                                     \
   }                                                                                                     \
-  int dense_colsum_##NAME(const float* p, int32_t blocks, int32_t n, void* out, void* stream) {         \
-    return colsum_launch<TYPE>(p, blocks, n, out, static_cast<hipStream_t>(stream));                    \
+  int dense_colsum_##NAME(const DenseColsum& s, void* stream) {                                         \
+    return colsum_launch<TYPE>(s, static_cast<hipStream_t>(stream));                                    \
   }
+
+#if EMBX_HAS_DPART(0)
+int dense_pack_launch(const DensePack& p, void* stream) {
+  dense_pack<<<dim3(p.groups, p.count), 256, 0, static_cast<hipStream_t>(stream)>>>(p);
+  return hipGetLastError();
+}
+#endif
 
 #if EMBX_HAS_DPART(0)
 EMBX_DENSE_TYPE(f32, kDenseF32)

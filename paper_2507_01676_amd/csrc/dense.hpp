@@ -34,8 +34,6 @@ struct DenseGemm {
   int32_t ni, nj, nr;      // C is [ni][nj], the sum over nr (in each part)
   int32_t parts, splits, act;
   int32_t variant;         // DenseVariant
-  int32_t aligned;         // operands' rows start at multiples of 16 bytes and hold whole chunks
-  int32_t vec;             // results, residual and bias may be read and written 16 bytes at a time
 };
 
 // dz = dy * act'(z), or dg, du; and partial column sums of them
@@ -46,13 +44,33 @@ struct DenseSlope {
   float* colsum[2];        // [row blocks][n], or NULL
   int64_t lddy, ldz[2], lddz;
   int32_t m, n, act, gated, row_blocks;
+  int32_t log_x;           // log2 of the eights of columns of a workgroup
+  int32_t whole;           // rows of all operands start at multiples of 16 bytes and hold whole eights
 };
+
+// matrices of 16-bit elements copied to rows of whole 16-byte chunks
+struct DensePack {
+  const void* src[3];
+  void* dst[3];
+  int64_t lds[3], ldd[3];
+  uint32_t rows[3], cols[3], wide[3];
+  int32_t count, groups;
+};
+
+// column sums from those of blocks of rows
+struct DenseColsum {
+  const float* partial[2];   // [blocks][n], or NULL
+  void* out[2];
+  int32_t blocks, n;
+};
+
+int dense_pack_launch(const DensePack& p, void* stream);
 
 // launches of the kernels of one type (dense.hip is compiled once per type); 0 or a hipError_t
 #define EMBX_DENSE_DECLARE(NAME)                                                        \
   int dense_gemm_##NAME(int kind, const DenseGemm& g, void* stream);                    \
   int dense_slope_##NAME(const DenseSlope& s, void* stream);                            \
-  int dense_colsum_##NAME(const float* p, int32_t blocks, int32_t n, void* out, void* stream);
+  int dense_colsum_##NAME(const DenseColsum& s, void* stream);
 EMBX_DENSE_DECLARE(f32)
 EMBX_DENSE_DECLARE(f16)
 EMBX_DENSE_DECLARE(bf16)

@@ -58,31 +58,15 @@ emb_status_t check_workspace(const void* ws, size_t have, size_t need) {
 
 emb_status_t run(int rc) { return rc == 0 ? EMB_OK : EMB_ERR_DEVICE; }
 
-// (a tile's offsets, 256 rows at most, are 32-bit)
-bool whole(const void* p, int64_t ld) { return !misaligned(p, 16) && ld % 8 == 0 && ld <= (int64_t(1) << 22); }
-
-// Whether rows of every operand and result start at multiples of 16 bytes and hold whole chunks of
-// eight elements (16-bit types).
-bool aligned16(int kind, const DenseGemm& g) {
-  const int parts = g.parts;
-  bool ok = g.nj % 8 == 0;
-  for (int p = 0; p < (kind == kGated ? 1 : parts); ++p) ok = ok && whole(g.a[p], g.lda);
-  for (int p = 0; p < (kind == kGated ? 2 : parts); ++p) ok = ok && whole(g.b[p], g.ldb[p]);
-  // along the reduction: whole chunks of it; reduction-major: whole chunks of results
-  if (kind != kWeightGrad) ok = ok && g.nr % 8 == 0;
-  if (kind == kWeightGrad) ok = ok && g.ni % 8 == 0;
-  return ok;
+// Whether the tiles of 16-bit types can read a matrix where it lies: rows that start at multiples of 16 bytes and
+// hold whole chunks of eight elements (and a tile's offsets, 256 rows at most, fit 32 bits).
+bool whole(const void* p, int64_t ld, int64_t cols) {
+  return !misaligned(p, 16) && ld % 8 == 0 && cols % 8 == 0 && ld <= (int64_t(1) << 22);
 }
 
-bool aligned_results(int kind, const DenseGemm& g) {
-  bool ok = g.nj % 8 == 0;
-  for (int p = 0; p < (kind == kWeightGrad ? g.parts : 1); ++p) ok = ok && whole(g.c[p], g.ldc[p]);
-  for (int p = 0; p < 2; ++p) {
-    if (g.z[p]) ok = ok && whole(g.z[p], g.ldz[p]);
-    if (g.bias[p]) ok = ok && !misaligned(g.bias[p], 16);
-  }
-  if (g.res) ok = ok && whole(g.res, g.ldr);
-  return ok;
+// the same for the elementwise passes, of every type
+bool whole16(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
+  return !misaligned(p, 16) && ld * esize(dtype) % 16 == 0 && cols % 8 == 0;
 }
 
 // Which tile a product takes and over how many workgroups its reduction is split.
@@ -110,14 +94,13 @@ double tile_us(int variant, double tiles, int steps, int s, double result_bytes)
   return us;
 }
 
-Choice choose(int kind, int64_t ni, int64_t nj, int64_t nr, int parts, bool large_tiles) {
+Choice choose(int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
   const int64_t steps = (nr + kStep - 1) / kStep * (kind == kInputGrad ? parts : 1);
   const int results = kind == kWeightGrad ? parts : kind == kGated ? 2 : 1;
   const double result_bytes = 4.0 * ni * nj * results;
   Choice best = {kTile128, 1};
   double least = 0.0;
   for (int variant = kTile256; variant >= kTile128; --variant) {
-    if (variant == kTile256 && !large_tiles) continue;
     const int64_t side = variant == kTile256 ? 256 : 128;
     const double tiles = double((ni + side - 1) / side) * ((nj * (kind == kGated ? 2 : 1) + side - 1) / side) *
                          (kind == kWeightGrad ? parts : 1);
@@ -129,16 +112,12 @@ Choice choose(int kind, int64_t ni, int64_t nj, int64_t nr, int parts, bool larg
   return best;
 }
 
-// Bytes of partial sums of a product, whatever its operands' alignment.
+// bytes of partial sums of a product
 size_t partial_bytes(int32_t dtype, int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
   if (dtype == EMB_DTYPE_F32) return 0;
   const int results = kind == kWeightGrad ? parts : kind == kGated ? 2 : 1;
-  size_t most = 0;
-  for (bool large : {false, true}) {
-    const int s = choose(kind, ni, nj, nr, parts, large).splits;
-    if (s > 1) most = std::max(most, size_t(s) * ni * nj * results * 4);
-  }
-  return most;
+  const int s = choose(kind, ni, nj, nr, parts).splits;
+  return s > 1 ? size_t(s) * ni * ((nj + 7) / 8 * 8) * results * 4 : 0;   // (rows of whole eights)
 }
 
 emb_status_t gemm(int32_t dtype, int kind, const DenseGemm& given, float* partial, void* stream) {
@@ -146,9 +125,7 @@ emb_status_t gemm(int32_t dtype, int kind, const DenseGemm& given, float* partia
   g.splits = 1;
   g.partial = partial;
   if (dtype != EMB_DTYPE_F32) {
-    g.aligned = aligned16(kind, g);
-    g.vec = aligned_results(kind, g);
-    const Choice c = choose(kind, g.ni, g.nj, g.nr, g.parts, g.aligned);
+    const Choice c = choose(kind, g.ni, g.nj, g.nr, g.parts);
     g.variant = c.variant, g.splits = c.splits;
   }
   switch (dtype) {
@@ -166,11 +143,11 @@ emb_status_t slope(int32_t dtype, const DenseSlope& s, void* stream) {
   }
 }
 
-emb_status_t colsum(int32_t dtype, const float* p, int32_t blocks, int64_t n, void* out, void* stream) {
+emb_status_t colsum(int32_t dtype, const DenseColsum& s, void* stream) {
   switch (dtype) {
-    case EMB_DTYPE_F32: return run(dense_colsum_f32(p, blocks, n, out, stream));
-    case EMB_DTYPE_F16: return run(dense_colsum_f16(p, blocks, n, out, stream));
-    default: return run(dense_colsum_bf16(p, blocks, n, out, stream));
+    case EMB_DTYPE_F32: return run(dense_colsum_f32(s, stream));
+    case EMB_DTYPE_F16: return run(dense_colsum_f16(s, stream));
+    default: return run(dense_colsum_bf16(s, stream));
   }
 }
 
@@ -186,44 +163,135 @@ struct Arena {
   }
 };
 
-// blocks of rows of the column sums
-int32_t slope_blocks(int64_t m) { return static_cast<int32_t>(std::max<int64_t>(1, std::min<int64_t>(256, m / 16))); }
-
-struct GradSpace {
-  void* dz[2] = {nullptr, nullptr};
-  float* colsum[2] = {nullptr, nullptr};
-  float* partial = nullptr;   // of one product after the other
-  int64_t lddz = 0;
-  int32_t blocks = 1;
+// A matrix as the products read it: where it lies, or a copy in the workspace.
+struct Operand {
+  const void* p;
+  int64_t ld;
 };
 
-// dz of `mats` results, and partial column sums, as wanted
-GradSpace grad_space(Arena& ar, int64_t m, int64_t n, int32_t dtype, int mats, bool dz, const bool* sums) {
-  GradSpace g;
-  g.lddz = (n + 63) / 64 * 64;
-  g.blocks = slope_blocks(m);
-  for (int i = 0; i < mats; ++i)
-    if (dz) g.dz[i] = ar.take<void>(m * g.lddz * esize(dtype));
-  for (int i = 0; i < mats; ++i)
-    if (sums[i]) g.colsum[i] = ar.take<float>(size_t(g.blocks) * n * 4);
-  return g;
+// Collects the matrices of a call that have to be copied.
+struct Packer {
+  Arena& ar;
+  int32_t dtype;
+  DensePack pack = {};
+  Operand use(const void* p, int64_t ld, int64_t rows, int64_t cols) {
+    if (dtype == EMB_DTYPE_F32 || rows == 0 || whole(p, ld, cols)) return {p, ld};
+    const int64_t ldd = (cols + 7) / 8 * 8;
+    const int at = pack.count++;
+    pack.src[at] = p, pack.lds[at] = ld;
+    pack.dst[at] = ar.take<void>(rows * ldd * 2), pack.ldd[at] = ldd;
+    pack.rows[at] = static_cast<uint32_t>(rows), pack.cols[at] = static_cast<uint32_t>(cols);
+    uint32_t wide = 8;
+    while (wide < 256 && wide < ldd) wide *= 2;
+    pack.wide[at] = wide;
+    // enough workgroups for the longest matrix, at most eight a CU
+    pack.groups = std::max<int32_t>(pack.groups, static_cast<int32_t>(std::min<int64_t>(8 * kCus, (rows * wide + 255) / 256)));
+    return {pack.dst[at], ldd};
+  }
+};
+
+// log2 of the eights of columns that a workgroup of the elementwise pass has side by side: as many as a row has, at
+// most 64 (a wavefront reads 1 KB of a row)
+int32_t slope_log_x(int64_t n) {
+  int32_t l = 0;
+  while (l < 6 && (int64_t(8) << l) < n) ++l;
+  return l;
 }
 
-GradSpace linear_grad_space(Arena& ar, const emb_linear_grad_t& a) {
-  const bool sums[2] = {a.dbias != nullptr, false};
-  GradSpace g = grad_space(ar, a.m, a.n, a.dtype, 1, a.activation != EMB_ACT_NONE && (a.dx || a.dweight), sums);
-  g.partial = ar.take<float>(std::max(a.dx ? partial_bytes(a.dtype, kInputGrad, a.m, a.k, a.n, 1) : 0,
+// blocks of rows of that pass: 1024 workgroups in all if every thread still has four rows, and at most 256 blocks, whose
+// column sums are added up afterwards
+int32_t slope_blocks(int64_t m, int64_t n) {
+  const int32_t log_x = slope_log_x(n);
+  const int64_t across = ((n + 7) / 8 + (1 << log_x) - 1) >> log_x;
+  const int64_t rows = int64_t(4) * (256 >> log_x);
+  return static_cast<int32_t>(std::max<int64_t>(1, std::min({int64_t(256), (1024 + across - 1) / across, (m + rows - 1) / rows})));
+}
+
+// The workspace of each call: copies of operands, dz, column sums and partial sums of products.
+struct Space {
+  Operand x, w[2], dz[2];
+  DensePack pack;
+  float* colsum[2] = {nullptr, nullptr};
+  float* partial = nullptr;   // of one product after the other
+  int32_t blocks = 1;         // of rows of column sums
+  bool slopes = false;        // dz is computed
+};
+
+Space linear_space(Arena& ar, const emb_linear_t& a) {
+  Space s;
+  Packer pk{ar, a.dtype};
+  if (a.m > 0) {
+    s.x = pk.use(a.x, a.ldx, a.m, a.k);
+    s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k);
+  }
+  s.pack = pk.pack;
+  s.partial = ar.take<float>(partial_bytes(a.dtype, kForward, a.m, a.n, a.k, 1));
+  return s;
+}
+
+Space gated_space(Arena& ar, const emb_gated_t& a) {
+  Space s;
+  Packer pk{ar, a.dtype};
+  if (a.m > 0) {
+    s.x = pk.use(a.x, a.ldx, a.m, a.k);
+    s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k);
+    s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k);
+  }
+  s.pack = pk.pack;
+  s.partial = ar.take<float>(partial_bytes(a.dtype, kGated, a.m, a.n, a.k, 1));
+  return s;
+}
+
+// a computed dz: rows padded to whole chunks
+Operand dz_space(Arena& ar, int64_t m, int64_t n, int32_t dtype) {
+  const int64_t ld = (n + 7) / 8 * 8;
+  return {ar.take<void>(m * ld * esize(dtype)), ld};
+}
+
+float* colsum_space(Arena& ar, bool wanted, int32_t blocks, int64_t n) {
+  return wanted ? ar.take<float>(size_t(blocks) * n * 4) : nullptr;
+}
+
+Space linear_grad_space(Arena& ar, const emb_linear_grad_t& a) {
+  Space s;
+  Packer pk{ar, a.dtype};
+  const bool dx = a.dx && a.m > 0;
+  s.slopes = a.activation != EMB_ACT_NONE && a.m > 0 && (dx || a.dweight);
+  if (s.slopes) s.dz[0] = dz_space(ar, a.m, a.n, a.dtype);
+  else if (dx || a.dweight) s.dz[0] = pk.use(a.dy, a.lddy, a.m, a.n);
+  if (dx) s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k);
+  if (a.dweight) s.x = pk.use(a.x, a.ldx, a.m, a.k);
+  s.pack = pk.pack;
+  s.blocks = slope_blocks(a.m, a.n);
+  s.colsum[0] = colsum_space(ar, a.dbias, s.blocks, a.n);
+  s.partial = ar.take<float>(std::max(dx ? partial_bytes(a.dtype, kInputGrad, a.m, a.k, a.n, 1) : 0,
                                       a.dweight ? partial_bytes(a.dtype, kWeightGrad, a.n, a.k, a.m, 1) : 0));
-  return g;
+  return s;
 }
 
-GradSpace gated_grad_space(Arena& ar, const emb_gated_grad_t& a) {
-  const bool sums[2] = {a.db_gate != nullptr, a.db_up != nullptr};
-  GradSpace g = grad_space(ar, a.m, a.n, a.dtype, 2, a.dx || a.dw_gate || a.dw_up, sums);
+Space gated_grad_space(Arena& ar, const emb_gated_grad_t& a) {
+  Space s;
+  Packer pk{ar, a.dtype};
+  const bool dx = a.dx && a.m > 0;
   const int weights = (a.dw_gate != nullptr) + (a.dw_up != nullptr);
-  g.partial = ar.take<float>(std::max(a.dx ? partial_bytes(a.dtype, kInputGrad, a.m, a.k, a.n, 2) : 0,
+  s.slopes = a.m > 0 && (dx || weights);
+  for (int i = 0; i < 2 && s.slopes; ++i) s.dz[i] = dz_space(ar, a.m, a.n, a.dtype);
+  if (dx) {
+    s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k);
+    s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k);
+  }
+  if (weights) s.x = pk.use(a.x, a.ldx, a.m, a.k);
+  s.pack = pk.pack;
+  s.blocks = slope_blocks(a.m, a.n);
+  s.colsum[0] = colsum_space(ar, a.db_gate, s.blocks, a.n);
+  s.colsum[1] = colsum_space(ar, a.db_up, s.blocks, a.n);
+  s.partial = ar.take<float>(std::max(dx ? partial_bytes(a.dtype, kInputGrad, a.m, a.k, a.n, 2) : 0,
                                       weights ? partial_bytes(a.dtype, kWeightGrad, a.n, a.k, a.m, weights) : 0));
-  return g;
+  return s;
+}
+
+emb_status_t run_pack(const DensePack& p, void* stream) {
+  return p.count ? run(dense_pack_launch(p, stream)) : EMB_OK;
 }
 
 }  // namespace
@@ -233,7 +301,9 @@ extern "C" {
 emb_status_t emb_linear_workspace(const emb_linear_t* a, size_t* bytes) {
   if (!a || !bytes) return EMB_ERR_INVALID_ARGUMENT;
   EMBX_TRY(check_shape(a->m, a->n, a->k, a->dtype, a->activation));
-  *bytes = partial_bytes(a->dtype, kForward, a->m, a->n, a->k, 1);
+  Arena ar{nullptr};
+  linear_space(ar, *a);
+  *bytes = ar.used;
   return EMB_OK;
 }
 
@@ -248,16 +318,19 @@ emb_status_t emb_linear(const emb_linear_t* a, void* workspace, size_t workspace
   EMBX_TRY(check_optional(a->z, a->ldz, a->m, a->n, a->dtype));
   EMBX_TRY(check_workspace(workspace, workspace_bytes, need));
   if (a->m == 0) return EMB_OK;
+  Arena ar{static_cast<char*>(workspace)};
+  const Space sp = linear_space(ar, *a);
+  EMBX_TRY(run_pack(sp.pack, stream));
   DenseGemm g = {};
-  g.a[0] = a->x, g.lda = a->ldx;
-  g.b[0] = a->weight, g.ldb[0] = a->ldw;
+  g.a[0] = sp.x.p, g.lda = sp.x.ld;
+  g.b[0] = sp.w[0].p, g.ldb[0] = sp.w[0].ld;
   g.c[0] = a->y, g.ldc[0] = a->ldy;
   g.z[0] = a->z, g.ldz[0] = a->ldz;
   g.bias[0] = a->bias;
   g.res = a->residual, g.ldr = a->ldr;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
-  g.parts = 1, g.splits = 1, g.act = a->activation;
-  return gemm(a->dtype, kForward, g, static_cast<float*>(workspace), stream);
+  g.parts = 1, g.act = a->activation;
+  return gemm(a->dtype, kForward, g, sp.partial, stream);
 }
 
 emb_status_t emb_linear_backward_workspace(const emb_linear_grad_t* a, size_t* bytes) {
@@ -282,29 +355,34 @@ emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, si
   EMBX_TRY(check_vector(a->dbias, a->dtype));
   EMBX_TRY(check_workspace(workspace, workspace_bytes, need));
   Arena ar{static_cast<char*>(workspace)};
-  const GradSpace sp = linear_grad_space(ar, *a);
-  const bool dz = sp.dz[0] != nullptr;
-  if (a->dbias || (dz && a->m > 0)) {
+  const Space sp = linear_grad_space(ar, *a);
+  EMBX_TRY(run_pack(sp.pack, stream));
+  if (a->dbias || sp.slopes) {
     DenseSlope s = {};
     s.dy = a->dy, s.lddy = a->lddy;
     s.z[0] = slopes ? a->z : nullptr, s.ldz[0] = a->ldz;
-    s.dz[0] = sp.dz[0], s.lddz = sp.lddz;
+    s.dz[0] = sp.slopes ? const_cast<void*>(sp.dz[0].p) : nullptr, s.lddz = sp.dz[0].ld;
     s.colsum[0] = sp.colsum[0];
     s.m = a->m, s.n = a->n, s.act = a->activation, s.gated = 0, s.row_blocks = sp.blocks;
+    s.log_x = slope_log_x(a->n);
+    s.whole = whole16(a->dy, a->lddy, a->n, a->dtype) && (!slopes || whole16(a->z, a->ldz, a->n, a->dtype));
     EMBX_TRY(slope(a->dtype, s, stream));
-    if (a->dbias) EMBX_TRY(colsum(a->dtype, sp.colsum[0], sp.blocks, a->n, a->dbias, stream));
+    if (a->dbias) {
+      const DenseColsum c = {{sp.colsum[0], nullptr}, {a->dbias, nullptr}, sp.blocks, static_cast<int32_t>(a->n)};
+      EMBX_TRY(colsum(a->dtype, c, stream));
+    }
   }
   DenseGemm g = {};
-  g.a[0] = dz ? sp.dz[0] : a->dy, g.lda = dz ? sp.lddz : a->lddy;
-  g.parts = 1, g.splits = 1;
+  g.a[0] = sp.dz[0].p, g.lda = sp.dz[0].ld;
+  g.parts = 1;
   if (a->dx && a->m > 0) {
-    g.b[0] = a->weight, g.ldb[0] = a->ldw;
+    g.b[0] = sp.w[0].p, g.ldb[0] = sp.w[0].ld;
     g.c[0] = a->dx, g.ldc[0] = a->lddx;
     g.ni = a->m, g.nj = a->k, g.nr = a->n;
     EMBX_TRY(gemm(a->dtype, kInputGrad, g, sp.partial, stream));
   }
   if (a->dweight) {
-    g.b[0] = a->x, g.ldb[0] = a->ldx;
+    g.b[0] = sp.x.p, g.ldb[0] = sp.x.ld;
     g.c[0] = a->dweight, g.ldc[0] = a->lddw;
     g.ni = a->n, g.nj = a->k, g.nr = a->m;
     EMBX_TRY(gemm(a->dtype, kWeightGrad, g, sp.partial, stream));
@@ -315,7 +393,9 @@ emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, si
 emb_status_t emb_gated_workspace(const emb_gated_t* a, size_t* bytes) {
   if (!a || !bytes) return EMB_ERR_INVALID_ARGUMENT;
   EMBX_TRY(check_shape(a->m, a->n, a->k, a->dtype, a->activation));
-  *bytes = partial_bytes(a->dtype, kGated, a->m, a->n, a->k, 1);
+  Arena ar{nullptr};
+  gated_space(ar, *a);
+  *bytes = ar.used;
   return EMB_OK;
 }
 
@@ -332,17 +412,20 @@ emb_status_t emb_gated(const emb_gated_t* a, void* workspace, size_t workspace_b
   EMBX_TRY(check_optional(a->u, a->ldu, a->m, a->n, a->dtype));
   EMBX_TRY(check_workspace(workspace, workspace_bytes, need));
   if (a->m == 0) return EMB_OK;
+  Arena ar{static_cast<char*>(workspace)};
+  const Space sp = gated_space(ar, *a);
+  EMBX_TRY(run_pack(sp.pack, stream));
   DenseGemm g = {};
-  g.a[0] = a->x, g.lda = a->ldx;
-  g.b[0] = a->w_gate, g.ldb[0] = a->ld_gate;
-  g.b[1] = a->w_up, g.ldb[1] = a->ld_up;
+  g.a[0] = sp.x.p, g.lda = sp.x.ld;
+  g.b[0] = sp.w[0].p, g.ldb[0] = sp.w[0].ld;
+  g.b[1] = sp.w[1].p, g.ldb[1] = sp.w[1].ld;
   g.c[0] = a->h, g.ldc[0] = a->ldh;
   g.z[0] = a->g, g.ldz[0] = a->ldg;
   g.z[1] = a->u, g.ldz[1] = a->ldu;
   g.bias[0] = a->b_gate, g.bias[1] = a->b_up;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
-  g.parts = 1, g.splits = 1, g.act = a->activation;
-  return gemm(a->dtype, kGated, g, static_cast<float*>(workspace), stream);
+  g.parts = 1, g.act = a->activation;
+  return gemm(a->dtype, kGated, g, sp.partial, stream);
 }
 
 emb_status_t emb_gated_backward_workspace(const emb_gated_grad_t* a, size_t* bytes) {
@@ -373,27 +456,31 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
   EMBX_TRY(check_vector(a->db_up, a->dtype));
   EMBX_TRY(check_workspace(workspace, workspace_bytes, need));
   Arena ar{static_cast<char*>(workspace)};
-  const GradSpace sp = gated_grad_space(ar, *a);
+  const Space sp = gated_grad_space(ar, *a);
+  EMBX_TRY(run_pack(sp.pack, stream));
   const bool sums = a->db_gate || a->db_up;
-  if (sums || (sp.dz[0] && a->m > 0)) {
+  if (sums || sp.slopes) {
     DenseSlope s = {};
     s.dy = a->dh, s.lddy = a->lddh;
     s.z[0] = a->g, s.ldz[0] = a->ldg;
     s.z[1] = a->u, s.ldz[1] = a->ldu;
-    s.dz[0] = sp.dz[0], s.dz[1] = sp.dz[1], s.lddz = sp.lddz;
+    for (int i = 0; i < 2; ++i) s.dz[i] = sp.slopes ? const_cast<void*>(sp.dz[i].p) : nullptr;
+    s.lddz = sp.dz[0].ld;
     s.colsum[0] = sp.colsum[0], s.colsum[1] = sp.colsum[1];
     s.m = a->m, s.n = a->n, s.act = a->activation, s.gated = 1, s.row_blocks = sp.blocks;
+    s.log_x = slope_log_x(a->n);
+    s.whole = whole16(a->dh, a->lddh, a->n, a->dtype) && whole16(a->g, a->ldg, a->n, a->dtype) &&
+              whole16(a->u, a->ldu, a->n, a->dtype);
     EMBX_TRY(slope(a->dtype, s, stream));
-    if (a->db_gate) EMBX_TRY(colsum(a->dtype, sp.colsum[0], sp.blocks, a->n, a->db_gate, stream));
-    if (a->db_up) EMBX_TRY(colsum(a->dtype, sp.colsum[1], sp.blocks, a->n, a->db_up, stream));
+    if (sums) {
+      const DenseColsum c = {{sp.colsum[0], sp.colsum[1]}, {a->db_gate, a->db_up}, sp.blocks, static_cast<int32_t>(a->n)};
+      EMBX_TRY(colsum(a->dtype, c, stream));
+    }
   }
   DenseGemm g = {};
-  g.lda = sp.lddz;
-  g.splits = 1;
+  g.lda = sp.dz[0].ld;
   if (a->dx && a->m > 0) {
-    g.a[0] = sp.dz[0], g.a[1] = sp.dz[1];
-    g.b[0] = a->w_gate, g.ldb[0] = a->ld_gate;
-    g.b[1] = a->w_up, g.ldb[1] = a->ld_up;
+    for (int i = 0; i < 2; ++i) g.a[i] = sp.dz[i].p, g.b[i] = sp.w[i].p, g.ldb[i] = sp.w[i].ld;
     g.c[0] = a->dx, g.ldc[0] = a->lddx;
     g.ni = a->m, g.nj = a->k, g.nr = a->n, g.parts = 2;
     EMBX_TRY(gemm(a->dtype, kInputGrad, g, sp.partial, stream));
@@ -403,11 +490,11 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
     for (int i = 0; i < 2; ++i) {
       void* dw = i == 0 ? a->dw_gate : a->dw_up;
       if (!dw) continue;
-      g.a[g.parts] = sp.dz[i];
+      g.a[g.parts] = sp.dz[i].p;
       g.c[g.parts] = dw, g.ldc[g.parts] = i == 0 ? a->ldd_gate : a->ldd_up;
       ++g.parts;
     }
-    g.b[0] = g.b[1] = a->x, g.ldb[0] = g.ldb[1] = a->ldx;
+    g.b[0] = g.b[1] = sp.x.p, g.ldb[0] = g.ldb[1] = sp.x.ld;
     g.ni = a->n, g.nj = a->k, g.nr = a->m;
     EMBX_TRY(gemm(a->dtype, kWeightGrad, g, sp.partial, stream));
   }

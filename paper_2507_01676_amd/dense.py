@@ -13,7 +13,6 @@ torch.cuda.Stream or a raw handle), the current stream by default.
 from __future__ import annotations
 
 import ctypes
-import functools
 
 import torch
 
@@ -53,20 +52,12 @@ def _entry(name, struct):
     fn = getattr(_lib, name)
     fn.restype, fn.argtypes = _i32, [ctypes.POINTER(struct), _vp, _sz, _vp]
 
-    @functools.lru_cache(maxsize=4096)
-    def workspace(m, n, k, dtype, act, wanted):
-        """Bytes of workspace: a function of the sizes, the types and the results that are wanted."""
-        a = struct(m, n, k, dtype, act)
-        for field in wanted:
-            setattr(a, field, 1)   # not NULL; never read
+    def call(a, device, stream):
         nbytes = _sz(0)
-        code = size(ctypes.byref(a), ctypes.byref(nbytes))
+        code = size(a, nbytes)
         if code != OK:
             raise EmbxError(code, name)
-        return nbytes.value
-
-    def call(a, wanted, device, stream):
-        nbytes = workspace(a.m, a.n, a.k, a.dtype, a.activation, wanted)
+        nbytes = nbytes.value
         ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
         code = fn(a, ws.data_ptr() if nbytes else None, nbytes, stream)
         if code != OK:
@@ -156,7 +147,7 @@ def _run_linear(stream, x, weight, bias, residual, activation, out, save):
                 _vector(bias, "bias", n, x), *(_matrix(residual, "residual", m, n, x) if residual is not None else (None, 0)),
                 *((y.data_ptr(), n) if out is None else _matrix(y, "out", m, n, x)),
                 *((z.data_ptr(), n) if save else (None, 0)))
-    _linear(a, (), device, stream)
+    _linear(a, device, stream)
     return (y, z) if save else y
 
 
@@ -180,12 +171,8 @@ def _run_linear_backward(stream, dy, x, weight, z, activation, bias, need_dx, ne
                     *_matrix(weight, "weight", n, k, x), *(_matrix(z, "z", m, n, x) if act else (None, 0)),
                     *((dx.data_ptr(), k) if need_dx else (None, 0)), *((dw.data_ptr(), k) if need_dw else (None, 0)),
                     db.data_ptr() if bias else None)
-    _linear_backward(a, _wanted(dx=need_dx and m > 0, dweight=need_dw, dbias=bias), device, stream)
+    _linear_backward(a, device, stream)
     return dx, dw, db
-
-
-def _wanted(**fields):
-    return tuple(name for name, yes in fields.items() if yes)
 
 
 def gated_ffn(x, w_gate, w_up, b_gate=None, b_up=None, *, activation="silu", out=None, save=False, stream=None):
@@ -204,7 +191,7 @@ def _run_gated(stream, x, w_gate, w_up, b_gate, b_up, activation, out, save):
                *_matrix(w_up, "w_up", n, k, x), _vector(b_gate, "b_gate", n, x), _vector(b_up, "b_up", n, x),
                *((h.data_ptr(), n) if out is None else _matrix(h, "out", m, n, x)),
                *((g.data_ptr(), n, u.data_ptr(), n) if save else (None, 0, None, 0)))
-    _gated(a, (), device, stream)
+    _gated(a, device, stream)
     return (h, g, u) if save else h
 
 
@@ -227,6 +214,5 @@ def _run_gated_backward(stream, dh, x, w_gate, w_up, g, u, activation, bias, nee
                    *_matrix(u, "u", m, n, x), *((dx.data_ptr(), k) if need_dx else (None, 0)),
                    *((dwg.data_ptr(), k, dwu.data_ptr(), k) if need_dw else (None, 0, None, 0)),
                    *((dbg.data_ptr(), dbu.data_ptr()) if bias else (None, None)))
-    _gated_backward(a, _wanted(dx=need_dx and m > 0, dw_gate=need_dw, dw_up=need_dw, db_gate=bias, db_up=bias), device,
-                    stream)
+    _gated_backward(a, device, stream)
     return dx, dwg, dwu, dbg, dbu
