@@ -59,18 +59,6 @@ __device__ inline float phi_f(float z, float* bell) {
   }
 }
 
-template <int TYPE>
-__device__ inline float act_f(float z, int act) {
-  float bell;
-  switch (act) {
-    case EMB_ACT_RELU: return z < 0.0f ? 0.0f : z;   // NaN passes
-    case EMB_ACT_SIGMOID: return sigmoid_f<TYPE>(z);
-    case EMB_ACT_SILU: return z * sigmoid_f<TYPE>(z);
-    case EMB_ACT_GELU: return z * phi_f<TYPE>(z, &bell);
-    default: return z;
-  }
-}
-
 // dy act'(z); *value = act(z).  The sigmoid's slope is s(z) s(-z), with both from exp(-|z|): 1 - s(z) would
 // lose all its digits where z is large.
 template <int TYPE>
@@ -123,120 +111,15 @@ __device__ inline void act8(float* z, int act) {
   }
 }
 
-// ---------------------------------------------------------------- epilogue
-
-// Stores one element of the result from its sums (s1: the up projection's).
-template <int TYPE, int KIND>
-__device__ inline void finish(const DenseGemm& g, int part, int i, int j, float s0, float s1) {
-  using T = typename Elem<TYPE>::T;
-  if constexpr (KIND == kForward || KIND == kGated) {
-    if (g.bias[0]) s0 += float(static_cast<const T*>(g.bias[0])[j]);
-    if (g.z[0]) static_cast<T*>(g.z[0])[i * g.ldz[0] + j] = T(s0);
-    float y = act_f<TYPE>(s0, g.act);
-    if constexpr (KIND == kGated) {
-      if (g.bias[1]) s1 += float(static_cast<const T*>(g.bias[1])[j]);
-      if (g.z[1]) static_cast<T*>(g.z[1])[i * g.ldz[1] + j] = T(s1);
-      y *= s1;
-    } else if (g.res) {
-      y += float(static_cast<const T*>(g.res)[i * g.ldr + j]);
-    }
-    static_cast<T*>(g.c[0])[i * g.ldc[0] + j] = T(y);
-  } else {
-    static_cast<T*>(g.c[part])[i * g.ldc[part] + j] = T(s0);
-  }
-}
-
-// ---------------------------------------------------------------- matrix products
-
-constexpr int kSM = 64, kSN = 64, kSK = 32, kPad = 8;
-
-// A tile of 64 x 64 results, four wavefronts of 32 x 32 each.
-template <int TYPE, int KIND>
-__global__ __launch_bounds__(256) void dense_tile(DenseGemm g) {
-  using T = typename Elem<TYPE>::T;
-  __shared__ T sa[kSM][kSK + kPad], sb[kSN][kSK + kPad];
-  constexpr bool kGate = KIND == kGated;
-  constexpr int kCols = kGate ? kSN / 2 : kSN;   // result columns of a tile
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int tiles_j = (g.nj + kCols - 1) / kCols;
-  const int i0 = static_cast<int>(blockIdx.x / tiles_j) * kSM, j0 = static_cast<int>(blockIdx.x % tiles_j) * kCols;
-  const int wi = (wave >> 1) * 32, wj = (wave & 1) * 32;
-  const int q = lane >> 4, c = lane & 15;
-  const int bpart = KIND == kWeightGrad ? blockIdx.z : 0;
-  f32x4 acc[2][2] = {};
-  const int parts = KIND == kInputGrad ? g.parts : 1;
-  for (int part = 0; part < parts; ++part) {
-    const T* a = static_cast<const T*>(g.a[KIND == kWeightGrad ? bpart : part]);
-    for (int r0 = 0; r0 < g.nr; r0 += kSK) {
-      __syncthreads();
-      for (int e = tid; e < kSM * kSK; e += 256) {
-        if constexpr (KIND == kWeightGrad) {
-          const int r = e / kSM, i = e % kSM;
-          sa[i][r] = r0 + r < g.nr && i0 + i < g.ni ? a[(r0 + r) * g.lda + i0 + i] : T(0.0f);
-        } else {
-          const int i = e / kSK, r = e % kSK;
-          sa[i][r] = r0 + r < g.nr && i0 + i < g.ni ? a[(i0 + i) * g.lda + r0 + r] : T(0.0f);
-        }
-      }
-      for (int e = tid; e < kSN * kSK; e += 256) {
-        if constexpr (KIND == kForward || KIND == kGated) {
-          const int row = e / kSK, r = e % kSK;
-          const int mat = kGate ? row / kCols : 0, j = row - mat * kCols;
-          const T* b = static_cast<const T*>(g.b[mat]);
-          sb[row][r] = r0 + r < g.nr && j0 + j < g.nj ? b[(j0 + j) * g.ldb[mat] + r0 + r] : T(0.0f);
-        } else {
-          const int r = e / kSN, j = e % kSN;
-          const int mat = KIND == kInputGrad ? part : 0;
-          const T* b = static_cast<const T*>(g.b[mat]);
-          sb[j][r] = r0 + r < g.nr && j0 + j < g.nj ? b[(r0 + r) * g.ldb[mat] + j0 + j] : T(0.0f);
-        }
-      }
-      __syncthreads();
-#pragma unroll
-      for (int fi = 0; fi < 2; ++fi)
-#pragma unroll
-        for (int fj = 0; fj < 2; ++fj) {
-          const T* pa = sa[wi + fi * 16 + c];
-          // gated: a wavefront's first fragment is of the gate, its second of the up projection
-          const T* pb = kGate ? sb[fj * kCols + (wave & 1) * 16 + c] : sb[wj + fj * 16 + c];
-          if constexpr (TYPE == kDenseF32) {
-#pragma unroll
-            for (int s = 0; s < kSK / 4; ++s)
-              acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x4f32(pb[4 * s + q], pa[4 * s + q], acc[fi][fj], 0, 0, 0);
-          } else {
-            using V = typename Elem<TYPE>::V;
-            const V va = *reinterpret_cast<const V*>(pa + 8 * q), vb = *reinterpret_cast<const V*>(pb + 8 * q);
-            if constexpr (TYPE == kDenseF16)
-              acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vb, va, acc[fi][fj], 0, 0, 0);
-            else
-              acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, va, acc[fi][fj], 0, 0, 0);
-          }
-        }
-    }
-  }
-  // lane: result row i = c, columns 4 q .. 4 q + 3 of a fragment
-#pragma unroll
-  for (int fi = 0; fi < 2; ++fi)
-#pragma unroll
-    for (int fj = 0; fj < (kGate ? 1 : 2); ++fj)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int i = i0 + wi + fi * 16 + c;
-        const int j = j0 + (kGate ? (wave & 1) * 16 : wj + fj * 16) + 4 * q + e;
-        if (i < g.ni && j < g.nj) finish<TYPE, KIND>(g, bpart, i, j, acc[fi][fj][e], kGate ? acc[fi][1][e] : 0.0f);
-      }
-}
-
-// ---------------------------------------------------------------- tiles of 16-bit types
+// ---------------------------------------------------------------- tiles
 //
 // A workgroup computes BM x BN sums (kGated: BN / 2 columns of each projection) in WI x WJ
-// wavefronts.  Each step takes kBK of the reduction of both operands from LDS, while later steps are
-// on their way there.  A tile lies in LDS as in memory: rows of kBK elements
-// (operand along the reduction) or kBK rows of BM or BN elements (reduction-major), with the
+// wavefronts.  Each step takes 128 bytes of the reduction (BK elements) of both operands from LDS, while
+// later steps are on their way there.  A tile lies in LDS as in memory: rows of BK elements (operand
+// along the reduction) or BK rows of BM or BN elements (reduction-major), with the
 // 16-byte chunks of a row permuted so that what a wavefront reads at once lies in different
 // banks.  Chunks go from memory to LDS without registers, so their order within a wavefront's
 // 1 KB is fixed in LDS, and the permutation is applied to the address each lane loads from.
-constexpr int kBK = 64;
 constexpr int kOutOfRange = static_cast<int>(0x80000000u);   // past every descriptor: reads zeros
 
 #define LDS_PTR(T) __attribute__((address_space(3))) T*
@@ -283,19 +166,21 @@ __device__ inline f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
 }
 
-// One operand's tile of ROWS results (rows of x or dz, columns of the result) by kBK.
-// RM: reduction-major in memory.
-template <int ROWS, bool RM, int WAVES>
+// One operand's tile of ROWS results (rows of x or dz, columns of the result) by 128 bytes of the reduction: BK elements
+// of ESIZE bytes.  RM: reduction-major in memory.
+template <int ROWS, bool RM, int WAVES, int ESIZE>
 struct Tile {
-  static constexpr int kBytes = ROWS * kBK * 2;
-  static constexpr int kLoads = kBytes / 1024 / WAVES;     // 1 KB pieces a wavefront loads
-  static constexpr int kRowBytes = RM ? ROWS * 2 : kBK * 2;
+  static constexpr int BK = 128 / ESIZE, kPer = 16 / ESIZE;   // elements of a step and of a chunk
+  static constexpr int kBytes = ROWS * 128;
+  static constexpr int kLoads = kBytes / 1024 / WAVES;        // 1 KB pieces a wavefront loads
+  static constexpr int kRowBytes = RM ? ROWS * ESIZE : 128;
   static constexpr int kChunks = kRowBytes / 16;
   static constexpr int kRowsPerLoad = 1024 / kRowBytes;
   static_assert(kBytes % (1024 * WAVES) == 0, "every wavefront loads alike");
 
   // the permutation of a row's chunks
   __device__ static int swizzle(int row) {
+    if (RM && ESIZE == 4) return ((row >> 2) & 3) << 2;
     if (RM) return (kChunks >= 16 ? (row & 3) | ((row >> 1) & 4) : row & 3) << 1;
     return (row >> 1) & 7;
   }
@@ -306,28 +191,28 @@ struct Tile {
 
   int voff[kLoads];
 
-  // rows: valid rows (RM: valid columns, a multiple of 8) from the tile's origin on
+  // rows: valid rows (RM: valid columns, whole chunks) from the tile's origin on
   __device__ void init(int wave, int lane, int64_t ld, int rows) {
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
       const int row = load_row(n, wave, lane), chunk = load_chunk(row, lane);
-      const bool in = RM ? chunk * 8 < rows : row < rows;
-      voff[n] = in ? static_cast<int>(row * ld * 2) + chunk * 16 : kOutOfRange;
+      const bool in = RM ? chunk * kPer < rows : row < rows;
+      voff[n] = in ? static_cast<int>(row * ld * ESIZE) + chunk * 16 : kOutOfRange;
     }
   }
 
-  // valid: how many of this step's kBK are inside
+  // valid: how many of this step's BK are inside
   __device__ void load(i32x4 rsrc, uint32_t lds, int wave, int lane, int valid, int n) const {
     int v = voff[n];
-    if (valid < kBK) {
+    if (valid < BK) {
       const int row = load_row(n, wave, lane), chunk = load_chunk(row, lane);
-      v = (RM ? row < valid : chunk * 8 < valid) ? v : kOutOfRange;
+      v = (RM ? row < valid : chunk * kPer < valid) ? v : kOutOfRange;
     }
     load_to_lds(rsrc, v, lds + (n * WAVES + wave) * 1024);
   }
 
-  // fragment of 16 results (from `first` on, a multiple of 16) by 32 of the reduction (half ks):
-  // lane: result lane % 16, reduction 8 (lane / 16) .. + 7
+  // 16 bits: fragment of 16 results (from `first` on, a multiple of 16) by 32 of the reduction (half ks): lane: result
+  // lane % 16, reduction 8 (lane / 16) .. + 7
   __device__ static s16x8 fragment(const char* tile, int first, int ks, int lane) {
     const int q = lane >> 4, c = lane & 15;
     if constexpr (RM) {
@@ -342,7 +227,68 @@ struct Tile {
       return *reinterpret_cast<const s16x8*>(tile + row * kRowBytes + (((ks * 4 + q) ^ swizzle(row)) << 4));
     }
   }
+
+  // f32: the same fragment's values; lane: reduction 4 (lane / 16) .. + 3 and 16 + 4 (lane / 16) .. + 3
+  __device__ static void fragment(const char* tile, int first, int lane, float* v) {
+    const int q = lane >> 4, c = lane & 15;
+    if constexpr (RM) {
+      const char* p = tile + 4 * q * kRowBytes + ((((first + c) >> 2) ^ (q << 2)) << 4) + (c & 3) * 4;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const float*>(p + ((e & 3) + (e >> 2) * 16) * kRowBytes);
+    } else {
+      const int row = first + c;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(tile + row * kRowBytes + (((h * 4 + q) ^ swizzle(row)) << 4));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[h * 4 + e] = x[e];
+      }
+    }
+  }
 };
+
+// f32 products.  The matrix cores multiply f32 at a sixteenth of their bf16 rate.  So each f32 value is taken as a sum of
+// three bf16 values (the value rounded, the rest rounded, the rest of that: 24 bits in all, exact for magnitudes from
+// 2^-110 on, below which the last part may vanish), and a product as the six of their nine products that count; the other
+// three come to 2^-23 of it at most.  Small ones are added first.  Six bf16 products for each f32 one are 2.7 times less
+// work than f32 products, at f32's accuracy.  Values of 2^128 - 2^119 or more, infinities and NaN cannot be taken apart
+// so: they turn every sum that they reach into NaN, and a tile with sums that are not finite is computed again with f32
+// products (tile_by_f32).
+struct Parts { s16x8 p[3]; };   // high to low
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ inline uint32_t round2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+
+__device__ inline Parts split3(const float* v) {
+  u32x4 part[3];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float a = v[2 * e], b = v[2 * e + 1];
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      part[p][e] = round2(a, b);
+      a -= __builtin_bit_cast(float, part[p][e] << 16), b -= __builtin_bit_cast(float, part[p][e] & 0xffff0000u);
+    }
+  }
+  return {{__builtin_bit_cast(s16x8, part[0]), __builtin_bit_cast(s16x8, part[1]), __builtin_bit_cast(s16x8, part[2])}};
+}
+
+// c[fi][fj] += the products of FI by FJ fragments
+template <int FI, int FJ>
+__device__ inline void products6(const Parts* a, const Parts* b, f32x4 (*c)[FJ]) {
+  constexpr int kA[6] = {2, 0, 1, 1, 0, 0}, kB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+  for (int n = 0; n < 6; ++n)
+#pragma unroll
+    for (int fi = 0; fi < FI; ++fi)
+#pragma unroll
+      for (int fj = 0; fj < FJ; ++fj) c[fi][fj] = mfma16<kDenseBF16>(b[fj].p[kB[n]], a[fi].p[kA[n]], c[fi][fj]);
+}
 
 // Which tile a workgroup computes.  Workgroups go round-robin over the 8 XCDs, each with an L2 of its
 // own: XCD x takes the x-th eighth of the tiles, in bands of kBand tile rows walked column by column,
@@ -436,19 +382,103 @@ __device__ inline void finish8(const DenseGemm& g, int part, int split, int64_t 
   }
 }
 
+// Stores a wavefront's sums, from row i0 and column j0 on, through 16 KB of LDS of its own: 64 x 64 sums at a time, so
+// that a lane has eight consecutive columns and the activation's code is there once.  Lane (q, c) holds row c and
+// columns 4 q .. + 3 of each fragment.  Rows of 256 bytes, their 16-byte chunks permuted by the row.
+template <int TYPE, int KIND, int FI, int FJ>
+__device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char* own, int lane, int64_t i0, int j0, int part,
+                                  int split) {
+  constexpr bool kGate = KIND == kGated;
+  const int q = lane >> 4, c = lane & 15;
+#pragma unroll
+  for (int h = 0; h < FI / 4; ++h) {
+#pragma unroll
+    for (int fi = 0; fi < 4; ++fi)
+#pragma unroll
+      for (int fj = 0; fj < 4; ++fj)
+        *reinterpret_cast<f32x4*>(own + (fi * 16 + c) * 256 + (((fj * 4 + q) ^ c) << 4)) = acc[h * 4 + fi][fj];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    constexpr int kLanes = kGate ? 4 : 8;      // of a row
+#pragma unroll 1
+    for (int row0 = 0; row0 < 64; row0 += 64 / kLanes) {
+      const int row = row0 + lane / kLanes, e = (lane % kLanes) * 2;   // e: the row's first chunk
+      const int64_t i = i0 + h * 64 + row;
+      const int j = j0 + e * 4;
+      float s0[8], s1[8];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(own + row * 256 + (((e + x) ^ (row & 15)) << 4));
+        s0[4 * x] = v[0], s0[4 * x + 1] = v[1], s0[4 * x + 2] = v[2], s0[4 * x + 3] = v[3];
+        if constexpr (kGate) {
+          const f32x4 w = *reinterpret_cast<const f32x4*>(own + row * 256 + (((8 + e + x) ^ (row & 15)) << 4));
+          s1[4 * x] = w[0], s1[4 * x + 1] = w[1], s1[4 * x + 2] = w[2], s1[4 * x + 3] = w[3];
+        }
+      }
+      if (i < g.ni && j < g.nj) finish8<TYPE, KIND>(g, part, split, i, j, s0, s1);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+}
+
+// A tile of BM x BN with f32 products: right for every value, and slow.
+template <int KIND, int BM, int BN, int WJ, int WAVES, int FI, int FJ>
+__device__ __noinline__ void tile_by_f32(const DenseGemm& g, char* lds, int i0, int j0, int wi, int wj, int begin, int end,
+                                         int per_part, int wpart, int split) {
+  constexpr bool kGate = KIND == kGated, kRm = KIND == kInputGrad || KIND == kWeightGrad;
+  constexpr int BK = 32, kRow = BK + 1, kCols = kGate ? BN / 2 : BN, kThreads = 64 * WAVES;
+  f32x4 acc[FI][FJ] = {};
+  float* sa = reinterpret_cast<float*>(lds);
+  float* sb = sa + BM * kRow;
+  const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
+  for (int step = begin; step < end; ++step) {
+    const int part = KIND == kInputGrad && step >= per_part ? 1 : 0;
+    const int r0 = (step - part * per_part) * BK;
+    const float* a = static_cast<const float*>(g.a[KIND == kWeightGrad ? wpart : part]);
+    __syncthreads();
+    for (int e = tid; e < BM * BK; e += kThreads) {
+      const int i = KIND == kWeightGrad ? e % BM : e / BK, r = KIND == kWeightGrad ? e / BM : e % BK;
+      const int64_t at = KIND == kWeightGrad ? (r0 + r) * g.lda + i0 + i : (i0 + i) * g.lda + r0 + r;
+      sa[i * kRow + r] = r0 + r < g.nr && i0 + i < g.ni ? a[at] : 0.0f;
+    }
+    for (int e = tid; e < BN * BK; e += kThreads) {
+      const int row = kRm ? e % BN : e / BK, r = kRm ? e / BN : e % BK;
+      const int mat = kGate ? row / kCols : part, j = kGate ? row % kCols : row;
+      const float* b = static_cast<const float*>(g.b[mat]);
+      const int64_t at = kRm ? (r0 + r) * g.ldb[mat] + j0 + j : (j0 + j) * g.ldb[mat] + r0 + r;
+      sb[row * kRow + r] = r0 + r < g.nr && j0 + j < g.nj ? b[at] : 0.0f;
+    }
+    __syncthreads();
+    for (int s = 0; s < BK; s += 4) {
+#pragma unroll
+      for (int fi = 0; fi < FI; ++fi)
+#pragma unroll
+        for (int fj = 0; fj < FJ; ++fj) {
+          const int row = kGate ? (fj / (FJ / 2)) * kCols + wj + (fj % (FJ / 2)) * 16 + c : wj + fj * 16 + c;
+          acc[fi][fj] = __builtin_amdgcn_mfma_f32_16x16x4f32(sb[row * kRow + s + q], sa[(wi + fi * 16 + c) * kRow + s + q],
+                                                             acc[fi][fj], 0, 0, 0);
+        }
+    }
+  }
+  __syncthreads();
+  store_sums<kDenseF32, KIND, FI, FJ>(g, acc, lds + (tid >> 6) * 16384, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
+}
+
 template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
-__global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile16(DenseGemm g) {
+__global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile(DenseGemm g) {
   constexpr bool kGate = KIND == kGated;
   constexpr bool kRmA = KIND == kWeightGrad, kRmB = KIND == kWeightGrad || KIND == kInputGrad;
   constexpr int kWaves = WI * WJ;
-  constexpr bool kTurns = kWaves == 8;                     // see the main loop
+  constexpr bool kTurns = kWaves == 8;                     // see the main loop (16 bits only)
   constexpr int kSlotsA = kTurns ? 3 : 2, kSlotsB = 2;     // tiles of steps in LDS
   constexpr int kCols = kGate ? BN / 2 : BN;               // result columns of a tile
   constexpr int kWI = BM / WI, kWJ = kCols / WJ;           // results of a wavefront
   constexpr int kFI = kWI / 16, kFJ = BN / WJ / 16;        // its fragments
-  using TileA = Tile<BM, kRmA, kWaves>;
-  using TileB = Tile<BN, kRmB, kWaves>;
-  using TileH = Tile<kCols, kRmB, kWaves>;                // one projection's half of B
+  constexpr bool kF32 = TYPE == kDenseF32;
+  constexpr int kSize = kF32 ? 4 : 2;
+  using TileA = Tile<BM, kRmA, kWaves, kSize>;
+  using TileB = Tile<BN, kRmB, kWaves, kSize>;
+  using TileH = Tile<kCols, kRmB, kWaves, kSize>;          // one projection's half of B
+  constexpr int BK = TileA::BK;
   constexpr int kStages = kSlotsA * TileA::kBytes + kSlotsB * TileB::kBytes;
   constexpr int kLds = kStages > kWaves * 16384 ? kStages : kWaves * 16384;   // (16 KB: epilogue)
   __shared__ __align__(1024) char lds[kLds];
@@ -458,7 +488,7 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
   tile_of(blockIdx.x, (g.ni + BM - 1) / BM, (g.nj + kCols - 1) / kCols, &ti, &tj);
   const int i0 = ti * BM, j0 = tj * kCols;
   const int split = blockIdx.y, wpart = KIND == kWeightGrad ? blockIdx.z : 0;
-  const int per_part = (g.nr + kBK - 1) / kBK;
+  const int per_part = (g.nr + BK - 1) / BK;
   const int steps = per_part * (KIND == kInputGrad ? g.parts : 1);
   const int begin = static_cast<int>(int64_t(steps) * split / g.splits);
   const int end = static_cast<int>(int64_t(steps) * (split + 1) / g.splits);
@@ -485,19 +515,19 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
   struct Next { i32x4 a, b0, b1; int valid_a, valid_b; uint32_t at_a, at_b; } next;
   auto set_a = [&](int step, int slot) {
     const int part = KIND == kInputGrad && step >= per_part && g.parts > 1 ? 1 : 0;
-    const int r0 = (step - part * per_part) * kBK;
+    const int r0 = (step - part * per_part) * BK;
     next.valid_a = step < end ? g.nr - r0 : 0;
     const char* a = static_cast<const char*>(g.a[KIND == kWeightGrad ? wpart : part]);
-    next.a = descriptor(a + (kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0) * 2);
+    next.a = descriptor(a + (kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0) * kSize);
     next.at_a = lds0 + slot * TileA::kBytes;
   };
   auto set_b = [&](int step, int slot) {
     const int part = KIND == kInputGrad && step >= per_part && g.parts > 1 ? 1 : 0;
-    const int r0 = (step - part * per_part) * kBK;
+    const int r0 = (step - part * per_part) * BK;
     next.valid_b = step < end ? g.nr - r0 : 0;
     const char* b = static_cast<const char*>(g.b[part]);
-    next.b0 = descriptor(b + (kRmB ? int64_t(r0) * g.ldb[part] + j0 : int64_t(j0) * g.ldb[part] + r0) * 2);
-    if constexpr (kGate) next.b1 = descriptor(static_cast<const char*>(g.b[1]) + (int64_t(j0) * g.ldb[1] + r0) * 2);
+    next.b0 = descriptor(b + (kRmB ? int64_t(r0) * g.ldb[part] + j0 : int64_t(j0) * g.ldb[part] + r0) * kSize);
+    if constexpr (kGate) next.b1 = descriptor(static_cast<const char*>(g.b[1]) + (int64_t(j0) * g.ldb[1] + r0) * kSize);
     if constexpr (KIND == kInputGrad) {
       if (part != tb_part) {
         tb.init(wave, lane, g.ldb[part], g.nj - j0);
@@ -522,6 +552,7 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
 
   const int wi = (wave / WJ) * kWI, wj = (wave % WJ) * kWJ;
   f32x4 acc[kFI][kFJ] = {};
+  // fragments of a half step (16 bits), or values of a step's (f32)
   auto fragments_a = [&](const char* sa, int ks, s16x8* f) {
 #pragma unroll
     for (int n = 0; n < kFI; ++n) f[n] = TileA::fragment(sa, wi + n * 16, ks, lane);
@@ -534,6 +565,11 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
       else
         f[n] = TileB::fragment(sb, wj + n * 16, ks, lane);
     }
+  };
+  auto value_a = [&](const char* sa, int n, float* v) { TileA::fragment(sa, wi + n * 16, lane, v); };
+  auto value_b = [&](const char* sb, int n, float* v) {
+    if constexpr (kGate) TileH::fragment(sb + (n >= kFJ / 2) * TileH::kBytes, wj + (n % (kFJ / 2)) * 16, lane, v);
+    else TileB::fragment(sb, wj + n * 16, lane, v);
   };
   int at_a = 0, at_b = 0;   // slots of the step that is multiplied
   if constexpr (!kTurns) {
@@ -551,15 +587,40 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
       set_b(step + 1, at_a);
 #pragma unroll
       for (int n = 0; n < kIssues; ++n) issue(n);
+      if constexpr (kF32) {
+        Parts fa[2][2], fb[kFJ];
+        auto part_a = [&](int n, Parts* f) {
+          float v[8];
+          value_a(sa, n, v);
+          *f = split3(v);
+        };
 #pragma unroll
-      for (int ks = 0; ks < kBK / 32; ++ks) {
-        s16x8 fa[kFI], fb[kFJ];
-        fragments_b(sb, ks, fb);
-        fragments_a(sa, ks, fa);
+        for (int n = 0; n < kFJ; ++n) {
+          float v[8];
+          value_b(sb, n, v);
+          fb[n] = split3(v);
+        }
+        part_a(0, &fa[0][0]);
+        part_a(1, &fa[0][1]);
 #pragma unroll
-        for (int fi = 0; fi < kFI; ++fi)
+        for (int h = 0; h < kFI; h += 2) {
+          if (h + 2 < kFI) {
+            part_a(h + 2, &fa[(h / 2 + 1) & 1][0]);
+            part_a(h + 3, &fa[(h / 2 + 1) & 1][1]);
+          }
+          products6<2, kFJ>(fa[(h / 2) & 1], fb, acc + h);
+        }
+      } else {
 #pragma unroll
-          for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[fj], fa[fi], acc[fi][fj]);
+        for (int ks = 0; ks < BK / 32; ++ks) {
+          s16x8 fa[kFI], fb[kFJ];
+          fragments_b(sb, ks, fb);
+          fragments_a(sa, ks, fa);
+#pragma unroll
+          for (int fi = 0; fi < kFI; ++fi)
+#pragma unroll
+            for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[fj], fa[fi], acc[fi][fj]);
+        }
       }
     }
   } else {
@@ -570,16 +631,6 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
     // have read it.
     constexpr int kUnderWay = TileA::kLoads;
     const bool late = wave >= 4;
-    s16x8 fa[kBK / 32][kFI], fb[kBK / 32][kFJ];
-    auto read = [&]() {
-      const char* sa = lds + at_a * TileA::kBytes;
-      const char* sb = lds + kAreaB + at_b * TileB::kBytes;
-#pragma unroll
-      for (int ks = 0; ks < kBK / 32; ++ks) {
-        fragments_b(sb, ks, fb[ks]);
-        fragments_a(sa, ks, fa[ks]);
-      }
-    };
     auto after = [](int slot) { return slot == 2 ? 0 : slot + 1; };
     set_a(begin, 0);
     set_b(begin, 0);
@@ -589,6 +640,16 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
 #pragma unroll
     for (int n = 0; n < TileA::kLoads; ++n) issue_a(n);
     stage_done<kUnderWay>();
+    s16x8 fa[BK / 32][kFI], fb[BK / 32][kFJ];
+    auto read = [&]() {
+      const char* sa = lds + at_a * TileA::kBytes;
+      const char* sb = lds + kAreaB + at_b * TileB::kBytes;
+#pragma unroll
+      for (int ks = 0; ks < BK / 32; ++ks) {
+        fragments_b(sb, ks, fb[ks]);
+        fragments_a(sa, ks, fa[ks]);
+      }
+    };
     if (!late) {
       for (int step = begin; step < end; ++step) {
         read();
@@ -603,7 +664,7 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int ks = 0; ks < kBK / 32; ++ks)
+        for (int ks = 0; ks < BK / 32; ++ks)
 #pragma unroll
           for (int fi = 0; fi < kFI; ++fi)
 #pragma unroll
@@ -630,7 +691,7 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int ks = 0; ks < kBK / 32; ++ks)
+        for (int ks = 0; ks < BK / 32; ++ks)
 #pragma unroll
           for (int fi = 0; fi < kFI; ++fi) {
 #pragma unroll
@@ -645,44 +706,28 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
     }
   }
 
-  // Results through LDS, 64 x 64 sums of a wavefront at a time, so that a lane has eight consecutive
-  // columns and the activation's code is there once: lane (q, c) has rows c and columns 4 q .. + 3 of
-  // each fragment.  Rows of 256 bytes, their 16-byte chunks permuted by the row.
   stage_done<0>();
-  char* own = lds + wave * 16384;
-  const int q = lane >> 4, c = lane & 15;
+  if constexpr (kF32) {
+    uint32_t largest = 0;
 #pragma unroll
-  for (int h = 0; h < (kFI / 4) * (kFJ / 4); ++h) {
-    const int hi = h / (kFJ / 4), hj = h % (kFJ / 4);
+    for (int fi = 0; fi < kFI; ++fi)
 #pragma unroll
-    for (int fi = 0; fi < 4; ++fi)
+      for (int fj = 0; fj < kFJ; ++fj)
 #pragma unroll
-      for (int fj = 0; fj < 4; ++fj) {
-        // kGated: two fragments of the gate, two of the up projection
-        const int f = kGate ? (fj / 2) * (kFJ / 2) + hj * 2 + fj % 2 : hj * 4 + fj;
-        *reinterpret_cast<f32x4*>(own + (fi * 16 + c) * 256 + (((fj * 4 + q) ^ c) << 4)) = acc[hi * 4 + fi][f];
-      }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    constexpr int kLanes = kGate ? 4 : 8;      // of a row
-#pragma unroll 1
-    for (int row0 = 0; row0 < 64; row0 += 64 / kLanes) {
-      const int row = row0 + lane / kLanes, e = (lane % kLanes) * 2;   // e: the row's first chunk
-      const int64_t i = i0 + wi + hi * 64 + row;
-      const int j = j0 + wj + hj * (kGate ? 32 : 64) + e * 4;
-      float s0[8], s1[8];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(own + row * 256 + (((e + x) ^ (row & 15)) << 4));
-        s0[4 * x] = v[0], s0[4 * x + 1] = v[1], s0[4 * x + 2] = v[2], s0[4 * x + 3] = v[3];
-        if constexpr (kGate) {
-          const f32x4 w = *reinterpret_cast<const f32x4*>(own + row * 256 + (((8 + e + x) ^ (row & 15)) << 4));
-          s1[4 * x] = w[0], s1[4 * x + 1] = w[1], s1[4 * x + 2] = w[2], s1[4 * x + 3] = w[3];
-        }
-      }
-      if (i < g.ni && j < g.nj) finish8<TYPE, KIND>(g, wpart, split, i, j, s0, s1);
+        for (int e = 0; e < 4; ++e) largest = max(largest, __float_as_uint(acc[fi][fj][e]) << 1);
+    int* redo = reinterpret_cast<int*>(lds);
+    if (tid == 0) *redo = 0;
+    __syncthreads();
+    if (largest >= 0xff000000u) *redo = 1;   // an infinity or NaN
+    __syncthreads();
+    const int again = __builtin_amdgcn_readfirstlane(*redo);
+    __syncthreads();
+    if (again) {
+      tile_by_f32<KIND, BM, BN, WJ, kWaves, kFI, kFJ>(g, lds, i0, j0, wi, wj, begin, end, per_part, wpart, split);
+      return;
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
+  store_sums<TYPE, KIND, kFI, kFJ>(g, acc, lds + wave * 16384, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
 }
 
 // Results of a product whose reduction was split: the splits' sums are added in order.  A thread has eight columns.
@@ -827,37 +872,29 @@ __global__ __launch_bounds__(256) void dense_colsum(DenseColsum s) {
 // Copies up to three matrices to rows that start at multiples of 16 bytes and end in zeros up to a whole chunk: the
 // tiles above read nothing else.  A wavefront takes 64 consecutive elements at a time, as rows that start anywhere
 // are read fastest (16-byte loads at odd addresses measured 1.1 TB/s).
+template <class E>
 __global__ __launch_bounds__(256) void dense_pack(DensePack p) {
   const int mat = blockIdx.y;
-  const uint32_t cols = p.cols[mat], padded = (cols + 7) / 8 * 8;
+  const uint32_t cols = p.cols[mat], padded = static_cast<uint32_t>(p.ldd[mat]);
   const uint32_t rows = p.rows[mat];
-  const uint16_t* src = static_cast<const uint16_t*>(p.src[mat]);
-  uint16_t* dst = static_cast<uint16_t*>(p.dst[mat]);
+  const E* src = static_cast<const E*>(p.src[mat]);
+  E* dst = static_cast<E*>(p.dst[mat]);
   // as many rows side by side as 256 threads hold
   const uint32_t wide = p.wide[mat], x = threadIdx.x % wide, y = threadIdx.x / wide, side = 256 / wide;
   for (uint64_t i = uint64_t(blockIdx.x) * side + y; i < rows; i += uint64_t(gridDim.x) * side)
 #pragma unroll 4
     for (uint32_t j = x; j < padded; j += wide) {
-      const uint16_t v = src[i * p.lds[mat] + min(j, cols - 1)];
+      const E v = src[i * p.lds[mat] + min(j, cols - 1)];
       dst[i * p.ldd[mat] + j] = j < cols ? v : 0;
     }
 }
 
-template <int TYPE, int KIND>
-int simple_launch(const DenseGemm& g, hipStream_t stream) {
-  const int cols = KIND == kGated ? kSN / 2 : kSN;
-  const int64_t tiles = int64_t((g.ni + kSM - 1) / kSM) * ((g.nj + cols - 1) / cols);
-  const dim3 grid(static_cast<uint32_t>(tiles), 1, KIND == kWeightGrad ? g.parts : 1);
-  dense_tile<TYPE, KIND><<<grid, 256, 0, stream>>>(g);
-  return hipGetLastError();
-}
-
 template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
-int tile16_launch(const DenseGemm& g, hipStream_t stream) {
+int tile_launch(const DenseGemm& g, hipStream_t stream) {
   const int cols = KIND == kGated ? BN / 2 : BN;
   const int64_t tiles = int64_t((g.ni + BM - 1) / BM) * ((g.nj + cols - 1) / cols);
   const dim3 grid(static_cast<uint32_t>(tiles), g.splits, KIND == kWeightGrad ? g.parts : 1);
-  dense_tile16<TYPE, KIND, BM, BN, WI, WJ, PER_CU><<<grid, 64 * WI * WJ, 0, stream>>>(g);
+  dense_tile<TYPE, KIND, BM, BN, WI, WJ, PER_CU><<<grid, 64 * WI * WJ, 0, stream>>>(g);
   return hipGetLastError();
 }
 
@@ -871,19 +908,16 @@ int join_launch(const DenseGemm& g, hipStream_t stream) {
 
 template <int TYPE, int KIND>
 int kind_launch(const DenseGemm& g, hipStream_t stream) {
-  if constexpr (TYPE != kDenseF32) {
-    if (g.variant == kTile256) return tile16_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
-    return tile16_launch<TYPE, KIND, 128, 128, 2, 2, 2>(g, stream);
-  }
-  return simple_launch<TYPE, KIND>(g, stream);
+  if constexpr (TYPE != kDenseF32)
+    if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
+  return tile_launch<TYPE, KIND, 128, 128, 2, 2, 2>(g, stream);
 }
 
 template <int TYPE, int KIND>
 int product_launch(const DenseGemm& g, hipStream_t stream) {
   const int rc = kind_launch<TYPE, KIND>(g, stream);
   if (rc != 0 || g.splits == 1) return rc;
-  if constexpr (TYPE != kDenseF32) return join_launch<TYPE, KIND>(g, stream);
-  return rc;
+  return join_launch<TYPE, KIND>(g, stream);
 }
 
 template <int TYPE>
@@ -928,7 +962,9 @@ int colsum_launch(const DenseColsum& s, hipStream_t stream) {
 
 #if EMBX_HAS_DPART(0)
 int dense_pack_launch(const DensePack& p, void* stream) {
-  dense_pack<<<dim3(p.groups, p.count), 256, 0, static_cast<hipStream_t>(stream)>>>(p);
+  const dim3 grid(p.groups, p.count);
+  if (p.esize == 4) dense_pack<uint32_t><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(p);
+  else dense_pack<uint16_t><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(p);
   return hipGetLastError();
 }
 #endif

@@ -18,7 +18,7 @@ enum DenseKind {
   kWeightGrad = 3    // C[i][j] = sum_r A[r][i] B[r][j]   A = dz, B = x       (R, R)
 };
 
-enum DenseVariant { kSimple = 0, kTile128 = 1, kTile256 = 2 };
+enum DenseVariant { kTile128 = 0, kTile256 = 1 };
 
 // One matrix product.  Arrays of two: kGated's two weights and results; kInputGrad's two
 // products summed into one result (parts = 2); kWeightGrad's two results (parts = 2).
@@ -48,13 +48,13 @@ struct DenseSlope {
   int32_t whole;           // rows of all operands start at multiples of 16 bytes and hold whole eights
 };
 
-// matrices of 16-bit elements copied to rows of whole 16-byte chunks
+// matrices copied to rows of whole 16-byte chunks
 struct DensePack {
   const void* src[3];
   void* dst[3];
   int64_t lds[3], ldd[3];
   uint32_t rows[3], cols[3], wide[3];
-  int32_t count, groups;
+  int32_t count, groups, esize;
 };
 
 // column sums from those of blocks of rows

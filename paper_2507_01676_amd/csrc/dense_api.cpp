@@ -58,10 +58,13 @@ emb_status_t check_workspace(const void* ws, size_t have, size_t need) {
 
 emb_status_t run(int rc) { return rc == 0 ? EMB_OK : EMB_ERR_DEVICE; }
 
-// Whether the tiles of 16-bit types can read a matrix where it lies: rows that start at multiples of 16 bytes and
-// hold whole chunks of eight elements (and a tile's offsets, 256 rows at most, fit 32 bits).
-bool whole(const void* p, int64_t ld, int64_t cols) {
-  return !misaligned(p, 16) && ld % 8 == 0 && cols % 8 == 0 && ld <= (int64_t(1) << 22);
+int64_t chunk(int32_t dtype) { return 16 / static_cast<int64_t>(esize(dtype)); }   // elements of 16 bytes
+
+// Whether the products can read a matrix where it lies: rows that start at multiples of 16 bytes and hold whole
+// chunks of 16 bytes (and a tile's offsets, 256 rows at most, fit 32 bits).
+bool whole(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
+  return !misaligned(p, 16) && ld % chunk(dtype) == 0 && cols % chunk(dtype) == 0 &&
+         ld * static_cast<int64_t>(esize(dtype)) <= (int64_t(1) << 23);
 }
 
 // the same for the elementwise passes, of every type
@@ -73,39 +76,42 @@ bool whole16(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
 struct Choice { int32_t variant, splits; };
 
 constexpr int kCus = 256;
-constexpr int kStep = 64;   // of the reduction
 
-// Microseconds of a product by tiles of 256 x 256 or 128 x 128 over `steps` steps, split s ways.  Measured on bf16
-// products of 256 to 8192 rows: a step of the large tile takes 0.97 us on a GPU that is otherwise idle and 1.50 us
-// with a workgroup on every CU (the clock drops, and L2 is shared); one of the small tile 0.62 us alone on its CU, 1.03
-// us where two share it.  A round starts and ends in 3 us.  Split products write their sums and read them back.
-double tile_us(int variant, double tiles, int steps, int s, double result_bytes) {
+// Microseconds of a product by tiles of 256 x 256 or 128 x 128 over `steps` steps of 128 bytes, split s ways.  Measured
+// on bf16 products of 256 to 8192 rows: a step of the large tile takes 0.97 us on a GPU that is otherwise idle and
+// 1.50 us with a workgroup on every CU (the clock drops, and L2 is shared); one of the small tile 0.62 us alone on its
+// CU, 1.03 us where two share it (f32: 1.6 and 2.7 us).  A round starts and ends in 3 us.  Split products write their
+// sums and read them back.
+double tile_us(int32_t dtype, int variant, double tiles, int steps, int s, double result_bytes) {
   const double groups = tiles * s, each = (steps + s - 1) / s;
   double us;
   if (variant == kTile256) {
-    const double rounds = std::ceil(groups / kCus);
-    us = rounds * (each * (0.97 + 0.53 * std::min(1.0, groups / kCus)) + 3.0);
+    us = std::ceil(groups / kCus) * (each * (0.97 + 0.53 * std::min(1.0, groups / kCus)) + 3.0);
   } else {
+    const bool f32 = dtype == EMB_DTYPE_F32;
+    const double alone = f32 ? 1.6 : 0.62, shared = f32 ? 2.7 : 1.03;
     const double whole = std::floor(groups / (2 * kCus)), rest = groups - whole * 2 * kCus;
-    us = whole * (each * 1.03 + 3.0);
-    if (rest > 0) us += each * (rest <= kCus ? 0.62 + 0.1 * rest / kCus : 1.03) + 3.0;
+    us = whole * (each * shared + 3.0);
+    if (rest > 0) us += each * (rest <= kCus ? alone : shared) + 3.0;
   }
   if (s > 1) us += 3.0 + result_bytes * s / 2.0e6;
   return us;
 }
 
-Choice choose(int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
-  const int64_t steps = (nr + kStep - 1) / kStep * (kind == kInputGrad ? parts : 1);
+Choice choose(int32_t dtype, int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
+  const int step = dtype == EMB_DTYPE_F32 ? 32 : 64;   // of the reduction
+  const int64_t steps = (nr + step - 1) / step * (kind == kInputGrad ? parts : 1);
   const int results = kind == kWeightGrad ? parts : kind == kGated ? 2 : 1;
   const double result_bytes = 4.0 * ni * nj * results;
   Choice best = {kTile128, 1};
   double least = 0.0;
-  for (int variant = kTile256; variant >= kTile128; --variant) {
+  for (int variant : {kTile256, kTile128}) {
+    if (variant == kTile256 && dtype == EMB_DTYPE_F32) continue;
     const int64_t side = variant == kTile256 ? 256 : 128;
     const double tiles = double((ni + side - 1) / side) * ((nj * (kind == kGated ? 2 : 1) + side - 1) / side) *
                          (kind == kWeightGrad ? parts : 1);
     for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= (256 << 20))); ++s) {
-      const double us = tile_us(variant, tiles, static_cast<int>(std::min<int64_t>(steps, 1 << 30)), s, result_bytes);
+      const double us = tile_us(dtype, variant, tiles, static_cast<int>(std::min<int64_t>(steps, 1 << 30)), s, result_bytes);
       if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, s};
     }
   }
@@ -114,20 +120,16 @@ Choice choose(int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
 
 // bytes of partial sums of a product
 size_t partial_bytes(int32_t dtype, int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
-  if (dtype == EMB_DTYPE_F32) return 0;
   const int results = kind == kWeightGrad ? parts : kind == kGated ? 2 : 1;
-  const int s = choose(kind, ni, nj, nr, parts).splits;
+  const int s = choose(dtype, kind, ni, nj, nr, parts).splits;
   return s > 1 ? size_t(s) * ni * ((nj + 7) / 8 * 8) * results * 4 : 0;   // (rows of whole eights)
 }
 
 emb_status_t gemm(int32_t dtype, int kind, const DenseGemm& given, float* partial, void* stream) {
   DenseGemm g = given;
-  g.splits = 1;
   g.partial = partial;
-  if (dtype != EMB_DTYPE_F32) {
-    const Choice c = choose(kind, g.ni, g.nj, g.nr, g.parts);
-    g.variant = c.variant, g.splits = c.splits;
-  }
+  const Choice c = choose(dtype, kind, g.ni, g.nj, g.nr, g.parts);
+  g.variant = c.variant, g.splits = c.splits;
   switch (dtype) {
     case EMB_DTYPE_F32: return run(dense_gemm_f32(kind, g, stream));
     case EMB_DTYPE_F16: return run(dense_gemm_f16(kind, g, stream));
@@ -175,11 +177,12 @@ struct Packer {
   int32_t dtype;
   DensePack pack = {};
   Operand use(const void* p, int64_t ld, int64_t rows, int64_t cols) {
-    if (dtype == EMB_DTYPE_F32 || rows == 0 || whole(p, ld, cols)) return {p, ld};
-    const int64_t ldd = (cols + 7) / 8 * 8;
+    if (rows == 0 || whole(p, ld, cols, dtype)) return {p, ld};
+    const int64_t ldd = (cols + chunk(dtype) - 1) / chunk(dtype) * chunk(dtype);
+    pack.esize = static_cast<int32_t>(esize(dtype));
     const int at = pack.count++;
     pack.src[at] = p, pack.lds[at] = ld;
-    pack.dst[at] = ar.take<void>(rows * ldd * 2), pack.ldd[at] = ldd;
+    pack.dst[at] = ar.take<void>(rows * ldd * esize(dtype)), pack.ldd[at] = ldd;
     pack.rows[at] = static_cast<uint32_t>(rows), pack.cols[at] = static_cast<uint32_t>(cols);
     uint32_t wide = 8;
     while (wide < 256 && wide < ldd) wide *= 2;
