@@ -2,6 +2,8 @@
 // feed-forward blocks, forward and backward.  See include/embx_dense.h for the formulas.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "../../include/embx_dense.h"
 #include "dense.hpp"
 
@@ -93,7 +95,7 @@ __device__ inline void act8(float* z, int act) {
   switch (act) {
     case EMB_ACT_RELU:
 #pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = z[e] < 0.0f ? 0.0f : z[e];
+      for (int e = 0; e < 8; ++e) z[e] = __builtin_elementwise_maximum(z[e], 0.0f);   // NaN passes
       break;
     case EMB_ACT_SIGMOID:
 #pragma unroll
@@ -337,50 +339,78 @@ __device__ inline void store8(void* p, int n, const float* v) {
   }
 }
 
-// Eight sums of a row become results.
-template <int TYPE, int KIND, bool JOINED = false>
-__device__ inline void finish8(const DenseGemm& g, int part, int split, int64_t i, int j, float* s0, float* s1) {
+// Turns sums into results: eight consecutive columns, from j on, of a lane's rows, which are `step` rows apart.  What does
+// not change from row to row is worked out once: of products with short sums the epilogue's instructions are a good part.
+template <int TYPE, int KIND>
+struct Finish {
   using T = typename Elem<TYPE>::T;
-  const int n = min(8, g.nj - j);
-  if (!JOINED && g.splits > 1) {
-    constexpr int kMats = KIND == kGated ? 2 : 1;
-    for (int mat = 0; mat < kMats; ++mat) {
-      // rows of partial sums are padded to whole eights
-      float* p = g.partial + ((int64_t(kMats == 2 ? mat : part) * g.splits + split) * g.ni + i) * ((g.nj + 7) / 8 * 8) + j;
-      const float* s = mat ? s1 : s0;
-      reinterpret_cast<f32x4*>(p)[0] = f32x4{s[0], s[1], s[2], s[3]};
-      reinterpret_cast<f32x4*>(p)[1] = f32x4{s[4], s[5], s[6], s[7]};
-    }
-    return;
-  }
-  if constexpr (KIND == kForward || KIND == kGated) {
-    float b[8];
-    if (g.bias[0]) {
-      load8<TYPE>(static_cast<const T*>(g.bias[0]) + j, n, b);
+  static constexpr bool kFwd = KIND == kForward || KIND == kGated;
+  static constexpr int kMats = KIND == kGated ? 2 : 1;
+  T* y;
+  T* z[kMats];
+  const T* r;
+  int64_t y_step, z_step[kMats], r_step;
+  float bias[kMats][8];
+  int n, act;
+  bool has_z[kMats], has_r, has_bias;
+
+  __device__ Finish(const DenseGemm& g, int part, int64_t i, int j, int step) : n(min(8, g.nj - j)), act(g.act) {
+    const int at = kFwd ? 0 : part;
+    y = static_cast<T*>(g.c[at]) + i * g.ldc[at] + j;
+    y_step = step * g.ldc[at];
+    if constexpr (kFwd) {
+      has_bias = g.bias[0] || (kMats == 2 && g.bias[1]);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s0[e] += b[e];
-    }
-    if (g.z[0]) store8<TYPE>(static_cast<T*>(g.z[0]) + i * g.ldz[0] + j, n, s0);
-    act8<TYPE>(s0, g.act);
-    if constexpr (KIND == kGated) {
-      if (g.bias[1]) {
-        load8<TYPE>(static_cast<const T*>(g.bias[1]) + j, n, b);
+      for (int m = 0; m < kMats; ++m) {
+        has_z[m] = g.z[m];
+        z[m] = static_cast<T*>(g.z[m]) + i * g.ldz[m] + j;
+        z_step[m] = step * g.ldz[m];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s1[e] += b[e];
+        for (int e = 0; e < 8; ++e) bias[m][e] = 0.0f;
+        if (g.bias[m] && n > 0) load8<TYPE>(static_cast<const T*>(g.bias[m]) + j, n, bias[m]);
       }
-      if (g.z[1]) store8<TYPE>(static_cast<T*>(g.z[1]) + i * g.ldz[1] + j, n, s1);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s0[e] *= s1[e];
-    } else if (g.res) {
-      load8<TYPE>(static_cast<const T*>(g.res) + i * g.ldr + j, n, b);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) s0[e] += b[e];
+      has_r = KIND == kForward && g.res;
+      r = static_cast<const T*>(g.res) + i * g.ldr + j;
+      r_step = step * g.ldr;
     }
-    store8<TYPE>(static_cast<T*>(g.c[0]) + i * g.ldc[0] + j, n, s0);
-  } else {
-    store8<TYPE>(static_cast<T*>(g.c[part]) + i * g.ldc[part] + j, n, s0);
   }
-}
+
+  __device__ void next() {
+    y += y_step;
+    if constexpr (kFwd) {
+#pragma unroll
+      for (int m = 0; m < kMats; ++m) z[m] += z_step[m];
+      r += r_step;
+    }
+  }
+
+  // of a row that is inside (n >= 1)
+  __device__ void put(float* s0, float* s1) const {
+    if constexpr (kFwd) {
+      if (has_bias) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s0[e] += bias[0][e];
+      }
+      if (has_z[0]) store8<TYPE>(z[0], n, s0);
+      act8<TYPE>(s0, act);
+      if constexpr (KIND == kGated) {
+        if (has_bias) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) s1[e] += bias[1][e];
+        }
+        if (has_z[1]) store8<TYPE>(z[1], n, s1);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s0[e] *= s1[e];
+      } else if (has_r) {
+        float b[8];
+        load8<TYPE>(r, n, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s0[e] += b[e];
+      }
+    }
+    store8<TYPE>(y, n, s0);
+  }
+};
 
 // Stores a wavefront's sums, from row i0 and column j0 on, through 16 KB of LDS of its own: 64 x 64 sums at a time, so
 // that a lane has eight consecutive columns and the activation's code is there once.  Lane (q, c) holds row c and
@@ -398,13 +428,10 @@ __device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char
       for (int fj = 0; fj < 4; ++fj)
         *reinterpret_cast<f32x4*>(own + (fi * 16 + c) * 256 + (((fj * 4 + q) ^ c) << 4)) = acc[h * 4 + fi][fj];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    constexpr int kLanes = kGate ? 4 : 8;      // of a row
-#pragma unroll 1
-    for (int row0 = 0; row0 < 64; row0 += 64 / kLanes) {
-      const int row = row0 + lane / kLanes, e = (lane % kLanes) * 2;   // e: the row's first chunk
-      const int64_t i = i0 + h * 64 + row;
-      const int j = j0 + e * 4;
-      float s0[8], s1[8];
+    constexpr int kLanes = kGate ? 4 : 8, kRows = 64 / kLanes;   // lanes of a row, rows at a time
+    const int e = lane % kLanes * 2, j = j0 + e * 4;             // the row's first chunk of this lane
+    const int64_t first = i0 + h * 64 + lane / kLanes;
+    auto sums = [&](int row, float* s0, float* s1) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const f32x4 v = *reinterpret_cast<const f32x4*>(own + row * 256 + (((e + x) ^ (row & 15)) << 4));
@@ -414,7 +441,34 @@ __device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char
           s1[4 * x] = w[0], s1[4 * x + 1] = w[1], s1[4 * x + 2] = w[2], s1[4 * x + 3] = w[3];
         }
       }
-      if (i < g.ni && j < g.nj) finish8<TYPE, KIND>(g, part, split, i, j, s0, s1);
+    };
+    if (j < g.nj) {
+      float s0[8], s1[8];
+      if (g.splits > 1) {
+        // partial sums: rows padded to whole eights
+        const int64_t ld = (g.nj + 7) / 8 * 8, slice = int64_t(g.ni) * ld;
+        float* p = g.partial + (int64_t(kGate ? 0 : part) * g.splits + split) * slice + first * ld + j;
+#pragma unroll 1
+        for (int row0 = 0; row0 < 64; row0 += kRows, p += kRows * ld) {
+          if (first + row0 >= g.ni) break;
+          sums(row0 + lane / kLanes, s0, s1);
+          reinterpret_cast<f32x4*>(p)[0] = f32x4{s0[0], s0[1], s0[2], s0[3]};
+          reinterpret_cast<f32x4*>(p)[1] = f32x4{s0[4], s0[5], s0[6], s0[7]};
+          if constexpr (kGate) {
+            float* u = p + g.splits * slice;
+            reinterpret_cast<f32x4*>(u)[0] = f32x4{s1[0], s1[1], s1[2], s1[3]};
+            reinterpret_cast<f32x4*>(u)[1] = f32x4{s1[4], s1[5], s1[6], s1[7]};
+          }
+        }
+      } else {
+        Finish<TYPE, KIND> out(g, part, first, j, kRows);
+#pragma unroll 1
+        for (int row0 = 0; row0 < 64; row0 += kRows, out.next()) {
+          if (first + row0 >= g.ni) break;
+          sums(row0 + lane / kLanes, s0, s1);
+          out.put(s0, s1);
+        }
+      }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
@@ -752,7 +806,206 @@ __global__ __launch_bounds__(256) void dense_join(DenseGemm g) {
       for (int e = 0; e < 4; ++e) s[mat][e] += lo[e], s[mat][4 + e] += hi[e];
     }
   }
-  finish8<TYPE, KIND, true>(g, part, 0, i, j, s[0], s[1]);
+  Finish<TYPE, KIND>(g, part, i, j, 0).put(s[0], s[1]);
+}
+
+// ---------------------------------------------------------------- few rows, or a short reduction
+//
+// Forward products that tiles suit badly, in one launch, without LDS on the way in and without copies: a wavefront loads
+// its fragments straight into registers, 16 rows of 64 bytes an instruction, at any alignment (WHOLE: 16 bytes a lane,
+// else element by element).
+template <int TYPE, bool WHOLE>
+struct Loader {
+  using T = typename Elem<TYPE>::T;
+  float v[TYPE == kDenseF32 ? 8 : 1];   // f32 values
+  s16x8 h;                              // or 16-bit ones
+
+  __device__ void read(const T* p) {   // whole, aligned
+    if constexpr (TYPE == kDenseF32) __builtin_memcpy(v, __builtin_assume_aligned(p, 16), 32);
+    else h = *reinterpret_cast<const s16x8*>(p);
+  }
+
+  // elements at .. at + 7 of a row; those from n on are zeros
+  __device__ void load(const T* row, int at, int n) {
+    if constexpr (TYPE == kDenseF32) {
+      if (WHOLE && at + 8 <= n) {
+        __builtin_memcpy(v, row + at, 32);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = row[min(at + e, n - 1)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = at + e < n ? v[e] : 0.0f;
+      }
+    } else if constexpr (WHOLE) {   // whole eights, at multiples of 16 bytes
+      h = *reinterpret_cast<const s16x8*>(row + min(at, n - 8));
+      if (at >= n) h = s16x8{};
+    } else {
+      const short* p = reinterpret_cast<const short*>(row);
+      short x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = p[min(at + e, n - 1)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) h[e] = at + e < n ? x[e] : short(0);
+    }
+  }
+};
+
+template <int TYPE, bool WHOLE>
+__device__ inline f32x4 multiply(const Loader<TYPE, WHOLE>& w, const Loader<TYPE, WHOLE>& x, f32x4 c) {
+  if constexpr (TYPE == kDenseF32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[e], x.v[e], c, 0, 0, 0);
+    return c;
+  } else {
+    return mfma16<TYPE>(w.h, x.h, c);
+  }
+}
+
+// Few rows: the weights are read once, and latency counts.  Eight wavefronts share FR * 16 rows by 16 columns and take
+// every eighth step of 32 each; their sums are added in order in LDS.
+template <int TYPE, int KIND, int FR, bool WHOLE>
+__global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
+  using T = typename Elem<TYPE>::T;
+  using L = Loader<TYPE, WHOLE>;
+  constexpr int kMats = KIND == kGated ? 2 : 1;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
+  const int j0 = blockIdx.x * 16;
+  const T* rows[FR];
+  const T* weights[kMats];
+#pragma unroll
+  for (int f = 0; f < FR; ++f) rows[f] = static_cast<const T*>(g.a[0]) + min(f * 16 + c, g.ni - 1) * g.lda;
+#pragma unroll
+  for (int m = 0; m < kMats; ++m) weights[m] = static_cast<const T*>(g.b[m]) + min(j0 + c, g.nj - 1) * g.ldb[m];
+  f32x4 acc[FR][kMats] = {};
+#pragma unroll 4
+  for (int r0 = wave * 32; r0 < g.nr; r0 += 8 * 32) {
+    L x[FR], w[kMats];
+#pragma unroll
+    for (int m = 0; m < kMats; ++m) w[m].load(weights[m], r0 + 8 * q, g.nr);
+#pragma unroll
+    for (int f = 0; f < FR; ++f) x[f].load(rows[f], r0 + 8 * q, g.nr);
+#pragma unroll
+    for (int f = 0; f < FR; ++f)
+#pragma unroll
+      for (int m = 0; m < kMats; ++m) acc[f][m] = multiply<TYPE, WHOLE>(w[m], x[f], acc[f][m]);
+  }
+  __shared__ float sums[8][FR][kMats][16][16];   // [wavefront][..][..][row][column]
+#pragma unroll
+  for (int f = 0; f < FR; ++f)
+#pragma unroll
+    for (int m = 0; m < kMats; ++m) *reinterpret_cast<f32x4*>(&sums[wave][f][m][c][4 * q]) = acc[f][m];
+  __syncthreads();
+  const int t = threadIdx.x, row = t >> 1, j = j0 + (t & 1) * 8;
+  if (row >= FR * 16 || row >= g.ni || j >= g.nj) return;
+  float s[2][8] = {};
+#pragma unroll
+  for (int w = 0; w < 8; ++w)
+#pragma unroll
+    for (int m = 0; m < kMats; ++m)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[m][e] += sums[w][row >> 4][m][row & 15][(t & 1) * 8 + e];
+  Finish<TYPE, KIND>(g, 0, row, j, 0).put(s[0], s[1]);
+}
+
+// A reduction of at most KS * 32: writing the results is all.  Four wavefronts, each with the weights of FC * 16 columns in
+// registers, walk rows of x by chunks of 64, which pass through LDS: loaded once for all columns of the workgroup, as
+// 16-byte chunks (WHOLE) or consecutive elements, while the chunk before is multiplied.  Where there are fewer columns
+// than the four hold, several take the same columns and other rows of the chunk.  Results leave through LDS, in whole
+// 128-byte lines.
+template <int TYPE, int KIND, int FC, int KS, bool WHOLE>
+__global__ __launch_bounds__(256) void dense_short(DenseGemm g) {
+  using T = typename Elem<TYPE>::T;
+  using L = Loader<TYPE, WHOLE>;
+  constexpr int kMats = KIND == kGated ? 2 : 1;
+  constexpr int kRow = KS * 32 + 16 / int(sizeof(T));   // of LDS: 16 rows' chunks lie in different banks
+  __shared__ __align__(16) T tile[2][64 * kRow];
+  __shared__ __align__(16) char sums[4][4096];          // 16 rows of 64 sums of each wavefront, as in store_sums
+  static_assert(FC * kMats == 4);
+  const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int waves_j = g.short_waves, waves_i = 4 / waves_j;        // 1, 2 or 4
+  const int across = (g.nj + waves_j * FC * 16 - 1) / (waves_j * FC * 16), chunks = (g.ni + 63) / 64;
+  const int j0 = (blockIdx.x % across * waves_j + wave % waves_j) * FC * 16;
+  const int first = blockIdx.x / across * g.row_chunks, end = min(chunks, first + g.row_chunks);
+  L w[kMats][FC][KS];
+  // the epilogue's lanes: eight consecutive columns of a row
+  constexpr int kLanes = KIND == kGated ? 4 : 8;
+  const int e0 = lane % kLanes * 2, j = j0 + e0 * 4;
+#pragma unroll
+  for (int m = 0; m < kMats; ++m) {
+#pragma unroll
+    for (int n = 0; n < FC; ++n) {
+      const int column = min(j0 + n * 16 + c, g.nj - 1);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) w[m][n][k].load(static_cast<const T*>(g.b[m]) + column * g.ldb[m], k * 32 + 8 * q, g.nr);
+    }
+  }
+  // a chunk of x: pieces of kPer elements, the same columns of different rows for a thread
+  constexpr int kPer = WHOLE ? 16 / sizeof(T) : 1;
+  constexpr int kWide = KS * 32 / kPer, kDown = 256 / kWide, kPieces = 64 / kDown;
+  typedef T Piece __attribute__((ext_vector_type(kPer)));
+  Piece held[kPieces];
+  const int at = tid % kWide * kPer, down = tid / kWide;
+  const bool inside = at < g.nr;
+  const T* const x = static_cast<const T*>(g.a[0]) + (inside ? at : 0);
+  auto fetch = [&](int chunk) {
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n) {
+      const int64_t i = min(int64_t(chunk) * 64 + n * kDown + down, int64_t(g.ni) - 1);
+      held[n] = *reinterpret_cast<const Piece*>(x + i * g.lda);
+    }
+  };
+  auto put = [&](int slot) {
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n)
+      *reinterpret_cast<Piece*>(&tile[slot][(n * kDown + down) * kRow + at]) = inside ? held[n] : Piece(T(0.0f));
+  };
+  if (first >= end) return;
+  constexpr int kDownRows = 64 / kLanes;   // rows that the epilogue takes at a time
+  Finish<TYPE, KIND> out(g, 0, int64_t(first) * 64 + wave / waves_j * 16 + lane / kLanes, j, kDownRows);
+  fetch(first);
+  put(0);
+  for (int chunk = first; chunk < end; ++chunk) {
+    const int slot = (chunk - first) & 1;
+    __syncthreads();
+    if (chunk + 1 < end) fetch(chunk + 1);
+#pragma unroll 1
+    for (int block = wave / waves_j; block < 4; block += waves_i) {
+      f32x4 acc[kMats][FC] = {};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        L v;
+        v.read(&tile[slot][(block * 16 + c) * kRow + k * 32 + 8 * q]);
+#pragma unroll
+        for (int m = 0; m < kMats; ++m)
+#pragma unroll
+          for (int n = 0; n < FC; ++n) acc[m][n] = multiply<TYPE, WHOLE>(w[m][n][k], v, acc[m][n]);
+      }
+      char* own = sums[wave];
+#pragma unroll
+      for (int m = 0; m < kMats; ++m)
+#pragma unroll
+        for (int n = 0; n < FC; ++n)
+          *reinterpret_cast<f32x4*>(own + c * 256 + ((((m * FC + n) * 4 + q) ^ c) << 4)) = acc[m][n];
+#pragma unroll
+      for (int row0 = 0; row0 < 16; row0 += kDownRows, out.next()) {
+        const int row = row0 + lane / kLanes;
+        const int64_t i = int64_t(chunk) * 64 + block * 16 + row;
+        float s[2][8];
+#pragma unroll
+        for (int m = 0; m < kMats; ++m)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const f32x4 v = *reinterpret_cast<const f32x4*>(own + row * 256 + (((m * FC * 4 + e0 + h) ^ row) << 4));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[m][4 * h + e] = v[e];
+          }
+        if (i < g.ni && j < g.nj) out.put(s[0], s[1]);
+      }
+      for (int skip = (waves_i - 1) * 16; skip > 0; skip -= kDownRows) out.next();   // the other wavefronts' blocks
+    }
+    if (chunk + 1 < end) put(slot ^ 1);
+  }
 }
 
 // ---------------------------------------------------------------- elementwise parts of the gradients
@@ -906,8 +1159,42 @@ int join_launch(const DenseGemm& g, hipStream_t stream) {
   return hipGetLastError();
 }
 
+template <int TYPE, int KIND, int FR>
+int rows_launch(const DenseGemm& g, hipStream_t stream) {
+  const dim3 grid((g.nj + 15) / 16);
+  if (g.whole) dense_rows<TYPE, KIND, FR, true><<<grid, 512, 0, stream>>>(g);
+  else dense_rows<TYPE, KIND, FR, false><<<grid, 512, 0, stream>>>(g);
+  return hipGetLastError();
+}
+
+template <int TYPE, int KIND, int FC, int KS>
+int short_launch(const DenseGemm& given, hipStream_t stream) {
+  DenseGemm g = given;
+  g.short_waves = g.nj <= FC * 16 ? 1 : g.nj <= FC * 32 ? 2 : 4;
+  const int64_t columns = g.short_waves * FC * 16, across = (g.nj + columns - 1) / columns, chunks = (g.ni + 63) / 64;
+  // four workgroups a CU, as long as each has a chunk of rows
+  const int64_t down = std::min(chunks, std::max<int64_t>(1, 1024 / across));
+  g.row_chunks = static_cast<int32_t>((chunks + down - 1) / down);
+  const dim3 grid(static_cast<uint32_t>((chunks + g.row_chunks - 1) / g.row_chunks * across));
+  if (g.whole) dense_short<TYPE, KIND, FC, KS, true><<<grid, 256, 0, stream>>>(g);
+  else dense_short<TYPE, KIND, FC, KS, false><<<grid, 256, 0, stream>>>(g);
+  return hipGetLastError();
+}
+
 template <int TYPE, int KIND>
 int kind_launch(const DenseGemm& g, hipStream_t stream) {
+  if constexpr (KIND == kForward || KIND == kGated) {
+    if (g.variant == kRows) {
+      if (g.ni <= 16) return rows_launch<TYPE, KIND, 1>(g, stream);
+      if (g.ni <= 32) return rows_launch<TYPE, KIND, 2>(g, stream);
+      return rows_launch<TYPE, KIND, 4>(g, stream);
+    }
+    if (g.variant == kShort) {
+      constexpr int kColumns = KIND == kGated ? 2 : 4;
+      if (g.nr <= 32) return short_launch<TYPE, KIND, kColumns, 1>(g, stream);
+      return short_launch<TYPE, KIND, kColumns, 2>(g, stream);
+    }
+  }
   if constexpr (TYPE != kDenseF32)
     if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
   return tile_launch<TYPE, KIND, 128, 128, 2, 2, 2>(g, stream);

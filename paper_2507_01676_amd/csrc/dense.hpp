@@ -18,7 +18,7 @@ enum DenseKind {
   kWeightGrad = 3    // C[i][j] = sum_r A[r][i] B[r][j]   A = dz, B = x       (R, R)
 };
 
-enum DenseVariant { kTile128 = 0, kTile256 = 1 };
+enum DenseVariant { kTile128 = 0, kTile256 = 1, kRows = 2, kShort = 3 };
 
 // One matrix product.  Arrays of two: kGated's two weights and results; kInputGrad's two
 // products summed into one result (parts = 2); kWeightGrad's two results (parts = 2).
@@ -34,6 +34,8 @@ struct DenseGemm {
   int32_t ni, nj, nr;      // C is [ni][nj], the sum over nr (in each part)
   int32_t parts, splits, act;
   int32_t variant;         // DenseVariant
+  int32_t row_chunks, short_waves;   // kShort: chunks of 64 rows of a workgroup, its wavefronts along columns
+  int32_t whole;           // kRows, kShort: operands' rows start at multiples of 16 bytes and hold whole chunks
 };
 
 // dz = dy * act'(z), or dg, du; and partial column sums of them

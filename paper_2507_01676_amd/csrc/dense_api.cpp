@@ -75,6 +75,8 @@ bool whole16(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
 // Which tile a product takes and over how many workgroups its reduction is split.
 struct Choice { int32_t variant, splits; };
 
+constexpr int64_t kFewRows = 64, kShortSum = 64;
+
 constexpr int kCus = 256;
 
 // Microseconds of a product by tiles of 256 x 256 or 128 x 128 over `steps` steps of 128 bytes, split s ways.  Measured
@@ -94,8 +96,15 @@ double tile_us(int32_t dtype, int variant, double tiles, int steps, int s, doubl
     us = whole * (each * shared + 3.0);
     if (rest > 0) us += each * (rest <= kCus ? alone : shared) + 3.0;
   }
-  if (s > 1) us += 3.0 + result_bytes * s / 2.0e6;
+  if (s > 1) us += 5.0 + result_bytes * s / 2.0e6;   // (another launch too)
   return us;
+}
+
+// The same of few rows: workgroups of 16 columns, a step being 32 of the reduction of each of eight wavefronts.  Measured
+// on 1 to 64 rows by 512 to 8192 columns and inputs: 0.5 us a step of 16 rows, 1.0 of 64, with a workgroup on every CU.
+double rows_us(int64_t ni, int64_t nj, int64_t nr) {
+  const double groups = double((nj + 15) / 16), steps = double((nr + 255) / 256);
+  return 3.0 + steps * (ni <= 16 ? 0.5 : ni <= 32 ? 0.7 : 1.0) * std::max(1.0, groups / kCus);
 }
 
 Choice choose(int32_t dtype, int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
@@ -103,8 +112,11 @@ Choice choose(int32_t dtype, int kind, int64_t ni, int64_t nj, int64_t nr, int p
   const int64_t steps = (nr + step - 1) / step * (kind == kInputGrad ? parts : 1);
   const int results = kind == kWeightGrad ? parts : kind == kGated ? 2 : 1;
   const double result_bytes = 4.0 * ni * nj * results;
+  const bool forward = kind == kForward || kind == kGated;
+  if (forward && nr <= kShortSum && ni > kFewRows) return {kShort, 1};
   Choice best = {kTile128, 1};
   double least = 0.0;
+  if (forward && ni <= kFewRows) best = {kRows, 1}, least = rows_us(ni, nj, nr);
   for (int variant : {kTile256, kTile128}) {
     if (variant == kTile256 && dtype == EMB_DTYPE_F32) continue;
     const int64_t side = variant == kTile256 ? 256 : 128;
@@ -176,8 +188,9 @@ struct Packer {
   Arena& ar;
   int32_t dtype;
   DensePack pack = {};
+  bool where_they_lie = false;   // nothing is copied
   Operand use(const void* p, int64_t ld, int64_t rows, int64_t cols) {
-    if (rows == 0 || whole(p, ld, cols, dtype)) return {p, ld};
+    if (rows == 0 || where_they_lie || whole(p, ld, cols, dtype)) return {p, ld};
     const int64_t ldd = (cols + chunk(dtype) - 1) / chunk(dtype) * chunk(dtype);
     pack.esize = static_cast<int32_t>(esize(dtype));
     const int at = pack.count++;
@@ -212,6 +225,7 @@ int32_t slope_blocks(int64_t m, int64_t n) {
 
 // The workspace of each call: copies of operands, dz, column sums and partial sums of products.
 struct Space {
+  Choice choice = {kTile128, 1};   // of the forward calls
   Operand x, w[2], dz[2];
   DensePack pack;
   float* colsum[2] = {nullptr, nullptr};
@@ -223,10 +237,10 @@ struct Space {
 Space linear_space(Arena& ar, const emb_linear_t& a) {
   Space s;
   Packer pk{ar, a.dtype};
-  if (a.m > 0) {
-    s.x = pk.use(a.x, a.ldx, a.m, a.k);
-    s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k);
-  }
+  s.choice = choose(a.dtype, kForward, a.m, a.n, a.k, 1);
+  pk.where_they_lie = s.choice.variant >= kRows;
+  s.x = pk.use(a.x, a.ldx, a.m, a.k);
+  s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k);
   s.pack = pk.pack;
   s.partial = ar.take<float>(partial_bytes(a.dtype, kForward, a.m, a.n, a.k, 1));
   return s;
@@ -235,11 +249,11 @@ Space linear_space(Arena& ar, const emb_linear_t& a) {
 Space gated_space(Arena& ar, const emb_gated_t& a) {
   Space s;
   Packer pk{ar, a.dtype};
-  if (a.m > 0) {
-    s.x = pk.use(a.x, a.ldx, a.m, a.k);
-    s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k);
-    s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k);
-  }
+  s.choice = choose(a.dtype, kGated, a.m, a.n, a.k, 1);
+  pk.where_they_lie = s.choice.variant >= kRows;
+  s.x = pk.use(a.x, a.ldx, a.m, a.k);
+  s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k);
+  s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k);
   s.pack = pk.pack;
   s.partial = ar.take<float>(partial_bytes(a.dtype, kGated, a.m, a.n, a.k, 1));
   return s;
@@ -333,6 +347,7 @@ emb_status_t emb_linear(const emb_linear_t* a, void* workspace, size_t workspace
   g.res = a->residual, g.ldr = a->ldr;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
   g.parts = 1, g.act = a->activation;
+  g.whole = whole(a->x, a->ldx, a->k, a->dtype) && whole(a->weight, a->ldw, a->k, a->dtype);
   return gemm(a->dtype, kForward, g, sp.partial, stream);
 }
 
@@ -428,6 +443,8 @@ emb_status_t emb_gated(const emb_gated_t* a, void* workspace, size_t workspace_b
   g.bias[0] = a->b_gate, g.bias[1] = a->b_up;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
   g.parts = 1, g.act = a->activation;
+  g.whole = whole(a->x, a->ldx, a->k, a->dtype) && whole(a->w_gate, a->ld_gate, a->k, a->dtype) &&
+            whole(a->w_up, a->ld_up, a->k, a->dtype);
   return gemm(a->dtype, kGated, g, sp.partial, stream);
 }
 
