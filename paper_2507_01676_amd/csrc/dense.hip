@@ -522,7 +522,7 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
   constexpr bool kGate = KIND == kGated;
   constexpr bool kRmA = KIND == kWeightGrad, kRmB = KIND == kWeightGrad || KIND == kInputGrad;
   constexpr int kWaves = WI * WJ;
-  constexpr bool kTurns = kWaves == 8;                     // see the main loop (16 bits only)
+  constexpr bool kTurns = kWaves == 8 && TYPE != kDenseF32;   // see the main loop
   constexpr int kSlotsA = kTurns ? 3 : 2, kSlotsB = 2;     // tiles of steps in LDS
   constexpr int kCols = kGate ? BN / 2 : BN;               // result columns of a tile
   constexpr int kWI = BM / WI, kWJ = kCols / WJ;           // results of a wavefront
@@ -627,7 +627,8 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
   };
   int at_a = 0, at_b = 0;   // slots of the step that is multiplied
   if constexpr (!kTurns) {
-    // Two workgroups a CU: one reads while the other multiplies.
+    // One step is on its way while another is multiplied.  Two workgroups share a CU, so that one reads while the other
+    // multiplies (f32's large tile: two wavefronts a SIMD do).
     set_a(begin, 0);
     set_b(begin, 0);
 #pragma unroll
@@ -642,27 +643,36 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
 #pragma unroll
       for (int n = 0; n < kIssues; ++n) issue(n);
       if constexpr (kF32) {
-        Parts fa[2][2], fb[kFJ];
-        auto part_a = [&](int n, Parts* f) {
-          float v[8];
-          value_a(sa, n, v);
-          *f = split3(v);
+        // 128 rows: the next pair of A's fragments is taken apart beside the products of this one.  256 rows: registers
+        // hold one pair, and fragments in any other order than this would not fit.
+        constexpr bool kLean = kFI == 8;
+        auto keep_order = [] {
+          if constexpr (kLean) __builtin_amdgcn_sched_barrier(0);
+        };
+        Parts fa[kLean ? 1 : 2][2], fb[kFJ];
+        auto pair_a = [&](int h, Parts* f) {
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            float v[8];
+            value_a(sa, h + n, v);
+            f[n] = split3(v);
+          }
+          keep_order();
         };
 #pragma unroll
         for (int n = 0; n < kFJ; ++n) {
           float v[8];
           value_b(sb, n, v);
           fb[n] = split3(v);
+          keep_order();
         }
-        part_a(0, &fa[0][0]);
-        part_a(1, &fa[0][1]);
+        if (!kLean) pair_a(0, fa[0]);
 #pragma unroll
         for (int h = 0; h < kFI; h += 2) {
-          if (h + 2 < kFI) {
-            part_a(h + 2, &fa[(h / 2 + 1) & 1][0]);
-            part_a(h + 3, &fa[(h / 2 + 1) & 1][1]);
-          }
-          products6<2, kFJ>(fa[(h / 2) & 1], fb, acc + h);
+          if (kLean) pair_a(h, fa[0]);
+          else if (h + 2 < kFI) pair_a(h + 2, fa[(h / 2 + 1) & 1]);
+          products6<2, kFJ>(fa[kLean ? 0 : (h / 2) & 1], fb, acc + h);
+          keep_order();
         }
       } else {
 #pragma unroll
@@ -1195,7 +1205,8 @@ int kind_launch(const DenseGemm& g, hipStream_t stream) {
       return short_launch<TYPE, KIND, kColumns, 2>(g, stream);
     }
   }
-  if constexpr (TYPE != kDenseF32)
+  // (f32's reads of reduction-major B do not fit the large tile's registers)
+  if constexpr (TYPE != kDenseF32 || KIND != kInputGrad)
     if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
   return tile_launch<TYPE, KIND, 128, 128, 2, 2, 2>(g, stream);
 }

@@ -80,23 +80,24 @@ constexpr int64_t kFewRows = 64, kShortSum = 64;
 constexpr int kCus = 256;
 
 // Microseconds of a product by tiles of 256 x 256 or 128 x 128 over `steps` steps of 128 bytes, split s ways.  Measured
-// on bf16 products of 256 to 8192 rows: a step of the large tile takes 0.97 us on a GPU that is otherwise idle and
-// 1.50 us with a workgroup on every CU (the clock drops, and L2 is shared); one of the small tile 0.62 us alone on its
-// CU, 1.03 us where two share it (f32: 1.6 and 2.7 us).  A round starts and ends in 3 us.  Split products write their
-// sums and read them back.
+// on bf16 (f32) products of 256 to 8192 rows: a step of the large tile takes 0.97 (4.6) us on a GPU that is otherwise
+// idle and 1.50 (5.0) us with a workgroup on every CU (the clock drops, and L2 is shared); one of the small tile 0.62
+// (1.6) us alone on its CU, 1.03 (2.7) us where two share it.  A round starts and ends in 3 us.  Split products write
+// their sums, and another launch of 5 us reads them back.
 double tile_us(int32_t dtype, int variant, double tiles, int steps, int s, double result_bytes) {
+  const bool f32 = dtype == EMB_DTYPE_F32;
   const double groups = tiles * s, each = (steps + s - 1) / s;
   double us;
   if (variant == kTile256) {
-    us = std::ceil(groups / kCus) * (each * (0.97 + 0.53 * std::min(1.0, groups / kCus)) + 3.0);
+    const double alone = f32 ? 4.6 : 0.97, full = f32 ? 5.0 : 1.50;
+    us = std::ceil(groups / kCus) * (each * (alone + (full - alone) * std::min(1.0, groups / kCus)) + 3.0);
   } else {
-    const bool f32 = dtype == EMB_DTYPE_F32;
     const double alone = f32 ? 1.6 : 0.62, shared = f32 ? 2.7 : 1.03;
     const double whole = std::floor(groups / (2 * kCus)), rest = groups - whole * 2 * kCus;
     us = whole * (each * shared + 3.0);
     if (rest > 0) us += each * (rest <= kCus ? alone : shared) + 3.0;
   }
-  if (s > 1) us += 5.0 + result_bytes * s / 2.0e6;   // (another launch too)
+  if (s > 1) us += 5.0 + result_bytes * s / 3.0e6;
   return us;
 }
 
@@ -118,7 +119,7 @@ Choice choose(int32_t dtype, int kind, int64_t ni, int64_t nj, int64_t nr, int p
   double least = 0.0;
   if (forward && ni <= kFewRows) best = {kRows, 1}, least = rows_us(ni, nj, nr);
   for (int variant : {kTile256, kTile128}) {
-    if (variant == kTile256 && dtype == EMB_DTYPE_F32) continue;
+    if (variant == kTile256 && dtype == EMB_DTYPE_F32 && kind == kInputGrad) continue;
     const int64_t side = variant == kTile256 ? 256 : 128;
     const double tiles = double((ni + side - 1) / side) * ((nj * (kind == kGated ? 2 : 1) + side - 1) / side) *
                          (kind == kWeightGrad ? parts : 1);
