@@ -517,8 +517,17 @@ __device__ __noinline__ void tile_by_f32(const DenseGemm& g, char* lds, int i0, 
   store_sums<kDenseF32, KIND, FI, FJ>(g, acc, lds + (tid >> 6) * 16384, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
 }
 
-template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
-__global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile(DenseGemm g) {
+// bytes of LDS of a tile: the steps under way, and 16 KB a wavefront for the epilogue
+template <int TYPE, int BM, int BN, int WAVES>
+constexpr int kTileLds = [] {
+  const bool turns = WAVES == 8 && TYPE != kDenseF32;
+  const int steps = ((turns ? 3 : 2) * BM + 2 * BN) * 128;
+  return steps > WAVES * 16384 ? steps : WAVES * 16384;
+}();
+
+// One tile of a product: `tile` of its tiles, `split` of its splits, `wpart` of kWeightGrad's two results.
+template <int TYPE, int KIND, int BM, int BN, int WI, int WJ>
+__device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint32_t tile, int split, int wpart) {
   constexpr bool kGate = KIND == kGated;
   constexpr bool kRmA = KIND == kWeightGrad, kRmB = KIND == kWeightGrad || KIND == kInputGrad;
   constexpr int kWaves = WI * WJ;
@@ -533,15 +542,12 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
   using TileB = Tile<BN, kRmB, kWaves, kSize>;
   using TileH = Tile<kCols, kRmB, kWaves, kSize>;          // one projection's half of B
   constexpr int BK = TileA::BK;
-  constexpr int kStages = kSlotsA * TileA::kBytes + kSlotsB * TileB::kBytes;
-  constexpr int kLds = kStages > kWaves * 16384 ? kStages : kWaves * 16384;   // (16 KB: epilogue)
-  __shared__ __align__(1024) char lds[kLds];
+  static_assert(kSlotsA * TileA::kBytes + kSlotsB * TileB::kBytes <= kTileLds<TYPE, BM, BN, kWaves>);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int ti, tj;
-  tile_of(blockIdx.x, (g.ni + BM - 1) / BM, (g.nj + kCols - 1) / kCols, &ti, &tj);
+  tile_of(tile, (g.ni + BM - 1) / BM, (g.nj + kCols - 1) / kCols, &ti, &tj);
   const int i0 = ti * BM, j0 = tj * kCols;
-  const int split = blockIdx.y, wpart = KIND == kWeightGrad ? blockIdx.z : 0;
   const int per_part = (g.nr + BK - 1) / BK;
   const int steps = per_part * (KIND == kInputGrad ? g.parts : 1);
   const int begin = static_cast<int>(int64_t(steps) * split / g.splits);
@@ -794,15 +800,36 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
   store_sums<TYPE, KIND, kFI, kFJ>(g, acc, lds + wave * 16384, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
 }
 
-// Results of a product whose reduction was split: the splits' sums are added in order.  A thread has eight columns.
+template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
+__global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile(DenseGemm g) {
+  __shared__ __align__(1024) char lds[kTileLds<TYPE, BM, BN, WI * WJ>];
+  tile_product<TYPE, KIND, BM, BN, WI, WJ>(g, lds, blockIdx.x, blockIdx.y, 0);
+}
+
+// Both products of a backward pass in one launch: the weights' gradient first, whose tiles are few and long, then the
+// input's, whose many short ones fill the CUs that are left (either may be absent).
+template <int TYPE, int BM, int BN, int WI, int WJ, int PER_CU>
+__global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_grads(DenseGemm w, DenseGemm x, uint32_t w_groups) {
+  __shared__ __align__(1024) char lds[kTileLds<TYPE, BM, BN, WI * WJ>];
+  uint32_t id = blockIdx.x;
+  if (id < w_groups) {
+    const uint32_t tiles = (w.ni + BM - 1) / BM * ((w.nj + BN - 1) / BN), rest = id / tiles;
+    if (rest >= uint32_t(w.splits * w.parts)) return;   // (w_groups is a multiple of the XCDs)
+    tile_product<TYPE, kWeightGrad, BM, BN, WI, WJ>(w, lds, id % tiles, rest % w.splits, rest / w.splits);
+  } else {
+    id -= w_groups;
+    const uint32_t tiles = (x.ni + BM - 1) / BM * ((x.nj + BN - 1) / BN);
+    tile_product<TYPE, kInputGrad, BM, BN, WI, WJ>(x, lds, id % tiles, id / tiles, 0);
+  }
+}
+
+// Eight columns of a result whose reduction was split: the splits' sums are added in order.
 template <int TYPE, int KIND>
-__global__ __launch_bounds__(256) void dense_join(DenseGemm g) {
+__device__ inline void join8(const DenseGemm& g, int64_t at, int part) {
   const int groups = (g.nj + 7) / 8;
-  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
   if (at >= int64_t(groups) * g.ni) return;
-  const int64_t i = at / groups;
-  const int j = static_cast<int>(at % groups) * 8, part = blockIdx.y;
-  const int64_t slice = int64_t(g.ni) * groups * 8;
+  const int64_t i = at / groups, slice = int64_t(g.ni) * groups * 8;
+  const int j = static_cast<int>(at % groups) * 8;
   float s[2][8];
 #pragma unroll
   for (int mat = 0; mat < (KIND == kGated ? 2 : 1); ++mat) {
@@ -817,6 +844,46 @@ __global__ __launch_bounds__(256) void dense_join(DenseGemm g) {
     }
   }
   Finish<TYPE, KIND>(g, part, i, j, 0).put(s[0], s[1]);
+}
+
+template <int TYPE, int KIND>
+__global__ __launch_bounds__(256) void dense_join(DenseGemm g) {
+  join8<TYPE, KIND>(g, int64_t(blockIdx.x) * 256 + threadIdx.x, 0);
+}
+
+// The last launch of a backward pass, as far as there is something left: the column sums from those of the blocks of
+// rows (32 columns a workgroup, eight threads a column), then the joins of both products.
+template <int TYPE>
+__global__ __launch_bounds__(256) void dense_tail(DenseGemm w, DenseGemm x, DenseColsum c, DenseTail t) {
+  using T = typename Elem<TYPE>::T;
+  uint32_t id = blockIdx.x;
+  if (id < t.colsum_groups) {
+    __shared__ float sums[8][32];
+    const uint32_t per = (c.n + 31) / 32;
+    const int mat = id / per, column = threadIdx.x & 31, y = threadIdx.x >> 5, j = id % per * 32 + column;
+    const float* p = c.partial[mat];
+    if (!p) return;
+    float sum = 0.0f;
+    if (j < c.n) {
+#pragma unroll 8
+      for (int b = y; b < c.blocks; b += 8) sum += p[int64_t(b) * c.n + j];
+    }
+    sums[y][column] = sum;
+    __syncthreads();
+    if (y == 0 && j < c.n) {
+#pragma unroll
+      for (int r = 1; r < 8; ++r) sum += sums[r][column];
+      static_cast<T*>(c.out[mat])[j] = T(sum);
+    }
+    return;
+  }
+  id -= t.colsum_groups;
+  if (id < t.w_groups * w.parts) {
+    join8<TYPE, kWeightGrad>(w, int64_t(id % t.w_groups) * 256 + threadIdx.x, id / t.w_groups);
+    return;
+  }
+  id -= t.w_groups * w.parts;
+  join8<TYPE, kInputGrad>(x, int64_t(id) * 256 + threadIdx.x, 0);
 }
 
 // ---------------------------------------------------------------- few rows, or a short reduction
@@ -1110,28 +1177,6 @@ __global__ __launch_bounds__(256) void dense_slope(DenseSlope s) {
   }
 }
 
-// sums of the blocks' column sums: 32 columns a workgroup, eight threads a column
-template <int TYPE>
-__global__ __launch_bounds__(256) void dense_colsum(DenseColsum s) {
-  using T = typename Elem<TYPE>::T;
-  __shared__ float sums[8][32];
-  const int c = threadIdx.x & 31, y = threadIdx.x >> 5, j = blockIdx.x * 32 + c;
-  const float* p = s.partial[blockIdx.y];
-  if (!p) return;
-  float sum = 0.0f;
-  if (j < s.n) {
-#pragma unroll 8
-    for (int b = y; b < s.blocks; b += 8) sum += p[int64_t(b) * s.n + j];
-  }
-  sums[y][c] = sum;
-  __syncthreads();
-  if (y == 0 && j < s.n) {
-#pragma unroll
-    for (int r = 1; r < 8; ++r) sum += sums[r][c];
-    static_cast<T*>(s.out[blockIdx.y])[j] = T(sum);
-  }
-}
-
 // Copies up to three matrices to rows that start at multiples of 16 bytes and end in zeros up to a whole chunk: the
 // tiles above read nothing else.  A wavefront takes 64 consecutive elements at a time, as rows that start anywhere
 // are read fastest (16-byte loads at odd addresses measured 1.1 TB/s).
@@ -1156,16 +1201,37 @@ template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
 int tile_launch(const DenseGemm& g, hipStream_t stream) {
   const int cols = KIND == kGated ? BN / 2 : BN;
   const int64_t tiles = int64_t((g.ni + BM - 1) / BM) * ((g.nj + cols - 1) / cols);
-  const dim3 grid(static_cast<uint32_t>(tiles), g.splits, KIND == kWeightGrad ? g.parts : 1);
-  dense_tile<TYPE, KIND, BM, BN, WI, WJ, PER_CU><<<grid, 64 * WI * WJ, 0, stream>>>(g);
+  dense_tile<TYPE, KIND, BM, BN, WI, WJ, PER_CU><<<dim3(static_cast<uint32_t>(tiles), g.splits), 64 * WI * WJ, 0, stream>>>(g);
+  if (const int rc = hipGetLastError(); rc != 0 || g.splits == 1) return rc;
+  const int64_t threads = int64_t((g.nj + 7) / 8) * g.ni;
+  dense_join<TYPE, KIND><<<static_cast<uint32_t>((threads + 255) / 256), 256, 0, stream>>>(g);
   return hipGetLastError();
 }
 
-template <int TYPE, int KIND>
-int join_launch(const DenseGemm& g, hipStream_t stream) {
-  const int64_t threads = int64_t((g.nj + 7) / 8) * g.ni;
-  const dim3 grid(static_cast<uint32_t>((threads + 255) / 256), KIND == kWeightGrad ? g.parts : 1);
-  dense_join<TYPE, KIND><<<grid, 256, 0, stream>>>(g);
+template <int TYPE, int BM, int BN, int WI, int WJ, int PER_CU>
+int grads_launch(const DenseGemm& w, const DenseGemm& x, hipStream_t stream) {
+  auto tiles = [](const DenseGemm& g) { return int64_t((g.ni + BM - 1) / BM) * ((g.nj + BN - 1) / BN) * g.splits; };
+  const int64_t w_groups = w.parts ? (tiles(w) * w.parts + kXcds - 1) / kXcds * kXcds : 0, x_groups = x.parts ? tiles(x) : 0;
+  if (w_groups + x_groups == 0) return 0;
+  dense_grads<TYPE, BM, BN, WI, WJ, PER_CU><<<static_cast<uint32_t>(w_groups + x_groups), 64 * WI * WJ, 0, stream>>>(
+      w, x, static_cast<uint32_t>(w_groups));
+  return hipGetLastError();
+}
+
+template <int TYPE>
+int backward_launch(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, int variant, hipStream_t stream) {
+  int rc;
+  if constexpr (TYPE == kDenseF32) rc = grads_launch<TYPE, 128, 128, 2, 2, 2>(w, x, stream);
+  else if (variant == kTile256) rc = grads_launch<TYPE, 256, 256, 2, 4, 1>(w, x, stream);
+  else rc = grads_launch<TYPE, 128, 128, 2, 2, 2>(w, x, stream);
+  if (rc != 0) return rc;
+  auto joins = [](const DenseGemm& g) {
+    return g.parts && g.splits > 1 ? static_cast<uint32_t>((int64_t((g.nj + 7) / 8) * g.ni + 255) / 256) : 0u;
+  };
+  const DenseTail t = {c.partial[0] || c.partial[1] ? uint32_t(c.n + 31) / 32 * 2 : 0u, joins(w)};
+  const uint32_t groups = t.colsum_groups + t.w_groups * w.parts + joins(x);
+  if (groups == 0) return 0;
+  dense_tail<TYPE><<<groups, 256, 0, stream>>>(w, x, c, t);
   return hipGetLastError();
 }
 
@@ -1192,40 +1258,19 @@ int short_launch(const DenseGemm& given, hipStream_t stream) {
 }
 
 template <int TYPE, int KIND>
-int kind_launch(const DenseGemm& g, hipStream_t stream) {
-  if constexpr (KIND == kForward || KIND == kGated) {
-    if (g.variant == kRows) {
-      if (g.ni <= 16) return rows_launch<TYPE, KIND, 1>(g, stream);
-      if (g.ni <= 32) return rows_launch<TYPE, KIND, 2>(g, stream);
-      return rows_launch<TYPE, KIND, 4>(g, stream);
-    }
-    if (g.variant == kShort) {
-      constexpr int kColumns = KIND == kGated ? 2 : 4;
-      if (g.nr <= 32) return short_launch<TYPE, KIND, kColumns, 1>(g, stream);
-      return short_launch<TYPE, KIND, kColumns, 2>(g, stream);
-    }
+int forward_launch(const DenseGemm& g, hipStream_t stream) {
+  if (g.variant == kRows) {
+    if (g.ni <= 16) return rows_launch<TYPE, KIND, 1>(g, stream);
+    if (g.ni <= 32) return rows_launch<TYPE, KIND, 2>(g, stream);
+    return rows_launch<TYPE, KIND, 4>(g, stream);
   }
-  // (f32's reads of reduction-major B do not fit the large tile's registers)
-  if constexpr (TYPE != kDenseF32 || KIND != kInputGrad)
-    if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
+  if (g.variant == kShort) {
+    constexpr int kColumns = KIND == kGated ? 2 : 4;
+    if (g.nr <= 32) return short_launch<TYPE, KIND, kColumns, 1>(g, stream);
+    return short_launch<TYPE, KIND, kColumns, 2>(g, stream);
+  }
+  if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
   return tile_launch<TYPE, KIND, 128, 128, 2, 2, 2>(g, stream);
-}
-
-template <int TYPE, int KIND>
-int product_launch(const DenseGemm& g, hipStream_t stream) {
-  const int rc = kind_launch<TYPE, KIND>(g, stream);
-  if (rc != 0 || g.splits == 1) return rc;
-  return join_launch<TYPE, KIND>(g, stream);
-}
-
-template <int TYPE>
-int gemm_launch(int kind, const DenseGemm& g, hipStream_t stream) {
-  switch (kind) {
-    case kForward: return product_launch<TYPE, kForward>(g, stream);
-    case kGated: return product_launch<TYPE, kGated>(g, stream);
-    case kInputGrad: return product_launch<TYPE, kInputGrad>(g, stream);
-    default: return product_launch<TYPE, kWeightGrad>(g, stream);
-  }
 }
 
 template <int TYPE>
@@ -1239,23 +1284,18 @@ int slope_launch(const DenseSlope& s, hipStream_t stream) {
   return hipGetLastError();
 }
 
-template <int TYPE>
-int colsum_launch(const DenseColsum& s, hipStream_t stream) {
-  dense_colsum<TYPE><<<dim3((s.n + 31) / 32, 2), 256, 0, stream>>>(s);
-  return hipGetLastError();
-}
-
 }  // namespace
 
-#define EMBX_DENSE_TYPE(NAME, TYPE)                                                                     \
-  int dense_gemm_##NAME(int kind, const DenseGemm& g, void* stream) {                                   \
-    return gemm_launch<TYPE>(kind, g, static_cast<hipStream_t>(stream));                                \
-  }                                                                                                     \
-  int dense_slope_##NAME(const DenseSlope& s, void* stream) {                                           \
-    return slope_launch<TYPE>(s, static_cast<hipStream_t>(stream));                                     \
-  }                                                                                                     \
-  int dense_colsum_##NAME(const DenseColsum& s, void* stream) {                                         \
-    return colsum_launch<TYPE>(s, static_cast<hipStream_t>(stream));                                    \
+#define EMBX_DENSE_TYPE(NAME, TYPE)                                                                             \
+  int dense_forward_##NAME(int kind, const DenseGemm& g, void* stream) {                                        \
+    const hipStream_t s = static_cast<hipStream_t>(stream);                                                     \
+    return kind == kGated ? forward_launch<TYPE, kGated>(g, s) : forward_launch<TYPE, kForward>(g, s);          \
+  }                                                                                                             \
+  int dense_backward_##NAME(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, int variant, void* stream) { \
+    return backward_launch<TYPE>(w, x, c, variant, static_cast<hipStream_t>(stream));                           \
+  }                                                                                                             \
+  int dense_slope_##NAME(const DenseSlope& s, void* stream) {                                                   \
+    return slope_launch<TYPE>(s, static_cast<hipStream_t>(stream));                                             \
   }
 
 #if EMBX_HAS_DPART(0)

@@ -32,7 +32,7 @@ struct DenseGemm {
   float* partial;          // [parts of the result][splits][ni][nj], with splits > 1
   int64_t lda, ldb[2], ldc[2], ldz[2], ldr;
   int32_t ni, nj, nr;      // C is [ni][nj], the sum over nr (in each part)
-  int32_t parts, splits, act;
+  int32_t parts, splits, act;   // parts = 0: no product
   int32_t variant;         // DenseVariant
   int32_t row_chunks, short_waves;   // kShort: chunks of 64 rows of a workgroup, its wavefronts along columns
   int32_t whole;           // kRows, kShort: operands' rows start at multiples of 16 bytes and hold whole chunks
@@ -48,6 +48,11 @@ struct DenseSlope {
   int32_t m, n, act, gated, row_blocks;
   int32_t log_x;           // log2 of the eights of columns of a workgroup
   int32_t whole;           // rows of all operands start at multiples of 16 bytes and hold whole eights
+};
+
+// workgroups of the last launch of a backward pass: of the column sums, and of the join of one of w's results
+struct DenseTail {
+  uint32_t colsum_groups, w_groups;
 };
 
 // matrices copied to rows of whole 16-byte chunks
@@ -70,9 +75,9 @@ int dense_pack_launch(const DensePack& p, void* stream);
 
 // launches of the kernels of one type (dense.hip is compiled once per type); 0 or a hipError_t
 #define EMBX_DENSE_DECLARE(NAME)                                                        \
-  int dense_gemm_##NAME(int kind, const DenseGemm& g, void* stream);                    \
-  int dense_slope_##NAME(const DenseSlope& s, void* stream);                            \
-  int dense_colsum_##NAME(const DenseColsum& s, void* stream);
+  int dense_forward_##NAME(int kind, const DenseGemm& g, void* stream);                 \
+  int dense_backward_##NAME(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, int variant, void* stream); \
+  int dense_slope_##NAME(const DenseSlope& s, void* stream);
 EMBX_DENSE_DECLARE(f32)
 EMBX_DENSE_DECLARE(f16)
 EMBX_DENSE_DECLARE(bf16)

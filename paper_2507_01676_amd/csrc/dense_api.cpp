@@ -79,25 +79,45 @@ constexpr int64_t kFewRows = 64, kShortSum = 64;
 
 constexpr int kCus = 256;
 
-// Microseconds of a product by tiles of 256 x 256 or 128 x 128 over `steps` steps of 128 bytes, split s ways.  Measured
-// on bf16 (f32) products of 256 to 8192 rows: a step of the large tile takes 0.97 (4.6) us on a GPU that is otherwise
-// idle and 1.50 (5.0) us with a workgroup on every CU (the clock drops, and L2 is shared); one of the small tile 0.62
-// (1.6) us alone on its CU, 1.03 (2.7) us where two share it.  A round starts and ends in 3 us.  Split products write
-// their sums, and another launch of 5 us reads them back.
-double tile_us(int32_t dtype, int variant, double tiles, int steps, int s, double result_bytes) {
+// Microseconds of a step of 128 bytes of a tile, of 256 x 256 or 128 x 128.  Measured on bf16 (f32) products of 256 to
+// 8192 rows: the large tile takes 0.97 (4.6) us on a GPU that is otherwise idle and 1.50 (5.0) us with a workgroup on
+// every CU (the clock drops, and L2 is shared); the small one 0.62 (1.6) us alone on its CU, 1.03 (2.7) us where two
+// share it.  A tile starts and ends in 3 us.
+struct StepTime { double alone, full; };
+
+StepTime step_us(int32_t dtype, int variant) {
   const bool f32 = dtype == EMB_DTYPE_F32;
-  const double groups = tiles * s, each = (steps + s - 1) / s;
+  if (variant == kTile256) return f32 ? StepTime{4.6, 5.0} : StepTime{0.97, 1.50};
+  return f32 ? StepTime{1.6, 2.7} : StepTime{0.62, 1.03};
+}
+
+constexpr double kTileUs = 3.0, kLaunchUs = 5.0;
+constexpr double kJoinBytes = 3.0e6;      // a microsecond, of partial sums written and read back
+constexpr double kMostPartial = 256 << 20;
+
+int64_t tiles_of(int variant, int64_t rows, int64_t columns) {
+  const int64_t side = variant == kTile256 ? 256 : 128;
+  return ((rows + side - 1) / side) * ((columns + side - 1) / side);
+}
+
+int64_t steps_of(int32_t dtype, int64_t nr) {
+  const int64_t step = 128 / static_cast<int64_t>(esize(dtype));
+  return (nr + step - 1) / step;
+}
+
+// a forward product whose reduction is split s ways
+double tile_us(int32_t dtype, int variant, double tiles, double steps, int s, double result_bytes) {
+  const StepTime t = step_us(dtype, variant);
+  const double groups = tiles * s, each = std::ceil(steps / s);
   double us;
   if (variant == kTile256) {
-    const double alone = f32 ? 4.6 : 0.97, full = f32 ? 5.0 : 1.50;
-    us = std::ceil(groups / kCus) * (each * (alone + (full - alone) * std::min(1.0, groups / kCus)) + 3.0);
+    us = std::ceil(groups / kCus) * (each * (t.alone + (t.full - t.alone) * std::min(1.0, groups / kCus)) + kTileUs);
   } else {
-    const double alone = f32 ? 1.6 : 0.62, shared = f32 ? 2.7 : 1.03;
     const double whole = std::floor(groups / (2 * kCus)), rest = groups - whole * 2 * kCus;
-    us = whole * (each * shared + 3.0);
-    if (rest > 0) us += each * (rest <= kCus ? alone : shared) + 3.0;
+    us = whole * (each * t.full + kTileUs);
+    if (rest > 0) us += each * (rest <= kCus ? t.alone : t.full) + kTileUs;
   }
-  if (s > 1) us += 5.0 + result_bytes * s / 3.0e6;
+  if (s > 1) us += kLaunchUs + result_bytes * s / kJoinBytes;
   return us;
 }
 
@@ -108,45 +128,85 @@ double rows_us(int64_t ni, int64_t nj, int64_t nr) {
   return 3.0 + steps * (ni <= 16 ? 0.5 : ni <= 32 ? 0.7 : 1.0) * std::max(1.0, groups / kCus);
 }
 
-Choice choose(int32_t dtype, int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
-  const int step = dtype == EMB_DTYPE_F32 ? 32 : 64;   // of the reduction
-  const int64_t steps = (nr + step - 1) / step * (kind == kInputGrad ? parts : 1);
-  const int results = kind == kWeightGrad ? parts : kind == kGated ? 2 : 1;
-  const double result_bytes = 4.0 * ni * nj * results;
-  const bool forward = kind == kForward || kind == kGated;
-  if (forward && nr <= kShortSum && ni > kFewRows) return {kShort, 1};
+Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k) {
+  if (k <= kShortSum && m > kFewRows) return {kShort, 1};
+  const int mats = kind == kGated ? 2 : 1;
+  const double steps = static_cast<double>(steps_of(dtype, k)), result_bytes = 4.0 * m * n * mats;
   Choice best = {kTile128, 1};
   double least = 0.0;
-  if (forward && ni <= kFewRows) best = {kRows, 1}, least = rows_us(ni, nj, nr);
+  if (m <= kFewRows) best = {kRows, 1}, least = rows_us(m, n, k);
   for (int variant : {kTile256, kTile128}) {
-    if (variant == kTile256 && dtype == EMB_DTYPE_F32 && kind == kInputGrad) continue;
-    const int64_t side = variant == kTile256 ? 256 : 128;
-    const double tiles = double((ni + side - 1) / side) * ((nj * (kind == kGated ? 2 : 1) + side - 1) / side) *
-                         (kind == kWeightGrad ? parts : 1);
-    for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= (256 << 20))); ++s) {
-      const double us = tile_us(dtype, variant, tiles, static_cast<int>(std::min<int64_t>(steps, 1 << 30)), s, result_bytes);
+    const double tiles = static_cast<double>(tiles_of(variant, m, n * mats));
+    for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial)); ++s) {
+      const double us = tile_us(dtype, variant, tiles, steps, s, result_bytes);
       if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, s};
     }
   }
   return best;
 }
 
-// bytes of partial sums of a product
-size_t partial_bytes(int32_t dtype, int kind, int64_t ni, int64_t nj, int64_t nr, int parts) {
-  const int results = kind == kWeightGrad ? parts : kind == kGated ? 2 : 1;
-  const int s = choose(dtype, kind, ni, nj, nr, parts).splits;
-  return s > 1 ? size_t(s) * ni * ((nj + 7) / 8 * 8) * results * 4 : 0;   // (rows of whole eights)
+// The tile of a backward pass's two products, and how often the reduction of each is split.
+struct GradChoice { int32_t variant, w_splits, x_splits; };
+
+// when `slots` workgroups at a time have done w_items of w us each and then x_items of x us each
+double both_us(int64_t slots, int64_t w_items, double w, int64_t x_items, double x) {
+  const int64_t rounds = w_items / slots, late = w_items % slots;
+  double end = rounds * w + (late ? w : 0.0);
+  // x's items fill the slots that end early, then all of them
+  const double early = rounds * w, gap = late ? w : 0.0;
+  const int64_t in_gap = late ? (slots - late) * static_cast<int64_t>(gap / x) : 0;
+  if (x_items <= in_gap) return std::max(end, early + x * std::ceil(double(x_items) / std::max<int64_t>(1, slots - late)));
+  const int64_t left = x_items - in_gap;
+  return std::max(end, early + gap) + x * std::ceil(double(left) / slots);
 }
 
-emb_status_t gemm(int32_t dtype, int kind, const DenseGemm& given, float* partial, void* stream) {
-  DenseGemm g = given;
-  g.partial = partial;
-  const Choice c = choose(dtype, kind, g.ni, g.nj, g.nr, g.parts);
-  g.variant = c.variant, g.splits = c.splits;
+GradChoice choose_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, int mats, bool want_x, int want_w, bool sums) {
+  static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
+  const int64_t w_steps = steps_of(dtype, m), x_steps = steps_of(dtype, n) * mats;
+  const double w_bytes = 4.0 * n * k * want_w, x_bytes = 4.0 * m * k;
+  GradChoice best = {kTile128, 1, 1};
+  double least = 0.0;
+  for (int variant : {kTile256, kTile128}) {
+    if (variant == kTile256 && dtype == EMB_DTYPE_F32) continue;   // (f32's reads of a reduction-major B spill registers)
+    const StepTime t = step_us(dtype, variant);
+    const int64_t w_tiles = want_w * tiles_of(variant, n, k), x_tiles = want_x ? tiles_of(variant, m, k) : 0;
+    for (int sw : kSplits) {
+      if (sw > 1 && (!want_w || sw * 4 > w_steps || w_bytes * sw > kMostPartial || w_tiles * sw > 8 * kCus)) break;
+      for (int sx : kSplits) {
+        if (sx > 1 && (!want_x || sx * 4 > x_steps || x_bytes * sx > kMostPartial || x_tiles * sx > 8 * kCus)) break;
+        const int64_t items = w_tiles * sw + x_tiles * sx;
+        const bool few = items <= kCus;
+        const int64_t slots = variant == kTile256 || few ? kCus : 2 * kCus;
+        const double step = few ? t.alone + (variant == kTile256 ? (t.full - t.alone) * items / kCus : 0.0) : t.full;
+        double us = both_us(slots, w_tiles * sw, (w_steps + sw - 1) / sw * step + kTileUs, x_tiles * sx,
+                            (x_steps + sx - 1) / sx * step + kTileUs);
+        if (sw > 1 || sx > 1 || sums) us += kLaunchUs;
+        us += ((sw > 1 ? w_bytes * sw : 0.0) + (sx > 1 ? x_bytes * sx : 0.0)) / kJoinBytes;
+        if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, sw, sx};
+      }
+    }
+  }
+  return best;
+}
+
+// bytes of partial sums: rows of whole eights
+size_t partial_bytes(int64_t rows, int64_t columns, int results, int splits) {
+  return splits > 1 ? size_t(splits) * rows * ((columns + 7) / 8 * 8) * results * 4 : 0;
+}
+
+emb_status_t forward(int32_t dtype, int kind, const DenseGemm& g, void* stream) {
   switch (dtype) {
-    case EMB_DTYPE_F32: return run(dense_gemm_f32(kind, g, stream));
-    case EMB_DTYPE_F16: return run(dense_gemm_f16(kind, g, stream));
-    default: return run(dense_gemm_bf16(kind, g, stream));
+    case EMB_DTYPE_F32: return run(dense_forward_f32(kind, g, stream));
+    case EMB_DTYPE_F16: return run(dense_forward_f16(kind, g, stream));
+    default: return run(dense_forward_bf16(kind, g, stream));
+  }
+}
+
+emb_status_t backward(int32_t dtype, const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, int variant, void* stream) {
+  switch (dtype) {
+    case EMB_DTYPE_F32: return run(dense_backward_f32(w, x, c, variant, stream));
+    case EMB_DTYPE_F16: return run(dense_backward_f16(w, x, c, variant, stream));
+    default: return run(dense_backward_bf16(w, x, c, variant, stream));
   }
 }
 
@@ -155,14 +215,6 @@ emb_status_t slope(int32_t dtype, const DenseSlope& s, void* stream) {
     case EMB_DTYPE_F32: return run(dense_slope_f32(s, stream));
     case EMB_DTYPE_F16: return run(dense_slope_f16(s, stream));
     default: return run(dense_slope_bf16(s, stream));
-  }
-}
-
-emb_status_t colsum(int32_t dtype, const DenseColsum& s, void* stream) {
-  switch (dtype) {
-    case EMB_DTYPE_F32: return run(dense_colsum_f32(s, stream));
-    case EMB_DTYPE_F16: return run(dense_colsum_f16(s, stream));
-    default: return run(dense_colsum_bf16(s, stream));
   }
 }
 
@@ -230,7 +282,9 @@ struct Space {
   Operand x, w[2], dz[2];
   DensePack pack;
   float* colsum[2] = {nullptr, nullptr};
-  float* partial = nullptr;   // of one product after the other
+  float* partial = nullptr;                   // of the forward product
+  GradChoice grads = {kTile128, 1, 1};        // of the backward calls
+  float *w_partial = nullptr, *x_partial = nullptr;
   int32_t blocks = 1;         // of rows of column sums
   bool slopes = false;        // dz is computed
 };
@@ -238,25 +292,25 @@ struct Space {
 Space linear_space(Arena& ar, const emb_linear_t& a) {
   Space s;
   Packer pk{ar, a.dtype};
-  s.choice = choose(a.dtype, kForward, a.m, a.n, a.k, 1);
+  s.choice = choose_forward(a.dtype, kForward, a.m, a.n, a.k);
   pk.where_they_lie = s.choice.variant >= kRows;
   s.x = pk.use(a.x, a.ldx, a.m, a.k);
   s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k);
   s.pack = pk.pack;
-  s.partial = ar.take<float>(partial_bytes(a.dtype, kForward, a.m, a.n, a.k, 1));
+  s.partial = ar.take<float>(partial_bytes(a.m, a.n, 1, s.choice.splits));
   return s;
 }
 
 Space gated_space(Arena& ar, const emb_gated_t& a) {
   Space s;
   Packer pk{ar, a.dtype};
-  s.choice = choose(a.dtype, kGated, a.m, a.n, a.k, 1);
+  s.choice = choose_forward(a.dtype, kGated, a.m, a.n, a.k);
   pk.where_they_lie = s.choice.variant >= kRows;
   s.x = pk.use(a.x, a.ldx, a.m, a.k);
   s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k);
   s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k);
   s.pack = pk.pack;
-  s.partial = ar.take<float>(partial_bytes(a.dtype, kGated, a.m, a.n, a.k, 1));
+  s.partial = ar.take<float>(partial_bytes(a.m, a.n, 2, s.choice.splits));
   return s;
 }
 
@@ -268,6 +322,13 @@ Operand dz_space(Arena& ar, int64_t m, int64_t n, int32_t dtype) {
 
 float* colsum_space(Arena& ar, bool wanted, int32_t blocks, int64_t n) {
   return wanted ? ar.take<float>(size_t(blocks) * n * 4) : nullptr;
+}
+
+void partial_space(Arena& ar, Space& s, int32_t dtype, int64_t m, int64_t n, int64_t k, int mats, bool want_x, int want_w,
+                   bool sums) {
+  s.grads = choose_backward(dtype, m, n, k, mats, want_x, want_w, sums);
+  s.w_partial = ar.take<float>(partial_bytes(n, k, want_w, s.grads.w_splits));
+  s.x_partial = ar.take<float>(partial_bytes(m, k, 1, s.grads.x_splits));
 }
 
 Space linear_grad_space(Arena& ar, const emb_linear_grad_t& a) {
@@ -282,8 +343,7 @@ Space linear_grad_space(Arena& ar, const emb_linear_grad_t& a) {
   s.pack = pk.pack;
   s.blocks = slope_blocks(a.m, a.n);
   s.colsum[0] = colsum_space(ar, a.dbias, s.blocks, a.n);
-  s.partial = ar.take<float>(std::max(dx ? partial_bytes(a.dtype, kInputGrad, a.m, a.k, a.n, 1) : 0,
-                                      a.dweight ? partial_bytes(a.dtype, kWeightGrad, a.n, a.k, a.m, 1) : 0));
+  partial_space(ar, s, a.dtype, a.m, a.n, a.k, 1, dx, a.dweight ? 1 : 0, a.dbias);
   return s;
 }
 
@@ -303,8 +363,7 @@ Space gated_grad_space(Arena& ar, const emb_gated_grad_t& a) {
   s.blocks = slope_blocks(a.m, a.n);
   s.colsum[0] = colsum_space(ar, a.db_gate, s.blocks, a.n);
   s.colsum[1] = colsum_space(ar, a.db_up, s.blocks, a.n);
-  s.partial = ar.take<float>(std::max(dx ? partial_bytes(a.dtype, kInputGrad, a.m, a.k, a.n, 2) : 0,
-                                      weights ? partial_bytes(a.dtype, kWeightGrad, a.n, a.k, a.m, weights) : 0));
+  partial_space(ar, s, a.dtype, a.m, a.n, a.k, 2, dx, weights, a.db_gate || a.db_up);
   return s;
 }
 
@@ -348,8 +407,9 @@ emb_status_t emb_linear(const emb_linear_t* a, void* workspace, size_t workspace
   g.res = a->residual, g.ldr = a->ldr;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
   g.parts = 1, g.act = a->activation;
+  g.variant = sp.choice.variant, g.splits = sp.choice.splits, g.partial = sp.partial;
   g.whole = whole(a->x, a->ldx, a->k, a->dtype) && whole(a->weight, a->ldw, a->k, a->dtype);
-  return gemm(a->dtype, kForward, g, sp.partial, stream);
+  return forward(a->dtype, kForward, g, stream);
 }
 
 emb_status_t emb_linear_backward_workspace(const emb_linear_grad_t* a, size_t* bytes) {
@@ -386,27 +446,24 @@ emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, si
     s.log_x = slope_log_x(a->n);
     s.whole = whole16(a->dy, a->lddy, a->n, a->dtype) && (!slopes || whole16(a->z, a->ldz, a->n, a->dtype));
     EMBX_TRY(slope(a->dtype, s, stream));
-    if (a->dbias) {
-      const DenseColsum c = {{sp.colsum[0], nullptr}, {a->dbias, nullptr}, sp.blocks, static_cast<int32_t>(a->n)};
-      EMBX_TRY(colsum(a->dtype, c, stream));
-    }
   }
-  DenseGemm g = {};
-  g.a[0] = sp.dz[0].p, g.lda = sp.dz[0].ld;
-  g.parts = 1;
+  DenseGemm w = {}, x = {};
   if (a->dx && a->m > 0) {
-    g.b[0] = sp.w[0].p, g.ldb[0] = sp.w[0].ld;
-    g.c[0] = a->dx, g.ldc[0] = a->lddx;
-    g.ni = a->m, g.nj = a->k, g.nr = a->n;
-    EMBX_TRY(gemm(a->dtype, kInputGrad, g, sp.partial, stream));
+    x.a[0] = sp.dz[0].p, x.lda = sp.dz[0].ld;
+    x.b[0] = sp.w[0].p, x.ldb[0] = sp.w[0].ld;
+    x.c[0] = a->dx, x.ldc[0] = a->lddx;
+    x.ni = a->m, x.nj = a->k, x.nr = a->n, x.parts = 1;
+    x.splits = sp.grads.x_splits, x.partial = sp.x_partial;
   }
   if (a->dweight) {
-    g.b[0] = sp.x.p, g.ldb[0] = sp.x.ld;
-    g.c[0] = a->dweight, g.ldc[0] = a->lddw;
-    g.ni = a->n, g.nj = a->k, g.nr = a->m;
-    EMBX_TRY(gemm(a->dtype, kWeightGrad, g, sp.partial, stream));
+    w.a[0] = sp.dz[0].p, w.lda = sp.dz[0].ld;
+    w.b[0] = sp.x.p, w.ldb[0] = sp.x.ld;
+    w.c[0] = a->dweight, w.ldc[0] = a->lddw;
+    w.ni = a->n, w.nj = a->k, w.nr = a->m, w.parts = 1;
+    w.splits = sp.grads.w_splits, w.partial = sp.w_partial;
   }
-  return EMB_OK;
+  const DenseColsum c = {{sp.colsum[0], nullptr}, {a->dbias, nullptr}, sp.blocks, static_cast<int32_t>(a->n)};
+  return backward(a->dtype, w, x, c, sp.grads.variant, stream);
 }
 
 emb_status_t emb_gated_workspace(const emb_gated_t* a, size_t* bytes) {
@@ -444,9 +501,10 @@ emb_status_t emb_gated(const emb_gated_t* a, void* workspace, size_t workspace_b
   g.bias[0] = a->b_gate, g.bias[1] = a->b_up;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
   g.parts = 1, g.act = a->activation;
+  g.variant = sp.choice.variant, g.splits = sp.choice.splits, g.partial = sp.partial;
   g.whole = whole(a->x, a->ldx, a->k, a->dtype) && whole(a->w_gate, a->ld_gate, a->k, a->dtype) &&
             whole(a->w_up, a->ld_up, a->k, a->dtype);
-  return gemm(a->dtype, kGated, g, sp.partial, stream);
+  return forward(a->dtype, kGated, g, stream);
 }
 
 emb_status_t emb_gated_backward_workspace(const emb_gated_grad_t* a, size_t* bytes) {
@@ -493,33 +551,30 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
     s.whole = whole16(a->dh, a->lddh, a->n, a->dtype) && whole16(a->g, a->ldg, a->n, a->dtype) &&
               whole16(a->u, a->ldu, a->n, a->dtype);
     EMBX_TRY(slope(a->dtype, s, stream));
-    if (sums) {
-      const DenseColsum c = {{sp.colsum[0], sp.colsum[1]}, {a->db_gate, a->db_up}, sp.blocks, static_cast<int32_t>(a->n)};
-      EMBX_TRY(colsum(a->dtype, c, stream));
-    }
   }
-  DenseGemm g = {};
-  g.lda = sp.dz[0].ld;
+  DenseGemm w = {}, x = {};
   if (a->dx && a->m > 0) {
-    for (int i = 0; i < 2; ++i) g.a[i] = sp.dz[i].p, g.b[i] = sp.w[i].p, g.ldb[i] = sp.w[i].ld;
-    g.c[0] = a->dx, g.ldc[0] = a->lddx;
-    g.ni = a->m, g.nj = a->k, g.nr = a->n, g.parts = 2;
-    EMBX_TRY(gemm(a->dtype, kInputGrad, g, sp.partial, stream));
+    for (int i = 0; i < 2; ++i) x.a[i] = sp.dz[i].p, x.b[i] = sp.w[i].p, x.ldb[i] = sp.w[i].ld;
+    x.lda = sp.dz[0].ld;
+    x.c[0] = a->dx, x.ldc[0] = a->lddx;
+    x.ni = a->m, x.nj = a->k, x.nr = a->n, x.parts = 2;
+    x.splits = sp.grads.x_splits, x.partial = sp.x_partial;
   }
   if (weights) {
-    g.parts = 0;
     for (int i = 0; i < 2; ++i) {
       void* dw = i == 0 ? a->dw_gate : a->dw_up;
       if (!dw) continue;
-      g.a[g.parts] = sp.dz[i].p;
-      g.c[g.parts] = dw, g.ldc[g.parts] = i == 0 ? a->ldd_gate : a->ldd_up;
-      ++g.parts;
+      w.a[w.parts] = sp.dz[i].p;
+      w.c[w.parts] = dw, w.ldc[w.parts] = i == 0 ? a->ldd_gate : a->ldd_up;
+      ++w.parts;
     }
-    g.b[0] = g.b[1] = sp.x.p, g.ldb[0] = g.ldb[1] = sp.x.ld;
-    g.ni = a->n, g.nj = a->k, g.nr = a->m;
-    EMBX_TRY(gemm(a->dtype, kWeightGrad, g, sp.partial, stream));
+    w.lda = sp.dz[0].ld;
+    w.b[0] = w.b[1] = sp.x.p, w.ldb[0] = w.ldb[1] = sp.x.ld;
+    w.ni = a->n, w.nj = a->k, w.nr = a->m;
+    w.splits = sp.grads.w_splits, w.partial = sp.w_partial;
   }
-  return EMB_OK;
+  const DenseColsum c = {{sp.colsum[0], sp.colsum[1]}, {a->db_gate, a->db_up}, sp.blocks, static_cast<int32_t>(a->n)};
+  return backward(a->dtype, w, x, c, sp.grads.variant, stream);
 }
 
 }  // extern "C"
