@@ -385,18 +385,18 @@ emb_status_t emb_linear_workspace(const emb_linear_t* a, size_t* bytes) {
 }
 
 emb_status_t emb_linear(const emb_linear_t* a, void* workspace, size_t workspace_bytes, void* stream) {
-  size_t need = 0;
-  EMBX_TRY(emb_linear_workspace(a, &need));
+  if (!a) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_shape(a->m, a->n, a->k, a->dtype, a->activation));
   EMBX_TRY(check_matrix(a->x, a->ldx, a->m, a->k, a->dtype));
   EMBX_TRY(check_matrix(a->weight, a->ldw, a->n, a->k, a->dtype));
   EMBX_TRY(check_vector(a->bias, a->dtype));
   EMBX_TRY(check_optional(a->residual, a->ldr, a->m, a->n, a->dtype));
   EMBX_TRY(check_matrix(a->y, a->ldy, a->m, a->n, a->dtype));
   EMBX_TRY(check_optional(a->z, a->ldz, a->m, a->n, a->dtype));
-  EMBX_TRY(check_workspace(workspace, workspace_bytes, need));
-  if (a->m == 0) return EMB_OK;
   Arena ar{static_cast<char*>(workspace)};
   const Space sp = linear_space(ar, *a);
+  EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
+  if (a->m == 0) return EMB_OK;
   EMBX_TRY(run_pack(sp.pack, stream));
   DenseGemm g = {};
   g.a[0] = sp.x.p, g.lda = sp.x.ld;
@@ -422,8 +422,8 @@ emb_status_t emb_linear_backward_workspace(const emb_linear_grad_t* a, size_t* b
 }
 
 emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, size_t workspace_bytes, void* stream) {
-  size_t need = 0;
-  EMBX_TRY(emb_linear_backward_workspace(a, &need));
+  if (!a) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_shape(a->m, a->n, a->k, a->dtype, a->activation));
   const bool slopes = a->activation != EMB_ACT_NONE;
   EMBX_TRY(check_matrix(a->dy, a->lddy, a->m, a->n, a->dtype));
   if (slopes) EMBX_TRY(check_matrix(a->z, a->ldz, a->m, a->n, a->dtype));
@@ -432,9 +432,9 @@ emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, si
   EMBX_TRY(check_optional(a->dx, a->lddx, a->m, a->k, a->dtype));
   EMBX_TRY(check_optional(a->dweight, a->lddw, a->n, a->k, a->dtype));
   EMBX_TRY(check_vector(a->dbias, a->dtype));
-  EMBX_TRY(check_workspace(workspace, workspace_bytes, need));
   Arena ar{static_cast<char*>(workspace)};
   const Space sp = linear_grad_space(ar, *a);
+  EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
   EMBX_TRY(run_pack(sp.pack, stream));
   if (a->dbias || sp.slopes) {
     DenseSlope s = {};
@@ -476,8 +476,8 @@ emb_status_t emb_gated_workspace(const emb_gated_t* a, size_t* bytes) {
 }
 
 emb_status_t emb_gated(const emb_gated_t* a, void* workspace, size_t workspace_bytes, void* stream) {
-  size_t need = 0;
-  EMBX_TRY(emb_gated_workspace(a, &need));
+  if (!a) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_shape(a->m, a->n, a->k, a->dtype, a->activation));
   EMBX_TRY(check_matrix(a->x, a->ldx, a->m, a->k, a->dtype));
   EMBX_TRY(check_matrix(a->w_gate, a->ld_gate, a->n, a->k, a->dtype));
   EMBX_TRY(check_matrix(a->w_up, a->ld_up, a->n, a->k, a->dtype));
@@ -486,10 +486,10 @@ emb_status_t emb_gated(const emb_gated_t* a, void* workspace, size_t workspace_b
   EMBX_TRY(check_matrix(a->h, a->ldh, a->m, a->n, a->dtype));
   EMBX_TRY(check_optional(a->g, a->ldg, a->m, a->n, a->dtype));
   EMBX_TRY(check_optional(a->u, a->ldu, a->m, a->n, a->dtype));
-  EMBX_TRY(check_workspace(workspace, workspace_bytes, need));
-  if (a->m == 0) return EMB_OK;
   Arena ar{static_cast<char*>(workspace)};
   const Space sp = gated_space(ar, *a);
+  EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
+  if (a->m == 0) return EMB_OK;
   EMBX_TRY(run_pack(sp.pack, stream));
   DenseGemm g = {};
   g.a[0] = sp.x.p, g.lda = sp.x.ld;
@@ -517,8 +517,8 @@ emb_status_t emb_gated_backward_workspace(const emb_gated_grad_t* a, size_t* byt
 }
 
 emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size_t workspace_bytes, void* stream) {
-  size_t need = 0;
-  EMBX_TRY(emb_gated_backward_workspace(a, &need));
+  if (!a) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_shape(a->m, a->n, a->k, a->dtype, a->activation));
   const bool weights = a->dw_gate || a->dw_up;
   EMBX_TRY(check_matrix(a->dh, a->lddh, a->m, a->n, a->dtype));
   EMBX_TRY(check_matrix(a->g, a->ldg, a->m, a->n, a->dtype));
@@ -533,9 +533,9 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
   EMBX_TRY(check_optional(a->dw_up, a->ldd_up, a->n, a->k, a->dtype));
   EMBX_TRY(check_vector(a->db_gate, a->dtype));
   EMBX_TRY(check_vector(a->db_up, a->dtype));
-  EMBX_TRY(check_workspace(workspace, workspace_bytes, need));
   Arena ar{static_cast<char*>(workspace)};
   const Space sp = gated_grad_space(ar, *a);
+  EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
   EMBX_TRY(run_pack(sp.pack, stream));
   const bool sums = a->db_gate || a->db_up;
   if (sums || sp.slopes) {

@@ -12,8 +12,20 @@ from paper_2507_01676_amd import dense as D
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 INVALID, UNSUPPORTED = embx.ERR_INVALID_ARGUMENT, embx.ERR_UNSUPPORTED
-OPS = {"emb_linear": D._Linear, "emb_linear_backward": D._LinearGrad, "emb_gated": D._Gated,
-       "emb_gated_backward": D._GatedGrad}
+
+
+def _struct(*fields):
+    """A struct as the header lists it: sizes, type, activation, then matrices (name) and vectors (name ending in '.')."""
+    out = [(f, ctypes.c_int64) for f in "mnk"] + [("dtype", ctypes.c_int32), ("activation", ctypes.c_int32)]
+    for f in fields:
+        out += [(f[:-1], ctypes.c_void_p)] if f.endswith(".") else [(f, ctypes.c_void_p), ("ld_" + f, ctypes.c_int64)]
+    return type("Args", (ctypes.Structure,), {"_fields_": out})
+
+
+OPS = {"emb_linear": _struct("x", "weight", "bias.", "residual", "y", "z"),
+       "emb_linear_backward": _struct("dy", "x", "weight", "z", "dx", "dweight", "dbias."),
+       "emb_gated": _struct("x", "w_gate", "w_up", "b_gate.", "b_up.", "h", "g", "u"),
+       "emb_gated_backward": _struct("dh", "x", "w_gate", "w_up", "g", "u", "dx", "dw_gate", "dw_up", "db_gate.", "db_up.")}
 M, N, K = 24, 40, 56
 SHAPE_OF = {"x": (M, K), "weight": (N, K), "w_gate": (N, K), "w_up": (N, K), "dx": (M, K), "dweight": (N, K),
             "dw_gate": (N, K), "dw_up": (N, K)}          # all other matrices are [M, N]
@@ -36,14 +48,18 @@ def good(op, **changes):
     return a
 
 
+def _bytes(a):
+    return None if a is None else bytes(a)
+
+
 def size(op, a):
     n = ctypes.c_size_t(0)
-    code = getattr(embx._lib, op + "_workspace")(ctypes.byref(a) if a is not None else None, ctypes.byref(n))
+    code = getattr(embx._lib, op + "_workspace")(_bytes(a), ctypes.byref(n))
     return code, n.value
 
 
 def call(op, a, ws=FAKE, nbytes=1 << 60):
-    return getattr(embx._lib, op)(ctypes.byref(a) if a is not None else None, ws, nbytes, None)
+    return getattr(embx._lib, op)(_bytes(a), ws, nbytes, None)
 
 
 @pytest.mark.parametrize("op", OPS)
@@ -56,7 +72,7 @@ def test_bad_sizes_types_and_activations(op):
         assert size(op, good(op, **change))[0] == code, change
     assert call(op, None) == INVALID
     assert size(op, None)[0] == INVALID
-    assert getattr(embx._lib, op + "_workspace")(ctypes.byref(good(op)), None) == INVALID
+    assert getattr(embx._lib, op + "_workspace")(bytes(good(op)), None) == INVALID
 
 
 @pytest.mark.parametrize("op", OPS)
@@ -108,6 +124,7 @@ def test_header_compiles_and_agrees_with_the_binding(tmp_path, lang):
     assert r.returncode == 0, r.stderr
     out = subprocess.run([str(exe)], capture_output=True, text=True, timeout=60).stdout
     assert [int(v) for v in out.split()] == [ctypes.sizeof(s) for s in OPS.values()]
+    assert [e.bytes for e in (D._linear, D._linear_backward, D._gated, D._gated_backward)] == [ctypes.sizeof(s) for s in OPS.values()]
 
 
 def test_binding_refuses_host_tensors():
@@ -117,14 +134,4 @@ def test_binding_refuses_host_tensors():
                   lambda: embx.linear_backward(torch.zeros(3, 5), x, w),
                   lambda: embx.gated_ffn_backward(torch.zeros(3, 5), x, w, w, torch.zeros(3, 5), torch.zeros(3, 5))):
         with pytest.raises(ValueError):
-            _without_a_stream(call_)
-
-
-def _without_a_stream(fn):
-    """The binding asks for the current stream first; without a GPU there is none to ask for."""
-    saved = D._current_stream_ptr
-    D._current_stream_ptr = lambda: 0
-    try:
-        return fn()
-    finally:
-        D._current_stream_ptr = saved
+            call_()
