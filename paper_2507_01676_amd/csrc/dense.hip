@@ -159,6 +159,8 @@ __device__ inline void stage_done() {
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(LOADS) : "memory");
 }
 
+__device__ f32x4 buffer_load_f32x4(i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.load.v4f32");
+
 template <int TYPE>
 __device__ inline f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
   using V = typename Elem<TYPE>::V;
@@ -182,7 +184,7 @@ struct Tile {
 
   // the permutation of a row's chunks
   __device__ static int swizzle(int row) {
-    if (RM && ESIZE == 4) return ((row >> 2) & 3) << 2;
+    if (ESIZE == 4) return 0;   // read along its rows
     if (RM) return (kChunks >= 16 ? (row & 3) | ((row >> 1) & 4) : row & 3) << 1;
     return (row >> 1) & 7;
   }
@@ -229,24 +231,6 @@ struct Tile {
       return *reinterpret_cast<const s16x8*>(tile + row * kRowBytes + (((ks * 4 + q) ^ swizzle(row)) << 4));
     }
   }
-
-  // f32: the same fragment's values; lane: reduction 4 (lane / 16) .. + 3 and 16 + 4 (lane / 16) .. + 3
-  __device__ static void fragment(const char* tile, int first, int lane, float* v) {
-    const int q = lane >> 4, c = lane & 15;
-    if constexpr (RM) {
-      const char* p = tile + 4 * q * kRowBytes + ((((first + c) >> 2) ^ (q << 2)) << 4) + (c & 3) * 4;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = *reinterpret_cast<const float*>(p + ((e & 3) + (e >> 2) * 16) * kRowBytes);
-    } else {
-      const int row = first + c;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(tile + row * kRowBytes + (((h * 4 + q) ^ swizzle(row)) << 4));
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[h * 4 + e] = x[e];
-      }
-    }
-  }
 };
 
 // f32 products.  The matrix cores multiply f32 at a sixteenth of their bf16 rate.  So each f32 value is taken as a sum of
@@ -274,11 +258,89 @@ __device__ inline Parts split3(const float* v) {
 #pragma unroll
     for (int p = 0; p < 3; ++p) {
       part[p][e] = round2(a, b);
-      a -= __builtin_bit_cast(float, part[p][e] << 16), b -= __builtin_bit_cast(float, part[p][e] & 0xffff0000u);
+      a -= __uint_as_float(part[p][e] << 16), b -= __uint_as_float(part[p][e] & 0xffff0000u);
     }
   }
   return {{__builtin_bit_cast(s16x8, part[0]), __builtin_bit_cast(s16x8, part[1]), __builtin_bit_cast(s16x8, part[2])}};
 }
+
+// The parts of a tile of f32 (ROWS results by 32 of the reduction) in LDS: a tile of bf16 for each.  Taken apart once for
+// the workgroup, not at each wavefront's fragments: the matrix cores and the other vector instructions of a SIMD hardly
+// overlap (with both in turns a step took the sum of their times), so every instruction of the latter counts.
+template <int ROWS, bool RM, int WAVES>
+struct PartTile {
+  static constexpr int kBytes = ROWS * 64;                     // of a part
+  static constexpr int kRowBytes = RM ? ROWS * 2 : 64, kChunks = kRowBytes / 16;   // chunks of eight values
+  static constexpr int kPieces = (ROWS * 4 + 64 * WAVES - 1) / (64 * WAVES);   // of a thread
+
+  __device__ static int swizzle(int row) {
+    if (RM) return (kChunks >= 16 ? (row & 3) | ((row >> 1) & 4) : row & 3) << 1;
+    return -(row >> 2) & 3;
+  }
+
+  // A thread's pieces of eight values: loaded from memory (what lies outside is read as zeros), then taken apart and
+  // written to the parts, `plane` bytes apart.
+  int voff[kPieces][2];
+  f32x4 held[kPieces][2];
+
+  __device__ static bool mine(int at) { return ROWS * 4 >= 64 * WAVES || at < ROWS * 4; }
+
+  // rows: valid rows (RM: valid columns, whole chunks) from the tile's origin on
+  __device__ void init(int tid, int64_t ld, int rows) {
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n) {
+      const int at = n * 64 * WAVES + tid, row = at / kChunks, first = at % kChunks * 8;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        voff[n][h] = mine(at) && (RM ? first + 4 * h < rows : row < rows) ? static_cast<int>(row * ld * 4) + (first + 4 * h) * 4
+                                                                          : kOutOfRange;
+    }
+  }
+
+  // valid: how many of this step's 32 are inside
+  __device__ void load(i32x4 rsrc, int tid, int valid) {
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n) {
+      const int at = n * 64 * WAVES + tid, row = at / kChunks, first = at % kChunks * 8;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        int v = voff[n][h];
+        if (valid < 32) v = (RM ? row < valid : first + 4 * h < valid) ? v : kOutOfRange;
+        held[n][h] = buffer_load_f32x4(rsrc, v, 0, 0);
+      }
+    }
+  }
+
+  __device__ void take_apart(char* to, int plane, int tid) const {
+#pragma unroll
+    for (int n = 0; n < kPieces; ++n) {
+      const int at = n * 64 * WAVES + tid, row = at / kChunks, chunk = at % kChunks;
+      if (!mine(at)) break;
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = held[n][e / 4][e % 4];
+      const Parts parts = split3(v);
+      char* p = to + row * kRowBytes + ((chunk ^ swizzle(row)) << 4);
+#pragma unroll
+      for (int part = 0; part < 3; ++part) *reinterpret_cast<s16x8*>(p + part * plane) = parts.p[part];
+    }
+  }
+
+  // as Tile::fragment
+  __device__ static s16x8 fragment(const char* tile, int first, int lane) {
+    const int q = lane >> 4, c = lane & 15;
+    if constexpr (RM) {
+      const int r = 8 * q + (c >> 2);
+      const char* p = tile + r * kRowBytes + (((first >> 4) ^ (swizzle(r) >> 1)) << 5) + (c & 3) * 8;
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))p);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LDS_PTR(s16x4))(p + 4 * kRowBytes));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      const int row = first + c;
+      return *reinterpret_cast<const s16x8*>(tile + row * kRowBytes + ((q ^ swizzle(row)) << 4));
+    }
+  }
+};
 
 // c[fi][fj] += the products of FI by FJ fragments
 template <int FI, int FJ>
@@ -412,32 +474,36 @@ struct Finish {
   }
 };
 
-// Stores a wavefront's sums, from row i0 and column j0 on, through 16 KB of LDS of its own: 64 x 64 sums at a time, so
+// Stores a wavefront's sums, from row i0 and column j0 on, through LDS of its own: 64 rows of FJ * 16 sums at a time, so
 // that a lane has eight consecutive columns and the activation's code is there once.  Lane (q, c) holds row c and
-// columns 4 q .. + 3 of each fragment.  Rows of 256 bytes, their 16-byte chunks permuted by the row.
+// columns 4 q .. + 3 of each fragment.  The 16-byte chunks of a row in LDS are permuted by the row.
+template <int FJ>
+constexpr int kSumsLds = 64 * FJ * 64;
+
 template <int TYPE, int KIND, int FI, int FJ>
 __device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char* own, int lane, int64_t i0, int j0, int part,
                                   int split) {
   constexpr bool kGate = KIND == kGated;
+  constexpr int kRowBytes = FJ * 64, kMask = FJ * 4 - 1, kUp = FJ * 2;   // kUp: first chunk of the up projection
   const int q = lane >> 4, c = lane & 15;
 #pragma unroll
   for (int h = 0; h < FI / 4; ++h) {
 #pragma unroll
     for (int fi = 0; fi < 4; ++fi)
 #pragma unroll
-      for (int fj = 0; fj < 4; ++fj)
-        *reinterpret_cast<f32x4*>(own + (fi * 16 + c) * 256 + (((fj * 4 + q) ^ c) << 4)) = acc[h * 4 + fi][fj];
+      for (int fj = 0; fj < FJ; ++fj)
+        *reinterpret_cast<f32x4*>(own + (fi * 16 + c) * kRowBytes + (((fj * 4 + q) ^ (c & kMask)) << 4)) = acc[h * 4 + fi][fj];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    constexpr int kLanes = kGate ? 4 : 8, kRows = 64 / kLanes;   // lanes of a row, rows at a time
-    const int e = lane % kLanes * 2, j = j0 + e * 4;             // the row's first chunk of this lane
+    constexpr int kLanes = kGate ? FJ : FJ * 2, kRows = 64 / kLanes;   // lanes of a row, rows at a time
+    const int e = lane % kLanes * 2, j = j0 + e * 4;                   // the row's first chunk of this lane
     const int64_t first = i0 + h * 64 + lane / kLanes;
     auto sums = [&](int row, float* s0, float* s1) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(own + row * 256 + (((e + x) ^ (row & 15)) << 4));
+        const f32x4 v = *reinterpret_cast<const f32x4*>(own + row * kRowBytes + (((e + x) ^ (row & kMask)) << 4));
         s0[4 * x] = v[0], s0[4 * x + 1] = v[1], s0[4 * x + 2] = v[2], s0[4 * x + 3] = v[3];
         if constexpr (kGate) {
-          const f32x4 w = *reinterpret_cast<const f32x4*>(own + row * 256 + (((8 + e + x) ^ (row & 15)) << 4));
+          const f32x4 w = *reinterpret_cast<const f32x4*>(own + row * kRowBytes + (((kUp + e + x) ^ (row & kMask)) << 4));
           s1[4 * x] = w[0], s1[4 * x + 1] = w[1], s1[4 * x + 2] = w[2], s1[4 * x + 3] = w[3];
         }
       }
@@ -514,15 +580,16 @@ __device__ __noinline__ void tile_by_f32(const DenseGemm& g, char* lds, int i0, 
     }
   }
   __syncthreads();
-  store_sums<kDenseF32, KIND, FI, FJ>(g, acc, lds + (tid >> 6) * 16384, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
+  store_sums<kDenseF32, KIND, FI, FJ>(g, acc, lds + (tid >> 6) * kSumsLds<FJ>, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
 }
 
-// bytes of LDS of a tile: the steps under way, and 16 KB a wavefront for the epilogue
-template <int TYPE, int BM, int BN, int WAVES>
+// bytes of LDS of a tile: the steps under way, or what the epilogue takes
+template <int TYPE, int BM, int BN, int WJ, int WAVES>
 constexpr int kTileLds = [] {
-  const bool turns = WAVES == 8 && TYPE != kDenseF32;
-  const int steps = ((turns ? 3 : 2) * BM + 2 * BN) * 128;
-  return steps > WAVES * 16384 ? steps : WAVES * 16384;
+  const int steps = TYPE == kDenseF32 ? (BM + BN) * 64 * 3 * 2     // three bf16 parts of two steps
+                                      : ((WAVES == 8 ? 3 : 2) * BM + 2 * BN) * 128;
+  const int sums = WAVES * kSumsLds<BN / WJ / 16>;
+  return steps > sums ? steps : sums;
 }();
 
 // One tile of a product: `tile` of its tiles, `split` of its splits, `wpart` of kWeightGrad's two results.
@@ -531,18 +598,18 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
   constexpr bool kGate = KIND == kGated;
   constexpr bool kRmA = KIND == kWeightGrad, kRmB = KIND == kWeightGrad || KIND == kInputGrad;
   constexpr int kWaves = WI * WJ;
-  constexpr bool kTurns = kWaves == 8 && TYPE != kDenseF32;   // see the main loop
-  constexpr int kSlotsA = kTurns ? 3 : 2, kSlotsB = 2;     // tiles of steps in LDS
+  constexpr bool kF32 = TYPE == kDenseF32;
+  constexpr bool kTurns = kWaves == 8 && !kF32;                   // see the main loop
+  constexpr int kSlotsA = kF32 ? 1 : kTurns ? 3 : 2, kSlotsB = kF32 ? 1 : 2;   // tiles of steps in LDS
   constexpr int kCols = kGate ? BN / 2 : BN;               // result columns of a tile
   constexpr int kWI = BM / WI, kWJ = kCols / WJ;           // results of a wavefront
   constexpr int kFI = kWI / 16, kFJ = BN / WJ / 16;        // its fragments
-  constexpr bool kF32 = TYPE == kDenseF32;
   constexpr int kSize = kF32 ? 4 : 2;
   using TileA = Tile<BM, kRmA, kWaves, kSize>;
   using TileB = Tile<BN, kRmB, kWaves, kSize>;
   using TileH = Tile<kCols, kRmB, kWaves, kSize>;          // one projection's half of B
   constexpr int BK = TileA::BK;
-  static_assert(kSlotsA * TileA::kBytes + kSlotsB * TileB::kBytes <= kTileLds<TYPE, BM, BN, kWaves>);
+  static_assert(kF32 || kSlotsA * TileA::kBytes + kSlotsB * TileB::kBytes <= kTileLds<TYPE, BM, BN, WJ, kWaves>);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int ti, tj;
@@ -612,7 +679,7 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
 
   const int wi = (wave / WJ) * kWI, wj = (wave % WJ) * kWJ;
   f32x4 acc[kFI][kFJ] = {};
-  // fragments of a half step (16 bits), or values of a step's (f32)
+  // fragments of a half step (16 bits)
   auto fragments_a = [&](const char* sa, int ks, s16x8* f) {
 #pragma unroll
     for (int n = 0; n < kFI; ++n) f[n] = TileA::fragment(sa, wi + n * 16, ks, lane);
@@ -626,15 +693,70 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
         f[n] = TileB::fragment(sb, wj + n * 16, ks, lane);
     }
   };
-  auto value_a = [&](const char* sa, int n, float* v) { TileA::fragment(sa, wi + n * 16, lane, v); };
-  auto value_b = [&](const char* sb, int n, float* v) {
-    if constexpr (kGate) TileH::fragment(sb + (n >= kFJ / 2) * TileH::kBytes, wj + (n % (kFJ / 2)) * 16, lane, v);
-    else TileB::fragment(sb, wj + n * 16, lane, v);
-  };
   int at_a = 0, at_b = 0;   // slots of the step that is multiplied
-  if constexpr (!kTurns) {
+  if constexpr (kF32) {
+    // The parts of two steps lie in LDS: while one is multiplied, the next, whose values are in registers, is taken apart,
+    // and the one after it is loaded.
+    using PartA = PartTile<BM, kRmA, kWaves>;
+    using PartB = PartTile<kGate ? kCols : BN, kRmB, kWaves>;
+    constexpr int kMats = kGate ? 2 : 1, kPlane = PartA::kBytes + kMats * PartB::kBytes;
+    PartA va;
+    PartB vb[kMats];
+    va.init(tid, g.lda, g.ni - i0);
+#pragma unroll
+    for (int m = 0; m < kMats; ++m) vb[m].init(tid, g.ldb[m], g.nj - j0);
+    auto fetch = [&](int step) {
+      const int part = KIND == kInputGrad && step >= per_part && g.parts > 1 ? 1 : 0;
+      const int r0 = (step - part * per_part) * BK, valid = step < end ? g.nr - r0 : 0;
+      const float* a = static_cast<const float*>(g.a[KIND == kWeightGrad ? wpart : part]);
+      va.load(descriptor(a + (kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0)), tid, valid);
+      if constexpr (KIND == kInputGrad) {
+        if (part != tb_part) {
+          vb[0].init(tid, g.ldb[part], g.nj - j0);
+          tb_part = part;
+        }
+      }
+#pragma unroll
+      for (int m = 0; m < kMats; ++m) {
+        const int mat = kGate ? m : part;
+        const float* b = static_cast<const float*>(g.b[mat]);
+        vb[m].load(descriptor(b + (kRmB ? int64_t(r0) * g.ldb[mat] + j0 : int64_t(j0) * g.ldb[mat] + r0)), tid, valid);
+      }
+    };
+    auto take_apart = [&](int slot) {
+      char* to = lds + slot * 3 * kPlane;
+      va.take_apart(to, kPlane, tid);
+#pragma unroll
+      for (int m = 0; m < kMats; ++m) vb[m].take_apart(to + PartA::kBytes + m * PartB::kBytes, kPlane, tid);
+    };
+    fetch(begin);
+    take_apart(0);
+    fetch(begin + 1);
+    int slot = 0;
+    for (int step = begin; step < end; ++step) {
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");   // (loads stay under way)
+      const char* parts = lds + slot * 3 * kPlane;
+      slot ^= 1;
+      Parts fa[kFI], fb[kFJ];
+#pragma unroll
+      for (int p = 2; p >= 0; --p) {
+        const char* pa = parts + p * kPlane;
+        const char* pb = pa + PartA::kBytes;
+#pragma unroll
+        for (int n = 0; n < kFI; ++n) fa[n].p[p] = PartA::fragment(pa, wi + n * 16, lane);
+#pragma unroll
+        for (int n = 0; n < kFJ; ++n) {
+          if constexpr (kGate) fb[n].p[p] = PartB::fragment(pb + (n >= kFJ / 2) * PartB::kBytes, wj + (n % (kFJ / 2)) * 16, lane);
+          else fb[n].p[p] = PartB::fragment(pb, wj + n * 16, lane);
+        }
+      }
+      take_apart(slot);
+      fetch(step + 2);
+      products6<kFI, kFJ>(fa, fb, acc);
+    }
+  } else if constexpr (!kTurns) {
     // One step is on its way while another is multiplied.  Two workgroups share a CU, so that one reads while the other
-    // multiplies (f32's large tile: two wavefronts a SIMD do).
+    // multiplies.
     set_a(begin, 0);
     set_b(begin, 0);
 #pragma unroll
@@ -648,49 +770,15 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
       set_b(step + 1, at_a);
 #pragma unroll
       for (int n = 0; n < kIssues; ++n) issue(n);
-      if constexpr (kF32) {
-        // 128 rows: the next pair of A's fragments is taken apart beside the products of this one.  256 rows: registers
-        // hold one pair, and fragments in any other order than this would not fit.
-        constexpr bool kLean = kFI == 8;
-        auto keep_order = [] {
-          if constexpr (kLean) __builtin_amdgcn_sched_barrier(0);
-        };
-        Parts fa[kLean ? 1 : 2][2], fb[kFJ];
-        auto pair_a = [&](int h, Parts* f) {
 #pragma unroll
-          for (int n = 0; n < 2; ++n) {
-            float v[8];
-            value_a(sa, h + n, v);
-            f[n] = split3(v);
-          }
-          keep_order();
-        };
+      for (int ks = 0; ks < 2; ++ks) {
+        s16x8 fa[kFI], fb[kFJ];
+        fragments_b(sb, ks, fb);
+        fragments_a(sa, ks, fa);
 #pragma unroll
-        for (int n = 0; n < kFJ; ++n) {
-          float v[8];
-          value_b(sb, n, v);
-          fb[n] = split3(v);
-          keep_order();
-        }
-        if (!kLean) pair_a(0, fa[0]);
+        for (int fi = 0; fi < kFI; ++fi)
 #pragma unroll
-        for (int h = 0; h < kFI; h += 2) {
-          if (kLean) pair_a(h, fa[0]);
-          else if (h + 2 < kFI) pair_a(h + 2, fa[(h / 2 + 1) & 1]);
-          products6<2, kFJ>(fa[kLean ? 0 : (h / 2) & 1], fb, acc + h);
-          keep_order();
-        }
-      } else {
-#pragma unroll
-        for (int ks = 0; ks < BK / 32; ++ks) {
-          s16x8 fa[kFI], fb[kFJ];
-          fragments_b(sb, ks, fb);
-          fragments_a(sa, ks, fa);
-#pragma unroll
-          for (int fi = 0; fi < kFI; ++fi)
-#pragma unroll
-            for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[fj], fa[fi], acc[fi][fj]);
-        }
+          for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[fj], fa[fi], acc[fi][fj]);
       }
     }
   } else {
@@ -710,15 +798,19 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
 #pragma unroll
     for (int n = 0; n < TileA::kLoads; ++n) issue_a(n);
     stage_done<kUnderWay>();
-    s16x8 fa[BK / 32][kFI], fb[BK / 32][kFJ];
+    s16x8 fa[2][kFI], fb[2][kFJ];
     auto read = [&]() {
       const char* sa = lds + at_a * TileA::kBytes;
       const char* sb = lds + kAreaB + at_b * TileB::kBytes;
 #pragma unroll
-      for (int ks = 0; ks < BK / 32; ++ks) {
+      for (int ks = 0; ks < 2; ++ks) {
         fragments_b(sb, ks, fb[ks]);
         fragments_a(sa, ks, fa[ks]);
       }
+    };
+    auto multiply = [&](int ks, int fi) {
+#pragma unroll
+      for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[ks][fj], fa[ks][fi], acc[fi][fj]);
     };
     if (!late) {
       for (int step = begin; step < end; ++step) {
@@ -734,11 +826,9 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int ks = 0; ks < BK / 32; ++ks)
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-          for (int fi = 0; fi < kFI; ++fi)
-#pragma unroll
-            for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[ks][fj], fa[ks][fi], acc[fi][fj]);
+          for (int fi = 0; fi < kFI; ++fi) multiply(ks, fi);
         __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
         stage_done<kUnderWay>();
@@ -761,11 +851,10 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int ks = 0; ks < BK / 32; ++ks)
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
           for (int fi = 0; fi < kFI; ++fi) {
-#pragma unroll
-            for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] = mfma16<TYPE>(fb[ks][fj], fa[ks][fi], acc[fi][fj]);
+            multiply(ks, fi);
             if (ks * kFI + fi < kIssues) issue(ks * kFI + fi);
             __builtin_amdgcn_sched_barrier(0);
           }
@@ -797,12 +886,12 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
       return;
     }
   }
-  store_sums<TYPE, KIND, kFI, kFJ>(g, acc, lds + wave * 16384, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
+  store_sums<TYPE, KIND, kFI, kFJ>(g, acc, lds + wave * kSumsLds<kFJ>, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
 }
 
 template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
 __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile(DenseGemm g) {
-  __shared__ __align__(1024) char lds[kTileLds<TYPE, BM, BN, WI * WJ>];
+  __shared__ __align__(1024) char lds[kTileLds<TYPE, BM, BN, WJ, WI * WJ>];
   tile_product<TYPE, KIND, BM, BN, WI, WJ>(g, lds, blockIdx.x, blockIdx.y, 0);
 }
 
@@ -810,7 +899,7 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
 // input's, whose many short ones fill the CUs that are left (either may be absent).
 template <int TYPE, int BM, int BN, int WI, int WJ, int PER_CU>
 __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_grads(DenseGemm w, DenseGemm x, uint32_t w_groups) {
-  __shared__ __align__(1024) char lds[kTileLds<TYPE, BM, BN, WI * WJ>];
+  __shared__ __align__(1024) char lds[kTileLds<TYPE, BM, BN, WJ, WI * WJ>];
   uint32_t id = blockIdx.x;
   if (id < w_groups) {
     const uint32_t tiles = (w.ni + BM - 1) / BM * ((w.nj + BN - 1) / BN), rest = id / tiles;
@@ -1221,8 +1310,10 @@ int grads_launch(const DenseGemm& w, const DenseGemm& x, hipStream_t stream) {
 template <int TYPE>
 int backward_launch(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, int variant, hipStream_t stream) {
   int rc;
-  if constexpr (TYPE == kDenseF32) rc = grads_launch<TYPE, 128, 128, 2, 2, 2>(w, x, stream);
-  else if (variant == kTile256) rc = grads_launch<TYPE, 256, 256, 2, 4, 1>(w, x, stream);
+  if constexpr (TYPE == kDenseF32) {
+    if (variant == kTile256) rc = grads_launch<TYPE, 256, 128, 4, 2, 1>(w, x, stream);
+    else rc = grads_launch<TYPE, 128, 128, 2, 4, 1>(w, x, stream);
+  } else if (variant == kTile256) rc = grads_launch<TYPE, 256, 256, 2, 4, 1>(w, x, stream);
   else rc = grads_launch<TYPE, 128, 128, 2, 2, 2>(w, x, stream);
   if (rc != 0) return rc;
   auto joins = [](const DenseGemm& g) {
@@ -1269,8 +1360,12 @@ int forward_launch(const DenseGemm& g, hipStream_t stream) {
     if (g.nr <= 32) return short_launch<TYPE, KIND, kColumns, 1>(g, stream);
     return short_launch<TYPE, KIND, kColumns, 2>(g, stream);
   }
-  if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
-  return tile_launch<TYPE, KIND, 128, 128, 2, 2, 2>(g, stream);
+  if constexpr (TYPE == kDenseF32) {
+    if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 128, 4, 2, 1>(g, stream);
+    return tile_launch<TYPE, KIND, 128, 128, 2, 4, 1>(g, stream);
+  }
+  else if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
+  else return tile_launch<TYPE, KIND, 128, 128, 2, 2, 2>(g, stream);
 }
 
 template <int TYPE>

@@ -79,25 +79,23 @@ constexpr int64_t kFewRows = 64, kShortSum = 64;
 
 constexpr int kCus = 256;
 
-// Microseconds of a step of 128 bytes of a tile, of 256 x 256 or 128 x 128.  Measured on bf16 (f32) products of 256 to
-// 8192 rows: the large tile takes 0.97 (4.6) us on a GPU that is otherwise idle and 1.50 (5.0) us with a workgroup on
-// every CU (the clock drops, and L2 is shared); the small one 0.62 (1.6) us alone on its CU, 1.03 (2.7) us where two
-// share it.  A tile starts and ends in 3 us.
-struct StepTime { double alone, full; };
+// Microseconds of a step of 128 bytes of the reduction: where a CU has one workgroup on a GPU that is otherwise idle, and
+// where every CU is full (the clock drops, and L2 is shared), with how many.  Measured on products of 256 to 8192 rows,
+// with 16-bit types by tiles of 256 x 256 or 128 x 128, with f32 by 256 x 128 or 128 x 128.  A tile starts and ends in 3 us.
+struct StepTime { double alone, full; int per_cu; };
 
 StepTime step_us(int32_t dtype, int variant) {
-  const bool f32 = dtype == EMB_DTYPE_F32;
-  if (variant == kTile256) return f32 ? StepTime{4.6, 5.0} : StepTime{0.97, 1.50};
-  return f32 ? StepTime{1.6, 2.7} : StepTime{0.62, 1.03};
+  if (dtype == EMB_DTYPE_F32) return variant == kTile256 ? StepTime{2.05, 2.35, 1} : StepTime{1.17, 1.30, 1};
+  return variant == kTile256 ? StepTime{0.97, 1.50, 1} : StepTime{0.62, 1.03, 2};
 }
 
 constexpr double kTileUs = 3.0, kLaunchUs = 5.0;
 constexpr double kJoinBytes = 3.0e6;      // a microsecond, of partial sums written and read back
 constexpr double kMostPartial = 256 << 20;
 
-int64_t tiles_of(int variant, int64_t rows, int64_t columns) {
-  const int64_t side = variant == kTile256 ? 256 : 128;
-  return ((rows + side - 1) / side) * ((columns + side - 1) / side);
+int64_t tiles_of(int32_t dtype, int variant, int64_t rows, int64_t columns) {
+  const int64_t down = variant == kTile256 ? 256 : 128, across = variant == kTile256 && dtype != EMB_DTYPE_F32 ? 256 : 128;
+  return ((rows + down - 1) / down) * ((columns + across - 1) / across);
 }
 
 int64_t steps_of(int32_t dtype, int64_t nr) {
@@ -105,18 +103,19 @@ int64_t steps_of(int32_t dtype, int64_t nr) {
   return (nr + step - 1) / step;
 }
 
+// of a step where `groups` workgroups are on the GPU
+double step_of(const StepTime& t, double groups) {
+  if (t.per_cu == 1) return t.alone + (t.full - t.alone) * std::min(1.0, groups / kCus);
+  return groups <= kCus ? t.alone : t.full;
+}
+
 // a forward product whose reduction is split s ways
 double tile_us(int32_t dtype, int variant, double tiles, double steps, int s, double result_bytes) {
   const StepTime t = step_us(dtype, variant);
-  const double groups = tiles * s, each = std::ceil(steps / s);
-  double us;
-  if (variant == kTile256) {
-    us = std::ceil(groups / kCus) * (each * (t.alone + (t.full - t.alone) * std::min(1.0, groups / kCus)) + kTileUs);
-  } else {
-    const double whole = std::floor(groups / (2 * kCus)), rest = groups - whole * 2 * kCus;
-    us = whole * (each * t.full + kTileUs);
-    if (rest > 0) us += each * (rest <= kCus ? t.alone : t.full) + kTileUs;
-  }
+  const double groups = tiles * s, each = std::ceil(steps / s), slots = kCus * t.per_cu;
+  const double whole = std::floor(groups / slots), rest = groups - whole * slots;
+  double us = whole * (each * t.full + kTileUs);
+  if (rest > 0) us += each * (whole > 0 && t.per_cu == 1 ? t.full : step_of(t, rest)) + kTileUs;
   if (s > 1) us += kLaunchUs + result_bytes * s / kJoinBytes;
   return us;
 }
@@ -136,7 +135,7 @@ Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k) 
   double least = 0.0;
   if (m <= kFewRows) best = {kRows, 1}, least = rows_us(m, n, k);
   for (int variant : {kTile256, kTile128}) {
-    const double tiles = static_cast<double>(tiles_of(variant, m, n * mats));
+    const double tiles = static_cast<double>(tiles_of(dtype, variant, m, n * mats));
     for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial)); ++s) {
       const double us = tile_us(dtype, variant, tiles, steps, s, result_bytes);
       if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, s};
@@ -167,17 +166,14 @@ GradChoice choose_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, int m
   GradChoice best = {kTile128, 1, 1};
   double least = 0.0;
   for (int variant : {kTile256, kTile128}) {
-    if (variant == kTile256 && dtype == EMB_DTYPE_F32) continue;   // (f32's reads of a reduction-major B spill registers)
     const StepTime t = step_us(dtype, variant);
-    const int64_t w_tiles = want_w * tiles_of(variant, n, k), x_tiles = want_x ? tiles_of(variant, m, k) : 0;
+    const int64_t w_tiles = want_w * tiles_of(dtype, variant, n, k), x_tiles = want_x ? tiles_of(dtype, variant, m, k) : 0;
     for (int sw : kSplits) {
       if (sw > 1 && (!want_w || sw * 4 > w_steps || w_bytes * sw > kMostPartial || w_tiles * sw > 8 * kCus)) break;
       for (int sx : kSplits) {
         if (sx > 1 && (!want_x || sx * 4 > x_steps || x_bytes * sx > kMostPartial || x_tiles * sx > 8 * kCus)) break;
-        const int64_t items = w_tiles * sw + x_tiles * sx;
-        const bool few = items <= kCus;
-        const int64_t slots = variant == kTile256 || few ? kCus : 2 * kCus;
-        const double step = few ? t.alone + (variant == kTile256 ? (t.full - t.alone) * items / kCus : 0.0) : t.full;
+        const int64_t items = w_tiles * sw + x_tiles * sx, slots = items <= kCus ? kCus : kCus * t.per_cu;
+        const double step = step_of(t, static_cast<double>(items));
         double us = both_us(slots, w_tiles * sw, (w_steps + sw - 1) / sw * step + kTileUs, x_tiles * sx,
                             (x_steps + sx - 1) / sx * step + kTileUs);
         if (sw > 1 || sx > 1 || sums) us += kLaunchUs;
