@@ -1176,6 +1176,30 @@ __global__ __launch_bounds__(256) void dense_short(DenseGemm g) {
 
 // ---------------------------------------------------------------- elementwise parts of the gradients
 
+// Copies up to three matrices to rows that start at multiples of 16 bytes and end in zeros up to a whole chunk: the
+// tiles above read nothing else.  A wavefront takes 64 consecutive elements at a time, as rows that start anywhere
+// are read fastest (16-byte loads at odd addresses measured 1.1 TB/s).
+template <class E>
+__device__ inline void pack_rows(const DensePack& p, uint32_t mat, uint32_t group) {
+  const uint32_t cols = p.cols[mat], padded = static_cast<uint32_t>(p.ldd[mat]);
+  const uint32_t rows = p.rows[mat];
+  const E* src = static_cast<const E*>(p.src[mat]);
+  E* dst = static_cast<E*>(p.dst[mat]);
+  // as many rows side by side as 256 threads hold
+  const uint32_t wide = p.wide[mat], x = threadIdx.x % wide, y = threadIdx.x / wide, side = 256 / wide;
+  for (uint64_t i = uint64_t(group) * side + y; i < rows; i += uint64_t(p.groups) * side)
+#pragma unroll 4
+    for (uint32_t j = x; j < padded; j += wide) {
+      const E v = src[i * p.lds[mat] + min(j, cols - 1)];
+      dst[i * p.ldd[mat] + j] = j < cols ? v : 0;
+    }
+}
+
+template <class E>
+__global__ __launch_bounds__(256) void dense_pack(DensePack p) {
+  pack_rows<E>(p, blockIdx.x / p.groups, blockIdx.x % p.groups);
+}
+
 // dz (or dg and du), and the sums of their columns over a block of rows.  A thread has eight columns and every
 // lanes_y-th row of its block: 256 threads are lanes_x eights of columns by lanes_y rows.  One pass over the data.
 // Where all rows start at multiples of 16 bytes and hold whole eights (WHOLE), a thread's columns are consecutive and
@@ -1188,9 +1212,16 @@ __global__ __launch_bounds__(256) void dense_slope(DenseSlope s) {
   __shared__ float sums[256][kMats * 8 + 1];
   const int lanes_x = 1 << s.log_x, x = threadIdx.x & (lanes_x - 1), y = threadIdx.x >> s.log_x;
   const int lanes_y = 256 >> s.log_x;
-  const int j = blockIdx.x * lanes_x * 8 + (WHOLE ? x * 8 : x), n8 = (s.n + 7) / 8 * 8;
+  const int n8 = (s.n + 7) / 8 * 8, across = (n8 / 8 + lanes_x - 1) >> s.log_x;
+  const int block = blockIdx.x / across, j0 = (blockIdx.x % across) * lanes_x * 8;
+  if (block >= s.row_blocks) {
+    const uint32_t id = blockIdx.x - static_cast<uint32_t>(s.row_blocks) * across;
+    pack_rows<std::conditional_t<TYPE == kDenseF32, uint32_t, uint16_t>>(s.pack, id / s.pack.groups, id % s.pack.groups);
+    return;
+  }
+  const int j = j0 + (WHOLE ? x * 8 : x);
   const int rows = (s.m + s.row_blocks - 1) / s.row_blocks;
-  const int64_t first = int64_t(blockIdx.y) * rows, end = min(int64_t(s.m), first + rows);
+  const int64_t first = int64_t(block) * rows, end = min(int64_t(s.m), first + rows);
   float sum[kMats][8] = {};
   auto load = [&](const void* base, int64_t row, float* v) {
     const T* p = static_cast<const T*>(base) + row + j;
@@ -1212,7 +1243,7 @@ __global__ __launch_bounds__(256) void dense_slope(DenseSlope s) {
     }
   };
   if (j < n8) {
-#pragma unroll 2
+#pragma unroll(WHOLE ? 2 : 1)
     for (int64_t i = first + y; i < end; i += lanes_y) {
       float dy[8], z[8], u[8], d0[8], d1[8];
       load(s.dy, i * s.lddy, dy);
@@ -1251,7 +1282,7 @@ __global__ __launch_bounds__(256) void dense_slope(DenseSlope s) {
       }
     }
   }
-  if (!s.colsum[0] && !s.colsum[1]) return;
+  if (!s.colsum[0] && !s.colsum[1] && !s.total[0] && !s.total[1]) return;
 #pragma unroll
   for (int e = 0; e < kMats * 8; ++e) sums[threadIdx.x][e] = sum[e / 8][e % 8];
   __syncthreads();
@@ -1261,29 +1292,11 @@ __global__ __launch_bounds__(256) void dense_slope(DenseSlope s) {
     const int thread = WHOLE ? column / 8 : column % lanes_x, e = WHOLE ? column % 8 : column / lanes_x;
     float total = 0.0f;
     for (int r = 0; r < lanes_y; ++r) total += sums[r * lanes_x + thread][mat * 8 + e];
-    const int at = blockIdx.x * lanes_x * 8 + column;
-    if (at < s.n && s.colsum[mat]) s.colsum[mat][int64_t(blockIdx.y) * s.n + at] = total;
+    const int at = j0 + column;
+    if (at >= s.n) continue;
+    if (s.colsum[mat]) s.colsum[mat][int64_t(block) * s.n + at] = total;
+    if (s.total[mat]) static_cast<T*>(s.total[mat])[at] = T(total);
   }
-}
-
-// Copies up to three matrices to rows that start at multiples of 16 bytes and end in zeros up to a whole chunk: the
-// tiles above read nothing else.  A wavefront takes 64 consecutive elements at a time, as rows that start anywhere
-// are read fastest (16-byte loads at odd addresses measured 1.1 TB/s).
-template <class E>
-__global__ __launch_bounds__(256) void dense_pack(DensePack p) {
-  const int mat = blockIdx.y;
-  const uint32_t cols = p.cols[mat], padded = static_cast<uint32_t>(p.ldd[mat]);
-  const uint32_t rows = p.rows[mat];
-  const E* src = static_cast<const E*>(p.src[mat]);
-  E* dst = static_cast<E*>(p.dst[mat]);
-  // as many rows side by side as 256 threads hold
-  const uint32_t wide = p.wide[mat], x = threadIdx.x % wide, y = threadIdx.x / wide, side = 256 / wide;
-  for (uint64_t i = uint64_t(blockIdx.x) * side + y; i < rows; i += uint64_t(gridDim.x) * side)
-#pragma unroll 4
-    for (uint32_t j = x; j < padded; j += wide) {
-      const E v = src[i * p.lds[mat] + min(j, cols - 1)];
-      dst[i * p.ldd[mat] + j] = j < cols ? v : 0;
-    }
 }
 
 template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
@@ -1371,7 +1384,7 @@ int forward_launch(const DenseGemm& g, hipStream_t stream) {
 template <int TYPE>
 int slope_launch(const DenseSlope& s, hipStream_t stream) {
   const int eights = (s.n + 7) / 8, x = 1 << s.log_x;
-  const dim3 grid((eights + x - 1) / x, s.row_blocks);
+  const uint32_t grid = static_cast<uint32_t>((eights + x - 1) / x) * s.row_blocks + s.pack.count * s.pack.groups;
   if (s.gated && s.whole) dense_slope<TYPE, true, true><<<grid, 256, 0, stream>>>(s);
   else if (s.gated) dense_slope<TYPE, true, false><<<grid, 256, 0, stream>>>(s);
   else if (s.whole) dense_slope<TYPE, false, true><<<grid, 256, 0, stream>>>(s);
@@ -1395,7 +1408,7 @@ int slope_launch(const DenseSlope& s, hipStream_t stream) {
 
 #if EMBX_HAS_DPART(0)
 int dense_pack_launch(const DensePack& p, void* stream) {
-  const dim3 grid(p.groups, p.count);
+  const uint32_t grid = p.groups * p.count;
   if (p.esize == 4) dense_pack<uint32_t><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(p);
   else dense_pack<uint16_t><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(p);
   return hipGetLastError();

@@ -38,23 +38,6 @@ struct DenseGemm {
   int32_t whole;           // kRows, kShort: operands' rows start at multiples of 16 bytes and hold whole chunks
 };
 
-// dz = dy * act'(z), or dg, du; and partial column sums of them
-struct DenseSlope {
-  const void* dy;
-  const void* z[2];        // z, or g and u; NULL z[0]: dz = dy (only column sums)
-  void* dz[2];             // NULL: not written
-  float* colsum[2];        // [row blocks][n], or NULL
-  int64_t lddy, ldz[2], lddz;
-  int32_t m, n, act, gated, row_blocks;
-  int32_t log_x;           // log2 of the eights of columns of a workgroup
-  int32_t whole;           // rows of all operands start at multiples of 16 bytes and hold whole eights
-};
-
-// workgroups of the last launch of a backward pass: of the column sums, and of the join of one of w's results
-struct DenseTail {
-  uint32_t colsum_groups, w_groups;
-};
-
 // matrices copied to rows of whole 16-byte chunks
 struct DensePack {
   const void* src[3];
@@ -62,6 +45,25 @@ struct DensePack {
   int64_t lds[3], ldd[3];
   uint32_t rows[3], cols[3], wide[3];
   int32_t count, groups, esize;
+};
+
+// dz = dy * act'(z), or dg, du; and column sums of them
+struct DenseSlope {
+  const void* dy;
+  const void* z[2];        // z, or g and u; NULL z[0]: dz = dy (only column sums)
+  void* dz[2];             // NULL: not written
+  float* colsum[2];        // [row blocks][n], or NULL: not wanted, or
+  void* total[2];          // [n], with one block of rows: the finished sums; or NULL
+  int64_t lddy, ldz[2], lddz;
+  int32_t m, n, act, gated, row_blocks;
+  int32_t log_x;           // log2 of the eights of columns of a workgroup
+  int32_t whole;           // rows of all operands start at multiples of 16 bytes and hold whole eights
+  DensePack pack;          // matrices that the same launch copies
+};
+
+// workgroups of the last launch of a backward pass: of the column sums, and of the join of one of w's results
+struct DenseTail {
+  uint32_t colsum_groups, w_groups;
 };
 
 // column sums from those of blocks of rows

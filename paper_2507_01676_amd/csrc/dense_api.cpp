@@ -263,13 +263,16 @@ int32_t slope_log_x(int64_t n) {
   return l;
 }
 
-// blocks of rows of that pass: 1024 workgroups in all if every thread still has four rows, and at most 256 blocks, whose
-// column sums are added up afterwards
+// Blocks of rows of that pass.  One where each thread has at most four rows: it adds the column sums up by itself, and
+// no other launch is needed for them (77 columns of 63 rows: 20.4 us a call against 23.2).  Else as many as there are
+// rows for, up to 1024 workgroups (3001 x 77 with one row a thread 29 us a call, with four 35) and 512 blocks, whose sums
+// are added up afterwards (16384 x 1024 with 256: 242 us a call, with 512: 234).
 int32_t slope_blocks(int64_t m, int64_t n) {
   const int32_t log_x = slope_log_x(n);
   const int64_t across = ((n + 7) / 8 + (1 << log_x) - 1) >> log_x;
-  const int64_t rows = int64_t(4) * (256 >> log_x);
-  return static_cast<int32_t>(std::max<int64_t>(1, std::min({int64_t(256), (1024 + across - 1) / across, (m + rows - 1) / rows})));
+  const int64_t rows = 256 >> log_x;
+  if (m <= 4 * rows) return 1;
+  return static_cast<int32_t>(std::min({int64_t(512), (1024 + across - 1) / across, (m + rows - 1) / rows}));
 }
 
 // The workspace of each call: copies of operands, dz, column sums and partial sums of products.
@@ -317,7 +320,7 @@ Operand dz_space(Arena& ar, int64_t m, int64_t n, int32_t dtype) {
 }
 
 float* colsum_space(Arena& ar, bool wanted, int32_t blocks, int64_t n) {
-  return wanted ? ar.take<float>(size_t(blocks) * n * 4) : nullptr;
+  return wanted && blocks > 1 ? ar.take<float>(size_t(blocks) * n * 4) : nullptr;
 }
 
 void partial_space(Arena& ar, Space& s, int32_t dtype, int64_t m, int64_t n, int64_t k, int mats, bool want_x, int want_w,
@@ -339,7 +342,7 @@ Space linear_grad_space(Arena& ar, const emb_linear_grad_t& a) {
   s.pack = pk.pack;
   s.blocks = slope_blocks(a.m, a.n);
   s.colsum[0] = colsum_space(ar, a.dbias, s.blocks, a.n);
-  partial_space(ar, s, a.dtype, a.m, a.n, a.k, 1, dx, a.dweight ? 1 : 0, a.dbias);
+  partial_space(ar, s, a.dtype, a.m, a.n, a.k, 1, dx, a.dweight ? 1 : 0, a.dbias && s.blocks > 1);
   return s;
 }
 
@@ -359,7 +362,7 @@ Space gated_grad_space(Arena& ar, const emb_gated_grad_t& a) {
   s.blocks = slope_blocks(a.m, a.n);
   s.colsum[0] = colsum_space(ar, a.db_gate, s.blocks, a.n);
   s.colsum[1] = colsum_space(ar, a.db_up, s.blocks, a.n);
-  partial_space(ar, s, a.dtype, a.m, a.n, a.k, 2, dx, weights, a.db_gate || a.db_up);
+  partial_space(ar, s, a.dtype, a.m, a.n, a.k, 2, dx, weights, (a.db_gate || a.db_up) && s.blocks > 1);
   return s;
 }
 
@@ -431,17 +434,20 @@ emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, si
   Arena ar{static_cast<char*>(workspace)};
   const Space sp = linear_grad_space(ar, *a);
   EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
-  EMBX_TRY(run_pack(sp.pack, stream));
   if (a->dbias || sp.slopes) {
     DenseSlope s = {};
     s.dy = a->dy, s.lddy = a->lddy;
     s.z[0] = slopes ? a->z : nullptr, s.ldz[0] = a->ldz;
     s.dz[0] = sp.slopes ? const_cast<void*>(sp.dz[0].p) : nullptr, s.lddz = sp.dz[0].ld;
     s.colsum[0] = sp.colsum[0];
+    if (sp.blocks == 1) s.total[0] = a->dbias;
     s.m = a->m, s.n = a->n, s.act = a->activation, s.gated = 0, s.row_blocks = sp.blocks;
     s.log_x = slope_log_x(a->n);
     s.whole = whole16(a->dy, a->lddy, a->n, a->dtype) && (!slopes || whole16(a->z, a->ldz, a->n, a->dtype));
+    s.pack = sp.pack;
     EMBX_TRY(slope(a->dtype, s, stream));
+  } else {
+    EMBX_TRY(run_pack(sp.pack, stream));
   }
   DenseGemm w = {}, x = {};
   if (a->dx && a->m > 0) {
@@ -532,7 +538,6 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
   Arena ar{static_cast<char*>(workspace)};
   const Space sp = gated_grad_space(ar, *a);
   EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
-  EMBX_TRY(run_pack(sp.pack, stream));
   const bool sums = a->db_gate || a->db_up;
   if (sums || sp.slopes) {
     DenseSlope s = {};
@@ -542,11 +547,15 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
     for (int i = 0; i < 2; ++i) s.dz[i] = sp.slopes ? const_cast<void*>(sp.dz[i].p) : nullptr;
     s.lddz = sp.dz[0].ld;
     s.colsum[0] = sp.colsum[0], s.colsum[1] = sp.colsum[1];
+    if (sp.blocks == 1) s.total[0] = a->db_gate, s.total[1] = a->db_up;
     s.m = a->m, s.n = a->n, s.act = a->activation, s.gated = 1, s.row_blocks = sp.blocks;
     s.log_x = slope_log_x(a->n);
     s.whole = whole16(a->dh, a->lddh, a->n, a->dtype) && whole16(a->g, a->ldg, a->n, a->dtype) &&
               whole16(a->u, a->ldu, a->n, a->dtype);
+    s.pack = sp.pack;
     EMBX_TRY(slope(a->dtype, s, stream));
+  } else {
+    EMBX_TRY(run_pack(sp.pack, stream));
   }
   DenseGemm w = {}, x = {};
   if (a->dx && a->m > 0) {
