@@ -117,10 +117,11 @@ __device__ inline void act8(float* z, int act) {
 //
 // A workgroup computes BM x BN sums (kGated: BN / 2 columns of each projection) in WI x WJ
 // wavefronts.  Each step takes 128 bytes of the reduction (BK elements) of both operands from LDS, while
-// later steps are on their way there.  A tile lies in LDS as in memory: rows of BK elements (operand
-// along the reduction) or BK rows of BM or BN elements (reduction-major), with the
+// later steps are on their way there.  A tile of 16-bit elements lies in LDS as in memory: rows of BK elements
+// (operand along the reduction) or BK rows of BM or BN elements (reduction-major), with the
 // 16-byte chunks of a row permuted so that what a wavefront reads at once lies in different
-// banks.  Chunks go from memory to LDS without registers, so their order within a wavefront's
+// banks (counted: no conflicts; half the step, rows of 64 bytes, had them in 49% of the LDS cycles).  Chunks go from
+// memory to LDS without registers, so their order within a wavefront's
 // 1 KB is fixed in LDS, and the permutation is applied to the address each lane loads from.
 constexpr int kOutOfRange = static_cast<int>(0x80000000u);   // past every descriptor: reads zeros
 
@@ -170,21 +171,20 @@ __device__ inline f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
 }
 
-// One operand's tile of ROWS results (rows of x or dz, columns of the result) by 128 bytes of the reduction: BK elements
-// of ESIZE bytes.  RM: reduction-major in memory.
-template <int ROWS, bool RM, int WAVES, int ESIZE>
+// One operand's tile of ROWS results (rows of x or dz, columns of the result) by BK 16-bit elements of the reduction.
+// RM: reduction-major in memory.
+template <int ROWS, bool RM, int WAVES>
 struct Tile {
-  static constexpr int BK = 128 / ESIZE, kPer = 16 / ESIZE;   // elements of a step and of a chunk
+  static constexpr int BK = 64;
   static constexpr int kBytes = ROWS * 128;
   static constexpr int kLoads = kBytes / 1024 / WAVES;        // 1 KB pieces a wavefront loads
-  static constexpr int kRowBytes = RM ? ROWS * ESIZE : 128;
-  static constexpr int kChunks = kRowBytes / 16;
+  static constexpr int kRowBytes = RM ? ROWS * 2 : 128;
+  static constexpr int kChunks = kRowBytes / 16;              // of eight elements
   static constexpr int kRowsPerLoad = 1024 / kRowBytes;
   static_assert(kBytes % (1024 * WAVES) == 0, "every wavefront loads alike");
 
   // the permutation of a row's chunks
   __device__ static int swizzle(int row) {
-    if (ESIZE == 4) return 0;   // read along its rows
     if (RM) return (kChunks >= 16 ? (row & 3) | ((row >> 1) & 4) : row & 3) << 1;
     return (row >> 1) & 7;
   }
@@ -200,8 +200,8 @@ struct Tile {
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
       const int row = load_row(n, wave, lane), chunk = load_chunk(row, lane);
-      const bool in = RM ? chunk * kPer < rows : row < rows;
-      voff[n] = in ? static_cast<int>(row * ld * ESIZE) + chunk * 16 : kOutOfRange;
+      const bool in = RM ? chunk * 8 < rows : row < rows;
+      voff[n] = in ? static_cast<int>(row * ld * 2) + chunk * 16 : kOutOfRange;
     }
   }
 
@@ -210,12 +210,12 @@ struct Tile {
     int v = voff[n];
     if (valid < BK) {
       const int row = load_row(n, wave, lane), chunk = load_chunk(row, lane);
-      v = (RM ? row < valid : chunk * kPer < valid) ? v : kOutOfRange;
+      v = (RM ? row < valid : chunk * 8 < valid) ? v : kOutOfRange;
     }
     load_to_lds(rsrc, v, lds + (n * WAVES + wave) * 1024);
   }
 
-  // 16 bits: fragment of 16 results (from `first` on, a multiple of 16) by 32 of the reduction (half ks): lane: result
+  // fragment of 16 results (from `first` on, a multiple of 16) by 32 of the reduction (half ks): lane: result
   // lane % 16, reduction 8 (lane / 16) .. + 7
   __device__ static s16x8 fragment(const char* tile, int first, int ks, int lane) {
     const int q = lane >> 4, c = lane & 15;
@@ -233,14 +233,17 @@ struct Tile {
   }
 };
 
-// f32 products.  The matrix cores multiply f32 at a sixteenth of their bf16 rate.  So each f32 value is taken as a sum of
-// three bf16 values (the value rounded, the rest rounded, the rest of that: 24 bits in all, exact for magnitudes from
-// 2^-110 on, below which the last part may vanish), and a product as the six of their nine products that count; the other
-// three come to 2^-23 of it at most.  Small ones are added first.  Six bf16 products for each f32 one are 2.7 times less
-// work than f32 products, at f32's accuracy.  Values of 2^128 - 2^119 or more, infinities and NaN cannot be taken apart
-// so: they turn every sum that they reach into NaN, and a tile with sums that are not finite is computed again with f32
-// products (tile_by_f32).
+// f32 products.  The matrix cores multiply f32 at a sixteenth of their bf16 rate.  So each f32 value, times 2^24, is taken as
+// a sum of three bf16 values (the value rounded, the rest rounded, the rest of that: 24 bits in all, exact for every normal
+// value: the last bit, 2^-149 at least, is 2^-125 at least then, and no part is too small for a normal bf16), and a product
+// as the six of their nine products that count; the other three come to 2^-23 of it at most.  Small ones are added first,
+// and the finished sum is multiplied by 2^-48.  Six bf16 products for each f32 one are 2.7 times less
+// work than f32 products, at f32's accuracy.  Values or sums too large for this (2^104 or 2^80, about), infinities and NaN
+// turn the sums that they reach into infinities or NaN, and a tile with sums that are not finite is computed again with f32
+// products (tile_by_f32).  The first factor costs 1% (4096^3 610 us, without it 606).
 struct Parts { s16x8 p[3]; };   // high to low
+
+constexpr float kScale = 0x1p24f;
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -254,7 +257,7 @@ __device__ inline Parts split3(const float* v) {
   u32x4 part[3];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    float a = v[2 * e], b = v[2 * e + 1];
+    float a = v[2 * e] * kScale, b = v[2 * e + 1] * kScale;
 #pragma unroll
     for (int p = 0; p < 3; ++p) {
       part[p][e] = round2(a, b);
@@ -265,8 +268,9 @@ __device__ inline Parts split3(const float* v) {
 }
 
 // The parts of a tile of f32 (ROWS results by 32 of the reduction) in LDS: a tile of bf16 for each.  Taken apart once for
-// the workgroup, not at each wavefront's fragments: the matrix cores and the other vector instructions of a SIMD hardly
-// overlap (with both in turns a step took the sum of their times), so every instruction of the latter counts.
+// the workgroup, not at each wavefront's fragments: the matrix cores and the other vector instructions of a SIMD overlap
+// by half at most (8 matrix instructions take 160 cycles, 32 others 173, all of them from two wavefronts 249), so every
+// instruction of the latter counts.  4096 x 4096 x 4096: 610 us, with the parts taken at the fragments 641.
 template <int ROWS, bool RM, int WAVES>
 struct PartTile {
   static constexpr int kBytes = ROWS * 64;                     // of a part
@@ -592,7 +596,17 @@ constexpr int kTileLds = [] {
   return steps > sums ? steps : sums;
 }();
 
-// One tile of a product: `tile` of its tiles, `split` of its splits, `wpart` of kWeightGrad's two results.
+// One tile of a product: `tile` of its tiles, `split` of its splits, `wpart` of kWeightGrad's two results.  Three main
+// loops:
+//   16 bits, 128 x 128, four wavefronts of 64 x 64, two workgroups a CU: for products that do not fill the GPU with larger
+//     ones; a tile's operands pass through L2 twice as often as those of 256 x 256 (bf16 8192^3: 1004 us, 1.1 PFLOP/s)
+//   16 bits, 256 x 256, eight wavefronts of 128 x 64 in turns, one workgroup a CU (its 160 KB of LDS, and 128 + 96 of the
+//     registers): bf16 8192^3 765 us, 1.44 PFLOP/s, where one library product reaches 1.42 to 1.61; 65536 x 1024 x 12800
+//     1255 us, 1.37.  Bound by the matrix cores at the clock that they leave (about 1.75 GHz), less some 7 us a tile for its
+//     first loads and its results, which nothing hides (one workgroup a CU that goes on to the next tile was slower: its
+//     loads wait for the stores before them)
+//   f32, 256 x 128 or 128 x 128, eight wavefronts, one workgroup a CU: see PartTile; 4096^3 610 us, 225 TFLOP/s (f32
+//     products on the matrix cores reach 153 in a library)
 template <int TYPE, int KIND, int BM, int BN, int WI, int WJ>
 __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint32_t tile, int split, int wpart) {
   constexpr bool kGate = KIND == kGated;
@@ -604,11 +618,10 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
   constexpr int kCols = kGate ? BN / 2 : BN;               // result columns of a tile
   constexpr int kWI = BM / WI, kWJ = kCols / WJ;           // results of a wavefront
   constexpr int kFI = kWI / 16, kFJ = BN / WJ / 16;        // its fragments
-  constexpr int kSize = kF32 ? 4 : 2;
-  using TileA = Tile<BM, kRmA, kWaves, kSize>;
-  using TileB = Tile<BN, kRmB, kWaves, kSize>;
-  using TileH = Tile<kCols, kRmB, kWaves, kSize>;          // one projection's half of B
-  constexpr int BK = TileA::BK;
+  using TileA = Tile<BM, kRmA, kWaves>;                    // (16 bits)
+  using TileB = Tile<BN, kRmB, kWaves>;
+  using TileH = Tile<kCols, kRmB, kWaves>;                 // one projection's half of B
+  constexpr int BK = kF32 ? 32 : TileA::BK;
   static_assert(kF32 || kSlotsA * TileA::kBytes + kSlotsB * TileB::kBytes <= kTileLds<TYPE, BM, BN, WJ, kWaves>);
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -645,7 +658,7 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
     const int r0 = (step - part * per_part) * BK;
     next.valid_a = step < end ? g.nr - r0 : 0;
     const char* a = static_cast<const char*>(g.a[KIND == kWeightGrad ? wpart : part]);
-    next.a = descriptor(a + (kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0) * kSize);
+    next.a = descriptor(a + (kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0) * 2);
     next.at_a = lds0 + slot * TileA::kBytes;
   };
   auto set_b = [&](int step, int slot) {
@@ -653,8 +666,8 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
     const int r0 = (step - part * per_part) * BK;
     next.valid_b = step < end ? g.nr - r0 : 0;
     const char* b = static_cast<const char*>(g.b[part]);
-    next.b0 = descriptor(b + (kRmB ? int64_t(r0) * g.ldb[part] + j0 : int64_t(j0) * g.ldb[part] + r0) * kSize);
-    if constexpr (kGate) next.b1 = descriptor(static_cast<const char*>(g.b[1]) + (int64_t(j0) * g.ldb[1] + r0) * kSize);
+    next.b0 = descriptor(b + (kRmB ? int64_t(r0) * g.ldb[part] + j0 : int64_t(j0) * g.ldb[part] + r0) * 2);
+    if constexpr (kGate) next.b1 = descriptor(static_cast<const char*>(g.b[1]) + (int64_t(j0) * g.ldb[1] + r0) * 2);
     if constexpr (KIND == kInputGrad) {
       if (part != tb_part) {
         tb.init(wave, lane, g.ldb[part], g.nj - j0);
@@ -886,6 +899,12 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
       return;
     }
   }
+  if constexpr (kF32) {
+#pragma unroll
+    for (int fi = 0; fi < kFI; ++fi)
+#pragma unroll
+      for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] *= 1.0f / (kScale * kScale);
+  }
   store_sums<TYPE, KIND, kFI, kFJ>(g, acc, lds + wave * kSumsLds<kFJ>, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
 }
 
@@ -896,7 +915,9 @@ __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile
 }
 
 // Both products of a backward pass in one launch: the weights' gradient first, whose tiles are few and long, then the
-// input's, whose many short ones fill the CUs that are left (either may be absent).
+// input's, whose many short ones fill the CUs that are left (either may be absent).  With this
+// launch and the last one instead of a launch for each, a call took 250 us instead of 265 (f16 16384 x 1024 x 3328), 272
+// instead of 315 (gated, bf16 8192 x 4096 x 1024) and 43 instead of 55 (gated, f16 777 x 1365 x 1001).
 template <int TYPE, int BM, int BN, int WI, int WJ, int PER_CU>
 __global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_grads(DenseGemm w, DenseGemm x, uint32_t w_groups) {
   __shared__ __align__(1024) char lds[kTileLds<TYPE, BM, BN, WJ, WI * WJ>];
@@ -941,7 +962,8 @@ __global__ __launch_bounds__(256) void dense_join(DenseGemm g) {
 }
 
 // The last launch of a backward pass, as far as there is something left: the column sums from those of the blocks of
-// rows (32 columns a workgroup, eight threads a column), then the joins of both products.
+// rows (32 columns a workgroup, eight threads a column), then the joins of both products.  No two of them depend on
+// each other.
 template <int TYPE>
 __global__ __launch_bounds__(256) void dense_tail(DenseGemm w, DenseGemm x, DenseColsum c, DenseTail t) {
   using T = typename Elem<TYPE>::T;
@@ -1028,7 +1050,8 @@ __device__ inline f32x4 multiply(const Loader<TYPE, WHOLE>& w, const Loader<TYPE
 }
 
 // Few rows: the weights are read once, and latency counts.  Eight wavefronts share FR * 16 rows by 16 columns and take
-// every eighth step of 32 each; their sums are added in order in LDS.
+// every eighth step of 32 each; their sums are added in order in LDS.  bf16, 1 x 512 x 1664: 4.5 us of GPU time, a launch
+// and two rounds of loads; gated 19 x 2816 x 1024: 6.4 us for 11.7 MB.
 template <int TYPE, int KIND, int FR, bool WHOLE>
 __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
   using T = typename Elem<TYPE>::T;
@@ -1077,7 +1100,8 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 // registers, walk rows of x by chunks of 64, which pass through LDS: loaded once for all columns of the workgroup, as
 // 16-byte chunks (WHOLE) or consecutive elements, while the chunk before is multiplied.  Where there are fewer columns
 // than the four hold, several take the same columns and other rows of the chunk.  Results leave through LDS, in whole
-// 128-byte lines.
+// 128-byte lines.  bf16, 65536 x 512 x 64: 75 MB in 21.7 us a call, 3.5 TB/s (without LDS on the way in 28.5, results
+// stored from the fragments' lanes 26.3); the stores and the epilogue's instructions bound it.
 template <int TYPE, int KIND, int FC, int KS, bool WHOLE>
 __global__ __launch_bounds__(256) void dense_short(DenseGemm g) {
   using T = typename Elem<TYPE>::T;
@@ -1203,7 +1227,7 @@ __global__ __launch_bounds__(256) void dense_pack(DensePack p) {
 // dz (or dg and du), and the sums of their columns over a block of rows.  A thread has eight columns and every
 // lanes_y-th row of its block: 256 threads are lanes_x eights of columns by lanes_y rows.  One pass over the data.
 // Where all rows start at multiples of 16 bytes and hold whole eights (WHOLE), a thread's columns are consecutive and
-// read and written 16 bytes at a time (8192 x 4096 gated: 335 MB in 67 us, 5.0 TB/s); else they are lanes_x apart, and a
+// read and written 16 bytes at a time (8192 x 4096 gated: 335 MB in 60 us, 5.6 TB/s); else they are lanes_x apart, and a
 // wavefront reads consecutive elements.  The column sums are of the 32-bit values, not of the rounded ones.
 template <int TYPE, bool GATED, bool WHOLE>
 __global__ __launch_bounds__(256) void dense_slope(DenseSlope s) {

@@ -121,19 +121,27 @@ double tile_us(int32_t dtype, int variant, double tiles, double steps, int s, do
 }
 
 // The same of few rows: workgroups of 16 columns, a step being 32 of the reduction of each of eight wavefronts.  Measured
-// on 1 to 64 rows by 512 to 8192 columns and inputs: 0.5 us a step of 16 rows, 1.0 of 64, with a workgroup on every CU.
-double rows_us(int64_t ni, int64_t nj, int64_t nr) {
+// on 1 to 64 rows by 512 to 8192 columns and inputs, with a workgroup on every CU.
+double rows_us(int32_t dtype, int64_t ni, int64_t nj, int64_t nr) {
   const double groups = double((nj + 15) / 16), steps = double((nr + 255) / 256);
-  return 3.0 + steps * (ni <= 16 ? 0.5 : ni <= 32 ? 0.7 : 1.0) * std::max(1.0, groups / kCus);
+  const double step = dtype == EMB_DTYPE_F32 ? (ni <= 16 ? 0.95 : ni <= 32 ? 1.3 : 2.2) : (ni <= 16 ? 0.5 : ni <= 32 ? 0.7 : 1.0);
+  return 3.0 + steps * step * std::max(1.0, groups / kCus);
 }
 
+// How a forward product is computed.  What the alternatives measured, in us a call (a call takes 8 from the host):
+//   a reduction of at most 64 and more than 64 rows: the kernel for it (bf16 65536 x 512 x 64 21.7, tiles of 128 27.0; x 32
+//     15.9 and 26.8; f32 x 64 50.5, tiles 72; 4096 x 4096 x 64 15.1 and 15.5)
+//   at most 64 rows: the kernel for them, unless a split tile is estimated to be faster (bf16 16 x 512 x 1664 8.2, best tile
+//     13.6; 16 x 4096 x 4096 9.6 and 13.4; but 64 x 8192 x 8192 72 and 30.4; f32 64 x 4096 x 4096 39.7 and 32.6)
+//   tiles of 256 where they fill the GPU (bf16 4096^3 100, tiles of 128 134), of 128 else (2048^3 44 and 27.7), their
+//     reductions split where there are few (f32 4096 x 512 x 1664 whole 65, in two 49.7, in four 62)
 Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k) {
   if (k <= kShortSum && m > kFewRows) return {kShort, 1};
   const int mats = kind == kGated ? 2 : 1;
   const double steps = static_cast<double>(steps_of(dtype, k)), result_bytes = 4.0 * m * n * mats;
   Choice best = {kTile128, 1};
   double least = 0.0;
-  if (m <= kFewRows) best = {kRows, 1}, least = rows_us(m, n, k);
+  if (m <= kFewRows) best = {kRows, 1}, least = rows_us(dtype, m, n, k);
   for (int variant : {kTile256, kTile128}) {
     const double tiles = static_cast<double>(tiles_of(dtype, variant, m, n * mats));
     for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial)); ++s) {

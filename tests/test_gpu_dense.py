@@ -411,3 +411,65 @@ def test_binding_refusals(gpu_lib):
 
 def embx_error(lib):
     return lib.EmbxError
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(64, 40, 64), (65, 40, 64), (65, 40, 65), (64, 40, 65), (66, 7, 32), (66, 7, 33), (200, 70, 64),
+                                  (300, 513, 33), (64, 1000, 1000), (65, 1000, 1000), (1000, 24, 1)], ids=str)
+def test_sizes_where_the_kernel_changes(gpu_lib, size, dtype):
+    """Few rows or not, a short reduction or not, and one below or above."""
+    m, n, k = size
+    log(f"change of kernel {size} {dtype}")
+    x, w, b, r = layer(dtype, 21, m, n, k, residual=True)
+    wu, = make(dtype, 22, ((n, k), k ** -0.5))
+    y, z = gpu_lib.linear(x, w, b, r, activation="gelu", save=True)
+    for v, want in zip((y, z), R.linear(x, w, b, r, "gelu", dtype)):
+        R.check(v, want, "linear")
+    for v, want in zip(gpu_lib.gated_ffn(x, w, wu, b, None, save=True), R.gated(x, w, wu, b, None, "silu", dtype)):
+        R.check(v, want, "gated")
+
+
+@pytest.mark.parametrize("size", [(20, 24, 300), (150, 264, 200), (100, 24, 40)], ids=str)
+def test_f32_at_the_ends_of_its_range(gpu_lib, size):
+    """The largest numbers, against small ones so that the products are ordinary, and numbers of 2^-100: both are as
+    accurate as any other."""
+    import torch
+    m, n, k = size
+    log(f"range of f32 {size}")
+    x, w, dy = make("f32", 23, ((m, k), 1.0), ((n, k), k ** -0.5), ((m, n), 1.0))
+    x[:, 3] *= 2.0 ** 120
+    x[1, 3] = torch.finfo(torch.float32).max
+    x[2, 3] = -torch.finfo(torch.float32).max
+    x[3, 3] = 2.0 ** 128 - 2.0 ** 119
+    w[:, 3] *= 2.0 ** -126
+    x[:, 4] *= 2.0 ** -100
+    w[:, 4] *= 2.0 ** 100
+    R.check(gpu_lib.linear(x, w), R.linear(x, w, None, None, "none", "f32")[0], "linear")
+    wu = w.flip(0).contiguous()
+    for v, want in zip(gpu_lib.gated_ffn(x, w, wu, activation="none", save=True), R.gated(x, w, wu, None, None, "none", "f32")):
+        R.check(v, want, "gated")
+    dx, dw, db = gpu_lib.linear_backward(dy, x * 2.0 ** -20, w)
+    for v, want in zip((dx, dw, db), R.linear_backward(dy, x * 2.0 ** -20, w, None, "none", "f32")):
+        R.check(v, want, "linear_backward")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(100, 72, 40), (65, 264, 64), (64, 40, 300), (1, 40, 300)], ids=str)
+def test_infinities_and_nan_with_every_kernel(gpu_lib, size, dtype):
+    """As above: only the results whose sums hold them, where there are few rows or the reduction is short."""
+    import torch
+    m, n, k = size
+    log(f"not finite {size} {dtype}")
+    x, w, dy, z = make(dtype, 24, ((m, k), 1.0), ((n, k), k ** -0.5), ((m, n), 0.5), ((m, n), 1.0))
+    x[x == 0] = 0.5
+    w[w == 0] = 0.5
+    x[0, k - 1] = float("inf")
+    x[m - 1, 5] = float("nan")
+    for act in ("none", "relu"):
+        want, got = R.linear(x, w, None, None, act, dtype)[0][0], R.d(gpu_lib.linear(x, w, activation=act))
+        assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    # an infinite gradient behind a relu that is closed goes nowhere
+    dy[0] = float("inf")
+    z[0] = -1.0
+    dx, dw, db = gpu_lib.linear_backward(dy, x.nan_to_num(1.0, 1.0), w, z, activation="relu")
+    assert not R.d(dx)[0].any() and bool(torch.isfinite(R.d(dw)).all()) and bool(torch.isfinite(R.d(db)).all())
