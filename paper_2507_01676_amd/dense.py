@@ -39,9 +39,8 @@ class _Entry:
         self.fn.restype, self.fn.argtypes = _i32, [ctypes.c_char_p, _vp, _sz, _vp]
         self.size.restype, self.size.argtypes = _i32, [ctypes.c_char_p, ctypes.POINTER(_sz)]
 
-    def __call__(self, a, device, stream):
-        if stream is None:
-            stream = _current_stream(device)
+    def __call__(self, a, device):
+        stream = _current_stream(device)
         code = self.fn(a, None, 0, stream)   # most small calls need no workspace
         if code == ERR_INVALID_ARGUMENT:
             nbytes = _sz(0)
@@ -69,22 +68,42 @@ def _activation(name) -> int:
 
 
 def _first(x, name):
-    """(rows, columns, dtype, its code, device index) of the matrix that the others are measured against."""
+    """(rows, columns, dtype, its code, device index, (pointer, row stride)) of the matrix that the others are measured
+    against."""
+    try:
+        rows, cols = x.shape
+        dtype, device = x.dtype, x.get_device()
+        code = _DTYPES[dtype]
+        if device >= 0 and device == _current_device():
+            ld, step = x.stride()
+            at = (x.data_ptr(), ld) if step == 1 and ld >= cols else _odd_matrix(x, name, rows, cols, dtype, device)
+            return rows, cols, dtype, code, device, at
+    except (AttributeError, KeyError, TypeError):
+        pass
+    except ValueError:
+        if isinstance(x, torch.Tensor) and x.dim() == 2:
+            raise
     if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 2):
         raise ValueError(f"{name} must be a 2-D device tensor")
-    dtype = x.dtype
-    code = _DTYPES.get(dtype)
-    if code is None:
-        raise ValueError(f"{name} must be float32, float16 or bfloat16, got {dtype}")
-    device = x.get_device()
-    if device != _current_device():
-        raise ValueError(f"{name} is on cuda:{device}, the current device is cuda:{_current_device()}")
-    rows, cols = x.shape
-    return rows, cols, dtype, code, device
+    if x.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32, float16 or bfloat16, got {x.dtype}")
+    raise ValueError(f"{name} is on cuda:{x.get_device()}, the current device is cuda:{_current_device()}")
 
 
 def _matrix(t, name, rows, cols, dtype, device):
     """(pointer, row stride) of a matrix [rows, cols]."""
+    try:
+        if t.dtype is dtype and t.get_device() == device and t.shape == (rows, cols):
+            ld, step = t.stride()
+            if step == 1 and ld >= cols:
+                return t.data_ptr(), ld
+    except AttributeError:
+        pass
+    return _odd_matrix(t, name, rows, cols, dtype, device)
+
+
+def _odd_matrix(t, name, rows, cols, dtype, device):
+    """The same of a matrix of one row or column with other strides; says what is wrong with any other."""
     if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.get_device() == device and t.dim() == 2):
         raise ValueError(f"{name} must be a 2-D {dtype} tensor on cuda:{device}")
     r, c = t.shape
@@ -109,18 +128,18 @@ def _rows(t, name):
 def _vector(t, name, n, dtype, device):
     if t is None:
         return 0
-    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.get_device() == device and t.dim() == 1
-            and t.shape[0] == n and (n == 1 or t.stride(0) == 1)):
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == (n,)
+            and (t.stride() == (1,) or n == 1)):
         raise ValueError(f"{name} must be a contiguous [{n}] {dtype} tensor on cuda:{device}")
     return t.data_ptr()
 
 
-def _on(stream, fn, *args):
-    """fn(raw stream handle, *args) with torch's allocations on that stream."""
+def _on(stream, fn, *args, **options):
+    """fn(...) with the launches and torch's allocations on that stream."""
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
     with torch.cuda.stream(stream):
-        return fn(stream.cuda_stream, *args)
+        return fn(*args, **options)
 
 
 def linear(x, weight, bias=None, residual=None, *, activation="none", out=None, save=False, stream=None):
@@ -128,21 +147,17 @@ def linear(x, weight, bias=None, residual=None, *, activation="none", out=None, 
     residual [m, n]; ``save``: also returns the sums before the activation, as
     linear_backward takes them.  ``out`` may be the residual."""
     if stream is not None:
-        return _on(stream, _run_linear, x, weight, bias, residual, activation, out, save)
-    return _run_linear(None, x, weight, bias, residual, activation, out, save)
-
-
-def _run_linear(stream, x, weight, bias, residual, activation, out, save):
+        return _on(stream, linear, x, weight, bias, residual, activation=activation, out=out, save=save)
     act = _activation(activation)
-    m, k, dtype, code, device = _first(x, "x")
+    m, k, dtype, code, device, at = _first(x, "x")
     n = _rows(weight, "weight")
-    y = x.new_empty((m, n)) if out is None else out
-    z = x.new_empty((m, n)) if save else None
-    _linear(_linear.pack(m, n, k, code, act, *_matrix(x, "x", m, k, dtype, device),
+    y = x.new_empty(m, n) if out is None else out
+    z = x.new_empty(m, n) if save else None
+    _linear(_linear.pack(m, n, k, code, act, *at,
                          *_matrix(weight, "weight", n, k, dtype, device), _vector(bias, "bias", n, dtype, device),
                          *(_NONE if residual is None else _matrix(residual, "residual", m, n, dtype, device)),
                          *((y.data_ptr(), n) if out is None else _matrix(y, "out", m, n, dtype, device)),
-                         *((z.data_ptr(), n) if save else _NONE)), device, stream)
+                         *((z.data_ptr(), n) if save else _NONE)), device)
     return (y, z) if save else y
 
 
@@ -151,24 +166,21 @@ def linear_backward(dy, x, weight, z=None, *, activation="none", bias=True, stre
     not wanted); z as linear(..., save=True) returned it (not needed with activation
     "none").  The residual's gradient is dy."""
     if stream is not None:
-        return _on(stream, _run_linear_backward, dy, x, weight, z, activation, bias, need_dx, need_dw)
-    return _run_linear_backward(None, dy, x, weight, z, activation, bias, need_dx, need_dw)
-
-
-def _run_linear_backward(stream, dy, x, weight, z, activation, bias, need_dx, need_dw):
+        return _on(stream, linear_backward, dy, x, weight, z, activation=activation, bias=bias, need_dx=need_dx,
+                   need_dw=need_dw)
     act = _activation(activation)
-    m, k, dtype, code, device = _first(x, "x")
+    m, k, dtype, code, device, at = _first(x, "x")
     n = _rows(weight, "weight")
     if act and z is None:
         raise ValueError(f"activation {activation!r} needs z, the sums that linear(..., save=True) returns")
-    dx = x.new_empty((m, k)) if need_dx else None
-    dw = x.new_empty((n, k)) if need_dw else None
+    dx = x.new_empty(m, k) if need_dx else None
+    dw = x.new_empty(n, k) if need_dw else None
     db = x.new_empty(n) if bias else None
     _linear_backward(_linear_backward.pack(
-        m, n, k, code, act, *_matrix(dy, "dy", m, n, dtype, device), *_matrix(x, "x", m, k, dtype, device),
+        m, n, k, code, act, *_matrix(dy, "dy", m, n, dtype, device), *at,
         *_matrix(weight, "weight", n, k, dtype, device), *(_matrix(z, "z", m, n, dtype, device) if act else _NONE),
         *((dx.data_ptr(), k) if need_dx else _NONE), *((dw.data_ptr(), k) if need_dw else _NONE),
-        db.data_ptr() if bias else 0), device, stream)
+        db.data_ptr() if bias else 0), device)
     return dx, dw, db
 
 
@@ -176,21 +188,17 @@ def gated_ffn(x, w_gate, w_up, b_gate=None, b_up=None, *, activation="silu", out
     """act(x w_gate^T + b_gate) * (x w_up^T + b_up) (emb_gated).  x [m, k], weights [n, k],
     biases [n]; ``save``: returns (h, g, u) with both projections, as gated_ffn_backward takes them."""
     if stream is not None:
-        return _on(stream, _run_gated, x, w_gate, w_up, b_gate, b_up, activation, out, save)
-    return _run_gated(None, x, w_gate, w_up, b_gate, b_up, activation, out, save)
-
-
-def _run_gated(stream, x, w_gate, w_up, b_gate, b_up, activation, out, save):
+        return _on(stream, gated_ffn, x, w_gate, w_up, b_gate, b_up, activation=activation, out=out, save=save)
     act = _activation(activation)
-    m, k, dtype, code, device = _first(x, "x")
+    m, k, dtype, code, device, at = _first(x, "x")
     n = _rows(w_gate, "w_gate")
-    h = x.new_empty((m, n)) if out is None else out
-    g, u = ((x.new_empty((m, n)), x.new_empty((m, n))) if save else (None, None))
-    _gated(_gated.pack(m, n, k, code, act, *_matrix(x, "x", m, k, dtype, device),
+    h = x.new_empty(m, n) if out is None else out
+    g, u = ((x.new_empty(m, n), x.new_empty(m, n)) if save else (None, None))
+    _gated(_gated.pack(m, n, k, code, act, *at,
                        *_matrix(w_gate, "w_gate", n, k, dtype, device), *_matrix(w_up, "w_up", n, k, dtype, device),
                        _vector(b_gate, "b_gate", n, dtype, device), _vector(b_up, "b_up", n, dtype, device),
                        *((h.data_ptr(), n) if out is None else _matrix(h, "out", m, n, dtype, device)),
-                       *((g.data_ptr(), n, u.data_ptr(), n) if save else (0, 0, 0, 0))), device, stream)
+                       *((g.data_ptr(), n, u.data_ptr(), n) if save else (0, 0, 0, 0))), device)
     return (h, g, u) if save else h
 
 
@@ -199,22 +207,19 @@ def gated_ffn_backward(dh, x, w_gate, w_up, g, u, *, activation="silu", bias=Fal
     """Gradients (dx, dw_gate, dw_up, db_gate, db_up) of gated_ffn at the gradient dh of its
     result (None where not wanted); g and u as gated_ffn(..., save=True) returned them."""
     if stream is not None:
-        return _on(stream, _run_gated_backward, dh, x, w_gate, w_up, g, u, activation, bias, need_dx, need_dw)
-    return _run_gated_backward(None, dh, x, w_gate, w_up, g, u, activation, bias, need_dx, need_dw)
-
-
-def _run_gated_backward(stream, dh, x, w_gate, w_up, g, u, activation, bias, need_dx, need_dw):
+        return _on(stream, gated_ffn_backward, dh, x, w_gate, w_up, g, u, activation=activation, bias=bias, need_dx=need_dx,
+                   need_dw=need_dw)
     act = _activation(activation)
-    m, k, dtype, code, device = _first(x, "x")
+    m, k, dtype, code, device, at = _first(x, "x")
     n = _rows(w_gate, "w_gate")
-    dx = x.new_empty((m, k)) if need_dx else None
-    dwg, dwu = ((x.new_empty((n, k)), x.new_empty((n, k))) if need_dw else (None, None))
+    dx = x.new_empty(m, k) if need_dx else None
+    dwg, dwu = ((x.new_empty(n, k), x.new_empty(n, k)) if need_dw else (None, None))
     dbg, dbu = ((x.new_empty(n), x.new_empty(n)) if bias else (None, None))
     _gated_backward(_gated_backward.pack(
-        m, n, k, code, act, *_matrix(dh, "dh", m, n, dtype, device), *_matrix(x, "x", m, k, dtype, device),
+        m, n, k, code, act, *_matrix(dh, "dh", m, n, dtype, device), *at,
         *_matrix(w_gate, "w_gate", n, k, dtype, device), *_matrix(w_up, "w_up", n, k, dtype, device),
         *_matrix(g, "g", m, n, dtype, device), *_matrix(u, "u", m, n, dtype, device),
         *((dx.data_ptr(), k) if need_dx else _NONE),
         *((dwg.data_ptr(), k, dwu.data_ptr(), k) if need_dw else (0, 0, 0, 0)),
-        *((dbg.data_ptr(), dbu.data_ptr()) if bias else (0, 0))), device, stream)
+        *((dbg.data_ptr(), dbu.data_ptr()) if bias else (0, 0))), device)
     return dx, dwg, dwu, dbg, dbu
