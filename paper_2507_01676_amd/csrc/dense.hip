@@ -1049,20 +1049,27 @@ __device__ inline f32x4 multiply(const Loader<TYPE, WHOLE>& w, const Loader<TYPE
   }
 }
 
-// Few rows: the weights are read once, and latency counts.  Eight wavefronts share FR * 16 rows by 16 columns and take
-// every eighth step of 32 each; their sums are added in order in LDS.  bf16, 1 x 512 x 1664: 4.5 us of GPU time, a launch
-// and two rounds of loads; gated 19 x 2816 x 1024: 6.4 us for 11.7 MB.
+// Few rows, few columns, or few of both: the longer operand is read once, and latency counts.  Eight wavefronts share FR *
+// 16 rows by 16 columns and take every eighth step of 32 each; their sums are added in order in LDS.  bf16, 1 x 512 x 1664:
+// 4.5 us of GPU time, a launch and two rounds of loads; gated 19 x 2816 x 1024: 6.4 us for 11.7 MB; f16 65536 x 1 x 1024:
+// 134 MB in 21 us, 6.3 TB/s.
 template <int TYPE, int KIND, int FR, bool WHOLE>
 __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
   using T = typename Elem<TYPE>::T;
   using L = Loader<TYPE, WHOLE>;
   constexpr int kMats = KIND == kGated ? 2 : 1;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
-  const int j0 = blockIdx.x * 16;
+  const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
+  uint32_t i = blockIdx.x / across, j_ = blockIdx.x % across;
+  if (down >= kXcds) {   // rows of x stay with one XCD's L2
+    j_ = blockIdx.x / kXcds % across, i = blockIdx.x / (kXcds * across) * kXcds + blockIdx.x % kXcds;
+    if (i >= down) return;
+  }
+  const int i0 = i * FR * 16, j0 = j_ * 16;
   const T* rows[FR];
   const T* weights[kMats];
 #pragma unroll
-  for (int f = 0; f < FR; ++f) rows[f] = static_cast<const T*>(g.a[0]) + min(f * 16 + c, g.ni - 1) * g.lda;
+  for (int f = 0; f < FR; ++f) rows[f] = static_cast<const T*>(g.a[0]) + min(i0 + f * 16 + c, g.ni - 1) * g.lda;
 #pragma unroll
   for (int m = 0; m < kMats; ++m) weights[m] = static_cast<const T*>(g.b[m]) + min(j0 + c, g.nj - 1) * g.ldb[m];
   f32x4 acc[FR][kMats] = {};
@@ -1085,7 +1092,7 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
     for (int m = 0; m < kMats; ++m) *reinterpret_cast<f32x4*>(&sums[wave][f][m][c][4 * q]) = acc[f][m];
   __syncthreads();
   const int t = threadIdx.x, row = t >> 1, j = j0 + (t & 1) * 8;
-  if (row >= FR * 16 || row >= g.ni || j >= g.nj) return;
+  if (row >= FR * 16 || i0 + row >= g.ni || j >= g.nj) return;
   float s[2][8] = {};
 #pragma unroll
   for (int w = 0; w < 8; ++w)
@@ -1093,7 +1100,7 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
     for (int m = 0; m < kMats; ++m)
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[m][e] += sums[w][row >> 4][m][row & 15][(t & 1) * 8 + e];
-  Finish<TYPE, KIND>(g, 0, row, j, 0).put(s[0], s[1]);
+  Finish<TYPE, KIND>(g, 0, i0 + row, j, 0).put(s[0], s[1]);
 }
 
 // A reduction of at most KS * 32: writing the results is all.  Four wavefronts, each with the weights of FC * 16 columns in
@@ -1365,7 +1372,8 @@ int backward_launch(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c
 
 template <int TYPE, int KIND, int FR>
 int rows_launch(const DenseGemm& g, hipStream_t stream) {
-  const dim3 grid((g.nj + 15) / 16);
+  const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
+  const uint32_t grid = across * (down >= kXcds ? (down + kXcds - 1) / kXcds * kXcds : down);
   if (g.whole) dense_rows<TYPE, KIND, FR, true><<<grid, 512, 0, stream>>>(g);
   else dense_rows<TYPE, KIND, FR, false><<<grid, 512, 0, stream>>>(g);
   return hipGetLastError();
@@ -1388,8 +1396,8 @@ int short_launch(const DenseGemm& given, hipStream_t stream) {
 template <int TYPE, int KIND>
 int forward_launch(const DenseGemm& g, hipStream_t stream) {
   if (g.variant == kRows) {
-    if (g.ni <= 16) return rows_launch<TYPE, KIND, 1>(g, stream);
-    if (g.ni <= 32) return rows_launch<TYPE, KIND, 2>(g, stream);
+    if (g.row_blocks == 1) return rows_launch<TYPE, KIND, 1>(g, stream);
+    if (g.row_blocks == 2) return rows_launch<TYPE, KIND, 2>(g, stream);
     return rows_launch<TYPE, KIND, 4>(g, stream);
   }
   if (g.variant == kShort) {

@@ -34,6 +34,7 @@ struct DenseGemm {
   int32_t ni, nj, nr;      // C is [ni][nj], the sum over nr (in each part)
   int32_t parts, splits, act;   // parts = 0: no product
   int32_t variant;         // DenseVariant
+  int32_t row_blocks;      // kRows: 16 rows each, of a workgroup: 1, 2 or 4
   int32_t row_chunks, short_waves;   // kShort: chunks of 64 rows of a workgroup, its wavefronts along columns
   int32_t whole;           // kRows, kShort: operands' rows start at multiples of 16 bytes and hold whole chunks
 };

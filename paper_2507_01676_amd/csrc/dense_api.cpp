@@ -73,9 +73,10 @@ bool whole16(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
 }
 
 // Which tile a product takes and over how many workgroups its reduction is split.
-struct Choice { int32_t variant, splits; };
+// row_blocks: of kRows.
+struct Choice { int32_t variant, splits, row_blocks; };
 
-constexpr int64_t kFewRows = 64, kShortSum = 64;
+constexpr int64_t kChunkRows = 64, kShortSum = 64;
 
 constexpr int kCus = 256;
 
@@ -120,36 +121,53 @@ double tile_us(int32_t dtype, int variant, double tiles, double steps, int s, do
   return us;
 }
 
-// The same of few rows: workgroups of 16 columns, a step being 32 of the reduction of each of eight wavefronts.  Measured
-// on 1 to 64 rows by 512 to 8192 columns and inputs, with a workgroup on every CU.
-double rows_us(int32_t dtype, int64_t ni, int64_t nj, int64_t nr) {
-  const double groups = double((nj + 15) / 16), steps = double((nr + 255) / 256);
-  const double step = dtype == EMB_DTYPE_F32 ? (ni <= 16 ? 0.95 : ni <= 32 ? 1.3 : 2.2) : (ni <= 16 ? 0.5 : ni <= 32 ? 0.7 : 1.0);
-  return 3.0 + steps * step * std::max(1.0, groups / kCus);
+// The same by workgroups of 16 columns and 16 times `blocks` rows, a step being 32 of the reduction of each of eight
+// wavefronts.  Measured on 1 to 65536 rows by 1 to 8192 columns and 256 to 8192 inputs.  Operands that are not whole are
+// read element by element.
+double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int64_t nj, int64_t nr) {
+  const double groups = double((nj + 15) / 16) * double((ni + 16 * blocks - 1) / (16 * blocks)), steps = double((nr + 255) / 256);
+  const int at = blocks == 1 ? 0 : blocks == 2 ? 1 : 2;
+  static const double k16[] = {0.5, 0.7, 1.05}, k32[] = {0.93, 1.35, 2.45}, kOdd[] = {1.25, 2.4, 4.8},
+                      kOddFull[] = {1.9, 3.05, 5.7}, kTwo16[] = {1.5, 1.33, 1.2}, kTwo32[] = {2.0, 1.6, 1.4};
+  const double step = (!whole ? (groups > kCus ? kOddFull : kOdd) : dtype != EMB_DTYPE_F32 ? k16 : k32)[at];
+  const double two = mats == 1 ? 1.0 : (dtype == EMB_DTYPE_F32 ? kTwo32 : kTwo16)[at];   // a second weight beside each
+  return 3.0 + steps * step * two * std::max(1.0, groups / kCus);
 }
 
-// How a forward product is computed.  What the alternatives measured, in us a call (a call takes 8 from the host):
+// the copies of operands that are not whole
+double pack_us(double bytes) { return 3.0 + bytes / 2.1e6; }
+
+// How a forward product is computed.  What the alternatives measured, in us a call (a call takes 7 from the host):
 //   a reduction of at most 64 and more than 64 rows: the kernel for it (bf16 65536 x 512 x 64 21.7, tiles of 128 27.0; x 32
 //     15.9 and 26.8; f32 x 64 50.5, tiles 72; 4096 x 4096 x 64 15.1 and 15.5)
-//   at most 64 rows: the kernel for them, unless a split tile is estimated to be faster (bf16 16 x 512 x 1664 8.2, best tile
-//     13.6; 16 x 4096 x 4096 9.6 and 13.4; but 64 x 8192 x 8192 72 and 30.4; f32 64 x 4096 x 4096 39.7 and 32.6)
+//   few rows or columns: the kernel for them, where it is estimated to be faster than tiles (bf16 16 x 512 x 1664 8.2, best
+//     tile 13.6; 16 x 4096 x 4096 9.6 and 13.4; f16 2048 x 64 x 1024 6.8 and 12.9, 65536 x 1 x 1024 21.2 and 25.0; but 64 x
+//     8192 x 8192 72 and 30.4, 65536 x 32 x 1024 41 and 24.6; f32 64 x 4096 x 4096 39.7 and 32.6)
 //   tiles of 256 where they fill the GPU (bf16 4096^3 100, tiles of 128 134), of 128 else (2048^3 44 and 27.7), their
 //     reductions split where there are few (f32 4096 x 512 x 1664 whole 65, in two 49.7, in four 62)
-Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k) {
-  if (k <= kShortSum && m > kFewRows) return {kShort, 1};
+// `whole`, `bytes`: whether both operands are, and the size of those that are not.
+Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, bool whole, double bytes) {
+  if (k <= kShortSum && m > kChunkRows) return {kShort, 1, 0};
   const int mats = kind == kGated ? 2 : 1;
   const double steps = static_cast<double>(steps_of(dtype, k)), result_bytes = 4.0 * m * n * mats;
-  Choice best = {kTile128, 1};
-  double least = 0.0;
-  if (m <= kFewRows) best = {kRows, 1}, least = rows_us(dtype, m, n, k);
+  Choice best = {kTile128, 1, 0}, few = {kRows, 1, 1};
+  double least = 0.0, few_us = 0.0;
   for (int variant : {kTile256, kTile128}) {
     const double tiles = static_cast<double>(tiles_of(dtype, variant, m, n * mats));
     for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial)); ++s) {
       const double us = tile_us(dtype, variant, tiles, steps, s, result_bytes);
-      if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, s};
+      if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, s, 0};
     }
   }
-  return best;
+  // weights that come from memory: f32 tiles ask for them two steps ahead, which reaches 2.2 TB/s
+  if (dtype == EMB_DTYPE_F32) least = std::max(least, 4.0 * n * k * mats / 2.2e6);
+  if (!whole) least += pack_us(bytes);
+  for (int blocks : {1, 2, 4}) {
+    if (blocks > 1 && m <= 8 * blocks) break;
+    const double us = rows_us(dtype, mats, whole, blocks, m, n, k);
+    if (few_us == 0.0 || us < few_us) few_us = us, few.row_blocks = blocks;
+  }
+  return few_us <= least ? few : best;
 }
 
 // The tile of a backward pass's two products, and how often the reduction of each is split.
@@ -285,7 +303,7 @@ int32_t slope_blocks(int64_t m, int64_t n) {
 
 // The workspace of each call: copies of operands, dz, column sums and partial sums of products.
 struct Space {
-  Choice choice = {kTile128, 1};   // of the forward calls
+  Choice choice = {kTile128, 1, 0};   // of the forward calls
   Operand x, w[2], dz[2];
   DensePack pack;
   float* colsum[2] = {nullptr, nullptr};
@@ -299,7 +317,9 @@ struct Space {
 Space linear_space(Arena& ar, const emb_linear_t& a) {
   Space s;
   Packer pk{ar, a.dtype};
-  s.choice = choose_forward(a.dtype, kForward, a.m, a.n, a.k);
+  const bool x = whole(a.x, a.ldx, a.k, a.dtype), w = whole(a.weight, a.ldw, a.k, a.dtype);
+  const double bytes = double(esize(a.dtype)) * a.k * ((x ? 0 : a.m) + (w ? 0 : a.n));
+  s.choice = choose_forward(a.dtype, kForward, a.m, a.n, a.k, x && w, bytes);
   pk.where_they_lie = s.choice.variant >= kRows;
   s.x = pk.use(a.x, a.ldx, a.m, a.k);
   s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k);
@@ -311,7 +331,9 @@ Space linear_space(Arena& ar, const emb_linear_t& a) {
 Space gated_space(Arena& ar, const emb_gated_t& a) {
   Space s;
   Packer pk{ar, a.dtype};
-  s.choice = choose_forward(a.dtype, kGated, a.m, a.n, a.k);
+  const bool x = whole(a.x, a.ldx, a.k, a.dtype), w = whole(a.w_gate, a.ld_gate, a.k, a.dtype) && whole(a.w_up, a.ld_up, a.k, a.dtype);
+  const double bytes = double(esize(a.dtype)) * a.k * ((x ? 0 : a.m) + (w ? 0 : 2 * a.n));
+  s.choice = choose_forward(a.dtype, kGated, a.m, a.n, a.k, x && w, bytes);
   pk.where_they_lie = s.choice.variant >= kRows;
   s.x = pk.use(a.x, a.ldx, a.m, a.k);
   s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k);
@@ -415,6 +437,7 @@ emb_status_t emb_linear(const emb_linear_t* a, void* workspace, size_t workspace
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
   g.parts = 1, g.act = a->activation;
   g.variant = sp.choice.variant, g.splits = sp.choice.splits, g.partial = sp.partial;
+  g.row_blocks = sp.choice.row_blocks;
   g.whole = whole(a->x, a->ldx, a->k, a->dtype) && whole(a->weight, a->ldw, a->k, a->dtype);
   return forward(a->dtype, kForward, g, stream);
 }
@@ -512,6 +535,7 @@ emb_status_t emb_gated(const emb_gated_t* a, void* workspace, size_t workspace_b
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
   g.parts = 1, g.act = a->activation;
   g.variant = sp.choice.variant, g.splits = sp.choice.splits, g.partial = sp.partial;
+  g.row_blocks = sp.choice.row_blocks;
   g.whole = whole(a->x, a->ldx, a->k, a->dtype) && whole(a->w_gate, a->ld_gate, a->k, a->dtype) &&
             whole(a->w_up, a->ld_up, a->k, a->dtype);
   return forward(a->dtype, kGated, g, stream);
