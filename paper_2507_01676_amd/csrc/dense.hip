@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/embx_dense.h"
 #include "dense.hpp"
@@ -946,12 +947,22 @@ __device__ inline void join8(const DenseGemm& g, int64_t at, int part) {
     const float* p = g.partial + int64_t(KIND == kGated ? mat : part) * g.splits * slice + at * 8;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[mat][e] = 0.0f;
-#pragma unroll 4
-    for (int split = 0; split < g.splits; ++split, p += slice) {
-      const f32x4 lo = reinterpret_cast<const f32x4*>(p)[0], hi = reinterpret_cast<const f32x4*>(p)[1];
+    int split = 0;
+    auto add = [&](auto count) {   // that many splits' loads at a time
+      constexpr int N = decltype(count)::value;
+      f32x4 lo[N], hi[N];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[mat][e] += lo[e], s[mat][4 + e] += hi[e];
-    }
+      for (int n = 0; n < N; ++n, p += slice) lo[n] = reinterpret_cast<const f32x4*>(p)[0], hi[n] = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[mat][e] += lo[n][e], s[mat][4 + e] += hi[n][e];
+      split += N;
+    };
+    while (g.splits - split >= 8) add(std::integral_constant<int, 8>{});
+    if (g.splits - split >= 4) add(std::integral_constant<int, 4>{});
+    if (g.splits - split >= 2) add(std::integral_constant<int, 2>{});
+    if (g.splits - split >= 1) add(std::integral_constant<int, 1>{});
   }
   Finish<TYPE, KIND>(g, part, i, j, 0).put(s[0], s[1]);
 }
@@ -976,8 +987,13 @@ __global__ __launch_bounds__(256) void dense_tail(DenseGemm w, DenseGemm x, Dens
     if (!p) return;
     float sum = 0.0f;
     if (j < c.n) {
-#pragma unroll 8
-      for (int b = y; b < c.blocks; b += 8) sum += p[int64_t(b) * c.n + j];
+      for (int first = y; first < c.blocks; first += 16 * 8) {
+        float v[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = p[int64_t(min(first + e * 8, c.blocks - 1)) * c.n + j];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) sum += first + e * 8 < c.blocks ? v[e] : 0.0f;
+      }
     }
     sums[y][column] = sum;
     __syncthreads();
