@@ -1400,8 +1400,10 @@ int short_launch(const DenseGemm& given, hipStream_t stream) {
   DenseGemm g = given;
   g.short_waves = g.nj <= FC * 16 ? 1 : g.nj <= FC * 32 ? 2 : 4;
   const int64_t columns = g.short_waves * FC * 16, across = (g.nj + columns - 1) / columns, chunks = (g.ni + 63) / 64;
-  // four workgroups a CU, as long as each has a chunk of rows
-  const int64_t down = std::min(chunks, std::max<int64_t>(1, 1024 / across));
+  // Workgroups, as long as each has a chunk of rows: two a CU, as each loads its weights first (f16 65536 x 64 x 64 7.7 us,
+  // with four 9.6; f32 65536 x 512 x 64 48, 51), but four where there is little to load (f16 65536 x 512 x 32 15.7, with two
+  // 18.1).
+  const int64_t most = KS == 1 && TYPE != kDenseF32 ? 1024 : 512, down = std::min(chunks, std::max<int64_t>(1, most / across));
   g.row_chunks = static_cast<int32_t>((chunks + down - 1) / down);
   const dim3 grid(static_cast<uint32_t>((chunks + g.row_chunks - 1) / g.row_chunks * across));
   if (g.whole) dense_short<TYPE, KIND, FC, KS, true><<<grid, 256, 0, stream>>>(g);
