@@ -31,32 +31,33 @@ class _Entry:
     activation, then matrices (pointer, row stride; "M") and vectors (pointer; "V").  (A small call's time is the
     host's: a ctypes.Structure takes three times as long to fill.)"""
 
-    def __init__(self, name, layout):
+    def __init__(self, name, layout, asks):
         self.name = name
+        self.asks = asks   # most calls need a workspace: its size is asked for first, not after a refusal
         packer = struct.Struct("@qqqii" + "".join("Pq" if f == "M" else "P" for f in layout))
         self.pack, self.bytes = packer.pack, packer.size
         self.fn, self.size = getattr(_lib, name), getattr(_lib, name + "_workspace")
         self.fn.restype, self.fn.argtypes = _i32, [ctypes.c_char_p, _vp, _sz, _vp]
         self.size.restype, self.size.argtypes = _i32, [ctypes.c_char_p, ctypes.POINTER(_sz)]
 
-    def __call__(self, a, device):
+    def __call__(self, a, x, device):
         stream = _current_stream(device)
-        code = self.fn(a, None, 0, stream)   # most small calls need no workspace
+        code = ERR_INVALID_ARGUMENT if self.asks else self.fn(a, None, 0, stream)
         if code == ERR_INVALID_ARGUMENT:
             nbytes = _sz(0)
             code = self.size(a, nbytes)
             if code == OK:
                 nbytes = nbytes.value
-                ws = torch.empty(nbytes, dtype=torch.uint8, device=device)
+                ws = x.new_empty(nbytes, dtype=torch.uint8)
                 code = self.fn(a, ws.data_ptr(), nbytes, stream)
         if code != OK:
             raise EmbxError(code, self.name)
 
 
-_linear = _Entry("emb_linear", "MMVMMM")                  # x weight bias residual y z
-_linear_backward = _Entry("emb_linear_backward", "MMMMMMV")   # dy x weight z dx dweight dbias
-_gated = _Entry("emb_gated", "MMMVVMMM")                  # x w_gate w_up b_gate b_up h g u
-_gated_backward = _Entry("emb_gated_backward", "MMMMMMMMMVV")   # dh x w_gate w_up g u dx dw_gate dw_up db_gate db_up
+_linear = _Entry("emb_linear", "MMVMMM", False)                  # x weight bias residual y z
+_linear_backward = _Entry("emb_linear_backward", "MMMMMMV", True)   # dy x weight z dx dweight dbias
+_gated = _Entry("emb_gated", "MMMVVMMM", False)                  # x w_gate w_up b_gate b_up h g u
+_gated_backward = _Entry("emb_gated_backward", "MMMMMMMMMVV", True)   # dh x w_gate w_up g u dx dw_gate dw_up db_gate db_up
 _NONE = (0, 0)
 
 
@@ -157,7 +158,7 @@ def linear(x, weight, bias=None, residual=None, *, activation="none", out=None, 
                          *_matrix(weight, "weight", n, k, dtype, device), _vector(bias, "bias", n, dtype, device),
                          *(_NONE if residual is None else _matrix(residual, "residual", m, n, dtype, device)),
                          *((y.data_ptr(), n) if out is None else _matrix(y, "out", m, n, dtype, device)),
-                         *((z.data_ptr(), n) if save else _NONE)), device)
+                         *((z.data_ptr(), n) if save else _NONE)), x, device)
     return (y, z) if save else y
 
 
@@ -180,7 +181,7 @@ def linear_backward(dy, x, weight, z=None, *, activation="none", bias=True, stre
         m, n, k, code, act, *_matrix(dy, "dy", m, n, dtype, device), *at,
         *_matrix(weight, "weight", n, k, dtype, device), *(_matrix(z, "z", m, n, dtype, device) if act else _NONE),
         *((dx.data_ptr(), k) if need_dx else _NONE), *((dw.data_ptr(), k) if need_dw else _NONE),
-        db.data_ptr() if bias else 0), device)
+        db.data_ptr() if bias else 0), x, device)
     return dx, dw, db
 
 
@@ -198,7 +199,7 @@ def gated_ffn(x, w_gate, w_up, b_gate=None, b_up=None, *, activation="silu", out
                        *_matrix(w_gate, "w_gate", n, k, dtype, device), *_matrix(w_up, "w_up", n, k, dtype, device),
                        _vector(b_gate, "b_gate", n, dtype, device), _vector(b_up, "b_up", n, dtype, device),
                        *((h.data_ptr(), n) if out is None else _matrix(h, "out", m, n, dtype, device)),
-                       *((g.data_ptr(), n, u.data_ptr(), n) if save else (0, 0, 0, 0))), device)
+                       *((g.data_ptr(), n, u.data_ptr(), n) if save else (0, 0, 0, 0))), x, device)
     return (h, g, u) if save else h
 
 
@@ -221,5 +222,5 @@ def gated_ffn_backward(dh, x, w_gate, w_up, g, u, *, activation="silu", bias=Fal
         *_matrix(g, "g", m, n, dtype, device), *_matrix(u, "u", m, n, dtype, device),
         *((dx.data_ptr(), k) if need_dx else _NONE),
         *((dwg.data_ptr(), k, dwu.data_ptr(), k) if need_dw else (0, 0, 0, 0)),
-        *((dbg.data_ptr(), dbu.data_ptr()) if bias else (0, 0))), device)
+        *((dbg.data_ptr(), dbu.data_ptr()) if bias else (0, 0))), x, device)
     return dx, dwg, dwu, dbg, dbu
