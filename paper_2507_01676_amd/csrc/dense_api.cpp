@@ -275,8 +275,8 @@ struct Packer {
     uint32_t wide = 8;
     while (wide < 256 && wide < ldd) wide *= 2;
     pack.wide[at] = wide;
-    // enough workgroups for the longest matrix, at most eight a CU
-    pack.groups = std::max<int32_t>(pack.groups, static_cast<int32_t>(std::min<int64_t>(8 * kCus, (rows * wide + 255) / 256)));
+    // enough workgroups for the longest matrix, with four rows a thread, at most eight a CU
+    pack.groups = std::max<int32_t>(pack.groups, static_cast<int32_t>(std::min<int64_t>(8 * kCus, (rows * wide + 1023) / 1024)));
     return {pack.dst[at], ldd};
   }
 };
