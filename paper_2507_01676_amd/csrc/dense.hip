@@ -375,8 +375,8 @@ __device__ inline void tile_of(uint32_t id, uint32_t tiles_i, uint32_t tiles_j, 
   *tj = in / rows;
 }
 
-// Eight consecutive elements at p, of which n >= 1 are inside (the last one stands for the others); whole eights are read and written 16 bytes at a time at
-// any alignment.
+// Eight consecutive elements at p, of which n >= 1 are inside (the last one stands for the others); whole eights are read
+// and written 16 bytes at a time at any alignment.
 template <int TYPE>
 __device__ inline void load8(const void* p, int n, float* v) {
   using T = typename Elem<TYPE>::T;
@@ -952,7 +952,10 @@ __device__ inline void join8(const DenseGemm& g, int64_t at, int part) {
       constexpr int N = decltype(count)::value;
       f32x4 lo[N], hi[N];
 #pragma unroll
-      for (int n = 0; n < N; ++n, p += slice) lo[n] = reinterpret_cast<const f32x4*>(p)[0], hi[n] = reinterpret_cast<const f32x4*>(p)[1];
+      for (int n = 0; n < N; ++n, p += slice) {
+        lo[n] = reinterpret_cast<const f32x4*>(p)[0];
+        hi[n] = reinterpret_cast<const f32x4*>(p)[1];
+      }
 #pragma unroll
       for (int n = 0; n < N; ++n)
 #pragma unroll

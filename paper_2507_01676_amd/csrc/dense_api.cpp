@@ -72,8 +72,8 @@ bool whole16(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
   return !misaligned(p, 16) && ld * esize(dtype) % 16 == 0 && cols % 8 == 0;
 }
 
-// Which tile a product takes and over how many workgroups its reduction is split.
-// row_blocks: of kRows.
+// Which kernel a product takes (DenseVariant), over how many workgroups its reduction is split and, of kRows, how many
+// times 16 rows a workgroup has.
 struct Choice { int32_t variant, splits, row_blocks; };
 
 constexpr int64_t kChunkRows = 64, kShortSum = 64;
@@ -331,7 +331,8 @@ Space linear_space(Arena& ar, const emb_linear_t& a) {
 Space gated_space(Arena& ar, const emb_gated_t& a) {
   Space s;
   Packer pk{ar, a.dtype};
-  const bool x = whole(a.x, a.ldx, a.k, a.dtype), w = whole(a.w_gate, a.ld_gate, a.k, a.dtype) && whole(a.w_up, a.ld_up, a.k, a.dtype);
+  const bool x = whole(a.x, a.ldx, a.k, a.dtype);
+  const bool w = whole(a.w_gate, a.ld_gate, a.k, a.dtype) && whole(a.w_up, a.ld_up, a.k, a.dtype);
   const double bytes = double(esize(a.dtype)) * a.k * ((x ? 0 : a.m) + (w ? 0 : 2 * a.n));
   s.choice = choose_forward(a.dtype, kGated, a.m, a.n, a.k, x && w, bytes);
   pk.where_they_lie = s.choice.variant >= kRows;
