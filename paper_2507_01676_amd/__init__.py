@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import sys
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -432,5 +433,6 @@ def dedup_tile(idx, stream=None):
     return uniq[:k], inv[:n]
 
 
-if torch is not None:
+# (This file alone, loaded under another name beside the package, has no package to import from: it has the lookup.)
+if torch is not None and __name__ in sys.modules:
     from .dense import ACTIVATIONS, gated_ffn, gated_ffn_backward, linear, linear_backward  # noqa: E402,F401

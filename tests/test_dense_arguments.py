@@ -135,3 +135,12 @@ def test_binding_refuses_host_tensors():
                   lambda: embx.gated_ffn_backward(torch.zeros(3, 5), x, w, w, torch.zeros(3, 5), torch.zeros(3, 5))):
         with pytest.raises(ValueError):
             call_()
+
+
+def test_the_package_file_loads_under_another_name():
+    """Beside the package, without being one: the lookup of another build of the library."""
+    import importlib.util
+    spec = importlib.util.spec_from_file_location("embx_other", embx.__file__)
+    other = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(other)
+    assert other.Plan is not embx.Plan and not hasattr(other, "linear") and hasattr(embx, "linear")
