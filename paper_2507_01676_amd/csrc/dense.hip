@@ -483,21 +483,22 @@ struct Finish {
 // that a lane has eight consecutive columns and the activation's code is there once.  Lane (q, c) holds row c and
 // columns 4 q .. + 3 of each fragment.  The 16-byte chunks of a row in LDS are permuted by the row.
 template <int FJ>
-constexpr int kSumsLds = 64 * FJ * 64;
+constexpr int kSumsLds = 64 * FJ * 64;   // (half of it with two fragments of rows)
 
 template <int TYPE, int KIND, int FI, int FJ>
 __device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char* own, int lane, int64_t i0, int j0, int part,
                                   int split) {
   constexpr bool kGate = KIND == kGated;
   constexpr int kRowBytes = FJ * 64, kMask = FJ * 4 - 1, kUp = FJ * 2;   // kUp: first chunk of the up projection
+  constexpr int kPass = FI < 4 ? FI : 4;   // fragments of rows at a time
   const int q = lane >> 4, c = lane & 15;
 #pragma unroll
-  for (int h = 0; h < FI / 4; ++h) {
+  for (int h = 0; h < FI / kPass; ++h) {
 #pragma unroll
-    for (int fi = 0; fi < 4; ++fi)
+    for (int fi = 0; fi < kPass; ++fi)
 #pragma unroll
       for (int fj = 0; fj < FJ; ++fj)
-        *reinterpret_cast<f32x4*>(own + (fi * 16 + c) * kRowBytes + (((fj * 4 + q) ^ (c & kMask)) << 4)) = acc[h * 4 + fi][fj];
+        *reinterpret_cast<f32x4*>(own + (fi * 16 + c) * kRowBytes + (((fj * 4 + q) ^ (c & kMask)) << 4)) = acc[h * kPass + fi][fj];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     constexpr int kLanes = kGate ? FJ : FJ * 2, kRows = 64 / kLanes;   // lanes of a row, rows at a time
     const int e = lane % kLanes * 2, j = j0 + e * 4;                   // the row's first chunk of this lane
@@ -520,7 +521,7 @@ __device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char
         const int64_t ld = (g.nj + 7) / 8 * 8, slice = int64_t(g.ni) * ld;
         float* p = g.partial + (int64_t(kGate ? 0 : part) * g.splits + split) * slice + first * ld + j;
 #pragma unroll 1
-        for (int row0 = 0; row0 < 64; row0 += kRows, p += kRows * ld) {
+        for (int row0 = 0; row0 < kPass * 16; row0 += kRows, p += kRows * ld) {
           if (first + row0 >= g.ni) break;
           sums(row0 + lane / kLanes, s0, s1);
           reinterpret_cast<f32x4*>(p)[0] = f32x4{s0[0], s0[1], s0[2], s0[3]};
@@ -534,7 +535,7 @@ __device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char
       } else {
         Finish<TYPE, KIND> out(g, part, first, j, kRows);
 #pragma unroll 1
-        for (int row0 = 0; row0 < 64; row0 += kRows, out.next()) {
+        for (int row0 = 0; row0 < kPass * 16; row0 += kRows, out.next()) {
           if (first + row0 >= g.ni) break;
           sums(row0 + lane / kLanes, s0, s1);
           out.put(s0, s1);
@@ -590,7 +591,7 @@ __device__ __noinline__ void tile_by_f32(const DenseGemm& g, char* lds, int i0, 
 
 // bytes of LDS of a tile: the steps under way, or what the epilogue takes
 template <int TYPE, int BM, int BN, int WJ, int WAVES>
-constexpr int kTileLds = [] {
+constexpr int kTileLds = [] {   // (of each half)
   const int steps = TYPE == kDenseF32 ? (BM + BN) * 64 * 3 * 2     // three bf16 parts of two steps
                                       : ((WAVES == 8 ? 3 : 2) * BM + 2 * BN) * 128;
   const int sums = WAVES * kSumsLds<BN / WJ / 16>;
@@ -601,6 +602,9 @@ constexpr int kTileLds = [] {
 // loops:
 //   16 bits, 128 x 128, four wavefronts of 64 x 64, two workgroups a CU: for products that do not fill the GPU with larger
 //     ones; a tile's operands pass through L2 twice as often as those of 256 x 256 (bf16 8192^3: 1004 us, 1.1 PFLOP/s)
+//     where there is no second tile for a CU (HALVES = 2), eight wavefronts of one workgroup: each four take half of the
+//     steps, as two workgroups would, and then half of the rows of the sum (bf16 4096 x 1024 x 1024 14.2 us a call, with
+//     four wavefronts 16.9)
 //   16 bits, 256 x 256, eight wavefronts of 128 x 64 in turns, one workgroup a CU (its 160 KB of LDS, and 128 + 96 of the
 //     registers): bf16 8192^3 765 us, 1.44 PFLOP/s, where one library product reaches 1.42 to 1.61; 65536 x 1024 x 12800
 //     1255 us, 1.37.  Bound by the matrix cores at the clock that they leave (about 1.75 GHz), less some 7 us a tile for its
@@ -608,8 +612,8 @@ constexpr int kTileLds = [] {
 //     loads wait for the stores before them)
 //   f32, 256 x 128 or 128 x 128, eight wavefronts, one workgroup a CU: see PartTile; 4096^3 610 us, 225 TFLOP/s (f32
 //     products on the matrix cores reach 153 in a library)
-template <int TYPE, int KIND, int BM, int BN, int WI, int WJ>
-__device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint32_t tile, int split, int wpart) {
+template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int HALVES>
+__device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint32_t tile, int split, int wpart) {
   constexpr bool kGate = KIND == kGated;
   constexpr bool kRmA = KIND == kWeightGrad, kRmB = KIND == kWeightGrad || KIND == kInputGrad;
   constexpr int kWaves = WI * WJ;
@@ -625,14 +629,22 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
   constexpr int BK = kF32 ? 32 : TileA::BK;
   static_assert(kF32 || kSlotsA * TileA::kBytes + kSlotsB * TileB::kBytes <= kTileLds<TYPE, BM, BN, WJ, kWaves>);
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  static_assert(HALVES == 1 || (!kF32 && !kTurns && kFI == 4));
+  const int half = HALVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x / (64 * kWaves));
+  char* const lds = all + half * kTileLds<TYPE, BM, BN, WJ, kWaves>;
+  const int tid = threadIdx.x - half * 64 * kWaves, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int ti, tj;
   tile_of(tile, (g.ni + BM - 1) / BM, (g.nj + kCols - 1) / kCols, &ti, &tj);
   const int i0 = ti * BM, j0 = tj * kCols;
   const int per_part = (g.nr + BK - 1) / BK;
   const int steps = per_part * (KIND == kInputGrad ? g.parts : 1);
-  const int begin = static_cast<int>(int64_t(steps) * split / g.splits);
-  const int end = static_cast<int>(int64_t(steps) * (split + 1) / g.splits);
+  int begin = static_cast<int>(int64_t(steps) * split / g.splits);
+  int end = static_cast<int>(int64_t(steps) * (split + 1) / g.splits);
+  const int trips = (end - begin + HALVES - 1) / HALVES;   // of both halves alike: a step past the end is zeros
+  if constexpr (HALVES == 2) {
+    if (half == 0) end = min(end, begin + trips);
+    else begin = min(end, begin + trips);
+  }
 
   TileA ta;
   ta.init(wave, lane, g.lda, g.ni - i0);
@@ -775,7 +787,7 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
     set_b(begin, 0);
 #pragma unroll
     for (int n = 0; n < kIssues; ++n) issue(n);
-    for (int step = begin; step < end; ++step) {
+    for (int step = begin, left = trips; left > 0; ++step, --left) {
       stage_done<0>();
       const char* sa = lds + at_a * TileA::kBytes;
       const char* sb = lds + kAreaB + at_a * TileB::kBytes;
@@ -906,31 +918,59 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* lds, uint
 #pragma unroll
       for (int fj = 0; fj < kFJ; ++fj) acc[fi][fj] *= 1.0f / (kScale * kScale);
   }
-  store_sums<TYPE, KIND, kFI, kFJ>(g, acc, lds + wave * kSumsLds<kFJ>, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
+  if constexpr (HALVES == 2) {
+    // the first half gives its lower rows away, the second its upper ones
+    char* const pass = all + wave * 2 * kFJ * 1024 + lane * 16;
+    constexpr int kGiven = kWaves * 2 * kFJ * 1024;   // bytes that a half gives
+    auto give = [&](int from) {
+#pragma unroll
+      for (int fi = 0; fi < 2; ++fi)
+#pragma unroll
+        for (int fj = 0; fj < kFJ; ++fj) *reinterpret_cast<f32x4*>(pass + half * kGiven + (fi * kFJ + fj) * 1024) = acc[from + fi][fj];
+    };
+    if (half == 0) give(2);
+    else give(0);
+    __syncthreads();
+    f32x4 sum[2][kFJ];
+    auto take = [&](int at) {
+#pragma unroll
+      for (int fi = 0; fi < 2; ++fi)
+#pragma unroll
+        for (int fj = 0; fj < kFJ; ++fj)
+          sum[fi][fj] = acc[at + fi][fj] + *reinterpret_cast<const f32x4*>(pass + (half ^ 1) * kGiven + (fi * kFJ + fj) * 1024);
+    };
+    if (half == 0) take(0);
+    else take(2);
+    char* const own = all + 2 * kGiven + (half * kWaves + wave) * (kSumsLds<kFJ> / 2);
+    static_assert(2 * kGiven + kWaves * kSumsLds<kFJ> <= HALVES * kTileLds<TYPE, BM, BN, WJ, kWaves>);
+    store_sums<TYPE, KIND, 2, kFJ>(g, sum, own, lane, int64_t(i0) + wi + half * 32, j0 + wj, wpart, split);
+  } else {
+    store_sums<TYPE, KIND, kFI, kFJ>(g, acc, lds + wave * kSumsLds<kFJ>, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
+  }
 }
 
-template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
-__global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_tile(DenseGemm g) {
-  __shared__ __align__(1024) char lds[kTileLds<TYPE, BM, BN, WJ, WI * WJ>];
-  tile_product<TYPE, KIND, BM, BN, WI, WJ>(g, lds, blockIdx.x, blockIdx.y, 0);
+template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU, int HALVES>
+__global__ __launch_bounds__(64 * WI * WJ * HALVES, WI * WJ * HALVES * PER_CU / 4) void dense_tile(DenseGemm g) {
+  __shared__ __align__(1024) char lds[HALVES * kTileLds<TYPE, BM, BN, WJ, WI * WJ>];
+  tile_product<TYPE, KIND, BM, BN, WI, WJ, HALVES>(g, lds, blockIdx.x, blockIdx.y, 0);
 }
 
 // Both products of a backward pass in one launch: the weights' gradient first, whose tiles are few and long, then the
 // input's, whose many short ones fill the CUs that are left (either may be absent).  With this
 // launch and the last one instead of a launch for each, a call took 250 us instead of 265 (f16 16384 x 1024 x 3328), 272
 // instead of 315 (gated, bf16 8192 x 4096 x 1024) and 43 instead of 55 (gated, f16 777 x 1365 x 1001).
-template <int TYPE, int BM, int BN, int WI, int WJ, int PER_CU>
-__global__ __launch_bounds__(64 * WI * WJ, WI * WJ * PER_CU / 4) void dense_grads(DenseGemm w, DenseGemm x, uint32_t w_groups) {
-  __shared__ __align__(1024) char lds[kTileLds<TYPE, BM, BN, WJ, WI * WJ>];
+template <int TYPE, int BM, int BN, int WI, int WJ, int PER_CU, int HALVES>
+__global__ __launch_bounds__(64 * WI * WJ * HALVES, WI * WJ * HALVES * PER_CU / 4) void dense_grads(DenseGemm w, DenseGemm x, uint32_t w_groups) {
+  __shared__ __align__(1024) char lds[HALVES * kTileLds<TYPE, BM, BN, WJ, WI * WJ>];
   uint32_t id = blockIdx.x;
   if (id < w_groups) {
     const uint32_t tiles = (w.ni + BM - 1) / BM * ((w.nj + BN - 1) / BN), rest = id / tiles;
     if (rest >= uint32_t(w.splits * w.parts)) return;   // (w_groups is a multiple of the XCDs)
-    tile_product<TYPE, kWeightGrad, BM, BN, WI, WJ>(w, lds, id % tiles, rest % w.splits, rest / w.splits);
+    tile_product<TYPE, kWeightGrad, BM, BN, WI, WJ, HALVES>(w, lds, id % tiles, rest % w.splits, rest / w.splits);
   } else {
     id -= w_groups;
     const uint32_t tiles = (x.ni + BM - 1) / BM * ((x.nj + BN - 1) / BN);
-    tile_product<TYPE, kInputGrad, BM, BN, WI, WJ>(x, lds, id % tiles, id / tiles, 0);
+    tile_product<TYPE, kInputGrad, BM, BN, WI, WJ, HALVES>(x, lds, id % tiles, id / tiles, 0);
   }
 }
 
@@ -1355,23 +1395,24 @@ __global__ __launch_bounds__(256) void dense_slope(DenseSlope s) {
   }
 }
 
-template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU>
+template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int PER_CU, int HALVES = 1>
 int tile_launch(const DenseGemm& g, hipStream_t stream) {
   const int cols = KIND == kGated ? BN / 2 : BN;
   const int64_t tiles = int64_t((g.ni + BM - 1) / BM) * ((g.nj + cols - 1) / cols);
-  dense_tile<TYPE, KIND, BM, BN, WI, WJ, PER_CU><<<dim3(static_cast<uint32_t>(tiles), g.splits), 64 * WI * WJ, 0, stream>>>(g);
+  const dim3 grid(static_cast<uint32_t>(tiles), g.splits);
+  dense_tile<TYPE, KIND, BM, BN, WI, WJ, PER_CU, HALVES><<<grid, 64 * WI * WJ * HALVES, 0, stream>>>(g);
   if (const int rc = hipGetLastError(); rc != 0 || g.splits == 1) return rc;
   const int64_t threads = int64_t((g.nj + 7) / 8) * g.ni;
   dense_join<TYPE, KIND><<<static_cast<uint32_t>((threads + 255) / 256), 256, 0, stream>>>(g);
   return hipGetLastError();
 }
 
-template <int TYPE, int BM, int BN, int WI, int WJ, int PER_CU>
+template <int TYPE, int BM, int BN, int WI, int WJ, int PER_CU, int HALVES = 1>
 int grads_launch(const DenseGemm& w, const DenseGemm& x, hipStream_t stream) {
   auto tiles = [](const DenseGemm& g) { return int64_t((g.ni + BM - 1) / BM) * ((g.nj + BN - 1) / BN) * g.splits; };
   const int64_t w_groups = w.parts ? (tiles(w) * w.parts + kXcds - 1) / kXcds * kXcds : 0, x_groups = x.parts ? tiles(x) : 0;
   if (w_groups + x_groups == 0) return 0;
-  dense_grads<TYPE, BM, BN, WI, WJ, PER_CU><<<static_cast<uint32_t>(w_groups + x_groups), 64 * WI * WJ, 0, stream>>>(
+  dense_grads<TYPE, BM, BN, WI, WJ, PER_CU, HALVES><<<static_cast<uint32_t>(w_groups + x_groups), 64 * WI * WJ * HALVES, 0, stream>>>(
       w, x, static_cast<uint32_t>(w_groups));
   return hipGetLastError();
 }
@@ -1383,6 +1424,7 @@ int backward_launch(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c
     if (variant == kTile256) rc = grads_launch<TYPE, 256, 128, 4, 2, 1>(w, x, stream);
     else rc = grads_launch<TYPE, 128, 128, 2, 4, 1>(w, x, stream);
   } else if (variant == kTile256) rc = grads_launch<TYPE, 256, 256, 2, 4, 1>(w, x, stream);
+  else if (variant == kTile128Halves) rc = grads_launch<TYPE, 128, 128, 2, 2, 1, 2>(w, x, stream);
   else rc = grads_launch<TYPE, 128, 128, 2, 2, 2>(w, x, stream);
   if (rc != 0) return rc;
   auto joins = [](const DenseGemm& g) {
@@ -1437,6 +1479,7 @@ int forward_launch(const DenseGemm& g, hipStream_t stream) {
     return tile_launch<TYPE, KIND, 128, 128, 2, 4, 1>(g, stream);
   }
   else if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 256, 2, 4, 1>(g, stream);
+  else if (g.variant == kTile128Halves) return tile_launch<TYPE, KIND, 128, 128, 2, 2, 1, 2>(g, stream);
   else return tile_launch<TYPE, KIND, 128, 128, 2, 2, 2>(g, stream);
 }
 

@@ -18,7 +18,7 @@ enum DenseKind {
   kWeightGrad = 3    // C[i][j] = sum_r A[r][i] B[r][j]   A = dz, B = x       (R, R)
 };
 
-enum DenseVariant { kTile128 = 0, kTile256 = 1, kRows = 2, kShort = 3 };
+enum DenseVariant { kTile128 = 0, kTile256 = 1, kTile128Halves = 2, kRows = 3, kShort = 4 };
 
 // One matrix product.  Arrays of two: kGated's two weights and results; kInputGrad's two
 // products summed into one result (parts = 2); kWeightGrad's two results (parts = 2).

@@ -81,16 +81,25 @@ constexpr int64_t kChunkRows = 64, kShortSum = 64;
 constexpr int kCus = 256;
 
 // Microseconds of a step of 128 bytes of the reduction: where a CU has one workgroup on a GPU that is otherwise idle, and
-// where every CU is full (the clock drops, and L2 is shared), with how many.  Measured on products of 256 to 8192 rows,
-// with 16-bit types by tiles of 256 x 256 or 128 x 128, with f32 by 256 x 128 or 128 x 128.  A tile starts and ends in 3 us.
-struct StepTime { double alone, full; int per_cu; };
+// where every CU is full (the clock drops, and L2 is shared), with how many; and those in which a tile starts and ends.
+// Measured on products of 256 to 8192 rows, with 16-bit types by tiles of 256 x 256 or 128 x 128, the latter whole or in
+// halves, which take two steps at a time, with f32 by 256 x 128 or 128 x 128.
+struct TileTime { double alone, full; int per_cu; double ends; int at_a_time; };
 
-StepTime step_us(int32_t dtype, int variant) {
-  if (dtype == EMB_DTYPE_F32) return variant == kTile256 ? StepTime{2.05, 2.35, 1} : StepTime{1.17, 1.30, 1};
-  return variant == kTile256 ? StepTime{0.97, 1.50, 1} : StepTime{0.62, 1.03, 2};
+TileTime tile_time(int32_t dtype, int variant) {
+  if (dtype == EMB_DTYPE_F32) return variant == kTile256 ? TileTime{2.05, 2.35, 1, 3.0, 1} : TileTime{1.17, 1.30, 1, 3.0, 1};
+  return variant == kTile256 ? TileTime{0.97, 1.50, 1, 3.0, 1}
+                             : variant == kTile128 ? TileTime{0.62, 1.03, 2, 3.0, 1} : TileTime{0.49, 0.55, 1, 2.6, 2};
 }
 
-constexpr double kTileUs = 3.0, kLaunchUs = 5.0;
+constexpr int kTiles[] = {kTile256, kTile128, kTile128Halves};
+
+int tile_count(int32_t dtype) { return dtype == EMB_DTYPE_F32 ? 2 : 3; }
+
+// steps of a tile whose reduction is split s ways
+double steps_each(const TileTime& t, double steps, int s) { return std::ceil(steps / s / t.at_a_time) * t.at_a_time; }
+
+constexpr double kLaunchUs = 5.0, kCallUs = 2.0;   // of a further launch, and what the first adds to the tiles' times
 constexpr double kJoinBytes = 3.0e6;      // a microsecond, of partial sums written and read back
 constexpr double kMostPartial = 256 << 20;
 
@@ -105,18 +114,18 @@ int64_t steps_of(int32_t dtype, int64_t nr) {
 }
 
 // of a step where `groups` workgroups are on the GPU
-double step_of(const StepTime& t, double groups) {
+double step_of(const TileTime& t, double groups) {
   if (t.per_cu == 1) return t.alone + (t.full - t.alone) * std::min(1.0, groups / kCus);
   return groups <= kCus ? t.alone : t.full;
 }
 
 // a forward product whose reduction is split s ways
 double tile_us(int32_t dtype, int variant, double tiles, double steps, int s, double result_bytes) {
-  const StepTime t = step_us(dtype, variant);
-  const double groups = tiles * s, each = std::ceil(steps / s), slots = kCus * t.per_cu;
+  const TileTime t = tile_time(dtype, variant);
+  const double groups = tiles * s, each = steps_each(t, steps, s), slots = kCus * t.per_cu;
   const double whole = std::floor(groups / slots), rest = groups - whole * slots;
-  double us = whole * (each * t.full + kTileUs);
-  if (rest > 0) us += each * (whole > 0 && t.per_cu == 1 ? t.full : step_of(t, rest)) + kTileUs;
+  double us = whole * (each * t.full + t.ends);
+  if (rest > 0) us += each * (whole > 0 && t.per_cu == 1 ? t.full : step_of(t, rest)) + t.ends;
   if (s > 1) us += kLaunchUs + result_bytes * s / kJoinBytes;
   return us;
 }
@@ -143,8 +152,9 @@ double pack_us(double bytes) { return 3.0 + bytes / 2.1e6; }
 //   few rows or columns: the kernel for them, where it is estimated to be faster than tiles (bf16 16 x 512 x 1664 8.2, best
 //     tile 13.6; 16 x 4096 x 4096 9.6 and 13.4; f16 2048 x 64 x 1024 6.8 and 12.9, 65536 x 1 x 1024 21.2 and 25.0; but 64 x
 //     8192 x 8192 72 and 30.4, 65536 x 32 x 1024 41 and 24.6; f32 64 x 4096 x 4096 39.7 and 32.6)
-//   tiles of 256 where they fill the GPU (bf16 4096^3 100, tiles of 128 134), of 128 else (2048^3 44 and 27.7), their
-//     reductions split where there are few (f32 4096 x 512 x 1664 whole 65, in two 49.7, in four 62)
+//   tiles of 256 where they fill the GPU (bf16 4096^3 100, tiles of 128 134), of 128 else (2048^3 44 and 27.7), in halves
+//     where a CU has one (4096 x 1024 x 1024 14.2, whole 16.9; 2 x 704 columns, 352 tiles, 13.2 and 9.3), their reductions
+//     split where there are few (f32 4096 x 512 x 1664 whole 65, in two 49.7, in four 62)
 // `whole`, `bytes`: whether both operands are, and the size of those that are not.
 Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, bool whole, double bytes) {
   if (k <= kShortSum && m > kChunkRows) return {kShort, 1, 0};
@@ -152,7 +162,8 @@ Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, 
   const double steps = static_cast<double>(steps_of(dtype, k)), result_bytes = 4.0 * m * n * mats;
   Choice best = {kTile128, 1, 0}, few = {kRows, 1, 1};
   double least = 0.0, few_us = 0.0;
-  for (int variant : {kTile256, kTile128}) {
+  for (int i = 0; i < tile_count(dtype); ++i) {
+    const int variant = kTiles[i];
     const double tiles = static_cast<double>(tiles_of(dtype, variant, m, n * mats));
     for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial)); ++s) {
       const double us = tile_us(dtype, variant, tiles, steps, s, result_bytes);
@@ -161,6 +172,7 @@ Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, 
   }
   // weights that come from memory: f32 tiles ask for them two steps ahead, which reaches 2.2 TB/s
   if (dtype == EMB_DTYPE_F32) least = std::max(least, 4.0 * n * k * mats / 2.2e6);
+  least += kCallUs;   // (rows_us counts from the launch)
   if (!whole) least += pack_us(bytes);
   for (int blocks : {1, 2, 4}) {
     if (blocks > 1 && m <= 8 * blocks) break;
@@ -191,8 +203,9 @@ GradChoice choose_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, int m
   const double w_bytes = 4.0 * n * k * want_w, x_bytes = 4.0 * m * k;
   GradChoice best = {kTile128, 1, 1};
   double least = 0.0;
-  for (int variant : {kTile256, kTile128}) {
-    const StepTime t = step_us(dtype, variant);
+  for (int i = 0; i < tile_count(dtype); ++i) {
+    const int variant = kTiles[i];
+    const TileTime t = tile_time(dtype, variant);
     const int64_t w_tiles = want_w * tiles_of(dtype, variant, n, k), x_tiles = want_x ? tiles_of(dtype, variant, m, k) : 0;
     for (int sw : kSplits) {
       if (sw > 1 && (!want_w || sw * 4 > w_steps || w_bytes * sw > kMostPartial || w_tiles * sw > 8 * kCus)) break;
@@ -200,8 +213,8 @@ GradChoice choose_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, int m
         if (sx > 1 && (!want_x || sx * 4 > x_steps || x_bytes * sx > kMostPartial || x_tiles * sx > 8 * kCus)) break;
         const int64_t items = w_tiles * sw + x_tiles * sx, slots = items <= kCus ? kCus : kCus * t.per_cu;
         const double step = step_of(t, static_cast<double>(items));
-        double us = both_us(slots, w_tiles * sw, (w_steps + sw - 1) / sw * step + kTileUs, x_tiles * sx,
-                            (x_steps + sx - 1) / sx * step + kTileUs);
+        double us = both_us(slots, w_tiles * sw, steps_each(t, w_steps, sw) * step + t.ends, x_tiles * sx,
+                            steps_each(t, x_steps, sx) * step + t.ends);
         if (sw > 1 || sx > 1 || sums) us += kLaunchUs;
         us += ((sw > 1 ? w_bytes * sw : 0.0) + (sx > 1 ? x_bytes * sx : 0.0)) / kJoinBytes;
         if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, sw, sx};

@@ -473,3 +473,38 @@ def test_infinities_and_nan_with_every_kernel(gpu_lib, size, dtype):
     z[0] = -1.0
     dx, dw, db = gpu_lib.linear_backward(dy, x.nan_to_num(1.0, 1.0), w, z, activation="relu")
     assert not R.d(dx)[0].any() and bool(torch.isfinite(R.d(dw)).all()) and bool(torch.isfinite(R.d(db)).all())
+
+
+@pytest.mark.parametrize("size", [(300, 136, 520), (70, 8, 520), (20, 136, 520), (1100, 24, 40)], ids=str)
+def test_every_kernel_beyond_32_bits(gpu_lib, size):
+    """As above, with tiles, with few columns, with few rows and a short reduction: rows of x 2^23 bytes or more apart."""
+    import torch
+    m, n, k = size
+    log(f"beyond 32 bits {size}")
+    x, w, wu = make("f16", 25, ((m, k), 1.0), ((n, k), k ** -0.5), ((n, k), k ** -0.5))
+    for ld in (1 << 22, (1 << 22) + 8):   # the second is more than the tiles take where it lies
+        far = torch.empty_strided((m, k), (ld, 1), dtype=torch.float16, device="cuda")
+        far.copy_(x)
+        R.check(gpu_lib.linear(far, w), R.linear(x, w, None, None, "none", "f16")[0], "y")
+        R.check(gpu_lib.gated_ffn(far, w, wu), R.gated(x, w, wu, None, None, "silu", "f16")[0], "h")
+        del far
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("size", [(512, 256, 64), (512, 256, 72), (512, 384, 192), (1000, 200, 1030), (2048, 256, 128)], ids=str)
+def test_tiles_in_halves(gpu_lib, size, dtype):
+    """One step, an odd number of steps and a ragged last one, shared by the halves of a workgroup; both products of the
+    gradients."""
+    m, n, k = size
+    log(f"halves {size} {dtype}")
+    x, w, b, r = layer(dtype, 26, m, n, k, residual=True)
+    dy, z = make(dtype, 27, ((m, n), 0.5), ((m, n), 1.0))
+    wu, u = make(dtype, 28, ((n, k), k ** -0.5), ((m, n), 1.0))
+    for v, want in zip(gpu_lib.linear(x, w, b, r, activation="relu", save=True), R.linear(x, w, b, r, "relu", dtype)):
+        R.check(v, want, "linear")
+    for v, want in zip(gpu_lib.gated_ffn(x, w, wu, None, b, save=True), R.gated(x, w, wu, None, b, "silu", dtype)):
+        R.check(v, want, "gated")
+    for v, want in zip(gpu_lib.linear_backward(dy, x, w, z, activation="silu"), R.linear_backward(dy, x, w, z, "silu", dtype)):
+        R.check(v, want, "linear_backward")
+    for v, want in zip(gpu_lib.gated_ffn_backward(dy, x, w, wu, z, u, bias=True), R.gated_backward(dy, x, w, wu, z, u, "silu", dtype)):
+        R.check(v, want, "gated_backward")
