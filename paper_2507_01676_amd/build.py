@@ -1,13 +1,16 @@
-"""Builds libembx.so (HIP kernels for gfx950 + the C ABI + the host planner) in-tree.
+"""Builds libembx.so (HIP kernels for gfx950 + the C ABI + the host planner) and, where torch is
+installed, the Python binding of the dense layers in-tree.
 
     python paper_2507_01676_amd/build.py
 """
 from __future__ import annotations
 
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -18,6 +21,7 @@ LIB = os.path.join(HERE, "libembx.so")
 # FAR lookups instead of 2^30, so that tests reach that code with ordinary batches
 FAR_LIB = os.path.join(HERE, "libembx_far.so")
 FAR = 100
+BINDING = os.path.join(HERE, "_dense.so")
 ARCH = "gfx950"
 
 HIP_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", "-ffp-contract=off",
@@ -58,6 +62,25 @@ GATHER_PARTS = 4
 GATHER_STEPS = (12, 13, 16)
 # dense.hip: one part per element type (f32, f16, bf16)
 DENSE_PARTS = 3
+
+
+def _torch():
+    """torch's folder, or None (found without importing it)."""
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec and spec.origin else None
+
+
+def binding_commands(torch):
+    """How dense_torch.cpp is compiled and linked: host C++ against torch and the HIP headers."""
+    o = os.path.join(BUILD, "dense_torch.o")
+    rocm = os.path.dirname(os.path.dirname(os.path.realpath(_hipcc())))
+    dirs = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+            sysconfig.get_paths()["include"], os.path.join(rocm, "include")]
+    compile_ = ["g++", *HOST_FLAGS, "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM", *[x for d in dirs for x in ("-isystem", d)], "-c",
+                os.path.join(CSRC, "dense_torch.cpp"), "-o", o]
+    link = ["g++", "-shared", "-o", BINDING + ".tmp", o, "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-ltorch",
+            "-lc10_hip", "-lc10"]
+    return compile_, link
 
 
 def _run_all(cmds, verbose):
@@ -110,7 +133,14 @@ def build(verbose: bool = False) -> str:
         o = os.path.join(BUILD, f"{name}.o")
         cmds.append(["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, f"{name}.cpp"), "-o", o])
         objs.append(o)
+    torch = _torch()
+    if torch:
+        compile_, link = binding_commands(torch)
+        cmds.append(compile_)
     _run_all(cmds, verbose)
+    if torch:
+        _run(link, verbose)
+        os.replace(BINDING + ".tmp", BINDING)
     for lib, parts in ((FAR_LIB, [far.get(o, o) for o in objs]), (LIB, objs)):
         tmp = lib + ".tmp"
         _run([hipcc, "-shared", f"--offload-arch={ARCH}", "-o", tmp, *parts], verbose)

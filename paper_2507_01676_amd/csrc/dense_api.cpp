@@ -146,7 +146,7 @@ double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int6
 // the copies of operands that are not whole
 double pack_us(double bytes) { return 3.0 + bytes / 2.1e6; }
 
-// How a forward product is computed.  What the alternatives measured, in us a call (a call takes 7 from the host):
+// How a forward product is computed.  What the alternatives measured, in us a call (a call took 7 from the host):
 //   a reduction of at most 64 and more than 64 rows: the kernel for it (bf16 65536 x 512 x 64 21.7, tiles of 128 27.0; x 32
 //     15.9 and 26.8; f32 x 64 50.5, tiles 72; 4096 x 4096 x 64 15.1 and 15.5)
 //   few rows or columns: the kernel for them, where it is estimated to be faster than tiles (bf16 16 x 512 x 1664 8.2, best

@@ -508,3 +508,31 @@ def test_tiles_in_halves(gpu_lib, size, dtype):
         R.check(v, want, "linear_backward")
     for v, want in zip(gpu_lib.gated_ffn_backward(dy, x, w, wu, z, u, bias=True), R.gated_backward(dy, x, w, wu, z, u, "silu", dtype)):
         R.check(v, want, "gated_backward")
+
+
+def test_calls_keep_nothing(gpu_lib):
+    """Neither memory nor references: results and workspace are the caller's or gone, after refusals too."""
+    import sys
+
+    import torch
+    log("nothing kept")
+    x, w, b, dy = make("f16", 29, ((70, 301), 1.0), ((90, 301), 0.1), ((90,), 0.3), ((70, 90), 1.0))
+    out = torch.empty_like(dy)
+
+    def calls():
+        assert gpu_lib.linear(x, w, b, out=out) is out
+        assert gpu_lib.linear(x, w, b, out=out, save=True)[0] is out
+        assert gpu_lib.gated_ffn(x, w, w, b, out=out) is out
+        gpu_lib.linear_backward(dy, x, w, dy, activation="silu")
+        gpu_lib.gated_ffn_backward(dy, x, w, w, dy, dy, bias=True, need_dw=False)
+        for bad in (lambda: gpu_lib.linear(x, w, b, activation=[]), lambda: gpu_lib.linear(x, w, dy)):
+            with pytest.raises(ValueError):
+                bad()
+
+    calls()
+    torch.cuda.synchronize()
+    counts, memory = [sys.getrefcount(t) for t in (x, w, b, dy, out)], torch.cuda.memory_allocated()
+    for _ in range(20):
+        calls()
+    assert [sys.getrefcount(t) for t in (x, w, b, dy, out)] == counts and torch.cuda.memory_allocated() == memory
+    assert gpu_lib.linear(x, w, save=1)[1].shape == (70, 90)
