@@ -1125,24 +1125,69 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
     if (i >= down) return;
   }
   const int i0 = i * FR * 16, j0 = j_ * 16;
-  const T* rows[FR];
-  const T* weights[kMats];
-#pragma unroll
-  for (int f = 0; f < FR; ++f) rows[f] = static_cast<const T*>(g.a[0]) + min(i0 + f * 16 + c, g.ni - 1) * g.lda;
-#pragma unroll
-  for (int m = 0; m < kMats; ++m) weights[m] = static_cast<const T*>(g.b[m]) + min(j0 + c, g.nj - 1) * g.ldb[m];
   f32x4 acc[FR][kMats] = {};
-#pragma unroll 4
-  for (int r0 = wave * 32; r0 < g.nr; r0 += 8 * 32) {
-    L x[FR], w[kMats];
-#pragma unroll
-    for (int m = 0; m < kMats; ++m) w[m].load(weights[m], r0 + 8 * q, g.nr);
-#pragma unroll
-    for (int f = 0; f < FR; ++f) x[f].load(rows[f], r0 + 8 * q, g.nr);
+  auto products = [&](const L* x, const L* w) {
 #pragma unroll
     for (int f = 0; f < FR; ++f)
 #pragma unroll
       for (int m = 0; m < kMats; ++m) acc[f][m] = multiply<TYPE, WHOLE>(w[m], x[f], acc[f][m]);
+  };
+  if constexpr (WHOLE) {
+    const T* rows[FR];
+    const T* weights[kMats];
+#pragma unroll
+    for (int f = 0; f < FR; ++f) rows[f] = static_cast<const T*>(g.a[0]) + min(i0 + f * 16 + c, g.ni - 1) * g.lda;
+#pragma unroll
+    for (int m = 0; m < kMats; ++m) weights[m] = static_cast<const T*>(g.b[m]) + min(j0 + c, g.nj - 1) * g.ldb[m];
+#pragma unroll 4
+    for (int r0 = wave * 32; r0 < g.nr; r0 += 8 * 32) {
+      L x[FR], w[kMats];
+#pragma unroll
+      for (int m = 0; m < kMats; ++m) w[m].load(weights[m], r0 + 8 * q, g.nr);
+#pragma unroll
+      for (int f = 0; f < FR; ++f) x[f].load(rows[f], r0 + 8 * q, g.nr);
+      products(x, w);
+    }
+  } else {
+    // A load reads consecutive elements, 32 of each of two rows, and LDS of the wavefront's own turns sixteen rows into a
+    // fragment; the next step's loads are under way meanwhile.  (One load for each lane's own row and place takes 64
+    // accesses of the cache: OLDNEW.)  A wavefront's LDS instructions run in order, so it waits for none of them.
+    constexpr int kRow = 32 + 16 / int(sizeof(T));
+    __shared__ __align__(16) T turned[8][2][16 * kRow];
+    const int column = lane & 31, row = lane >> 5;
+    T held[FR + kMats][8];
+    auto ask = [&](T* h, const void* from, int64_t ld, int first, int count, int at) {
+      const T* const p = static_cast<const T*>(from);
+      if (ld < (1 << 24) && first + 16 <= count) {
+        const uint32_t mine = static_cast<uint32_t>(row) * static_cast<uint32_t>(ld) + at;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = p[(first + e * 2) * ld + mine];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = p[min(first + e * 2 + row, count - 1) * ld + at];
+      }
+    };
+    auto fetch = [&](int r0) {
+      const int at = min(r0 + column, g.nr - 1);
+#pragma unroll
+      for (int m = 0; m < kMats; ++m) ask(held[FR + m], g.b[m], g.ldb[m], j0, g.nj, at);
+#pragma unroll
+      for (int f = 0; f < FR; ++f) ask(held[f], g.a[0], g.lda, i0 + f * 16, g.ni, at);
+    };
+    int r0 = wave * 32;
+    if (r0 < g.nr) fetch(r0);
+    for (; r0 < g.nr; r0 += 8 * 32) {
+      L v[FR + kMats];
+#pragma unroll
+      for (int f = 0; f < FR + kMats; ++f) {
+        T* const own = turned[wave][f & 1];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) own[(e * 2 + row) * kRow + column] = r0 + column < g.nr ? held[f][e] : T(0.0f);
+        v[f].read(own + c * kRow + 8 * q);
+      }
+      if (r0 + 8 * 32 < g.nr) fetch(r0 + 8 * 32);
+      products(v, v + FR);
+    }
   }
   __shared__ float sums[8][FR][kMats][16][16];   // [wavefront][..][..][row][column]
 #pragma unroll
@@ -1187,14 +1232,41 @@ __global__ __launch_bounds__(256) void dense_short(DenseGemm g) {
   // the epilogue's lanes: eight consecutive columns of a row
   constexpr int kLanes = KIND == kGated ? 4 : 8;
   const int e0 = lane % kLanes * 2, j = j0 + e0 * 4;
+  if constexpr (WHOLE) {
 #pragma unroll
-  for (int m = 0; m < kMats; ++m) {
+    for (int m = 0; m < kMats; ++m)
 #pragma unroll
-    for (int n = 0; n < FC; ++n) {
-      const int column = min(j0 + n * 16 + c, g.nj - 1);
+      for (int n = 0; n < FC; ++n) {
+        const int column = min(j0 + n * 16 + c, g.nj - 1);
 #pragma unroll
-      for (int k = 0; k < KS; ++k) w[m][n][k].load(static_cast<const T*>(g.b[m]) + column * g.ldb[m], k * 32 + 8 * q, g.nr);
+        for (int k = 0; k < KS; ++k) w[m][n][k].load(static_cast<const T*>(g.b[m]) + column * g.ldb[m], k * 32 + 8 * q, g.nr);
+      }
+  } else {
+    // Sixteen rows at a time through LDS of the wavefront's own, so that a load reads consecutive elements: one for each
+    // lane's own row and place is 64 accesses of the cache (f16 65536 x 512 x 13 in all 9.5 M instead of 2 M, 21.9 us a
+    // call, so 2.6 M and 21.1; 16384 x 512 x 61 15.5 and 12.0).
+    constexpr int kSide = 2 / KS, kLoads = 16 / kSide;   // rows of a load
+    T* const own = &tile[0][0] + wave * 32 * kRow;
+    const int column = lane % (KS * 32), row = lane / (KS * 32);
+#pragma unroll
+    for (int m = 0; m < kMats; ++m) {
+      const T* const from = static_cast<const T*>(g.b[m]) + min(column, g.nr - 1);
+      T held[FC][kLoads];
+#pragma unroll
+      for (int n = 0; n < FC; ++n)
+#pragma unroll
+        for (int e = 0; e < kLoads; ++e) held[n][e] = from[min(j0 + n * 16 + e * kSide + row, g.nj - 1) * g.ldb[m]];
+#pragma unroll
+      for (int n = 0; n < FC; ++n) {
+#pragma unroll
+        for (int e = 0; e < kLoads; ++e) own[(e * kSide + row) * kRow + column] = column < g.nr ? held[n][e] : T(0.0f);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int k = 0; k < KS; ++k) w[m][n][k].read(own + c * kRow + k * 32 + 8 * q);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      }
     }
+    __syncthreads();
   }
   // a chunk of x: pieces of kPer elements, the same columns of different rows for a thread
   constexpr int kPer = WHOLE ? 16 / sizeof(T) : 1;
