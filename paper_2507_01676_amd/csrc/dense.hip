@@ -1101,7 +1101,7 @@ __device__ inline f32x4 multiply(const Loader<TYPE>& w, const Loader<TYPE>& x, f
 
 // Few rows, few columns, or few of both: the longer operand is read once, and latency counts.  Eight wavefronts share FR *
 // 16 rows by 16 columns and take every eighth step of 32 each; their sums are added in order in LDS.  bf16, 1 x 512 x 1664:
-// 4.5 us of GPU time, a launch and two rounds of loads; gated 19 x 2816 x 1024: 6.4 us for 11.7 MB; f16 65536 x 1 x 1024:
+// 4.3 us of GPU time, a launch and two rounds of loads; gated 19 x 2816 x 1024: 5.8 us for 11.7 MB; f16 65536 x 1 x 1024:
 // 134 MB in 21 us, 6.3 TB/s.
 template <int TYPE, int KIND, int FR, bool WHOLE>
 __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
@@ -1202,8 +1202,8 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 // registers, walk rows of x by chunks of 64, which pass through LDS: loaded once for all columns of the workgroup, as
 // 16-byte chunks (WHOLE) or consecutive elements, while the chunk before is multiplied.  Where there are fewer columns
 // than the four hold, several take the same columns and other rows of the chunk.  Results leave through LDS, in whole
-// 128-byte lines.  bf16, 65536 x 512 x 64: 75 MB in 21.7 us a call, 3.5 TB/s (without LDS on the way in 28.5, results
-// stored from the fragments' lanes 26.3); the stores and the epilogue's instructions bound it.
+// 128-byte lines.  bf16, 65536 x 512 x 64: 75 MB in 20.9 us a call, 3.6 TB/s (at first, without LDS on the way in,
+// 28.5, and with results stored from the fragments' lanes 26.3); the stores and the epilogue's instructions bound it.
 template <int TYPE, int KIND, int FC, int KS, bool WHOLE>
 __global__ __launch_bounds__(256) void dense_short(DenseGemm g) {
   using T = typename Elem<TYPE>::T;
