@@ -960,7 +960,8 @@ __global__ __launch_bounds__(64 * WI * WJ * HALVES, WI * WJ * HALVES * PER_CU / 
 // launch and the last one instead of a launch for each, a call took 250 us instead of 265 (f16 16384 x 1024 x 3328), 272
 // instead of 315 (gated, bf16 8192 x 4096 x 1024) and 43 instead of 55 (gated, f16 777 x 1365 x 1001).
 template <int TYPE, int BM, int BN, int WI, int WJ, int PER_CU, int HALVES>
-__global__ __launch_bounds__(64 * WI * WJ * HALVES, WI * WJ * HALVES * PER_CU / 4) void dense_grads(DenseGemm w, DenseGemm x, uint32_t w_groups) {
+__global__ __launch_bounds__(64 * WI * WJ * HALVES, WI * WJ * HALVES * PER_CU / 4) void dense_grads(DenseGemm w, DenseGemm x,
+                                                                                                  uint32_t w_groups) {
   __shared__ __align__(1024) char lds[HALVES * kTileLds<TYPE, BM, BN, WJ, WI * WJ>];
   uint32_t id = blockIdx.x;
   if (id < w_groups) {
@@ -1142,7 +1143,8 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
   } else {
     // A load reads consecutive elements, 32 of each of two rows, and LDS of the wavefront's own turns sixteen rows into a
     // fragment; the next step's loads are under way meanwhile.  (One load for each lane's own row and place takes 64
-    // accesses of the cache: f16 32 x 512 x 1001 12.2 us a call, so 5.7.)  A wavefront's LDS instructions run in order, so it waits for none of them.
+    // accesses of the cache: f16 32 x 512 x 1001 12.2 us a call, so 5.7.)  A wavefront's LDS instructions run in order, so
+    // it waits for none of them.
     constexpr int kRow = 32 + 16 / int(sizeof(T));
     __shared__ __align__(16) T turned[8][2][16 * kRow];
     const int column = lane & 31, row = lane >> 5;
@@ -1475,8 +1477,8 @@ int grads_launch(const DenseGemm& w, const DenseGemm& x, hipStream_t stream) {
   auto tiles = [](const DenseGemm& g) { return int64_t((g.ni + BM - 1) / BM) * ((g.nj + BN - 1) / BN) * g.splits; };
   const int64_t w_groups = w.parts ? (tiles(w) * w.parts + kXcds - 1) / kXcds * kXcds : 0, x_groups = x.parts ? tiles(x) : 0;
   if (w_groups + x_groups == 0) return 0;
-  dense_grads<TYPE, BM, BN, WI, WJ, PER_CU, HALVES><<<static_cast<uint32_t>(w_groups + x_groups), 64 * WI * WJ * HALVES, 0, stream>>>(
-      w, x, static_cast<uint32_t>(w_groups));
+  const uint32_t grid = static_cast<uint32_t>(w_groups + x_groups);
+  dense_grads<TYPE, BM, BN, WI, WJ, PER_CU, HALVES><<<grid, 64 * WI * WJ * HALVES, 0, stream>>>(w, x, static_cast<uint32_t>(w_groups));
   return hipGetLastError();
 }
 
