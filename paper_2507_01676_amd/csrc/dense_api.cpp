@@ -131,16 +131,20 @@ double tile_us(int32_t dtype, int variant, double tiles, double steps, int s, do
 }
 
 // The same by workgroups of 16 columns and 16 times `blocks` rows, a step being 32 of the reduction of each of eight
-// wavefronts.  Measured on 1 to 65536 rows by 1 to 8192 columns and 256 to 8192 inputs.  Operands that are not whole are
-// read element by element.
+// wavefronts.  Measured on 1 to 65536 rows by 1 to 8192 columns and 256 to 8192 inputs, whole operands and others.
 double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int64_t nj, int64_t nr) {
-  const double groups = double((nj + 15) / 16) * double((ni + 16 * blocks - 1) / (16 * blocks)), steps = double((nr + 255) / 256);
+  const double groups = double((nj + 15) / 16) * double((ni + 16 * blocks - 1) / (16 * blocks)), a_cu = groups / kCus;
+  // a last step that some of the wavefronts have counts whole where nothing else runs meanwhile, and so does a second group
+  // that some of the CUs have, by half
+  const double steps = a_cu > 1.0 ? std::max(1.0, nr / 256.0) : std::ceil(nr / 256.0);
+  const double load = a_cu <= 1.0 ? 1.0 : a_cu <= 2.0 ? (a_cu + 2.0) / 2.0 : a_cu;
   const int at = blocks == 1 ? 0 : blocks == 2 ? 1 : 2;
-  static const double k16[] = {0.5, 0.7, 1.05}, k32[] = {0.93, 1.35, 2.45}, kOdd[] = {1.25, 2.4, 4.8},
-                      kOddFull[] = {1.9, 3.05, 5.7}, kTwo16[] = {1.5, 1.33, 1.2}, kTwo32[] = {2.0, 1.6, 1.4};
-  const double step = (!whole ? (groups > kCus ? kOddFull : kOdd) : dtype != EMB_DTYPE_F32 ? k16 : k32)[at];
-  const double two = mats == 1 ? 1.0 : (dtype == EMB_DTYPE_F32 ? kTwo32 : kTwo16)[at];   // a second weight beside each
-  return 3.0 + steps * step * two * std::max(1.0, groups / kCus);
+  static const double k16[] = {0.5, 0.7, 1.05}, kOdd16[] = {0.58, 0.8, 1.3}, kOddFull16[] = {0.58, 0.8, 2.0},
+                      k32[] = {0.93, 1.35, 2.45}, kTwo16[] = {1.5, 1.33, 1.2}, kTwo[] = {2.0, 1.6, 1.4};
+  const bool f32 = dtype == EMB_DTYPE_F32;
+  const double step = (f32 ? k32 : whole ? k16 : a_cu > 1.0 ? kOddFull16 : kOdd16)[at];
+  const double two = mats == 1 ? 1.0 : (f32 || !whole ? kTwo : kTwo16)[at];   // a second weight beside each
+  return 3.0 + steps * step * two * load;
 }
 
 // the copies of operands that are not whole
