@@ -19,7 +19,7 @@
  * three bf16 parts of each value, which hold all 24 bits of every normal number: a product
  * is off by less than 2^-22 of itself.  Where sums leave the range of that (beyond 2^80,
  * about), or operands are infinite or NaN, the products are formed in fp32 instead: the
- * same results, six times slower for the tile of up to 256 rows and columns that has them.
+ * same results, five times slower for the tile of up to 256 rows and columns that has them.
  * Results do not depend on timing: equal calls give equal bits.
  *
  * Calls take plain device pointers of the current HIP device, aligned to their element

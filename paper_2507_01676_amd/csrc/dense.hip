@@ -241,7 +241,7 @@ struct Tile {
 // and the finished sum is multiplied by 2^-48.  Six bf16 products for each f32 one are 2.7 times less
 // work than f32 products, at f32's accuracy.  Values or sums too large for this (2^104 or 2^80, about), infinities and NaN
 // turn the sums that they reach into infinities or NaN, and a tile with sums that are not finite is computed again with f32
-// products (tile_by_f32).  The first factor costs 1% (4096^3 610 us, without it 606).
+// products (tile_by_f32).  The first factor costs 1% (4096^3 610 us when it was added, without it 606).
 struct Parts { s16x8 p[3]; };   // high to low
 
 constexpr float kScale = 0x1p24f;
@@ -271,7 +271,8 @@ __device__ inline Parts split3(const float* v) {
 // The parts of a tile of f32 (ROWS results by 32 of the reduction) in LDS: a tile of bf16 for each.  Taken apart once for
 // the workgroup, not at each wavefront's fragments: the matrix cores and the other vector instructions of a SIMD overlap
 // by half at most (8 matrix instructions take 160 cycles, 32 others 173, all of them from two wavefronts 249), so every
-// instruction of the latter counts.  4096 x 4096 x 4096: 610 us, with the parts taken at the fragments 641.
+// instruction of the latter counts.  4096 x 4096 x 4096: 595 us; with the parts taken at the fragments
+// 46 more.
 template <int ROWS, bool RM, int WAVES>
 struct PartTile {
   static constexpr int kBytes = ROWS * 64;                     // of a part
@@ -611,7 +612,7 @@ constexpr int kTileLds = [] {   // (of each half)
 //     1255 us, 1.37.  Bound by the matrix cores at the clock that they leave (about 1.75 GHz), less some 7 us a tile for its
 //     first loads and its results, which nothing hides (one workgroup a CU that goes on to the next tile was slower: its
 //     loads wait for the stores before them)
-//   f32, 256 x 128 or 128 x 128, eight wavefronts, one workgroup a CU: see PartTile; 4096^3 610 us, 225 TFLOP/s (f32
+//   f32, 256 x 128 or 128 x 128, eight wavefronts, one workgroup a CU: see PartTile; 4096^3 595 us, 231 TFLOP/s (f32
 //     products on the matrix cores reach 153 in a library)
 template <int TYPE, int KIND, int BM, int BN, int WI, int WJ, int HALVES>
 __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint32_t tile, int split, int wpart) {

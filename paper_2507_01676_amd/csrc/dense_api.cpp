@@ -155,10 +155,10 @@ double pack_us(double bytes) { return 3.0 + bytes / 2.1e6; }
 //     and 26.7; f32 x 64 48.8 and 72; 4096 x 4096 x 64 14.2 and 15.6)
 //   few rows or columns: the kernel for them, where it is estimated to be faster than tiles (bf16 16 x 512 x 1664 5.3, best
 //     tile 9.0; 16 x 4096 x 4096 9.9 and 13.0; f16 2048 x 64 x 1024 5.3 and 9.8, 65536 x 1 x 1024 21.6 and 25.3; but 64 x 8192
-//     x 8192 73 and 29.5, 65536 x 32 x 1024 39.7 and 24.6; f32 64 x 4096 x 4096 38.8 and 32.5)
+//     x 8192 73 and 29.5, 65536 x 32 x 1024 39.7 and 24.6; f32 64 x 4096 x 4096 38.6 and 27.6)
 //   tiles of 256 where they fill the GPU (bf16 4096^3 100, tiles of 128 135), of 128 else (2048^3 44 and 27.6), in halves
 //     where a CU has one (2048^3 23.1, 4096 x 1024 x 1024 14.1, whole 16.8; 2 x 704 columns, 352 tiles, 13.2 and 9.3), their
-//     reductions split where there are few (f32 4096 x 512 x 1664 whole 68, in two 50.3, in four 62)
+//     reductions split where there are few (f32 4096 x 512 x 1664 whole 61, in two 45, in four 54)
 // `whole`, `bytes`: whether both operands are, and the size of those that are not.
 Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, bool whole, double bytes) {
   if (k <= kShortSum && m > kChunkRows) return {kShort, 1, 0};
