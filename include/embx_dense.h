@@ -16,11 +16,12 @@
  * are held in fp32 whatever the type; each result is rounded once, to the call's type,
  * except that dz, dg and du are rounded to it before the products that read them, as the
  * matrix cores take them (in fp16 one beyond 65504 is an infinity there; biases' gradients
- * are summed from the values before rounding).  Large products of fp32 operands go through the matrix cores as
- * three bf16 parts of each value, which hold all 24 bits of every normal number: a product
- * is off by less than 2^-22 of itself.  Where sums leave the range of that (beyond 2^80,
- * about), or operands are infinite or NaN, the products are formed in fp32 instead: the
- * same results, five times slower for the tile of up to 256 rows and columns that has them.
+ * are summed from the values before rounding).  Large products of fp32 operands go through
+ * the matrix cores as three bf16 parts of each value, which hold all 24 bits of every normal
+ * number: a product is off by less than 2^-22 of itself.  Where sums leave the range of that
+ * (beyond 2^80, about), or operands are infinite or NaN, the products are formed in fp32
+ * instead: the same results, five times slower for the tile of up to 256 rows and columns
+ * that has them.
  * Results do not depend on timing: equal calls give equal bits.
  *
  * Calls take plain device pointers of the current HIP device, aligned to their element
