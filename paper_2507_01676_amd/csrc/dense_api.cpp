@@ -76,7 +76,7 @@ bool whole16(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
 // times 16 rows a workgroup has.
 struct Choice { int32_t variant, splits, row_blocks; };
 
-constexpr int64_t kChunkRows = 64, kShortSum = 64;
+constexpr int64_t kShortSum = 64;   // the longest reduction that kShort takes
 
 constexpr int kCus = 256;
 
@@ -136,7 +136,7 @@ double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int6
   const double groups = double((nj + 15) / 16) * double((ni + 16 * blocks - 1) / (16 * blocks)), a_cu = groups / kCus;
   // a last step that some of the wavefronts have counts whole where nothing else runs meanwhile, and so does a second group
   // that some of the CUs have, by half
-  const double steps = a_cu > 1.0 ? std::max(1.0, nr / 256.0) : std::ceil(nr / 256.0);
+  const double steps = a_cu > 1.0 ? std::max(whole ? 0.6 : 1.0, nr / 256.0) : std::ceil(nr / 256.0);
   const double load = a_cu <= 1.0 ? 1.0 : a_cu <= 2.0 ? (a_cu + 2.0) / 2.0 : a_cu;
   const int at = blocks == 1 ? 0 : blocks == 2 ? 1 : 2;
   static const double k16[] = {0.5, 0.7, 1.05}, kOdd16[] = {0.58, 0.8, 1.3}, kOddFull16[] = {0.58, 0.8, 2.0},
@@ -147,12 +147,26 @@ double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int6
   return 3.0 + steps * step * two * load;
 }
 
+// The same of the kernel for short reductions: its workgroups (the launch's own arithmetic), each with `rows` chunks of 64
+// rows one after another.  A chunk takes 6.6 us in f32 (4 of at most 32 inputs) and 3 (2.2) in 16 bits where a CU has one
+// workgroup, and two to four share a CU at 0.85 of each one's time.
+double short_us(int32_t dtype, int mats, int64_t ni, int64_t nj, int64_t nr) {
+  const int64_t wide = 64 / mats, waves = nj <= wide ? 1 : nj <= 2 * wide ? 2 : 4, across = (nj + waves * wide - 1) / (waves * wide);
+  const int64_t most = nr <= 32 && dtype != EMB_DTYPE_F32 ? 1024 : 512, chunks = std::max<int64_t>(1, (ni + 63) / 64);
+  const int64_t down = std::min(chunks, std::max<int64_t>(1, most / across)), rows = (chunks + down - 1) / down;
+  const double a_cu = std::ceil(double((chunks + rows - 1) / rows * across) / kCus);
+  const double chunk = dtype == EMB_DTYPE_F32 ? (nr <= 32 ? 4.0 : 6.6) : nr <= 32 ? 2.2 : 3.0;
+  const double later = std::max<double>(0.0, rows - 2.0) * (dtype == EMB_DTYPE_F32 ? 0.9 : 0.6);   // the loads are ahead by then
+  return 3.3 + (std::min<double>(2.0, rows) + later) * chunk * waves / 4.0 * (a_cu > 1.0 ? 0.85 * a_cu : 1.0);
+}
+
 // the copies of operands that are not whole
 double pack_us(double bytes) { return 3.0 + bytes / 2.1e6; }
 
 // How a forward product is computed.  What the alternatives measured, in us a call (a call takes 4.4 from the host):
-//   a reduction of at most 64 and more than 64 rows: the kernel for it (bf16 65536 x 512 x 64 20.9, best tile 26.8; x 32 15.8
-//     and 26.7; f32 x 64 48.8 and 72; 4096 x 4096 x 64 14.2 and 15.6)
+//   a reduction of at most 64: the kernel for it, unless another is estimated to be faster (f16 65536 x 512 x 64 20.7, best
+//     tile 26.8; x 32 15.9 and 26.7; f32 x 64 49.0 and 53.9; but f32 12247 x 576 x 64 27.4 and 15.2, f16 12.8 and 9.0; f32 408
+//     x 256 x 64 9.8, the kernel of few rows 4.7)
 //   few rows or columns: the kernel for them, where it is estimated to be faster than tiles (bf16 16 x 512 x 1664 5.3, best
 //     tile 9.0; 16 x 4096 x 4096 9.9 and 13.0; f16 2048 x 64 x 1024 5.3 and 9.8, 65536 x 1 x 1024 21.6 and 25.3; but 64 x 8192
 //     x 8192 73 and 29.5, 65536 x 32 x 1024 39.7 and 24.6; f32 64 x 4096 x 4096 38.6 and 27.6)
@@ -161,7 +175,6 @@ double pack_us(double bytes) { return 3.0 + bytes / 2.1e6; }
 //     reductions split where there are few (f32 4096 x 512 x 1664 whole 61, in two 45, in four 54)
 // `whole`, `bytes`: whether both operands are, and the size of those that are not.
 Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, bool whole, double bytes) {
-  if (k <= kShortSum && m > kChunkRows) return {kShort, 1, 0};
   const int mats = kind == kGated ? 2 : 1;
   const double steps = static_cast<double>(steps_of(dtype, k)), result_bytes = 4.0 * m * n * mats;
   Choice best = {kTile128, 1, 0}, few = {kRows, 1, 1};
@@ -176,13 +189,15 @@ Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, 
   }
   // weights that come from memory: f32 tiles ask for them two steps ahead, which reaches 2.2 TB/s
   if (dtype == EMB_DTYPE_F32) least = std::max(least, 4.0 * n * k * mats / 2.2e6);
-  least += kCallUs;   // (rows_us counts from the launch)
+  least += kCallUs;   // (the other estimates count from the launch)
+  if (k <= kShortSum) least += double(esize(dtype)) * m * n / 5.1e6;   // writing the results is not hidden then
   if (!whole) least += pack_us(bytes);
   for (int blocks : {1, 2, 4}) {
     if (blocks > 1 && m <= 8 * blocks) break;
     const double us = rows_us(dtype, mats, whole, blocks, m, n, k);
     if (few_us == 0.0 || us < few_us) few_us = us, few.row_blocks = blocks;
   }
+  if (k <= kShortSum && short_us(dtype, mats, m, n, k) < std::min(1.25 * least, few_us)) return {kShort, 1, 0};
   return few_us <= least ? few : best;
 }
 
