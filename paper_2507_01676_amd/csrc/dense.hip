@@ -928,7 +928,8 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
 #pragma unroll
       for (int fi = 0; fi < 2; ++fi)
 #pragma unroll
-        for (int fj = 0; fj < kFJ; ++fj) *reinterpret_cast<f32x4*>(pass + half * kGiven + (fi * kFJ + fj) * 1024) = acc[from + fi][fj];
+        for (int fj = 0; fj < kFJ; ++fj)
+          *reinterpret_cast<f32x4*>(pass + half * kGiven + (fi * kFJ + fj) * 1024) = acc[from + fi][fj];
     };
     if (half == 0) give(2);
     else give(0);
@@ -1480,7 +1481,8 @@ int grads_launch(const DenseGemm& w, const DenseGemm& x, hipStream_t stream) {
   const int64_t w_groups = w.parts ? (tiles(w) * w.parts + kXcds - 1) / kXcds * kXcds : 0, x_groups = x.parts ? tiles(x) : 0;
   if (w_groups + x_groups == 0) return 0;
   const uint32_t grid = static_cast<uint32_t>(w_groups + x_groups);
-  dense_grads<TYPE, BM, BN, WI, WJ, PER_CU, HALVES><<<grid, 64 * WI * WJ * HALVES, 0, stream>>>(w, x, static_cast<uint32_t>(w_groups));
+  dense_grads<TYPE, BM, BN, WI, WJ, PER_CU, HALVES><<<grid, 64 * WI * WJ * HALVES, 0, stream>>>(w, x,
+                                                                                               static_cast<uint32_t>(w_groups));
   return hipGetLastError();
 }
 

@@ -140,7 +140,7 @@ double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int6
   const double load = a_cu <= 1.0 ? 1.0 : a_cu <= 2.0 ? (a_cu + 2.0) / 2.0 : a_cu;
   const int at = blocks == 1 ? 0 : blocks == 2 ? 1 : 2;
   static const double k16[] = {0.5, 0.7, 1.05}, kOdd16[] = {0.58, 0.8, 1.3}, kOddFull16[] = {0.58, 0.8, 2.0},
-                      k32[] = {0.93, 1.35, 2.45}, kTwo16[] = {1.5, 1.33, 1.2}, kTwo[] = {2.0, 1.6, 1.4};
+                      k32[] = {0.93, 1.35, 2.45}, kTwo16[] = {1.5, 1.33, 1.2}, kTwo[] = {1.6, 1.6, 1.4};
   const bool f32 = dtype == EMB_DTYPE_F32;
   const double step = (f32 ? k32 : whole ? k16 : a_cu > 1.0 ? kOddFull16 : kOdd16)[at];
   const double two = mats == 1 ? 1.0 : (f32 || !whole ? kTwo : kTwo16)[at];   // a second weight beside each
@@ -151,7 +151,8 @@ double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int6
 // rows one after another.  A chunk takes 6.6 us in f32 (4 of at most 32 inputs) and 3 (2.2) in 16 bits where a CU has one
 // workgroup, and two to four share a CU at 0.85 of each one's time.
 double short_us(int32_t dtype, int mats, int64_t ni, int64_t nj, int64_t nr) {
-  const int64_t wide = 64 / mats, waves = nj <= wide ? 1 : nj <= 2 * wide ? 2 : 4, across = (nj + waves * wide - 1) / (waves * wide);
+  const int64_t wide = 64 / mats, waves = nj <= wide ? 1 : nj <= 2 * wide ? 2 : 4;
+  const int64_t across = (nj + waves * wide - 1) / (waves * wide);
   const int64_t most = nr <= 32 && dtype != EMB_DTYPE_F32 ? 1024 : 512, chunks = std::max<int64_t>(1, (ni + 63) / 64);
   const int64_t down = std::min(chunks, std::max<int64_t>(1, most / across)), rows = (chunks + down - 1) / down;
   const double a_cu = std::ceil(double((chunks + rows - 1) / rows * across) / kCus);
