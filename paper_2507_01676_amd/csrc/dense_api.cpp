@@ -144,7 +144,8 @@ double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int6
   const bool f32 = dtype == EMB_DTYPE_F32;
   const double step = (f32 ? k32 : whole ? k16 : a_cu > 1.0 ? kOddFull16 : kOdd16)[at];
   const double two = mats == 1 ? 1.0 : (f32 || !whole ? kTwo : kTwo16)[at];   // a second weight beside each
-  return 3.0 + steps * step * two * load;
+  const double idle = a_cu <= 0.5 ? 0.75 : 1.0;   // fewer groups than half of the CUs load faster
+  return 3.0 + steps * step * two * load * idle;
 }
 
 // The same of the kernel for short reductions: its workgroups (the launch's own arithmetic), each with `rows` chunks of 64
