@@ -119,8 +119,9 @@ typedef struct {
  * its sizes, types and wanted gradients and from the alignment of its pointers and row
  * strides modulo 16 bytes; nothing is read through a pointer, and no device is touched.  The
  * workspace holds partial sums of a product whose long axis is split over the GPU, dz (dg,
- * du), and copies of matrices whose rows do not start at multiples of 16 bytes or do not hold
- * whole multiples of 16 bytes.  256-byte aligned; its contents mean nothing before or after. */
+ * du), and copies of matrices whose rows do not start at multiples of 16 bytes, do not hold
+ * whole multiples of 16 bytes or start more than 2^23 bytes apart.  256-byte aligned; its
+ * contents mean nothing before or after. */
 emb_status_t emb_linear_workspace(const emb_linear_t* a, size_t* bytes);
 emb_status_t emb_linear_backward_workspace(const emb_linear_grad_t* a, size_t* bytes);
 emb_status_t emb_gated_workspace(const emb_gated_t* a, size_t* bytes);

@@ -128,6 +128,11 @@ constexpr int kOutOfRange = static_cast<int>(0x80000000u);   // past every descr
 
 #define LDS_PTR(T) __attribute__((address_space(3))) T*
 
+// elements from an operand's start to a column of its first row: see kPanel
+__device__ inline int64_t column_at(int column, int64_t panel) {
+  return int64_t(column >> kPanelLog) * panel + (column & (int(kPanel) - 1));
+}
+
 __device__ inline uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((LDS_PTR(const void))p));
 }
@@ -517,10 +522,10 @@ __device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char
     };
     if (j < g.nj) {
       float s0[8], s1[8];
-      if (g.splits > 1) {
+      if (g.slots > 1) {
         // partial sums: rows padded to whole eights
         const int64_t ld = (g.nj + 7) / 8 * 8, slice = int64_t(g.ni) * ld;
-        float* p = g.partial + (int64_t(kGate ? 0 : part) * g.splits + split) * slice + first * ld + j;
+        float* p = g.partial + (int64_t(kGate ? 0 : part) * g.slots + g.first + split) * slice + first * ld + j;
 #pragma unroll 1
         for (int row0 = 0; row0 < kPass * 16; row0 += kRows, p += kRows * ld) {
           if (first + row0 >= g.ni) break;
@@ -528,7 +533,7 @@ __device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char
           reinterpret_cast<f32x4*>(p)[0] = f32x4{s0[0], s0[1], s0[2], s0[3]};
           reinterpret_cast<f32x4*>(p)[1] = f32x4{s0[4], s0[5], s0[6], s0[7]};
           if constexpr (kGate) {
-            float* u = p + g.splits * slice;
+            float* u = p + g.slots * slice;
             reinterpret_cast<f32x4*>(u)[0] = f32x4{s1[0], s1[1], s1[2], s1[3]};
             reinterpret_cast<f32x4*>(u)[1] = f32x4{s1[4], s1[5], s1[6], s1[7]};
           }
@@ -561,18 +566,20 @@ __device__ __forceinline__ void tile_by_f32(const DenseGemm& g, char* lds, int i
   for (int step = begin; step < end; ++step) {
     const int part = KIND == kInputGrad && step >= per_part ? 1 : 0;
     const int r0 = (step - part * per_part) * BK;
-    const float* a = static_cast<const float*>(g.a[KIND == kWeightGrad ? wpart : part]);
+    const float* a = static_cast<const float*>(g.a[KIND == kWeightGrad ? wpart : part]) +
+                     (KIND == kWeightGrad ? r0 * g.lda + column_at(i0, g.panel_a) : i0 * g.lda + r0);
     __syncthreads();
     for (int e = tid; e < BM * BK; e += kThreads) {
       const int i = KIND == kWeightGrad ? e % BM : e / BK, r = KIND == kWeightGrad ? e / BM : e % BK;
-      const int64_t at = KIND == kWeightGrad ? (r0 + r) * g.lda + i0 + i : (i0 + i) * g.lda + r0 + r;
+      const int64_t at = KIND == kWeightGrad ? r * g.lda + i : i * g.lda + r;
       sa[i * kRow + r] = r0 + r < g.nr && i0 + i < g.ni ? a[at] : 0.0f;
     }
     for (int e = tid; e < BN * BK; e += kThreads) {
       const int row = kRm ? e % BN : e / BK, r = kRm ? e / BN : e % BK;
       const int mat = kGate ? row / kCols : part, j = kGate ? row % kCols : row;
-      const float* b = static_cast<const float*>(g.b[mat]);
-      const int64_t at = kRm ? (r0 + r) * g.ldb[mat] + j0 + j : (j0 + j) * g.ldb[mat] + r0 + r;
+      const float* b = static_cast<const float*>(g.b[mat]) +
+                       (kRm ? r0 * g.ldb[mat] + column_at(j0, g.panel_b[mat]) : j0 * g.ldb[mat] + r0);
+      const int64_t at = kRm ? r * g.ldb[mat] + j : j * g.ldb[mat] + r;
       sb[row * kRow + r] = r0 + r < g.nr && j0 + j < g.nj ? b[at] : 0.0f;
     }
     __syncthreads();
@@ -673,7 +680,7 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
     const int r0 = (step - part * per_part) * BK;
     next.valid_a = step < end ? g.nr - r0 : 0;
     const char* a = static_cast<const char*>(g.a[KIND == kWeightGrad ? wpart : part]);
-    next.a = descriptor(a + (kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0) * 2);
+    next.a = descriptor(a + (kRmA ? int64_t(r0) * g.lda + column_at(i0, g.panel_a) : int64_t(i0) * g.lda + r0) * 2);
     next.at_a = lds0 + slot * TileA::kBytes;
   };
   auto set_b = [&](int step, int slot) {
@@ -681,7 +688,7 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
     const int r0 = (step - part * per_part) * BK;
     next.valid_b = step < end ? g.nr - r0 : 0;
     const char* b = static_cast<const char*>(g.b[part]);
-    next.b0 = descriptor(b + (kRmB ? int64_t(r0) * g.ldb[part] + j0 : int64_t(j0) * g.ldb[part] + r0) * 2);
+    next.b0 = descriptor(b + (kRmB ? int64_t(r0) * g.ldb[part] + column_at(j0, g.panel_b[part]) : int64_t(j0) * g.ldb[part] + r0) * 2);
     if constexpr (kGate) next.b1 = descriptor(static_cast<const char*>(g.b[1]) + (int64_t(j0) * g.ldb[1] + r0) * 2);
     if constexpr (KIND == kInputGrad) {
       if (part != tb_part) {
@@ -737,7 +744,7 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
       const int part = KIND == kInputGrad && step >= per_part && g.parts > 1 ? 1 : 0;
       const int r0 = (step - part * per_part) * BK, valid = step < end ? g.nr - r0 : 0;
       const float* a = static_cast<const float*>(g.a[KIND == kWeightGrad ? wpart : part]);
-      va.load(descriptor(a + (kRmA ? int64_t(r0) * g.lda + i0 : int64_t(i0) * g.lda + r0)), tid, valid);
+      va.load(descriptor(a + (kRmA ? int64_t(r0) * g.lda + column_at(i0, g.panel_a) : int64_t(i0) * g.lda + r0)), tid, valid);
       if constexpr (KIND == kInputGrad) {
         if (part != tb_part) {
           vb[0].init(tid, g.ldb[part], g.nj - j0);
@@ -748,7 +755,8 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
       for (int m = 0; m < kMats; ++m) {
         const int mat = kGate ? m : part;
         const float* b = static_cast<const float*>(g.b[mat]);
-        vb[m].load(descriptor(b + (kRmB ? int64_t(r0) * g.ldb[mat] + j0 : int64_t(j0) * g.ldb[mat] + r0)), tid, valid);
+        vb[m].load(descriptor(b + (kRmB ? int64_t(r0) * g.ldb[mat] + column_at(j0, g.panel_b[mat]) : int64_t(j0) * g.ldb[mat] + r0)),
+                   tid, valid);
       }
     };
     auto take_apart = [&](int slot) {
@@ -988,7 +996,7 @@ __device__ inline void join8(const DenseGemm& g, int64_t at, int part) {
   float s[2][8];
 #pragma unroll
   for (int mat = 0; mat < (KIND == kGated ? 2 : 1); ++mat) {
-    const float* p = g.partial + int64_t(KIND == kGated ? mat : part) * g.splits * slice + at * 8;
+    const float* p = g.partial + int64_t(KIND == kGated ? mat : part) * g.slots * slice + at * 8;
 #pragma unroll
     for (int e = 0; e < 8; ++e) s[mat][e] = 0.0f;
     int split = 0;
@@ -1006,10 +1014,10 @@ __device__ inline void join8(const DenseGemm& g, int64_t at, int part) {
         for (int e = 0; e < 4; ++e) s[mat][e] += lo[n][e], s[mat][4 + e] += hi[n][e];
       split += N;
     };
-    while (g.splits - split >= 8) add(std::integral_constant<int, 8>{});
-    if (g.splits - split >= 4) add(std::integral_constant<int, 4>{});
-    if (g.splits - split >= 2) add(std::integral_constant<int, 2>{});
-    if (g.splits - split >= 1) add(std::integral_constant<int, 1>{});
+    while (g.slots - split >= 8) add(std::integral_constant<int, 8>{});
+    if (g.slots - split >= 4) add(std::integral_constant<int, 4>{});
+    if (g.slots - split >= 2) add(std::integral_constant<int, 2>{});
+    if (g.slots - split >= 1) add(std::integral_constant<int, 1>{});
   }
   Finish<TYPE, KIND>(g, part, i, j, 0).put(s[0], s[1]);
 }
@@ -1340,7 +1348,8 @@ __global__ __launch_bounds__(256) void dense_short(DenseGemm g) {
 // 4.4 TB/s, with four rows of a thread under way (one: 81 us).
 template <class E>
 __device__ inline void pack_rows(const DensePack& p, uint32_t mat, uint32_t group) {
-  const uint32_t cols = p.cols[mat], padded = static_cast<uint32_t>(p.ldd[mat]);
+  constexpr uint32_t kChunk = 16 / sizeof(E);
+  const uint32_t cols = p.cols[mat], padded = (cols + kChunk - 1) / kChunk * kChunk;
   const uint32_t rows = p.rows[mat];
   const E* src = static_cast<const E*>(p.src[mat]);
   E* dst = static_cast<E*>(p.dst[mat]);
@@ -1355,7 +1364,7 @@ __device__ inline void pack_rows(const DensePack& p, uint32_t mat, uint32_t grou
       for (int r = 0; r < 4; ++r) v[r] = src[min(i + r * step, uint64_t(rows) - 1) * p.lds[mat] + min(j, cols - 1)];
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        if (i + r * step < rows) dst[(i + r * step) * p.ldd[mat] + j] = j < cols ? v[r] : 0;
+        if (i + r * step < rows) dst[(i + r * step) * p.ldd[mat] + column_at(j, p.panel[mat])] = j < cols ? v[r] : 0;
     }
 }
 
@@ -1396,8 +1405,9 @@ __global__ __launch_bounds__(256) void dense_slope(DenseSlope s) {
       for (int e = 0; e < 8; ++e) v[e] = float(p[min(e * lanes_x, s.n - 1 - j)]);   // no branches between loads
     }
   };
+  const int64_t dz_at = column_at(j, s.dz_panel);   // (a workgroup's columns are in one panel)
   auto store = [&](void* base, int64_t row, const float* v) {   // rows of dz are padded to whole eights, with zeros
-    T* p = static_cast<T*>(base) + row + j;
+    T* p = static_cast<T*>(base) + row + dz_at;
     if constexpr (WHOLE) {
       store8<TYPE>(p, 8, v);
     } else {
@@ -1469,7 +1479,7 @@ int tile_launch(const DenseGemm& g, hipStream_t stream) {
   const int64_t tiles = int64_t((g.ni + BM - 1) / BM) * ((g.nj + cols - 1) / cols);
   const dim3 grid(static_cast<uint32_t>(tiles), g.splits);
   dense_tile<TYPE, KIND, BM, BN, WI, WJ, PER_CU, HALVES><<<grid, 64 * WI * WJ * HALVES, 0, stream>>>(g);
-  if (const int rc = hipGetLastError(); rc != 0 || g.splits == 1) return rc;
+  if (const int rc = hipGetLastError(); rc != 0 || g.slots == 1 || g.first + g.splits < g.slots) return rc;
   const int64_t threads = int64_t((g.nj + 7) / 8) * g.ni;
   dense_join<TYPE, KIND><<<static_cast<uint32_t>((threads + 255) / 256), 256, 0, stream>>>(g);
   return hipGetLastError();
@@ -1487,17 +1497,19 @@ int grads_launch(const DenseGemm& w, const DenseGemm& x, hipStream_t stream) {
 }
 
 template <int TYPE>
-int backward_launch(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, int variant, hipStream_t stream) {
-  int rc;
+int products_launch(const DenseGemm& w, const DenseGemm& x, int variant, hipStream_t stream) {
   if constexpr (TYPE == kDenseF32) {
-    if (variant == kTile256) rc = grads_launch<TYPE, 256, 128, 4, 2, 1>(w, x, stream);
-    else rc = grads_launch<TYPE, 128, 128, 2, 4, 1>(w, x, stream);
-  } else if (variant == kTile256) rc = grads_launch<TYPE, 256, 256, 2, 4, 1>(w, x, stream);
-  else if (variant == kTile128Halves) rc = grads_launch<TYPE, 128, 128, 2, 2, 1, 2>(w, x, stream);
-  else rc = grads_launch<TYPE, 128, 128, 2, 2, 2>(w, x, stream);
-  if (rc != 0) return rc;
+    if (variant == kTile256) return grads_launch<TYPE, 256, 128, 4, 2, 1>(w, x, stream);
+    return grads_launch<TYPE, 128, 128, 2, 4, 1>(w, x, stream);
+  } else if (variant == kTile256) return grads_launch<TYPE, 256, 256, 2, 4, 1>(w, x, stream);
+  else if (variant == kTile128Halves) return grads_launch<TYPE, 128, 128, 2, 2, 1, 2>(w, x, stream);
+  else return grads_launch<TYPE, 128, 128, 2, 2, 2>(w, x, stream);
+}
+
+template <int TYPE>
+int tail_launch(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, hipStream_t stream) {
   auto joins = [](const DenseGemm& g) {
-    return g.parts && g.splits > 1 ? static_cast<uint32_t>((int64_t((g.nj + 7) / 8) * g.ni + 255) / 256) : 0u;
+    return g.parts && g.slots > 1 ? static_cast<uint32_t>((int64_t((g.nj + 7) / 8) * g.ni + 255) / 256) : 0u;
   };
   const DenseTail t = {c.partial[0] || c.partial[1] ? uint32_t(c.n + 31) / 32 * 2 : 0u, joins(w)};
   const uint32_t groups = t.colsum_groups + t.w_groups * w.parts + joins(x);
@@ -1570,8 +1582,11 @@ int slope_launch(const DenseSlope& s, hipStream_t stream) {
     const hipStream_t s = static_cast<hipStream_t>(stream);                                                     \
     return kind == kGated ? forward_launch<TYPE, kGated>(g, s) : forward_launch<TYPE, kForward>(g, s);          \
   }                                                                                                             \
-  int dense_backward_##NAME(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, int variant, void* stream) { \
-    return backward_launch<TYPE>(w, x, c, variant, static_cast<hipStream_t>(stream));                           \
+  int dense_grads_##NAME(const DenseGemm& w, const DenseGemm& x, int variant, void* stream) {                   \
+    return products_launch<TYPE>(w, x, variant, static_cast<hipStream_t>(stream));                              \
+  }                                                                                                             \
+  int dense_tail_##NAME(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, void* stream) {           \
+    return tail_launch<TYPE>(w, x, c, static_cast<hipStream_t>(stream));                                        \
   }                                                                                                             \
   int dense_slope_##NAME(const DenseSlope& s, void* stream) {                                                   \
     return slope_launch<TYPE>(s, static_cast<hipStream_t>(stream));                                             \

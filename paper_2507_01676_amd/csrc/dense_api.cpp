@@ -61,10 +61,10 @@ emb_status_t run(int rc) { return rc == 0 ? EMB_OK : EMB_ERR_DEVICE; }
 int64_t chunk(int32_t dtype) { return 16 / static_cast<int64_t>(esize(dtype)); }   // elements of 16 bytes
 
 // Whether the products can read a matrix where it lies: rows that start at multiples of 16 bytes and hold whole
-// chunks of 16 bytes (and a tile's offsets, 256 rows at most, fit 32 bits).
+// chunks of 16 bytes (and a tile's offsets fit 32 bits).
 bool whole(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
   return !misaligned(p, 16) && ld % chunk(dtype) == 0 && cols % chunk(dtype) == 0 &&
-         ld * static_cast<int64_t>(esize(dtype)) <= (int64_t(1) << 23);
+         ld * static_cast<int64_t>(esize(dtype)) <= kMostStride;
 }
 
 // the same for the elementwise passes, of every type
@@ -258,11 +258,19 @@ emb_status_t forward(int32_t dtype, int kind, const DenseGemm& g, void* stream) 
   }
 }
 
-emb_status_t backward(int32_t dtype, const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, int variant, void* stream) {
+emb_status_t grads(int32_t dtype, const DenseGemm& w, const DenseGemm& x, int variant, void* stream) {
   switch (dtype) {
-    case EMB_DTYPE_F32: return run(dense_backward_f32(w, x, c, variant, stream));
-    case EMB_DTYPE_F16: return run(dense_backward_f16(w, x, c, variant, stream));
-    default: return run(dense_backward_bf16(w, x, c, variant, stream));
+    case EMB_DTYPE_F32: return run(dense_grads_f32(w, x, variant, stream));
+    case EMB_DTYPE_F16: return run(dense_grads_f16(w, x, variant, stream));
+    default: return run(dense_grads_bf16(w, x, variant, stream));
+  }
+}
+
+emb_status_t tail(int32_t dtype, const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, void* stream) {
+  switch (dtype) {
+    case EMB_DTYPE_F32: return run(dense_tail_f32(w, x, c, stream));
+    case EMB_DTYPE_F16: return run(dense_tail_f16(w, x, c, stream));
+    default: return run(dense_tail_bf16(w, x, c, stream));
   }
 }
 
@@ -286,11 +294,30 @@ struct Arena {
   }
 };
 
-// A matrix as the products read it: where it lies, or a copy in the workspace.
+// A matrix as the products read it: where it lies, or in the workspace.
 struct Operand {
   const void* p;
-  int64_t ld;
+  int64_t ld, panel = kPanel;
+  int32_t panels = 1;
 };
+
+// A matrix of the workspace whose rows are padded to multiples of `pad` elements; long rows in panels (whose rows are kept
+// from starting a power of two apart).
+Operand matrix_space(Arena& ar, int64_t rows, int64_t cols, int64_t pad, int32_t dtype) {
+  const int64_t size = static_cast<int64_t>(esize(dtype));
+  Operand o = {nullptr, (cols + pad - 1) / pad * pad};
+  if (o.ld * size > kMostStride) {
+    o.panels = static_cast<int32_t>((cols + kPanel - 1) / kPanel);
+    o.ld = kPanel + 64, o.panel = rows * o.ld;
+  }
+  o.p = ar.take<void>(static_cast<size_t>(o.panels) * rows * o.ld * size);
+  return o;
+}
+
+// its panel p
+const void* panel_of(const Operand& o, int32_t p, int32_t dtype) {
+  return static_cast<const char*>(o.p) + p * o.panel * static_cast<int64_t>(esize(dtype));
+}
 
 // Collects the matrices of a call that have to be copied.
 struct Packer {
@@ -300,18 +327,18 @@ struct Packer {
   bool where_they_lie = false;   // nothing is copied
   Operand use(const void* p, int64_t ld, int64_t rows, int64_t cols) {
     if (rows == 0 || where_they_lie || whole(p, ld, cols, dtype)) return {p, ld};
-    const int64_t ldd = (cols + chunk(dtype) - 1) / chunk(dtype) * chunk(dtype);
+    const Operand copy = matrix_space(ar, rows, cols, chunk(dtype), dtype);
     pack.esize = static_cast<int32_t>(esize(dtype));
     const int at = pack.count++;
     pack.src[at] = p, pack.lds[at] = ld;
-    pack.dst[at] = ar.take<void>(rows * ldd * esize(dtype)), pack.ldd[at] = ldd;
+    pack.dst[at] = const_cast<void*>(copy.p), pack.ldd[at] = copy.ld, pack.panel[at] = copy.panel;
     pack.rows[at] = static_cast<uint32_t>(rows), pack.cols[at] = static_cast<uint32_t>(cols);
     uint32_t wide = 8;
-    while (wide < 256 && wide < ldd) wide *= 2;
+    while (wide < 256 && wide < cols) wide *= 2;
     pack.wide[at] = wide;
     // enough workgroups for the longest matrix, with four rows a thread, at most eight a CU
     pack.groups = std::max<int32_t>(pack.groups, static_cast<int32_t>(std::min<int64_t>(8 * kCus, (rows * wide + 1023) / 1024)));
-    return {pack.dst[at], ldd};
+    return copy;
   }
 };
 
@@ -342,11 +369,20 @@ struct Space {
   DensePack pack;
   float* colsum[2] = {nullptr, nullptr};
   float* partial = nullptr;                   // of the forward product
-  GradChoice grads = {kTile128, 1, 1};        // of the backward calls
+  GradChoice grads = {kTile128, 1, 1};        // of the backward calls (x's splits: of a panel)
   float *w_partial = nullptr, *x_partial = nullptr;
   int32_t blocks = 1;         // of rows of column sums
   bool slopes = false;        // dz is computed
 };
+
+// The splits of each launch where a reduction takes one for each of its panels.
+int32_t splits_each(int32_t splits, int32_t panels) { return (splits + panels - 1) / panels; }
+
+void forward_partial(Arena& ar, Space& s, int64_t m, int64_t n, int mats) {
+  if (s.choice.variant >= kRows) return;
+  s.choice.splits = splits_each(s.choice.splits, s.x.panels);
+  s.partial = ar.take<float>(partial_bytes(m, n, mats, s.choice.splits * s.x.panels));
+}
 
 Space linear_space(Arena& ar, const emb_linear_t& a) {
   Space s;
@@ -358,7 +394,7 @@ Space linear_space(Arena& ar, const emb_linear_t& a) {
   s.x = pk.use(a.x, a.ldx, a.m, a.k);
   s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k);
   s.pack = pk.pack;
-  s.partial = ar.take<float>(partial_bytes(a.m, a.n, 1, s.choice.splits));
+  forward_partial(ar, s, a.m, a.n, 1);
   return s;
 }
 
@@ -374,15 +410,12 @@ Space gated_space(Arena& ar, const emb_gated_t& a) {
   s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k);
   s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k);
   s.pack = pk.pack;
-  s.partial = ar.take<float>(partial_bytes(a.m, a.n, 2, s.choice.splits));
+  forward_partial(ar, s, a.m, a.n, 2);
   return s;
 }
 
-// a computed dz: rows padded to whole chunks
-Operand dz_space(Arena& ar, int64_t m, int64_t n, int32_t dtype) {
-  const int64_t ld = (n + 7) / 8 * 8;
-  return {ar.take<void>(m * ld * esize(dtype)), ld};
-}
+// a computed dz: rows padded to whole eights
+Operand dz_space(Arena& ar, int64_t m, int64_t n, int32_t dtype) { return matrix_space(ar, m, n, 8, dtype); }
 
 float* colsum_space(Arena& ar, bool wanted, int32_t blocks, int64_t n) {
   return wanted && blocks > 1 ? ar.take<float>(size_t(blocks) * n * 4) : nullptr;
@@ -392,7 +425,8 @@ void partial_space(Arena& ar, Space& s, int32_t dtype, int64_t m, int64_t n, int
                    bool sums) {
   s.grads = choose_backward(dtype, m, n, k, mats, want_x, want_w, sums);
   s.w_partial = ar.take<float>(partial_bytes(n, k, want_w, s.grads.w_splits));
-  s.x_partial = ar.take<float>(partial_bytes(m, k, 1, s.grads.x_splits));
+  s.grads.x_splits = splits_each(s.grads.x_splits, s.dz[0].panels);
+  s.x_partial = ar.take<float>(partial_bytes(m, k, 1, s.grads.x_splits * s.dz[0].panels));
 }
 
 Space linear_grad_space(Arena& ar, const emb_linear_grad_t& a) {
@@ -431,6 +465,44 @@ Space gated_grad_space(Arena& ar, const emb_gated_grad_t& a) {
   return s;
 }
 
+// A forward product: a launch, or one for each panel of its reduction.
+emb_status_t run_forward(int32_t dtype, int kind, DenseGemm g, const Space& sp, void* stream) {
+  const bool tiles = sp.choice.variant < kRows;
+  g.a[0] = sp.x.p, g.lda = sp.x.ld, g.panel_a = sp.x.panel;
+  for (int i = 0; i < (kind == kGated ? 2 : 1); ++i)
+    g.b[i] = sp.w[i].p, g.ldb[i] = sp.w[i].ld, g.panel_b[i] = sp.w[i].panel;
+  g.parts = 1, g.variant = sp.choice.variant, g.splits = sp.choice.splits, g.row_blocks = sp.choice.row_blocks;
+  g.partial = sp.partial, g.slots = g.splits * sp.x.panels;
+  if (!tiles || sp.x.panels == 1) return forward(dtype, kind, g, stream);
+  const int32_t nr = g.nr;
+  for (int32_t p = 0; p < sp.x.panels; ++p) {
+    g.a[0] = panel_of(sp.x, p, dtype);
+    for (int i = 0; i < (kind == kGated ? 2 : 1); ++i) g.b[i] = panel_of(sp.w[i], p, dtype);
+    g.nr = static_cast<int32_t>(std::min<int64_t>(kPanel, nr - p * kPanel));
+    g.first = p * g.splits;
+    EMBX_TRY(forward(dtype, kind, g, stream));
+  }
+  return EMB_OK;
+}
+
+// Both products of a backward pass: a launch, or one for each panel of x's reduction; then the joins.
+emb_status_t run_backward(int32_t dtype, const DenseGemm& w, DenseGemm x, const DenseColsum& c, const Space& sp, void* stream) {
+  const int32_t panels = x.parts ? sp.dz[0].panels : 1, nr = x.nr;
+  x.slots = x.splits * panels;
+  for (int32_t p = 0; p < panels; ++p) {
+    if (panels > 1) {
+      for (int i = 0; i < x.parts; ++i) {
+        x.a[i] = panel_of(sp.dz[i], p, dtype);
+        x.b[i] = static_cast<const char*>(sp.w[i].p) + p * kPanel * sp.w[i].ld * static_cast<int64_t>(esize(dtype));
+      }
+      x.nr = static_cast<int32_t>(std::min<int64_t>(kPanel, nr - p * kPanel));
+      x.first = p * x.splits;
+    }
+    EMBX_TRY(grads(dtype, p == 0 ? w : DenseGemm{}, x, sp.grads.variant, stream));
+  }
+  return tail(dtype, w, x, c, stream);
+}
+
 emb_status_t run_pack(const DensePack& p, void* stream) {
   return p.count ? run(dense_pack_launch(p, stream)) : EMB_OK;
 }
@@ -463,18 +535,14 @@ emb_status_t emb_linear(const emb_linear_t* a, void* workspace, size_t workspace
   if (a->m == 0) return EMB_OK;
   EMBX_TRY(run_pack(sp.pack, stream));
   DenseGemm g = {};
-  g.a[0] = sp.x.p, g.lda = sp.x.ld;
-  g.b[0] = sp.w[0].p, g.ldb[0] = sp.w[0].ld;
   g.c[0] = a->y, g.ldc[0] = a->ldy;
   g.z[0] = a->z, g.ldz[0] = a->ldz;
   g.bias[0] = a->bias;
   g.res = a->residual, g.ldr = a->ldr;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
-  g.parts = 1, g.act = a->activation;
-  g.variant = sp.choice.variant, g.splits = sp.choice.splits, g.partial = sp.partial;
-  g.row_blocks = sp.choice.row_blocks;
+  g.act = a->activation;
   g.whole = whole(a->x, a->ldx, a->k, a->dtype) && whole(a->weight, a->ldw, a->k, a->dtype);
-  return forward(a->dtype, kForward, g, stream);
+  return run_forward(a->dtype, kForward, g, sp, stream);
 }
 
 emb_status_t emb_linear_backward_workspace(const emb_linear_grad_t* a, size_t* bytes) {
@@ -504,7 +572,7 @@ emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, si
     DenseSlope s = {};
     s.dy = a->dy, s.lddy = a->lddy;
     s.z[0] = slopes ? a->z : nullptr, s.ldz[0] = a->ldz;
-    s.dz[0] = sp.slopes ? const_cast<void*>(sp.dz[0].p) : nullptr, s.lddz = sp.dz[0].ld;
+    s.dz[0] = sp.slopes ? const_cast<void*>(sp.dz[0].p) : nullptr, s.lddz = sp.dz[0].ld, s.dz_panel = sp.dz[0].panel;
     s.colsum[0] = sp.colsum[0];
     if (sp.blocks == 1) s.total[0] = a->dbias;
     s.m = a->m, s.n = a->n, s.act = a->activation, s.gated = 0, s.row_blocks = sp.blocks;
@@ -517,21 +585,21 @@ emb_status_t emb_linear_backward(const emb_linear_grad_t* a, void* workspace, si
   }
   DenseGemm w = {}, x = {};
   if (a->dx && a->m > 0) {
-    x.a[0] = sp.dz[0].p, x.lda = sp.dz[0].ld;
-    x.b[0] = sp.w[0].p, x.ldb[0] = sp.w[0].ld;
+    x.a[0] = sp.dz[0].p, x.lda = sp.dz[0].ld, x.panel_a = sp.dz[0].panel;
+    x.b[0] = sp.w[0].p, x.ldb[0] = sp.w[0].ld, x.panel_b[0] = sp.w[0].panel;
     x.c[0] = a->dx, x.ldc[0] = a->lddx;
     x.ni = a->m, x.nj = a->k, x.nr = a->n, x.parts = 1;
     x.splits = sp.grads.x_splits, x.partial = sp.x_partial;
   }
   if (a->dweight) {
-    w.a[0] = sp.dz[0].p, w.lda = sp.dz[0].ld;
-    w.b[0] = sp.x.p, w.ldb[0] = sp.x.ld;
+    w.a[0] = sp.dz[0].p, w.lda = sp.dz[0].ld, w.panel_a = sp.dz[0].panel;
+    w.b[0] = sp.x.p, w.ldb[0] = sp.x.ld, w.panel_b[0] = sp.x.panel;
     w.c[0] = a->dweight, w.ldc[0] = a->lddw;
     w.ni = a->n, w.nj = a->k, w.nr = a->m, w.parts = 1;
-    w.splits = sp.grads.w_splits, w.partial = sp.w_partial;
+    w.splits = w.slots = sp.grads.w_splits, w.partial = sp.w_partial;
   }
   const DenseColsum c = {{sp.colsum[0], nullptr}, {a->dbias, nullptr}, sp.blocks, static_cast<int32_t>(a->n)};
-  return backward(a->dtype, w, x, c, sp.grads.variant, stream);
+  return run_backward(a->dtype, w, x, c, sp, stream);
 }
 
 emb_status_t emb_gated_workspace(const emb_gated_t* a, size_t* bytes) {
@@ -560,20 +628,15 @@ emb_status_t emb_gated(const emb_gated_t* a, void* workspace, size_t workspace_b
   if (a->m == 0) return EMB_OK;
   EMBX_TRY(run_pack(sp.pack, stream));
   DenseGemm g = {};
-  g.a[0] = sp.x.p, g.lda = sp.x.ld;
-  g.b[0] = sp.w[0].p, g.ldb[0] = sp.w[0].ld;
-  g.b[1] = sp.w[1].p, g.ldb[1] = sp.w[1].ld;
   g.c[0] = a->h, g.ldc[0] = a->ldh;
   g.z[0] = a->g, g.ldz[0] = a->ldg;
   g.z[1] = a->u, g.ldz[1] = a->ldu;
   g.bias[0] = a->b_gate, g.bias[1] = a->b_up;
   g.ni = a->m, g.nj = a->n, g.nr = a->k;
-  g.parts = 1, g.act = a->activation;
-  g.variant = sp.choice.variant, g.splits = sp.choice.splits, g.partial = sp.partial;
-  g.row_blocks = sp.choice.row_blocks;
+  g.act = a->activation;
   g.whole = whole(a->x, a->ldx, a->k, a->dtype) && whole(a->w_gate, a->ld_gate, a->k, a->dtype) &&
             whole(a->w_up, a->ld_up, a->k, a->dtype);
-  return forward(a->dtype, kGated, g, stream);
+  return run_forward(a->dtype, kGated, g, sp, stream);
 }
 
 emb_status_t emb_gated_backward_workspace(const emb_gated_grad_t* a, size_t* bytes) {
@@ -612,7 +675,7 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
     s.z[0] = a->g, s.ldz[0] = a->ldg;
     s.z[1] = a->u, s.ldz[1] = a->ldu;
     for (int i = 0; i < 2; ++i) s.dz[i] = sp.slopes ? const_cast<void*>(sp.dz[i].p) : nullptr;
-    s.lddz = sp.dz[0].ld;
+    s.lddz = sp.dz[0].ld, s.dz_panel = sp.dz[0].panel;
     s.colsum[0] = sp.colsum[0], s.colsum[1] = sp.colsum[1];
     if (sp.blocks == 1) s.total[0] = a->db_gate, s.total[1] = a->db_up;
     s.m = a->m, s.n = a->n, s.act = a->activation, s.gated = 1, s.row_blocks = sp.blocks;
@@ -626,8 +689,8 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
   }
   DenseGemm w = {}, x = {};
   if (a->dx && a->m > 0) {
-    for (int i = 0; i < 2; ++i) x.a[i] = sp.dz[i].p, x.b[i] = sp.w[i].p, x.ldb[i] = sp.w[i].ld;
-    x.lda = sp.dz[0].ld;
+    for (int i = 0; i < 2; ++i) x.a[i] = sp.dz[i].p, x.b[i] = sp.w[i].p, x.ldb[i] = sp.w[i].ld, x.panel_b[i] = sp.w[i].panel;
+    x.lda = sp.dz[0].ld, x.panel_a = sp.dz[0].panel;
     x.c[0] = a->dx, x.ldc[0] = a->lddx;
     x.ni = a->m, x.nj = a->k, x.nr = a->n, x.parts = 2;
     x.splits = sp.grads.x_splits, x.partial = sp.x_partial;
@@ -640,13 +703,13 @@ emb_status_t emb_gated_backward(const emb_gated_grad_t* a, void* workspace, size
       w.c[w.parts] = dw, w.ldc[w.parts] = i == 0 ? a->ldd_gate : a->ldd_up;
       ++w.parts;
     }
-    w.lda = sp.dz[0].ld;
-    w.b[0] = w.b[1] = sp.x.p, w.ldb[0] = w.ldb[1] = sp.x.ld;
+    w.lda = sp.dz[0].ld, w.panel_a = sp.dz[0].panel;
+    w.b[0] = w.b[1] = sp.x.p, w.ldb[0] = w.ldb[1] = sp.x.ld, w.panel_b[0] = w.panel_b[1] = sp.x.panel;
     w.ni = a->n, w.nj = a->k, w.nr = a->m;
-    w.splits = sp.grads.w_splits, w.partial = sp.w_partial;
+    w.splits = w.slots = sp.grads.w_splits, w.partial = sp.w_partial;
   }
   const DenseColsum c = {{sp.colsum[0], sp.colsum[1]}, {a->db_gate, a->db_up}, sp.blocks, static_cast<int32_t>(a->n)};
-  return backward(a->dtype, w, x, c, sp.grads.variant, stream);
+  return run_backward(a->dtype, w, x, c, sp, stream);
 }
 
 }  // extern "C"
