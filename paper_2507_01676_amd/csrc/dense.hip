@@ -368,7 +368,7 @@ __device__ inline void products6(const Parts* a, const Parts* b, f32x4 (*c)[FJ])
 // Which tile a workgroup computes.  Workgroups go round-robin over the 8 XCDs, each with an L2 of its
 // own: XCD x takes the x-th eighth of the tiles, in bands of kBand tile rows walked column by column,
 // so that the tiles in flight on one XCD share few rows of A and of B.
-constexpr int kXcds = 8, kBand = 4;
+constexpr int kBand = 4;
 
 __device__ inline void tile_of(uint32_t id, uint32_t tiles_i, uint32_t tiles_j, int* ti, int* tj) {
   const uint32_t tiles = tiles_i * tiles_j;

@@ -67,7 +67,13 @@ bool whole(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
          ld * static_cast<int64_t>(esize(dtype)) <= kMostStride;
 }
 
-// the same for the elementwise passes, of every type
+// In how many panels a matrix of the workspace is: one, where a tile with so many of its rows (256 at most) can be addressed.
+int32_t panels_of(int64_t rows, int64_t cols, int32_t dtype) {
+  const int64_t last = (std::min<int64_t>(rows, 256) - 1) * cols * static_cast<int64_t>(esize(dtype));
+  return last > kMostOffset ? static_cast<int32_t>((cols + kPanel - 1) / kPanel) : 1;
+}
+
+// the same as whole() for the elementwise passes, of every type
 bool whole16(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
   return !misaligned(p, 16) && ld * esize(dtype) % 16 == 0 && cols % 8 == 0;
 }
@@ -175,20 +181,22 @@ double pack_us(double bytes) { return 3.0 + bytes / 2.1e6; }
 //   tiles of 256 where they fill the GPU (bf16 4096^3 100, tiles of 128 135), of 128 else (2048^3 44 and 27.6), in halves
 //     where a CU has one (2048^3 23.1, 4096 x 1024 x 1024 14.1, whole 16.8; 2 x 704 columns, 352 tiles, 13.2 and 9.3), their
 //     reductions split where there are few (f32 4096 x 512 x 1664 whole 61, in two 45, in four 54)
-// `whole`, `bytes`: whether both operands are, and the size of those that are not.
-Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, bool whole, double bytes) {
+// `whole`, `bytes`: whether both operands are, and the size of those that are not; `panels`: launches that tiles take, one
+// after another.
+Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, bool whole, double bytes, int panels) {
   const int mats = kind == kGated ? 2 : 1;
-  const double steps = static_cast<double>(steps_of(dtype, k)), result_bytes = 4.0 * m * n * mats;
+  const double steps = static_cast<double>(steps_of(dtype, panels > 1 ? kPanel : k)), result_bytes = 4.0 * m * n * mats;
   Choice best = {kTile128, 1, 0}, few = {kRows, 1, 1};
   double least = 0.0, few_us = 0.0;
   for (int i = 0; i < tile_count(dtype); ++i) {
     const int variant = kTiles[i];
     const double tiles = static_cast<double>(tiles_of(dtype, variant, m, n * mats));
-    for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial)); ++s) {
+    for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s * panels <= kMostPartial)); ++s) {
       const double us = tile_us(dtype, variant, tiles, steps, s, result_bytes);
       if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, s, 0};
     }
   }
+  least *= panels;
   // weights that come from memory: f32 tiles ask for them two steps ahead, which reaches 2.2 TB/s
   if (dtype == EMB_DTYPE_F32) least = std::max(least, 4.0 * n * k * mats / 2.2e6);
   least += kCallUs;   // (the other estimates count from the launch)
@@ -218,9 +226,11 @@ double both_us(int64_t slots, int64_t w_items, double w, int64_t x_items, double
   return std::max(end, early + gap) + x * std::ceil(double(left) / slots);
 }
 
-GradChoice choose_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, int mats, bool want_x, int want_w, bool sums) {
+// `panels`: of x's reduction, a launch each.
+GradChoice choose_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, int mats, bool want_x, int want_w, bool sums,
+                           int panels) {
   static const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128};
-  const int64_t w_steps = steps_of(dtype, m), x_steps = steps_of(dtype, n) * mats;
+  const int64_t w_steps = steps_of(dtype, m), x_steps = steps_of(dtype, panels > 1 ? kPanel : n) * mats;
   const double w_bytes = 4.0 * n * k * want_w, x_bytes = 4.0 * m * k;
   GradChoice best = {kTile128, 1, 1};
   double least = 0.0;
@@ -231,7 +241,7 @@ GradChoice choose_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, int m
     for (int sw : kSplits) {
       if (sw > 1 && (!want_w || sw * 4 > w_steps || w_bytes * sw > kMostPartial || w_tiles * sw > 8 * kCus)) break;
       for (int sx : kSplits) {
-        if (sx > 1 && (!want_x || sx * 4 > x_steps || x_bytes * sx > kMostPartial || x_tiles * sx > 8 * kCus)) break;
+        if (sx > 1 && (!want_x || sx * 4 > x_steps || x_bytes * sx * panels > kMostPartial || x_tiles * sx > 8 * kCus)) break;
         const int64_t items = w_tiles * sw + x_tiles * sx, slots = items <= kCus ? kCus : kCus * t.per_cu;
         const double step = step_of(t, static_cast<double>(items));
         double us = both_us(slots, w_tiles * sw, steps_each(t, w_steps, sw) * step + t.ends, x_tiles * sx,
@@ -303,13 +313,11 @@ struct Operand {
 
 // A matrix of the workspace whose rows are padded to multiples of `pad` elements; long rows in panels (whose rows are kept
 // from starting a power of two apart).
-Operand matrix_space(Arena& ar, int64_t rows, int64_t cols, int64_t pad, int32_t dtype) {
+Operand matrix_space(Arena& ar, int64_t rows, int64_t cols, int64_t pad, int32_t panels, int32_t dtype) {
   const int64_t size = static_cast<int64_t>(esize(dtype));
   Operand o = {nullptr, (cols + pad - 1) / pad * pad};
-  if (o.ld * size > kMostStride) {
-    o.panels = static_cast<int32_t>((cols + kPanel - 1) / kPanel);
-    o.ld = kPanel + 64, o.panel = rows * o.ld;
-  }
+  o.panels = panels;
+  if (panels > 1) o.ld = kPanel + 64, o.panel = rows * o.ld;
   o.p = ar.take<void>(static_cast<size_t>(o.panels) * rows * o.ld * size);
   return o;
 }
@@ -325,9 +333,10 @@ struct Packer {
   int32_t dtype;
   DensePack pack = {};
   bool where_they_lie = false;   // nothing is copied
-  Operand use(const void* p, int64_t ld, int64_t rows, int64_t cols) {
+  // panels: of a copy
+  Operand use(const void* p, int64_t ld, int64_t rows, int64_t cols, int32_t panels) {
     if (rows == 0 || where_they_lie || whole(p, ld, cols, dtype)) return {p, ld};
-    const Operand copy = matrix_space(ar, rows, cols, chunk(dtype), dtype);
+    const Operand copy = matrix_space(ar, rows, cols, chunk(dtype), panels, dtype);
     pack.esize = static_cast<int32_t>(esize(dtype));
     const int at = pack.count++;
     pack.src[at] = p, pack.lds[at] = ld;
@@ -375,12 +384,8 @@ struct Space {
   bool slopes = false;        // dz is computed
 };
 
-// The splits of each launch where a reduction takes one for each of its panels.
-int32_t splits_each(int32_t splits, int32_t panels) { return (splits + panels - 1) / panels; }
-
 void forward_partial(Arena& ar, Space& s, int64_t m, int64_t n, int mats) {
   if (s.choice.variant >= kRows) return;
-  s.choice.splits = splits_each(s.choice.splits, s.x.panels);
   s.partial = ar.take<float>(partial_bytes(m, n, mats, s.choice.splits * s.x.panels));
 }
 
@@ -389,10 +394,11 @@ Space linear_space(Arena& ar, const emb_linear_t& a) {
   Packer pk{ar, a.dtype};
   const bool x = whole(a.x, a.ldx, a.k, a.dtype), w = whole(a.weight, a.ldw, a.k, a.dtype);
   const double bytes = double(esize(a.dtype)) * a.k * ((x ? 0 : a.m) + (w ? 0 : a.n));
-  s.choice = choose_forward(a.dtype, kForward, a.m, a.n, a.k, x && w, bytes);
+  const int32_t panels = panels_of(std::max(a.m, a.n), a.k, a.dtype);   // of both operands alike
+  s.choice = choose_forward(a.dtype, kForward, a.m, a.n, a.k, x && w, bytes, panels);
   pk.where_they_lie = s.choice.variant >= kRows;
-  s.x = pk.use(a.x, a.ldx, a.m, a.k);
-  s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k);
+  s.x = pk.use(a.x, a.ldx, a.m, a.k, panels);
+  s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k, panels);
   s.pack = pk.pack;
   forward_partial(ar, s, a.m, a.n, 1);
   return s;
@@ -404,18 +410,21 @@ Space gated_space(Arena& ar, const emb_gated_t& a) {
   const bool x = whole(a.x, a.ldx, a.k, a.dtype);
   const bool w = whole(a.w_gate, a.ld_gate, a.k, a.dtype) && whole(a.w_up, a.ld_up, a.k, a.dtype);
   const double bytes = double(esize(a.dtype)) * a.k * ((x ? 0 : a.m) + (w ? 0 : 2 * a.n));
-  s.choice = choose_forward(a.dtype, kGated, a.m, a.n, a.k, x && w, bytes);
+  const int32_t panels = panels_of(std::max(a.m, a.n), a.k, a.dtype);   // of both operands alike
+  s.choice = choose_forward(a.dtype, kGated, a.m, a.n, a.k, x && w, bytes, panels);
   pk.where_they_lie = s.choice.variant >= kRows;
-  s.x = pk.use(a.x, a.ldx, a.m, a.k);
-  s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k);
-  s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k);
+  s.x = pk.use(a.x, a.ldx, a.m, a.k, panels);
+  s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k, panels);
+  s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k, panels);
   s.pack = pk.pack;
   forward_partial(ar, s, a.m, a.n, 2);
   return s;
 }
 
 // a computed dz: rows padded to whole eights
-Operand dz_space(Arena& ar, int64_t m, int64_t n, int32_t dtype) { return matrix_space(ar, m, n, 8, dtype); }
+Operand dz_space(Arena& ar, int64_t m, int64_t n, int32_t dtype) {
+  return matrix_space(ar, m, n, 8, panels_of(m, n, dtype), dtype);
+}
 
 float* colsum_space(Arena& ar, bool wanted, int32_t blocks, int64_t n) {
   return wanted && blocks > 1 ? ar.take<float>(size_t(blocks) * n * 4) : nullptr;
@@ -423,9 +432,8 @@ float* colsum_space(Arena& ar, bool wanted, int32_t blocks, int64_t n) {
 
 void partial_space(Arena& ar, Space& s, int32_t dtype, int64_t m, int64_t n, int64_t k, int mats, bool want_x, int want_w,
                    bool sums) {
-  s.grads = choose_backward(dtype, m, n, k, mats, want_x, want_w, sums);
+  s.grads = choose_backward(dtype, m, n, k, mats, want_x, want_w, sums, s.dz[0].panels);
   s.w_partial = ar.take<float>(partial_bytes(n, k, want_w, s.grads.w_splits));
-  s.grads.x_splits = splits_each(s.grads.x_splits, s.dz[0].panels);
   s.x_partial = ar.take<float>(partial_bytes(m, k, 1, s.grads.x_splits * s.dz[0].panels));
 }
 
@@ -435,9 +443,9 @@ Space linear_grad_space(Arena& ar, const emb_linear_grad_t& a) {
   const bool dx = a.dx && a.m > 0;
   s.slopes = a.activation != EMB_ACT_NONE && a.m > 0 && (dx || a.dweight);
   if (s.slopes) s.dz[0] = dz_space(ar, a.m, a.n, a.dtype);
-  else if (dx || a.dweight) s.dz[0] = pk.use(a.dy, a.lddy, a.m, a.n);
-  if (dx) s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k);
-  if (a.dweight) s.x = pk.use(a.x, a.ldx, a.m, a.k);
+  else if (dx || a.dweight) s.dz[0] = pk.use(a.dy, a.lddy, a.m, a.n, panels_of(a.m, a.n, a.dtype));
+  if (dx) s.w[0] = pk.use(a.weight, a.ldw, a.n, a.k, panels_of(a.n, a.k, a.dtype));
+  if (a.dweight) s.x = pk.use(a.x, a.ldx, a.m, a.k, panels_of(a.m, a.k, a.dtype));
   s.pack = pk.pack;
   s.blocks = slope_blocks(a.m, a.n);
   s.colsum[0] = colsum_space(ar, a.dbias, s.blocks, a.n);
@@ -453,10 +461,10 @@ Space gated_grad_space(Arena& ar, const emb_gated_grad_t& a) {
   s.slopes = a.m > 0 && (dx || weights);
   for (int i = 0; i < 2 && s.slopes; ++i) s.dz[i] = dz_space(ar, a.m, a.n, a.dtype);
   if (dx) {
-    s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k);
-    s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k);
+    s.w[0] = pk.use(a.w_gate, a.ld_gate, a.n, a.k, panels_of(a.n, a.k, a.dtype));
+    s.w[1] = pk.use(a.w_up, a.ld_up, a.n, a.k, panels_of(a.n, a.k, a.dtype));
   }
-  if (weights) s.x = pk.use(a.x, a.ldx, a.m, a.k);
+  if (weights) s.x = pk.use(a.x, a.ldx, a.m, a.k, panels_of(a.m, a.k, a.dtype));
   s.pack = pk.pack;
   s.blocks = slope_blocks(a.m, a.n);
   s.colsum[0] = colsum_space(ar, a.db_gate, s.blocks, a.n);
@@ -487,7 +495,8 @@ emb_status_t run_forward(int32_t dtype, int kind, DenseGemm g, const Space& sp, 
 
 // Both products of a backward pass: a launch, or one for each panel of x's reduction; then the joins.
 emb_status_t run_backward(int32_t dtype, const DenseGemm& w, DenseGemm x, const DenseColsum& c, const Space& sp, void* stream) {
-  const int32_t panels = x.parts ? sp.dz[0].panels : 1, nr = x.nr;
+  const int32_t variant = sp.grads.variant, panels = x.parts ? sp.dz[0].panels : 1, nr = x.nr;
+  const DenseGemm none = {};
   x.slots = x.splits * panels;
   for (int32_t p = 0; p < panels; ++p) {
     if (panels > 1) {
@@ -498,7 +507,7 @@ emb_status_t run_backward(int32_t dtype, const DenseGemm& w, DenseGemm x, const 
       x.nr = static_cast<int32_t>(std::min<int64_t>(kPanel, nr - p * kPanel));
       x.first = p * x.splits;
     }
-    EMBX_TRY(grads(dtype, p == 0 ? w : DenseGemm{}, x, sp.grads.variant, stream));
+    EMBX_TRY(grads(dtype, p == 0 ? w : none, x, variant, stream));
   }
   return tail(dtype, w, x, c, stream);
 }

@@ -22,9 +22,9 @@ def check_strides(op, dtype, m, n, k, **kw):
         rows = 256 if f["variant"] == L.TILE256 else 128
         a_rows = rows if name in ("forward", "dx") else 64
         b_rows = rows if name == "forward" else 64
-        strides = [(f["lda"], min(a_rows, f["ni"]) if a_rows != 64 else 64)]
+        strides = [(f["lda"], min(a_rows, f["ni"] if a_rows != 64 else f["nr"]))]
         for at in range(2 if (op.startswith("emb_gated") and name != "dw") else 1):
-            strides.append((f[f"ldb{at}"], min(b_rows, f["nj"]) if b_rows != 64 else 64))
+            strides.append((f[f"ldb{at}"], min(b_rows, f["nj"] if b_rows != 64 else f["nr"])))
         for ld, across in strides:
             last = (across - 1) * ld * L.ESIZE[dtype] + 256 * L.ESIZE[dtype]
             assert last < 1 << 31, f"{op} {name} {dtype} {m} x {n} x {k}: row {across - 1} of a tile starts {last} bytes on"
