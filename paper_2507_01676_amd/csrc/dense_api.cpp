@@ -105,6 +105,13 @@ int tile_count(int32_t dtype) { return dtype == EMB_DTYPE_F32 ? 2 : 3; }
 // steps of a tile whose reduction is split s ways
 double steps_each(const TileTime& t, double steps, int s) { return std::ceil(steps / s / t.at_a_time) * t.at_a_time; }
 
+constexpr double kMostThreads = 4294967295.0;   // of a launch, along an axis of its grid
+
+// whether a launch may have so many workgroups of a tile's kernel
+bool launches(int32_t dtype, int variant, double groups) {
+  return groups * (dtype != EMB_DTYPE_F32 && variant == kTile128 ? 256 : 512) <= kMostThreads;
+}
+
 constexpr double kLaunchUs = 5.0, kCallUs = 2.0;   // of a further launch, and what the first adds to the tiles' times
 constexpr double kJoinBytes = 3.0e6;      // a microsecond, of partial sums written and read back
 constexpr double kMostPartial = 256 << 20;
@@ -191,6 +198,7 @@ Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, 
   for (int i = 0; i < tile_count(dtype); ++i) {
     const int variant = kTiles[i];
     const double tiles = static_cast<double>(tiles_of(dtype, variant, m, n * mats));
+    if (i > 0 && !launches(dtype, variant, tiles)) continue;
     for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s * panels <= kMostPartial)); ++s) {
       const double us = tile_us(dtype, variant, tiles, steps, s, result_bytes);
       if (least == 0.0 || us < 0.98 * least) least = us, best = {variant, s, 0};
@@ -204,9 +212,11 @@ Choice choose_forward(int32_t dtype, int kind, int64_t m, int64_t n, int64_t k, 
   if (!whole) least += pack_us(bytes);
   for (int blocks : {1, 2, 4}) {
     if (blocks > 1 && m <= 8 * blocks) break;
+    if (512.0 * ((n + 15) / 16) * ((m + 16 * blocks - 1) / (16 * blocks) + kXcds) > kMostThreads) continue;
     const double us = rows_us(dtype, mats, whole, blocks, m, n, k);
     if (few_us == 0.0 || us < few_us) few_us = us, few.row_blocks = blocks;
   }
+  if (few_us == 0.0) few_us = HUGE_VAL;
   if (k <= kShortSum && short_us(dtype, mats, m, n, k) < std::min(1.25 * least, few_us)) return {kShort, 1, 0};
   return few_us <= least ? few : best;
 }
@@ -238,6 +248,7 @@ GradChoice choose_backward(int32_t dtype, int64_t m, int64_t n, int64_t k, int m
     const int variant = kTiles[i];
     const TileTime t = tile_time(dtype, variant);
     const int64_t w_tiles = want_w * tiles_of(dtype, variant, n, k), x_tiles = want_x ? tiles_of(dtype, variant, m, k) : 0;
+    if (i > 0 && !launches(dtype, variant, static_cast<double>(w_tiles + x_tiles) + kXcds)) continue;
     for (int sw : kSplits) {
       if (sw > 1 && (!want_w || sw * 4 > w_steps || w_bytes * sw > kMostPartial || w_tiles * sw > 8 * kCus)) break;
       for (int sx : kSplits) {
@@ -498,6 +509,15 @@ emb_status_t run_backward(int32_t dtype, const DenseGemm& w, DenseGemm x, const 
   const int32_t variant = sp.grads.variant, panels = x.parts ? sp.dz[0].panels : 1, nr = x.nr;
   const DenseGemm none = {};
   x.slots = x.splits * panels;
+  double groups = kXcds;
+  if (w.parts) groups += double(w.splits) * w.parts * tiles_of(dtype, variant, w.ni, w.nj);
+  if (x.parts) groups += double(x.splits) * tiles_of(dtype, variant, x.ni, x.nj);
+  const bool together = launches(dtype, variant, groups);
+  for (int i = 0; i < w.parts && !together; ++i) {   // (so many results are not split: there are no partial sums)
+    DenseGemm one = w;
+    one.parts = 1, one.a[0] = w.a[i], one.c[0] = w.c[i], one.ldc[0] = w.ldc[i];
+    EMBX_TRY(grads(dtype, one, none, variant, stream));
+  }
   for (int32_t p = 0; p < panels; ++p) {
     if (panels > 1) {
       for (int i = 0; i < x.parts; ++i) {
@@ -507,7 +527,7 @@ emb_status_t run_backward(int32_t dtype, const DenseGemm& w, DenseGemm x, const 
       x.nr = static_cast<int32_t>(std::min<int64_t>(kPanel, nr - p * kPanel));
       x.first = p * x.splits;
     }
-    EMBX_TRY(grads(dtype, p == 0 ? w : none, x, variant, stream));
+    EMBX_TRY(grads(dtype, p == 0 && together ? w : none, x, variant, stream));
   }
   return tail(dtype, w, x, c, stream);
 }
