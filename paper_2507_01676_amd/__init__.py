@@ -7,6 +7,7 @@ package fails loudly if the native library has not been built.
 from __future__ import annotations
 
 import ctypes
+import importlib
 import os
 import sys
 from typing import List, Optional, Sequence
@@ -433,6 +434,19 @@ def dedup_tile(idx, stream=None):
     return uniq[:k], inv[:n]
 
 
-# (This file alone, loaded under another name beside the package, has no package to import from: it has the lookup.)
-if torch is not None and __name__ in sys.modules:
-    from .dense import ACTIVATIONS, gated_ffn, gated_ffn_backward, linear, linear_backward  # noqa: E402,F401
+# The dense layers are imported with the first use of one of their names: the lookup does not need their binding (_dense.so,
+# built for one torch).  (This file alone, loaded under another name beside the package, has no package to import from: it
+# has the lookup.)
+_DENSE = ("ACTIVATIONS", "gated_ffn", "gated_ffn_backward", "linear", "linear_backward")
+
+
+def __getattr__(name):
+    if name not in (*_DENSE, "dense") or torch is None or __name__ not in sys.modules:
+        raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+    dense = importlib.import_module(".dense", __name__)
+    globals().update((n, getattr(dense, n)) for n in _DENSE)
+    return globals()[name]
+
+
+def __dir__():
+    return sorted({*globals(), *(_DENSE if torch is not None and __name__ in sys.modules else ())})

@@ -1,10 +1,11 @@
-"""Builds libembx.so (HIP kernels for gfx950 + the C ABI + the host planner) and, where torch is
-installed, the Python binding of the dense layers in-tree.
+"""Builds libembx.so (HIP kernels for gfx950 + the C ABI + the host planner) and, where a torch for
+HIP is installed, the Python binding of the dense layers in-tree.
 
     python paper_2507_01676_amd/build.py
 """
 from __future__ import annotations
 
+import concurrent.futures
 import importlib.util
 import os
 import shutil
@@ -65,9 +66,10 @@ DENSE_PARTS = 3
 
 
 def _torch():
-    """torch's folder, or None (found without importing it)."""
+    """The folder of a torch for HIP, or None (found without importing it)."""
     spec = importlib.util.find_spec("torch")
-    return os.path.dirname(spec.origin) if spec and spec.origin else None
+    folder = os.path.dirname(spec.origin) if spec and spec.origin else None
+    return folder if folder and os.path.exists(os.path.join(folder, "lib", "libc10_hip.so")) else None
 
 
 def binding_commands(torch):
@@ -134,17 +136,19 @@ def build(verbose: bool = False) -> str:
         cmds.append(["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, f"{name}.cpp"), "-o", o])
         objs.append(o)
     torch = _torch()
-    if torch:
-        compile_, link = binding_commands(torch)
-        cmds.append(compile_)
-    _run_all(cmds, verbose)
-    if torch:
-        _run(link, verbose)
-        os.replace(BINDING + ".tmp", BINDING)
-    for lib, parts in ((FAR_LIB, [far.get(o, o) for o in objs]), (LIB, objs)):
-        tmp = lib + ".tmp"
-        _run([hipcc, "-shared", f"--offload-arch={ARCH}", "-o", tmp, *parts], verbose)
-        os.replace(tmp, lib)
+    with concurrent.futures.ThreadPoolExecutor(1) as beside:
+        if torch:
+            compile_, link = binding_commands(torch)
+            binding = beside.submit(_run, compile_, verbose)
+        _run_all(cmds, verbose)
+        for lib, parts in ((FAR_LIB, [far.get(o, o) for o in objs]), (LIB, objs)):
+            tmp = lib + ".tmp"
+            _run([hipcc, "-shared", f"--offload-arch={ARCH}", "-o", tmp, *parts], verbose)
+            os.replace(tmp, lib)
+        if torch:   # (the library is there if this fails)
+            binding.result()
+            _run(link, verbose)
+            os.replace(BINDING + ".tmp", BINDING)
     return LIB
 
 
