@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -83,6 +84,13 @@ const char* type_name(at::ScalarType t) {
   return t == at::kFloat ? "torch.float32" : t == at::kHalf ? "torch.float16" : "torch.bfloat16";
 }
 
+// The calls record nothing for torch's differentiation: a result would lack its gradient without a word.
+void check_gradient(const at::Tensor& t, const char* name) {
+  if (c10::GradMode::is_enabled() && t.requires_grad())
+    throw Refused(std::string(name) + " requires a gradient, which this call does not record: call it under torch.no_grad() or in "
+                  "a torch.autograd.Function, or give " + name + ".detach(); the _backward functions compute the gradients");
+}
+
 struct Matrix {
   void* p;
   int64_t ld;
@@ -123,6 +131,7 @@ struct Common {
     if (t.size(0) != r || t.size(1) != c)
       throw Refused(std::string(name) + " must be [" + std::to_string(r) + ", " + std::to_string(c) + "], got [" +
                     std::to_string(t.size(0)) + ", " + std::to_string(t.size(1)) + "]");
+    check_gradient(t, name);
     int64_t ld = t.stride(0);
     if (t.stride(1) != 1 && c > 1)
       throw Refused(std::string(name) + " must have contiguous rows, got strides (" + std::to_string(ld) + ", " +
@@ -143,8 +152,10 @@ struct Common {
     if (THPVariable_Check(o)) {
       const at::Tensor& t = THPVariable_Unpack(o);
       if (t.is_cuda() && t.get_device() == device && t.scalar_type() == type && t.dim() == 1 && t.size(0) == n &&
-          (n == 1 || t.stride(0) == 1))
+          (n == 1 || t.stride(0) == 1)) {
+        check_gradient(t, name);
         return t.data_ptr();
+      }
     }
     throw Refused(std::string(name) + " must be a contiguous [" + std::to_string(n) + "] " + like());
   }

@@ -9,6 +9,10 @@ Matrices are 2-D device tensors whose rows are contiguous (any row stride of at 
 vectors contiguous 1-D ones, all of one dtype: float32, float16 or bfloat16.  Results are
 allocated (torch's allocator) unless ``out`` is given; calls run on ``stream`` (a
 torch.cuda.Stream or a raw handle), the current stream by default.
+
+The calls are not differentiated by torch: tensors that require a gradient are refused where
+gradients are recorded.  Call them under torch.no_grad(), or in forward and backward of a
+torch.autograd.Function (``linear`` and ``linear_backward``, say).
 """
 from __future__ import annotations
 
