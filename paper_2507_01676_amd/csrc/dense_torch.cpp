@@ -195,6 +195,13 @@ bool flag(PyObject* o) {
   return is;
 }
 
+// A tensor given for the result, which now holds it: it counts as changed (one made in inference mode has no count).
+at::Tensor written(PyObject* o) {
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+  return t;
+}
+
 void* pointer(const std::optional<at::Tensor>& t) { return t ? t->data_ptr() : nullptr; }
 
 // body() with C++'s exceptions as Python's
@@ -242,7 +249,7 @@ PyObject* linear(PyObject*, Args a, Py_ssize_t count) {
     std::optional<at::Tensor> z;
     if (save) z = c.empty(m, n);
     g_linear({m, n, k, c.code, act, c.at.p, c.at.ld, w.p, w.ld, bias, r.p, r.ld, y.p, y.ld, pointer(z), save ? n : 0}, c.first);
-    if (given) made = THPVariable_Unpack(a[5]);
+    if (given) made = written(a[5]);
     if (!save && given) {
       Py_INCREF(a[5]);
       return a[5];
@@ -293,7 +300,7 @@ PyObject* gated(PyObject*, Args a, Py_ssize_t count) {
     const int64_t ld = save ? n : 0;
     g_gated({m, n, k, c.code, act, c.at.p, c.at.ld, wg.p, wg.ld, wu.p, wu.ld, bg, bu, h.p, h.ld, pointer(g), ld, pointer(u), ld},
             c.first);
-    if (given) made = THPVariable_Unpack(a[6]);
+    if (given) made = written(a[6]);
     if (!save && given) {
       Py_INCREF(a[6]);
       return a[6];
