@@ -153,11 +153,15 @@ __device__ inline i32x4 descriptor(const void* base) {
 
 // 16 bytes a lane from descriptor + voffset to LDS at lds + 16 * lane.  The wait for it is
 // written out where the tile is needed (stage_done): the compiler, told of the write, would
-// wait at the next LDS read of any kind.
+// wait at the next LDS read of any kind.  (It is told of m0, which it reserves for instructions like this one, and warns
+// that it will not save it.)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void load_to_lds(i32x4 rsrc, int voffset, uint32_t lds) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-               :: "s"(lds), "v"(voffset), "s"(rsrc) : "memory");
+               :: "s"(lds), "v"(voffset), "s"(rsrc) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // Waits until all but this wavefront's last LOADS loads are in LDS and every LDS read of it is done,
 // then for the other wavefronts.
