@@ -85,10 +85,9 @@ const char* type_name(at::ScalarType t) {
 }
 
 // The calls record nothing for torch's differentiation: a result would lack its gradient without a word.
-void check_gradient(const at::Tensor& t, const char* name) {
-  if (c10::GradMode::is_enabled() && t.requires_grad())
-    throw Refused(std::string(name) + " requires a gradient, which this call does not record: call it under torch.no_grad() or in "
-                  "a torch.autograd.Function, or give " + name + ".detach(); the _backward functions compute the gradients");
+[[gnu::noinline]] void refuse_gradient(const char* name) {
+  throw Refused(std::string(name) + " requires a gradient, which this call does not record: call it under torch.no_grad() or in "
+                "a torch.autograd.Function, or give " + name + ".detach(); the _backward functions compute the gradients");
 }
 
 struct Matrix {
@@ -102,6 +101,7 @@ struct Common {
   at::ScalarType type;
   int32_t code;
   int64_t device, rows, cols;
+  const bool recording = c10::GradMode::is_enabled();
   Matrix at;
 
   Common(PyObject* o, const char* name) {
@@ -131,7 +131,7 @@ struct Common {
     if (t.size(0) != r || t.size(1) != c)
       throw Refused(std::string(name) + " must be [" + std::to_string(r) + ", " + std::to_string(c) + "], got [" +
                     std::to_string(t.size(0)) + ", " + std::to_string(t.size(1)) + "]");
-    check_gradient(t, name);
+    if (recording && t.requires_grad()) refuse_gradient(name);
     int64_t ld = t.stride(0);
     if (t.stride(1) != 1 && c > 1)
       throw Refused(std::string(name) + " must have contiguous rows, got strides (" + std::to_string(ld) + ", " +
@@ -153,7 +153,7 @@ struct Common {
       const at::Tensor& t = THPVariable_Unpack(o);
       if (t.is_cuda() && t.get_device() == device && t.scalar_type() == type && t.dim() == 1 && t.size(0) == n &&
           (n == 1 || t.stride(0) == 1)) {
-        check_gradient(t, name);
+        if (recording && t.requires_grad()) refuse_gradient(name);
         return t.data_ptr();
       }
     }
