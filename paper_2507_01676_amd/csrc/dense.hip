@@ -29,7 +29,7 @@ template <> struct Elem<kDenseBF16> { using T = __bf16; using V = bf16x8; };
 // rest of that product, which would be up to |z| / 2^24 of the result, into a second factor 1 + rest ln 2 (three ulps in
 // all; f32 12247 x 576 x 64 with a sigmoid, on the kernel for short reductions, 30.8 us instead of the library functions'
 // 37); the 16-bit types round it away, and take the normal distribution function by formula 7.1.26 of Abramowitz and Stegun,
-// Handbook of Mathematical Functions (off by less than 1e-7), where f32 takes the library's erf.
+// Handbook of Mathematical Functions (off by less than 1e-7), where f32 takes the library's erfc.
 template <int TYPE>
 __device__ inline float exp_f(float z) {
   const float hi = z * 1.44269504f, e = __builtin_amdgcn_exp2f(hi);
@@ -50,7 +50,7 @@ __device__ inline float phi_f(float z, float* bell) {
   const float e = exp_f<TYPE>(-0.5f * z * z);
   *bell = e;
   if constexpr (TYPE == kDenseF32) {
-    return 0.5f * (1.0f + erff(z * 0.70710678f));
+    return 0.5f * erfcf(z * -0.70710678f);   // (1 + erf loses the small values of negative z)
   } else {
     const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
     float p = fmaf(1.061405429f, t, -1.453152027f);
