@@ -25,24 +25,37 @@ template <> struct Elem<kDenseF32> { using T = float; };
 template <> struct Elem<kDenseF16> { using T = _Float16; using V = f16x8; };
 template <> struct Elem<kDenseBF16> { using T = __bf16; using V = bf16x8; };
 
-// Activations in 32 bits, from the hardware's exp2 and reciprocal (an ulp each).  exp(z) = 2^(z log2 e): f32 carries the
-// rest of that product, which would be up to |z| / 2^24 of the result, into a second factor 1 + rest ln 2 (three ulps in
-// all; f32 12247 x 576 x 64 with a sigmoid, on the kernel for short reductions, 30.8 us instead of the library functions'
-// 37); the 16-bit types round it away, and take the normal distribution function by formula 7.1.26 of Abramowitz and Stegun,
-// Handbook of Mathematical Functions (off by less than 1e-7), where f32 takes the library's erfc.
-template <int TYPE>
+// Activations in 32 bits, from the hardware's exp2 and reciprocal (an ulp each).  exp(z) = 2^(z log2 e).  f32 carries the
+// rest of that product, which would be up to |z| / 2^24 of the result, into a second factor 1 + rest ln 2 (two ulps in all).
+// With FAR it forms small results 2^64 times as large first, as the hardware's are nought below the normal numbers (z <= 0
+// there, and below -150 as at -150, where the result is nought and the rest still finite).  The 16-bit types round the rest
+// away, and take the normal distribution function by formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical
+// Functions (off by less than 1e-7, not of itself where it is small), where f32 takes the library's erfc.
+template <int TYPE, bool FAR = true>
 __device__ inline float exp_f(float z) {
-  const float hi = z * 1.44269504f, e = __builtin_amdgcn_exp2f(hi);
-  if constexpr (TYPE != kDenseF32) return e;
-  const float rest = fmaf(z, 1.92596299e-8f, fmaf(z, 1.44269504f, -hi));
-  return fabsf(hi) < 127.0f ? fmaf(e, rest * 0.69314718f, e) : e;   // (infinities and NaN have no rest)
+  if constexpr (TYPE != kDenseF32) return __builtin_amdgcn_exp2f(z * 1.44269504f);
+  if constexpr (FAR) z = __builtin_elementwise_maximum(z, -150.0f);   // NaN passes
+  const float hi = z * 1.44269504f, rest = fmaf(z, 1.92596299e-8f, fmaf(z, 1.44269504f, -hi)) * 0.69314718f;
+  if constexpr (FAR) {
+    const bool small = hi < -100.0f;
+    const float e = __builtin_amdgcn_exp2f(hi + (small ? 64.0f : 0.0f));
+    return fmaf(e, rest, e) * (small ? 0x1p-64f : 1.0f);
+  }
+  const float e = __builtin_amdgcn_exp2f(hi);
+  return fmaf(e, rest, e);
 }
 
 template <int TYPE>
 __device__ inline float rcp_f(float z) { return __builtin_amdgcn_rcpf(z); }
 
-template <int TYPE>
-__device__ inline float sigmoid_f(float z) { return rcp_f<TYPE>(1.0f + exp_f<TYPE>(-z)); }
+// In f32 from exp(-|z|), so that the reciprocal is never below the normal numbers (five ulps in all).  16 bits: nought below
+// 2^-126.
+template <int TYPE, bool FAR>
+__device__ inline float sigmoid_f(float z) {
+  if constexpr (TYPE != kDenseF32) return rcp_f<TYPE>(1.0f + exp_f<TYPE>(-z));
+  const float t = exp_f<TYPE, FAR>(-fabsf(z)), r = rcp_f<TYPE>(1.0f + t);
+  return z >= 0.0f ? r : t * r;
+}
 
 // the normal distribution function, and exp(-z^2 / 2) on the way
 template <int TYPE>
@@ -89,6 +102,27 @@ __device__ inline float slope_f(float dy, float z, int act, float* value) {
   }
 }
 
+// whether exp(-|z|) has small results among a wavefront's eights of values: asked of all at once, they hardly ever cost
+// anything (f32 65536 x 512 x 64 with a sigmoid 59.4 us a call, with small results considered for each value 61.4)
+template <int TYPE>
+__device__ inline bool far_out(const float* z) {
+  if constexpr (TYPE != kDenseF32) return false;
+  float largest = fabsf(z[0]);
+#pragma unroll
+  for (int e = 1; e < 8; ++e) largest = fmaxf(largest, fabsf(z[e]));
+  return __any(largest > 69.0f);
+}
+
+// the sigmoid of eight values, or (TIMES) each value times its
+template <int TYPE, bool FAR, bool TIMES>
+__device__ inline void sigmoid8(float* z) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float s = sigmoid_f<TYPE, FAR>(z[e]);
+    z[e] = TIMES ? z[e] * s : s;
+  }
+}
+
 // act of eight values: one branch
 template <int TYPE>
 __device__ inline void act8(float* z, int act) {
@@ -99,12 +133,12 @@ __device__ inline void act8(float* z, int act) {
       for (int e = 0; e < 8; ++e) z[e] = __builtin_elementwise_maximum(z[e], 0.0f);   // NaN passes
       break;
     case EMB_ACT_SIGMOID:
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = sigmoid_f<TYPE>(z[e]);
+      if (far_out<TYPE>(z)) sigmoid8<TYPE, true, false>(z);
+      else sigmoid8<TYPE, false, false>(z);
       break;
     case EMB_ACT_SILU:
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] *= sigmoid_f<TYPE>(z[e]);
+      if (far_out<TYPE>(z)) sigmoid8<TYPE, true, true>(z);
+      else sigmoid8<TYPE, false, true>(z);
       break;
     case EMB_ACT_GELU:
 #pragma unroll

@@ -36,7 +36,7 @@ def check(got, want, bound, z):
     assert off[at] <= bound[at], f"z = {z[at].item()!r}: {got.view(-1)[at].item()!r}, not {want[at].item()!r}; {off[at] / bound[at]:.2f} of the bound"
 
 
-@pytest.mark.parametrize("act,top", [("gelu", 12.5)])
+@pytest.mark.parametrize("act,top", [("sigmoid", 100.0), ("silu", 100.0), ("gelu", 12.5)])
 def test_values(gpu_lib, act, top):
     import torch
     log(act)
@@ -57,7 +57,7 @@ def test_values(gpu_lib, act, top):
     check(gated, want, bound, z)
 
 
-@pytest.mark.parametrize("act,top", [("gelu", 12.0)])
+@pytest.mark.parametrize("act,top", [("sigmoid", 80.0), ("silu", 80.0), ("gelu", 12.0)])
 def test_slopes(gpu_lib, act, top):
     import torch
     log(act)
