@@ -1394,16 +1394,19 @@ __device__ inline void pack_rows(const DensePack& p, uint32_t mat, uint32_t grou
   // as many rows side by side as 256 threads hold, four at a time
   const uint32_t wide = p.wide[mat], x = threadIdx.x % wide, y = threadIdx.x / wide, side = 256 / wide;
   const uint64_t step = uint64_t(p.groups) * side;
-  for (uint64_t i = uint64_t(group) * side + y; i < rows; i += 4 * step)
+  for (uint32_t panel = 0; panel < padded; panel += kPanel, dst += p.panel[mat] - kPanel) {
+    const uint32_t end = min(padded, panel + static_cast<uint32_t>(kPanel));
+    for (uint64_t i = uint64_t(group) * side + y; i < rows; i += 4 * step)
 #pragma unroll 2
-    for (uint32_t j = x; j < padded; j += wide) {
-      E v[4];
+      for (uint32_t j = panel + x; j < end; j += wide) {
+        E v[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = src[min(i + r * step, uint64_t(rows) - 1) * p.lds[mat] + min(j, cols - 1)];
+        for (int r = 0; r < 4; ++r) v[r] = src[min(i + r * step, uint64_t(rows) - 1) * p.lds[mat] + min(j, cols - 1)];
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        if (i + r * step < rows) dst[(i + r * step) * p.ldd[mat] + column_at(j, p.panel[mat])] = j < cols ? v[r] : 0;
-    }
+        for (int r = 0; r < 4; ++r)
+          if (i + r * step < rows) dst[(i + r * step) * p.ldd[mat] + j] = j < cols ? v[r] : 0;
+      }
+  }
 }
 
 template <class E>
