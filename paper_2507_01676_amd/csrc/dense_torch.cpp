@@ -90,6 +90,10 @@ const char* type_name(at::ScalarType t) {
                 "a torch.autograd.Function, or give " + name + ".detach(); the _backward functions compute the gradients");
 }
 
+[[gnu::noinline]] void refuse_negated(const char* name) {
+  throw Refused(std::string(name) + " is a view that is negated when it is read: give " + name + ".resolve_neg()");
+}
+
 struct Matrix {
   void* p;
   int64_t ld;
@@ -132,6 +136,7 @@ struct Common {
       throw Refused(std::string(name) + " must be [" + std::to_string(r) + ", " + std::to_string(c) + "], got [" +
                     std::to_string(t.size(0)) + ", " + std::to_string(t.size(1)) + "]");
     if (recording && t.requires_grad()) refuse_gradient(name);
+    if (t.is_neg()) refuse_negated(name);
     int64_t ld = t.stride(0);
     if (t.stride(1) != 1 && c > 1)
       throw Refused(std::string(name) + " must have contiguous rows, got strides (" + std::to_string(ld) + ", " +
@@ -154,6 +159,7 @@ struct Common {
       if (t.is_cuda() && t.get_device() == device && t.scalar_type() == type && t.dim() == 1 && t.size(0) == n &&
           (n == 1 || t.stride(0) == 1)) {
         if (recording && t.requires_grad()) refuse_gradient(name);
+        if (t.is_neg()) refuse_negated(name);
         return t.data_ptr();
       }
     }
