@@ -15,8 +15,11 @@
  * row's length; vectors are contiguous.  Every operand of a call has the call's type.  Sums
  * are held in fp32 whatever the type; each result is rounded once, to the call's type,
  * except that dz, dg and du are rounded to it before the products that read them, as the
- * matrix cores take them (in fp16 one beyond 65504 is an infinity there; biases' gradients
- * are summed from the values before rounding).  Large products of fp32 operands go through
+ * matrix cores take them: 16-bit gradients are then 1.4 times as far from the exact ones as
+ * their own rounding makes them (more for a few values), and in fp16 a dz beyond 65504 is an
+ * infinity and one below 2^-14 loses bits.  Where that matters, give the call's operands in
+ * fp32, whose dz is not rounded.  Biases' gradients are summed from the values before
+ * rounding, and without an activation, or with relu, dz is exact.  Large products of fp32 operands go through
  * the matrix cores as three bf16 parts of each value, which hold all 24 bits of every normal
  * number: a product is off by less than 2^-22 of itself.  Where sums leave the range of that
  * (beyond 2^80, about), or operands are infinite or NaN, the products are formed in fp32
