@@ -88,3 +88,22 @@ def test_gradients_gated(gpu_lib, dtype, m, n, k):
     same(dwu, du.t() @ x.float(), "dwu")
     same(dbg.view(1, -1), dg.sum(0).view(1, -1), "dbg")
     same(dbu.view(1, -1), du.sum(0).view(1, -1), "dbu")
+
+
+def test_an_infinite_gradient(gpu_lib):
+    """f32: the tiles that it reaches are computed again, from panels too."""
+    import torch
+    m, n, k = 512, 2200000, 64
+    log(f"infinite gradient {m} {n} {k}")
+    gen = generator(5)
+    x, w, dy = units(gen, "f32", m, k), units(gen, "f32", n, k), units(gen, "f32", m, n)
+    x[300], w[n - 5] = 1.0, 1.0
+    dy[300, n - 5] = 0.0
+    want = [dy @ w, dy.t() @ x]
+    dy[300, n - 5] = float("inf")
+    dx, dw, db = gpu_lib.linear_backward(dy, x, w)
+    for got, value, row in ((dx, want[0], 300), (dw, want[1], n - 5)):
+        assert bool(torch.isinf(got[row]).all())
+        value[row] = float("inf")
+        same(got, value, "dx, dw")
+    assert int((~torch.isfinite(db)).sum()) == 1 and bool(torch.isinf(db[n - 5]))
