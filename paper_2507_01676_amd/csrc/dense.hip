@@ -726,7 +726,8 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
     const int r0 = (step - part * per_part) * BK;
     next.valid_b = step < end ? g.nr - r0 : 0;
     const char* b = static_cast<const char*>(g.b[part]);
-    next.b0 = descriptor(b + (kRmB ? int64_t(r0) * g.ldb[part] + column_at(j0, g.panel_b[part]) : int64_t(j0) * g.ldb[part] + r0) * 2);
+    const int64_t at = kRmB ? int64_t(r0) * g.ldb[part] + column_at(j0, g.panel_b[part]) : int64_t(j0) * g.ldb[part] + r0;
+    next.b0 = descriptor(b + at * 2);
     if constexpr (kGate) next.b1 = descriptor(static_cast<const char*>(g.b[1]) + (int64_t(j0) * g.ldb[1] + r0) * 2);
     if constexpr (KIND == kInputGrad) {
       if (part != tb_part) {
@@ -793,8 +794,8 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
       for (int m = 0; m < kMats; ++m) {
         const int mat = kGate ? m : part;
         const float* b = static_cast<const float*>(g.b[mat]);
-        vb[m].load(descriptor(b + (kRmB ? int64_t(r0) * g.ldb[mat] + column_at(j0, g.panel_b[mat]) : int64_t(j0) * g.ldb[mat] + r0)),
-                   tid, valid);
+        const int64_t at = kRmB ? int64_t(r0) * g.ldb[mat] + column_at(j0, g.panel_b[mat]) : int64_t(j0) * g.ldb[mat] + r0;
+        vb[m].load(descriptor(b + at), tid, valid);
       }
     };
     auto take_apart = [&](int slot) {

@@ -22,12 +22,13 @@ enum DenseVariant { kTile128 = 0, kTile256 = 1, kTile128Halves = 2, kRows = 3, k
 
 // Offsets within a tile of an operand have 32 bits: rows further apart than kMostStride bytes are copied first.  Where the
 // rows of a copy, or of dz, are so long that a tile's would still reach too far, it is in panels of kPanel columns, each a
-// matrix of its own; a product whose reduction runs along such rows takes a launch for each panel, which leave partial sums.  Columns of a matrix that
-// is not in panels lie as if panels were kPanel elements apart.
+// matrix of its own; a product whose reduction runs along such rows takes a launch for each panel, which leave partial
+// sums.  Columns of a matrix that is not in panels lie as if panels were kPanel elements apart.
 constexpr int kPanelLog = 19;
 constexpr int64_t kPanel = int64_t(1) << kPanelLog;
-constexpr int64_t kMostStride = int64_t(1) << 23;               // 256 rows, and 256 elements of the last, stay below 2^31 bytes
-constexpr int64_t kMostOffset = (int64_t(1) << 31) - (1 << 20);   // of a tile's last row
+constexpr int64_t kMostStride = int64_t(1) << 23;   // 256 rows, and 256 elements of the last, stay below 2^31 bytes
+constexpr int64_t kMostOffset = (int64_t(1) << 31) - (1 << 20);   // bytes to a tile's last row
+
 constexpr int kXcds = 8;
 
 // One matrix product.  Arrays of two: kGated's two weights and results; kInputGrad's two

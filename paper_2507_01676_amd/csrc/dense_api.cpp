@@ -505,7 +505,8 @@ emb_status_t run_forward(int32_t dtype, int kind, DenseGemm& g, const Space& sp,
 }
 
 // Both products of a backward pass: a launch, or one for each panel of x's reduction; then the joins.
-emb_status_t run_backward(int32_t dtype, const DenseGemm& w, DenseGemm& x, const DenseColsum& c, const Space& sp, void* stream) {
+emb_status_t run_backward(int32_t dtype, const DenseGemm& w, DenseGemm& x, const DenseColsum& c, const Space& sp,
+                          void* stream) {
   const int32_t variant = sp.grads.variant, panels = x.parts ? sp.dz[0].panels : 1, nr = x.nr;
   const DenseGemm none = {};
   x.slots = x.splits * panels;

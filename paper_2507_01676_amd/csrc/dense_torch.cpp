@@ -86,8 +86,8 @@ const char* type_name(at::ScalarType t) {
 
 // The calls record nothing for torch's differentiation: a result would lack its gradient without a word.
 [[gnu::noinline]] void refuse_gradient(const char* name) {
-  throw Refused(std::string(name) + " requires a gradient, which this call does not record: call it under torch.no_grad() or in "
-                "a torch.autograd.Function, or give " + name + ".detach(); the _backward functions compute the gradients");
+  throw Refused(std::string(name) + " requires a gradient, which this call does not record: call it under torch.no_grad() or "
+                "in a torch.autograd.Function, or give " + name + ".detach(); the _backward functions compute the gradients");
 }
 
 [[gnu::noinline]] void refuse_negated(const char* name) {

@@ -9,10 +9,11 @@ import dense_launches as L
 pytestmark = pytest.mark.skipif(not L.available(), reason="g++ not available")
 
 # as many as fit 288 GB: one query against the weights of 2^27 items and more, as many queries of small layers
-SIZES = [("f16", 1, 1 << 27, 128), ("f32", 1, 1 << 28, 65), ("bf16", 17, 1 << 28, 66), ("f32", 1 << 29, 1, 72), ("f16", 1 << 30, 1, 100),
-         ("f16", 1 << 28, 16, 100), ("bf16", 1 << 30, 8, 100), ("f32", 3, 1 << 30, 20), ("f32", 1, 1 << 30, 8), ("f32", 1 << 30, 1, 8),
-         ("f16", 1 << 30, 40, 8), ("f32", 1 << 30, 40, 8), ("f16", 1, 1 << 30, 8), ("f16", 1 << 30, 40, 66), ("f32", 1 << 27, 200, 40),
-         ("f16", 1 << 24, 4000, 40), ("bf16", 300000, 300000, 66)]
+SIZES = [("f16", 1, 1 << 27, 128), ("f32", 1, 1 << 28, 65), ("bf16", 17, 1 << 28, 66), ("f32", 1 << 29, 1, 72),
+         ("f16", 1 << 30, 1, 100), ("f16", 1 << 28, 16, 100), ("bf16", 1 << 30, 8, 100), ("f32", 3, 1 << 30, 20),
+         ("f32", 1, 1 << 30, 8), ("f32", 1 << 30, 1, 8), ("f16", 1 << 30, 40, 8), ("f32", 1 << 30, 40, 8),
+         ("f16", 1, 1 << 30, 8),
+         ("f16", 1 << 30, 40, 66), ("f32", 1 << 27, 200, 40), ("f16", 1 << 24, 4000, 40), ("bf16", 300000, 300000, 66)]
 
 
 def threads(name, f, dtype):

@@ -40,9 +40,9 @@ def test_long_rows(op, dtype, m, n, k):
         check_strides(op, dtype, m, n, k, act=0, leave=("z",))
 
 
-@pytest.mark.parametrize("op,dtype,m,n,k", [("emb_linear", "f32", 256, 256, 2200000), ("emb_gated", "bf16", 512, 260, 5000001),
-                                            ("emb_linear_backward", "f16", 300, 9000000, 40),
-                                            ("emb_gated_backward", "f32", 300, 2200001, 40), ("emb_linear", "f16", 700, 700, 700)])
+@pytest.mark.parametrize("op,dtype,m,n,k", [
+    ("emb_linear", "f32", 256, 256, 2200000), ("emb_gated", "bf16", 512, 260, 5000001), ("emb_linear", "f16", 700, 700, 700),
+    ("emb_linear_backward", "f16", 300, 9000000, 40), ("emb_gated_backward", "f32", 300, 2200001, 40)])
 def test_launches_cover_the_reduction(op, dtype, m, n, k):
     """Launches that share a reduction take all of it, and their partial sums lie one after another."""
     kind = "forward" if "backward" not in op else "dx"

@@ -33,7 +33,8 @@ def phi(z):
 def check(got, want, bound, z):
     off = (got.double().cpu().view(-1) - want).abs()
     at = int((off / bound).argmax())
-    assert off[at] <= bound[at], f"z = {z[at].item()!r}: {got.view(-1)[at].item()!r}, not {want[at].item()!r}; {off[at] / bound[at]:.2f} of the bound"
+    assert off[at] <= bound[at], \
+        f"z = {z[at].item()!r}: {got.view(-1)[at].item()!r}, not {want[at].item()!r}; {off[at] / bound[at]:.2f} of the bound"
 
 
 @pytest.mark.parametrize("act,top", [("sigmoid", 100.0), ("silu", 100.0), ("gelu", 12.5)])

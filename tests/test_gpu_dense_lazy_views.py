@@ -14,10 +14,10 @@ def test_negated_views(gpu_lib):
     f = gpu_lib
     want = f.linear(-x, w)
     column = torch.complex(x[:, :1], x[:, :1]).conj().imag   # [6, 1], minus x's first column
-    for call in (lambda: f.linear(torch._neg_view(x), w), lambda: f.linear(x, torch._neg_view(w)), lambda: f.linear(x, w, torch._neg_view(b)),
-                 lambda: f.linear(x, w, b, torch._neg_view(r)), lambda: f.linear(x, w, out=torch._neg_view(r)),
-                 lambda: f.linear_backward(torch._neg_view(r), x, w), lambda: f.gated_ffn(x, w, torch._neg_view(w)),
-                 lambda: f.linear(column, w[:, :1].contiguous())):
+    for call in (lambda: f.linear(torch._neg_view(x), w), lambda: f.linear(x, torch._neg_view(w)),
+                 lambda: f.linear(x, w, torch._neg_view(b)), lambda: f.linear(x, w, b, torch._neg_view(r)),
+                 lambda: f.linear(x, w, out=torch._neg_view(r)), lambda: f.linear_backward(torch._neg_view(r), x, w),
+                 lambda: f.gated_ffn(x, w, torch._neg_view(w)), lambda: f.linear(column, w[:, :1].contiguous())):
         with pytest.raises(ValueError, match="resolve_neg"):
             call()
     assert torch.equal(f.linear(torch._neg_view(x).resolve_neg(), w), want)

@@ -24,11 +24,13 @@ def same(got, want, what):
     want = want.to(got.dtype)
     if not torch.equal(got, want):
         wrong = (got != want).nonzero()
-        raise AssertionError(f"{what}: {len(wrong)} of {want.numel()} elements differ, rows {sorted(set(wrong[:, 0].tolist()))[:8]}")
+        rows = sorted(set(wrong[:, 0].tolist()))[:8]
+        raise AssertionError(f"{what}: {len(wrong)} of {want.numel()} elements differ, rows {rows}")
 
 
 # the last: rows that are also copied for their alignment
-@pytest.mark.parametrize("dtype,m,n,k", [("f32", 256, 256, 2200000), ("bf16", 512, 260, 5000000), ("f16", 300, 136, 4300001)], ids=str)
+@pytest.mark.parametrize("dtype,m,n,k", [("f32", 256, 256, 2200000), ("bf16", 512, 260, 5000000), ("f16", 300, 136, 4300001)],
+                         ids=str)
 def test_many_inputs(gpu_lib, dtype, m, n, k):
     import torch
     log(f"many inputs {dtype} {m} {n} {k}")
