@@ -434,19 +434,20 @@ def dedup_tile(idx, stream=None):
     return uniq[:k], inv[:n]
 
 
-# The dense layers are imported with the first use of one of their names: the lookup does not need their binding (_dense.so,
-# built for one torch).  (This file alone, loaded under another name beside the package, has no package to import from: it
+# The dense layers and their serving forms are imported with the first use of one of their names: the lookup does not need
+# their binding (_dense.so, built for one torch).  (This file alone, loaded under another name beside the package, has no package to import from: it
 # has the lookup.)
-_DENSE = ("ACTIVATIONS", "gated_ffn", "gated_ffn_backward", "linear", "linear_backward")
+_LATE = {**dict.fromkeys(("dense", "ACTIVATIONS", "gated_ffn", "gated_ffn_backward", "linear", "linear_backward"), "dense"),
+         **dict.fromkeys(("serving", "linear_int8", "moe_ffn", "quantize_rows"), "serving")}
 
 
 def __getattr__(name):
-    if name not in (*_DENSE, "dense") or torch is None or __name__ not in sys.modules:
+    if name not in _LATE or torch is None or __name__ not in sys.modules:
         raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
-    dense = importlib.import_module(".dense", __name__)
-    globals().update((n, getattr(dense, n)) for n in _DENSE)
+    module = importlib.import_module("." + _LATE[name], __name__)
+    globals().update((n, getattr(module, n)) for n, home in _LATE.items() if home == _LATE[name] != n)
     return globals()[name]
 
 
 def __dir__():
-    return sorted({*globals(), *(_DENSE if torch is not None and __name__ in sys.modules else ())})
+    return sorted({*globals(), *(_LATE if torch is not None and __name__ in sys.modules else ())})

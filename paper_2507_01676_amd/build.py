@@ -61,8 +61,10 @@ LOOKUP_UNIFORM_PARTS = (5, 6, 11)
 # of row loads in flight per step a plan may choose (kGatherStepChoices in device_types.hpp)
 GATHER_PARTS = 4
 GATHER_STEPS = (12, 13, 16)
-# dense.hip: one part per element type (f32, f16, bf16)
-DENSE_PARTS = 3
+# dense.hip: one part per element type (f32, f16, bf16, 8-bit integers)
+DENSE_PARTS = 4
+# moe.hip: one part per element type
+MOE_PARTS = 3
 
 
 def _torch():
@@ -127,11 +129,18 @@ def build(verbose: bool = False) -> str:
         o = os.path.join(BUILD, f"dense_{part}.o")
         cmds.append([hipcc, *HIP_FLAGS, f"-DEMBX_DPART={part}", "-c", os.path.join(CSRC, "dense.hip"), "-o", o])
         objs.append(o)
+    for part in range(MOE_PARTS):
+        o = os.path.join(BUILD, f"moe_{part}.o")
+        cmds.append([hipcc, *HIP_FLAGS, f"-DEMBX_MPART={part}", "-c", os.path.join(CSRC, "moe.hip"), "-o", o])
+        objs.append(o)
+    o = os.path.join(BUILD, "quantize.o")
+    cmds.append([hipcc, *HIP_FLAGS, "-c", os.path.join(CSRC, "quantize.hip"), "-o", o])
+    objs.append(o)
     o = os.path.join(BUILD, "api.o")
     cmds.append([hipcc, *HIP_FLAGS, "-x", "hip", "-c", os.path.join(CSRC, "api.cpp"), "-o", o])
     objs.append(o)
     # the planner is plain host C++: every binary64 operation rounds as written
-    for name in ("planner", "queues", "dense_api"):
+    for name in ("planner", "queues", "dense_api", "serving_api"):
         o = os.path.join(BUILD, f"{name}.o")
         cmds.append(["g++", *HOST_FLAGS, "-c", os.path.join(CSRC, f"{name}.cpp"), "-o", o])
         objs.append(o)

@@ -7,6 +7,7 @@
 
 #include "../../include/embx_dense.h"
 #include "dense.hpp"
+#include "dense_device.hpp"
 
 #ifndef EMBX_DPART
 #define EMBX_DPART -1
@@ -15,138 +16,6 @@
 
 namespace embx {
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-
-template <int TYPE> struct Elem;
-template <> struct Elem<kDenseF32> { using T = float; };
-template <> struct Elem<kDenseF16> { using T = _Float16; using V = f16x8; };
-template <> struct Elem<kDenseBF16> { using T = __bf16; using V = bf16x8; };
-
-// Activations in 32 bits, from the hardware's exp2 and reciprocal (an ulp each).  exp(z) = 2^(z log2 e).  f32 carries the
-// rest of that product, which would be up to |z| / 2^24 of the result, into a second factor 1 + rest ln 2 (two ulps in all).
-// With FAR it forms small results 2^64 times as large first, as the hardware's are nought below the normal numbers (z <= 0
-// there, and below -150 as at -150, where the result is nought and the rest still finite).  The 16-bit types round the rest
-// away, and take the normal distribution function by formula 7.1.26 of Abramowitz and Stegun, Handbook of Mathematical
-// Functions (off by less than 1e-7, and of itself by 0.2% at z = -5 and 1% at -8), where f32 takes the library's erfc.
-template <int TYPE, bool FAR = true>
-__device__ inline float exp_f(float z) {
-  if constexpr (TYPE != kDenseF32) return __builtin_amdgcn_exp2f(z * 1.44269504f);
-  if constexpr (FAR) z = __builtin_elementwise_maximum(z, -150.0f);   // NaN passes
-  const float hi = z * 1.44269504f, rest = fmaf(z, 1.92596299e-8f, fmaf(z, 1.44269504f, -hi)) * 0.69314718f;
-  if constexpr (FAR) {
-    const bool small = hi < -100.0f;
-    const float e = __builtin_amdgcn_exp2f(hi + (small ? 64.0f : 0.0f));
-    return fmaf(e, rest, e) * (small ? 0x1p-64f : 1.0f);
-  }
-  const float e = __builtin_amdgcn_exp2f(hi);
-  return fmaf(e, rest, e);
-}
-
-template <int TYPE>
-__device__ inline float rcp_f(float z) { return __builtin_amdgcn_rcpf(z); }
-
-// In f32 from exp(-|z|), so that the reciprocal is never below the normal numbers (five ulps in all).  16 bits: nought below
-// 2^-126.
-template <int TYPE, bool FAR>
-__device__ inline float sigmoid_f(float z) {
-  if constexpr (TYPE != kDenseF32) return rcp_f<TYPE>(1.0f + exp_f<TYPE>(-z));
-  const float t = exp_f<TYPE, FAR>(-fabsf(z)), r = rcp_f<TYPE>(1.0f + t);
-  return z >= 0.0f ? r : t * r;
-}
-
-// the normal distribution function, and exp(-z^2 / 2) on the way
-template <int TYPE>
-__device__ inline float phi_f(float z, float* bell) {
-  const float e = exp_f<TYPE>(-0.5f * z * z);
-  *bell = e;
-  if constexpr (TYPE == kDenseF32) {
-    return 0.5f * erfcf(z * -0.70710678f);   // (1 + erf loses the small values of negative z)
-  } else {
-    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(z), 1.0f));
-    float p = fmaf(1.061405429f, t, -1.453152027f);
-    p = fmaf(p, t, 1.421413741f);
-    p = fmaf(p, t, -0.284496736f);
-    p = fmaf(p, t, 0.254829592f) * t;
-    const float tail = 0.5f * p * e;   // of |z|
-    return z < 0.0f ? tail : 1.0f - tail;
-  }
-}
-
-// dy act'(z); *value = act(z).  The sigmoid's slope is s(z) s(-z), with both from exp(-|z|): 1 - s(z) would
-// lose all its digits where z is large.
-template <int TYPE>
-__device__ inline float slope_f(float dy, float z, int act, float* value) {
-  switch (act) {
-    case EMB_ACT_RELU:
-      *value = z < 0.0f ? 0.0f : z;
-      return z <= 0.0f ? 0.0f : dy;   // an infinite dy is not multiplied by 0
-    case EMB_ACT_SIGMOID:
-    case EMB_ACT_SILU: {
-      const float t = exp_f<TYPE>(-fabsf(z)), r = rcp_f<TYPE>(1.0f + t), w = t * r;
-      const float s = z >= 0.0f ? r : w, c = z >= 0.0f ? w : r;
-      *value = act == EMB_ACT_SIGMOID ? s : z * s;
-      return dy * (act == EMB_ACT_SIGMOID ? s * c : s * (1.0f + z * c));
-    }
-    case EMB_ACT_GELU: {
-      float bell;
-      const float p = phi_f<TYPE>(z, &bell);
-      *value = z * p;
-      return dy * (p + z * 0.39894228f * bell);
-    }
-    default:
-      *value = z;
-      return dy;
-  }
-}
-
-// whether exp(-|z|) has small results among a wavefront's eights of values: asked of all at once, they hardly ever cost
-// anything (f32 65536 x 512 x 64 with a sigmoid 59.4 us a call, with small results considered for each value 61.4)
-template <int TYPE>
-__device__ inline bool far_out(const float* z) {
-  if constexpr (TYPE != kDenseF32) return false;
-  float largest = fabsf(z[0]);
-#pragma unroll
-  for (int e = 1; e < 8; ++e) largest = fmaxf(largest, fabsf(z[e]));
-  return __any(largest > 69.0f);
-}
-
-// the sigmoid of eight values, or (TIMES) each value times its
-template <int TYPE, bool FAR, bool TIMES>
-__device__ inline void sigmoid8(float* z) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float s = sigmoid_f<TYPE, FAR>(z[e]);
-    z[e] = TIMES ? z[e] * s : s;
-  }
-}
-
-// act of eight values: one branch
-template <int TYPE>
-__device__ inline void act8(float* z, int act) {
-  float bell;
-  switch (act) {
-    case EMB_ACT_RELU:
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] = __builtin_elementwise_maximum(z[e], 0.0f);   // NaN passes
-      break;
-    case EMB_ACT_SIGMOID:
-      if (far_out<TYPE>(z)) sigmoid8<TYPE, true, false>(z);
-      else sigmoid8<TYPE, false, false>(z);
-      break;
-    case EMB_ACT_SILU:
-      if (far_out<TYPE>(z)) sigmoid8<TYPE, true, true>(z);
-      else sigmoid8<TYPE, false, true>(z);
-      break;
-    case EMB_ACT_GELU:
-#pragma unroll
-      for (int e = 0; e < 8; ++e) z[e] *= phi_f<TYPE>(z[e], &bell);
-      break;
-    default: break;
-  }
-}
 
 // ---------------------------------------------------------------- tiles
 //
@@ -171,9 +40,7 @@ __device__ inline uint32_t lds_address(const void* p) {
   return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((LDS_PTR(const void))p));
 }
 
-typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 __device__ inline i32x4 descriptor(const void* base) {
   const uint64_t p = reinterpret_cast<uint64_t>(base);
@@ -206,24 +73,16 @@ __device__ inline void stage_done() {
 
 __device__ f32x4 buffer_load_f32x4(i32x4 rsrc, int voffset, int soffset, int aux) __asm("llvm.amdgcn.raw.buffer.load.v4f32");
 
-template <int TYPE>
-__device__ inline f32x4 mfma16(s16x8 a, s16x8 b, f32x4 c) {
-  using V = typename Elem<TYPE>::V;
-  if constexpr (TYPE == kDenseF16)
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
-  else
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b), c, 0, 0, 0);
-}
-
-// One operand's tile of ROWS results (rows of x or dz, columns of the result) by BK 16-bit elements of the reduction.
-// RM: reduction-major in memory.
-template <int ROWS, bool RM, int WAVES>
+// One operand's tile of ROWS results (rows of x or dz, columns of the result) by BK elements of SIZE bytes of the reduction.
+// RM: reduction-major in memory (16-bit elements).
+template <int ROWS, bool RM, int WAVES, int SIZE = 2>
 struct Tile {
-  static constexpr int BK = 64;
+  static constexpr int BK = 128 / SIZE, kPer = 16 / SIZE;     // kPer: elements of a chunk
+  static_assert(!RM || SIZE == 2);
   static constexpr int kBytes = ROWS * 128;
   static constexpr int kLoads = kBytes / 1024 / WAVES;        // 1 KB pieces a wavefront loads
   static constexpr int kRowBytes = RM ? ROWS * 2 : 128;
-  static constexpr int kChunks = kRowBytes / 16;              // of eight elements
+  static constexpr int kChunks = kRowBytes / 16;
   static constexpr int kRowsPerLoad = 1024 / kRowBytes;
   static_assert(kBytes % (1024 * WAVES) == 0, "every wavefront loads alike");
 
@@ -244,8 +103,8 @@ struct Tile {
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
       const int row = load_row(n, wave, lane), chunk = load_chunk(row, lane);
-      const bool in = RM ? chunk * 8 < rows : row < rows;
-      voff[n] = in ? static_cast<int>(row * ld * 2) + chunk * 16 : kOutOfRange;
+      const bool in = RM ? chunk * kPer < rows : row < rows;
+      voff[n] = in ? static_cast<int>(row * ld * SIZE) + chunk * 16 : kOutOfRange;
     }
   }
 
@@ -254,13 +113,13 @@ struct Tile {
     int v = voff[n];
     if (valid < BK) {
       const int row = load_row(n, wave, lane), chunk = load_chunk(row, lane);
-      v = (RM ? row < valid : chunk * 8 < valid) ? v : kOutOfRange;
+      v = (RM ? row < valid : chunk * kPer < valid) ? v : kOutOfRange;
     }
     load_to_lds(rsrc, v, lds + (n * WAVES + wave) * 1024);
   }
 
-  // fragment of 16 results (from `first` on, a multiple of 16) by 32 of the reduction (half ks): lane: result
-  // lane % 16, reduction 8 (lane / 16) .. + 7
+  // fragment of 16 results (from `first` on, a multiple of 16) by half of the step (half ks): lane: result
+  // lane % 16, chunk lane / 16 of the half
   __device__ static s16x8 fragment(const char* tile, int first, int ks, int lane) {
     const int q = lane >> 4, c = lane & 15;
     if constexpr (RM) {
@@ -419,37 +278,6 @@ __device__ inline void tile_of(uint32_t id, uint32_t tiles_i, uint32_t tiles_j, 
   *tj = in / rows;
 }
 
-// Eight consecutive elements at p, of which n >= 1 are inside (the last one stands for the others); whole eights are read
-// and written 16 bytes at a time at any alignment.
-template <int TYPE>
-__device__ inline void load8(const void* p, int n, float* v) {
-  using T = typename Elem<TYPE>::T;
-  T x[8];
-  if (n == 8) {
-    __builtin_memcpy(x, p, sizeof(x));
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = float(x[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = float(static_cast<const T*>(p)[min(e, n - 1)]);
-  }
-}
-
-template <int TYPE>
-__device__ inline void store8(void* p, int n, const float* v) {
-  using T = typename Elem<TYPE>::T;
-  T x[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = T(v[e]);
-  if (n == 8) {
-    __builtin_memcpy(p, x, sizeof(x));
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) static_cast<T*>(p)[e] = x[e];
-  }
-}
-
 // Turns sums into results: eight consecutive columns, from j on, of a lane's rows, which are `step` rows apart.  What does
 // not change from row to row is worked out once: of products with short sums the epilogue's instructions are a good part.
 template <int TYPE, int KIND>
@@ -523,6 +351,53 @@ struct Finish {
   }
 };
 
+// The same for products of 8-bit integers: y = act(s_i t_j sum + b_j) + r, whose bias, residual and result have a type of
+// their own.  Sums become f32 here (2^-24 of themselves at most, as the products with both scales).
+template <>
+struct Finish<kDenseI8, kForward> {
+  const DenseGemm& g;
+  int64_t i;
+  int j, n, step;
+  float scale[8], bias[8];
+
+  __device__ Finish(const DenseGemm& g_, int, int64_t i_, int j_, int step_) : g(g_), i(i_), j(j_), n(min(8, g_.nj - j_)), step(step_) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) bias[e] = 0.0f, scale[e] = n > 0 ? g.scale_b[j + min(e, n - 1)] : 0.0f;
+    if (g.bias[0] && n > 0) load(static_cast<const char*>(g.bias[0]), j, bias);
+  }
+
+  __device__ void next() { i += step; }
+
+  __device__ void load(const char* p, int64_t at, float* v) const {
+    switch (g.result) {
+      case kDenseF32: load8<kDenseF32>(p + at * 4, n, v); break;
+      case kDenseF16: load8<kDenseF16>(p + at * 2, n, v); break;
+      default: load8<kDenseBF16>(p + at * 2, n, v); break;
+    }
+  }
+
+  __device__ void put(float* s, float*) const {
+    const float row = g.scale_a[i];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s[e] = static_cast<float>(__float_as_int(s[e])) * row * scale[e] + bias[e];
+    if (g.result == kDenseF32) act8<kDenseF32>(s, g.act);
+    else act8<kDenseBF16>(s, g.act);
+    if (g.res) {
+      float b[8];
+      load(static_cast<const char*>(g.res), i * g.ldr + j, b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] += b[e];
+    }
+    char* const y = static_cast<char*>(g.c[0]);
+    const int64_t at = i * g.ldc[0] + j;
+    switch (g.result) {
+      case kDenseF32: store8<kDenseF32>(y + at * 4, n, s); break;
+      case kDenseF16: store8<kDenseF16>(y + at * 2, n, s); break;
+      default: store8<kDenseBF16>(y + at * 2, n, s); break;
+    }
+  }
+};
+
 // Stores a wavefront's sums, from row i0 and column j0 on, through LDS of its own: 64 rows of FJ * 16 sums at a time, so
 // that a lane has eight consecutive columns and the activation's code is there once.  Lane (q, c) holds row c and
 // columns 4 q .. + 3 of each fragment.  The 16-byte chunks of a row in LDS are permuted by the row.
@@ -530,7 +405,7 @@ template <int FJ>
 constexpr int kSumsLds = 64 * FJ * 64;   // (half of it with two fragments of rows)
 
 template <int TYPE, int KIND, int FI, int FJ>
-__device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char* own, int lane, int64_t i0, int j0, int part,
+__device__ inline void store_sums(const DenseGemm& g, Sums<TYPE> (&acc)[FI][FJ], char* own, int lane, int64_t i0, int j0, int part,
                                   int split) {
   constexpr bool kGate = KIND == kGated;
   constexpr int kRowBytes = FJ * 64, kMask = FJ * 4 - 1, kUp = FJ * 2;   // kUp: first chunk of the up projection
@@ -542,7 +417,7 @@ __device__ inline void store_sums(const DenseGemm& g, f32x4 (&acc)[FI][FJ], char
     for (int fi = 0; fi < kPass; ++fi)
 #pragma unroll
       for (int fj = 0; fj < FJ; ++fj)
-        *reinterpret_cast<f32x4*>(own + (fi * 16 + c) * kRowBytes + (((fj * 4 + q) ^ (c & kMask)) << 4)) = acc[h * kPass + fi][fj];
+        *reinterpret_cast<Sums<TYPE>*>(own + (fi * 16 + c) * kRowBytes + (((fj * 4 + q) ^ (c & kMask)) << 4)) = acc[h * kPass + fi][fj];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     constexpr int kLanes = kGate ? FJ : FJ * 2, kRows = 64 / kLanes;   // lanes of a row, rows at a time
     const int e = lane % kLanes * 2, j = j0 + e * 4;                   // the row's first chunk of this lane
@@ -670,9 +545,10 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
   constexpr int kCols = kGate ? BN / 2 : BN;               // result columns of a tile
   constexpr int kWI = BM / WI, kWJ = kCols / WJ;           // results of a wavefront
   constexpr int kFI = kWI / 16, kFJ = BN / WJ / 16;        // its fragments
-  using TileA = Tile<BM, kRmA, kWaves>;                    // (16 bits)
-  using TileB = Tile<BN, kRmB, kWaves>;
-  using TileH = Tile<kCols, kRmB, kWaves>;                 // one projection's half of B
+  constexpr int kSize = TYPE == kDenseI8 ? 1 : 2;          // of elements that go to LDS as they are
+  using TileA = Tile<BM, kRmA, kWaves, kSize>;             // (not f32)
+  using TileB = Tile<BN, kRmB, kWaves, kSize>;
+  using TileH = Tile<kCols, kRmB, kWaves, kSize>;          // one projection's half of B
   constexpr int BK = kF32 ? 32 : TileA::BK;
   static_assert(kF32 || kSlotsA * TileA::kBytes + kSlotsB * TileB::kBytes <= kTileLds<TYPE, BM, BN, WJ, kWaves>);
 
@@ -718,7 +594,7 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
     const int r0 = (step - part * per_part) * BK;
     next.valid_a = step < end ? g.nr - r0 : 0;
     const char* a = static_cast<const char*>(g.a[KIND == kWeightGrad ? wpart : part]);
-    next.a = descriptor(a + (kRmA ? int64_t(r0) * g.lda + column_at(i0, g.panel_a) : int64_t(i0) * g.lda + r0) * 2);
+    next.a = descriptor(a + (kRmA ? int64_t(r0) * g.lda + column_at(i0, g.panel_a) : int64_t(i0) * g.lda + r0) * kSize);
     next.at_a = lds0 + slot * TileA::kBytes;
   };
   auto set_b = [&](int step, int slot) {
@@ -727,8 +603,8 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
     next.valid_b = step < end ? g.nr - r0 : 0;
     const char* b = static_cast<const char*>(g.b[part]);
     const int64_t at = kRmB ? int64_t(r0) * g.ldb[part] + column_at(j0, g.panel_b[part]) : int64_t(j0) * g.ldb[part] + r0;
-    next.b0 = descriptor(b + at * 2);
-    if constexpr (kGate) next.b1 = descriptor(static_cast<const char*>(g.b[1]) + (int64_t(j0) * g.ldb[1] + r0) * 2);
+    next.b0 = descriptor(b + at * kSize);
+    if constexpr (kGate) next.b1 = descriptor(static_cast<const char*>(g.b[1]) + (int64_t(j0) * g.ldb[1] + r0) * kSize);
     if constexpr (KIND == kInputGrad) {
       if (part != tb_part) {
         tb.init(wave, lane, g.ldb[part], g.nj - j0);
@@ -752,8 +628,8 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
   };
 
   const int wi = (wave / WJ) * kWI, wj = (wave % WJ) * kWJ;
-  f32x4 acc[kFI][kFJ] = {};
-  // fragments of a half step (16 bits)
+  Sums<TYPE> acc[kFI][kFJ] = {};
+  // fragments of a half step (not f32)
   auto fragments_a = [&](const char* sa, int ks, s16x8* f) {
 #pragma unroll
     for (int n = 0; n < kFI; ++n) f[n] = TileA::fragment(sa, wi + n * 16, ks, lane);
@@ -976,18 +852,18 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
       for (int fi = 0; fi < 2; ++fi)
 #pragma unroll
         for (int fj = 0; fj < kFJ; ++fj)
-          *reinterpret_cast<f32x4*>(pass + half * kGiven + (fi * kFJ + fj) * 1024) = acc[from + fi][fj];
+          *reinterpret_cast<Sums<TYPE>*>(pass + half * kGiven + (fi * kFJ + fj) * 1024) = acc[from + fi][fj];
     };
     if (half == 0) give(2);
     else give(0);
     __syncthreads();
-    f32x4 sum[2][kFJ];
+    Sums<TYPE> sum[2][kFJ];
     auto take = [&](int at) {
 #pragma unroll
       for (int fi = 0; fi < 2; ++fi)
 #pragma unroll
         for (int fj = 0; fj < kFJ; ++fj)
-          sum[fi][fj] = acc[at + fi][fj] + *reinterpret_cast<const f32x4*>(pass + (half ^ 1) * kGiven + (fi * kFJ + fj) * 1024);
+          sum[fi][fj] = acc[at + fi][fj] + *reinterpret_cast<const Sums<TYPE>*>(pass + (half ^ 1) * kGiven + (fi * kFJ + fj) * 1024);
     };
     if (half == 0) take(0);
     else take(2);
@@ -1025,6 +901,12 @@ __global__ __launch_bounds__(64 * WI * WJ * HALVES, WI * WJ * HALVES * PER_CU / 
   }
 }
 
+// of sums as they are held (8-bit integers': whole numbers' bits)
+template <int TYPE>
+__device__ inline float plus(float a, float b) {
+  return TYPE == kDenseI8 ? __int_as_float(__float_as_int(a) + __float_as_int(b)) : a + b;
+}
+
 // Eight columns of a result whose reduction was split: the splits' sums are added in order.
 template <int TYPE, int KIND>
 __device__ inline void join8(const DenseGemm& g, int64_t at, int part) {
@@ -1050,7 +932,10 @@ __device__ inline void join8(const DenseGemm& g, int64_t at, int part) {
 #pragma unroll
       for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[mat][e] += lo[n][e], s[mat][4 + e] += hi[n][e];
+        for (int e = 0; e < 4; ++e) {
+          s[mat][e] = plus<TYPE>(s[mat][e], lo[n][e]);
+          s[mat][4 + e] = plus<TYPE>(s[mat][4 + e], hi[n][e]);
+        }
       split += N;
     };
     while (g.slots - split >= 8) add(std::integral_constant<int, 8>{});
@@ -1133,14 +1018,15 @@ struct Loader {
         for (int e = 0; e < 4; ++e) v[4 * h + e] = at + 4 * h < n ? x[e] : 0.0f;
       }
     } else {
-      h = *reinterpret_cast<const s16x8*>(row + min(at, n - 8));
+      constexpr int kPer = 16 / sizeof(T);   // (the last chunk of 8-bit integers may hold fewer)
+      h = *reinterpret_cast<const s16x8*>(row + (TYPE == kDenseI8 ? min(at, (n - 1) / kPer * kPer) : min(at, n - 8)));
       if (at >= n) h = s16x8{};
     }
   }
 };
 
 template <int TYPE>
-__device__ inline f32x4 multiply(const Loader<TYPE>& w, const Loader<TYPE>& x, f32x4 c) {
+__device__ inline Sums<TYPE> multiply(const Loader<TYPE>& w, const Loader<TYPE>& x, Sums<TYPE> c) {
   if constexpr (TYPE == kDenseF32) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[e], x.v[e], c, 0, 0, 0);
@@ -1159,6 +1045,7 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
   using T = typename Elem<TYPE>::T;
   using L = Loader<TYPE>;
   constexpr int kMats = KIND == kGated ? 2 : 1;
+  constexpr int kPer = TYPE == kDenseI8 ? 16 : 8, kStep = 4 * kPer;   // elements of a lane, and of a wavefront's step
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
   uint32_t i = blockIdx.x / across, j_ = blockIdx.x % across;
@@ -1167,7 +1054,7 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
     if (i >= down) return;
   }
   const int i0 = i * FR * 16, j0 = j_ * 16;
-  f32x4 acc[FR][kMats] = {};
+  Sums<TYPE> acc[FR][kMats] = {};
   auto products = [&](const L* x, const L* w) {
 #pragma unroll
     for (int f = 0; f < FR; ++f)
@@ -1182,12 +1069,12 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 #pragma unroll
     for (int m = 0; m < kMats; ++m) weights[m] = static_cast<const T*>(g.b[m]) + min(j0 + c, g.nj - 1) * g.ldb[m];
 #pragma unroll 4
-    for (int r0 = wave * 32; r0 < g.nr; r0 += 8 * 32) {
+    for (int r0 = wave * kStep; r0 < g.nr; r0 += 8 * kStep) {
       L x[FR], w[kMats];
 #pragma unroll
-      for (int m = 0; m < kMats; ++m) w[m].load(weights[m], r0 + 8 * q, g.nr);
+      for (int m = 0; m < kMats; ++m) w[m].load(weights[m], r0 + kPer * q, g.nr);
 #pragma unroll
-      for (int f = 0; f < FR; ++f) x[f].load(rows[f], r0 + 8 * q, g.nr);
+      for (int f = 0; f < FR; ++f) x[f].load(rows[f], r0 + kPer * q, g.nr);
       products(x, w);
     }
   } else {
@@ -1236,7 +1123,7 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 #pragma unroll
   for (int f = 0; f < FR; ++f)
 #pragma unroll
-    for (int m = 0; m < kMats; ++m) *reinterpret_cast<f32x4*>(&sums[wave][f][m][c][4 * q]) = acc[f][m];
+    for (int m = 0; m < kMats; ++m) *reinterpret_cast<Sums<TYPE>*>(&sums[wave][f][m][c][4 * q]) = acc[f][m];
   __syncthreads();
   const int t = threadIdx.x, row = t >> 1, j = j0 + (t & 1) * 8;
   if (row >= FR * 16 || i0 + row >= g.ni || j >= g.nj) return;
@@ -1246,7 +1133,7 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 #pragma unroll
     for (int m = 0; m < kMats; ++m)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[m][e] += sums[w][row >> 4][m][row & 15][(t & 1) * 8 + e];
+      for (int e = 0; e < 8; ++e) s[m][e] = plus<TYPE>(s[m][e], sums[w][row >> 4][m][row & 15][(t & 1) * 8 + e]);
   Finish<TYPE, KIND>(g, 0, i0 + row, j, 0).put(s[0], s[1]);
 }
 
@@ -1567,8 +1454,8 @@ template <int TYPE, int KIND, int FR>
 int rows_launch(const DenseGemm& g, hipStream_t stream) {
   const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
   const uint32_t grid = across * (down >= kXcds ? (down + kXcds - 1) / kXcds * kXcds : down);
-  if (g.whole) dense_rows<TYPE, KIND, FR, true><<<grid, 512, 0, stream>>>(g);
-  else dense_rows<TYPE, KIND, FR, false><<<grid, 512, 0, stream>>>(g);
+  if (TYPE == kDenseI8 || g.whole) dense_rows<TYPE, KIND, FR, true><<<grid, 512, 0, stream>>>(g);
+  else if constexpr (TYPE != kDenseI8) dense_rows<TYPE, KIND, FR, false><<<grid, 512, 0, stream>>>(g);
   return hipGetLastError();
 }
 
@@ -1595,10 +1482,12 @@ int forward_launch(const DenseGemm& g, hipStream_t stream) {
     if (g.row_blocks == 2) return rows_launch<TYPE, KIND, 2>(g, stream);
     return rows_launch<TYPE, KIND, 4>(g, stream);
   }
-  if (g.variant == kShort) {
-    constexpr int kColumns = KIND == kGated ? 2 : 4;
-    if (g.nr <= 32) return short_launch<TYPE, KIND, kColumns, 1>(g, stream);
-    return short_launch<TYPE, KIND, kColumns, 2>(g, stream);
+  if constexpr (TYPE != kDenseI8) {
+    if (g.variant == kShort) {
+      constexpr int kColumns = KIND == kGated ? 2 : 4;
+      if (g.nr <= 32) return short_launch<TYPE, KIND, kColumns, 1>(g, stream);
+      return short_launch<TYPE, KIND, kColumns, 2>(g, stream);
+    }
   }
   if constexpr (TYPE == kDenseF32) {
     if (g.variant == kTile256) return tile_launch<TYPE, KIND, 256, 128, 4, 2, 1>(g, stream);
@@ -1641,6 +1530,7 @@ int slope_launch(const DenseSlope& s, hipStream_t stream) {
 int dense_pack_launch(const DensePack& p, void* stream) {
   const uint32_t grid = p.groups * p.count;
   if (p.esize == 4) dense_pack<uint32_t><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(p);
+  else if (p.esize == 1) dense_pack<uint8_t><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(p);
   else dense_pack<uint16_t><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(p);
   return hipGetLastError();
 }
@@ -1654,6 +1544,9 @@ EMBX_DENSE_TYPE(f16, kDenseF16)
 #endif
 #if EMBX_HAS_DPART(2)
 EMBX_DENSE_TYPE(bf16, kDenseBF16)
+#endif
+#if EMBX_HAS_DPART(3)
+int dense_forward_i8(const DenseGemm& g, void* stream) { return forward_launch<kDenseI8, kForward>(g, static_cast<hipStream_t>(stream)); }
 #endif
 
 }  // namespace embx

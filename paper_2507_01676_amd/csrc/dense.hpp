@@ -7,7 +7,7 @@
 
 namespace embx {
 
-enum DenseType { kDenseF32 = 0, kDenseF16 = 1, kDenseBF16 = 2 };
+enum DenseType { kDenseF32 = 0, kDenseF16 = 1, kDenseBF16 = 2, kDenseI8 = 3 };
 
 // The three products of a layer.  A matrix is "reduction-major" (R) where consecutive
 // elements in memory step along the outputs, and "along the reduction" (K) otherwise.
@@ -50,6 +50,8 @@ struct DenseGemm {
   int32_t whole;           // kRows, kShort: operands' rows start at multiples of 16 bytes and hold whole chunks
   int32_t slots, first;    // tiles: partial sums, the splits of all launches, and the first one of this
   int64_t panel_a, panel_b[2];   // tiles: elements from a panel of columns to the next
+  const float *scale_a, *scale_b;   // 8-bit integers: of the rows of A and of B
+  int32_t result;                // 8-bit integers: DenseType of bias, residual and result
 };
 
 // matrices copied to rows of whole 16-byte chunks, in panels
@@ -87,6 +89,12 @@ struct DenseColsum {
   int32_t blocks, n;
 };
 
+// Which kernel a product takes (DenseVariant), over how many workgroups its reduction is split and, of kRows, how many
+// times 16 rows a workgroup has.
+struct DenseChoice { int32_t variant, splits, row_blocks; };
+
+DenseChoice dense_choose_i8(int64_t m, int64_t n, int64_t k);   // of 8-bit integers; variant -1: too large for a launch
+
 int dense_pack_launch(const DensePack& p, void* stream);
 
 // launches of the kernels of one type (dense.hip is compiled once per type); 0 or a hipError_t
@@ -99,6 +107,7 @@ EMBX_DENSE_DECLARE(f32)
 EMBX_DENSE_DECLARE(f16)
 EMBX_DENSE_DECLARE(bf16)
 #undef EMBX_DENSE_DECLARE
+int dense_forward_i8(const DenseGemm& g, void* stream);   // kForward of 8-bit integers, which are whole
 
 }  // namespace embx
 #endif

@@ -78,9 +78,7 @@ bool whole16(const void* p, int64_t ld, int64_t cols, int32_t dtype) {
   return !misaligned(p, 16) && ld * esize(dtype) % 16 == 0 && cols % 8 == 0;
 }
 
-// Which kernel a product takes (DenseVariant), over how many workgroups its reduction is split and, of kRows, how many
-// times 16 rows a workgroup has.
-struct Choice { int32_t variant, splits, row_blocks; };
+using Choice = DenseChoice;
 
 constexpr int64_t kShortSum = 64;   // the longest reduction that kShort takes
 
@@ -538,6 +536,30 @@ emb_status_t run_pack(const DensePack& p, void* stream) {
 }
 
 }  // namespace
+
+// Products of 8-bit integers: the same tiles take as long for a step of 128 bytes as with 16-bit elements, of which it holds
+// half as many, and so does the kernel of few rows.
+DenseChoice embx::dense_choose_i8(int64_t m, int64_t n, int64_t k) {
+  const double steps = std::ceil(k / 128.0), result_bytes = 4.0 * m * n;
+  Choice best = {-1, 1, 0}, few = {kRows, 1, 1};
+  double least = HUGE_VAL, few_us = HUGE_VAL;
+  for (const int variant : kTiles) {
+    const double tiles = static_cast<double>(tiles_of(EMB_DTYPE_BF16, variant, m, n));
+    if (!launches(EMB_DTYPE_BF16, variant, tiles)) continue;
+    for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial)); ++s) {
+      const double us = tile_us(EMB_DTYPE_BF16, variant, tiles, steps, s, result_bytes);
+      if (us < 0.98 * least) least = us, best = {variant, s, 0};
+    }
+  }
+  least += kCallUs;
+  for (const int blocks : {1, 2, 4}) {
+    if (blocks > 1 && m <= 8 * blocks) break;
+    if (512.0 * ((n + 15) / 16) * ((m + 16 * blocks - 1) / (16 * blocks) + kXcds) > kMostThreads) continue;
+    const double us = rows_us(EMB_DTYPE_BF16, 1, true, blocks, m, n, (k + 1) / 2);
+    if (us < few_us) few_us = us, few.row_blocks = blocks;
+  }
+  return few_us <= least ? few : best;
+}
 
 extern "C" {
 

@@ -1,5 +1,5 @@
-// The dense layers' calls for Python: checks torch tensors, allocates results and workspace with torch's allocator and
-// calls include/embx_dense.h on the current stream.  Argument marshalling only.  It is compiled because a small call's time
+// The dense layers' calls and their serving forms' for Python: checks torch tensors, allocates results and workspace with
+// torch's allocator and calls include/embx_dense.h and embx_serving.h on the current stream.  Argument marshalling only.  It is compiled because a small call's time
 // is the host's: 4.4 us with it, of which a launch is 2.6, and 7.1 with the same checks in Python.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -8,14 +8,17 @@
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <optional>
 #include <stdexcept>
 #include <string>
 
 #include "../../include/embx_dense.h"
+#include "../../include/embx_serving.h"
 
 namespace {
 
@@ -60,6 +63,9 @@ Entry<emb_linear_t> g_linear = {"emb_linear", false};
 Entry<emb_linear_grad_t> g_linear_backward = {"emb_linear_backward", true};
 Entry<emb_gated_t> g_gated = {"emb_gated", false};
 Entry<emb_gated_grad_t> g_gated_backward = {"emb_gated_backward", true};
+Entry<emb_linear_int8_t> g_linear_int8 = {"emb_linear_int8", true};
+Entry<emb_moe_t> g_moe = {"emb_moe", true};
+emb_status_t (*g_quantize)(const emb_quantize_t*, void*) = nullptr;
 
 std::string text(PyObject* repr) {
   const char* s = repr ? PyUnicode_AsUTF8(repr) : nullptr;
@@ -81,7 +87,7 @@ int32_t activation(PyObject* name) {
 }
 
 const char* type_name(at::ScalarType t) {
-  return t == at::kFloat ? "torch.float32" : t == at::kHalf ? "torch.float16" : "torch.bfloat16";
+  return t == at::kFloat ? "torch.float32" : t == at::kHalf ? "torch.float16" : t == at::kChar ? "torch.int8" : "torch.bfloat16";
 }
 
 // The calls record nothing for torch's differentiation: a result would lack its gradient without a word.
@@ -108,15 +114,13 @@ struct Common {
   const bool recording = c10::GradMode::is_enabled();
   Matrix at;
 
-  Common(PyObject* o, const char* name) {
+  // eight: 8-bit integers are taken too; type_is() then names the call's type
+  Common(PyObject* o, const char* name, bool eight = false) {
     if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda() || THPVariable_Unpack(o).dim() != 2)
       throw Refused(std::string(name) + " must be a 2-D device tensor");
     first = THPVariable_Unpack(o);
     type = first.scalar_type();
-    if (type == at::kFloat) code = EMB_DTYPE_F32;
-    else if (type == at::kHalf) code = EMB_DTYPE_F16;
-    else if (type == at::kBFloat16) code = EMB_DTYPE_BF16;
-    else throw Refused(std::string(name) + " must be float32, float16 or bfloat16, got " + at::toString(type));
+    if (!(eight && type == at::kChar)) type_is(type, name);
     device = first.get_device();
     if (device != c10::hip::current_device())
       throw Refused(std::string(name) + " is on cuda:" + std::to_string(device) + ", the current device is cuda:" +
@@ -125,13 +129,23 @@ struct Common {
     at = matrix(o, name, rows, cols);
   }
 
-  std::string like() const { return std::string(type_name(type)) + " tensor on cuda:" + std::to_string(device); }
+  void type_is(at::ScalarType t, const char* name) {
+    type = t;
+    if (type == at::kFloat) code = EMB_DTYPE_F32;
+    else if (type == at::kHalf) code = EMB_DTYPE_F16;
+    else if (type == at::kBFloat16) code = EMB_DTYPE_BF16;
+    else throw Refused(std::string(name) + " must be float32, float16 or bfloat16, got " + at::toString(type));
+  }
 
-  Matrix matrix(PyObject* o, const char* name, int64_t r, int64_t c) const {
-    if (!THPVariable_Check(o)) throw Refused(std::string(name) + " must be a 2-D " + like());
+  std::string like(at::ScalarType t) const { return std::string(type_name(t)) + " tensor on cuda:" + std::to_string(device); }
+
+  Matrix matrix(PyObject* o, const char* name, int64_t r, int64_t c) const { return matrix(o, name, r, c, type); }
+
+  Matrix matrix(PyObject* o, const char* name, int64_t r, int64_t c, at::ScalarType type) const {
+    if (!THPVariable_Check(o)) throw Refused(std::string(name) + " must be a 2-D " + like(type));
     const at::Tensor& t = THPVariable_Unpack(o);
     if (!t.is_cuda() || t.get_device() != device || t.scalar_type() != type || t.dim() != 2)
-      throw Refused(std::string(name) + " must be a 2-D " + like());
+      throw Refused(std::string(name) + " must be a 2-D " + like(type));
     if (t.size(0) != r || t.size(1) != c)
       throw Refused(std::string(name) + " must be [" + std::to_string(r) + ", " + std::to_string(c) + "], got [" +
                     std::to_string(t.size(0)) + ", " + std::to_string(t.size(1)) + "]");
@@ -152,7 +166,9 @@ struct Common {
     return o == Py_None ? Matrix{nullptr, 0} : matrix(o, name, r, c);
   }
 
-  void* vector(PyObject* o, const char* name, int64_t n) const {
+  void* vector(PyObject* o, const char* name, int64_t n) const { return vector(o, name, n, type); }
+
+  void* vector(PyObject* o, const char* name, int64_t n, at::ScalarType type) const {
     if (o == Py_None) return nullptr;
     if (THPVariable_Check(o)) {
       const at::Tensor& t = THPVariable_Unpack(o);
@@ -163,7 +179,41 @@ struct Common {
         return t.data_ptr();
       }
     }
-    throw Refused(std::string(name) + " must be a contiguous [" + std::to_string(n) + "] " + like());
+    throw Refused(std::string(name) + " must be a contiguous [" + std::to_string(n) + "] " + like(type));
+  }
+
+  // matrices of all experts, and their scales, if they have any
+  emb_experts_t experts(PyObject* o, const char* name, PyObject* scale, const char* scale_name, int64_t n, int64_t r, int64_t c) const {
+    const at::ScalarType type = scale == Py_None ? this->type : at::kChar;
+    if (!THPVariable_Check(o)) throw Refused(std::string(name) + " must be a 3-D " + like(type));
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.get_device() != device || t.scalar_type() != type || t.dim() != 3)
+      throw Refused(std::string(name) + " must be a 3-D " + like(type));
+    if (t.size(0) != n || t.size(1) != r || t.size(2) != c)
+      throw Refused(std::string(name) + " must be [" + std::to_string(n) + ", " + std::to_string(r) + ", " + std::to_string(c) +
+                    "], got [" + std::to_string(t.size(0)) + ", " + std::to_string(t.size(1)) + ", " + std::to_string(t.size(2)) + "]");
+    if (recording && t.requires_grad()) refuse_gradient(name);
+    if (t.is_neg()) refuse_negated(name);
+    int64_t ld = t.stride(1);
+    if ((t.stride(2) != 1 && c > 1) || (ld < c && r > 1))
+      throw Refused(std::string(name) + " must have contiguous rows that do not overlap, got strides (" + std::to_string(t.stride(0)) +
+                    ", " + std::to_string(ld) + ", " + std::to_string(t.stride(2)) + ")");
+    emb_experts_t w = {t.data_ptr(), std::max(ld, c), n > 1 ? t.stride(0) : 0, nullptr};
+    if (scale != Py_None) {
+      if (THPVariable_Check(scale)) {
+        const at::Tensor& s = THPVariable_Unpack(scale);
+        if (s.is_cuda() && s.get_device() == device && s.scalar_type() == at::kFloat && s.dim() == 2 && s.size(0) == n &&
+            s.size(1) == r && s.is_contiguous()) {
+          if (recording && s.requires_grad()) refuse_gradient(scale_name);
+          if (s.is_neg()) refuse_negated(scale_name);
+          w.scale = static_cast<const float*>(s.data_ptr());
+          return w;
+        }
+      }
+      throw Refused(std::string(scale_name) + " must be a contiguous [" + std::to_string(n) + ", " + std::to_string(r) + "] " +
+                    like(at::kFloat));
+    }
+    return w;
   }
 
   at::Tensor empty(int64_t r, int64_t c) const { return at::empty({r, c}, first.options()); }
@@ -333,6 +383,133 @@ PyObject* gated_backward(PyObject*, Args a, Py_ssize_t count) {
   });
 }
 
+// x, q, scale (both or none: results)
+PyObject* quantize(PyObject*, Args a, Py_ssize_t count) {
+  return guarded(count, 3, [&]() -> PyObject* {
+    const Common c(a[0], "x");
+    const int64_t m = c.rows, k = c.cols;
+    const bool given = a[1] != Py_None || a[2] != Py_None;
+    Matrix q;
+    at::Tensor made_q, made_scale;
+    float* scale;
+    if (given) {
+      if (a[2] == Py_None) throw Refused("out must be a pair of tensors, q and scale");
+      q = c.matrix(a[1], "q", m, k, at::kChar);
+      scale = static_cast<float*>(c.vector(a[2], "scale", m, at::kFloat));
+    } else {
+      const int64_t ld = (k + 15) / 16 * 16;
+      made_q = at::empty({m, ld}, c.first.options().dtype(at::kChar));
+      if (ld != k) made_q = made_q.narrow(1, 0, k);
+      made_scale = at::empty({m}, c.first.options().dtype(at::kFloat));
+      q = {made_q.data_ptr(), ld}, scale = static_cast<float*>(made_scale.data_ptr());
+    }
+    const emb_quantize_t s = {m, k, c.code, c.at.p, c.at.ld, static_cast<int8_t*>(q.p), q.ld, scale};
+    const emb_status_t code = g_quantize(&s, c10::hip::getCurrentHIPStream(c.first.get_device()).stream());
+    if (code != EMB_OK) throw Failed{"emb_quantize", code};
+    if (given) made_q = written(a[1]), made_scale = written(a[2]);
+    return wrap_all(std::optional<at::Tensor>(made_q), std::optional<at::Tensor>(made_scale));
+  });
+}
+
+// x, weight, w_scale, bias, residual, x_scale, activation, dtype, out
+PyObject* linear_int8(PyObject*, Args a, Py_ssize_t count) {
+  return guarded(count, 9, [&]() -> PyObject* {
+    const int32_t act = activation(a[6]);
+    const bool eight = a[5] != Py_None;
+    Common c(a[0], "x", true);
+    if (eight != (c.type == at::kChar))
+      throw Refused(eight ? "x_scale is given: x must be int8" : "x is int8: x_scale must be given");
+    if (a[7] != Py_None) {
+      if (!THPDtype_Check(a[7])) throw Refused("dtype must be a torch.dtype, got " + text(PyObject_Repr(a[7])));
+      const at::ScalarType type = reinterpret_cast<THPDtype*>(a[7])->scalar_type;
+      if (!eight && type != c.type) throw Refused(std::string("dtype must be x's, ") + type_name(c.type));
+      c.type_is(type, "dtype");
+    } else if (eight) {
+      c.type_is(at::kBFloat16, "dtype");
+    }
+    const int64_t m = c.rows, k = c.cols, n = rows_of(a[1], "weight");
+    const Matrix w = c.matrix(a[1], "weight", n, k, at::kChar), r = c.optional(a[4], "residual", m, n);
+    if (a[2] == Py_None) throw Refused("w_scale must be a contiguous [" + std::to_string(n) + "] " + c.like(at::kFloat));
+    const float* ws = static_cast<const float*>(c.vector(a[2], "w_scale", n, at::kFloat));
+    const float* xs = static_cast<const float*>(c.vector(a[5], "x_scale", m, at::kFloat));
+    void* bias = c.vector(a[3], "bias", n);
+    const bool given = a[8] != Py_None;
+    Matrix y;
+    at::Tensor made;
+    if (given) {
+      y = c.matrix(a[8], "out", m, n);
+    } else {
+      made = at::empty({m, n}, c.first.options().dtype(c.type));
+      y = {made.data_ptr(), n};
+    }
+    g_linear_int8({m, n, k, c.code, act, c.at.p, c.at.ld, xs, static_cast<const int8_t*>(w.p), w.ld, ws, bias, r.p, r.ld, y.p, y.ld},
+                  c.first);
+    if (!given) return THPVariable_Wrap(made);
+    written(a[8]);
+    Py_INCREF(a[8]);
+    return a[8];
+  });
+}
+
+// x, router, w_gate, w_up, w_down, top_k, s_gate, s_up, s_down, activation, renormalize, out, routing
+PyObject* moe(PyObject*, Args a, Py_ssize_t count) {
+  return guarded(count, 13, [&]() -> PyObject* {
+    const int32_t act = activation(a[9]);
+    const Common c(a[0], "x");
+    const int64_t m = c.rows, d = c.cols, e = rows_of(a[1], "router");
+    const Matrix router = c.matrix(a[1], "router", e, d);
+    const long top = PyLong_Check(a[5]) ? PyLong_AsLong(a[5]) : -1;
+    PyErr_Clear();
+    if (top < 1 || top > e)
+      throw Refused("top_k must be a whole number from 1 to the experts' " + std::to_string(e) + ", got " + text(PyObject_Repr(a[5])));
+    if (!THPVariable_Check(a[2]) || THPVariable_Unpack(a[2]).dim() != 3) throw Refused("w_gate must be a 3-D device tensor");
+    const int64_t f = THPVariable_Unpack(a[2]).size(1);
+    const bool eight = a[6] != Py_None;
+    if (eight != (a[7] != Py_None) || eight != (a[8] != Py_None)) throw Refused("scales must be of all three matrices, or None");
+    emb_moe_t s = {};
+    s.m = m, s.f = f, s.d = d, s.experts = static_cast<int32_t>(e), s.top_k = static_cast<int32_t>(top);
+    if (e > INT32_MAX) throw Failed{"emb_moe", EMB_ERR_UNSUPPORTED};
+    s.dtype = c.code, s.activation = act, s.renormalize = flag(a[10]);
+    s.x = c.at.p, s.ldx = c.at.ld, s.router = router.p, s.ldr = router.ld;
+    s.gate = c.experts(a[2], "w_gate", a[6], "scales[0]", e, f, d);
+    s.up = c.experts(a[3], "w_up", a[7], "scales[1]", e, f, d);
+    s.down = c.experts(a[4], "w_down", a[8], "scales[2]", e, d, f);
+    const bool given = a[11] != Py_None, routing = flag(a[12]);
+    at::Tensor made;
+    if (given) {
+      const Matrix y = c.matrix(a[11], "out", m, d);
+      s.y = y.p, s.ldy = y.ld;
+    } else {
+      made = c.empty(m, d);
+      s.y = made.data_ptr(), s.ldy = d;
+    }
+    std::optional<at::Tensor> chosen, share;
+    if (routing) {
+      chosen = at::empty({m, top}, c.first.options().dtype(at::kInt));
+      share = at::empty({m, top}, c.first.options().dtype(at::kFloat));
+      s.chosen = static_cast<int32_t*>(chosen->data_ptr()), s.share = static_cast<float*>(share->data_ptr());
+    }
+    g_moe(s, c.first);
+    if (given) made = written(a[11]);
+    if (routing) return wrap_all(std::optional<at::Tensor>(made), chosen, share);
+    if (!given) return THPVariable_Wrap(made);
+    Py_INCREF(a[11]);
+    return a[11];
+  });
+}
+
+// addresses of the library's functions: emb_quantize, then the others, each call and its workspace
+PyObject* bind_serving(PyObject*, PyObject* args) {
+  unsigned long long p[5];
+  if (!PyArg_ParseTuple(args, "(KKKKK)", p, p + 1, p + 2, p + 3, p + 4)) return nullptr;
+  g_quantize = reinterpret_cast<decltype(g_quantize)>(p[0]);
+  g_linear_int8.run = reinterpret_cast<decltype(g_linear_int8.run)>(p[1]);
+  g_linear_int8.size = reinterpret_cast<decltype(g_linear_int8.size)>(p[2]);
+  g_moe.run = reinterpret_cast<decltype(g_moe.run)>(p[3]);
+  g_moe.size = reinterpret_cast<decltype(g_moe.size)>(p[4]);
+  Py_RETURN_NONE;
+}
+
 // (addresses of the library's eight functions, each call and its workspace; the error class; activations)
 PyObject* bind(PyObject*, PyObject* args) {
   unsigned long long p[8];
@@ -359,6 +536,10 @@ PyMethodDef g_methods[] = {{"bind", bind, METH_VARARGS, nullptr},
                            {"linear_backward", method(linear_backward), METH_FASTCALL, nullptr},
                            {"gated", method(gated), METH_FASTCALL, nullptr},
                            {"gated_backward", method(gated_backward), METH_FASTCALL, nullptr},
+                           {"bind_serving", bind_serving, METH_VARARGS, nullptr},
+                           {"quantize", method(quantize), METH_FASTCALL, nullptr},
+                           {"linear_int8", method(linear_int8), METH_FASTCALL, nullptr},
+                           {"moe", method(moe), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_dense", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 

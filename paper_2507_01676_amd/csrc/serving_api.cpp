@@ -1,0 +1,258 @@
+// C entry points of the dense layers' serving forms: argument checks, the layout of the workspace and the launches.  See
+// include/embx_serving.h for the contract.
+#include <algorithm>
+#include <cstdint>
+
+#include "../../include/embx_serving.h"
+#include "dense.hpp"
+#include "serving.hpp"
+
+using namespace embx;
+
+namespace {
+
+constexpr int64_t kMaxSize = int64_t(1) << 30, kMaxStride = int64_t(1) << 40;
+constexpr int64_t kMostInputs = 131071;        // of sums of 8-bit products in 32 bits: 2^14 each
+constexpr int64_t kMostRows = 65536, kMostColumns = int64_t(1) << 26;   // moe
+constexpr size_t kAlign = 256;
+
+#define EMBX_TRY(x)                       \
+  do {                                    \
+    const emb_status_t s_ = (x);          \
+    if (s_ != EMB_OK) return s_;          \
+  } while (0)
+
+size_t esize(int32_t dtype) { return dtype == EMB_DTYPE_F32 ? 4 : 2; }
+
+bool misaligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a != 0; }
+
+emb_status_t check_type(int32_t dtype) {
+  return dtype == EMB_DTYPE_F32 || dtype == EMB_DTYPE_F16 || dtype == EMB_DTYPE_BF16 ? EMB_OK : EMB_ERR_UNSUPPORTED;
+}
+
+emb_status_t check_activation(int32_t act) {
+  return act < EMB_ACT_NONE || act > EMB_ACT_GELU ? EMB_ERR_INVALID_ARGUMENT : EMB_OK;
+}
+
+// a matrix [rows, cols] of elements of `size` bytes that has to be there (unless it has no rows)
+emb_status_t check_matrix(const void* p, int64_t ld, int64_t rows, int64_t cols, size_t size) {
+  if (rows == 0) return EMB_OK;
+  if (!p || misaligned(p, size) || ld < cols) return EMB_ERR_INVALID_ARGUMENT;
+  return ld > kMaxStride ? EMB_ERR_UNSUPPORTED : EMB_OK;
+}
+
+emb_status_t check_vector(const void* p, int64_t n, size_t size) {
+  return n > 0 && (!p || misaligned(p, size)) ? EMB_ERR_INVALID_ARGUMENT : EMB_OK;
+}
+
+emb_status_t check_workspace(const void* ws, size_t have, size_t need) {
+  if (need == 0) return EMB_OK;
+  return !ws || misaligned(ws, kAlign) || have < need ? EMB_ERR_INVALID_ARGUMENT : EMB_OK;
+}
+
+emb_status_t run(int rc) { return rc == 0 ? EMB_OK : EMB_ERR_DEVICE; }
+
+// Hands out the workspace; with a NULL base it only counts.
+struct Arena {
+  char* base;
+  size_t used = 0;
+  template <class P>
+  P* take(size_t bytes) {
+    char* p = base ? base + used : nullptr;
+    used += (bytes + kAlign - 1) / kAlign * kAlign;
+    return reinterpret_cast<P*>(p);
+  }
+};
+
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+
+// Whether the products can read 8-bit rows where they lie, as chunks of 16 bytes (and a tile's offsets fit 32 bits).
+bool whole(const void* p, int64_t ld) { return !misaligned(p, 16) && ld % 16 == 0 && ld <= kMostStride; }
+
+// ---------------------------------------------------------------- linear_int8
+
+emb_status_t check_shape(const emb_linear_int8_t& a) {
+  if (a.m < 0 || a.n < 1 || a.k < 1) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_activation(a.activation));
+  if (a.m > kMaxSize || a.n > kMaxSize || a.k > kMostInputs) return EMB_ERR_UNSUPPORTED;
+  EMBX_TRY(check_type(a.dtype));
+  return a.m > 0 && dense_choose_i8(a.m, a.n, a.k).variant < 0 ? EMB_ERR_UNSUPPORTED : EMB_OK;
+}
+
+// x as the products read it: 8-bit rows that end in zeros up to a whole chunk, so that what lies behind the weights' rows
+// counts for nothing.
+struct Int8Space {
+  DenseChoice choice;
+  bool quantized, packed_x, packed_w;
+  const int8_t *x, *w;
+  int64_t ldx, ldw;
+  const float* scale;
+  float* partial;
+};
+
+Int8Space int8_space(Arena& ar, const emb_linear_int8_t& a) {
+  Int8Space s = {};
+  s.choice = dense_choose_i8(a.m, a.n, a.k);
+  s.quantized = !a.x_scale;
+  s.packed_x = !s.quantized && !(whole(a.x, a.ldx) && a.k % 16 == 0);
+  s.packed_w = !whole(a.weight, a.ldw);
+  s.x = static_cast<const int8_t*>(a.x), s.ldx = a.ldx, s.scale = a.x_scale;
+  s.w = a.weight, s.ldw = a.ldw;
+  if (s.quantized || s.packed_x) s.x = ar.take<int8_t>(a.m * up16(a.k)), s.ldx = up16(a.k);
+  if (s.quantized) s.scale = ar.take<float>(a.m * 4);
+  if (s.packed_w) s.w = ar.take<int8_t>(a.n * up16(a.k)), s.ldw = up16(a.k);
+  if (s.choice.splits > 1) s.partial = ar.take<float>(size_t(s.choice.splits) * a.m * ((a.n + 7) / 8 * 8) * 4);
+  return s;
+}
+
+// a matrix that is copied to rows of whole chunks
+void add_copy(DensePack& p, const void* src, int64_t ld, const void* dst, int64_t rows, int64_t cols) {
+  const int at = p.count++;
+  p.esize = 1;
+  p.src[at] = src, p.lds[at] = ld;
+  p.dst[at] = const_cast<void*>(dst), p.ldd[at] = up16(cols), p.panel[at] = kPanel;
+  p.rows[at] = static_cast<uint32_t>(rows), p.cols[at] = static_cast<uint32_t>(cols);
+  uint32_t wide = 16;
+  while (wide < 256 && wide < cols) wide *= 2;
+  p.wide[at] = wide;
+  p.groups = std::max<int32_t>(p.groups, static_cast<int32_t>(std::min<int64_t>(2048, (rows * wide + 1023) / 1024)));
+}
+
+// ---------------------------------------------------------------- moe
+
+emb_status_t check_experts(const emb_experts_t& w, const emb_moe_t& a, int64_t rows, int64_t cols) {
+  EMBX_TRY(check_matrix(w.p, w.ld, rows, cols, w.scale ? 1 : esize(a.dtype)));
+  EMBX_TRY(check_vector(w.scale, w.scale ? 1 : 0, 4));
+  if (w.stride < 0) return EMB_ERR_INVALID_ARGUMENT;
+  return w.stride > kMaxStride ? EMB_ERR_UNSUPPORTED : EMB_OK;
+}
+
+emb_status_t check_shape(const emb_moe_t& a) {
+  if (a.m < 0 || a.f < 1 || a.d < 1 || a.experts < 1 || a.top_k < 1 || a.top_k > a.experts) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_activation(a.activation));
+  if (!a.gate.scale != !a.up.scale || !a.gate.scale != !a.down.scale) return EMB_ERR_INVALID_ARGUMENT;
+  if (a.m > kMostRows || a.f > kMostColumns || a.d > kMostColumns) return EMB_ERR_UNSUPPORTED;
+  if (a.experts > kMostExperts || a.top_k > kMostTopK) return EMB_ERR_UNSUPPORTED;
+  return check_type(a.dtype);
+}
+
+struct MoeSpace {
+  void* h;
+  int64_t ldh;
+  int32_t* chosen;
+  float* share;
+};
+
+MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
+  const int64_t uses = a.m * a.top_k;
+  MoeSpace s = {nullptr, (a.f + 7) / 8 * 8, a.chosen, a.share};
+  s.h = ar.take<void>(uses * s.ldh * esize(a.dtype));
+  if (!s.chosen) s.chosen = ar.take<int32_t>(uses * 4);
+  if (!s.share) s.share = ar.take<float>(uses * 4);
+  return s;
+}
+
+}  // namespace
+
+extern "C" {
+
+emb_status_t emb_quantize(const emb_quantize_t* a, void* stream) {
+  if (!a || a->m < 0 || a->k < 1) return EMB_ERR_INVALID_ARGUMENT;
+  if (a->m > kMaxSize || a->k > kMaxSize) return EMB_ERR_UNSUPPORTED;
+  EMBX_TRY(check_type(a->dtype));
+  EMBX_TRY(check_matrix(a->x, a->ldx, a->m, a->k, esize(a->dtype)));
+  EMBX_TRY(check_matrix(a->q, a->ldq, a->m, a->k, 1));
+  EMBX_TRY(check_vector(a->scale, a->m, 4));
+  if (a->m == 0) return EMB_OK;
+  return run(quantize_launch(a->dtype, {a->x, a->q, a->scale, a->ldx, a->ldq, a->m, static_cast<int32_t>(a->k),
+                                        static_cast<int32_t>(a->k)}, stream));
+}
+
+emb_status_t emb_linear_int8_workspace(const emb_linear_int8_t* a, size_t* bytes) {
+  if (!a || !bytes) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_shape(*a));
+  Arena ar{nullptr};
+  if (a->m > 0) int8_space(ar, *a);
+  *bytes = ar.used;
+  return EMB_OK;
+}
+
+emb_status_t emb_linear_int8(const emb_linear_int8_t* a, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!a) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_shape(*a));
+  EMBX_TRY(check_matrix(a->x, a->ldx, a->m, a->k, a->x_scale ? 1 : esize(a->dtype)));
+  EMBX_TRY(check_vector(a->x_scale, a->x_scale ? 1 : 0, 4));
+  EMBX_TRY(check_matrix(a->weight, a->ldw, a->n, a->k, 1));
+  EMBX_TRY(check_vector(a->w_scale, a->n, 4));
+  EMBX_TRY(check_vector(a->bias, a->bias ? 1 : 0, esize(a->dtype)));
+  if (a->residual) EMBX_TRY(check_matrix(a->residual, a->ldr, a->m, a->n, esize(a->dtype)));
+  EMBX_TRY(check_matrix(a->y, a->ldy, a->m, a->n, esize(a->dtype)));
+  if (a->m == 0) return EMB_OK;
+  Arena ar{static_cast<char*>(workspace)};
+  const Int8Space s = int8_space(ar, *a);
+  EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
+  DensePack pack = {};
+  if (s.packed_x) add_copy(pack, a->x, a->ldx, s.x, a->m, a->k);
+  if (s.packed_w) add_copy(pack, a->weight, a->ldw, s.w, a->n, a->k);
+  if (pack.count) EMBX_TRY(run(dense_pack_launch(pack, stream)));
+  if (s.quantized)
+    EMBX_TRY(run(quantize_launch(a->dtype, {a->x, const_cast<int8_t*>(s.x), const_cast<float*>(s.scale), a->ldx, s.ldx, a->m,
+                                            static_cast<int32_t>(a->k), static_cast<int32_t>(s.ldx)}, stream)));
+  DenseGemm g = {};
+  g.a[0] = s.x, g.lda = s.ldx, g.panel_a = kPanel;
+  g.b[0] = s.w, g.ldb[0] = s.ldw, g.panel_b[0] = kPanel;
+  g.c[0] = a->y, g.ldc[0] = a->ldy;
+  g.bias[0] = a->bias;
+  g.res = a->residual, g.ldr = a->ldr;
+  g.scale_a = s.scale, g.scale_b = a->w_scale;
+  g.result = a->dtype == EMB_DTYPE_F32 ? kDenseF32 : a->dtype == EMB_DTYPE_F16 ? kDenseF16 : kDenseBF16;
+  g.ni = static_cast<int32_t>(a->m), g.nj = static_cast<int32_t>(a->n), g.nr = static_cast<int32_t>(a->k);
+  g.act = a->activation, g.parts = 1, g.whole = 1;
+  g.variant = s.choice.variant, g.splits = g.slots = s.choice.splits, g.row_blocks = s.choice.row_blocks;
+  g.partial = s.partial;
+  return run(dense_forward_i8(g, stream));
+}
+
+emb_status_t emb_moe_workspace(const emb_moe_t* a, size_t* bytes) {
+  if (!a || !bytes) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_shape(*a));
+  Arena ar{nullptr};
+  if (a->m > 0) moe_space(ar, *a);
+  *bytes = ar.used;
+  return EMB_OK;
+}
+
+emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!a) return EMB_ERR_INVALID_ARGUMENT;
+  EMBX_TRY(check_shape(*a));
+  EMBX_TRY(check_matrix(a->x, a->ldx, a->m, a->d, esize(a->dtype)));
+  EMBX_TRY(check_matrix(a->router, a->ldr, a->experts, a->d, esize(a->dtype)));
+  EMBX_TRY(check_experts(a->gate, *a, a->f, a->d));
+  EMBX_TRY(check_experts(a->up, *a, a->f, a->d));
+  EMBX_TRY(check_experts(a->down, *a, a->d, a->f));
+  EMBX_TRY(check_matrix(a->y, a->ldy, a->m, a->d, esize(a->dtype)));
+  EMBX_TRY(check_vector(a->chosen, a->chosen ? 1 : 0, 4));
+  EMBX_TRY(check_vector(a->share, a->share ? 1 : 0, 4));
+  if (a->m == 0) return EMB_OK;
+  Arena ar{static_cast<char*>(workspace)};
+  const MoeSpace s = moe_space(ar, *a);
+  EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
+  Moe g = {};
+  g.x = a->x, g.ldx = a->ldx, g.router = a->router, g.ldr = a->ldr;
+  int i = 0;
+  for (const emb_experts_t* w : {&a->gate, &a->up, &a->down}) {
+    g.w[i] = w->p, g.ldw[i] = w->ld, g.stride[i] = w->stride, g.scale[i] = w->scale;
+    ++i;
+  }
+  g.h = s.h, g.ldh = s.ldh, g.chosen = s.chosen, g.share = s.share;
+  g.y = a->y, g.ldy = a->ldy;
+  g.m = static_cast<int32_t>(a->m), g.f = static_cast<int32_t>(a->f), g.d = static_cast<int32_t>(a->d);
+  g.experts = a->experts, g.top_k = a->top_k, g.act = a->activation, g.renormalize = a->renormalize != 0;
+  switch (a->dtype) {
+    case EMB_DTYPE_F32: return run(moe_launch_f32(g, stream));
+    case EMB_DTYPE_F16: return run(moe_launch_f16(g, stream));
+    default: return run(moe_launch_bf16(g, stream));
+  }
+}
+
+}  // extern "C"
