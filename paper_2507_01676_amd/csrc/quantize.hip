@@ -10,48 +10,197 @@
 namespace embx {
 namespace {
 
-// x / s to the nearest whole number, half to even, exactly: the product with the rounded reciprocal is off by less than one
-// of the nearest, and what is left of x after it, x - r s, is exact near the borders (a multiple of the smaller operand's
-// last place, and at most s), so that a comparison with s / 2 mends it.
-__device__ inline float nearest(float x, float s, float inverse) {
-  float r = rintf(x * inverse);
-  const float left = 2.0f * fmaf(-r, s, x);
-  const float one = copysignf(1.0f, left);
-  if (fabsf(left) > s || (fabsf(left) == s && fabsf(rintf(r * 0.5f) * 2.0f - r) == 1.0f)) r += one;
-  return r;
+typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x8 __attribute__((ext_vector_type(8)));
+
+// Eight consecutive elements as their bits.
+template <int TYPE> struct Eight { using V = u16x8; };
+template <> struct Eight<kDenseF32> { using V = u32x8; };
+
+template <int TYPE>
+__device__ inline float value(uint32_t bits) {
+  if constexpr (TYPE == kDenseF32) return __uint_as_float(bits);
+  else if constexpr (TYPE == kDenseBF16) return __uint_as_float(bits << 16);
+  else return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(bits)));
+}
+
+constexpr float kRound = 0x1.8p23f;   // a float with this added has its whole part, rounded half to even, in its low bits
+
+// A row's scale from the largest of its magnitudes' bits; false where that is an infinity or NaN.
+struct Scale {
+  float s, inverse;
+  bool fine;
+
+  template <int TYPE>
+  __device__ static Scale of(uint32_t largest) {
+    Scale r;
+    const float most = value<TYPE>(largest);
+    r.fine = most < __builtin_inff();   // (NaN is not)
+    r.s = r.fine ? fmaxf(most / 127.0f, 0x1p-126f) : 1.0f;
+    r.inverse = 1.0f / r.s;
+    return r;
+  }
+
+  __device__ float stored() const { return fine ? s : __builtin_nanf(""); }
+
+  // x / s to the nearest whole number, half to even, exactly, in the low 8 bits of the result: x times the rounded
+  // reciprocal is off by less than one of the nearest, and what is left of x after it, x - r s, is exact near the borders
+  // (a multiple of the smaller operand's last place, and at most s).  *far: whether that is s / 2 or more, for mend().
+  __device__ uint32_t nearest(float x, bool* far) const {
+    const float u = fmaf(x, inverse, kRound), left = fmaf(kRound - u, s, x);
+    *far |= fabsf(left + left) >= s;
+    return __float_as_uint(u);
+  }
+
+  __device__ uint32_t mend(float x) const {
+    float u = fmaf(x, inverse, kRound);
+    const float left = fmaf(kRound - u, s, x), twice = fabsf(left + left);
+    if (twice > s || (twice == s && (__float_as_uint(u) & 1))) u += copysignf(1.0f, left);
+    return __float_as_uint(u);
+  }
+};
+
+// of LANES threads of a workgroup of 256
+template <int LANES>
+__device__ inline uint32_t most_of(uint32_t v) {
+  for (int step = (LANES < 64 ? LANES : 64) / 2; step > 0; step >>= 1)
+    v = max(v, static_cast<uint32_t>(__shfl_xor(static_cast<int>(v), step)));
+  if constexpr (LANES == 256) {
+    __shared__ uint32_t most[4];
+    __syncthreads();   // (the last row's are read)
+    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = max(max(most[0], most[1]), max(most[2], most[3]));
+  }
+  return v;
+}
+
+// A row in the registers of LANES threads, CH chunks of eight elements each: read once, 16 bytes at a time, and bound by
+// memory.  x's rows start at multiples of 16 bytes, q's at multiples of 8.
+template <int TYPE, int LANES, int CH>
+__global__ __launch_bounds__(256) void quantize_held(Quantize a) {
+  using V = typename Eight<TYPE>::V;
+  constexpr int kRows = 256 / LANES;
+  constexpr uint32_t kSign = TYPE == kDenseF32 ? 0x7fffffffu : 0x7fffu;
+  const int lane = threadIdx.x % LANES;
+  const int chunks = (a.k + 7) / 8, wide = (a.padded + 7) / 8;
+  for (int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; i < a.m; i += int64_t(gridDim.x) * kRows) {
+    const char* const x = static_cast<const char*>(a.x) + i * a.ldx * (TYPE == kDenseF32 ? 4 : 2);
+    V v[CH], most = {};
+#pragma unroll
+    for (int c = 0; c < CH; ++c) v[c] = reinterpret_cast<const V*>(x)[min(lane + c * LANES, chunks - 1)];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int at = lane + c * LANES;
+      if (at >= chunks - 1) {   // what is behind the row's end counts as zeros
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (at * 8 + e >= a.k) v[c][e] = 0;
+      }
+      most = __builtin_elementwise_max(most, v[c] & static_cast<decltype(most[0] + 0)>(kSign));
+    }
+    uint32_t largest = most[0];
+#pragma unroll
+    for (int e = 1; e < 8; ++e) largest = max(largest, static_cast<uint32_t>(most[e]));
+    const Scale s = Scale::of<TYPE>(most_of<LANES>(largest));
+    if (lane == 0) a.scale[i] = s.stored();
+    int8_t* const q = a.q + i * a.ldq;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int at = lane + c * LANES;
+      uint32_t u[8];
+      bool far = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u[e] = s.nearest(value<TYPE>(v[c][e]), &far);
+      if (__any(far)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = s.mend(value<TYPE>(v[c][e]));
+      }
+      u32x2 out;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        out[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[4 * h + 3], u[4 * h + 2], 0x0c0c0400),
+                                       __builtin_amdgcn_perm(u[4 * h + 1], u[4 * h], 0x0c0c0400), 0x05040100);
+      if (!s.fine) out = u32x2{0, 0};
+      if (at * 8 + 8 <= a.padded) {
+        *reinterpret_cast<u32x2*>(q + at * 8) = out;
+      } else if (at < wide) {
+        for (int e = 0; e < a.padded - at * 8; ++e) q[at * 8 + e] = static_cast<int8_t>(out[e >> 2] >> 8 * (e & 3));
+      }
+    }
+  }
+}
+
+// Any rows: read twice, consecutive elements by consecutive threads.
+template <int TYPE, int LANES>
+__global__ __launch_bounds__(256) void quantize_any(Quantize a) {
+  using T = typename Elem<TYPE>::T;
+  constexpr int kRows = 256 / LANES, kMany = 8;   // elements of a thread under way
+  const int lane = threadIdx.x % LANES;
+  for (int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; i < a.m; i += int64_t(gridDim.x) * kRows) {
+    const T* const x = static_cast<const T*>(a.x) + i * a.ldx;
+    uint32_t largest = 0;
+    for (int j = lane; j < a.k; j += LANES * kMany) {
+      T v[kMany];
+#pragma unroll
+      for (int e = 0; e < kMany; ++e) v[e] = x[min(j + e * LANES, a.k - 1)];
+#pragma unroll
+      for (int e = 0; e < kMany; ++e) largest = max(largest, __float_as_uint(float(v[e])) & 0x7fffffffu);
+    }
+    const Scale s = Scale::of<kDenseF32>(most_of<LANES>(largest));
+    if (lane == 0) a.scale[i] = s.stored();
+    int8_t* const q = a.q + i * a.ldq;
+    for (int j = lane; j < a.padded; j += LANES * kMany) {
+      T v[kMany];
+#pragma unroll
+      for (int e = 0; e < kMany; ++e) v[e] = x[min(j + e * LANES, a.k - 1)];
+#pragma unroll
+      for (int e = 0; e < kMany; ++e)
+        if (j + e * LANES < a.padded)
+          q[j + e * LANES] = j + e * LANES < a.k && s.fine ? static_cast<int8_t>(s.mend(float(v[e]))) : int8_t(0);
+    }
+  }
+}
+
+template <int TYPE, int LANES, int CH>
+int held(const Quantize& a, hipStream_t s) {
+  const int64_t groups = (a.m + 256 / LANES - 1) / (256 / LANES);
+  quantize_held<TYPE, LANES, CH><<<static_cast<uint32_t>(std::min<int64_t>(groups, 1 << 20)), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+template <int TYPE, int LANES>
+int any(const Quantize& a, hipStream_t s) {
+  const int64_t groups = (a.m + 256 / LANES - 1) / (256 / LANES);
+  quantize_any<TYPE, LANES><<<static_cast<uint32_t>(std::min<int64_t>(groups, 1 << 20)), 256, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(256) void quantize_rows(Quantize a) {
-  using T = typename Elem<TYPE>::T;
-  __shared__ uint32_t most[4];
-  for (int64_t i = blockIdx.x; i < a.m; i += gridDim.x) {
-    const T* const x = static_cast<const T*>(a.x) + i * a.ldx;
-    uint32_t largest = 0;
-    for (int j = threadIdx.x; j < a.k; j += 256) largest = max(largest, __float_as_uint(float(x[j])) & 0x7fffffffu);
-    for (int step = 32; step > 0; step >>= 1) largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), step)));
-    if ((threadIdx.x & 63) == 0) most[threadIdx.x >> 6] = largest;
-    __syncthreads();
-    largest = max(max(most[0], most[1]), max(most[2], most[3]));
-    const bool fine = largest < 0x7f800000u;
-    const float s = fmaxf(__uint_as_float(largest) / 127.0f, 0x1p-126f), inverse = 1.0f / s;
-    if (threadIdx.x == 0) a.scale[i] = fine ? s : __uint_as_float(0x7fc00000u);
-    int8_t* const q = a.q + i * a.ldq;
-    for (int j = threadIdx.x; j < a.padded; j += 256)
-      q[j] = j < a.k && fine ? static_cast<int8_t>(nearest(float(x[j]), s, inverse)) : 0;
-    __syncthreads();
-  }
+int launch(const Quantize& a, hipStream_t s) {
+  constexpr int kSize = TYPE == kDenseF32 ? 4 : 2;
+  const bool whole = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * kSize % 16 == 0 &&
+                     reinterpret_cast<uintptr_t>(a.q) % 8 == 0 && a.ldq % 8 == 0 && a.ldx >= (a.k + 7) / 8 * 8;
+  const int chunks = std::max(a.k, a.padded) <= 16384 ? (std::max(a.k, a.padded) + 7) / 8 : 0;
+  if (!whole || chunks == 0) return a.k <= 128 ? any<TYPE, 16>(a, s) : a.k <= 2048 ? any<TYPE, 64>(a, s) : any<TYPE, 256>(a, s);
+  if (chunks <= 8) return held<TYPE, 8, 1>(a, s);
+  if (chunks <= 16) return held<TYPE, 16, 1>(a, s);
+  if (chunks <= 32) return held<TYPE, 32, 1>(a, s);
+  if (chunks <= 64) return held<TYPE, 64, 1>(a, s);
+  if (chunks <= 128) return held<TYPE, 64, 2>(a, s);
+  if (chunks <= 256) return a.m >= 1024 ? held<TYPE, 64, 4>(a, s) : held<TYPE, 256, 1>(a, s);
+  if (chunks <= 512) return held<TYPE, 256, 2>(a, s);
+  if (chunks <= 1024) return held<TYPE, 256, 4>(a, s);
+  return held<TYPE, 256, 8>(a, s);
 }
 
 }  // namespace
 
 int quantize_launch(int dtype, const Quantize& a, void* stream) {
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  const uint32_t grid = static_cast<uint32_t>(std::min<int64_t>(a.m, 65536));
-  if (dtype == EMB_DTYPE_F32) quantize_rows<kDenseF32><<<grid, 256, 0, s>>>(a);
-  else if (dtype == EMB_DTYPE_F16) quantize_rows<kDenseF16><<<grid, 256, 0, s>>>(a);
-  else quantize_rows<kDenseBF16><<<grid, 256, 0, s>>>(a);
-  return hipGetLastError();
+  if (dtype == EMB_DTYPE_F32) return launch<kDenseF32>(a, s);
+  return dtype == EMB_DTYPE_F16 ? launch<kDenseF16>(a, s) : launch<kDenseBF16>(a, s);
 }
 
 }  // namespace embx

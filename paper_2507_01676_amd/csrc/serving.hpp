@@ -23,13 +23,20 @@ struct Moe {
   const void* router;
   const void* w[3];
   const float* scale[3];   // 8-bit matrices, or NULL
-  void* h;                 // [m * top_k][ldh]: act(gate) * up of each row's experts
+  void* h;                 // [2][m * top_k][ldh]: act(gate) * up of each row's experts, and (16 bits) what rounding left
   void* y;
   int32_t* chosen;         // [m][top_k]
   float* share;            // [m][top_k]
   int64_t ldx, ldr, ldh, ldy, ldw[3], stride[3];
+  float* partial;          // [splits][m][d], with splits > 1
   int32_t m, f, d, experts, top_k, act, renormalize;
+  int32_t variant;         // MoeVariant
+  int32_t whole;           // rows of all operands start at multiples of 16 bytes
+  int32_t splits, split_step;   // parts of the down projection's reduction, and their length
 };
+
+// By how many rows of x an expert is expected to have: at most 4, 8 or 16 at a time, or 64.
+enum MoeVariant { kMoeFew = 0, kMoeSome = 1, kMoeMore = 2, kMoeMany = 3 };
 
 constexpr int kMostExperts = 1024, kMostTopK = 32;
 

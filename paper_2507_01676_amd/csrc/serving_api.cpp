@@ -136,17 +136,34 @@ emb_status_t check_shape(const emb_moe_t& a) {
   return check_type(a.dtype);
 }
 
+// Rows that start at multiples of 16 bytes
+bool aligned(const void* p, int64_t ld, size_t size) { return !misaligned(p, 16) && ld * static_cast<int64_t>(size) % 16 == 0; }
+
+bool aligned(const emb_experts_t& w, size_t size) {
+  return aligned(w.p, w.ld, w.scale ? 1 : size) && aligned(w.p, w.stride, w.scale ? 1 : size);
+}
+
 struct MoeSpace {
   void* h;
   int64_t ldh;
   int32_t* chosen;
   float* share;
+  float* partial;
+  int32_t variant, splits, split_step;
 };
 
 MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   const int64_t uses = a.m * a.top_k;
   MoeSpace s = {nullptr, (a.f + 7) / 8 * 8, a.chosen, a.share};
-  s.h = ar.take<void>(uses * s.ldh * esize(a.dtype));
+  s.variant = a.m <= 4 ? kMoeFew : a.m <= 8 ? kMoeSome : uses <= 12 * a.experts ? kMoeMore : kMoeMany;
+  // enough workgroups of the down projection to fill the GPU, each with some steps of its eight wavefronts
+  const int64_t cols = s.variant >= kMoeMore ? 32 : 4, rows = std::min<int64_t>(64, 512 / a.top_k);
+  const int64_t groups = (a.d + cols - 1) / cols * ((a.m + rows - 1) / rows);
+  const int64_t splits = s.variant >= kMoeMore ? std::min<int64_t>(std::min<int64_t>(16, a.f / 512), 512 / groups) : 1;
+  s.split_step = static_cast<int32_t>((a.f + std::max<int64_t>(1, splits) - 1) / std::max<int64_t>(1, splits) + 127) / 128 * 128;
+  s.splits = static_cast<int32_t>((a.f + s.split_step - 1) / s.split_step);
+  if (s.splits > 1) s.partial = ar.take<float>(s.splits * a.m * a.d * 4);
+  s.h = ar.take<void>(2 * uses * s.ldh * esize(a.dtype));
   if (!s.chosen) s.chosen = ar.take<int32_t>(uses * 4);
   if (!s.share) s.share = ar.take<float>(uses * 4);
   return s;
@@ -245,6 +262,10 @@ emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes
     ++i;
   }
   g.h = s.h, g.ldh = s.ldh, g.chosen = s.chosen, g.share = s.share;
+  g.partial = s.partial, g.variant = s.variant, g.splits = s.splits, g.split_step = s.split_step;
+  const size_t size = esize(a->dtype);
+  g.whole = aligned(a->x, a->ldx, size) && aligned(a->router, a->ldr, size) && aligned(a->gate, size) && aligned(a->up, size) &&
+            aligned(a->down, size);
   g.y = a->y, g.ldy = a->ldy;
   g.m = static_cast<int32_t>(a->m), g.f = static_cast<int32_t>(a->f), g.d = static_cast<int32_t>(a->d);
   g.experts = a->experts, g.top_k = a->top_k, g.act = a->activation, g.renormalize = a->renormalize != 0;
