@@ -46,8 +46,8 @@
  * experts, an unknown activation, scales of some of the experts' matrices only, or a workspace
  * that is NULL or too small; EMB_ERR_UNSUPPORTED for an unknown type, m or n above 2^30,
  * a stride above 2^40, linear_int8's k above 131071 (its sums have to fit 32 bits) and
- * quantize's above 2^30, experts above 1024, top_k above 32, moe's m above 65536 and its f or
- * d above 2^26, or a product too large for a launch; EMB_ERR_DEVICE if a launch fails.  With
+ * quantize's above 2^30, experts above 1024, top_k above 32, moe's m above 65536, its f, d or
+ * experts' row strides above 2^25, or a product too large for a launch; EMB_ERR_DEVICE if a launch fails.  With
  * m == 0 calls do nothing.
  */
 #ifndef EMBX_SERVING_H

@@ -32,108 +32,93 @@ __device__ inline uint64_t order_of(double v) {
   return b >> 63 ? ~b : b | uint64_t(1) << 63;
 }
 
-// A row's 16 bytes at element `at` of n: eight elements, or 16 of 8 bits.  Where rows start at multiples of 16 bytes (WHOLE)
-// the last ones are read whole; what lies behind the row's end counts as zeros.
-template <int TYPE>
-struct Piece {
-  using T = typename Elem<TYPE>::T;
-  float v[TYPE == kDenseF32 ? 8 : 1];
-  s16x8 h;
+// Consecutive elements of SIZE bytes of a row, WORDS * 4 bytes in all.
+template <int SIZE, int WORDS>
+struct Chunk {
+  u32x4 v[WORDS / 4];
+  static constexpr int kPer = WORDS * 4 / SIZE, kPer16 = 16 / SIZE;
 
-  __device__ void set(const T* x) {
-    if constexpr (TYPE == kDenseF32) {
+  template <bool WHOLE>
+  __device__ void load(const char* p) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = x[e];
-    } else {
-      __builtin_memcpy(&h, x, 16);
+    for (int h = 0; h < WORDS / 4; ++h) {
+      if constexpr (WHOLE) v[h] = *reinterpret_cast<const u32x4*>(p + 16 * h);
+      else __builtin_memcpy(&v[h], p + 16 * h, 16);
     }
   }
 
+  // elements at .. of a row of n: what is behind its end is something else.  Where rows start at multiples of 16 bytes (WHOLE)
+  // their last 16 bytes are read whole.
+  template <bool WHOLE>
+  __device__ void load_end(const char* row, int at, int n) {
+#pragma unroll
+    for (int h = 0; h < WORDS / 4; ++h) {
+      if constexpr (WHOLE) {
+        v[h] = *reinterpret_cast<const u32x4*>(row + int64_t(min(at + h * kPer16, (n - 1) / kPer16 * kPer16)) * SIZE);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[h][i] = 0;
+          using E = std::conditional_t<SIZE == 1, uint8_t, std::conditional_t<SIZE == 2, uint16_t, uint32_t>>;
+#pragma unroll
+          for (int e = 0; e < 4 / SIZE; ++e)
+            v[h][i] |= uint32_t(reinterpret_cast<const E*>(row)[min(at + h * kPer16 + i * (4 / SIZE) + e, n - 1)]) << 8 * SIZE * e;
+        }
+      }
+    }
+  }
+
+  // keeps `left` elements, zeros behind them
+  __device__ void keep(int left) {
+#pragma unroll
+    for (int h = 0; h < WORDS / 4; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int bytes = left * SIZE - (h * 4 + i) * 4;
+        v[h][i] = bytes >= 4 ? v[h][i] : bytes <= 0 ? 0 : v[h][i] & ((1u << 8 * bytes) - 1);
+      }
+  }
+};
+
+template <int TYPE>
+struct Piece : Chunk<TYPE == kDenseF32 ? 4 : 2, TYPE == kDenseF32 ? 8 : 4> {   // eight elements
   __device__ float get(int e) const {
-    if constexpr (TYPE == kDenseF32) return v[e];
-    else if constexpr (TYPE == kDenseBF16) return __uint_as_float(uint32_t(static_cast<uint16_t>(h[e])) << 16);
-    else return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<short>(h[e])));
-  }
-
-  // FULL: all of it is inside
-  template <bool WHOLE, bool FULL>
-  __device__ void load(const T* row, int at, int n) {
-    T x[8];
-    if constexpr (FULL) {
-      if constexpr (WHOLE) __builtin_memcpy(x, __builtin_assume_aligned(row + at, 16), sizeof(x));
-      else __builtin_memcpy(x, row + at, sizeof(x));
-    } else if constexpr (WHOLE) {
-      constexpr int kPer = 16 / sizeof(T);   // (f32: two chunks, of which the second may be outside)
-      const int last = (n - 1) / kPer * kPer;
-#pragma unroll
-      for (int c = 0; c < 8; c += kPer) __builtin_memcpy(x + c, __builtin_assume_aligned(row + min(at + c, last), 16), 16);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = at + e < n ? x[e] : T(0.0f);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = row[min(at + e, n - 1)];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] = at + e < n ? x[e] : T(0.0f);
-    }
-    set(x);
+    if constexpr (TYPE == kDenseF32) return __uint_as_float(this->v[e / 4][e % 4]);
+    const uint32_t word = this->v[0][e / 2 % 4];
+    if constexpr (TYPE == kDenseBF16) return __uint_as_float(e % 2 ? word & 0xffff0000u : word << 16);
+    return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(e % 2 ? word >> 16 : word)));
   }
 };
 
-// The same of an expert's matrix, whose elements may have 8 bits (EIGHT): whole numbers, exact in every type.
+// The same of an expert's matrix, whose elements may have 8 bits (EIGHT): 16 whole numbers, exact in every type.
 template <int TYPE, bool EIGHT>
-struct Weights {
-  using W = typename Elem<TYPE>::T;
-  static constexpr int kPieces = 1, kPer = 8;
-  Piece<TYPE> p;
-
-  template <bool WHOLE, bool FULL>
-  __device__ void load(const W* row, int at, int n) { p.template load<WHOLE, FULL>(row, at, n); }
-
-  __device__ const Piece<TYPE>& piece(int) const { return p; }
+struct Weights : Piece<TYPE> {
+  static constexpr int kSize = TYPE == kDenseF32 ? 4 : 2, kPieces = 1;
+  __device__ const Piece<TYPE>& piece(int) const { return *this; }
 };
 
 template <int TYPE>
-struct Weights<TYPE, true> {
-  using W = int8_t;
-  static constexpr int kPieces = 2, kPer = 16;
-  u32x4 b;
-
-  template <bool WHOLE, bool FULL>
-  __device__ void load(const W* row, int at, int n) {
-    if constexpr (FULL && !WHOLE) {
-      __builtin_memcpy(&b, row + at, 16);
-    } else if constexpr (WHOLE) {
-      b = *reinterpret_cast<const u32x4*>(row + (FULL ? at : min(at, (n - 1) / 16 * 16)));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        b[e] = 0;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) b[e] |= uint32_t(static_cast<uint8_t>(row[min(at + 4 * e + x, n - 1)])) << 8 * x;
-      }
-    }
-    if constexpr (!FULL) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int left = n - at - 4 * e;   // bytes of this word that are inside
-        b[e] = left >= 4 ? b[e] : left <= 0 ? 0 : b[e] & ((1u << 8 * left) - 1);
-      }
-    }
-  }
+struct Weights<TYPE, true> : Chunk<1, 4> {
+  static constexpr int kSize = 1, kPieces = 2;
 
   __device__ Piece<TYPE> piece(int i) const {
     Piece<TYPE> out;
-    u32x4 pairs;
+    uint32_t words[2] = {this->v[0][2 * i], this->v[0][2 * i + 1]};
+    // (keeps the compiler from taking the bytes apart where they are loaded, a register each)
+    asm("" : "+v"(words[0]), "+v"(words[1]));
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
-      const uint32_t word = b[2 * i + e / 4];
+      const uint32_t word = words[e / 4];
       const float lo = static_cast<float>(static_cast<int8_t>(word >> 8 * (e & 3)));
-      const float hi = static_cast<float>(static_cast<int8_t>(word >> 8 * (e & 3) + 8));
-      if constexpr (TYPE == kDenseF32) out.v[e] = lo, out.v[e + 1] = hi;
-      else if constexpr (TYPE == kDenseBF16) pairs[e / 2] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);
-      else pairs[e / 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+      const float hi = static_cast<float>(static_cast<int8_t>(word >> (8 * (e & 3) + 8)));
+      if constexpr (TYPE == kDenseF32) {
+        out.v[e / 4][e % 4] = __float_as_uint(lo), out.v[e / 4][e % 4 + 1] = __float_as_uint(hi);
+      } else if constexpr (TYPE == kDenseBF16) {
+        out.v[0][e / 2] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302);   // (the rest is zeros)
+      } else {
+        out.v[0][e / 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(lo, hi));
+      }
     }
-    if constexpr (TYPE != kDenseF32) out.h = __builtin_bit_cast(s16x8, pairs);
     return out;
   }
 };
@@ -142,79 +127,117 @@ template <int TYPE>
 __device__ inline f32x4 product(const Piece<TYPE>& w, const Piece<TYPE>& x, f32x4 c) {
   if constexpr (TYPE == kDenseF32) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[e], x.v[e], c, 0, 0, 0);
+    for (int e = 0; e < 8; ++e)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.v[e / 4][e % 4]), __uint_as_float(x.v[e / 4][e % 4]), c, 0, 0, 0);
     return c;
   } else {
-    return mfma16<TYPE>(w.h, x.h, c);
+    return mfma16<TYPE>(__builtin_bit_cast(s16x8, w.v[0]), __builtin_bit_cast(s16x8, x.v[0]), c);
   }
 }
 
-// A workgroup takes a row: a wavefront four experts' logits at a time, summed in 64 bits, then the first one the choice.
-template <int TYPE, bool WHOLE>
-__global__ __launch_bounds__(512) void moe_route(Moe a) {
+// What the router works out of some rows of x, in LDS: up to DOTS logits.
+template <int DOTS>
+struct Routing {
+  double logit[DOTS];
+  uint64_t key[DOTS];
+  int chosen[DOTS];    // [rows][top_k], as shares
+  float share[DOTS];
+};
+
+// MANY logits at a time in a wavefront, summed in 64 bits.
+template <int TYPE, bool WHOLE, int MANY, int DOTS>
+__device__ inline void logits(const Moe& a, int first_row, int rows, Routing<DOTS>& out, int wave, int lane) {
   using T = typename Elem<TYPE>::T;
-  __shared__ double logit[kMostExperts];
-  __shared__ uint64_t key[kMostExperts];
-  constexpr int kMany = 4;
-  const int64_t i = blockIdx.x;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const T* const x = static_cast<const T*>(a.x) + i * a.ldx;
-  for (int first = wave; first < a.experts; first += 8 * kMany) {
-    const T* r[kMany];
-    double sum[kMany] = {};
+  const int dots = rows * a.experts;
+  for (int first = wave; first < dots; first += 8 * MANY) {
+    const T *r[MANY], *x[MANY];
+    double sum[MANY] = {};
 #pragma unroll
-    for (int n = 0; n < kMany; ++n) r[n] = static_cast<const T*>(a.router) + int64_t(min(first + n * 8, a.experts - 1)) * a.ldr;
+    for (int n = 0; n < MANY; ++n) {
+      const int dot = min(first + n * 8, dots - 1), row = dot / a.experts;
+      r[n] = static_cast<const T*>(a.router) + int64_t(dot - row * a.experts) * a.ldr;
+      x[n] = static_cast<const T*>(a.x) + int64_t(first_row + row) * a.ldx;
+    }
     auto add = [&](int j, auto full) {
-      constexpr bool kFull = decltype(full)::value;
-      Piece<TYPE> px, pr[kMany];
-      px.template load<WHOLE, kFull>(x, j, a.d);
+      Piece<TYPE> px[MANY], pr[MANY];
+      auto load = [&](Piece<TYPE>& p, const T* row) {
+        if constexpr (decltype(full)::value) p.template load<WHOLE>(reinterpret_cast<const char*>(row + j));
+        else p.template load_end<WHOLE>(reinterpret_cast<const char*>(row), j, a.d), p.keep(a.d - j);
+      };
 #pragma unroll
-      for (int n = 0; n < kMany; ++n) pr[n].template load<WHOLE, kFull>(r[n], j, a.d);
+      for (int n = 0; n < MANY; ++n) load(pr[n], r[n]), load(px[n], x[n]);
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
-        for (int n = 0; n < kMany; ++n) sum[n] = fma(double(px.get(e)), double(pr[n].get(e)), sum[n]);
+        for (int n = 0; n < MANY; ++n) sum[n] = fma(double(px[n].get(e)), double(pr[n].get(e)), sum[n]);
     };
     int j = lane * 8;
+#pragma unroll 2
     for (; j + 8 <= a.d; j += 512) add(j, std::true_type());
     if (j < a.d) add(j, std::false_type());
 #pragma unroll
-    for (int n = 0; n < kMany; ++n) {
+    for (int n = 0; n < MANY; ++n)
       for (int step = 32; step > 0; step >>= 1) sum[n] += __shfl_xor(sum[n], step);
-      if (lane == 0 && first + n * 8 < a.experts) logit[first + n * 8] = sum[n], key[first + n * 8] = order_of(sum[n]);
+#pragma unroll
+    for (int n = 0; n < MANY; ++n)
+      if (lane == n && first + n * 8 < dots) out.logit[first + n * 8] = sum[n], out.key[first + n * 8] = order_of(sum[n]);
+  }
+}
+
+// The experts of some rows and their shares; a workgroup of 512.
+template <int TYPE, bool WHOLE, int DOTS>
+__device__ inline void route(const Moe& a, int first_row, int rows, Routing<DOTS>& out) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), dots = rows * a.experts;
+  if (dots <= 8) logits<TYPE, WHOLE, 1>(a, first_row, rows, out, wave, lane);
+  else if (dots <= 16) logits<TYPE, WHOLE, 2>(a, first_row, rows, out, wave, lane);
+  else logits<TYPE, WHOLE, DOTS <= kFused ? 2 : 4>(a, first_row, rows, out, wave, lane);
+  __syncthreads();
+  // an expert's place: how many come before it
+  for (int dot = threadIdx.x; dot < dots; dot += 512) {
+    const int row = dot / a.experts, e = dot - row * a.experts;
+    const uint64_t mine = out.key[dot];
+    int place = 0;
+#pragma unroll 8
+    for (int other = 0; other < a.experts; ++other) {
+      const uint64_t its = out.key[row * a.experts + other];
+      place += its > mine || (its == mine && other < e);
     }
+    if (place < a.top_k) out.chosen[row * a.top_k + place] = e;
   }
   __syncthreads();
-  if (wave != 0) return;
-  int mine = 0;          // lane p: the expert in place p
-  double best_logit = 0.0;
-  for (int place = 0; place < a.top_k; ++place) {
-    uint64_t best = 0;   // (a key is never 0: that would be a NaN with its sign)
-    int at = kMostExperts;
-    for (int e = lane; e < a.experts; e += 64)
-      if (key[e] > best) best = key[e], at = e;
-    for (int step = 32; step > 0; step >>= 1) {
-      const uint64_t other = __shfl_xor(static_cast<unsigned long long>(best), step);
-      const int its = __shfl_xor(at, step);
-      if (other > best || (other == best && its < at)) best = other, at = its;
+  for (int row = wave; row < rows; row += 8) {
+    const double* const l = out.logit + row * a.experts;
+    const int* const chosen = out.chosen + row * a.top_k;
+    const double most = l[chosen[0]];
+    const float e = lane < a.top_k ? expf(static_cast<float>(l[chosen[min(lane, a.top_k - 1)]] - most)) : 0.0f;
+    float total = e;
+    if (!a.renormalize) {
+      total = 0.0f;
+      for (int n = lane; n < a.experts; n += 64) total += expf(static_cast<float>(l[n] - most));
     }
-    if (place == 0) best_logit = logit[at];
-    if (lane == place) mine = at;
-    if (lane == 0) key[at] = 0;
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    for (int step = 32; step > 0; step >>= 1) total += __shfl_xor(total, step);
+    if (lane < a.top_k) out.share[row * a.top_k + lane] = e / total;
   }
-  float total = 0.0f, e = 0.0f;
-  if (lane < a.top_k) e = expf(static_cast<float>(logit[mine] - best_logit));
-  if (a.renormalize) {
-    total = e;
-  } else {
-    for (int n = lane; n < a.experts; n += 64) total += expf(static_cast<float>(logit[n] - best_logit));
-  }
-  for (int step = 32; step > 0; step >>= 1) total += __shfl_xor(total, step);
-  if (lane < a.top_k) {
-    a.chosen[i * a.top_k + lane] = mine;
-    a.share[i * a.top_k + lane] = e / total;
-  }
+}
+
+// what route() has found, to memory; by the wavefronts that have found it
+template <int DOTS>
+__device__ inline void store(const Moe& a, int first_row, int rows, const Routing<DOTS>& r) {
+  const int lane = threadIdx.x & 63;
+  for (int row = threadIdx.x >> 6; row < rows; row += 8)
+    if (lane < a.top_k) {
+      const int64_t to = int64_t(first_row + row) * a.top_k + lane;
+      a.chosen[to] = r.chosen[row * a.top_k + lane];
+      a.share[to] = r.share[row * a.top_k + lane];
+    }
+}
+
+// a workgroup a row
+template <int TYPE, bool WHOLE>
+__global__ __launch_bounds__(512) void moe_route(Moe a) {
+  __shared__ Routing<kMostExperts> r;
+  route<TYPE, WHOLE>(a, blockIdx.x, 1, r);
+  store(a, blockIdx.x, 1, r);
 }
 
 // ---------------------------------------------------------------- products
@@ -225,51 +248,85 @@ __global__ __launch_bounds__(512) void moe_route(Moe a) {
 
 constexpr int kWaves = 8;
 
-// acc += the reduction from `begin` to `end` of a lane's R rows of weights by FR rows of x (in PARTS parts, added up), of
-// which each wavefront takes every eighth step.
+// What a wavefront multiplies at a time: of R * 16 / S rows of weights by FR * 16 / S rows of x (in PARTS parts, added up),
+// kAll of the reduction.  It is loaded while the one before it is multiplied.
 template <int TYPE, bool EIGHT, bool WHOLE, int S, int R, int FR, int PARTS>
-__device__ inline void accumulate(const typename Weights<TYPE, EIGHT>::W* const (&w)[R], const typename Elem<TYPE>::T* const (&x)[FR],
-                                  int64_t part, int begin, int end, int wave, int lane, f32x4 (&acc)[R][FR]) {
+struct Step {
   using Ws = Weights<TYPE, EIGHT>;
-  constexpr int kSpan = 4 * Ws::kPer, kStep = kSpan * S;
-  constexpr int kGo = S == 1 && TYPE != kDenseF32 && FR * PARTS < 4 ? 2 : 1;   // steps at a time: 128 bytes of a row
-  const int own = (lane & (S - 1)) * kSpan + (lane >> 4) * Ws::kPer;
-  auto go = [&](int r0, auto full) {
-    constexpr bool kFull = decltype(full)::value;
-    Ws pw[kGo][R];
-    Piece<TYPE> px[kGo][FR][PARTS][Ws::kPieces];
+  using X = Piece<TYPE>;
+  static constexpr int kSizeX = TYPE == kDenseF32 ? 4 : 2;
+  static constexpr int kSpan = 4 * Ws::kPer, kStep = kSpan * S;
+  static constexpr int kGo = S == 1 && TYPE != kDenseF32 && FR * PARTS < 4 ? 2 : 1;   // 128 bytes of a row
+  static constexpr int kAll = kStep * kGo;
+  Ws w[kGo][R];
+  X x[kGo][FR][PARTS][Ws::kPieces];
+  // a lane's first element of a step
+  __device__ static int own(int lane) { return (lane & (S - 1)) * kSpan + (lane >> 4) * Ws::kPer; }
+
+  // A whole step of weights from r0 on: `base` the first row of 16 / S, `row` bytes to the lane's own row and element.
+  __device__ void load_w(const char* const (&base)[R], const uint32_t (&row)[R], int r0) {
 #pragma unroll
     for (int g = 0; g < kGo; ++g)
 #pragma unroll
-      for (int r = 0; r < R; ++r) pw[g][r].template load<WHOLE, kFull>(w[r], r0 + g * kStep + own, end);
+      for (int r = 0; r < R; ++r) w[g][r].template load<WHOLE>(base[r] + int64_t(r0 + g * kStep) * Ws::kSize + row[r]);
+  }
+
+  // and of x's rows: p, at the lane's own element
+  __device__ void load_x(const char* const (&p)[FR], int64_t part, int r0) {
 #pragma unroll
     for (int g = 0; g < kGo; ++g)
 #pragma unroll
       for (int f = 0; f < FR; ++f)
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p)
+        for (int n = 0; n < PARTS; ++n)
 #pragma unroll
           for (int i = 0; i < Ws::kPieces; ++i)
-            px[g][f][p][i].template load<WHOLE, kFull>(x[f] + p * part, r0 + g * kStep + own + 8 * i, end);
+            x[g][f][n][i].template load<WHOLE>(p[f] + n * part + int64_t(r0 + g * kStep + 8 * i) * kSizeX);
+  }
+
+  __device__ void multiply(f32x4 (&acc)[R][FR]) const {
 #pragma unroll
-    for (int g = 0; g < kGo; ++g)
+    for (int g = 0; g < kGo; ++g) products(g, acc);
+  }
+
+  // The last step, of which only what is below `end` is there; not loaded ahead.
+  __device__ void rest(const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], int64_t part, int r0,
+                       int end, int lane, f32x4 (&acc)[R][FR]) {
+    for (; r0 < end; r0 += kStep) {
+      const int at = r0 + own(lane);
 #pragma unroll
-      for (int i = 0; i < Ws::kPieces; ++i)
+      for (int r = 0; r < R; ++r) {
+        w[0][r].template load_end<WHOLE>(base[r] + row[r] - own(lane) * Ws::kSize, at, end);
+        w[0][r].keep(end - at);
+        if constexpr (!WHOLE) __builtin_amdgcn_sched_barrier(0);   // (element by element: not all at once)
+      }
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const Piece<TYPE> one = pw[g][r].piece(i);
+      for (int f = 0; f < FR; ++f)
 #pragma unroll
-          for (int p = PARTS - 1; p >= 0; --p)
+        for (int n = 0; n < PARTS; ++n)
 #pragma unroll
-            for (int f = 0; f < FR; ++f) acc[r][f] = product<TYPE>(one, px[g][f][p][i], acc[r][f]);
-        }
-  };
-  int r0 = begin + wave * kStep * kGo;
-  constexpr int kUnroll = FR * PARTS * Ws::kPieces < 8 ? 2 : 1;
-#pragma unroll kUnroll
-  for (; r0 + kStep * kGo <= end; r0 += kWaves * kStep * kGo) go(r0, std::true_type());
-  if (r0 < end) go(r0, std::false_type());
-}
+          for (int i = 0; i < Ws::kPieces; ++i) {
+            x[0][f][n][i].template load_end<WHOLE>(p[f] + n * part - own(lane) * kSizeX, at + 8 * i, end);
+            x[0][f][n][i].keep(end - at - 8 * i);
+            if constexpr (!WHOLE) __builtin_amdgcn_sched_barrier(0);
+          }
+      products(0, acc);
+    }
+  }
+
+  __device__ void products(int g, f32x4 (&acc)[R][FR]) const {
+#pragma unroll
+    for (int i = 0; i < Ws::kPieces; ++i)
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const X one = w[g][r].piece(i);
+#pragma unroll
+        for (int n = PARTS - 1; n >= 0; --n)
+#pragma unroll
+          for (int f = 0; f < FR; ++f) acc[r][f] = product<TYPE>(one, x[g][f][n][i], acc[r][f]);
+      }
+  }
+};
 
 // With segments: a lane's own sum of row lane / 16 and x's row (lane % 16) / 4, in all four lanes that share them.
 __device__ inline float segments(f32x4 v, int lane) {
@@ -279,6 +336,12 @@ __device__ inline float segments(f32x4 v, int lane) {
   return sum + __shfl_xor(sum, 2);
 }
 
+// Wavefronts of a SIMD, by the registers that two steps take, of which each has so many fragments of x: without a stack.
+template <int TYPE, bool EIGHT, bool WHOLE>
+constexpr int waves_of(int fragments) {
+  return fragments * (EIGHT ? 2 : 1) * (TYPE == kDenseF32 ? 2 : 1) + (EIGHT && !WHOLE ? 2 : 0) < 4 ? 4 : 2;
+}
+
 constexpr int kUses = 512;   // that a workgroup looks at at a time
 
 // The uses of one expert among up to kUses of them, `first` .. `first + count - 1`: a wavefront lists them in LDS of its own,
@@ -286,12 +349,19 @@ constexpr int kUses = 512;   // that a workgroup looks at at a time
 struct Uses {
   int id[kUses / 64];   // the experts of a lane's uses
 
-  __device__ void read(const Moe& a, int64_t first, int count, int lane) {
+  __device__ void read(const int32_t* chosen, int count, int lane) {
 #pragma unroll
     for (int n = 0; n < kUses / 64; ++n) {
       id[n] = -1;
-      if (n * 64 < count && n * 64 + lane < count) id[n] = a.chosen[first + n * 64 + lane];
+      if (n * 64 < count && n * 64 + lane < count) id[n] = chosen[n * 64 + lane];
     }
+  }
+
+  __device__ bool any(int expert) const {
+    bool is = false;
+#pragma unroll
+    for (int n = 0; n < kUses / 64; ++n) is |= id[n] == expert;
+    return __any(is);
   }
 
   __device__ int list(int expert, uint16_t* to, int count, int lane) const {
@@ -306,55 +376,77 @@ struct Uses {
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     return have;
   }
-
-  // the least expert above `last`, or kMostExperts
-  __device__ int next(int last, int count) const {
-    int least = kMostExperts;
-#pragma unroll
-    for (int n = 0; n < kUses / 64; ++n) {
-      if (n * 64 >= count) break;
-      if (id[n] > last) least = min(least, id[n]);
-    }
-    for (int step = 32; step > 0; step >>= 1) least = min(least, __shfl_xor(least, step));
-    return __builtin_amdgcn_readfirstlane(least);
-  }
 };
 
-// act(x Wg^T) * (x Wu^T) of an expert's uses: 16 / S columns a workgroup, whose eight wavefronts share the reduction.  The
+// act(x Wg^T) * (x Wu^T) of an expert's uses: 16 / S columns of each of which some wavefronts share the reduction.  The
 // result is stored as two values of the type, the rounded one and the rest, so that the product with Wd has it in nearly 32
 // bits: one part alone would make results 1.4 times as far from exact ones as their own rounding makes them.
-template <int TYPE, bool EIGHT, bool WHOLE, int S, int FR>
-__global__ __launch_bounds__(512) void moe_up(Moe a) {
+// ROUTE: for few rows and experts (a.m * a.experts of kFused at most) every workgroup works out the routing by itself, and the
+// first one stores it, instead of a launch before this one.
+template <int TYPE, bool EIGHT, bool WHOLE, int S, int FR, bool ROUTE>
+__global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_up(Moe a) {
   using T = typename Elem<TYPE>::T;
-  using W = typename Weights<TYPE, EIGHT>::W;
   constexpr int kRows = 16 / S, kTokens = 16 / S * FR;
   __shared__ uint16_t lists[kWaves][kUses];
   __shared__ float sums[kWaves][2][kTokens][kRows + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
-  const int j0 = blockIdx.x * kRows;
+  const int sharing = a.up_waves, groups = kWaves / sharing;   // wavefronts that share a reduction; 16 / S columns each
+  const int j0 = (blockIdx.x * groups + wave / sharing) * kRows;
   const int64_t uses = int64_t(a.m) * a.top_k;
+  __shared__ Routing<ROUTE ? kFused : 1> r;
+  const int32_t* chosen = a.chosen;
+  if constexpr (ROUTE) {
+    route<TYPE, WHOLE>(a, 0, a.m, r);
+    if (blockIdx.x == 0 && blockIdx.y == 0) store(a, 0, a.m, r);
+    chosen = r.chosen;
+  }
   int expert = blockIdx.y;
   if (uses < a.experts) {   // a workgroup for each use, of which the first one of an expert does the work
     const int use = expert;
-    expert = __builtin_amdgcn_readfirstlane(a.chosen[use]);
+    expert = __builtin_amdgcn_readfirstlane(chosen[use]);
     for (int at = 0; at < use; at += 64)
-      if (__any(at + lane < use && a.chosen[min(at + lane, use)] == expert)) return;
+      if (__any(at + lane < use && chosen[min(at + lane, use)] == expert)) return;
   }
-  const int64_t row = min(j0 + c / S, a.f - 1);
-  const W* const w[2] = {static_cast<const W*>(a.w[0]) + expert * a.stride[0] + row * a.ldw[0],
-                         static_cast<const W*>(a.w[1]) + expert * a.stride[1] + row * a.ldw[1]};
+  using P = Step<TYPE, EIGHT, WHOLE, S, 2, FR, 1>;
+  // (16 rows of at most 2^25 elements of a row's stride: 32 bits)
+  const int row0 = min(j0, a.f - 1), lane_row = min(j0 + c / S, a.f - 1) - row0;
+  const char* base[2];
+  uint32_t row[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    base[n] = static_cast<const char*>(a.w[n]) + (expert * a.stride[n] + row0 * a.ldw[n]) * P::Ws::kSize;
+    row[n] = (static_cast<uint32_t>(lane_row) * static_cast<uint32_t>(a.ldw[n]) + P::own(lane)) * P::Ws::kSize;
+  }
+  const int begin = wave % sharing * P::kAll, every = sharing * P::kAll;
   for (int64_t first = 0; first < uses; first += kUses) {
     const int count = static_cast<int>(min(uses - first, int64_t(kUses)));
     Uses u;
-    u.read(a, first, count, lane);
+    u.read(chosen + first, count, lane);
+    if (!u.any(expert)) continue;
+    P one, two;
+    if (begin + P::kAll <= a.d) one.load_w(base, row, begin);   // before the uses are listed
     const int have = u.list(expert, lists[wave], count, lane);
     for (int at = 0; at < have; at += kTokens) {
-      const T* x[FR];
+      const char* x[FR];
 #pragma unroll
       for (int f = 0; f < FR; ++f)
-        x[f] = static_cast<const T*>(a.x) + (first + lists[wave][min(at + f * kRows + c / S, have - 1)]) / a.top_k * a.ldx;
+        x[f] = static_cast<const char*>(a.x) +
+               ((first + lists[wave][min(at + f * kRows + c / S, have - 1)]) / a.top_k * a.ldx + P::own(lane)) * P::kSizeX;
       f32x4 acc[2][FR] = {};
-      accumulate<TYPE, EIGHT, WHOLE, S, 2, FR, 1>(w, x, 0, 0, a.d, wave, lane, acc);
+      int r0 = begin;
+      if (begin + P::kAll <= a.d) {
+        if (at > 0) one.load_w(base, row, begin);
+        one.load_x(x, 0, begin);
+        auto go = [&](const P& now, P& next) {   // whether there is a next one
+          r0 += every;
+          const bool more = r0 + P::kAll <= a.d;
+          if (more) next.load_w(base, row, r0), next.load_x(x, 0, r0);
+          now.multiply(acc);
+          return more;
+        };
+        while (go(one, two) && go(two, one)) {}
+      }
+      if (r0 < a.d) one.rest(base, row, x, 0, r0, a.d, lane, acc);
 #pragma unroll
       for (int f = 0; f < FR; ++f)
 #pragma unroll
@@ -368,19 +460,23 @@ __global__ __launch_bounds__(512) void moe_up(Moe a) {
           }
         }
       __syncthreads();
-      for (int t = threadIdx.x; t < kTokens * kRows; t += 512) {
-        const int r = t / kRows, j = t % kRows;
-        if (at + r >= have || j0 + j >= a.f) continue;
+      for (int t = threadIdx.x; t < kTokens * kRows * groups; t += 512) {
+        const int r = t / (kRows * groups), group = t / kRows % groups, column = t % kRows;
+        const int j = (blockIdx.x * groups + group) * kRows + column;
+        if (at + r >= have || j >= a.f) continue;
         float g[8] = {}, v = 0.0f;
 #pragma unroll
-        for (int n = 0; n < kWaves; ++n) g[0] += sums[n][0][r][j], v += sums[n][1][r][j];
+        for (int n = 0; n < kWaves; ++n) {
+          const int from = group * sharing + min(n, sharing - 1);
+          g[0] += n < sharing ? sums[from][0][r][column] : 0.0f, v += n < sharing ? sums[from][1][r][column] : 0.0f;
+        }
         if constexpr (EIGHT) {
-          g[0] *= a.scale[0][int64_t(expert) * a.f + j0 + j];
-          v *= a.scale[1][int64_t(expert) * a.f + j0 + j];
+          g[0] *= a.scale[0][int64_t(expert) * a.f + j];
+          v *= a.scale[1][int64_t(expert) * a.f + j];
         }
         act8<TYPE>(g, a.act);
         v *= g[0];
-        T* const h = static_cast<T*>(a.h) + (first + lists[wave][at + r]) * a.ldh + j0 + j;
+        T* const h = static_cast<T*>(a.h) + (first + lists[wave][at + r]) * a.ldh + j;
         *h = T(v);
         if constexpr (TYPE != kDenseF32) {
           const float rest = v - float(T(v));
@@ -395,62 +491,131 @@ __global__ __launch_bounds__(512) void moe_up(Moe a) {
 constexpr int kDownRows = 64;   // rows of x that a workgroup of the down projection has at a time
 
 // y = sum of a row's experts' h Wd^T times their shares: FI * 16 / S columns a workgroup, and one of a.splits parts of the
-// reduction.  Each wavefront adds up sums of its own, over the experts in order.
-template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI, int FR>
-__global__ __launch_bounds__(512) void moe_down(Moe a) {
+// reduction.  Its work is items, an expert and a.chunk of the reduction, in order; each wavefront takes every eighth and adds
+// up sums of its own, so that no expert waits for another.
+template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI>
+__global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(TYPE == kDenseF32 ? 1 : 2))) void moe_down(Moe a) {
   using T = typename Elem<TYPE>::T;
-  using W = typename Weights<TYPE, EIGHT>::W;
   constexpr int kParts = TYPE == kDenseF32 ? 1 : 2;
-  constexpr int kRows = 16 / S, kCols = kRows * FI, kTokens = kRows * FR;
-  __shared__ uint16_t lists[kWaves][kUses];
+  constexpr int FR = 1, kRows = 16 / S, kCols = kRows * FI, kTokens = kRows * FR;
+  __shared__ uint16_t lists[kWaves][2][kUses], used[kUses];
+  __shared__ uint32_t mask[kMostExperts / 32];
   __shared__ float sums[kWaves][kDownRows][kCols];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
   const int j0 = blockIdx.x * kCols;
   const int rows_each = min(kDownRows, kUses / a.top_k), first_row = blockIdx.y * rows_each;
   const int rows = min(rows_each, a.m - first_row), count = rows * a.top_k;
-  const int64_t first = int64_t(first_row) * a.top_k, part = int64_t(a.m) * a.top_k * a.ldh;
+  const int64_t first = int64_t(first_row) * a.top_k, part = int64_t(a.m) * a.top_k * a.ldh * sizeof(T);
   const int begin = static_cast<int>(int64_t(a.split_step) * blockIdx.z), end = min(a.f, begin + a.split_step);
-  for (int at = lane; at < rows * kCols; at += 64) sums[wave][at / kCols][at % kCols] = 0.0f;
   Uses u;
-  u.read(a, first, count, lane);
-  for (int expert = u.next(-1, count); expert < kMostExperts; expert = u.next(expert, count)) {
-    const int have = u.list(expert, lists[wave], count, lane);
-    const W* w[FI];
+  u.read(a.chosen + first, count, lane);
+  if (tid < kMostExperts / 32) mask[tid] = 0;
+  for (int at = lane; at < rows * kCols; at += 64) sums[wave][at / kCols][at % kCols] = 0.0f;
+  __syncthreads();
+  // the experts that are used, in order
 #pragma unroll
-    for (int i = 0; i < FI; ++i)
-      w[i] = static_cast<const W*>(a.w[2]) + expert * a.stride[2] + int64_t(min(j0 + i * kRows + c / S, a.d - 1)) * a.ldw[2];
-    for (int at = 0; at < have; at += kTokens) {
-      const T* h[FR];
-      int use[FR];
+  for (int n = 0; n < kUses / 64; ++n)
+    if (n == wave && u.id[n] >= 0) atomicOr(&mask[u.id[n] >> 5], 1u << (u.id[n] & 31));
+  __syncthreads();
+  for (int e = tid; e < a.experts; e += 512) {
+    if (!(mask[e >> 5] >> (e & 31) & 1)) continue;
+    int at = __popc(mask[e >> 5] & ((1u << (e & 31)) - 1));
+    for (int n = 0; n < e >> 5; ++n) at += __popc(mask[n]);
+    used[at] = static_cast<uint16_t>(e);
+  }
+  int total = 0;
+  for (int n = 0; n < (a.experts + 31) / 32; ++n) total += __popc(mask[n]);
+  __syncthreads();
+  const int chunks = (end - begin + a.chunk - 1) / a.chunk;
+  using P = Step<TYPE, EIGHT, WHOLE, S, FI, FR, kParts>;
+  // Where a wavefront is: an item, its expert's uses from `at` on, and r0 of its reduction.
+  struct Place {
+    int item, expert, to, have, at, r0, which;
+    const char* w[FI];
+    uint32_t row[FI];
+    const char* h[FR];
+    int use[FR];
+  };
+  auto begin_item = [&](Place& p) {
+    p.expert = __builtin_amdgcn_readfirstlane(used[p.item / chunks]);
+    p.which ^= 1;
+    p.have = u.list(p.expert, lists[wave][p.which], count, lane);
 #pragma unroll
-      for (int f = 0; f < FR; ++f) {
-        use[f] = lists[wave][min(at + f * kRows + c / S, have - 1)];
-        h[f] = static_cast<const T*>(a.h) + (first + use[f]) * a.ldh;
-      }
-      f32x4 acc[FI][FR] = {};
-      accumulate<TYPE, EIGHT, WHOLE, S, FI, FR, kParts>(w, h, part, begin, end, wave, lane, acc);
+    for (int i = 0; i < FI; ++i) {
+      const int row0 = min(j0 + i * kRows, a.d - 1);
+      p.w[i] = static_cast<const char*>(a.w[2]) + (p.expert * a.stride[2] + row0 * a.ldw[2]) * P::Ws::kSize;
+      p.row[i] = (static_cast<uint32_t>(min(j0 + i * kRows + c / S, a.d - 1) - row0) * static_cast<uint32_t>(a.ldw[2]) + P::own(lane)) *
+                 P::Ws::kSize;
+    }
+    p.at = 0;
+  };
+  auto begin_rows = [&](Place& p) {
+    p.r0 = begin + p.item % chunks * a.chunk, p.to = min(end, p.r0 + a.chunk);
 #pragma unroll
-      for (int f = 0; f < FR; ++f) {
-        const bool in = at + f * kRows + c / S < have;
-        const float share = a.share[first + use[f]];
-        float* const mine = sums[wave][use[f] / a.top_k];
+    for (int f = 0; f < FR; ++f) {
+      p.use[f] = lists[wave][p.which][min(p.at + f * kRows + c / S, p.have - 1)];
+      p.h[f] = static_cast<const char*>(a.h) + ((first + p.use[f]) * a.ldh + P::own(lane)) * P::kSizeX;
+    }
+  };
+  auto load = [&](P& s, const Place& p) {
+    if (p.r0 + P::kAll <= p.to) s.load_w(p.w, p.row, p.r0), s.load_x(p.h, part, p.r0);
+  };
+  f32x4 acc[FI][FR] = {};
+  auto finish = [&](const Place& p) {
 #pragma unroll
-        for (int i = 0; i < FI; ++i) {
-          auto add = [&](int j, float s) {
-            s *= share;
-            if constexpr (EIGHT) s *= a.scale[2][int64_t(expert) * a.d + min(j0 + j, a.d - 1)];
-            if (in) mine[j] += s;
-          };
-          if constexpr (S == 1) {
+    for (int f = 0; f < FR; ++f) {
+      const bool in = p.at + f * kRows + c / S < p.have;
+      const float share = a.share[first + p.use[f]];
+      float* const mine = sums[wave][p.use[f] / a.top_k];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) add(i * 16 + 4 * q + e, acc[i][f][e]);
-          } else {
-            const float s = segments(acc[i][f], lane);
-            if ((c & 3) == 0) add(i * 4 + q, s);
-          }
+      for (int i = 0; i < FI; ++i) {
+        auto add = [&](int j, float s) {
+          s *= share;
+          if constexpr (EIGHT) s *= a.scale[2][int64_t(p.expert) * a.d + min(j0 + j, a.d - 1)];
+          if (in) mine[j] += s;
+        };
+        if constexpr (S == 1) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) add(i * 16 + 4 * q + e, acc[i][f][e]);
+        } else {
+          const float s = segments(acc[i][f], lane);
+          if ((c & 3) == 0) add(i * 4 + q, s);
         }
+        acc[i][f] = f32x4{};
       }
     }
+  };
+  const int items = total * chunks;
+  P one, two;
+  Place now = {wave}, then;
+  bool more = now.item < items;
+  if (more) begin_item(now), begin_rows(now), load(one, now);
+  auto go = [&](P& s, P& other) {
+    then = now;
+    if (now.r0 + P::kAll <= now.to) then.r0 += P::kAll;
+    const bool last = then.r0 + P::kAll > then.to;
+    const int left = then.r0;   // where whole steps end
+    if (last) {
+      then.at += kTokens;
+      if (then.at >= then.have) {
+        then.item += kWaves;
+        more = then.item < items;
+        if (more) begin_item(then);
+      }
+      if (more) begin_rows(then);
+    }
+    if (more) load(other, then);
+    if (left > now.r0) s.multiply(acc);
+    if (last) {
+      if (left < now.to) s.rest(now.w, now.row, now.h, part, left, now.to, lane, acc);
+      finish(now);
+    }
+    now = then;
+  };
+  while (more) {
+    go(one, two);
+    if (!more) break;
+    go(two, one);
   }
   __syncthreads();
   for (int at = threadIdx.x; at < rows * kCols; at += 512) {
@@ -474,29 +639,41 @@ __global__ __launch_bounds__(256) void moe_join(Moe a) {
   static_cast<typename Elem<TYPE>::T*>(a.y)[at / a.d * a.ldy + at % a.d] = typename Elem<TYPE>::T(s);
 }
 
-template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI, int FR>
-int products(const Moe& a, hipStream_t s) {
-  constexpr int kRows = 16 / S;
-  const int64_t uses = int64_t(a.m) * a.top_k;
-  moe_up<TYPE, EIGHT, WHOLE, S, FR><<<dim3((a.f + kRows - 1) / kRows, static_cast<uint32_t>(std::min<int64_t>(uses, a.experts))), 512, 0, s>>>(a);
-  if (const int rc = hipGetLastError(); rc != 0) return rc;
-  const int rows = std::min(kDownRows, kUses / a.top_k), cols = kRows * FI;
-  moe_down<TYPE, EIGHT, WHOLE, S, FI, FR><<<dim3((a.d + cols - 1) / cols, (a.m + rows - 1) / rows, a.splits), 512, 0, s>>>(a);
-  if (const int rc = hipGetLastError(); rc != 0 || a.splits == 1) return rc;
-  moe_join<TYPE><<<static_cast<uint32_t>((int64_t(a.m) * a.d + 255) / 256), 256, 0, s>>>(a);
+template <int TYPE, bool EIGHT, bool WHOLE, int S, int FR>
+int up(const Moe& a, hipStream_t s) {
+  const int columns = 16 / S * (kWaves / a.up_waves);
+  const dim3 grid((a.f + columns - 1) / columns, static_cast<uint32_t>(std::min<int64_t>(int64_t(a.m) * a.top_k, a.experts)));
+  if (a.fused && FR == 1) {
+    moe_up<TYPE, EIGHT, WHOLE, S, 1, true><<<grid, 512, 0, s>>>(a);
+  } else {
+    moe_route<TYPE, WHOLE><<<static_cast<uint32_t>(a.m), 512, 0, s>>>(a);
+    if (const int rc = hipGetLastError(); rc != 0) return rc;
+    moe_up<TYPE, EIGHT, WHOLE, S, FR, false><<<grid, 512, 0, s>>>(a);
+  }
+  return hipGetLastError();
+}
+
+template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI>
+int down(const Moe& a, hipStream_t s) {
+  const int rows = std::min(kDownRows, kUses / a.top_k), columns = 16 / S * FI;
+  moe_down<TYPE, EIGHT, WHOLE, S, FI><<<dim3((a.d + columns - 1) / columns, (a.m + rows - 1) / rows, a.splits), 512, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <int TYPE, bool EIGHT, bool WHOLE>
 int launch(const Moe& a, hipStream_t s) {
-  moe_route<TYPE, WHOLE><<<static_cast<uint32_t>(a.m), 512, 0, s>>>(a);
-  if (const int rc = hipGetLastError(); rc != 0) return rc;
-  switch (a.variant) {
-    case kMoeFew: return products<TYPE, EIGHT, WHOLE, 4, 1, 1>(a, s);
-    case kMoeSome: return products<TYPE, EIGHT, WHOLE, 4, 1, 2>(a, s);
-    case kMoeMore: return products<TYPE, EIGHT, WHOLE, 1, 2, 1>(a, s);
-    default: return products<TYPE, EIGHT, WHOLE, 1, 2, 4>(a, s);
+  constexpr int kMany = EIGHT || TYPE == kDenseF32 ? 2 : 4;   // (as many as there are registers for)
+  int rc;
+  switch (a.up_variant) {
+    case kMoeFew: rc = up<TYPE, EIGHT, WHOLE, 4, 1>(a, s); break;
+    case kMoeMore: rc = up<TYPE, EIGHT, WHOLE, 1, 1>(a, s); break;
+    default: rc = up<TYPE, EIGHT, WHOLE, 1, kMany>(a, s); break;
   }
+  if (rc != 0) return rc;
+  rc = a.down_variant == kMoeFew ? down<TYPE, EIGHT, WHOLE, 4, 1>(a, s) : down<TYPE, EIGHT, WHOLE, 1, 2>(a, s);
+  if (rc != 0 || a.splits == 1) return rc;
+  moe_join<TYPE><<<static_cast<uint32_t>((int64_t(a.m) * a.d + 255) / 256), 256, 0, s>>>(a);
+  return hipGetLastError();
 }
 
 template <int TYPE>

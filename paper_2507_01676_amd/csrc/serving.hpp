@@ -30,13 +30,18 @@ struct Moe {
   int64_t ldx, ldr, ldh, ldy, ldw[3], stride[3];
   float* partial;          // [splits][m][d], with splits > 1
   int32_t m, f, d, experts, top_k, act, renormalize;
-  int32_t variant;         // MoeVariant
+  int32_t up_variant, down_variant;   // MoeVariant
+  int32_t up_waves;        // wavefronts that share a reduction of the up projections: 1, 2, 4 or 8
+  int32_t fused;           // see kFused
   int32_t whole;           // rows of all operands start at multiples of 16 bytes
   int32_t splits, split_step;   // parts of the down projection's reduction, and their length
+  int32_t chunk;           // of a part, that a wavefront takes at a time
 };
 
-// By how many rows of x an expert is expected to have: at most 4, 8 or 16 at a time, or 64.
-enum MoeVariant { kMoeFew = 0, kMoeSome = 1, kMoeMore = 2, kMoeMany = 3 };
+// How many rows of x an expert has at a time: at most 4 (by 4 rows of weights), 16, or several times 16.
+enum MoeVariant { kMoeFew = 0, kMoeMore = 1, kMoeMany = 2 };
+
+constexpr int kFused = 32;   // logits of all rows that every workgroup of the up projections works out by itself
 
 constexpr int kMostExperts = 1024, kMostTopK = 32;
 

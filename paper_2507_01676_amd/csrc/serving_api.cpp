@@ -13,7 +13,7 @@ namespace {
 
 constexpr int64_t kMaxSize = int64_t(1) << 30, kMaxStride = int64_t(1) << 40;
 constexpr int64_t kMostInputs = 131071;        // of sums of 8-bit products in 32 bits: 2^14 each
-constexpr int64_t kMostRows = 65536, kMostColumns = int64_t(1) << 26;   // moe
+constexpr int64_t kMostRows = 65536, kMostColumns = int64_t(1) << 25;   // moe
 constexpr size_t kAlign = 256;
 
 #define EMBX_TRY(x)                       \
@@ -124,7 +124,7 @@ emb_status_t check_experts(const emb_experts_t& w, const emb_moe_t& a, int64_t r
   EMBX_TRY(check_matrix(w.p, w.ld, rows, cols, w.scale ? 1 : esize(a.dtype)));
   EMBX_TRY(check_vector(w.scale, w.scale ? 1 : 0, 4));
   if (w.stride < 0) return EMB_ERR_INVALID_ARGUMENT;
-  return w.stride > kMaxStride ? EMB_ERR_UNSUPPORTED : EMB_OK;
+  return w.stride > kMaxStride || w.ld > kMostColumns ? EMB_ERR_UNSUPPORTED : EMB_OK;
 }
 
 emb_status_t check_shape(const emb_moe_t& a) {
@@ -149,19 +149,32 @@ struct MoeSpace {
   int32_t* chosen;
   float* share;
   float* partial;
-  int32_t variant, splits, split_step;
+  int32_t up_variant, down_variant, up_waves, fused, splits, split_step, chunk;
 };
 
 MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   const int64_t uses = a.m * a.top_k;
   MoeSpace s = {nullptr, (a.f + 7) / 8 * 8, a.chosen, a.share};
-  s.variant = a.m <= 4 ? kMoeFew : a.m <= 8 ? kMoeSome : uses <= 12 * a.experts ? kMoeMore : kMoeMany;
-  // enough workgroups of the down projection to fill the GPU, each with some steps of its eight wavefronts
-  const int64_t cols = s.variant >= kMoeMore ? 32 : 4, rows = std::min<int64_t>(64, 512 / a.top_k);
-  const int64_t groups = (a.d + cols - 1) / cols * ((a.m + rows - 1) / rows);
-  const int64_t splits = s.variant >= kMoeMore ? std::min<int64_t>(std::min<int64_t>(16, a.f / 512), 512 / groups) : 1;
-  s.split_step = static_cast<int32_t>((a.f + std::max<int64_t>(1, splits) - 1) / std::max<int64_t>(1, splits) + 127) / 128 * 128;
+  const int64_t used = std::min<int64_t>(uses, a.experts);   // experts, at most
+  const int64_t step = a.gate.scale ? 64 : 32;               // of the reduction: a matrix instruction, or two
+  // The up projections: 16 columns of an expert to so many wavefronts, or 4 where there would be few workgroups.
+  const int64_t tiles = (a.f + 15) / 16 * used;
+  s.up_variant = a.m <= 4 && tiles < 256 ? kMoeFew : uses <= 12 * a.experts ? kMoeMore : kMoeMany;
+  s.up_waves = s.up_variant != kMoeFew && tiles >= 352 ? 4 : 8;
+  const int64_t up_step = s.up_variant == kMoeFew ? step * 4 : step * 2;
+  while (s.up_waves > 1 && s.up_waves * up_step > a.d) s.up_waves /= 2;
+  s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kFused && a.m * a.experts * a.d <= 65536 && a.m * tiles <= 1024;
+  // The down projection: 32 columns a workgroup, or 4, and about 256 workgroups.
+  s.down_variant = (a.m <= 4 && a.d <= 2048) || (a.m <= 8 && a.d <= 512) ? kMoeFew : kMoeMore;
+  const int64_t columns = s.down_variant == kMoeFew ? 4 : 32, rows = std::min<int64_t>(64, 512 / a.top_k);
+  const int64_t groups = (a.d + columns - 1) / columns * ((a.m + rows - 1) / rows);
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({16, a.f / 160, 256 / groups}));
+  const int64_t down_step = s.down_variant == kMoeFew ? step * 4 : step * 2;
+  s.split_step = static_cast<int32_t>(((a.f + splits - 1) / splits + down_step - 1) / down_step * down_step);
   s.splits = static_cast<int32_t>((a.f + s.split_step - 1) / s.split_step);
+  // an expert's part of the reduction is an item of a wavefront; with few experts several are, so that there are 16 or so
+  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(s.split_step / (2 * down_step), 16 / used));
+  s.chunk = static_cast<int32_t>(((s.split_step + chunks - 1) / chunks + down_step - 1) / down_step * down_step);
   if (s.splits > 1) s.partial = ar.take<float>(s.splits * a.m * a.d * 4);
   s.h = ar.take<void>(2 * uses * s.ldh * esize(a.dtype));
   if (!s.chosen) s.chosen = ar.take<int32_t>(uses * 4);
@@ -262,7 +275,9 @@ emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes
     ++i;
   }
   g.h = s.h, g.ldh = s.ldh, g.chosen = s.chosen, g.share = s.share;
-  g.partial = s.partial, g.variant = s.variant, g.splits = s.splits, g.split_step = s.split_step;
+  g.up_variant = s.up_variant, g.down_variant = s.down_variant, g.up_waves = s.up_waves;
+  g.fused = s.fused;
+  g.partial = s.partial, g.splits = s.splits, g.split_step = s.split_step, g.chunk = s.chunk;
   const size_t size = esize(a->dtype);
   g.whole = aligned(a->x, a->ldx, size) && aligned(a->router, a->ldr, size) && aligned(a->gate, size) && aligned(a->up, size) &&
             aligned(a->down, size);
