@@ -8,6 +8,7 @@
 #include "../../include/embx_dense.h"
 #include "dense.hpp"
 #include "dense_device.hpp"
+#include "quantize_device.hpp"
 
 #ifndef EMBX_DPART
 #define EMBX_DPART -1
@@ -366,8 +367,6 @@ struct Finish<kDenseI8, kForward> {
     if (g.bias[0] && n > 0) load(static_cast<const char*>(g.bias[0]), j, bias);
   }
 
-  __device__ void next() { i += step; }
-
   __device__ void load(const char* p, int64_t at, float* v) const {
     switch (g.result) {
       case kDenseF32: load8<kDenseF32>(p + at * 4, n, v); break;
@@ -376,26 +375,60 @@ struct Finish<kDenseI8, kForward> {
     }
   }
 
-  __device__ void put(float* s, float*) const {
-    const float row = g.scale_a[i];
+  // What a row needs from memory, asked for before the rows before it are finished: the `which`-th from here on.
+  struct Held {
+    float row, lo[4], hi[4];   // (of a residual of 16 bits: lo)
+  };
+
+  __device__ Held ask(int which) const {
+    Held h = ask_residual(which);
+    h.row = g.scale_a[min(i + which * step, int64_t(g.ni) - 1)];
+    return h;
+  }
+
+  __device__ Held ask_residual(int which = 0) const {
+    Held h = {};
+    const int64_t at = min(i + which * step, int64_t(g.ni) - 1);
+    if (g.res && n == 8) {
+      const char* const p = static_cast<const char*>(g.res) + (at * g.ldr + j) * (g.result == kDenseF32 ? 4 : 2);
+      __builtin_memcpy(h.lo, p, 16);
+      if (g.result == kDenseF32) __builtin_memcpy(h.hi, p + 16, 16);
+    }
+    return h;
+  }
+
+  __device__ void put(float* s, const Held& h, int which) const {
+    const int64_t row = i + which * step;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = static_cast<float>(__float_as_int(s[e])) * row * scale[e] + bias[e];
+    for (int e = 0; e < 8; ++e) s[e] = static_cast<float>(__float_as_int(s[e])) * h.row * scale[e] + bias[e];
     if (g.result == kDenseF32) act8<kDenseF32>(s, g.act);
     else act8<kDenseBF16>(s, g.act);
     if (g.res) {
       float b[8];
-      load(static_cast<const char*>(g.res), i * g.ldr + j, b);
+      if (n < 8) {
+        load(static_cast<const char*>(g.res), row * g.ldr + j, b);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t pair = __float_as_uint(h.lo[e / 2]);
+          b[e] = g.result == kDenseF32   ? (e < 4 ? h.lo[e % 4] : h.hi[e % 4])
+                 : g.result == kDenseF16 ? static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(e % 2 ? pair >> 16 : pair)))
+                                         : __uint_as_float(e % 2 ? pair & 0xffff0000u : pair << 16);
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) s[e] += b[e];
     }
     char* const y = static_cast<char*>(g.c[0]);
-    const int64_t at = i * g.ldc[0] + j;
+    const int64_t at = row * g.ldc[0] + j;
     switch (g.result) {
       case kDenseF32: store8<kDenseF32>(y + at * 4, n, s); break;
       case kDenseF16: store8<kDenseF16>(y + at * 2, n, s); break;
       default: store8<kDenseBF16>(y + at * 2, n, s); break;
     }
   }
+
+  __device__ void put(float* s, float*) const { put(s, ask(0), 0); }
 };
 
 // Stores a wavefront's sums, from row i0 and column j0 on, through LDS of its own: 64 rows of FJ * 16 sums at a time, so
@@ -449,6 +482,24 @@ __device__ inline void store_sums(const DenseGemm& g, Sums<TYPE> (&acc)[FI][FJ],
             float* u = p + g.slots * slice;
             reinterpret_cast<f32x4*>(u)[0] = f32x4{s1[0], s1[1], s1[2], s1[3]};
             reinterpret_cast<f32x4*>(u)[1] = f32x4{s1[4], s1[5], s1[6], s1[7]};
+          }
+        }
+      } else if constexpr (TYPE == kDenseI8) {
+        // four rows' scales and residuals are asked for together: one after another, each waits for memory
+        constexpr int kTogether = 4;
+        static_assert(kPass * 16 % (kTogether * kRows) == 0);
+        Finish<TYPE, KIND> out(g, part, first, j, kRows);
+#pragma unroll 1
+        for (int row0 = 0; row0 < kPass * 16; row0 += kTogether * kRows, out.i += kTogether * kRows) {
+          if (first + row0 >= g.ni) break;
+          typename Finish<TYPE, KIND>::Held held[kTogether];
+#pragma unroll
+          for (int x = 0; x < kTogether; ++x) held[x] = out.ask(x);
+#pragma unroll
+          for (int x = 0; x < kTogether; ++x) {
+            if (first + row0 + x * kRows >= g.ni) break;
+            sums(row0 + x * kRows + lane / kLanes, s0, s1);
+            out.put(s0, held[x], x);
           }
         }
       } else {
@@ -1018,15 +1069,14 @@ struct Loader {
         for (int e = 0; e < 4; ++e) v[4 * h + e] = at + 4 * h < n ? x[e] : 0.0f;
       }
     } else {
-      constexpr int kPer = 16 / sizeof(T);   // (the last chunk of 8-bit integers may hold fewer)
-      h = *reinterpret_cast<const s16x8*>(row + (TYPE == kDenseI8 ? min(at, (n - 1) / kPer * kPer) : min(at, n - 8)));
+      h = *reinterpret_cast<const s16x8*>(row + min(at, n - 8));
       if (at >= n) h = s16x8{};
     }
   }
 };
 
 template <int TYPE>
-__device__ inline Sums<TYPE> multiply(const Loader<TYPE>& w, const Loader<TYPE>& x, Sums<TYPE> c) {
+__device__ inline f32x4 multiply(const Loader<TYPE>& w, const Loader<TYPE>& x, f32x4 c) {
   if constexpr (TYPE == kDenseF32) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[e], x.v[e], c, 0, 0, 0);
@@ -1045,7 +1095,6 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
   using T = typename Elem<TYPE>::T;
   using L = Loader<TYPE>;
   constexpr int kMats = KIND == kGated ? 2 : 1;
-  constexpr int kPer = TYPE == kDenseI8 ? 16 : 8, kStep = 4 * kPer;   // elements of a lane, and of a wavefront's step
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
   uint32_t i = blockIdx.x / across, j_ = blockIdx.x % across;
@@ -1054,7 +1103,7 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
     if (i >= down) return;
   }
   const int i0 = i * FR * 16, j0 = j_ * 16;
-  Sums<TYPE> acc[FR][kMats] = {};
+  f32x4 acc[FR][kMats] = {};
   auto products = [&](const L* x, const L* w) {
 #pragma unroll
     for (int f = 0; f < FR; ++f)
@@ -1069,12 +1118,12 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 #pragma unroll
     for (int m = 0; m < kMats; ++m) weights[m] = static_cast<const T*>(g.b[m]) + min(j0 + c, g.nj - 1) * g.ldb[m];
 #pragma unroll 4
-    for (int r0 = wave * kStep; r0 < g.nr; r0 += 8 * kStep) {
+    for (int r0 = wave * 32; r0 < g.nr; r0 += 8 * 32) {
       L x[FR], w[kMats];
 #pragma unroll
-      for (int m = 0; m < kMats; ++m) w[m].load(weights[m], r0 + kPer * q, g.nr);
+      for (int m = 0; m < kMats; ++m) w[m].load(weights[m], r0 + 8 * q, g.nr);
 #pragma unroll
-      for (int f = 0; f < FR; ++f) x[f].load(rows[f], r0 + kPer * q, g.nr);
+      for (int f = 0; f < FR; ++f) x[f].load(rows[f], r0 + 8 * q, g.nr);
       products(x, w);
     }
   } else {
@@ -1123,7 +1172,7 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 #pragma unroll
   for (int f = 0; f < FR; ++f)
 #pragma unroll
-    for (int m = 0; m < kMats; ++m) *reinterpret_cast<Sums<TYPE>*>(&sums[wave][f][m][c][4 * q]) = acc[f][m];
+    for (int m = 0; m < kMats; ++m) *reinterpret_cast<f32x4*>(&sums[wave][f][m][c][4 * q]) = acc[f][m];
   __syncthreads();
   const int t = threadIdx.x, row = t >> 1, j = j0 + (t & 1) * 8;
   if (row >= FR * 16 || i0 + row >= g.ni || j >= g.nj) return;
@@ -1133,8 +1182,131 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 #pragma unroll
     for (int m = 0; m < kMats; ++m)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s[m][e] = plus<TYPE>(s[m][e], sums[w][row >> 4][m][row & 15][(t & 1) * 8 + e]);
+      for (int e = 0; e < 8; ++e) s[m][e] += sums[w][row >> 4][m][row & 15][(t & 1) * 8 + e];
   Finish<TYPE, KIND>(g, 0, i0 + row, j, 0).put(s[0], s[1]);
+}
+
+// The same for 8-bit integers: of few rows, bound by reading the weights.  A wavefront takes 128 bytes of every eighth step of
+// 1024, and asks for the weights of eight loads at a time, the next eight while it multiplies.  x is 8-bit rows in memory
+// (XT kDenseI8), or a few rows of the result's type (g.m of 8 at most) that each workgroup quantizes by itself, while its
+// weights are on their way, instead of a launch before this one.
+constexpr int kQuantizedLds = 16640;   // up to 16384 elements
+
+template <int XT, int FR>
+__global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
+  constexpr bool kQuantize = XT != kDenseI8;
+  constexpr int kRounds = 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
+  const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
+  uint32_t i = blockIdx.x / across, j_ = blockIdx.x % across;
+  if (down >= kXcds) {   // rows of x stay with one XCD's L2
+    j_ = blockIdx.x / kXcds % across, i = blockIdx.x / (kXcds * across) * kXcds + blockIdx.x % kXcds;
+    if (i >= down) return;
+  }
+  const int i0 = i * FR * 16, j0 = j_ * 16;
+  const int8_t* const weights = static_cast<const int8_t*>(g.b[0]) + min(j0 + c, g.nj - 1) * g.ldb[0];
+  const int last = (g.nr - 1) / 16 * 16;   // the last chunk of a row; what lies behind the row's end meets zeros of x
+  s16x8 w[2][kRounds][2];
+  auto ask = [&](s16x8 (*to)[2], int r0) {
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        to[r][h] = *reinterpret_cast<const s16x8*>(weights + min(r0 + r * 1024 + h * 64 + q * 16, last));
+  };
+  ask(w[0], wave * 128);
+  __shared__ __align__(16) int8_t quantized[kQuantize ? kQuantizedLds : 16];
+  __shared__ float row_scale[8];
+  const int wide = (g.nr + 127) / 128 * 128 + 16;   // of a row in LDS: 16 rows' chunks lie in different banks
+  if constexpr (kQuantize) {
+    using T = typename Elem<XT>::T;
+    __shared__ uint32_t most[8];
+    // wavefronts of a row: all of its elements are in their registers
+    const int each = g.ni == 1 ? 8 : g.ni == 2 ? 4 : g.ni <= 4 ? 2 : 1, row = wave / each, first = (wave % each) * 64 + lane;
+    const bool mine = row < g.ni;
+    const T* const x = static_cast<const T*>(g.a[0]) + min(row, g.ni - 1) * g.lda;
+    float v[4][8];
+    uint32_t largest = 0;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int at = (first + n * each * 64) * 8;
+      if (n * each * 512 < g.nr) load8<XT>(x + min(at, g.nr - 1), min(8, max(1, g.nr - at)), v[n]);
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int at = (first + n * each * 64) * 8;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (at + e >= g.nr) v[n][e] = 0.0f;
+        largest = max(largest, __float_as_uint(v[n][e]) & 0x7fffffffu);
+      }
+    }
+    for (int step = 32; step > 0; step >>= 1) largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), step)));
+    if (lane == 0) most[wave] = largest;
+    __syncthreads();
+    for (int n = 0; n < each; ++n) largest = max(largest, most[wave / each * each + n]);
+    const Scale s = Scale::of(__uint_as_float(largest));
+    if (mine && first == 0) row_scale[row] = s.stored();
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int at = (first + n * each * 64) * 8;
+      uint32_t out[2];
+      quantize8(s, v[n], out);
+      if (mine && at < wide - 16) *reinterpret_cast<uint2*>(quantized + row * wide + at) = uint2{out[0], out[1]};
+    }
+    __syncthreads();
+  }
+  const int8_t* rows[FR];
+#pragma unroll
+  for (int f = 0; f < FR; ++f)
+    rows[f] = kQuantize ? quantized + min(c, g.ni - 1) * wide
+                        : static_cast<const int8_t*>(g.a[0]) + min(i0 + f * 16 + c, g.ni - 1) * g.lda;
+  i32x4 acc[FR] = {};
+  auto multiply = [&](const s16x8 (*with)[2], int r0) {
+#pragma unroll
+    for (int r = 0; r < kRounds; ++r) {
+      if (r0 + r * 1024 >= g.nr) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = r0 + r * 1024 + h * 64 + q * 16;
+#pragma unroll
+        for (int f = 0; f < FR; ++f) {
+          s16x8 x = *reinterpret_cast<const s16x8*>(rows[f] + (kQuantize ? at : min(at, last)));
+          if (!kQuantize && at >= g.nr) x = s16x8{};
+          acc[f] = mfma16<kDenseI8>(with[r][h], x, acc[f]);
+        }
+      }
+    }
+  };
+  for (int r0 = wave * 128; r0 < g.nr; r0 += 2 * kRounds * 1024) {
+    if (r0 + kRounds * 1024 < g.nr) ask(w[1], r0 + kRounds * 1024);
+    multiply(w[0], r0);
+    if (r0 + kRounds * 1024 >= g.nr) break;
+    if (r0 + 2 * kRounds * 1024 < g.nr) ask(w[0], r0 + 2 * kRounds * 1024);
+    multiply(w[1], r0 + kRounds * 1024);
+  }
+  __shared__ int sums[8][FR][16][16];   // [wavefront][..][row][column]
+#pragma unroll
+  for (int f = 0; f < FR; ++f) *reinterpret_cast<i32x4*>(&sums[wave][f][c][4 * q]) = acc[f];
+  const int t = threadIdx.x, row = t >> 1, j = j0 + (t & 1) * 8;
+  const bool in = row < FR * 16 && i0 + row < g.ni && j < g.nj;
+  Finish<kDenseI8, kForward> out(g, 0, min(i0 + row, g.ni - 1), min(j, g.nj - 1), 0);
+  typename Finish<kDenseI8, kForward>::Held held = {};
+  if (in) {
+    if constexpr (kQuantize) held = out.ask_residual(), held.row = row_scale[row];
+    else held = out.ask(0);
+  }
+  __syncthreads();
+  if (!in) return;
+  float s[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    int sum = 0;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) sum += sums[n][row >> 4][row & 15][(t & 1) * 8 + e];
+    s[e] = __int_as_float(sum);
+  }
+  out.put(s, held, 0);
 }
 
 // A reduction of at most KS * 32: writing the results is all.  Four wavefronts, each with the weights of FC * 16 columns in
@@ -1267,35 +1439,6 @@ __global__ __launch_bounds__(256) void dense_short(DenseGemm g) {
 }
 
 // ---------------------------------------------------------------- elementwise parts of the gradients
-
-// Copies up to three matrices to rows that start at multiples of 16 bytes and end in zeros up to a whole chunk: the
-// tiles above read nothing else.  A wavefront takes 64 consecutive elements at a time, as rows that start anywhere
-// are read fastest (16-byte loads at odd addresses measured 1.1 TB/s).  f16 65536 x 1001: 262 MB read and written in 60 us,
-// 4.4 TB/s, with four rows of a thread under way (one: 81 us).
-template <class E>
-__device__ inline void pack_rows(const DensePack& p, uint32_t mat, uint32_t group) {
-  constexpr uint32_t kChunk = 16 / sizeof(E);
-  const uint32_t cols = p.cols[mat], padded = (cols + kChunk - 1) / kChunk * kChunk;
-  const uint32_t rows = p.rows[mat];
-  const E* src = static_cast<const E*>(p.src[mat]);
-  E* dst = static_cast<E*>(p.dst[mat]);
-  // as many rows side by side as 256 threads hold, four at a time
-  const uint32_t wide = p.wide[mat], x = threadIdx.x % wide, y = threadIdx.x / wide, side = 256 / wide;
-  const uint64_t step = uint64_t(p.groups) * side;
-  for (uint32_t panel = 0; panel < padded; panel += kPanel, dst += p.panel[mat] - kPanel) {
-    const uint32_t end = min(padded, panel + static_cast<uint32_t>(kPanel));
-    for (uint64_t i = uint64_t(group) * side + y; i < rows; i += 4 * step)
-#pragma unroll 2
-      for (uint32_t j = panel + x; j < end; j += wide) {
-        E v[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = src[min(i + r * step, uint64_t(rows) - 1) * p.lds[mat] + min(j, cols - 1)];
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (i + r * step < rows) dst[(i + r * step) * p.ldd[mat] + j] = j < cols ? v[r] : 0;
-      }
-  }
-}
 
 template <class E>
 __global__ __launch_bounds__(256) void dense_pack(DensePack p) {
@@ -1454,8 +1597,13 @@ template <int TYPE, int KIND, int FR>
 int rows_launch(const DenseGemm& g, hipStream_t stream) {
   const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
   const uint32_t grid = across * (down >= kXcds ? (down + kXcds - 1) / kXcds * kXcds : down);
-  if (TYPE == kDenseI8 || g.whole) dense_rows<TYPE, KIND, FR, true><<<grid, 512, 0, stream>>>(g);
-  else if constexpr (TYPE != kDenseI8) dense_rows<TYPE, KIND, FR, false><<<grid, 512, 0, stream>>>(g);
+  if constexpr (TYPE == kDenseI8) {
+    if (FR > 1 || !g.quantize) dense_rows_i8<kDenseI8, FR><<<grid, 512, 0, stream>>>(g);
+    else if (g.result == kDenseF32) dense_rows_i8<kDenseF32, 1><<<grid, 512, 0, stream>>>(g);
+    else if (g.result == kDenseF16) dense_rows_i8<kDenseF16, 1><<<grid, 512, 0, stream>>>(g);
+    else dense_rows_i8<kDenseBF16, 1><<<grid, 512, 0, stream>>>(g);
+  } else if (g.whole) dense_rows<TYPE, KIND, FR, true><<<grid, 512, 0, stream>>>(g);
+  else dense_rows<TYPE, KIND, FR, false><<<grid, 512, 0, stream>>>(g);
   return hipGetLastError();
 }
 

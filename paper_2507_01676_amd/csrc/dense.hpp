@@ -52,6 +52,7 @@ struct DenseGemm {
   int64_t panel_a, panel_b[2];   // tiles: elements from a panel of columns to the next
   const float *scale_a, *scale_b;   // 8-bit integers: of the rows of A and of B
   int32_t result;                // 8-bit integers: DenseType of bias, residual and result
+  int32_t quantize;              // kRows of 8-bit integers: A is of the result's type, and quantized by the workgroups
 };
 
 // matrices copied to rows of whole 16-byte chunks, in panels

@@ -546,7 +546,7 @@ DenseChoice embx::dense_choose_i8(int64_t m, int64_t n, int64_t k) {
   for (const int variant : kTiles) {
     const double tiles = static_cast<double>(tiles_of(EMB_DTYPE_BF16, variant, m, n));
     if (!launches(EMB_DTYPE_BF16, variant, tiles)) continue;
-    for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial)); ++s) {
+    for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial && tiles * s <= 4 * kCus)); ++s) {
       const double us = tile_us(EMB_DTYPE_BF16, variant, tiles, steps, s, result_bytes);
       if (us < 0.98 * least) least = us, best = {variant, s, 0};
     }

@@ -50,7 +50,9 @@ struct Entry {
     if (code == EMB_ERR_INVALID_ARGUMENT) {
       size_t bytes = 0;
       code = size(&s, &bytes);
-      if (code == EMB_OK) {
+      if (code == EMB_OK && bytes == 0) {
+        code = run(&s, nullptr, 0, stream);
+      } else if (code == EMB_OK) {
         const at::Tensor ws = at::empty({static_cast<int64_t>(bytes)}, x.options().dtype(at::kByte));
         code = run(&s, ws.data_ptr(), bytes, stream);
       }
@@ -425,7 +427,8 @@ PyObject* linear_int8(PyObject*, Args a, Py_ssize_t count) {
       if (!eight && type != c.type) throw Refused(std::string("dtype must be x's, ") + type_name(c.type));
       c.type_is(type, "dtype");
     } else if (eight) {
-      c.type_is(at::kBFloat16, "dtype");
+      PyObject* const like = a[8] != Py_None ? a[8] : a[4] != Py_None ? a[4] : a[3];
+      c.type_is(THPVariable_Check(like) ? THPVariable_Unpack(like).scalar_type() : at::kBFloat16, "dtype");
     }
     const int64_t m = c.rows, k = c.cols, n = rows_of(a[1], "weight");
     const Matrix w = c.matrix(a[1], "weight", n, k, at::kChar), r = c.optional(a[4], "residual", m, n);

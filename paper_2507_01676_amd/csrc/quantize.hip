@@ -5,6 +5,7 @@
 
 #include "../../include/embx_serving.h"
 #include "dense_device.hpp"
+#include "quantize_device.hpp"
 #include "serving.hpp"
 
 namespace embx {
@@ -25,42 +26,6 @@ __device__ inline float value(uint32_t bits) {
   else return static_cast<float>(__builtin_bit_cast(_Float16, static_cast<uint16_t>(bits)));
 }
 
-constexpr float kRound = 0x1.8p23f;   // a float with this added has its whole part, rounded half to even, in its low bits
-
-// A row's scale from the largest of its magnitudes' bits; false where that is an infinity or NaN.
-struct Scale {
-  float s, inverse;
-  bool fine;
-
-  template <int TYPE>
-  __device__ static Scale of(uint32_t largest) {
-    Scale r;
-    const float most = value<TYPE>(largest);
-    r.fine = most < __builtin_inff();   // (NaN is not)
-    r.s = r.fine ? fmaxf(most / 127.0f, 0x1p-126f) : 1.0f;
-    r.inverse = 1.0f / r.s;
-    return r;
-  }
-
-  __device__ float stored() const { return fine ? s : __builtin_nanf(""); }
-
-  // x / s to the nearest whole number, half to even, exactly, in the low 8 bits of the result: x times the rounded
-  // reciprocal is off by less than one of the nearest, and what is left of x after it, x - r s, is exact near the borders
-  // (a multiple of the smaller operand's last place, and at most s).  *far: whether that is s / 2 or more, for mend().
-  __device__ uint32_t nearest(float x, bool* far) const {
-    const float u = fmaf(x, inverse, kRound), left = fmaf(kRound - u, s, x);
-    *far |= fabsf(left + left) >= s;
-    return __float_as_uint(u);
-  }
-
-  __device__ uint32_t mend(float x) const {
-    float u = fmaf(x, inverse, kRound);
-    const float left = fmaf(kRound - u, s, x), twice = fabsf(left + left);
-    if (twice > s || (twice == s && (__float_as_uint(u) & 1))) u += copysignf(1.0f, left);
-    return __float_as_uint(u);
-  }
-};
-
 // of LANES threads of a workgroup of 256
 template <int LANES>
 __device__ inline uint32_t most_of(uint32_t v) {
@@ -76,6 +41,14 @@ __device__ inline uint32_t most_of(uint32_t v) {
   return v;
 }
 
+// whether this workgroup copies instead
+__device__ inline bool copies(const Quantize& a) {
+  if (blockIdx.x < a.groups) return false;
+  const uint32_t id = blockIdx.x - a.groups;
+  pack_rows<uint8_t>(a.pack, id / a.pack.groups, id % a.pack.groups);
+  return true;
+}
+
 // A row in the registers of LANES threads, CH chunks of eight elements each: read once, 16 bytes at a time, and bound by
 // memory.  x's rows start at multiples of 16 bytes, q's at multiples of 8.
 template <int TYPE, int LANES, int CH>
@@ -83,9 +56,10 @@ __global__ __launch_bounds__(256) void quantize_held(Quantize a) {
   using V = typename Eight<TYPE>::V;
   constexpr int kRows = 256 / LANES;
   constexpr uint32_t kSign = TYPE == kDenseF32 ? 0x7fffffffu : 0x7fffu;
+  if (copies(a)) return;
   const int lane = threadIdx.x % LANES;
   const int chunks = (a.k + 7) / 8, wide = (a.padded + 7) / 8;
-  for (int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; i < a.m; i += int64_t(gridDim.x) * kRows) {
+  for (int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; i < a.m; i += int64_t(a.groups) * kRows) {
     const char* const x = static_cast<const char*>(a.x) + i * a.ldx * (TYPE == kDenseF32 ? 4 : 2);
     V v[CH], most = {};
 #pragma unroll
@@ -103,28 +77,19 @@ __global__ __launch_bounds__(256) void quantize_held(Quantize a) {
     uint32_t largest = most[0];
 #pragma unroll
     for (int e = 1; e < 8; ++e) largest = max(largest, static_cast<uint32_t>(most[e]));
-    const Scale s = Scale::of<TYPE>(most_of<LANES>(largest));
+    const Scale s = Scale::of(value<TYPE>(most_of<LANES>(largest)));
     if (lane == 0) a.scale[i] = s.stored();
     int8_t* const q = a.q + i * a.ldq;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int at = lane + c * LANES;
-      uint32_t u[8];
-      bool far = false;
+      float x[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) u[e] = s.nearest(value<TYPE>(v[c][e]), &far);
-      if (__any(far)) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = s.mend(value<TYPE>(v[c][e]));
-      }
-      u32x2 out;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-        out[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[4 * h + 3], u[4 * h + 2], 0x0c0c0400),
-                                       __builtin_amdgcn_perm(u[4 * h + 1], u[4 * h], 0x0c0c0400), 0x05040100);
-      if (!s.fine) out = u32x2{0, 0};
+      for (int e = 0; e < 8; ++e) x[e] = value<TYPE>(v[c][e]);
+      uint32_t out[2];
+      quantize8(s, x, out);
       if (at * 8 + 8 <= a.padded) {
-        *reinterpret_cast<u32x2*>(q + at * 8) = out;
+        *reinterpret_cast<u32x2*>(q + at * 8) = u32x2{out[0], out[1]};
       } else if (at < wide) {
         for (int e = 0; e < a.padded - at * 8; ++e) q[at * 8 + e] = static_cast<int8_t>(out[e >> 2] >> 8 * (e & 3));
       }
@@ -137,8 +102,9 @@ template <int TYPE, int LANES>
 __global__ __launch_bounds__(256) void quantize_any(Quantize a) {
   using T = typename Elem<TYPE>::T;
   constexpr int kRows = 256 / LANES, kMany = 8;   // elements of a thread under way
+  if (copies(a)) return;
   const int lane = threadIdx.x % LANES;
-  for (int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; i < a.m; i += int64_t(gridDim.x) * kRows) {
+  for (int64_t i = int64_t(blockIdx.x) * kRows + threadIdx.x / LANES; i < a.m; i += int64_t(a.groups) * kRows) {
     const T* const x = static_cast<const T*>(a.x) + i * a.ldx;
     uint32_t largest = 0;
     for (int j = lane; j < a.k; j += LANES * kMany) {
@@ -148,7 +114,7 @@ __global__ __launch_bounds__(256) void quantize_any(Quantize a) {
 #pragma unroll
       for (int e = 0; e < kMany; ++e) largest = max(largest, __float_as_uint(float(v[e])) & 0x7fffffffu);
     }
-    const Scale s = Scale::of<kDenseF32>(most_of<LANES>(largest));
+    const Scale s = Scale::of(__uint_as_float(most_of<LANES>(largest)));
     if (lane == 0) a.scale[i] = s.stored();
     int8_t* const q = a.q + i * a.ldq;
     for (int j = lane; j < a.padded; j += LANES * kMany) {
@@ -163,17 +129,24 @@ __global__ __launch_bounds__(256) void quantize_any(Quantize a) {
   }
 }
 
+// grid of a launch with rows of LANES threads
+template <int LANES>
+uint32_t grid_of(Quantize& a) {
+  a.groups = static_cast<uint32_t>(std::min<int64_t>((a.m + 256 / LANES - 1) / (256 / LANES), 1 << 20));
+  return a.groups + a.pack.count * a.pack.groups;
+}
+
 template <int TYPE, int LANES, int CH>
-int held(const Quantize& a, hipStream_t s) {
-  const int64_t groups = (a.m + 256 / LANES - 1) / (256 / LANES);
-  quantize_held<TYPE, LANES, CH><<<static_cast<uint32_t>(std::min<int64_t>(groups, 1 << 20)), 256, 0, s>>>(a);
+int held(Quantize a, hipStream_t s) {
+  const uint32_t grid = grid_of<LANES>(a);
+  quantize_held<TYPE, LANES, CH><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <int TYPE, int LANES>
-int any(const Quantize& a, hipStream_t s) {
-  const int64_t groups = (a.m + 256 / LANES - 1) / (256 / LANES);
-  quantize_any<TYPE, LANES><<<static_cast<uint32_t>(std::min<int64_t>(groups, 1 << 20)), 256, 0, s>>>(a);
+int any(Quantize a, hipStream_t s) {
+  const uint32_t grid = grid_of<LANES>(a);
+  quantize_any<TYPE, LANES><<<grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

@@ -15,6 +15,8 @@ struct Quantize {
   float* scale;
   int64_t ldx, ldq, m;
   int32_t k, padded;       // q's rows are written with zeros up to `padded` elements
+  DensePack pack;          // 8-bit matrices that the same launch copies
+  uint32_t groups;         // workgroups for the rows (set by the launch); those behind them copy
 };
 
 // A layer of experts.  The matrices: gate, up, down.

@@ -75,15 +75,14 @@ emb_status_t check_shape(const emb_linear_int8_t& a) {
   if (a.m < 0 || a.n < 1 || a.k < 1) return EMB_ERR_INVALID_ARGUMENT;
   EMBX_TRY(check_activation(a.activation));
   if (a.m > kMaxSize || a.n > kMaxSize || a.k > kMostInputs) return EMB_ERR_UNSUPPORTED;
-  EMBX_TRY(check_type(a.dtype));
-  return a.m > 0 && dense_choose_i8(a.m, a.n, a.k).variant < 0 ? EMB_ERR_UNSUPPORTED : EMB_OK;
+  return check_type(a.dtype);
 }
 
 // x as the products read it: 8-bit rows that end in zeros up to a whole chunk, so that what lies behind the weights' rows
 // counts for nothing.
 struct Int8Space {
   DenseChoice choice;
-  bool quantized, packed_x, packed_w;
+  bool inside, quantized, packed_x, packed_w;
   const int8_t *x, *w;
   int64_t ldx, ldw;
   const float* scale;
@@ -93,8 +92,11 @@ struct Int8Space {
 Int8Space int8_space(Arena& ar, const emb_linear_int8_t& a) {
   Int8Space s = {};
   s.choice = dense_choose_i8(a.m, a.n, a.k);
-  s.quantized = !a.x_scale;
-  s.packed_x = !s.quantized && !(whole(a.x, a.ldx) && a.k % 16 == 0);
+  // A few rows that a workgroup's registers hold are quantized by each of the product's workgroups.
+  s.inside = !a.x_scale && s.choice.variant == kRows && s.choice.row_blocks == 1 && a.m <= 8 &&
+             a.k * (a.m == 1 ? 1 : a.m == 2 ? 2 : a.m <= 4 ? 4 : 8) <= 16384;
+  s.quantized = !a.x_scale && !s.inside;
+  s.packed_x = a.x_scale && !(whole(a.x, a.ldx) && a.k % 16 == 0);
   s.packed_w = !whole(a.weight, a.ldw);
   s.x = static_cast<const int8_t*>(a.x), s.ldx = a.ldx, s.scale = a.x_scale;
   s.w = a.weight, s.ldw = a.ldw;
@@ -195,14 +197,14 @@ emb_status_t emb_quantize(const emb_quantize_t* a, void* stream) {
   EMBX_TRY(check_vector(a->scale, a->m, 4));
   if (a->m == 0) return EMB_OK;
   return run(quantize_launch(a->dtype, {a->x, a->q, a->scale, a->ldx, a->ldq, a->m, static_cast<int32_t>(a->k),
-                                        static_cast<int32_t>(a->k)}, stream));
+                                        static_cast<int32_t>(a->k), {}, 0}, stream));
 }
 
 emb_status_t emb_linear_int8_workspace(const emb_linear_int8_t* a, size_t* bytes) {
   if (!a || !bytes) return EMB_ERR_INVALID_ARGUMENT;
   EMBX_TRY(check_shape(*a));
   Arena ar{nullptr};
-  if (a->m > 0) int8_space(ar, *a);
+  if (a->m > 0 && int8_space(ar, *a).choice.variant < 0) return EMB_ERR_UNSUPPORTED;
   *bytes = ar.used;
   return EMB_OK;
 }
@@ -220,20 +222,23 @@ emb_status_t emb_linear_int8(const emb_linear_int8_t* a, void* workspace, size_t
   if (a->m == 0) return EMB_OK;
   Arena ar{static_cast<char*>(workspace)};
   const Int8Space s = int8_space(ar, *a);
+  if (s.choice.variant < 0) return EMB_ERR_UNSUPPORTED;
   EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
   DensePack pack = {};
   if (s.packed_x) add_copy(pack, a->x, a->ldx, s.x, a->m, a->k);
   if (s.packed_w) add_copy(pack, a->weight, a->ldw, s.w, a->n, a->k);
-  if (pack.count) EMBX_TRY(run(dense_pack_launch(pack, stream)));
   if (s.quantized)
     EMBX_TRY(run(quantize_launch(a->dtype, {a->x, const_cast<int8_t*>(s.x), const_cast<float*>(s.scale), a->ldx, s.ldx, a->m,
-                                            static_cast<int32_t>(a->k), static_cast<int32_t>(s.ldx)}, stream)));
+                                            static_cast<int32_t>(a->k), static_cast<int32_t>(s.ldx), pack, 0}, stream)));
+  else if (pack.count)
+    EMBX_TRY(run(dense_pack_launch(pack, stream)));
   DenseGemm g = {};
   g.a[0] = s.x, g.lda = s.ldx, g.panel_a = kPanel;
   g.b[0] = s.w, g.ldb[0] = s.ldw, g.panel_b[0] = kPanel;
   g.c[0] = a->y, g.ldc[0] = a->ldy;
   g.bias[0] = a->bias;
   g.res = a->residual, g.ldr = a->ldr;
+  g.quantize = s.inside;
   g.scale_a = s.scale, g.scale_b = a->w_scale;
   g.result = a->dtype == EMB_DTYPE_F32 ? kDenseF32 : a->dtype == EMB_DTYPE_F16 ? kDenseF16 : kDenseBF16;
   g.ni = static_cast<int32_t>(a->m), g.nj = static_cast<int32_t>(a->n), g.nr = static_cast<int32_t>(a->k);

@@ -14,8 +14,6 @@ from __future__ import annotations
 
 import ctypes
 
-import torch
-
 from . import _lib
 from .dense import _dense, _on
 
@@ -41,9 +39,6 @@ def linear_int8(x, weight, w_scale, bias=None, residual=None, *, x_scale=None, a
     if stream is not None:
         return _on(stream, linear_int8, x, weight, w_scale, bias, residual, x_scale=x_scale, activation=activation, dtype=dtype,
                    out=out)
-    if dtype is None and x_scale is not None:
-        like = next((t for t in (out, residual, bias) if t is not None), None)
-        dtype = torch.bfloat16 if like is None else like.dtype
     return _dense.linear_int8(x, weight, w_scale, bias, residual, x_scale, activation, dtype, out)
 
 
