@@ -437,9 +437,34 @@ struct Finish<kDenseI8, kForward> {
 template <int FJ>
 constexpr int kSumsLds = 64 * FJ * 64;   // (half of it with two fragments of rows)
 
+// Of 8-bit integers: what a lane's first four rows need from memory, which can be asked for before the sums are there.  (One
+// row after another, each waits for memory.)
+template <int TYPE, int KIND, int FJ>
+struct Asked {};
+template <int FJ>
+struct Asked<kDenseI8, kForward, FJ> {
+  static constexpr int kTogether = 4, kLanes = FJ * 2, kRows = 64 / kLanes;
+  using F = Finish<kDenseI8, kForward>;
+  F out;
+  typename F::Held held[kTogether];
+
+  // of a wavefront's sums from row i0 and column j0 on
+  __device__ Asked(const DenseGemm& g, int lane, int64_t i0, int j0)
+      : out(g, 0, i0 + lane / kLanes, min(j0 + lane % kLanes * 8, g.nj - 1), kRows) {
+    ask();
+  }
+
+  __device__ void ask() {
+#pragma unroll
+    for (int x = 0; x < kTogether; ++x) held[x] = out.ask(x);
+  }
+
+  __device__ void next() { out.i += kTogether * kRows; }
+};
+
 template <int TYPE, int KIND, int FI, int FJ>
 __device__ inline void store_sums(const DenseGemm& g, Sums<TYPE> (&acc)[FI][FJ], char* own, int lane, int64_t i0, int j0, int part,
-                                  int split) {
+                                  int split, const Asked<TYPE, KIND, FJ>* asked = nullptr) {
   constexpr bool kGate = KIND == kGated;
   constexpr int kRowBytes = FJ * 64, kMask = FJ * 4 - 1, kUp = FJ * 2;   // kUp: first chunk of the up projection
   constexpr int kPass = FI < 4 ? FI : 4;   // fragments of rows at a time
@@ -485,21 +510,25 @@ __device__ inline void store_sums(const DenseGemm& g, Sums<TYPE> (&acc)[FI][FJ],
           }
         }
       } else if constexpr (TYPE == kDenseI8) {
-        // four rows' scales and residuals are asked for together: one after another, each waits for memory
-        constexpr int kTogether = 4;
-        static_assert(kPass * 16 % (kTogether * kRows) == 0);
-        Finish<TYPE, KIND> out(g, part, first, j, kRows);
-#pragma unroll 1
-        for (int row0 = 0; row0 < kPass * 16; row0 += kTogether * kRows, out.i += kTogether * kRows) {
-          if (first + row0 >= g.ni) break;
-          typename Finish<TYPE, KIND>::Held held[kTogether];
+        using A = Asked<TYPE, KIND, FJ>;
+        static_assert(kPass * 16 % (A::kTogether * kRows) == 0 && A::kRows == kRows);
+        auto put = [&](const A& four, int row0) {
 #pragma unroll
-          for (int x = 0; x < kTogether; ++x) held[x] = out.ask(x);
-#pragma unroll
-          for (int x = 0; x < kTogether; ++x) {
+          for (int x = 0; x < A::kTogether; ++x) {
             if (first + row0 + x * kRows >= g.ni) break;
             sums(row0 + x * kRows + lane / kLanes, s0, s1);
-            out.put(s0, held[x], x);
+            four.out.put(s0, four.held[x], x);
+          }
+        };
+        if constexpr (kPass * 16 == A::kTogether * kRows) {   // (all of them)
+          if (first < g.ni) put(*asked, 0);
+        } else {
+          A four(g, lane, i0 + h * 64, j0);
+#pragma unroll 1
+          for (int row0 = 0; row0 < kPass * 16; row0 += A::kTogether * kRows) {
+            if (first + row0 >= g.ni) break;
+            if (row0 > 0) four.next(), four.ask();
+            put(four, row0);
           }
         }
       } else {
@@ -679,6 +708,11 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
   };
 
   const int wi = (wave / WJ) * kWI, wj = (wave % WJ) * kWJ;
+  // (asked for here, as a CU's one workgroup has nothing else to hide it: 4096 x 1024 x 1024 with a residual)
+  const auto asked = [&] {
+    if constexpr (TYPE == kDenseI8 && HALVES == 2) return Asked<TYPE, KIND, kFJ>(g, lane, int64_t(i0) + wi + half * 32, j0 + wj);
+    else return 0;
+  }();
   Sums<TYPE> acc[kFI][kFJ] = {};
   // fragments of a half step (not f32)
   auto fragments_a = [&](const char* sa, int ks, s16x8* f) {
@@ -920,7 +954,10 @@ __device__ __forceinline__ void tile_product(const DenseGemm& g, char* all, uint
     else take(2);
     char* const own = all + 2 * kGiven + (half * kWaves + wave) * (kSumsLds<kFJ> / 2);
     static_assert(2 * kGiven + kWaves * kSumsLds<kFJ> <= HALVES * kTileLds<TYPE, BM, BN, WJ, kWaves>);
-    store_sums<TYPE, KIND, 2, kFJ>(g, sum, own, lane, int64_t(i0) + wi + half * 32, j0 + wj, wpart, split);
+    if constexpr (TYPE == kDenseI8)
+      store_sums<TYPE, KIND, 2, kFJ>(g, sum, own, lane, int64_t(i0) + wi + half * 32, j0 + wj, wpart, split, &asked);
+    else
+      store_sums<TYPE, KIND, 2, kFJ>(g, sum, own, lane, int64_t(i0) + wi + half * 32, j0 + wj, wpart, split);
   } else {
     store_sums<TYPE, KIND, kFI, kFJ>(g, acc, lds + wave * kSumsLds<kFJ>, lane, int64_t(i0) + wi, j0 + wj, wpart, split);
   }
@@ -1192,27 +1229,31 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 // weights are on their way, instead of a launch before this one.
 constexpr int kQuantizedLds = 16640;   // up to 16384 elements
 
-template <int XT, int FR>
+template <int XT, int FR, int FJ>
 __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
   constexpr bool kQuantize = XT != kDenseI8;
-  constexpr int kRounds = 4;
+  constexpr int kRounds = 4 / FJ;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
-  const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
+  const uint32_t across = (g.nj + FJ * 16 - 1) / (FJ * 16), down = (g.ni + FR * 16 - 1) / (FR * 16);
   uint32_t i = blockIdx.x / across, j_ = blockIdx.x % across;
   if (down >= kXcds) {   // rows of x stay with one XCD's L2
     j_ = blockIdx.x / kXcds % across, i = blockIdx.x / (kXcds * across) * kXcds + blockIdx.x % kXcds;
     if (i >= down) return;
   }
-  const int i0 = i * FR * 16, j0 = j_ * 16;
-  const int8_t* const weights = static_cast<const int8_t*>(g.b[0]) + min(j0 + c, g.nj - 1) * g.ldb[0];
+  const int i0 = i * FR * 16, j0 = j_ * FJ * 16;
+  const int8_t* weights[FJ];
+#pragma unroll
+  for (int f = 0; f < FJ; ++f) weights[f] = static_cast<const int8_t*>(g.b[0]) + min(j0 + f * 16 + c, g.nj - 1) * g.ldb[0];
   const int last = (g.nr - 1) / 16 * 16;   // the last chunk of a row; what lies behind the row's end meets zeros of x
-  s16x8 w[2][kRounds][2];
-  auto ask = [&](s16x8 (*to)[2], int r0) {
+  s16x8 w[2][kRounds][2][FJ];
+  auto ask = [&](s16x8 (*to)[2][FJ], int r0) {
 #pragma unroll
     for (int r = 0; r < kRounds; ++r)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
-        to[r][h] = *reinterpret_cast<const s16x8*>(weights + min(r0 + r * 1024 + h * 64 + q * 16, last));
+#pragma unroll
+        for (int f = 0; f < FJ; ++f)
+          to[r][h][f] = *reinterpret_cast<const s16x8*>(weights[f] + min(r0 + r * 1024 + h * 64 + q * 16, last));
   };
   ask(w[0], wave * 128);
   __shared__ __align__(16) int8_t quantized[kQuantize ? kQuantizedLds : 16];
@@ -1235,6 +1276,7 @@ __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int at = (first + n * each * 64) * 8;
+      if (n * each * 512 >= wide) break;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (at + e >= g.nr) v[n][e] = 0.0f;
@@ -1244,12 +1286,14 @@ __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
     for (int step = 32; step > 0; step >>= 1) largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), step)));
     if (lane == 0) most[wave] = largest;
     __syncthreads();
-    for (int n = 0; n < each; ++n) largest = max(largest, most[wave / each * each + n]);
+#pragma unroll
+    for (int n = 0; n < 8; ++n) largest = max(largest, most[row * each + (n & (each - 1))]);
     const Scale s = Scale::of(__uint_as_float(largest));
     if (mine && first == 0) row_scale[row] = s.stored();
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int at = (first + n * each * 64) * 8;
+      if (n * each * 512 >= wide) break;
       uint32_t out[2];
       quantize8(s, v[n], out);
       if (mine && at < wide - 16) *reinterpret_cast<uint2*>(quantized + row * wide + at) = uint2{out[0], out[1]};
@@ -1261,8 +1305,8 @@ __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
   for (int f = 0; f < FR; ++f)
     rows[f] = kQuantize ? quantized + min(c, g.ni - 1) * wide
                         : static_cast<const int8_t*>(g.a[0]) + min(i0 + f * 16 + c, g.ni - 1) * g.lda;
-  i32x4 acc[FR] = {};
-  auto multiply = [&](const s16x8 (*with)[2], int r0) {
+  i32x4 acc[FR][FJ] = {};
+  auto multiply = [&](const s16x8 (*with)[2][FJ], int r0) {
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
       if (r0 + r * 1024 >= g.nr) break;
@@ -1273,7 +1317,8 @@ __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
         for (int f = 0; f < FR; ++f) {
           s16x8 x = *reinterpret_cast<const s16x8*>(rows[f] + (kQuantize ? at : min(at, last)));
           if (!kQuantize && at >= g.nr) x = s16x8{};
-          acc[f] = mfma16<kDenseI8>(with[r][h], x, acc[f]);
+#pragma unroll
+          for (int j = 0; j < FJ; ++j) acc[f][j] = mfma16<kDenseI8>(with[r][h][j], x, acc[f][j]);
         }
       }
     }
@@ -1285,10 +1330,13 @@ __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
     if (r0 + 2 * kRounds * 1024 < g.nr) ask(w[0], r0 + 2 * kRounds * 1024);
     multiply(w[1], r0 + kRounds * 1024);
   }
-  __shared__ int sums[8][FR][16][16];   // [wavefront][..][row][column]
+  __shared__ int sums[8][FR * 16][FJ * 16];   // [wavefront][row][column]
 #pragma unroll
-  for (int f = 0; f < FR; ++f) *reinterpret_cast<i32x4*>(&sums[wave][f][c][4 * q]) = acc[f];
-  const int t = threadIdx.x, row = t >> 1, j = j0 + (t & 1) * 8;
+  for (int f = 0; f < FR; ++f)
+#pragma unroll
+    for (int j = 0; j < FJ; ++j) *reinterpret_cast<i32x4*>(&sums[wave][f * 16 + c][j * 16 + 4 * q]) = acc[f][j];
+  constexpr int kEights = FJ * 2;   // of a row
+  const int row = threadIdx.x / kEights, column = threadIdx.x % kEights * 8, j = j0 + column;
   const bool in = row < FR * 16 && i0 + row < g.ni && j < g.nj;
   Finish<kDenseI8, kForward> out(g, 0, min(i0 + row, g.ni - 1), min(j, g.nj - 1), 0);
   typename Finish<kDenseI8, kForward>::Held held = {};
@@ -1303,7 +1351,7 @@ __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
   for (int e = 0; e < 8; ++e) {
     int sum = 0;
 #pragma unroll
-    for (int n = 0; n < 8; ++n) sum += sums[n][row >> 4][row & 15][(t & 1) * 8 + e];
+    for (int n = 0; n < 8; ++n) sum += sums[n][row][column + e];
     s[e] = __int_as_float(sum);
   }
   out.put(s, held, 0);
@@ -1598,10 +1646,12 @@ int rows_launch(const DenseGemm& g, hipStream_t stream) {
   const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
   const uint32_t grid = across * (down >= kXcds ? (down + kXcds - 1) / kXcds * kXcds : down);
   if constexpr (TYPE == kDenseI8) {
-    if (FR > 1 || !g.quantize) dense_rows_i8<kDenseI8, FR><<<grid, 512, 0, stream>>>(g);
-    else if (g.result == kDenseF32) dense_rows_i8<kDenseF32, 1><<<grid, 512, 0, stream>>>(g);
-    else if (g.result == kDenseF16) dense_rows_i8<kDenseF16, 1><<<grid, 512, 0, stream>>>(g);
-    else dense_rows_i8<kDenseBF16, 1><<<grid, 512, 0, stream>>>(g);
+    const uint32_t wide = (g.nj + 31) / 32;
+    if ((FR > 1 || !g.quantize) && down < kXcds && wide * down >= 256) dense_rows_i8<kDenseI8, FR, 2><<<wide * down, 512, 0, stream>>>(g);
+    else if (FR > 1 || !g.quantize) dense_rows_i8<kDenseI8, FR, 1><<<grid, 512, 0, stream>>>(g);
+    else if (g.result == kDenseF32) dense_rows_i8<kDenseF32, 1, 1><<<grid, 512, 0, stream>>>(g);
+    else if (g.result == kDenseF16) dense_rows_i8<kDenseF16, 1, 1><<<grid, 512, 0, stream>>>(g);
+    else dense_rows_i8<kDenseBF16, 1, 1><<<grid, 512, 0, stream>>>(g);
   } else if (g.whole) dense_rows<TYPE, KIND, FR, true><<<grid, 512, 0, stream>>>(g);
   else dense_rows<TYPE, KIND, FR, false><<<grid, 512, 0, stream>>>(g);
   return hipGetLastError();
