@@ -38,8 +38,8 @@
  * A call's outputs and workspace must not overlap its inputs, except that linear_int8's y may
  * be the residual itself (same pointer and row stride).  Calls that share a workspace must
  * not overlap in time.  Nothing is kept between calls, and equal calls give equal bits.
- * Of 8-bit rows that start at multiples of 16 bytes, the 16 bytes that hold a row's end are
- * read whole; what they hold behind it does not matter.
+ * Where an operand's rows start at multiples of 16 bytes, the 16 bytes that hold a row's end
+ * are read whole; what they hold behind it does not matter.
  *
  * Errors (emb_status_t of embx.h): EMB_ERR_INVALID_ARGUMENT for a NULL or misaligned pointer,
  * a size below its least (m >= 0, the others >= 1), a row stride below its row, top_k above

@@ -159,6 +159,18 @@ double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int6
   return 3.0 + steps * step * two * load * idle;
 }
 
+// Microseconds of the kernel of few rows of 8-bit integers, measured on 1 to 512 rows by 16 to 8192 columns and 64 to 12800
+// inputs: of each round of workgroups, and of each 1024 of the reduction in it, with 16 or 32 columns a workgroup (which the
+// launch chooses).
+double rows_i8_us(int blocks, int64_t m, int64_t n, int64_t k) {
+  const double down = double((m + 16 * blocks - 1) / (16 * blocks)), wide = double((n + 31) / 32);
+  const bool two = down < kXcds && wide * down >= kCus;
+  const int at = (blocks == 1 ? 0 : blocks == 2 ? 1 : 2) + (two ? 3 : 0);
+  static const double kRound[] = {1.6, 1.8, 2.2, 1.2, 1.6, 2.6}, kStep[] = {0.8, 1.2, 2.05, 1.25, 1.6, 2.3};
+  const double rounds = std::max(1.0, down * (two ? wide : double((n + 15) / 16)) / kCus);
+  return 3.0 + rounds * (kRound[at] + kStep[at] * std::max(1.0, k / 1024.0));
+}
+
 // The same of the kernel for short reductions: its workgroups (the launch's own arithmetic), each with `rows` chunks of 64
 // rows one after another.  A chunk takes 6.6 us in f32 (4 of at most 32 inputs) and 3 (2.2) in 16 bits where a CU has one
 // workgroup, and two to four share a CU at 0.85 of each one's time.
@@ -538,7 +550,7 @@ emb_status_t run_pack(const DensePack& p, void* stream) {
 }  // namespace
 
 // Products of 8-bit integers: the same tiles take as long for a step of 128 bytes as with 16-bit elements, of which it holds
-// half as many, and so does the kernel of few rows.
+// half as many.
 DenseChoice embx::dense_choose_i8(int64_t m, int64_t n, int64_t k) {
   const double steps = std::ceil(k / 128.0), result_bytes = 4.0 * m * n;
   Choice best = {-1, 1, 0}, few = {kRows, 1, 1};
@@ -552,13 +564,14 @@ DenseChoice embx::dense_choose_i8(int64_t m, int64_t n, int64_t k) {
     }
   }
   least += kCallUs;
+  if (k <= 128) least += 1.5 + 2.0 * m * n / 5.1e6;   // a tile's first loads and its results are all
   for (const int blocks : {1, 2, 4}) {
     if (blocks > 1 && m <= 8 * blocks) break;
     if (512.0 * ((n + 15) / 16) * ((m + 16 * blocks - 1) / (16 * blocks) + kXcds) > kMostThreads) continue;
-    const double us = rows_us(EMB_DTYPE_BF16, 1, true, blocks, m, n, (k + 1) / 2);
+    const double us = rows_i8_us(blocks, m, n, k);
     if (us < few_us) few_us = us, few.row_blocks = blocks;
   }
-  return few_us <= least ? few : best;
+  return few_us < HUGE_VAL && few_us <= least ? few : best;
 }
 
 extern "C" {

@@ -63,7 +63,15 @@ __global__ __launch_bounds__(256) void quantize_held(Quantize a) {
     const char* const x = static_cast<const char*>(a.x) + i * a.ldx * (TYPE == kDenseF32 ? 4 : 2);
     V v[CH], most = {};
 #pragma unroll
-    for (int c = 0; c < CH; ++c) v[c] = reinterpret_cast<const V*>(x)[min(lane + c * LANES, chunks - 1)];
+    for (int c = 0; c < CH; ++c) {
+      const int at = min(lane + c * LANES, chunks - 1) * 8;
+      if constexpr (TYPE == kDenseF32) {   // (16 bytes with none of the row's elements are not read)
+        __builtin_memcpy(&v[c], __builtin_assume_aligned(x + at * int64_t(4), 16), 16);
+        __builtin_memcpy(reinterpret_cast<char*>(&v[c]) + 16, __builtin_assume_aligned(x + min(at + 4, (a.k - 1) / 4 * 4) * int64_t(4), 16), 16);
+      } else {
+        v[c] = *reinterpret_cast<const V*>(x + at * int64_t(2));
+      }
+    }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int at = lane + c * LANES;
@@ -154,7 +162,7 @@ template <int TYPE>
 int launch(const Quantize& a, hipStream_t s) {
   constexpr int kSize = TYPE == kDenseF32 ? 4 : 2;
   const bool whole = reinterpret_cast<uintptr_t>(a.x) % 16 == 0 && a.ldx * kSize % 16 == 0 &&
-                     reinterpret_cast<uintptr_t>(a.q) % 8 == 0 && a.ldq % 8 == 0 && a.ldx >= (a.k + 7) / 8 * 8;
+                     reinterpret_cast<uintptr_t>(a.q) % 8 == 0 && a.ldq % 8 == 0;
   const int chunks = std::max(a.k, a.padded) <= 16384 ? (std::max(a.k, a.padded) + 7) / 8 : 0;
   if (!whole || chunks == 0) return a.k <= 128 ? any<TYPE, 16>(a, s) : a.k <= 2048 ? any<TYPE, 64>(a, s) : any<TYPE, 256>(a, s);
   if (chunks <= 8) return held<TYPE, 8, 1>(a, s);

@@ -379,3 +379,35 @@ def test_streams(gpu_lib):
     y2 = gpu_lib.linear_int8(xs[1], *p["first"], p["bias"])
     assert torch.equal(y, y2)
     assert torch.equal(z, gpu_lib.moe_ffn(y2, p["router"], *p["ws"], top_k=2, scales=p["scales"]))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("k", [1, 3, 4, 5, 12, 13, 31, 100])
+def test_rows_that_end_inside_16_bytes(gpu_lib, dtype, k):
+    """Rows that start at multiples of 16 bytes and end inside of some: what lies behind them, NaN, is not used."""
+    import torch
+    gen = generator(k)
+    m, e = 5, 4
+
+    def padded(t):
+        big = torch.full((*t.shape[:-1], (t.shape[-1] + 15) // 16 * 16), float("nan") if t.is_floating_point() else 77, dtype=t.dtype, device="cuda")
+        big[..., :t.shape[-1]] = t
+        return big[..., :t.shape[-1]]
+
+    x, w, ws = padded(normal(gen, dtype, m, k)), padded(eights(gen, 40, k)), some(gen, 40)
+    q, s = gpu_lib.quantize_rows(x)
+    want_q, want_s = S.quantize(x)
+    assert torch.equal(R.d(q), want_q) and torch.equal(R.d(s), want_s)
+    R.check(gpu_lib.linear_int8(x, w, ws), S.linear_int8(q, s, w, ws, None, None, "none", dtype), "quantized inside")
+    many = padded(normal(gen, dtype, 300, k))
+    R.check(gpu_lib.linear_int8(many, w, ws), S.linear_int8(*S.quantize(many), w, ws, None, None, "none", dtype), "quantized before")
+    for f in (7, 40):
+        router = padded(normal(gen, dtype, e, k))
+        mats = [padded(normal(gen, dtype, e, f, k)), padded(normal(gen, dtype, e, f, k)), padded(normal(gen, dtype, e, k, f))]
+        for rows in (x, many[:70]):
+            want, _, _ = S.moe(rows, router, *mats, 2, "silu", dtype)
+            R.check(gpu_lib.moe_ffn(rows, router, *mats, top_k=2), want, "experts")
+        eight = [padded(eights(gen, *t.shape)) for t in mats]
+        scales = tuple(some(gen, *t.shape[:2], of=0.01) for t in mats)
+        want, _, _ = S.moe(x, router, *eight, 2, "silu", dtype, scales)
+        R.check(gpu_lib.moe_ffn(x, router, *eight, top_k=2, scales=scales), want, "experts of 8 bits")
