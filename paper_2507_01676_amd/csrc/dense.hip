@@ -1229,8 +1229,48 @@ __global__ __launch_bounds__(512) void dense_rows(DenseGemm g) {
 // weights are on their way, instead of a launch before this one.
 constexpr int kQuantizedLds = 16640;   // up to 16384 elements
 
-template <int XT, int FR, int FJ>
-__global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
+// Sixteen bytes of a row, at a multiple of ALIGN bytes: 16, 4 or 1.  At odd addresses, the words that they lie in, shifted when
+// they are needed (16-byte loads there take twice as long: 4 x 2100 x 11991 25.7 us, so 18.3; at multiples of 4 13.4, so 18.5).
+// Where rows do not start at multiples of 16, `left` bytes can be read from p on, at least one: to the end of the matrix.  No
+// word without one of them is read.
+template <int ALIGN>
+struct Eights {
+  i32x4 v;
+  int more[ALIGN == 1 ? 1 : 0];
+
+  __device__ static Eights load(const int8_t* p, int64_t left) {
+    Eights e;
+    if constexpr (ALIGN == 16) {
+      e.v = *reinterpret_cast<const i32x4*>(p);
+    } else {
+      const uintptr_t shift = ALIGN == 1 ? reinterpret_cast<uintptr_t>(p) & 3 : 0;
+      const int8_t* const a = p - shift;
+      const int64_t last = left >= 16 ? 16 : (shift + left - 1) / 4 * 4;
+      if (left >= 16) {
+        __builtin_memcpy(&e.v, __builtin_assume_aligned(a, 4), 16);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e.v[i] = *reinterpret_cast<const int*>(a + min(int64_t(4 * i), last));
+      }
+      if constexpr (ALIGN == 1) e.more[0] = *reinterpret_cast<const int*>(a + (shift ? min(int64_t(16), last) : 0));
+    }
+    return e;
+  }
+
+  // row: any address as far from a multiple of 4 as p was
+  __device__ s16x8 get(const int8_t* row) const {
+    i32x4 out = v;
+    if constexpr (ALIGN == 1) {
+      const uint32_t shift = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(row)) & 3;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[i] = __builtin_amdgcn_alignbyte(i < 3 ? v[i + 1] : more[0], v[i], shift);
+    }
+    return __builtin_bit_cast(s16x8, out);
+  }
+};
+
+template <int XT, int FR, int FJ, int ALIGN>
+__global__ __launch_bounds__(512, (FR > 1 && ALIGN < 16 ? 2 : 4)) void dense_rows_i8(DenseGemm g) {
   constexpr bool kQuantize = XT != kDenseI8;
   constexpr int kRounds = 4 / FJ;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
@@ -1245,20 +1285,29 @@ __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
 #pragma unroll
   for (int f = 0; f < FJ; ++f) weights[f] = static_cast<const int8_t*>(g.b[0]) + min(j0 + f * 16 + c, g.nj - 1) * g.ldb[0];
   const int last = (g.nr - 1) / 16 * 16;   // the last chunk of a row; what lies behind the row's end meets zeros of x
-  s16x8 w[2][kRounds][2][FJ];
-  auto ask = [&](s16x8 (*to)[2][FJ], int r0) {
+  using Raw = Eights<ALIGN>;
+  // (rows at any alignment are read up to the end of the matrix, `after` bytes behind the row's)
+  auto chunk = [&](const int8_t* row, int at, int64_t after) {
+    at = min(at, last);
+    return Raw::load(row + at, g.nr - at + after);
+  };
+  int64_t after_w[FJ];
+#pragma unroll
+  for (int f = 0; f < FJ; ++f) after_w[f] = (g.nj - 1 - min(j0 + f * 16 + c, g.nj - 1)) * g.ldb[0];
+  Raw w[2][kRounds][2][FJ];
+  auto ask = [&](Raw (*to)[2][FJ], int r0) {
 #pragma unroll
     for (int r = 0; r < kRounds; ++r)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int f = 0; f < FJ; ++f)
-          to[r][h][f] = *reinterpret_cast<const s16x8*>(weights[f] + min(r0 + r * 1024 + h * 64 + q * 16, last));
+          to[r][h][f] = chunk(weights[f], r0 + r * 1024 + h * 64 + q * 16, after_w[f]);
   };
   ask(w[0], wave * 128);
   __shared__ __align__(16) int8_t quantized[kQuantize ? kQuantizedLds : 16];
   __shared__ float row_scale[8];
-  const int wide = (g.nr + 127) / 128 * 128 + 16;   // of a row in LDS: 16 rows' chunks lie in different banks
+  const int row_bytes = (g.nr + 127) / 128 * 128 + 16;   // of a row in LDS: 16 rows' chunks lie in different banks
   if constexpr (kQuantize) {
     using T = typename Elem<XT>::T;
     __shared__ uint32_t most[8];
@@ -1276,7 +1325,7 @@ __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int at = (first + n * each * 64) * 8;
-      if (n * each * 512 >= wide) break;
+      if (n * each * 512 >= row_bytes) break;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (at + e >= g.nr) v[n][e] = 0.0f;
@@ -1293,32 +1342,43 @@ __global__ __launch_bounds__(512, 4) void dense_rows_i8(DenseGemm g) {
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int at = (first + n * each * 64) * 8;
-      if (n * each * 512 >= wide) break;
+      if (n * each * 512 >= row_bytes) break;
       uint32_t out[2];
       quantize8(s, v[n], out);
-      if (mine && at < wide - 16) *reinterpret_cast<uint2*>(quantized + row * wide + at) = uint2{out[0], out[1]};
+      if (mine && at < row_bytes - 16) *reinterpret_cast<uint2*>(quantized + row * row_bytes + at) = uint2{out[0], out[1]};
     }
     __syncthreads();
   }
   const int8_t* rows[FR];
+  int64_t after_x[FR];
 #pragma unroll
-  for (int f = 0; f < FR; ++f)
-    rows[f] = kQuantize ? quantized + min(c, g.ni - 1) * wide
-                        : static_cast<const int8_t*>(g.a[0]) + min(i0 + f * 16 + c, g.ni - 1) * g.lda;
+  for (int f = 0; f < FR; ++f) {
+    const int row = min(i0 + f * 16 + c, g.ni - 1);
+    rows[f] = kQuantize ? quantized + row * row_bytes : static_cast<const int8_t*>(g.a[0]) + row * g.lda;
+    after_x[f] = (g.ni - 1 - row) * g.lda;
+  }
   i32x4 acc[FR][FJ] = {};
-  auto multiply = [&](const s16x8 (*with)[2][FJ], int r0) {
+  auto multiply = [&](const Raw (*with)[2][FJ], int r0) {
 #pragma unroll
     for (int r = 0; r < kRounds; ++r) {
       if (r0 + r * 1024 >= g.nr) break;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int at = r0 + r * 1024 + h * 64 + q * 16;
+        s16x8 wide[FJ];
+#pragma unroll
+        for (int j = 0; j < FJ; ++j) wide[j] = with[r][h][j].get(weights[j]);
 #pragma unroll
         for (int f = 0; f < FR; ++f) {
-          s16x8 x = *reinterpret_cast<const s16x8*>(rows[f] + (kQuantize ? at : min(at, last)));
-          if (!kQuantize && at >= g.nr) x = s16x8{};
+          s16x8 x;
+          if constexpr (kQuantize) {
+            x = *reinterpret_cast<const s16x8*>(rows[f] + at);
+          } else {
+            x = chunk(rows[f], at, after_x[f]).get(rows[f]);
+            if (at + 16 > g.nr) x = keep16(x, g.nr - at);
+          }
 #pragma unroll
-          for (int j = 0; j < FJ; ++j) acc[f][j] = mfma16<kDenseI8>(with[r][h][j], x, acc[f][j]);
+          for (int j = 0; j < FJ; ++j) acc[f][j] = mfma16<kDenseI8>(wide[j], x, acc[f][j]);
         }
       }
     }
@@ -1490,7 +1550,8 @@ __global__ __launch_bounds__(256) void dense_short(DenseGemm g) {
 
 template <class E>
 __global__ __launch_bounds__(256) void dense_pack(DensePack p) {
-  pack_rows<E>(p, blockIdx.x / p.groups, blockIdx.x % p.groups);
+  if constexpr (sizeof(E) == 1) pack_eights(p, blockIdx.x / p.groups, blockIdx.x % p.groups);
+  else pack_rows<E>(p, blockIdx.x / p.groups, blockIdx.x % p.groups);
 }
 
 // dz (or dg and du), and the sums of their columns over a block of rows.  A thread has eight columns and every
@@ -1641,17 +1702,30 @@ int tail_launch(const DenseGemm& w, const DenseGemm& x, const DenseColsum& c, hi
   return hipGetLastError();
 }
 
+template <int FR, int ALIGN>
+int rows_i8_launch(const DenseGemm& g, uint32_t grid, uint32_t down, hipStream_t stream) {
+  const uint32_t wide = (g.nj + 31) / 32;
+  if (FR > 1 || !g.quantize) {
+    // 32 columns, which read x half as often, where there are workgroups enough (19 x 8192 x 4096 11.8 us, with 16 13.5)
+    if (down < kXcds && wide * down >= 256) dense_rows_i8<kDenseI8, FR, 2, ALIGN><<<wide * down, 512, 0, stream>>>(g);
+    else dense_rows_i8<kDenseI8, FR, 1, ALIGN><<<grid, 512, 0, stream>>>(g);
+  } else if (g.result == kDenseF32) {
+    dense_rows_i8<kDenseF32, 1, 1, ALIGN><<<grid, 512, 0, stream>>>(g);
+  } else if (g.result == kDenseF16) {
+    dense_rows_i8<kDenseF16, 1, 1, ALIGN><<<grid, 512, 0, stream>>>(g);
+  } else {
+    dense_rows_i8<kDenseBF16, 1, 1, ALIGN><<<grid, 512, 0, stream>>>(g);
+  }
+  return hipGetLastError();
+}
+
 template <int TYPE, int KIND, int FR>
 int rows_launch(const DenseGemm& g, hipStream_t stream) {
   const uint32_t across = (g.nj + 15) / 16, down = (g.ni + FR * 16 - 1) / (FR * 16);
   const uint32_t grid = across * (down >= kXcds ? (down + kXcds - 1) / kXcds * kXcds : down);
   if constexpr (TYPE == kDenseI8) {
-    const uint32_t wide = (g.nj + 31) / 32;
-    if ((FR > 1 || !g.quantize) && down < kXcds && wide * down >= 256) dense_rows_i8<kDenseI8, FR, 2><<<wide * down, 512, 0, stream>>>(g);
-    else if (FR > 1 || !g.quantize) dense_rows_i8<kDenseI8, FR, 1><<<grid, 512, 0, stream>>>(g);
-    else if (g.result == kDenseF32) dense_rows_i8<kDenseF32, 1, 1><<<grid, 512, 0, stream>>>(g);
-    else if (g.result == kDenseF16) dense_rows_i8<kDenseF16, 1, 1><<<grid, 512, 0, stream>>>(g);
-    else dense_rows_i8<kDenseBF16, 1, 1><<<grid, 512, 0, stream>>>(g);
+    if (g.whole == 16) return rows_i8_launch<FR, 16>(g, grid, down, stream);
+    return g.whole == 4 ? rows_i8_launch<FR, 4>(g, grid, down, stream) : rows_i8_launch<FR, 1>(g, grid, down, stream);
   } else if (g.whole) dense_rows<TYPE, KIND, FR, true><<<grid, 512, 0, stream>>>(g);
   else dense_rows<TYPE, KIND, FR, false><<<grid, 512, 0, stream>>>(g);
   return hipGetLastError();

@@ -47,7 +47,8 @@ struct DenseGemm {
   int32_t variant;         // DenseVariant
   int32_t row_blocks;      // kRows: 16 rows each, of a workgroup: 1, 2 or 4
   int32_t row_chunks, short_waves;   // kShort: chunks of 64 rows of a workgroup, its wavefronts along columns
-  int32_t whole;           // kRows, kShort: operands' rows start at multiples of 16 bytes and hold whole chunks
+  int32_t whole;           // kRows, kShort: operands' rows start at multiples of 16 bytes and hold whole chunks; of 8-bit
+                           // integers: they start at multiples of so many bytes, 16 (and hold whole chunks of x), 4 or 1
   int32_t slots, first;    // tiles: partial sums, the splits of all launches, and the first one of this
   int64_t panel_a, panel_b[2];   // tiles: elements from a panel of columns to the next
   const float *scale_a, *scale_b;   // 8-bit integers: of the rows of A and of B
@@ -94,7 +95,9 @@ struct DenseColsum {
 // times 16 rows a workgroup has.
 struct DenseChoice { int32_t variant, splits, row_blocks; };
 
-DenseChoice dense_choose_i8(int64_t m, int64_t n, int64_t k);   // of 8-bit integers; variant -1: too large for a launch
+// Of 8-bit integers; `align`: DenseGemm::whole; `copied`: bytes of operands that tiles would have copied first.  Variant -1:
+// too large for a launch.
+DenseChoice dense_choose_i8(int64_t m, int64_t n, int64_t k, int align, double copied);
 
 int dense_pack_launch(const DensePack& p, void* stream);
 

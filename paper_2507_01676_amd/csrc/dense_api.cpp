@@ -90,7 +90,13 @@ constexpr int kCus = 256;
 // halves, which take two steps at a time, with f32 by 256 x 128 or 128 x 128.
 struct TileTime { double alone, full; int per_cu; double ends; int at_a_time; };
 
+constexpr int32_t kInt8 = -8;   // "type" of products of 8-bit integers
+
 TileTime tile_time(int32_t dtype, int variant) {
+  // (a step of 128 bytes holds twice as many 8-bit integers as of 16; their results take longer, with both scales)
+  if (dtype == kInt8)
+    return variant == kTile256 ? TileTime{0.95, 1.54, 1, 11.0, 1}
+                               : variant == kTile128 ? TileTime{0.60, 1.08, 2, 5.0, 1} : TileTime{0.47, 0.55, 1, 4.3, 2};
   if (dtype == EMB_DTYPE_F32) return variant == kTile256 ? TileTime{2.05, 2.35, 1, 3.0, 1} : TileTime{1.17, 1.30, 1, 3.0, 1};
   return variant == kTile256 ? TileTime{0.97, 1.50, 1, 3.0, 1}
                              : variant == kTile128 ? TileTime{0.62, 1.03, 2, 3.0, 1} : TileTime{0.49, 0.55, 1, 2.6, 2};
@@ -162,13 +168,14 @@ double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int6
 // Microseconds of the kernel of few rows of 8-bit integers, measured on 1 to 512 rows by 16 to 8192 columns and 64 to 12800
 // inputs: of each round of workgroups, and of each 1024 of the reduction in it, with 16 or 32 columns a workgroup (which the
 // launch chooses).
-double rows_i8_us(int blocks, int64_t m, int64_t n, int64_t k) {
+double rows_i8_us(int blocks, int64_t m, int64_t n, int64_t k, int align) {
   const double down = double((m + 16 * blocks - 1) / (16 * blocks)), wide = double((n + 31) / 32);
   const bool two = down < kXcds && wide * down >= kCus;
   const int at = (blocks == 1 ? 0 : blocks == 2 ? 1 : 2) + (two ? 3 : 0);
   static const double kRound[] = {1.6, 1.8, 2.2, 1.2, 1.6, 2.6}, kStep[] = {0.8, 1.2, 2.05, 1.25, 1.6, 2.3};
   const double rounds = std::max(1.0, down * (two ? wide : double((n + 15) / 16)) / kCus);
-  return 3.0 + rounds * (kRound[at] + kStep[at] * std::max(1.0, k / 1024.0));
+  const double slower = align == 16 ? 1.0 : align == 4 ? 1.2 : blocks == 1 ? 1.5 : 2.0;
+  return 3.0 + rounds * (kRound[at] + kStep[at] * std::max(1.0, k / 1024.0)) * slower;
 }
 
 // The same of the kernel for short reductions: its workgroups (the launch's own arithmetic), each with `rows` chunks of 64
@@ -549,26 +556,26 @@ emb_status_t run_pack(const DensePack& p, void* stream) {
 
 }  // namespace
 
-// Products of 8-bit integers: the same tiles take as long for a step of 128 bytes as with 16-bit elements, of which it holds
-// half as many.
-DenseChoice embx::dense_choose_i8(int64_t m, int64_t n, int64_t k) {
+// Products of 8-bit integers: the same tiles, whose steps hold twice as many of the reduction as of 16-bit elements.
+DenseChoice embx::dense_choose_i8(int64_t m, int64_t n, int64_t k, int align, double copied) {
   const double steps = std::ceil(k / 128.0), result_bytes = 4.0 * m * n;
   Choice best = {-1, 1, 0}, few = {kRows, 1, 1};
   double least = HUGE_VAL, few_us = HUGE_VAL;
   for (const int variant : kTiles) {
-    const double tiles = static_cast<double>(tiles_of(EMB_DTYPE_BF16, variant, m, n));
-    if (!launches(EMB_DTYPE_BF16, variant, tiles)) continue;
+    const double tiles = static_cast<double>(tiles_of(kInt8, variant, m, n));
+    if (!launches(kInt8, variant, tiles)) continue;
     for (int s = 1; s <= 128 && (s == 1 || (s * 4 <= steps && result_bytes * s <= kMostPartial && tiles * s <= 4 * kCus)); ++s) {
-      const double us = tile_us(EMB_DTYPE_BF16, variant, tiles, steps, s, result_bytes);
+      const double us = tile_us(kInt8, variant, tiles, steps, s, result_bytes);
       if (us < 0.98 * least) least = us, best = {variant, s, 0};
     }
   }
   least += kCallUs;
+  if (copied > 0) least += 2.0 + copied / 2.2e6;
   if (k <= 128) least += 1.5 + 2.0 * m * n / 5.1e6;   // a tile's first loads and its results are all
   for (const int blocks : {1, 2, 4}) {
     if (blocks > 1 && m <= 8 * blocks) break;
     if (512.0 * ((n + 15) / 16) * ((m + 16 * blocks - 1) / (16 * blocks) + kXcds) > kMostThreads) continue;
-    const double us = rows_i8_us(blocks, m, n, k);
+    const double us = rows_i8_us(blocks, m, n, k, align);
     if (us < few_us) few_us = us, few.row_blocks = blocks;
   }
   return few_us < HUGE_VAL && few_us <= least ? few : best;

@@ -226,6 +226,56 @@ __device__ inline void pack_rows(const DensePack& p, uint32_t mat, uint32_t grou
   }
 }
 
+// Sixteen bytes at p at any alignment, of which those from `left` on (of what can be read there) are something else.
+__device__ inline s16x8 load16(const int8_t* p, int64_t left) {
+  s16x8 v;
+  if (left >= 16) {
+    __builtin_memcpy(&v, p, 16);
+  } else {
+    int8_t b[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) b[e] = p[min(int64_t(e), left - 1)];
+    __builtin_memcpy(&v, b, 16);
+  }
+  return v;
+}
+
+// keeps `left` bytes of sixteen, zeros behind them
+__device__ inline s16x8 keep16(s16x8 v, int left) {
+  i32x4 w = __builtin_bit_cast(i32x4, v);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int bytes = left - 4 * i;
+    w[i] = bytes >= 4 ? w[i] : bytes <= 0 ? 0 : w[i] & static_cast<int>((1u << 8 * bytes) - 1);
+  }
+  return __builtin_bit_cast(s16x8, w);
+}
+
+// pack_rows of 8-bit integers, 16 bytes a thread: read at any alignment those run at a copy's rate (5.0 TB/s; 1 byte a
+// thread at 1.2).
+__device__ inline void pack_eights(const DensePack& p, uint32_t mat, uint32_t group) {
+  const uint32_t cols = p.cols[mat], chunks = (cols + 15) / 16, rows = p.rows[mat];
+  const int8_t* const src = static_cast<const int8_t*>(p.src[mat]);
+  int8_t* const dst = static_cast<int8_t*>(p.dst[mat]);
+  const int64_t last = int64_t(rows - 1) * p.lds[mat] + cols;   // bytes of the matrix
+  const uint32_t wide = p.wide[mat], x = threadIdx.x % wide, y = threadIdx.x / wide, side = 256 / wide;
+  const uint64_t step = uint64_t(p.groups) * side;
+  for (uint64_t i = uint64_t(group) * side + y; i < rows; i += 4 * step)
+    for (uint32_t j = x; j < chunks; j += wide) {
+      s16x8 v[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t at = static_cast<int64_t>(min(i + r * step, uint64_t(rows) - 1)) * p.lds[mat] + j * 16;
+        v[r] = load16(src + at, last - at);
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (i + r * step < rows)
+          *reinterpret_cast<s16x8*>(dst + static_cast<int64_t>(i + r * step) * p.ldd[mat] + j * 16) =
+              keep16(v[r], static_cast<int>(min(16u, cols - j * 16)));
+    }
+}
+
 }  // namespace
 }  // namespace embx
 #endif

@@ -45,7 +45,7 @@ __device__ inline uint32_t most_of(uint32_t v) {
 __device__ inline bool copies(const Quantize& a) {
   if (blockIdx.x < a.groups) return false;
   const uint32_t id = blockIdx.x - a.groups;
-  pack_rows<uint8_t>(a.pack, id / a.pack.groups, id % a.pack.groups);
+  pack_eights(a.pack, id / a.pack.groups, id % a.pack.groups);
   return true;
 }
 

@@ -83,6 +83,7 @@ emb_status_t check_shape(const emb_linear_int8_t& a) {
 struct Int8Space {
   DenseChoice choice;
   bool inside, quantized, packed_x, packed_w;
+  int32_t align;
   const int8_t *x, *w;
   int64_t ldx, ldw;
   const float* scale;
@@ -91,13 +92,17 @@ struct Int8Space {
 
 Int8Space int8_space(Arena& ar, const emb_linear_int8_t& a) {
   Int8Space s = {};
-  s.choice = dense_choose_i8(a.m, a.n, a.k);
+  const bool x = a.x_scale && whole(a.x, a.ldx) && a.k % 16 == 0, w = whole(a.weight, a.ldw);
+  auto words = [](const void* p, int64_t ld) { return !misaligned(p, 4) && ld % 4 == 0; };
+  s.align = w && (x || !a.x_scale) ? 16 : words(a.weight, a.ldw) && (!a.x_scale || words(a.x, a.ldx)) ? 4 : 1;
+  s.choice = dense_choose_i8(a.m, a.n, a.k, s.align, double(a.k) * ((a.x_scale && !x ? a.m : 0) + (w ? 0 : a.n)));
   // A few rows that a workgroup's registers hold are quantized by each of the product's workgroups.
   s.inside = !a.x_scale && s.choice.variant == kRows && s.choice.row_blocks == 1 && a.m <= 8 &&
              a.k * (a.m == 1 ? 1 : a.m == 2 ? 2 : a.m <= 4 ? 4 : 8) <= 16384;
   s.quantized = !a.x_scale && !s.inside;
-  s.packed_x = a.x_scale && !(whole(a.x, a.ldx) && a.k % 16 == 0);
-  s.packed_w = !whole(a.weight, a.ldw);
+  const bool rows = s.choice.variant == kRows;   // reads any rows where they lie
+  s.packed_x = a.x_scale && !x && !rows;
+  s.packed_w = !w && !rows;
   s.x = static_cast<const int8_t*>(a.x), s.ldx = a.ldx, s.scale = a.x_scale;
   s.w = a.weight, s.ldw = a.ldw;
   if (s.quantized || s.packed_x) s.x = ar.take<int8_t>(a.m * up16(a.k)), s.ldx = up16(a.k);
@@ -114,8 +119,8 @@ void add_copy(DensePack& p, const void* src, int64_t ld, const void* dst, int64_
   p.src[at] = src, p.lds[at] = ld;
   p.dst[at] = const_cast<void*>(dst), p.ldd[at] = up16(cols), p.panel[at] = kPanel;
   p.rows[at] = static_cast<uint32_t>(rows), p.cols[at] = static_cast<uint32_t>(cols);
-  uint32_t wide = 16;
-  while (wide < 256 && wide < cols) wide *= 2;
+  uint32_t wide = 1;
+  while (wide < 256 && wide * 16 < cols) wide *= 2;
   p.wide[at] = wide;
   p.groups = std::max<int32_t>(p.groups, static_cast<int32_t>(std::min<int64_t>(2048, (rows * wide + 1023) / 1024)));
 }
@@ -242,7 +247,7 @@ emb_status_t emb_linear_int8(const emb_linear_int8_t* a, void* workspace, size_t
   g.scale_a = s.scale, g.scale_b = a->w_scale;
   g.result = a->dtype == EMB_DTYPE_F32 ? kDenseF32 : a->dtype == EMB_DTYPE_F16 ? kDenseF16 : kDenseBF16;
   g.ni = static_cast<int32_t>(a->m), g.nj = static_cast<int32_t>(a->n), g.nr = static_cast<int32_t>(a->k);
-  g.act = a->activation, g.parts = 1, g.whole = 1;
+  g.act = a->activation, g.parts = 1, g.whole = s.align;
   g.variant = s.choice.variant, g.splits = g.slots = s.choice.splits, g.row_blocks = s.choice.row_blocks;
   g.partial = s.partial;
   return run(dense_forward_i8(g, stream));
