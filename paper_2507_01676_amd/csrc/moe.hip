@@ -339,7 +339,7 @@ __device__ inline float segments(f32x4 v, int lane) {
 // Wavefronts of a SIMD, by the registers that two steps take, of which each has so many fragments of x: without a stack.
 template <int TYPE, bool EIGHT, bool WHOLE>
 constexpr int waves_of(int fragments) {
-  return fragments * (EIGHT ? 2 : 1) * (TYPE == kDenseF32 ? 2 : 1) + (EIGHT && !WHOLE ? 2 : 0) < 4 ? 4 : 2;
+  return fragments * (EIGHT ? 2 : 1) * (TYPE == kDenseF32 ? 2 : 1) + (WHOLE ? 0 : EIGHT ? 2 : 3) <= (TYPE == kDenseF32 || EIGHT ? 3 : 4) ? 4 : 2;
 }
 
 constexpr int kUses = 512;   // that a workgroup looks at at a time
@@ -498,7 +498,7 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(TYPE == kDenseF3
   using T = typename Elem<TYPE>::T;
   constexpr int kParts = TYPE == kDenseF32 ? 1 : 2;
   constexpr int FR = 1, kRows = 16 / S, kCols = kRows * FI, kTokens = kRows * FR;
-  __shared__ uint16_t lists[kWaves][2][kUses], used[kUses];
+  __shared__ uint16_t lists[kWaves][2][kDownRows], used[kUses];   // (a row uses an expert once)
   __shared__ uint32_t mask[kMostExperts / 32];
   __shared__ float sums[kWaves][kDownRows][kCols];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;

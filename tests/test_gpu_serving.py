@@ -186,7 +186,9 @@ def test_linear_int8_rows_that_are_not_finite(gpu_lib):
 # rows, f, d, experts, top_k
 MOE = [(1, 1, 1, 1, 1), (1, 16, 16, 2, 1), (1, 40, 24, 4, 2), (1, 704, 256, 16, 4), (2, 333, 1001, 7, 3), (4, 128, 320, 8, 8),
        (5, 64, 130, 3, 2), (17, 48, 200, 5, 5), (19, 100, 64, 8, 2), (33, 65, 33, 40, 1), (64, 256, 128, 32, 4), (70, 31, 96, 2, 2),
-       (200, 33, 65, 16, 4), (7, 24, 40, 130, 32), (300, 40, 48, 6, 3), (600, 32, 64, 3, 2), (1, 2000, 72, 2, 2), (9, 8, 4100, 1024, 8)]
+       (200, 33, 65, 16, 4), (7, 24, 40, 130, 32), (300, 40, 48, 6, 3), (600, 32, 64, 3, 2), (1, 2000, 72, 2, 2), (9, 8, 4100, 1024, 8),
+       (20, 700, 96, 4, 2), (70, 500, 100, 3, 2), (12, 1500, 300, 2, 1), (2, 400, 2100, 4, 2), (130, 72, 60, 2, 2), (40, 6000, 17, 8, 2),
+       (2, 300, 9000, 6, 2)]
 
 
 def moe_operands(size, dtype, seed, eight):
