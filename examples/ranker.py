@@ -6,7 +6,8 @@
     score = sigmoid(x Ws^T + bs)
 
 ``Ranker.scores`` serves; ``Ranker.train_step`` takes one step of gradient descent on the logistic loss (the tables stay
-as they are).  Run as a script it does both on seeded synthetic queries:
+as they are).  ``Ranker.quantize`` makes 8-bit copies of the two fully connected layers' weights, with which
+``scores(..., eight=True)`` serves.  Run as a script it does all of it on seeded synthetic queries:
 
     python examples/ranker.py [--dtype f32|f16|bf16] [--batch 4096] [--steps 50]
 """
@@ -55,13 +56,23 @@ class Ranker:
         out = self.plan.lookup(indices, offsets, batch)
         return (out.view(batch, -1) * 10.0).to(self.dtype)
 
-    def scores(self, indices, offsets, dense):
-        """[B] probabilities, in the type of the layers."""
+    def quantize(self):
+        """8-bit copies, as the weights are now."""
+        self.eight = {name: embx.quantize_rows(self.p[name]) for name in ("w0", "wo")}
+
+    def scores(self, indices, offsets, dense, eight=False):
+        """[B] probabilities, in the type of the layers; ``eight``: with the weights of the last quantize()."""
         p, batch = self.p, dense.shape[0]
+
+        def layer(x, weight, bias, residual, activation):
+            if eight:
+                return embx.linear_int8(x, *self.eight[weight], p[bias], residual, activation=activation)
+            return embx.linear(x, p[weight], p[bias], residual, activation=activation)
+
         side = embx.linear(dense, p["wd"], p["bd"], activation="relu")
-        x = embx.linear(self.pooled(indices, offsets, batch), p["w0"], p["b0"], side, activation="relu")
+        x = layer(self.pooled(indices, offsets, batch), "w0", "b0", side, "relu")
         h = embx.gated_ffn(x, p["wg"], p["wu"])
-        x = embx.linear(h, p["wo"], p["bo"], x)
+        x = layer(h, "wo", "bo", x, "none")
         return embx.linear(x, p["ws"], p["bs"], activation="sigmoid").view(-1)
 
     def gradients(self, indices, offsets, dense, labels):
@@ -121,14 +132,17 @@ def main():
         loss = r.train_step(*q)
         if step % 10 == 0 or step == a.steps - 1:
             print(f"step {step}: loss {loss.item():.4f}", flush=True)
-    scores = r.scores(*q[:3])
-    right = ((scores.float() > 0.5).float() == q[3]).float().mean().item()
-    torch.cuda.synchronize()
-    start = time.perf_counter()
-    for _ in range(100):
-        r.scores(*q[:3])
-    torch.cuda.synchronize()
-    print(f"{right:.1%} of {a.batch} labels right; {(time.perf_counter() - start) * 1e4:.0f} us a batch of scores")
+    r.quantize()
+    for eight in (False, True):
+        scores = r.scores(*q[:3], eight=eight)
+        right = ((scores.float() > 0.5).float() == q[3]).float().mean().item()
+        torch.cuda.synchronize()
+        start = time.perf_counter()
+        for _ in range(100):
+            r.scores(*q[:3], eight=eight)
+        torch.cuda.synchronize()
+        print(f"{'8-bit weights: ' if eight else ''}{right:.1%} of {a.batch} labels right; "
+              f"{(time.perf_counter() - start) * 1e4:.0f} us a batch of scores")
 
 
 if __name__ == "__main__":

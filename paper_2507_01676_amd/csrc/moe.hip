@@ -493,14 +493,14 @@ constexpr int kDownRows = 64;   // rows of x that a workgroup of the down projec
 // y = sum of a row's experts' h Wd^T times their shares: FI * 16 / S columns a workgroup, and one of a.splits parts of the
 // reduction.  Its work is items, an expert and a.chunk of the reduction, in order; each wavefront takes every eighth and adds
 // up sums of its own, so that no expert waits for another.
-template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI>
-__global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(TYPE == kDenseF32 ? 1 : 2))) void moe_down(Moe a) {
+template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT, WHOLE>(TYPE == kDenseF32 ? 1 : 2))) void moe_down(Moe a) {
   using T = typename Elem<TYPE>::T;
   constexpr int kParts = TYPE == kDenseF32 ? 1 : 2;
   constexpr int FR = 1, kRows = 16 / S, kCols = kRows * FI, kTokens = kRows * FR;
-  __shared__ uint16_t lists[kWaves][2][kDownRows], used[kUses];   // (a row uses an expert once)
+  __shared__ uint16_t lists[WAVES][2][kDownRows], used[kUses];   // (a row uses an expert once)
   __shared__ uint32_t mask[kMostExperts / 32];
-  __shared__ float sums[kWaves][kDownRows][kCols];
+  __shared__ float sums[WAVES][kDownRows][kCols];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
   const int j0 = blockIdx.x * kCols;
   const int rows_each = min(kDownRows, kUses / a.top_k), first_row = blockIdx.y * rows_each;
@@ -517,7 +517,7 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(TYPE == kDenseF3
   for (int n = 0; n < kUses / 64; ++n)
     if (n == wave && u.id[n] >= 0) atomicOr(&mask[u.id[n] >> 5], 1u << (u.id[n] & 31));
   __syncthreads();
-  for (int e = tid; e < a.experts; e += 512) {
+  for (int e = tid; e < a.experts; e += 64 * WAVES) {
     if (!(mask[e >> 5] >> (e & 31) & 1)) continue;
     int at = __popc(mask[e >> 5] & ((1u << (e & 31)) - 1));
     for (int n = 0; n < e >> 5; ++n) at += __popc(mask[n]);
@@ -598,7 +598,7 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(TYPE == kDenseF3
     if (last) {
       then.at += kTokens;
       if (then.at >= then.have) {
-        then.item += kWaves;
+        then.item += WAVES;
         more = then.item < items;
         if (more) begin_item(then);
       }
@@ -618,12 +618,12 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(TYPE == kDenseF3
     go(two, one);
   }
   __syncthreads();
-  for (int at = threadIdx.x; at < rows * kCols; at += 512) {
+  for (int at = threadIdx.x; at < rows * kCols; at += 64 * WAVES) {
     const int r = at / kCols, j = j0 + at % kCols;
     if (j >= a.d) continue;
     float s = 0.0f;
 #pragma unroll
-    for (int n = 0; n < kWaves; ++n) s += sums[n][r][at % kCols];
+    for (int n = 0; n < WAVES; ++n) s += sums[n][r][at % kCols];
     if (a.splits > 1) a.partial[(int64_t(blockIdx.z) * a.m + first_row + r) * a.d + j] = s;
     else static_cast<T*>(a.y)[(first_row + r) * a.ldy + j] = T(s);
   }
@@ -653,10 +653,11 @@ int up(const Moe& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI>
+template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI, int WAVES>
 int down(const Moe& a, hipStream_t s) {
   const int rows = std::min(kDownRows, kUses / a.top_k), columns = 16 / S * FI;
-  moe_down<TYPE, EIGHT, WHOLE, S, FI><<<dim3((a.d + columns - 1) / columns, (a.m + rows - 1) / rows, a.splits), 512, 0, s>>>(a);
+  const dim3 grid((a.d + columns - 1) / columns, (a.m + rows - 1) / rows, a.splits);
+  moe_down<TYPE, EIGHT, WHOLE, S, FI, WAVES><<<grid, 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -670,7 +671,9 @@ int launch(const Moe& a, hipStream_t s) {
     default: rc = up<TYPE, EIGHT, WHOLE, 1, kMany>(a, s); break;
   }
   if (rc != 0) return rc;
-  rc = a.down_variant == kMoeFew ? down<TYPE, EIGHT, WHOLE, 4, 1>(a, s) : down<TYPE, EIGHT, WHOLE, 1, 2>(a, s);
+  if (a.down_variant != kMoeFew) rc = down<TYPE, EIGHT, WHOLE, 1, 2, 8>(a, s);
+  else if (a.down_waves == 16) rc = down<TYPE, EIGHT, WHOLE, 4, 1, 16>(a, s);
+  else rc = down<TYPE, EIGHT, WHOLE, 4, 1, 8>(a, s);
   if (rc != 0 || a.splits == 1) return rc;
   moe_join<TYPE><<<static_cast<uint32_t>((int64_t(a.m) * a.d + 255) / 256), 256, 0, s>>>(a);
   return hipGetLastError();

@@ -34,6 +34,7 @@ struct Moe {
   int32_t m, f, d, experts, top_k, act, renormalize;
   int32_t up_variant, down_variant;   // MoeVariant
   int32_t up_waves;        // wavefronts that share a reduction of the up projections: 1, 2, 4 or 8
+  int32_t down_waves;      // kMoeFew: wavefronts of a workgroup of the down projection, 8 or 16
   int32_t fused;           // see kFused
   int32_t whole;           // rows of all operands start at multiples of 16 bytes
   int32_t splits, split_step;   // parts of the down projection's reduction, and their length

@@ -156,7 +156,7 @@ struct MoeSpace {
   int32_t* chosen;
   float* share;
   float* partial;
-  int32_t up_variant, down_variant, up_waves, fused, splits, split_step, chunk;
+  int32_t up_variant, down_variant, up_waves, down_waves, fused, splits, split_step, chunk;
 };
 
 MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
@@ -164,14 +164,23 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   MoeSpace s = {nullptr, (a.f + 7) / 8 * 8, a.chosen, a.share};
   const int64_t used = std::min<int64_t>(uses, a.experts);   // experts, at most
   const int64_t step = a.gate.scale ? 64 : 32;               // of the reduction: a matrix instruction, or two
-  // The up projections: 16 columns of an expert to so many wavefronts, or 4 where there would be few workgroups.
+  // The up projections: 16 columns of an expert to so many wavefronts, or 4 where there would be few workgroups and few rows
+  // (us a call: one query, one expert of 1024 x 4096 28.4 with 16 columns, 23.3 with 4; two of eight of 2816 x 1024 22.6 and
+  // 26.3).  Four wavefronts share the reduction, and a workgroup has 32 columns, where that leaves workgroups enough (64 rows,
+  // 4 of 32 experts of 5632 x 2048 441 with eight, 432 with four; 19 rows, 3 of 7 of 333 x 1001 35.7 and 40.9).  Several times
+  // 16 rows of an expert at once where it is expected to have more than 12 (128 rows, 2 of 8 91.5 with 16 at a time, 75.8 with
+  // 64).
   const int64_t tiles = (a.f + 15) / 16 * used;
   s.up_variant = a.m <= 4 && tiles < 256 ? kMoeFew : uses <= 12 * a.experts ? kMoeMore : kMoeMany;
   s.up_waves = s.up_variant != kMoeFew && tiles >= 352 ? 4 : 8;
   const int64_t up_step = s.up_variant == kMoeFew ? step * 4 : step * 2;
   while (s.up_waves > 1 && s.up_waves * up_step > a.d) s.up_waves /= 2;
+  // (one query, eight experts: 18.4 with the routing in every workgroup, 20.5 with a launch for it; five queries 41 and 35)
   s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kFused && a.m * a.experts * a.d <= 65536 && a.m * tiles <= 1024;
-  // The down projection: 32 columns a workgroup, or 4, and about 256 workgroups.
+  // The down projection: 32 columns a workgroup, or 4 (one query, two of eight experts of 2816 x 1024: 17.9 with 4 columns,
+  // 19.6 with 32; five queries 34.4 and 31.6; one, 1024 x 4096 19.8 and 17.9; f32, 8 rows, 4 of 16 of 704 x 256 24.3 and 32),
+  // and its reduction split over about 256 workgroups (64 rows, 4 of 32 of 5632 x 2048 in four 431, in eight 440; 16 rows, 2 of
+  // 8 of 2816 x 1024 in two 47, in eight 42.7).
   s.down_variant = (a.m <= 4 && a.d <= 2048) || (a.m <= 8 && a.d <= 512) ? kMoeFew : kMoeMore;
   const int64_t columns = s.down_variant == kMoeFew ? 4 : 32, rows = std::min<int64_t>(64, 512 / a.top_k);
   const int64_t groups = (a.d + columns - 1) / columns * ((a.m + rows - 1) / rows);
@@ -179,6 +188,9 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   const int64_t down_step = s.down_variant == kMoeFew ? step * 4 : step * 2;
   s.split_step = static_cast<int32_t>(((a.f + splits - 1) / splits + down_step - 1) / down_step * down_step);
   s.splits = static_cast<int32_t>((a.f + s.split_step - 1) / s.split_step);
+  // 16 wavefronts where a CU has one workgroup (one query, two of eight experts of 2816 x 1024: 6.4 us of GPU time, with eight
+  // 8.0; but of 5632 x 2048, two workgroups a CU, a call 46.2 and with eight 44.0)
+  s.down_waves = groups * splits <= 256 ? 16 : 8;
   // an expert's part of the reduction is an item of a wavefront; with few experts several are, so that there are 16 or so
   const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(s.split_step / (2 * down_step), 16 / used));
   s.chunk = static_cast<int32_t>(((s.split_step + chunks - 1) / chunks + down_step - 1) / down_step * down_step);
@@ -286,7 +298,7 @@ emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes
   }
   g.h = s.h, g.ldh = s.ldh, g.chosen = s.chosen, g.share = s.share;
   g.up_variant = s.up_variant, g.down_variant = s.down_variant, g.up_waves = s.up_waves;
-  g.fused = s.fused;
+  g.down_waves = s.down_waves, g.fused = s.fused;
   g.partial = s.partial, g.splits = s.splits, g.split_step = s.split_step, g.chunk = s.chunk;
   const size_t size = esize(a->dtype);
   g.whole = aligned(a->x, a->ldx, size) && aligned(a->router, a->ldr, size) && aligned(a->gate, size) && aligned(a->up, size) &&
