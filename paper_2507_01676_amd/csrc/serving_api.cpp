@@ -178,10 +178,11 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   // (one query, eight experts: 18.4 with the routing in every workgroup, 20.5 with a launch for it; five queries 41 and 35)
   s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kFused && a.m * a.experts * a.d <= 65536 && a.m * tiles <= 1024;
   // The down projection: 32 columns a workgroup, or 4 (one query, two of eight experts of 2816 x 1024: 17.9 with 4 columns,
-  // 19.6 with 32; five queries 34.4 and 31.6; one, 1024 x 4096 19.8 and 17.9; f32, 8 rows, 4 of 16 of 704 x 256 24.3 and 32),
+  // 19.6 with 32; eight queries 37.8 and 41.7, but five with 8-bit weights 32.9 and 31.8; one, 1024 x 4096 19.8 and 17.9; f32,
+  // 8 rows, 4 of 16 of 704 x 256 24.3 and 32),
   // and its reduction split over about 256 workgroups (64 rows, 4 of 32 of 5632 x 2048 in four 431, in eight 440; 16 rows, 2 of
   // 8 of 2816 x 1024 in two 47, in eight 42.7).
-  s.down_variant = (a.m <= 4 && a.d <= 2048) || (a.m <= 8 && a.d <= 512) ? kMoeFew : kMoeMore;
+  s.down_variant = (a.m <= 4 && a.d <= 2048) || (a.m <= 8 && a.d <= (a.down.scale ? 512 : 1024)) ? kMoeFew : kMoeMore;
   const int64_t columns = s.down_variant == kMoeFew ? 4 : 32, rows = std::min<int64_t>(64, 512 / a.top_k);
   const int64_t groups = (a.d + columns - 1) / columns * ((a.m + rows - 1) / rows);
   const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({16, a.f / 160, 256 / groups}));
