@@ -80,6 +80,37 @@ struct Chunk {
   }
 };
 
+// A chunk as it was loaded.  Where rows of less than 32 bits start anywhere, that is the words that it lies in, which are shifted
+// when they are needed: 16-byte loads at odd addresses take twice as long.
+template <int SIZE, int WORDS, bool WHOLE>
+struct Loaded : Chunk<SIZE, WORDS> {
+  static constexpr bool kShifted = !WHOLE && SIZE < 4;
+  uint32_t more[kShifted ? 1 : 0];
+
+  // bytes behind a word's start
+  __device__ static uint32_t shift_of(const char* p) { return kShifted ? static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & 3 : 0; }
+
+  __device__ void load_at(const char* p) {
+    if constexpr (kShifted) {
+      const uint32_t shift = shift_of(p);
+      const char* const a = p - shift;
+      __builtin_memcpy(&this->v[0], __builtin_assume_aligned(a, 4), 16);
+      more[0] = *reinterpret_cast<const uint32_t*>(a + (shift ? 16 : 0));   // (no word without a byte of the chunk)
+    } else {
+      this->template load<WHOLE>(p);
+    }
+  }
+
+  __device__ Chunk<SIZE, WORDS> shifted(uint32_t shift) const {
+    Chunk<SIZE, WORDS> out = *this;
+    if constexpr (kShifted) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out.v[0][i] = __builtin_amdgcn_alignbyte(i < 3 ? this->v[0][i + 1] : more[0], this->v[0][i], shift);
+    }
+    return out;
+  }
+};
+
 template <int TYPE>
 struct Piece : Chunk<TYPE == kDenseF32 ? 4 : 2, TYPE == kDenseF32 ? 8 : 4> {   // eight elements
   __device__ float get(int e) const {
@@ -93,13 +124,13 @@ struct Piece : Chunk<TYPE == kDenseF32 ? 4 : 2, TYPE == kDenseF32 ? 8 : 4> {   /
 // The same of an expert's matrix, whose elements may have 8 bits (EIGHT): 16 whole numbers, exact in every type.
 template <int TYPE, bool EIGHT>
 struct Weights : Piece<TYPE> {
-  static constexpr int kSize = TYPE == kDenseF32 ? 4 : 2, kPieces = 1;
+  static constexpr int kSize = TYPE == kDenseF32 ? 4 : 2, kWords = TYPE == kDenseF32 ? 8 : 4, kPieces = 1;
   __device__ const Piece<TYPE>& piece(int) const { return *this; }
 };
 
 template <int TYPE>
 struct Weights<TYPE, true> : Chunk<1, 4> {
-  static constexpr int kSize = 1, kPieces = 2;
+  static constexpr int kSize = 1, kWords = 4, kPieces = 2;
 
   __device__ Piece<TYPE> piece(int i) const {
     Piece<TYPE> out;
@@ -250,7 +281,7 @@ constexpr int kWaves = 8;
 
 // What a wavefront multiplies at a time: of R * 16 / S rows of weights by FR * 16 / S rows of x (in PARTS parts, added up),
 // kAll of the reduction.  It is loaded while the one before it is multiplied.
-template <int TYPE, bool EIGHT, bool WHOLE, int S, int R, int FR, int PARTS>
+template <int TYPE, bool EIGHT, bool WHOLE, bool WHOLE_X, int S, int R, int FR, int PARTS>
 struct Step {
   using Ws = Weights<TYPE, EIGHT>;
   using X = Piece<TYPE>;
@@ -258,8 +289,8 @@ struct Step {
   static constexpr int kSpan = 4 * Ws::kPer, kStep = kSpan * S;
   static constexpr int kGo = S == 1 && TYPE != kDenseF32 && FR * PARTS < 4 ? 2 : 1;   // 128 bytes of a row
   static constexpr int kAll = kStep * kGo;
-  Ws w[kGo][R];
-  X x[kGo][FR][PARTS][Ws::kPieces];
+  Loaded<Ws::kSize, Ws::kWords, WHOLE> w[kGo][R];
+  Loaded<kSizeX, TYPE == kDenseF32 ? 8 : 4, WHOLE_X> x[kGo][FR][PARTS][Ws::kPieces];
   // a lane's first element of a step
   __device__ static int own(int lane) { return (lane & (S - 1)) * kSpan + (lane >> 4) * Ws::kPer; }
 
@@ -268,7 +299,7 @@ struct Step {
 #pragma unroll
     for (int g = 0; g < kGo; ++g)
 #pragma unroll
-      for (int r = 0; r < R; ++r) w[g][r].template load<WHOLE>(base[r] + int64_t(r0 + g * kStep) * Ws::kSize + row[r]);
+      for (int r = 0; r < R; ++r) w[g][r].load_at(base[r] + int64_t(r0 + g * kStep) * Ws::kSize + row[r]);
   }
 
   // and of x's rows: p, at the lane's own element
@@ -281,12 +312,18 @@ struct Step {
         for (int n = 0; n < PARTS; ++n)
 #pragma unroll
           for (int i = 0; i < Ws::kPieces; ++i)
-            x[g][f][n][i].template load<WHOLE>(p[f] + n * part + int64_t(r0 + g * kStep + 8 * i) * kSizeX);
+            x[g][f][n][i].load_at(p[f] + n * part + int64_t(r0 + g * kStep + 8 * i) * kSizeX);
   }
 
-  __device__ void multiply(f32x4 (&acc)[R][FR]) const {
+  // with the pointers that it was loaded from, as far as they lie behind words' starts
+  __device__ void multiply(const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], f32x4 (&acc)[R][FR]) const {
+    uint32_t of_w[R], of_x[FR];
 #pragma unroll
-    for (int g = 0; g < kGo; ++g) products(g, acc);
+    for (int r = 0; r < R; ++r) of_w[r] = w[0][r].shift_of(base[r] + row[r]);   // (steps are whole words)
+#pragma unroll
+    for (int f = 0; f < FR; ++f) of_x[f] = x[0][f][0][0].shift_of(p[f]);
+#pragma unroll
+    for (int g = 0; g < kGo; ++g) products(g, of_w, of_x, acc);
   }
 
   // The last step, of which only what is below `end` is there; not loaded ahead.
@@ -306,25 +343,34 @@ struct Step {
         for (int n = 0; n < PARTS; ++n)
 #pragma unroll
           for (int i = 0; i < Ws::kPieces; ++i) {
-            x[0][f][n][i].template load_end<WHOLE>(p[f] + n * part - own(lane) * kSizeX, at + 8 * i, end);
+            x[0][f][n][i].template load_end<WHOLE_X>(p[f] + n * part - own(lane) * kSizeX, at + 8 * i, end);
             x[0][f][n][i].keep(end - at - 8 * i);
             if constexpr (!WHOLE) __builtin_amdgcn_sched_barrier(0);
           }
-      products(0, acc);
+      const uint32_t of_w[R] = {}, of_x[FR] = {};   // (not loaded by words)
+      products(0, of_w, of_x, acc);
     }
   }
 
-  __device__ void products(int g, f32x4 (&acc)[R][FR]) const {
+  __device__ void products(int g, const uint32_t (&of_w)[R], const uint32_t (&of_x)[FR], f32x4 (&acc)[R][FR]) const {
 #pragma unroll
-    for (int i = 0; i < Ws::kPieces; ++i)
+    for (int i = 0; i < Ws::kPieces; ++i) {
+      X xs[FR][PARTS];
+#pragma unroll
+      for (int f = 0; f < FR; ++f)
+#pragma unroll
+        for (int n = 0; n < PARTS; ++n) static_cast<Chunk<kSizeX, TYPE == kDenseF32 ? 8 : 4>&>(xs[f][n]) = x[g][f][n][i].shifted(of_x[f]);
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        const X one = w[g][r].piece(i);
+        Ws all;
+        static_cast<Chunk<Ws::kSize, Ws::kWords>&>(all) = w[g][r].shifted(of_w[r]);
+        const X one = all.piece(i);
 #pragma unroll
         for (int n = PARTS - 1; n >= 0; --n)
 #pragma unroll
-          for (int f = 0; f < FR; ++f) acc[r][f] = product<TYPE>(one, x[g][f][n][i], acc[r][f]);
+          for (int f = 0; f < FR; ++f) acc[r][f] = product<TYPE>(one, xs[f][n], acc[r][f]);
       }
+    }
   }
 };
 
@@ -339,7 +385,7 @@ __device__ inline float segments(f32x4 v, int lane) {
 // Wavefronts of a SIMD, by the registers that two steps take, of which each has so many fragments of x: without a stack.
 template <int TYPE, bool EIGHT, bool WHOLE>
 constexpr int waves_of(int fragments) {
-  return fragments * (EIGHT ? 2 : 1) * (TYPE == kDenseF32 ? 2 : 1) + (WHOLE ? 0 : EIGHT ? 2 : 3) <= (TYPE == kDenseF32 || EIGHT ? 3 : 4) ? 4 : 2;
+  return fragments * (EIGHT ? 2 : 1) * (TYPE == kDenseF32 ? 2 : 1) + (WHOLE ? 0 : EIGHT ? 2 : 4) <= (TYPE == kDenseF32 || EIGHT ? 3 : 4) ? 4 : 2;
 }
 
 constexpr int kUses = 512;   // that a workgroup looks at at a time
@@ -407,7 +453,7 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
     for (int at = 0; at < use; at += 64)
       if (__any(at + lane < use && chosen[min(at + lane, use)] == expert)) return;
   }
-  using P = Step<TYPE, EIGHT, WHOLE, S, 2, FR, 1>;
+  using P = Step<TYPE, EIGHT, WHOLE, WHOLE, S, 2, FR, 1>;
   // (16 rows of at most 2^25 elements of a row's stride: 32 bits)
   const int row0 = min(j0, a.f - 1), lane_row = min(j0 + c / S, a.f - 1) - row0;
   const char* base[2];
@@ -441,7 +487,7 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
           r0 += every;
           const bool more = r0 + P::kAll <= a.d;
           if (more) next.load_w(base, row, r0), next.load_x(x, 0, r0);
-          now.multiply(acc);
+          now.multiply(base, row, x, acc);
           return more;
         };
         while (go(one, two) && go(two, one)) {}
@@ -527,7 +573,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   for (int n = 0; n < (a.experts + 31) / 32; ++n) total += __popc(mask[n]);
   __syncthreads();
   const int chunks = (end - begin + a.chunk - 1) / a.chunk;
-  using P = Step<TYPE, EIGHT, WHOLE, S, FI, FR, kParts>;
+  using P = Step<TYPE, EIGHT, WHOLE, true, S, FI, FR, kParts>;   // (rows of h start at multiples of 16 bytes)
   // Where a wavefront is: an item, its expert's uses from `at` on, and r0 of its reduction.
   struct Place {
     int item, expert, to, have, at, r0, which;
@@ -605,7 +651,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
       if (more) begin_rows(then);
     }
     if (more) load(other, then);
-    if (left > now.r0) s.multiply(acc);
+    if (left > now.r0) s.multiply(now.w, now.row, now.h, acc);
     if (last) {
       if (left < now.to) s.rest(now.w, now.row, now.h, part, left, now.to, lane, acc);
       finish(now);

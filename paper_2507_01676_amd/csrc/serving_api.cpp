@@ -185,7 +185,7 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   s.down_variant = (a.m <= 4 && a.d <= 2048) || (a.m <= 8 && a.d <= (a.down.scale ? 512 : 1024)) ? kMoeFew : kMoeMore;
   const int64_t columns = s.down_variant == kMoeFew ? 4 : 32, rows = std::min<int64_t>(64, 512 / a.top_k);
   const int64_t groups = (a.d + columns - 1) / columns * ((a.m + rows - 1) / rows);
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({16, a.f / 160, 256 / groups}));
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({16, a.f / (s.down_variant == kMoeFew ? 160 : 80), 256 / groups}));
   const int64_t down_step = s.down_variant == kMoeFew ? step * 4 : step * 2;
   s.split_step = static_cast<int32_t>(((a.f + splits - 1) / splits + down_step - 1) / down_step * down_step);
   s.splits = static_cast<int32_t>((a.f + s.split_step - 1) / s.split_step);
