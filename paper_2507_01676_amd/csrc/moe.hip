@@ -36,7 +36,7 @@ __device__ inline uint64_t order_of(double v) {
 template <int SIZE, int WORDS>
 struct Chunk {
   u32x4 v[WORDS / 4];
-  static constexpr int kPer = WORDS * 4 / SIZE, kPer16 = 16 / SIZE;
+  static constexpr int kPer = WORDS * 4 / SIZE;
 
   template <bool WHOLE>
   __device__ void load(const char* p) {
@@ -44,27 +44,6 @@ struct Chunk {
     for (int h = 0; h < WORDS / 4; ++h) {
       if constexpr (WHOLE) v[h] = *reinterpret_cast<const u32x4*>(p + 16 * h);
       else __builtin_memcpy(&v[h], p + 16 * h, 16);
-    }
-  }
-
-  // elements at .. of a row of n: what is behind its end is something else.  Where rows start at multiples of 16 bytes (WHOLE)
-  // their last 16 bytes are read whole.
-  template <bool WHOLE>
-  __device__ void load_end(const char* row, int at, int n) {
-#pragma unroll
-    for (int h = 0; h < WORDS / 4; ++h) {
-      if constexpr (WHOLE) {
-        v[h] = *reinterpret_cast<const u32x4*>(row + int64_t(min(at + h * kPer16, (n - 1) / kPer16 * kPer16)) * SIZE);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[h][i] = 0;
-          using E = std::conditional_t<SIZE == 1, uint8_t, std::conditional_t<SIZE == 2, uint16_t, uint32_t>>;
-#pragma unroll
-          for (int e = 0; e < 4 / SIZE; ++e)
-            v[h][i] |= uint32_t(reinterpret_cast<const E*>(row)[min(at + h * kPer16 + i * (4 / SIZE) + e, n - 1)]) << 8 * SIZE * e;
-        }
-      }
     }
   }
 
@@ -98,6 +77,29 @@ struct Loaded : Chunk<SIZE, WORDS> {
       more[0] = *reinterpret_cast<const uint32_t*>(a + (shift ? 16 : 0));   // (no word without a byte of the chunk)
     } else {
       this->template load<WHOLE>(p);
+    }
+  }
+
+  // Elements at .. of a row of n, of which some may be behind its end and are something else.  Nothing is read without one of
+  // the row's bytes in the same 16, or word.
+  __device__ void load_end(const char* row, int at, int n) {
+    constexpr int kPer16 = 16 / SIZE;
+    if constexpr (kShifted) {
+      const int first = min(at, n - 1);
+      const char* const p = row + int64_t(first) * SIZE;
+      const uint32_t shift = shift_of(p), last = (shift + min((n - first) * SIZE, 20) - 1) / 4 * 4;
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i) this->v[0][i] = *reinterpret_cast<const uint32_t*>(p - shift + min(4 * i, last));
+      more[0] = *reinterpret_cast<const uint32_t*>(p - shift + min(16u, last));
+    } else if constexpr (WHOLE) {
+#pragma unroll
+      for (int h = 0; h < WORDS / 4; ++h)
+        this->v[h] = *reinterpret_cast<const u32x4*>(row + int64_t(min(at + h * kPer16, (n - 1) / kPer16 * kPer16)) * SIZE);
+    } else {
+#pragma unroll
+      for (int h = 0; h < WORDS / 4; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) this->v[h][i] = reinterpret_cast<const uint32_t*>(row)[min(at + h * 4 + i, n - 1)];
     }
   }
 
@@ -192,8 +194,15 @@ __device__ inline void logits(const Moe& a, int first_row, int rows, Routing<DOT
     auto add = [&](int j, auto full) {
       Piece<TYPE> px[MANY], pr[MANY];
       auto load = [&](Piece<TYPE>& p, const T* row) {
-        if constexpr (decltype(full)::value) p.template load<WHOLE>(reinterpret_cast<const char*>(row + j));
-        else p.template load_end<WHOLE>(reinterpret_cast<const char*>(row), j, a.d), p.keep(a.d - j);
+        const char* const bytes = reinterpret_cast<const char*>(row);
+        if constexpr (decltype(full)::value) {
+          p.template load<WHOLE>(bytes + int64_t(j) * sizeof(T));
+        } else {
+          Loaded<sizeof(T), TYPE == kDenseF32 ? 8 : 4, WHOLE> end;
+          end.load_end(bytes, j, a.d);
+          static_cast<Chunk<sizeof(T), TYPE == kDenseF32 ? 8 : 4>&>(p) = end.shifted(end.shift_of(bytes));
+          p.keep(a.d - j);
+        }
       };
 #pragma unroll
       for (int n = 0; n < MANY; ++n) load(pr[n], r[n]), load(px[n], x[n]);
@@ -317,53 +326,64 @@ struct Step {
 
   // with the pointers that it was loaded from, as far as they lie behind words' starts
   __device__ void multiply(const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], f32x4 (&acc)[R][FR]) const {
-    uint32_t of_w[R], of_x[FR];
 #pragma unroll
-    for (int r = 0; r < R; ++r) of_w[r] = w[0][r].shift_of(base[r] + row[r]);   // (steps are whole words)
-#pragma unroll
-    for (int f = 0; f < FR; ++f) of_x[f] = x[0][f][0][0].shift_of(p[f]);
-#pragma unroll
-    for (int g = 0; g < kGo; ++g) products(g, of_w, of_x, acc);
+    for (int g = 0; g < kGo; ++g) products<false>(g, base, row, p, 0, acc);
   }
 
   // The last step, of which only what is below `end` is there; not loaded ahead.
   __device__ void rest(const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], int64_t part, int r0,
                        int end, int lane, f32x4 (&acc)[R][FR]) {
-    for (; r0 < end; r0 += kStep) {
-      const int at = r0 + own(lane);
+    auto load = [&](int g, int at) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) {
-        w[0][r].template load_end<WHOLE>(base[r] + row[r] - own(lane) * Ws::kSize, at, end);
-        w[0][r].keep(end - at);
-        if constexpr (!WHOLE) __builtin_amdgcn_sched_barrier(0);   // (element by element: not all at once)
-      }
+      for (int r = 0; r < R; ++r) w[g][r].load_end(base[r] + row[r] - own(lane) * Ws::kSize, at, end);
 #pragma unroll
       for (int f = 0; f < FR; ++f)
 #pragma unroll
         for (int n = 0; n < PARTS; ++n)
 #pragma unroll
-          for (int i = 0; i < Ws::kPieces; ++i) {
-            x[0][f][n][i].template load_end<WHOLE_X>(p[f] + n * part - own(lane) * kSizeX, at + 8 * i, end);
-            x[0][f][n][i].keep(end - at - 8 * i);
-            if constexpr (!WHOLE) __builtin_amdgcn_sched_barrier(0);
-          }
-      const uint32_t of_w[R] = {}, of_x[FR] = {};   // (not loaded by words)
-      products(0, of_w, of_x, acc);
+          for (int i = 0; i < Ws::kPieces; ++i) x[g][f][n][i].load_end(p[f] + n * part - own(lane) * kSizeX, at + 8 * i, end);
+    };
+    if constexpr (WHOLE) {   // (one at a time, in place: fewer registers)
+      for (; r0 < end; r0 += kStep) {
+        const int left = end - r0 - own(lane);
+        load(0, r0 + own(lane));
+#pragma unroll
+        for (int r = 0; r < R; ++r) w[0][r].keep(left);
+#pragma unroll
+        for (int f = 0; f < FR; ++f)
+#pragma unroll
+          for (int n = 0; n < PARTS; ++n)
+#pragma unroll
+            for (int i = 0; i < Ws::kPieces; ++i) x[0][f][n][i].keep(left - 8 * i);
+        products<false>(0, base, row, p, 0, acc);
+      }
+    } else {
+#pragma unroll
+      for (int g = 0; g < kGo; ++g) load(g, r0 + g * kStep + own(lane));
+#pragma unroll
+      for (int g = 0; g < kGo; ++g) products<true>(g, base, row, p, end - r0 - g * kStep - own(lane), acc);
     }
   }
 
-  __device__ void products(int g, const uint32_t (&of_w)[R], const uint32_t (&of_x)[FR], f32x4 (&acc)[R][FR]) const {
+  // END: only `left` of the reduction from the lane's first element on are there
+  template <bool END>
+  __device__ void products(int g, const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], int left,
+                           f32x4 (&acc)[R][FR]) const {
 #pragma unroll
     for (int i = 0; i < Ws::kPieces; ++i) {
       X xs[FR][PARTS];
 #pragma unroll
       for (int f = 0; f < FR; ++f)
 #pragma unroll
-        for (int n = 0; n < PARTS; ++n) static_cast<Chunk<kSizeX, TYPE == kDenseF32 ? 8 : 4>&>(xs[f][n]) = x[g][f][n][i].shifted(of_x[f]);
+        for (int n = 0; n < PARTS; ++n) {
+          static_cast<Chunk<kSizeX, TYPE == kDenseF32 ? 8 : 4>&>(xs[f][n]) = x[g][f][n][i].shifted(x[g][f][n][i].shift_of(p[f]));
+          if constexpr (END) xs[f][n].keep(left - 8 * i);
+        }
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         Ws all;
-        static_cast<Chunk<Ws::kSize, Ws::kWords>&>(all) = w[g][r].shifted(of_w[r]);
+        static_cast<Chunk<Ws::kSize, Ws::kWords>&>(all) = w[g][r].shifted(w[g][r].shift_of(base[r] + row[r]));   // (steps are whole words)
+        if constexpr (END) all.keep(left);
         const X one = all.piece(i);
 #pragma unroll
         for (int n = PARTS - 1; n >= 0; --n)
