@@ -408,8 +408,6 @@ constexpr int waves_of(int fragments) {
   return fragments * (EIGHT ? 2 : 1) * (TYPE == kDenseF32 ? 2 : 1) + (WHOLE ? 0 : EIGHT ? 2 : 4) <= (TYPE == kDenseF32 || EIGHT ? 3 : 4) ? 4 : 2;
 }
 
-constexpr int kUses = 512;   // that a workgroup looks at at a time
-
 // The uses of one expert among up to kUses of them, `first` .. `first + count - 1`: a wavefront lists them in LDS of its own,
 // in order, and has their number.
 struct Uses {
@@ -463,7 +461,7 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
   const int32_t* chosen = a.chosen;
   if constexpr (ROUTE) {
     route<TYPE, WHOLE>(a, 0, a.m, r);
-    if (blockIdx.x == 0 && blockIdx.y == 0) store(a, 0, a.m, r);
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) store(a, 0, a.m, r);
     chosen = r.chosen;
   }
   int expert = blockIdx.y;
@@ -491,8 +489,8 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
     if (!u.any(expert)) continue;
     P one, two;
     if (begin + P::kAll <= a.d) one.load_w(base, row, begin);   // before the uses are listed
-    const int have = u.list(expert, lists[wave], count, lane);
-    for (int at = 0; at < have; at += kTokens) {
+    const int have = u.list(expert, lists[wave], count, lane);   // (which the workgroups along z share)
+    for (int at = blockIdx.z * kTokens; at < have; at += gridDim.z * kTokens) {
       const char* x[FR];
 #pragma unroll
       for (int f = 0; f < FR; ++f)
@@ -501,7 +499,7 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
       f32x4 acc[2][FR] = {};
       int r0 = begin;
       if (begin + P::kAll <= a.d) {
-        if (at > 0) one.load_w(base, row, begin);
+        if (at != static_cast<int>(blockIdx.z) * kTokens) one.load_w(base, row, begin);
         one.load_x(x, 0, begin);
         auto go = [&](const P& now, P& next) {   // whether there is a next one
           r0 += every;
@@ -554,11 +552,10 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
   }
 }
 
-constexpr int kDownRows = 64;   // rows of x that a workgroup of the down projection has at a time
-
-// y = sum of a row's experts' h Wd^T times their shares: FI * 16 / S columns a workgroup, and one of a.splits parts of the
-// reduction.  Its work is items, an expert and a.chunk of the reduction, in order; each wavefront takes every eighth and adds
-// up sums of its own, so that no expert waits for another.
+// y = sum of a row's experts' h Wd^T times their shares: FI * 16 / S columns of a.down_rows rows.  That is items, an expert and
+// a.chunk of the reduction, which the wavefronts of a.splits workgroups take in turn; each adds up sums of its own, so that no
+// expert waits for another.  Neighbouring items go to neighbouring workgroups: experts have unlike numbers of rows (five rows,
+// 2 of 8 of 2816 x 1024, 8-bit weights 31.3 us a call, 32.7 with eight items in a row to a workgroup; 128 rows 75.8 and 78.8).
 template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT, WHOLE>(TYPE == kDenseF32 ? 1 : 2))) void moe_down(Moe a) {
   using T = typename Elem<TYPE>::T;
@@ -569,10 +566,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   __shared__ float sums[WAVES][kDownRows][kCols];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
   const int j0 = blockIdx.x * kCols;
-  const int rows_each = min(kDownRows, kUses / a.top_k), first_row = blockIdx.y * rows_each;
-  const int rows = min(rows_each, a.m - first_row), count = rows * a.top_k;
+  const int first_row = blockIdx.y * a.down_rows, rows = min(a.down_rows, a.m - first_row), count = rows * a.top_k;
   const int64_t first = int64_t(first_row) * a.top_k, part = int64_t(a.m) * a.top_k * a.ldh * sizeof(T);
-  const int begin = static_cast<int>(int64_t(a.split_step) * blockIdx.z), end = min(a.f, begin + a.split_step);
   Uses u;
   u.read(a.chosen + first, count, lane);
   if (tid < kMostExperts / 32) mask[tid] = 0;
@@ -592,7 +587,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   int total = 0;
   for (int n = 0; n < (a.experts + 31) / 32; ++n) total += __popc(mask[n]);
   __syncthreads();
-  const int chunks = (end - begin + a.chunk - 1) / a.chunk;
+  const int chunks = (a.f + a.chunk - 1) / a.chunk;
   using P = Step<TYPE, EIGHT, WHOLE, true, S, FI, FR, kParts>;   // (rows of h start at multiples of 16 bytes)
   // Where a wavefront is: an item, its expert's uses from `at` on, and r0 of its reduction.
   struct Place {
@@ -616,7 +611,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
     p.at = 0;
   };
   auto begin_rows = [&](Place& p) {
-    p.r0 = begin + p.item % chunks * a.chunk, p.to = min(end, p.r0 + a.chunk);
+    p.r0 = p.item % chunks * a.chunk, p.to = min(a.f, p.r0 + a.chunk);
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
       p.use[f] = lists[wave][p.which][min(p.at + f * kRows + c / S, p.have - 1)];
@@ -653,7 +648,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   };
   const int items = total * chunks;
   P one, two;
-  Place now = {wave}, then;
+  Place now = {wave * static_cast<int>(gridDim.z) + static_cast<int>(blockIdx.z)}, then;
   bool more = now.item < items;
   if (more) begin_item(now), begin_rows(now), load(one, now);
   auto go = [&](P& s, P& other) {
@@ -664,7 +659,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
     if (last) {
       then.at += kTokens;
       if (then.at >= then.have) {
-        then.item += WAVES;
+        then.item += static_cast<int>(gridDim.z) * WAVES;
         more = then.item < items;
         if (more) begin_item(then);
       }
@@ -708,7 +703,8 @@ __global__ __launch_bounds__(256) void moe_join(Moe a) {
 template <int TYPE, bool EIGHT, bool WHOLE, int S, int FR>
 int up(const Moe& a, hipStream_t s) {
   const int columns = 16 / S * (kWaves / a.up_waves);
-  const dim3 grid((a.f + columns - 1) / columns, static_cast<uint32_t>(std::min<int64_t>(int64_t(a.m) * a.top_k, a.experts)));
+  const int64_t experts = std::min<int64_t>(int64_t(a.m) * a.top_k, a.experts);
+  const dim3 grid((a.f + columns - 1) / columns, static_cast<uint32_t>(experts), a.up_parts);
   if (a.fused && FR == 1) {
     moe_up<TYPE, EIGHT, WHOLE, S, 1, true><<<grid, 512, 0, s>>>(a);
   } else {
@@ -721,8 +717,8 @@ int up(const Moe& a, hipStream_t s) {
 
 template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI, int WAVES>
 int down(const Moe& a, hipStream_t s) {
-  const int rows = std::min(kDownRows, kUses / a.top_k), columns = 16 / S * FI;
-  const dim3 grid((a.d + columns - 1) / columns, (a.m + rows - 1) / rows, a.splits);
+  const int columns = 16 / S * FI;
+  const dim3 grid((a.d + columns - 1) / columns, (a.m + a.down_rows - 1) / a.down_rows, a.splits);
   moe_down<TYPE, EIGHT, WHOLE, S, FI, WAVES><<<grid, 64 * WAVES, 0, s>>>(a);
   return hipGetLastError();
 }

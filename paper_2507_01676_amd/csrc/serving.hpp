@@ -37,8 +37,10 @@ struct Moe {
   int32_t down_waves;      // kMoeFew: wavefronts of a workgroup of the down projection, 8 or 16
   int32_t fused;           // see kFused
   int32_t whole;           // rows of all operands start at multiples of 16 bytes
-  int32_t splits, split_step;   // parts of the down projection's reduction, and their length
-  int32_t chunk;           // of a part, that a wavefront takes at a time
+  int32_t up_parts;        // workgroups that share an expert's rows and columns of the up projections
+  int32_t down_rows;       // of x that a workgroup of the down projection has: kDownRows, and kUses / top_k, at most
+  int32_t splits;          // workgroups that share those rows and its columns
+  int32_t chunk;           // of the down projection's reduction, that a wavefront takes at a time
 };
 
 // How many rows of x an expert has at a time: at most 4 (by 4 rows of weights), 16, or several times 16.
@@ -47,6 +49,8 @@ enum MoeVariant { kMoeFew = 0, kMoeMore = 1, kMoeMany = 2 };
 constexpr int kFused = 32;   // logits of all rows that every workgroup of the up projections works out by itself
 
 constexpr int kMostExperts = 1024, kMostTopK = 32;
+constexpr int kUses = 512;       // uses, row * top_k + place, that a workgroup looks at at a time
+constexpr int kDownRows = 64;
 
 int quantize_launch(int dtype, const Quantize& a, void* stream);
 

@@ -156,7 +156,7 @@ struct MoeSpace {
   int32_t* chosen;
   float* share;
   float* partial;
-  int32_t up_variant, down_variant, up_waves, down_waves, fused, splits, split_step, chunk;
+  int32_t up_variant, down_variant, up_waves, down_waves, fused, up_parts, down_rows, splits, chunk;
 };
 
 MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
@@ -174,27 +174,42 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   s.up_variant = a.m <= 4 && tiles < 256 ? kMoeFew : uses <= 12 * a.experts ? kMoeMore : kMoeMany;
   s.up_waves = s.up_variant != kMoeFew && tiles >= 352 ? 4 : 8;
   const int64_t up_step = s.up_variant == kMoeFew ? step * 4 : step * 2;
-  while (s.up_waves > 1 && s.up_waves * up_step > a.d) s.up_waves /= 2;
+  // fewer where d has no step for each, unless that leaves few workgroups (f32, 115 rows, 4 of 4 of 64 x 256, 8-bit weights
+  // 30.3 with two, 18.4 with eight; 69 rows, 4 of 35 of 64 x 832 51.6 with one, 30.0 with eight; but 3 rows, 2 of 8 of
+  // 256 x 512, which kMoeFew takes, 12.9 with four, 14.9 with eight), and several workgroups an expert for 32 rows each where
+  // there are few (the 115 rows: 18.2 with three, 15.2 with four).
+  while (s.up_waves > 1 && s.up_waves * up_step > a.d && (tiles >= 256 || s.up_variant == kMoeFew)) s.up_waves /= 2;
+  const int64_t up_groups = (a.f * s.up_waves + 127) / 128 * used;
+  s.up_parts = static_cast<int32_t>(std::max<int64_t>(1, std::min(256 / up_groups, (uses + used * 32 - 1) / (used * 32))));
   // (one query, eight experts: 18.4 with the routing in every workgroup, 20.5 with a launch for it; five queries 41 and 35)
   s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kFused && a.m * a.experts * a.d <= 65536 && a.m * tiles <= 1024;
   // The down projection: 32 columns a workgroup, or 4 (one query, two of eight experts of 2816 x 1024: 17.9 with 4 columns,
   // 19.6 with 32; eight queries 37.8 and 41.7, but five with 8-bit weights 32.9 and 31.8; one, 1024 x 4096 19.8 and 17.9; f32,
-  // 8 rows, 4 of 16 of 704 x 256 24.3 and 32),
-  // and its reduction split over about 256 workgroups (64 rows, 4 of 32 of 5632 x 2048 in four 431, in eight 440; 16 rows, 2 of
-  // 8 of 2816 x 1024 in two 47, in eight 42.7).
+  // 8 rows, 4 of 16 of 704 x 256 24.3 and 32).
   s.down_variant = (a.m <= 4 && a.d <= 2048) || (a.m <= 8 && a.d <= (a.down.scale ? 512 : 1024)) ? kMoeFew : kMoeMore;
-  const int64_t columns = s.down_variant == kMoeFew ? 4 : 32, rows = std::min<int64_t>(64, 512 / a.top_k);
-  const int64_t groups = (a.d + columns - 1) / columns * ((a.m + rows - 1) / rows);
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>({16, a.f / (s.down_variant == kMoeFew ? 160 : 80), 256 / groups}));
+  const int64_t columns = s.down_variant == kMoeFew ? 4 : 32, across = (a.d + columns - 1) / columns;
+  s.down_rows = static_cast<int32_t>(std::min<int64_t>(kDownRows, kUses / a.top_k));
+  int64_t groups = across * ((a.m + s.down_rows - 1) / s.down_rows);
   const int64_t down_step = s.down_variant == kMoeFew ? step * 4 : step * 2;
-  s.split_step = static_cast<int32_t>(((a.f + splits - 1) / splits + down_step - 1) / down_step * down_step);
-  s.splits = static_cast<int32_t>((a.f + s.split_step - 1) / s.split_step);
+  // Its items, of about two steps at least, are shared by up to about 256 workgroups, five items or more to each (64 rows, 4 of
+  // 32 of 5632 x 2048 431 in four parts, 440 in eight; 16 rows, 2 of 8 of 2816 x 1024 47 in two, 42.7 in eight; 23 rows, 2 of
+  // 29 of 32 x 165 32.8 in one, 24.6 in five; one row, one of 16 of 1024 x 4096 18.0 in one, 20.0 in two).  With few of those a
+  // workgroup has fewer rows, as long as an expert has four of them or so (bf16, 1000 rows, 4 of 4 of 64 x 256 with 64 rows
+  // 84, with 16 50; 115 rows, 4 of 8 of 64 x 1024 28 and 20.3; but 128 rows, 2 of 8 of 2816 x 1024 76, with 32 79).
+  const int64_t shortest = (a.f + 2 * down_step - 1) / (2 * down_step);   // (parts of two steps)
+  s.splits = static_cast<int32_t>(std::max<int64_t>(1, std::min({int64_t(16), used * shortest / 5, 256 / groups})));
+  while (groups * s.splits <= 128 && s.down_rows > 8 && a.m > s.down_rows / 2 && s.down_rows * a.top_k >= 4 * used) {
+    s.down_rows /= 2;
+    groups = across * ((a.m + s.down_rows - 1) / s.down_rows);
+  }
   // 16 wavefronts where a CU has one workgroup (one query, two of eight experts of 2816 x 1024: 6.4 us of GPU time, with eight
   // 8.0; but of 5632 x 2048, two workgroups a CU, a call 46.2 and with eight 44.0)
-  s.down_waves = groups * splits <= 256 ? 16 : 8;
-  // an expert's part of the reduction is an item of a wavefront; with few experts several are, so that there are 16 or so
-  const int64_t chunks = std::max<int64_t>(1, std::min<int64_t>(s.split_step / (2 * down_step), 16 / used));
-  s.chunk = static_cast<int32_t>(((s.split_step + chunks - 1) / chunks + down_step - 1) / down_step * down_step);
+  s.down_waves = s.down_variant == kMoeFew && groups * s.splits <= 256 ? 16 : 8;
+  const int64_t waves = s.splits * s.down_waves;
+  // (an item a wavefront; where there are more experts than wavefronts, every workgroup has its part of each, since experts
+  // have unlike numbers of rows: 64 rows, 4 of 32 of 5632 x 2048 432 us, an item an expert 436.5)
+  const int64_t chunks = std::min(shortest, waves > used ? (waves + used - 1) / used : s.splits);
+  s.chunk = static_cast<int32_t>(((a.f + chunks - 1) / chunks + down_step - 1) / down_step * down_step);
   if (s.splits > 1) s.partial = ar.take<float>(s.splits * a.m * a.d * 4);
   s.h = ar.take<void>(2 * uses * s.ldh * esize(a.dtype));
   if (!s.chosen) s.chosen = ar.take<int32_t>(uses * 4);
@@ -300,7 +315,8 @@ emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes
   g.h = s.h, g.ldh = s.ldh, g.chosen = s.chosen, g.share = s.share;
   g.up_variant = s.up_variant, g.down_variant = s.down_variant, g.up_waves = s.up_waves;
   g.down_waves = s.down_waves, g.fused = s.fused;
-  g.partial = s.partial, g.splits = s.splits, g.split_step = s.split_step, g.chunk = s.chunk;
+  g.up_parts = s.up_parts, g.down_rows = s.down_rows;
+  g.partial = s.partial, g.splits = s.splits, g.chunk = s.chunk;
   const size_t size = esize(a->dtype);
   g.whole = aligned(a->x, a->ldx, size) && aligned(a->router, a->ldr, size) && aligned(a->gate, size) && aligned(a->up, size) &&
             aligned(a->down, size);
