@@ -1,9 +1,15 @@
 // A layer of experts for few rows on gfx950 (MI355X).  See include/embx_serving.h for the formulas.
 //
-// Three launches: the router (which experts a row takes, and their shares), the gate and up projections of each row's
-// experts with the activation between them, and the down projection, which adds up a row's experts.  Rows and their
-// experts are pairs ("uses"), number row * top_k + place; a workgroup finds the uses of an expert by itself, so nothing is
-// sorted or counted in memory.
+// Two launches with few rows and experts, the gate and up projections of each row's experts with the activation between them
+// and the down projection, which adds up a row's experts; up to three more with more: the router's logits, which experts a
+// row takes and their shares, and a sum over the workgroups that shared the down projection.  Rows and their experts are pairs
+// ("uses"), number row * top_k + place; a workgroup finds the uses of an expert by itself, so nothing is sorted or counted in
+// memory.
+//
+// What bounds it is reading the weights of the experts that are used, once: 64 rows of bf16, 4 of 32 experts of 5632 x 2048, 432
+// us a call, 2.2 GB at 5.1 TB/s (the up projections 272 us, 5.4 TB/s; down 145).  With few rows a launch is not long enough to
+// get there (about 5 us each, of which the loads' and the routing's latency is most): one query, two of eight of 2816 x 1024,
+// 16.6 us, 35 MB; five with 8-bit weights 31.3.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -177,12 +183,12 @@ struct Routing {
   float share[DOTS];
 };
 
-// MANY logits at a time in a wavefront, summed in 64 bits.
-template <int TYPE, bool WHOLE, int MANY, int DOTS>
-__device__ inline void logits(const Moe& a, int first_row, int rows, Routing<DOTS>& out, int wave, int lane) {
+// The logits of x's rows from first_row on, numbers row * experts + expert, MANY at a time in a wavefront, summed in 64 bits: those
+// from `from` on, every eighth, which put(number, logit) takes.
+template <int TYPE, bool WHOLE, int MANY, class PUT>
+__device__ inline void logits(const Moe& a, int first_row, int from, int dots, int lane, PUT put) {
   using T = typename Elem<TYPE>::T;
-  const int dots = rows * a.experts;
-  for (int first = wave; first < dots; first += 8 * MANY) {
+  for (int first = from; first < dots; first += 8 * MANY) {
     const T *r[MANY], *x[MANY];
     double sum[MANY] = {};
 #pragma unroll
@@ -212,7 +218,7 @@ __device__ inline void logits(const Moe& a, int first_row, int rows, Routing<DOT
         for (int n = 0; n < MANY; ++n) sum[n] = fma(double(px[n].get(e)), double(pr[n].get(e)), sum[n]);
     };
     int j = lane * 8;
-#pragma unroll 2
+#pragma unroll (MANY == 1 ? 4 : 2)
     for (; j + 8 <= a.d; j += 512) add(j, std::true_type());
     if (j < a.d) add(j, std::false_type());
 #pragma unroll
@@ -220,7 +226,7 @@ __device__ inline void logits(const Moe& a, int first_row, int rows, Routing<DOT
       for (int step = 32; step > 0; step >>= 1) sum[n] += __shfl_xor(sum[n], step);
 #pragma unroll
     for (int n = 0; n < MANY; ++n)
-      if (lane == n && first + n * 8 < dots) out.logit[first + n * 8] = sum[n], out.key[first + n * 8] = order_of(sum[n]);
+      if (lane == n && first + n * 8 < dots) put(first + n * 8, sum[n]);
   }
 }
 
@@ -228,9 +234,12 @@ __device__ inline void logits(const Moe& a, int first_row, int rows, Routing<DOT
 template <int TYPE, bool WHOLE, int DOTS>
 __device__ inline void route(const Moe& a, int first_row, int rows, Routing<DOTS>& out) {
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), dots = rows * a.experts;
-  if (dots <= 8) logits<TYPE, WHOLE, 1>(a, first_row, rows, out, wave, lane);
-  else if (dots <= 16) logits<TYPE, WHOLE, 2>(a, first_row, rows, out, wave, lane);
-  else logits<TYPE, WHOLE, DOTS <= kFused ? 2 : 4>(a, first_row, rows, out, wave, lane);
+  auto put = [&](int dot, double logit) { out.logit[dot] = logit, out.key[dot] = order_of(logit); };
+  if (a.logits)
+    for (int dot = threadIdx.x; dot < dots; dot += 512) put(dot, a.logits[int64_t(first_row) * a.experts + dot]);
+  else if (dots <= 8) logits<TYPE, WHOLE, 1>(a, first_row, wave, dots, lane, put);
+  else if (DOTS == kPicked || dots <= 16) logits<TYPE, WHOLE, 2>(a, first_row, wave, dots, lane, put);
+  else logits<TYPE, WHOLE, 4>(a, first_row, wave, dots, lane, put);
   __syncthreads();
   // an expert's place: how many come before it
   for (int dot = threadIdx.x; dot < dots; dot += 512) {
@@ -270,6 +279,14 @@ __device__ inline void store(const Moe& a, int first_row, int rows, const Routin
       a.chosen[to] = r.chosen[row * a.top_k + lane];
       a.share[to] = r.share[row * a.top_k + lane];
     }
+}
+
+// Eight logits a workgroup: one workgroup that reads the rows of 256 experts of 4096 took 70 us of the 125 of one query.
+template <int TYPE, bool WHOLE>
+__global__ __launch_bounds__(512) void moe_logits(Moe a) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), first = blockIdx.x * 8;
+  logits<TYPE, WHOLE, 1>(a, blockIdx.y, first + wave, min(a.experts, first + 8), lane,
+                         [&](int e, double logit) { a.logits[int64_t(blockIdx.y) * a.experts + e] = logit; });
 }
 
 // a workgroup a row
@@ -445,8 +462,11 @@ struct Uses {
 // act(x Wg^T) * (x Wu^T) of an expert's uses: 16 / S columns of each of which some wavefronts share the reduction.  The
 // result is stored as two values of the type, the rounded one and the rest, so that the product with Wd has it in nearly 32
 // bits: one part alone would make results 1.4 times as far from exact ones as their own rounding makes them.
-// ROUTE: for few rows and experts (a.m * a.experts of kFused at most) every workgroup works out the routing by itself, and the
-// first one stores it, instead of a launch before this one.
+// ROUTE: every workgroup routes by itself (kFused, kPicked logits at most), and the first one stores it, instead of a launch
+// before this one.
+// Every wavefront loads the next 128 bytes of its rows of both matrices, or 256 where 4 rows are all, while it multiplies those
+// before: whole lines, and enough under way with the CU's other wavefronts.  64 bytes at a time instead took 64 rows, 4 of 32 of
+// 5632 x 2048 from 433 us to 517.
 template <int TYPE, bool EIGHT, bool WHOLE, int S, int FR, bool ROUTE>
 __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_up(Moe a) {
   using T = typename Elem<TYPE>::T;
@@ -457,7 +477,7 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
   const int sharing = a.up_waves, groups = kWaves / sharing;   // wavefronts that share a reduction; 16 / S columns each
   const int j0 = (blockIdx.x * groups + wave / sharing) * kRows;
   const int64_t uses = int64_t(a.m) * a.top_k;
-  __shared__ Routing<ROUTE ? kFused : 1> r;
+  __shared__ Routing<ROUTE ? kPicked : 1> r;
   const int32_t* chosen = a.chosen;
   if constexpr (ROUTE) {
     route<TYPE, WHOLE>(a, 0, a.m, r);
@@ -690,7 +710,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   }
 }
 
-// the parts of a split reduction, added up in order
+// the parts of workgroups that shared a down projection, added up in order.  (About 3 us a call.  The last workgroup to arrive can
+// do it, but has to write its CUs' caches back first and the others' parts may not be in its own: five rows, 2 of 8 of
+// 2816 x 1024 with 8-bit weights 66 us so, 32 with this launch.)
 template <int TYPE>
 __global__ __launch_bounds__(256) void moe_join(Moe a) {
   const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x, all = int64_t(a.m) * a.d;
@@ -705,6 +727,10 @@ int up(const Moe& a, hipStream_t s) {
   const int columns = 16 / S * (kWaves / a.up_waves);
   const int64_t experts = std::min<int64_t>(int64_t(a.m) * a.top_k, a.experts);
   const dim3 grid((a.f + columns - 1) / columns, static_cast<uint32_t>(experts), a.up_parts);
+  if (a.logits) {
+    moe_logits<TYPE, WHOLE><<<dim3((a.experts + 7) / 8, static_cast<uint32_t>(a.m)), 512, 0, s>>>(a);
+    if (const int rc = hipGetLastError(); rc != 0) return rc;
+  }
   if (a.fused && FR == 1) {
     moe_up<TYPE, EIGHT, WHOLE, S, 1, true><<<grid, 512, 0, s>>>(a);
   } else {

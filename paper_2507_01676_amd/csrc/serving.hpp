@@ -35,7 +35,8 @@ struct Moe {
   int32_t up_variant, down_variant;   // MoeVariant
   int32_t up_waves;        // wavefronts that share a reduction of the up projections: 1, 2, 4 or 8
   int32_t down_waves;      // kMoeFew: wavefronts of a workgroup of the down projection, 8 or 16
-  int32_t fused;           // see kFused
+  double* logits;          // [m][experts], which a launch of its own works out, or NULL
+  int32_t fused;           // every workgroup of the up projections routes by itself: see kFused and kPicked
   int32_t whole;           // rows of all operands start at multiples of 16 bytes
   int32_t up_parts;        // workgroups that share an expert's rows and columns of the up projections
   int32_t down_rows;       // of x that a workgroup of the down projection has: kDownRows, and kUses / top_k, at most
@@ -46,7 +47,8 @@ struct Moe {
 // How many rows of x an expert has at a time: at most 4 (by 4 rows of weights), 16, or several times 16.
 enum MoeVariant { kMoeFew = 0, kMoeMore = 1, kMoeMany = 2 };
 
-constexpr int kFused = 32;   // logits of all rows that every workgroup of the up projections works out by itself
+// Logits of all rows that every workgroup of the up projections works out, or of which it picks the experts, by itself
+constexpr int kFused = 32, kPicked = 256;
 
 constexpr int kMostExperts = 1024, kMostTopK = 32;
 constexpr int kUses = 512;       // uses, row * top_k + place, that a workgroup looks at at a time

@@ -156,22 +156,24 @@ struct MoeSpace {
   int32_t* chosen;
   float* share;
   float* partial;
+  double* logits;
   int32_t up_variant, down_variant, up_waves, down_waves, fused, up_parts, down_rows, splits, chunk;
 };
 
 MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   const int64_t uses = a.m * a.top_k;
-  MoeSpace s = {nullptr, (a.f + 7) / 8 * 8, a.chosen, a.share};
+  MoeSpace s = {};
+  s.ldh = (a.f + 7) / 8 * 8, s.chosen = a.chosen, s.share = a.share;
   const int64_t used = std::min<int64_t>(uses, a.experts);   // experts, at most
   const int64_t step = a.gate.scale ? 64 : 32;               // of the reduction: a matrix instruction, or two
   // The up projections: 16 columns of an expert to so many wavefronts, or 4 where there would be few workgroups and few rows
   // (us a call: one query, one expert of 1024 x 4096 28.4 with 16 columns, 23.3 with 4; two of eight of 2816 x 1024 22.6 and
   // 26.3).  Four wavefronts share the reduction, and a workgroup has 32 columns, where that leaves workgroups enough (64 rows,
   // 4 of 32 experts of 5632 x 2048 441 with eight, 432 with four; 19 rows, 3 of 7 of 333 x 1001 35.7 and 40.9).  Several times
-  // 16 rows of an expert at once where it is expected to have more than 12 (128 rows, 2 of 8 91.5 with 16 at a time, 75.8 with
-  // 64).
+  // 16 rows of an expert at once where it is expected to have more than 14 (128 rows, 2 of 8 91.6 with 16 at a time, 75.7 with
+  // 64; f32, 64 rows, 2 of 8 of 704 x 1024 48.0 and 44.0; but 200 rows, 4 of 64 of 704 x 4096 555 and 604).
   const int64_t tiles = (a.f + 15) / 16 * used;
-  s.up_variant = a.m <= 4 && tiles < 256 ? kMoeFew : uses <= 12 * a.experts ? kMoeMore : kMoeMany;
+  s.up_variant = a.m <= 4 && tiles < 256 ? kMoeFew : uses <= 14 * a.experts ? kMoeMore : kMoeMany;
   s.up_waves = s.up_variant != kMoeFew && tiles >= 352 ? 4 : 8;
   const int64_t up_step = s.up_variant == kMoeFew ? step * 4 : step * 2;
   // fewer where d has no step for each, unless that leaves few workgroups (f32, 115 rows, 4 of 4 of 64 x 256, 8-bit weights
@@ -183,6 +185,13 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   s.up_parts = static_cast<int32_t>(std::max<int64_t>(1, std::min(256 / up_groups, (uses + used * 32 - 1) / (used * 32))));
   // (one query, eight experts: 18.4 with the routing in every workgroup, 20.5 with a launch for it; five queries 41 and 35)
   s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kFused && a.m * a.experts * a.d <= 65536 && a.m * tiles <= 1024;
+  // Logits in workgroups of their own where one would read the rows of many experts (one query, 8 of 256 of 1024 x 4096 125 us,
+  // so 61; 4 of 64 of 704 x 2048 29 and 23.7; 22 rows, 2 of 20 of 1792 x 1088 62.6 and 62.0; but 8 rows, 4 of 16 of 704 x 256 23.0
+  // and 24.5), and what is left of the routing in every workgroup of the up projections up to kPicked (those of 256 63 us with
+  // a launch for it; f32, two rows, 4 of 64 of 512 x 1024 24.4 and 25.9)
+  const bool apart = a.m <= 256 && a.experts > 16;
+  if (apart) s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kPicked;
+  if (apart) s.logits = ar.take<double>(a.m * a.experts * 8);
   // The down projection: 32 columns a workgroup, or 4 (one query, two of eight experts of 2816 x 1024: 17.9 with 4 columns,
   // 19.6 with 32; eight queries 37.8 and 41.7, but five with 8-bit weights 32.9 and 31.8; one, 1024 x 4096 19.8 and 17.9; f32,
   // 8 rows, 4 of 16 of 704 x 256 24.3 and 32).
@@ -314,7 +323,7 @@ emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes
   }
   g.h = s.h, g.ldh = s.ldh, g.chosen = s.chosen, g.share = s.share;
   g.up_variant = s.up_variant, g.down_variant = s.down_variant, g.up_waves = s.up_waves;
-  g.down_waves = s.down_waves, g.fused = s.fused;
+  g.down_waves = s.down_waves, g.fused = s.fused, g.logits = s.logits;
   g.up_parts = s.up_parts, g.down_rows = s.down_rows;
   g.partial = s.partial, g.splits = s.splits, g.chunk = s.chunk;
   const size_t size = esize(a->dtype);

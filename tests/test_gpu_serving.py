@@ -228,6 +228,15 @@ def test_moe(gpu_lib, size, dtype, eight):
     assert bool(torch.isnan(around).all()), "written outside the result"
 
 
+@pytest.mark.parametrize("eight", [False, True], ids=["float", "int8"])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [(1, 40, 600, 256, 8), (2, 33, 65, 64, 6), (3, 24, 1500, 17, 17), (12, 130, 48, 20, 2), (15, 16, 33, 17, 1),
+                                  (1, 20, 7, 1024, 32), (256, 17, 20, 18, 3), (257, 17, 20, 18, 3)], ids=str)
+def test_moe_many_experts(gpu_lib, size, dtype, eight):
+    """Logits in a launch of their own, and their experts picked in the next one's workgroups or in a launch too."""
+    test_moe(gpu_lib, size, dtype, eight)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_moe_shares_over_all(gpu_lib, dtype):
     size = (21, 40, 72, 9, 3)
