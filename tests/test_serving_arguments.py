@@ -141,8 +141,8 @@ def test_linear_int8_workspace(x_scale, m, n, k):
         code, need = size(a)
         assert code == embx.OK and need < 4 << 30
         padded = (k + 15) // 16 * 16
-        if not whole:
-            assert need >= n * padded           # the weights' copy
+        if not whole and m > 1000:
+            assert need >= n * padded           # the weights' copy; few rows' kernels read them where they lie
         if x_scale is None and m > 8:
             assert need >= m * padded + 4 * m   # quantized x
         if need:
