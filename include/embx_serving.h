@@ -26,8 +26,9 @@
  * moe: logits are summed in 64 bits, so which experts a row takes does not depend on the order
  * of the sums; NaN counts as the largest logit, and makes the row's shares and results NaN,
  * as does an infinite one that is the largest.  Sums are held in f32, and so are shares.
- * act(..) * (..) is rounded to the call's type before the product with Wd, as the matrix
- * cores take it; the result is rounded once.  The experts' matrices have the call's type, or
+ * act(..) * (..) goes into the product with Wd in f32 or, with 16-bit types, as two values of
+ * the type, the rounded one and the rest (in f16 an infinity beyond 65504); the result is
+ * rounded once.  The experts' matrices have the call's type, or
  * are 8-bit integers with a scale for each of their rows (all three or none).  A row's result
  * depends on that row and its experts only.  It is made for few rows, where the layer is bound
  * by reading the experts' matrices; any number is right.
@@ -38,8 +39,8 @@
  * A call's outputs and workspace must not overlap its inputs, except that linear_int8's y may
  * be the residual itself (same pointer and row stride).  Calls that share a workspace must
  * not overlap in time.  Nothing is kept between calls, and equal calls give equal bits.
- * Where an operand's rows start at multiples of 16 bytes, the 16 bytes that hold a row's end
- * are read whole; what they hold behind it does not matter.
+ * The aligned 16 bytes, or 4, that hold a row's start or end may be read whole; what they hold
+ * beside the row does not matter.
  *
  * Errors (emb_status_t of embx.h): EMB_ERR_INVALID_ARGUMENT for a NULL or misaligned pointer,
  * a size below its least (m >= 0, the others >= 1), a row stride below its row, top_k above
@@ -47,8 +48,8 @@
  * that is NULL or too small; EMB_ERR_UNSUPPORTED for an unknown type, m or n above 2^30,
  * a stride above 2^40, linear_int8's k above 131071 (its sums have to fit 32 bits) and
  * quantize's above 2^30, experts above 1024, top_k above 32, moe's m above 65536, its f, d or
- * experts' row strides above 2^25, or a product too large for a launch; EMB_ERR_DEVICE if a launch fails.  With
- * m == 0 calls do nothing.
+ * experts' row strides above 2^25, or a product too large for a launch; EMB_ERR_DEVICE if a
+ * launch fails.  With m == 0 calls do nothing.
  */
 #ifndef EMBX_SERVING_H
 #define EMBX_SERVING_H
