@@ -30,8 +30,9 @@
  * the type, the rounded one and the rest (in f16 an infinity beyond 65504); the result is
  * rounded once.  The experts' matrices have the call's type, or
  * are 8-bit integers with a scale for each of their rows (all three or none).  A row's result
- * depends on that row and its experts only.  It is made for few rows, where the layer is bound
- * by reading the experts' matrices; any number is right.
+ * comes from that row and its experts only; in which order its sums are added up, and so
+ * their last bits in f32, is up to the whole call.  It is made for few rows, where the layer
+ * is bound by reading the experts' matrices; any number is right.
  *
  * Calls take plain device pointers of the current HIP device, aligned to their element; the
  * structs are host memory, read during the call.  No call allocates or synchronizes; each

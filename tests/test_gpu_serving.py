@@ -274,7 +274,7 @@ def test_moe_ties_and_values_that_are_not_finite(gpu_lib):
 
 
 def test_moe_a_row_alone(gpu_lib):
-    """A row's result depends on that row and its experts: the same bits alone and among others that hold NaN."""
+    """A row's result comes from that row and its experts, also beside a row of NaN; equal calls give equal bits."""
     import torch
     for dtype in TYPES:
         o = moe_operands((30, 70, 90, 4, 2), dtype, 4, False)
