@@ -425,6 +425,10 @@ constexpr int waves_of(int fragments) {
   return fragments * (EIGHT ? 2 : 1) * (TYPE == kDenseF32 ? 2 : 1) + (WHOLE ? 0 : EIGHT ? 2 : 4) <= (TYPE == kDenseF32 || EIGHT ? 3 : 4) ? 4 : 2;
 }
 
+// Uses of an expert that a workgroup lists before it multiplies, so that it reads the weights once for them: as many as leave
+// room for two workgroups a CU.
+constexpr int kListed = kUses + 192;
+
 // The uses of one expert among up to kUses of them, `first` .. `first + count - 1`: a wavefront lists them in LDS of its own,
 // in order, and has their number.
 struct Uses {
@@ -445,13 +449,13 @@ struct Uses {
     return __any(is);
   }
 
-  __device__ int list(int expert, uint16_t* to, int count, int lane) const {
-    int have = 0;
+  // behind the `have` that are listed, with `before` added
+  __device__ int list(int expert, uint16_t* to, int have, int before, int count, int lane) const {
 #pragma unroll
     for (int n = 0; n < kUses / 64; ++n) {
       if (n * 64 >= count) break;
       const uint64_t mask = __ballot(id[n] == expert);
-      if (id[n] == expert) to[have + __popcll(mask & ((uint64_t(1) << lane) - 1))] = static_cast<uint16_t>(n * 64 + lane);
+      if (id[n] == expert) to[have + __popcll(mask & ((uint64_t(1) << lane) - 1))] = static_cast<uint16_t>(before + n * 64 + lane);
       have += __popcll(mask);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -471,7 +475,7 @@ template <int TYPE, bool EIGHT, bool WHOLE, int S, int FR, bool ROUTE>
 __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_up(Moe a) {
   using T = typename Elem<TYPE>::T;
   constexpr int kRows = 16 / S, kTokens = 16 / S * FR;
-  __shared__ uint16_t lists[kWaves][kUses];
+  __shared__ uint16_t lists[kWaves][kListed];
   __shared__ float sums[kWaves][2][kTokens][kRows + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const int sharing = a.up_waves, groups = kWaves / sharing;   // wavefronts that share a reduction; 16 / S columns each
@@ -502,14 +506,20 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
     row[n] = (static_cast<uint32_t>(lane_row) * static_cast<uint32_t>(a.ldw[n]) + P::own(lane)) * P::Ws::kSize;
   }
   const int begin = wave % sharing * P::kAll, every = sharing * P::kAll;
-  for (int64_t first = 0; first < uses; first += kUses) {
-    const int count = static_cast<int>(min(uses - first, int64_t(kUses)));
-    Uses u;
-    u.read(chosen + first, count, lane);
-    if (!u.any(expert)) continue;
+  for (int64_t first = 0, next = 0; first < uses; first = next) {
     P one, two;
-    if (begin + P::kAll <= a.d) one.load_w(base, row, begin);   // before the uses are listed
-    const int have = u.list(expert, lists[wave], count, lane);   // (which the workgroups along z share)
+    int have = 0;   // uses, which the workgroups along z share
+    do {
+      const int count = static_cast<int>(min(uses - next, int64_t(kUses)));
+      Uses u;
+      u.read(chosen + next, count, lane);
+      if (u.any(expert)) {
+        if (have == 0 && begin + P::kAll <= a.d) one.load_w(base, row, begin);   // before they are listed
+        have = u.list(expert, lists[wave], have, static_cast<int>(next - first), count, lane);
+      }
+      next += count;
+    } while (next < uses && have <= kListed - kUses && next - first <= 65536 - kUses);
+    if (have == 0) continue;
     for (int at = blockIdx.z * kTokens; at < have; at += gridDim.z * kTokens) {
       const char* x[FR];
 #pragma unroll
@@ -620,7 +630,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   auto begin_item = [&](Place& p) {
     p.expert = __builtin_amdgcn_readfirstlane(used[p.item / chunks]);
     p.which ^= 1;
-    p.have = u.list(p.expert, lists[wave][p.which], count, lane);
+    p.have = u.list(p.expert, lists[wave][p.which], 0, 0, count, lane);
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
       const int row0 = min(j0 + i * kRows, a.d - 1);
@@ -710,6 +720,95 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   }
 }
 
+// The same for many rows: the uses of one expert and 32 columns for some wavefronts, as in moe_up, so that its weights are read
+// once, and not once for every a.down_rows rows: 200 rows, 4 of 64 of 704 x 4096 302 us a call, by rows 445.  Results go to
+// memory in f32, a row for each use, without their shares.
+template <int TYPE, bool WHOLE, int FR>
+__global__ __launch_bounds__(512, (waves_of<TYPE, false, WHOLE>(TYPE == kDenseF32 ? FR : 2 * FR))) void moe_down_each(Moe a) {
+  using T = typename Elem<TYPE>::T;
+  constexpr int kParts = TYPE == kDenseF32 ? 1 : 2, kTokens = 16 * FR, kCols = 32;
+  __shared__ uint16_t lists[kWaves][kListed];
+  __shared__ float sums[kWaves][kTokens][kCols + 1];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
+  const int sharing = a.down_waves, groups = kWaves / sharing, expert = blockIdx.y;
+  const int j0 = (blockIdx.x * groups + wave / sharing) * kCols;
+  const int64_t uses = int64_t(a.m) * a.top_k, part = uses * a.ldh * sizeof(T);
+  using P = Step<TYPE, false, WHOLE, true, 1, 2, FR, kParts>;
+  const char* base[2];
+  uint32_t row[2];
+#pragma unroll
+  for (int n = 0; n < 2; ++n) {
+    const int row0 = min(j0 + n * 16, a.d - 1), lane_row = min(j0 + n * 16 + c, a.d - 1) - row0;
+    base[n] = static_cast<const char*>(a.w[2]) + (expert * a.stride[2] + row0 * a.ldw[2]) * P::Ws::kSize;
+    row[n] = (static_cast<uint32_t>(lane_row) * static_cast<uint32_t>(a.ldw[2]) + P::own(lane)) * P::Ws::kSize;
+  }
+  const int begin = wave % sharing * P::kAll, every = sharing * P::kAll;
+  for (int64_t first = 0, next = 0; first < uses; first = next) {
+    P one, two;
+    int have = 0;   // uses, which the workgroups along z share
+    do {
+      const int count = static_cast<int>(min(uses - next, int64_t(kUses)));
+      Uses u;
+      u.read(a.chosen + next, count, lane);
+      if (u.any(expert)) {
+        if (have == 0 && begin + P::kAll <= a.f) one.load_w(base, row, begin);   // before they are listed
+        have = u.list(expert, lists[wave], have, static_cast<int>(next - first), count, lane);
+      }
+      next += count;
+    } while (next < uses && have <= kListed - kUses && next - first <= 65536 - kUses);
+    if (have == 0) continue;
+    for (int at = blockIdx.z * kTokens; at < have; at += gridDim.z * kTokens) {
+      const char* h[FR];
+#pragma unroll
+      for (int f = 0; f < FR; ++f)
+        h[f] = static_cast<const char*>(a.h) + ((first + lists[wave][min(at + f * 16 + c, have - 1)]) * a.ldh + P::own(lane)) * P::kSizeX;
+      f32x4 acc[2][FR] = {};
+      int r0 = begin;
+      if (begin + P::kAll <= a.f) {
+        if (at != static_cast<int>(blockIdx.z) * kTokens) one.load_w(base, row, begin);
+        one.load_x(h, part, begin);
+        auto go = [&](const P& now, P& next) {   // whether there is a next one
+          r0 += every;
+          const bool more = r0 + P::kAll <= a.f;
+          if (more) next.load_w(base, row, r0), next.load_x(h, part, r0);
+          now.multiply(base, row, h, acc);
+          return more;
+        };
+        while (go(one, two) && go(two, one)) {}
+      }
+      if (r0 < a.f) one.rest(base, row, h, part, r0, a.f, lane, acc);
+#pragma unroll
+      for (int f = 0; f < FR; ++f)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sums[wave][f * 16 + c][i * 16 + 4 * q + e] = acc[i][f][e];
+      __syncthreads();
+      for (int t = threadIdx.x; t < kTokens * kCols * groups; t += 512) {
+        const int r = t / (kCols * groups), group = t / kCols % groups, column = t % kCols;
+        const int j = (blockIdx.x * groups + group) * kCols + column;
+        if (at + r >= have || j >= a.d) continue;
+        float v = 0.0f;
+#pragma unroll
+        for (int n = 0; n < kWaves; ++n) v += n < sharing ? sums[group * sharing + min(n, sharing - 1)][r][column] : 0.0f;
+        a.partial[(first + lists[wave][at + r]) * a.d + j] = v;
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// and the sums over a row's experts
+template <int TYPE>
+__global__ __launch_bounds__(256) void moe_join_uses(Moe a) {
+  const int64_t at = int64_t(blockIdx.x) * 256 + threadIdx.x;
+  const int64_t row = at / a.d, j = at % a.d;
+  if (row >= a.m) return;
+  float s = 0.0f;
+  for (int64_t use = row * a.top_k; use < (row + 1) * a.top_k; ++use) s += a.share[use] * a.partial[use * a.d + j];
+  static_cast<typename Elem<TYPE>::T*>(a.y)[row * a.ldy + j] = typename Elem<TYPE>::T(s);
+}
+
 // the parts of workgroups that shared a down projection, added up in order.  (About 3 us a call.  The last workgroup to arrive can
 // do it, but has to write its CUs' caches back first and the others' parts may not be in its own: five rows, 2 of 8 of
 // 2816 x 1024 with 8-bit weights 66 us so, 32 with this launch.)
@@ -749,6 +848,17 @@ int down(const Moe& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <int TYPE, bool WHOLE>
+int down_each(const Moe& a, hipStream_t s) {
+  const int columns = 32 * (kWaves / a.down_waves);
+  const dim3 grid((a.d + columns - 1) / columns, a.experts, a.down_parts);
+  if (TYPE == kDenseF32 || a.down_blocks == 1) moe_down_each<TYPE, WHOLE, 1><<<grid, 512, 0, s>>>(a);
+  else moe_down_each<TYPE, WHOLE, TYPE == kDenseF32 ? 1 : 2><<<grid, 512, 0, s>>>(a);
+  if (const int rc = hipGetLastError(); rc != 0) return rc;
+  moe_join_uses<TYPE><<<static_cast<uint32_t>((int64_t(a.m) * a.d + 255) / 256), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
 template <int TYPE, bool EIGHT, bool WHOLE>
 int launch(const Moe& a, hipStream_t s) {
   constexpr int kMany = EIGHT || TYPE == kDenseF32 ? 2 : 4;   // (as many as there are registers for)
@@ -759,6 +869,8 @@ int launch(const Moe& a, hipStream_t s) {
     default: rc = up<TYPE, EIGHT, WHOLE, 1, kMany>(a, s); break;
   }
   if (rc != 0) return rc;
+  if constexpr (!EIGHT)
+    if (a.down_variant == kMoeMany) return down_each<TYPE, WHOLE>(a, s);
   if (a.down_variant != kMoeFew) rc = down<TYPE, EIGHT, WHOLE, 1, 2, 8>(a, s);
   else if (a.down_waves == 16) rc = down<TYPE, EIGHT, WHOLE, 4, 1, 16>(a, s);
   else rc = down<TYPE, EIGHT, WHOLE, 4, 1, 8>(a, s);

@@ -30,21 +30,23 @@ struct Moe {
   int32_t* chosen;         // [m][top_k]
   float* share;            // [m][top_k]
   int64_t ldx, ldr, ldh, ldy, ldw[3], stride[3];
-  float* partial;          // [splits][m][d], with splits > 1
+  float* partial;          // [splits][m][d], with splits > 1; kMoeMany: [m][top_k][d]
   int32_t m, f, d, experts, top_k, act, renormalize;
   int32_t up_variant, down_variant;   // MoeVariant
   int32_t up_waves;        // wavefronts that share a reduction of the up projections: 1, 2, 4 or 8
-  int32_t down_waves;      // kMoeFew: wavefronts of a workgroup of the down projection, 8 or 16
+  int32_t down_waves;      // of the down projection.  kMoeFew: wavefronts of a workgroup, 8 or 16; kMoeMany: that share a reduction
   double* logits;          // [m][experts], which a launch of its own works out, or NULL
   int32_t fused;           // every workgroup of the up projections routes by itself: see kFused and kPicked
   int32_t whole;           // rows of all operands start at multiples of 16 bytes
+  int32_t down_parts, down_blocks;   // kMoeMany: workgroups that share an expert's rows and columns, and 16s of rows at a time
   int32_t up_parts;        // workgroups that share an expert's rows and columns of the up projections
   int32_t down_rows;       // of x that a workgroup of the down projection has: kDownRows, and kUses / top_k, at most
   int32_t splits;          // workgroups that share those rows and its columns
   int32_t chunk;           // of the down projection's reduction, that a wavefront takes at a time
 };
 
-// How many rows of x an expert has at a time: at most 4 (by 4 rows of weights), 16, or several times 16.
+// How many rows of x an expert has at a time: at most 4 (by 4 rows of weights), 16, or several times 16; of the down
+// projection kMoeMany works by experts, the others by rows.
 enum MoeVariant { kMoeFew = 0, kMoeMore = 1, kMoeMany = 2 };
 
 // Logits of all rows that every workgroup of the up projections works out, or of which it picks the experts, by itself

@@ -14,6 +14,7 @@ namespace {
 constexpr int64_t kMaxSize = int64_t(1) << 30, kMaxStride = int64_t(1) << 40;
 constexpr int64_t kMostInputs = 131071;        // of sums of 8-bit products in 32 bits: 2^14 each
 constexpr int64_t kMostRows = 65536, kMostColumns = int64_t(1) << 25;   // moe
+constexpr int64_t kMostPartial = 64 << 20;   // moe: elements
 constexpr size_t kAlign = 256;
 
 #define EMBX_TRY(x)                       \
@@ -157,7 +158,7 @@ struct MoeSpace {
   float* share;
   float* partial;
   double* logits;
-  int32_t up_variant, down_variant, up_waves, down_waves, fused, up_parts, down_rows, splits, chunk;
+  int32_t up_variant, down_variant, down_parts, down_blocks, up_waves, down_waves, fused, up_parts, down_rows, splits, chunk;
 };
 
 MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
@@ -169,12 +170,14 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   // The up projections: 16 columns of an expert to so many wavefronts, or 4 where there would be few workgroups and few rows
   // (us a call: one query, one expert of 1024 x 4096 28.4 with 16 columns, 23.3 with 4; two of eight of 2816 x 1024 22.6 and
   // 26.3).  Four wavefronts share the reduction, and a workgroup has 32 columns, where that leaves workgroups enough (64 rows,
-  // 4 of 32 experts of 5632 x 2048 441 with eight, 432 with four; 19 rows, 3 of 7 of 333 x 1001 35.7 and 40.9).  Several times
+  // 4 of 32 experts of 5632 x 2048 441 with eight, 432 with four; 19 rows, 3 of 7 of 333 x 1001 35.7 and 40.9) and rows are not
+  // long (16 rows, 4 of 32 of 2048 x 4096 252 and 284; 200 rows, 4 of 64 of 704 x 4096 302 and 320).  Several times
   // 16 rows of an expert at once where it is expected to have more than 14 (128 rows, 2 of 8 91.6 with 16 at a time, 75.7 with
   // 64; f32, 64 rows, 2 of 8 of 704 x 1024 48.0 and 44.0; but 200 rows, 4 of 64 of 704 x 4096 555 and 604).
   const int64_t tiles = (a.f + 15) / 16 * used;
   s.up_variant = a.m <= 4 && tiles < 256 ? kMoeFew : uses <= 14 * a.experts ? kMoeMore : kMoeMany;
-  s.up_waves = s.up_variant != kMoeFew && tiles >= 352 ? 4 : 8;
+  const int64_t size = a.gate.scale ? 1 : static_cast<int64_t>(esize(a.dtype));   // of a weight
+  s.up_waves = s.up_variant != kMoeFew && tiles >= 352 && a.d * size < 8192 ? 4 : 8;
   const int64_t up_step = s.up_variant == kMoeFew ? step * 4 : step * 2;
   // fewer where d has no step for each, unless that leaves few workgroups (f32, 115 rows, 4 of 4 of 64 x 256, 8-bit weights
   // 30.3 with two, 18.4 with eight; 69 rows, 4 of 35 of 64 x 832 51.6 with one, 30.0 with eight; but 3 rows, 2 of 8 of
@@ -196,6 +199,12 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   // 19.6 with 32; eight queries 37.8 and 41.7, but five with 8-bit weights 32.9 and 31.8; one, 1024 x 4096 19.8 and 17.9; f32,
   // 8 rows, 4 of 16 of 704 x 256 24.3 and 32).
   s.down_variant = (a.m <= 4 && a.d <= 2048) || (a.m <= 8 && a.d <= (a.down.scale ? 512 : 1024)) ? kMoeFew : kMoeMore;
+  // Or, for more rows than that has at a time, an expert's uses together, and the sums over a row's experts in another launch
+  // (200 rows, 4 of 64 of 704 x 4096 333 and 445; 1000 rows, 6 of 64 of 704 x 1024 337 and 433; 128 rows, 2 of 8 of
+  // 2816 x 1024 71.9 and 75.5), unless the weights are few or of 8 bits (512 rows, 4 of 8 of 256 x 512 37 and 32; 128 rows, 4 of
+  // 32 of 704 x 2048 with 8 bits 94 and 82).
+  const bool many = a.m > kDownRows && !a.down.scale && a.experts * a.f * a.d * size >= 4 << 20;
+  if (many && uses * a.d <= kMostPartial) s.down_variant = kMoeMany;
   const int64_t columns = s.down_variant == kMoeFew ? 4 : 32, across = (a.d + columns - 1) / columns;
   s.down_rows = static_cast<int32_t>(std::min<int64_t>(kDownRows, kUses / a.top_k));
   int64_t groups = across * ((a.m + s.down_rows - 1) / s.down_rows);
@@ -219,6 +228,20 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   // have unlike numbers of rows: 64 rows, 4 of 32 of 5632 x 2048 432 us, an item an expert 436.5)
   const int64_t chunks = std::min(shortest, waves > used ? (waves + used - 1) / used : s.splits);
   s.chunk = static_cast<int32_t>(((a.f + chunks - 1) / chunks + down_step - 1) / down_step * down_step);
+  if (s.down_variant == kMoeMany) {
+    // (eight wavefronts share a reduction, or fewer where that leaves workgroups and steps enough: the 200 rows 493 with eight,
+    // 478 with two; 256 rows, 2 of 16 of 1408 x 2048 128 and 130.  16 rows at a time, or 32 where there are as many: the 200
+    // rows 478 with 16, 501 with 32; 100 rows, 2 of 9 of 1111 x 777 48.6 and 44.4)
+    auto workgroups = [&](int64_t sharing) { return (a.d * sharing + 255) / 256 * a.experts; };
+    s.down_waves = 8;
+    auto fewer = [&] { return s.down_waves * 64 > a.f || (s.down_waves > 2 && workgroups(s.down_waves / 2) >= 512); };
+    while (s.down_waves > 1 && fewer()) s.down_waves /= 2;
+    s.down_blocks = uses > 14 * a.experts && a.dtype != EMB_DTYPE_F32 ? 2 : 1;
+    const int64_t tile = 16 * s.down_blocks, tiles_each = (uses / a.experts + 16 + tile - 1) / tile;
+    s.down_parts = static_cast<int32_t>(std::max<int64_t>(1, std::min(512 / workgroups(s.down_waves), tiles_each)));
+    s.splits = 1;
+    s.partial = ar.take<float>(uses * a.d * 4);
+  }
   if (s.splits > 1) s.partial = ar.take<float>(s.splits * a.m * a.d * 4);
   s.h = ar.take<void>(2 * uses * s.ldh * esize(a.dtype));
   if (!s.chosen) s.chosen = ar.take<int32_t>(uses * 4);
@@ -324,6 +347,7 @@ emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes
   g.h = s.h, g.ldh = s.ldh, g.chosen = s.chosen, g.share = s.share;
   g.up_variant = s.up_variant, g.down_variant = s.down_variant, g.up_waves = s.up_waves;
   g.down_waves = s.down_waves, g.fused = s.fused, g.logits = s.logits;
+  g.down_parts = s.down_parts, g.down_blocks = s.down_blocks;
   g.up_parts = s.up_parts, g.down_rows = s.down_rows;
   g.partial = s.partial, g.splits = s.splits, g.chunk = s.chunk;
   const size_t size = esize(a->dtype);

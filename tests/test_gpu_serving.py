@@ -238,6 +238,14 @@ def test_moe_many_experts(gpu_lib, size, dtype, eight):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [(65, 500, 1100, 4, 2), (70, 501, 1101, 4, 1), (800, 300, 1000, 8, 4), (700, 100, 700, 64, 2),
+                                  (100, 64, 1100, 32, 16), (1300, 20, 3000, 40, 1), (90, 4000, 33, 17, 3), (66, 31, 3001, 24, 24)], ids=str)
+def test_moe_by_experts(gpu_lib, size, dtype):
+    """Down projections by experts: more than 64 rows and 4 MB of weights; uses in one list and several, tiles full and not."""
+    test_moe(gpu_lib, size, dtype, False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
 def test_moe_shares_over_all(gpu_lib, dtype):
     size = (21, 40, 72, 9, 3)
     o = moe_operands(size, dtype, 2, False)
