@@ -1714,8 +1714,9 @@ template <int FR, int ALIGN>
 int rows_i8_launch(const DenseGemm& g, uint32_t grid, uint32_t down, hipStream_t stream) {
   const uint32_t wide = (g.nj + 31) / 32;
   if (FR > 1 || !g.quantize) {
-    // 32 columns, which read x half as often, where there are workgroups enough (19 x 8192 x 4096 11.8 us, with 16 13.5)
-    if (down < kXcds && wide * down >= 256) dense_rows_i8<kDenseI8, FR, 2, ALIGN><<<wide * down, 512, 0, stream>>>(g);
+    // (32 columns read x half as often, and may be one round of workgroups instead of two: 19 x 8192 x 4096 11.8 us, with 16
+    // 13.5; 16 x 5120 x 1024 4.8 and 7.6; but 1 x 8192 x 8192 20.7 and 16.0)
+    if (g.row_columns == 2) dense_rows_i8<kDenseI8, FR, 2, ALIGN><<<wide * down, 512, 0, stream>>>(g);
     else dense_rows_i8<kDenseI8, FR, 1, ALIGN><<<grid, 512, 0, stream>>>(g);
   } else if (g.result == kDenseF32) {
     dense_rows_i8<kDenseF32, 1, 1, ALIGN><<<grid, 512, 0, stream>>>(g);

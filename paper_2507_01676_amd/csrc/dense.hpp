@@ -46,6 +46,7 @@ struct DenseGemm {
   int32_t parts, splits, act;   // parts = 0: no product
   int32_t variant;         // DenseVariant
   int32_t row_blocks;      // kRows: 16 rows each, of a workgroup: 1, 2 or 4
+  int32_t row_columns;     // kRows of 8-bit integers: 16 columns each, of a workgroup: 1 or 2
   int32_t row_chunks, short_waves;   // kShort: chunks of 64 rows of a workgroup, its wavefronts along columns
   int32_t whole;           // kRows, kShort: operands' rows start at multiples of 16 bytes and hold whole chunks; of 8-bit
                            // integers: they start at multiples of so many bytes, 16 (and hold whole chunks of x), 4 or 1
@@ -93,7 +94,7 @@ struct DenseColsum {
 
 // Which kernel a product takes (DenseVariant), over how many workgroups its reduction is split and, of kRows, how many
 // times 16 rows a workgroup has.
-struct DenseChoice { int32_t variant, splits, row_blocks; };
+struct DenseChoice { int32_t variant, splits, row_blocks, row_columns; };
 
 // Of 8-bit integers; `align`: DenseGemm::whole; `copied`: bytes of operands that tiles would have copied first.  Variant -1:
 // too large for a launch.

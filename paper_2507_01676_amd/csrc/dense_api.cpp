@@ -165,17 +165,19 @@ double rows_us(int32_t dtype, int mats, bool whole, int blocks, int64_t ni, int6
   return 3.0 + steps * step * two * load * idle;
 }
 
-// Microseconds of the kernel of few rows of 8-bit integers, measured on 1 to 512 rows by 16 to 8192 columns and 64 to 12800
-// inputs: of each round of workgroups, and of each 1024 of the reduction in it, with 16 or 32 columns a workgroup (which the
-// launch chooses).
-double rows_i8_us(int blocks, int64_t m, int64_t n, int64_t k, int align) {
-  const double down = double((m + 16 * blocks - 1) / (16 * blocks)), wide = double((n + 31) / 32);
-  const bool two = down < kXcds && wide * down >= kCus;
-  const int at = (blocks == 1 ? 0 : blocks == 2 ? 1 : 2) + (two ? 3 : 0);
-  static const double kRound[] = {1.6, 1.8, 2.2, 1.2, 1.6, 2.6}, kStep[] = {0.8, 1.2, 2.05, 1.25, 1.6, 2.3};
-  const double rounds = std::max(1.0, down * (two ? wide : double((n + 15) / 16)) / kCus);
+// Microseconds of the kernel of few rows of 8-bit integers, with 16 times `blocks` rows and `columns` columns a workgroup:
+// measured on 1 to 256 rows by 512 to 14336 columns and 256 to 8192 inputs, whole operands and others.  A round of a workgroup
+// a CU takes so much, and so much for each 1024 of the reduction (a round that some of the CUs have counts whole); and what
+// reading the weights adds.
+double rows_i8_us(int blocks, int columns, int64_t m, int64_t n, int64_t k, int align) {
+  struct Round { double start, step, read; };
+  static const Round kRound[3][2] = {{{1.32, 0.65, 0.03}, {0.63, 1.16, 0.23}}, {{1.57, 1.03, 0.27}, {1.18, 1.54, 0.29}},
+                                     {{1.91, 1.67, 0.0}, {2.12, 2.42, 0.20}}};
+  const Round& r = kRound[blocks == 1 ? 0 : blocks == 2 ? 1 : 2][columns == 1 ? 0 : 1];
+  const int64_t groups = ((m + 16 * blocks - 1) / (16 * blocks)) * ((n + 16 * columns - 1) / (16 * columns));
+  const double rounds = std::ceil(double(groups) / kCus), steps = std::max(0.25, k / 1024.0);
   const double slower = align == 16 ? 1.0 : align == 4 ? 1.2 : blocks == 1 ? 1.5 : 2.0;
-  return 3.0 + rounds * (kRound[at] + kStep[at] * std::max(1.0, k / 1024.0)) * slower;
+  return 3.0 + rounds * (r.start * std::clamp(steps, 0.5, 1.0) + r.step * steps) * slower + r.read * n * k / 5e6;
 }
 
 // The same of the kernel for short reductions: its workgroups (the launch's own arithmetic), each with `rows` chunks of 64
@@ -574,9 +576,13 @@ DenseChoice embx::dense_choose_i8(int64_t m, int64_t n, int64_t k, int align, do
   if (k <= 128) least += 1.5 + 2.0 * m * n / 5.1e6;   // a tile's first loads and its results are all
   for (const int blocks : {1, 2, 4}) {
     if (blocks > 1 && m <= 8 * blocks) break;
-    if (512.0 * ((n + 15) / 16) * ((m + 16 * blocks - 1) / (16 * blocks) + kXcds) > kMostThreads) continue;
-    const double us = rows_i8_us(blocks, m, n, k, align);
-    if (us < few_us) few_us = us, few.row_blocks = blocks;
+    const int64_t down = (m + 16 * blocks - 1) / (16 * blocks);
+    if (512.0 * ((n + 15) / 16) * (down + kXcds) > kMostThreads) continue;
+    for (const int columns : {1, 2}) {
+      if (columns == 2 && down >= kXcds) continue;
+      const double us = rows_i8_us(blocks, columns, m, n, k, align);
+      if (us < few_us) few_us = us, few.row_blocks = blocks, few.row_columns = columns;
+    }
   }
   return few_us < HUGE_VAL && few_us <= least ? few : best;
 }

@@ -97,9 +97,13 @@ Int8Space int8_space(Arena& ar, const emb_linear_int8_t& a) {
   auto words = [](const void* p, int64_t ld) { return !misaligned(p, 4) && ld % 4 == 0; };
   s.align = w && (x || !a.x_scale) ? 16 : words(a.weight, a.ldw) && (!a.x_scale || words(a.x, a.ldx)) ? 4 : 1;
   s.choice = dense_choose_i8(a.m, a.n, a.k, s.align, double(a.k) * ((a.x_scale && !x ? a.m : 0) + (w ? 0 : a.n)));
-  // A few rows that a workgroup's registers hold are quantized by each of the product's workgroups.
+  // A few rows that a workgroup's registers hold are quantized by each of the product's workgroups, as long as that is a round
+  // of them and little beside the weights (one row of 512 x 1664 6.0 us a call, with a launch for it 7.6, of 4096 x 4096 8.2 and
+  // 10.3, four 11.6 and 10.4; of 14336 x 2048 16.0 and 10.9, of 14336 x 8192 30 and 36).
+  const int64_t across = (a.n + 15) / 16;
   s.inside = !a.x_scale && s.choice.variant == kRows && s.choice.row_blocks == 1 && a.m <= 8 &&
-             a.k * (a.m == 1 ? 1 : a.m == 2 ? 2 : a.m <= 4 ? 4 : 8) <= 16384;
+             a.k * (a.m == 1 ? 1 : a.m == 2 ? 2 : a.m <= 4 ? 4 : 8) <= (a.m <= 2 ? 16384 : 8192) &&
+             (across <= 256 || (a.m == 1 && across * 8 <= a.k));
   s.quantized = !a.x_scale && !s.inside;
   const bool rows = s.choice.variant == kRows;   // reads any rows where they lie
   s.packed_x = a.x_scale && !x && !rows;
@@ -309,6 +313,7 @@ emb_status_t emb_linear_int8(const emb_linear_int8_t* a, void* workspace, size_t
   g.ni = static_cast<int32_t>(a->m), g.nj = static_cast<int32_t>(a->n), g.nr = static_cast<int32_t>(a->k);
   g.act = a->activation, g.parts = 1, g.whole = s.align;
   g.variant = s.choice.variant, g.splits = g.slots = s.choice.splits, g.row_blocks = s.choice.row_blocks;
+  g.row_columns = s.choice.row_columns;
   g.partial = s.partial;
   return run(dense_forward_i8(g, stream));
 }
