@@ -171,17 +171,25 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   s.ldh = (a.f + 7) / 8 * 8, s.chosen = a.chosen, s.share = a.share;
   const int64_t used = std::min<int64_t>(uses, a.experts);   // experts, at most
   const int64_t step = a.gate.scale ? 64 : 32;               // of the reduction: a matrix instruction, or two
-  // The up projections: 16 columns of an expert to so many wavefronts, or 4 where there would be few workgroups and few rows
-  // (us a call: one query, one expert of 1024 x 4096 28.4 with 16 columns, 23.3 with 4; two of eight of 2816 x 1024 22.6 and
-  // 26.3).  Four wavefronts share the reduction, and a workgroup has 32 columns, where that leaves workgroups enough (64 rows,
-  // 4 of 32 experts of 5632 x 2048 441 with eight, 432 with four; 19 rows, 3 of 7 of 333 x 1001 35.7 and 40.9) and rows are not
-  // long (16 rows, 4 of 32 of 2048 x 4096 252 and 284; 200 rows, 4 of 64 of 704 x 4096 302 and 320).  Several times
-  // 16 rows of an expert at once where it is expected to have more than 14 (128 rows, 2 of 8 91.6 with 16 at a time, 75.7 with
-  // 64; f32, 64 rows, 2 of 8 of 704 x 1024 48.0 and 44.0; but 200 rows, 4 of 64 of 704 x 4096 555 and 604).
+  // The up projections: four rows of x at most go by columns of four to a wavefront (kMoeFew; us a call: one query, one expert
+  // of 1024 x 4096 23.3, by 16 columns 28.4; two of eight of 2816 x 1024 16.3 and 16.5, of 5632 x 2048 40.8 and 43; four rows
+  // 32.9 and 33.9), unless there are many long rows (one query, 8 of 256 of 1024 x 4096 60.6 and 59.2), or, of f32 and 8-bit
+  // weights, more than a few columns (f32, two of eight of 1408 x 1024 19.7 and 18.2, of 1024 x 1024 15.3 and 16.4; 8 bits
+  // 13.7 and 13.3).  As many wavefronts share the reduction as make about a workgroup a CU (two of eight of 1408 x 1024 12.9
+  // with two, 16.5 with eight; of 512 x 1024 12.1 and 11.2).
+  // Others by 16 columns to four wavefronts, and a workgroup has 32, where that leaves workgroups enough (64 rows, 4 of 32
+  // experts of 5632 x 2048 441 with eight, 432 with four; f32, one, two of eight of 2112 x 1024 26.0 and 23.8; 19 rows, 3 of 7 of
+  // 333 x 1001 35.7 and 40.9) and rows are not long (16 rows, 4 of 32 of 2048 x 4096 252 and 284; 200 rows, 4 of 64 of
+  // 704 x 4096 302 and 320), else to eight.  Several times 16 rows of an expert at once where it is expected to have more than
+  // 14 (128 rows, 2 of 8 91.6 with 16 at a time, 75.7 with 64; f32, 64 rows, 2 of 8 of 704 x 1024 48.0 and 44.0; but 200 rows, 4
+  // of 64 of 704 x 4096 555 and 604).
   const int64_t tiles = (a.f + 15) / 16 * used;
-  s.up_variant = a.m <= 4 && tiles < 256 ? kMoeFew : uses <= 14 * a.experts ? kMoeMore : kMoeMany;
   const int64_t size = a.gate.scale ? 1 : static_cast<int64_t>(esize(a.dtype));   // of a weight
-  s.up_waves = s.up_variant != kMoeFew && tiles >= 352 && a.d * size < 8192 ? 4 : 8;
+  const bool few = size == 2 ? tiles < 352 || a.d * size < 8192 : tiles <= 128;
+  s.up_variant = a.m <= 4 && few ? kMoeFew : uses <= 14 * a.experts ? kMoeMore : kMoeMany;
+  s.up_waves = s.up_variant != kMoeFew && tiles > 256 && a.d * size < 8192 ? 4 : 8;
+  if (s.up_variant == kMoeFew && size == 2)
+    while (s.up_waves > 1 && (a.f * s.up_waves + 31) / 32 * used > 256) s.up_waves /= 2;
   const int64_t up_step = s.up_variant == kMoeFew ? step * 4 : step * 2;
   // fewer where d has no step for each, unless that leaves few workgroups (f32, 115 rows, 4 of 4 of 64 x 256, 8-bit weights
   // 30.3 with two, 18.4 with eight; 69 rows, 4 of 35 of 64 x 832 51.6 with one, 30.0 with eight; but 3 rows, 2 of 8 of
