@@ -50,7 +50,7 @@ struct Moe {
 enum MoeVariant { kMoeFew = 0, kMoeMore = 1, kMoeMany = 2 };
 
 // Logits of all rows that every workgroup of the up projections works out, or of which it picks the experts, by itself
-constexpr int kFused = 32, kPicked = 256;
+constexpr int kFused = 16, kPicked = 256;
 
 constexpr int kMostExperts = 1024, kMostTopK = 32;
 constexpr int kUses = 512;       // uses, row * top_k + place, that a workgroup looks at at a time

@@ -198,8 +198,9 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   while (s.up_waves > 1 && s.up_waves * up_step > a.d && (tiles >= 256 || s.up_variant == kMoeFew)) s.up_waves /= 2;
   const int64_t up_groups = (a.f * s.up_waves + 127) / 128 * used;
   s.up_parts = static_cast<int32_t>(std::max<int64_t>(1, std::min(256 / up_groups, (uses + used * 32 - 1) / (used * 32))));
-  // (one query, eight experts: 18.4 with the routing in every workgroup, 20.5 with a launch for it; five queries 41 and 35)
-  s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kFused && a.m * a.experts * a.d <= 65536 && a.m * tiles <= 1024;
+  // The routing in every workgroup, without a launch (two of eight of 2816 x 1024: one query 16.3, with one 18.9; two 24.2 and
+  // 25.9; but three 28.6 and 27.8).
+  s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kFused && a.m * a.experts * a.d <= 65536;
   // Logits in workgroups of their own where one would read the rows of many experts (one query, 8 of 256 of 1024 x 4096 125 us,
   // so 61; 4 of 64 of 704 x 2048 29 and 23.7; 22 rows, 2 of 20 of 1792 x 1088 62.6 and 62.0; but 8 rows, 4 of 16 of 704 x 256 23.0
   // and 24.5), and what is left of the routing in every workgroup of the up projections up to kPicked (those of 256 63 us with
