@@ -9,7 +9,7 @@
 // What bounds it is reading the weights of the experts that are used, once: 64 rows of bf16, 4 of 32 experts of 5632 x 2048, 432
 // us a call, 2.2 GB at 5.1 TB/s (the up projections 272 us, 5.4 TB/s; down 145).  With few rows a launch is not long enough to
 // get there (about 5 us each, of which the loads' and the routing's latency is most): one query, two of eight of 2816 x 1024,
-// 16.6 us, 35 MB; five with 8-bit weights 31.3.
+// 16.2 us, 35 MB; five with 8-bit weights 31.3.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
