@@ -861,12 +861,17 @@ int down_each(const Moe& a, hipStream_t s) {
 
 template <int TYPE, bool EIGHT, bool WHOLE>
 int launch(const Moe& a, hipStream_t s) {
-  constexpr int kMany = EIGHT || TYPE == kDenseF32 ? 2 : 4;   // (as many as there are registers for)
   int rc;
   switch (a.up_variant) {
     case kMoeFew: rc = up<TYPE, EIGHT, WHOLE, 4, 1>(a, s); break;
     case kMoeMore: rc = up<TYPE, EIGHT, WHOLE, 1, 1>(a, s); break;
-    default: rc = up<TYPE, EIGHT, WHOLE, 1, kMany>(a, s); break;
+    default:
+      if (a.up_blocks == 2) {
+        rc = up<TYPE, EIGHT, WHOLE, 1, 2>(a, s);
+        break;
+      }
+      if constexpr (!EIGHT && TYPE != kDenseF32) rc = up<TYPE, EIGHT, WHOLE, 1, 4>(a, s);   // (the others have no registers for it)
+      else rc = hipErrorInvalidValue;
   }
   if (rc != 0) return rc;
   if constexpr (!EIGHT)

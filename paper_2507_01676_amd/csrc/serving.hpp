@@ -33,6 +33,7 @@ struct Moe {
   float* partial;          // [splits][m][d], with splits > 1; kMoeMany: [m][top_k][d]
   int32_t m, f, d, experts, top_k, act, renormalize;
   int32_t up_variant, down_variant;   // MoeVariant
+  int32_t up_blocks;       // kMoeMany: 16s of rows at a time, 2 or, of weights of 16 bits, 4
   int32_t up_waves;        // wavefronts that share a reduction of the up projections: 1, 2, 4 or 8
   int32_t down_waves;      // of the down projection.  kMoeFew: wavefronts of a workgroup, 8 or 16; kMoeMany: that share a reduction
   double* logits;          // [m][experts], which a launch of its own works out, or NULL

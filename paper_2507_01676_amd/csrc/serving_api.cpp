@@ -162,7 +162,8 @@ struct MoeSpace {
   float* share;
   float* partial;
   double* logits;
-  int32_t up_variant, down_variant, down_parts, down_blocks, up_waves, down_waves, fused, up_parts, down_rows, splits, chunk;
+  int32_t up_variant, up_waves, up_blocks, up_parts, fused;
+  int32_t down_variant, down_waves, down_blocks, down_parts, down_rows, splits, chunk;
 };
 
 MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
@@ -182,12 +183,14 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   // 333 x 1001 35.7 and 40.9) and rows are not long (16 rows, 4 of 32 of 2048 x 4096 252 and 284; 200 rows, 4 of 64 of
   // 704 x 4096 302 and 320), else to eight.  Several times 16 rows of an expert at once where it is expected to have more than
   // 14 (128 rows, 2 of 8 91.6 with 16 at a time, 75.7 with 64; f32, 64 rows, 2 of 8 of 704 x 1024 48.0 and 44.0; but 200 rows, 4
-  // of 64 of 704 x 4096 555 and 604).
+  // of 64 of 704 x 4096 555 and 604), and 64 instead of 32 where it is more than 26 (128 rows, 2 of 8 of 2816 x 1024 72 and 80;
+  // but 128 rows, 4 of 32 of 1408 x 2048 178 and 163).
   const int64_t tiles = (a.f + 15) / 16 * used;
   const int64_t size = a.gate.scale ? 1 : static_cast<int64_t>(esize(a.dtype));   // of a weight
   const bool few = size == 2 ? tiles < 352 || a.d * size < 8192 : tiles <= 128;
   s.up_variant = a.m <= 4 && few ? kMoeFew : uses <= 14 * a.experts ? kMoeMore : kMoeMany;
   s.up_waves = s.up_variant != kMoeFew && tiles > 256 && a.d * size < 8192 ? 4 : 8;
+  s.up_blocks = size == 2 && uses > 26 * a.experts ? 4 : 2;
   if (s.up_variant == kMoeFew && size == 2)
     while (s.up_waves > 1 && (a.f * s.up_waves + 31) / 32 * used > 256) s.up_waves /= 2;
   const int64_t up_step = s.up_variant == kMoeFew ? step * 4 : step * 2;
@@ -359,7 +362,7 @@ emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes
     ++i;
   }
   g.h = s.h, g.ldh = s.ldh, g.chosen = s.chosen, g.share = s.share;
-  g.up_variant = s.up_variant, g.down_variant = s.down_variant, g.up_waves = s.up_waves;
+  g.up_variant = s.up_variant, g.up_blocks = s.up_blocks, g.down_variant = s.down_variant, g.up_waves = s.up_waves;
   g.down_waves = s.down_waves, g.fused = s.fused, g.logits = s.logits;
   g.down_parts = s.down_parts, g.down_blocks = s.down_blocks;
   g.up_parts = s.up_parts, g.down_rows = s.down_rows;
