@@ -259,7 +259,7 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
     s.partial = ar.take<float>(uses * a.d * 4);
   }
   if (s.splits > 1) s.partial = ar.take<float>(s.splits * a.m * a.d * 4);
-  s.h = ar.take<void>(2 * uses * s.ldh * esize(a.dtype));
+  s.h = ar.take<void>(uses * s.ldh * 4);   // (in f32, or as two values of 16 bits)
   if (!s.chosen) s.chosen = ar.take<int32_t>(uses * 4);
   if (!s.share) s.share = ar.take<float>(uses * 4);
   return s;
