@@ -26,10 +26,10 @@
  * moe: logits are summed in 64 bits, so which experts a row takes does not depend on the order
  * of the sums; NaN counts as the largest logit, and makes the row's shares and results NaN,
  * as does an infinite one that is the largest.  Sums are held in f32, and so are shares.
- * act(..) * (..) goes into the product with Wd in f32 or, with 16-bit types, as two values of
- * the type, the rounded one and the rest (in f16 an infinity beyond 65504); the result is
- * rounded once.  The experts' matrices have the call's type, or
- * are 8-bit integers with a scale for each of their rows (all three or none).  A row's result
+ * act(..) * (..) is f32 with every type, and goes into the product with Wd as it is, but for
+ * 2^-23 of it, or 2^-36 of the largest of its row, where Wd is f16; the result is rounded once.
+ * (An infinite element of Wd gives an infinity or NaN.)  The experts' matrices have the call's
+ * type, or are 8-bit integers with a scale for each of their rows (all three or none).  A row's result
  * comes from that row and its experts only; in which order its sums are added up, and so
  * their last bits in f32, is up to the whole call.  It is made for few rows, where the layer
  * is bound by reading the experts' matrices; any number is right.

@@ -148,6 +148,18 @@ __device__ inline void act8(float* z, int act) {
   }
 }
 
+// act of one f32 value
+__device__ inline float act_f(float z, int act) {
+  float bell;
+  switch (act) {
+    case EMB_ACT_RELU: return __builtin_elementwise_maximum(z, 0.0f);   // NaN passes
+    case EMB_ACT_SIGMOID: return sigmoid_f<kDenseF32, true>(z);
+    case EMB_ACT_SILU: return z * sigmoid_f<kDenseF32, true>(z);
+    case EMB_ACT_GELU: return z * phi_f<kDenseF32>(z, &bell);
+    default: return z;
+  }
+}
+
 // Eight consecutive elements at p, of which n >= 1 are inside (the last one stands for the others); whole eights are read
 // and written 16 bytes at a time at any alignment.
 template <int TYPE>

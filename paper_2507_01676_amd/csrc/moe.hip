@@ -162,6 +162,46 @@ struct Weights<TYPE, true> : Chunk<1, 4> {
   }
 };
 
+// The largest magnitude of eight values and `most`; NaN is passed over.
+__device__ inline float largest(const Chunk<4, 8>& x, float most) {
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(most) : "v"(x.v[e / 4][e % 4]), "v"(x.v[e / 4][e % 4 + 1]));
+  return most;
+}
+
+// f32 values are three bf16 ones that add up to them, 8 of their 24 bits each: this takes the first one off.  (FIRST: an
+// infinity's rest is that of the largest number, so that its product is no NaN.)
+template <bool FIRST>
+__device__ inline Piece<kDenseBF16> third(Piece<kDenseF32>* x) {
+  Piece<kDenseBF16> out;
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    float v[2] = {x->get(e), x->get(e + 1)};
+    out.v[0][e / 2] = __builtin_amdgcn_perm(__float_as_uint(v[1]), __float_as_uint(v[0]), 0x07060302);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if constexpr (FIRST) v[i] = __builtin_amdgcn_fmed3f(v[i], -0x1.fffffep127f, 0x1.fffffep127f);
+      v[i] -= __uint_as_float(__float_as_uint(v[i]) & 0xffff0000u);
+      x->v[e / 4][e % 4 + i] = __float_as_uint(v[i]);
+    }
+  }
+  return out;
+}
+
+// f32 values times a power of two as two f16 ones, the rounded and the rest.  (An infinity's is a number.)
+__device__ inline void two_halves(const Piece<kDenseF32>& x, float scale, Piece<kDenseF16>* rounded, Piece<kDenseF16>* left) {
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+  for (int e = 0; e < 8; e += 2) {
+    const float v[2] = {x.get(e) * scale, x.get(e + 1) * scale};
+    const f16x2 near = {static_cast<_Float16>(v[0]), static_cast<_Float16>(v[1])};
+    const f16x2 rest = {static_cast<_Float16>(fmaf(static_cast<float>(near[0]), -1.0f, v[0])),
+                        static_cast<_Float16>(fmaf(static_cast<float>(near[1]), -1.0f, v[1]))};
+    rounded->v[0][e / 2] = __builtin_bit_cast(uint32_t, near);
+    left->v[0][e / 2] = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(rest, f16x2{65504.0f, 65504.0f}));
+  }
+}
+
 template <int TYPE>
 __device__ inline f32x4 product(const Piece<TYPE>& w, const Piece<TYPE>& x, f32x4 c) {
   if constexpr (TYPE == kDenseF32) {
@@ -305,20 +345,47 @@ __global__ __launch_bounds__(512) void moe_route(Moe a) {
 
 constexpr int kWaves = 8;
 
-// What a wavefront multiplies at a time: of R * 16 / S rows of weights by FR * 16 / S rows of x (in PARTS parts, added up),
-// kAll of the reduction.  It is loaded while the one before it is multiplied.
-template <int TYPE, bool EIGHT, bool WHOLE, bool WHOLE_X, int S, int R, int FR, int PARTS>
+// What a wavefront multiplies at a time: of R * 16 / S rows of weights by FR * 16 / S rows of x, or (HANDED) of what moe_up
+// handed on, kAll of the reduction.  It is loaded while the one before it is multiplied.
+//
+// What is handed on is f32, and multiplied as it is.  Weights of bf16 or 8 bits multiply it as three bf16 values, which have its
+// range and all of its bits.  Those of f16 multiply two f16 values of it times a power of two, which a lane keeps for its row's
+// sums: the largest of the row so far is below 2^16 with it.  A larger one makes it smaller, and the sums with it.  So it has 23
+// bits, or 2^-36 of the row's largest, whatever its range.
+template <int TYPE, bool EIGHT, bool WHOLE, bool WHOLE_X, int S, int R, int FR, bool HANDED>
 struct Step {
-  using Ws = Weights<TYPE, EIGHT>;
-  using X = Piece<TYPE>;
-  static constexpr int kSizeX = TYPE == kDenseF32 ? 4 : 2;
+  static constexpr bool kThirds = HANDED && (TYPE == kDenseBF16 || (TYPE == kDenseF16 && EIGHT));
+  static constexpr bool kScaled = HANDED && TYPE == kDenseF16 && !EIGHT;
+  static constexpr int kType = kThirds ? kDenseBF16 : TYPE;   // of the products
+  using Ws = Weights<kType, EIGHT>;
+  static constexpr int kSizeX = HANDED || TYPE == kDenseF32 ? 4 : 2;
+  using X = Piece<kSizeX == 4 ? kDenseF32 : TYPE>;
   static constexpr int kSpan = 4 * Ws::kPer, kStep = kSpan * S;
-  static constexpr int kGo = S == 1 && TYPE != kDenseF32 && FR * PARTS < 4 ? 2 : 1;   // 128 bytes of a row
+  static constexpr int kGo = S == 1 && TYPE != kDenseF32 && FR * (HANDED ? 2 : 1) < 4 ? 2 : 1;   // 128 bytes of a row, or 64
   static constexpr int kAll = kStep * kGo;
+  static_assert(!HANDED || WHOLE_X);
   Loaded<Ws::kSize, Ws::kWords, WHOLE> w[kGo][R];
-  Loaded<kSizeX, TYPE == kDenseF32 ? 8 : 4, WHOLE_X> x[kGo][FR][PARTS][Ws::kPieces];
+  Loaded<kSizeX, kSizeX * 2, WHOLE_X> x[kGo][FR][Ws::kPieces];
   // a lane's first element of a step
   __device__ static int own(int lane) { return (lane & (S - 1)) * kSpan + (lane >> 4) * Ws::kPer; }
+
+  // the power of two that a lane's sums are times, by its exponent
+  struct Power {
+    int at[kScaled ? FR : 1];
+    __device__ Power() { reset(); }
+    __device__ void reset() {
+#pragma unroll
+      for (int f = 0; f < (kScaled ? FR : 1); ++f) at[f] = 126;
+    }
+    __device__ f32x4 undo(f32x4 sums, int f) const {
+      if constexpr (kScaled) {
+        const float back = __uint_as_float(static_cast<uint32_t>(127 - at[f]) << 23);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sums[e] *= back;
+      }
+      return sums;
+    }
+  };
 
   // A whole step of weights from r0 on: `base` the first row of 16 / S, `row` bytes to the lane's own row and element.
   __device__ void load_w(const char* const (&base)[R], const uint32_t (&row)[R], int r0) {
@@ -329,36 +396,36 @@ struct Step {
   }
 
   // and of x's rows: p, at the lane's own element
-  __device__ void load_x(const char* const (&p)[FR], int64_t part, int r0) {
+  __device__ void load_x(const char* const (&p)[FR], int r0) {
 #pragma unroll
     for (int g = 0; g < kGo; ++g)
 #pragma unroll
       for (int f = 0; f < FR; ++f)
 #pragma unroll
-        for (int n = 0; n < PARTS; ++n)
-#pragma unroll
-          for (int i = 0; i < Ws::kPieces; ++i)
-            x[g][f][n][i].load_at(p[f] + n * part + int64_t(r0 + g * kStep + 8 * i) * kSizeX);
+        for (int i = 0; i < Ws::kPieces; ++i) x[g][f][i].load_at(p[f] + int64_t(r0 + g * kStep + 8 * i) * kSizeX);
   }
 
   // with the pointers that it was loaded from, as far as they lie behind words' starts
-  __device__ void multiply(const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], f32x4 (&acc)[R][FR]) const {
+  __device__ void multiply(const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], f32x4 (&acc)[R][FR],
+                           Power& power) const {
+    fit<kGo>(acc, power);
 #pragma unroll
-    for (int g = 0; g < kGo; ++g) products<false>(g, base, row, p, 0, acc);
+    for (int g = 0; g < kGo; ++g) products<false>(g, base, row, p, 0, acc, power);
   }
 
   // The last step, of which only what is below `end` is there; not loaded ahead.
-  __device__ void rest(const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], int64_t part, int r0,
-                       int end, int lane, f32x4 (&acc)[R][FR]) {
+  __device__ void rest(const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], int r0, int end, int lane,
+                       f32x4 (&acc)[R][FR], Power& power) {
     auto load = [&](int g, int at) {
 #pragma unroll
       for (int r = 0; r < R; ++r) w[g][r].load_end(base[r] + row[r] - own(lane) * Ws::kSize, at, end);
 #pragma unroll
       for (int f = 0; f < FR; ++f)
 #pragma unroll
-        for (int n = 0; n < PARTS; ++n)
-#pragma unroll
-          for (int i = 0; i < Ws::kPieces; ++i) x[g][f][n][i].load_end(p[f] + n * part - own(lane) * kSizeX, at + 8 * i, end);
+        for (int i = 0; i < Ws::kPieces; ++i) {
+          x[g][f][i].load_end(p[f] - own(lane) * kSizeX, at + 8 * i, end);
+          if constexpr (WHOLE_X) x[g][f][i].keep(end - at - 8 * i);
+        }
     };
     if constexpr (WHOLE) {   // (one at a time, in place: fewer registers)
       for (; r0 < end; r0 += kStep) {
@@ -366,46 +433,87 @@ struct Step {
         load(0, r0 + own(lane));
 #pragma unroll
         for (int r = 0; r < R; ++r) w[0][r].keep(left);
-#pragma unroll
-        for (int f = 0; f < FR; ++f)
-#pragma unroll
-          for (int n = 0; n < PARTS; ++n)
-#pragma unroll
-            for (int i = 0; i < Ws::kPieces; ++i) x[0][f][n][i].keep(left - 8 * i);
-        products<false>(0, base, row, p, 0, acc);
+        fit<1>(acc, power);
+        products<false>(0, base, row, p, 0, acc, power);
       }
     } else {
 #pragma unroll
       for (int g = 0; g < kGo; ++g) load(g, r0 + g * kStep + own(lane));
+      fit<kGo>(acc, power);
 #pragma unroll
-      for (int g = 0; g < kGo; ++g) products<true>(g, base, row, p, end - r0 - g * kStep - own(lane), acc);
+      for (int g = 0; g < kGo; ++g) products<true>(g, base, row, p, end - r0 - g * kStep - own(lane), acc, power);
+    }
+  }
+
+  // Brings sums and their power down to what the step's first GO are about to take.
+  template <int GO>
+  __device__ void fit(f32x4 (&acc)[R][FR], Power& power) const {
+    if constexpr (kScaled) {
+#pragma unroll
+      for (int f = 0; f < FR; ++f) {
+        float most = 0.0f;
+#pragma unroll
+        for (int g = 0; g < GO; ++g)
+#pragma unroll
+          for (int i = 0; i < Ws::kPieces; ++i) most = largest(x[g][f][i], most);
+        if (!__any(__builtin_amdgcn_ldexpf(most, power.at[f]) > 61440.0f)) continue;   // (what rounds to a number of f16)
+        // the four lanes that hold a row's step
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        // to 2^12 and more, so that the next ones hardly ever bring it down again
+        const int to = min(power.at[f], 12 + 127 - static_cast<int>(min(__float_as_uint(most) >> 23, 254u)));
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[r][f][e] = __builtin_amdgcn_ldexpf(acc[r][f][e], to - power.at[f]);
+        power.at[f] = to;
+      }
     }
   }
 
   // END: only `left` of the reduction from the lane's first element on are there
   template <bool END>
   __device__ void products(int g, const char* const (&base)[R], const uint32_t (&row)[R], const char* const (&p)[FR], int left,
-                           f32x4 (&acc)[R][FR]) const {
+                           f32x4 (&acc)[R][FR], const Power& power) const {
 #pragma unroll
     for (int i = 0; i < Ws::kPieces; ++i) {
-      X xs[FR][PARTS];
+      X xs[FR];
 #pragma unroll
-      for (int f = 0; f < FR; ++f)
-#pragma unroll
-        for (int n = 0; n < PARTS; ++n) {
-          static_cast<Chunk<kSizeX, TYPE == kDenseF32 ? 8 : 4>&>(xs[f][n]) = x[g][f][n][i].shifted(x[g][f][n][i].shift_of(p[f]));
-          if constexpr (END) xs[f][n].keep(left - 8 * i);
-        }
+      for (int f = 0; f < FR; ++f) {
+        static_cast<Chunk<kSizeX, kSizeX * 2>&>(xs[f]) = x[g][f][i].shifted(x[g][f][i].shift_of(p[f]));
+        if constexpr (END && !WHOLE_X) xs[f].keep(left - 8 * i);
+      }
+      Piece<kType> ws[R];
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         Ws all;
         static_cast<Chunk<Ws::kSize, Ws::kWords>&>(all) = w[g][r].shifted(w[g][r].shift_of(base[r] + row[r]));   // (steps are whole words)
         if constexpr (END) all.keep(left);
-        const X one = all.piece(i);
+        ws[r] = all.piece(i);
+      }
+      auto add = [&](const Piece<kType>(&part)[FR]) {
 #pragma unroll
-        for (int n = PARTS - 1; n >= 0; --n)
+        for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int f = 0; f < FR; ++f) acc[r][f] = product<TYPE>(one, xs[f][n], acc[r][f]);
+          for (int f = 0; f < FR; ++f) acc[r][f] = product<kType>(ws[r], part[f], acc[r][f]);
+      };
+      if constexpr (kThirds) {
+        Piece<kType> part[FR];
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {   // (one after another: fewer registers)
+#pragma unroll
+          for (int f = 0; f < FR; ++f) part[f] = n == 0 ? third<true>(&xs[f]) : third<false>(&xs[f]);
+          add(part);
+          if constexpr (S == 1) __builtin_amdgcn_sched_barrier(0);
+        }
+      } else if constexpr (kScaled) {
+        Piece<kType> rounded[FR], rest[FR];
+#pragma unroll
+        for (int f = 0; f < FR; ++f) two_halves(xs[f], __builtin_amdgcn_ldexpf(1.0f, power.at[f]), &rounded[f], &rest[f]);
+        add(rest);
+        add(rounded);
+      } else {
+        add(xs);
       }
     }
   }
@@ -434,7 +542,8 @@ constexpr int kListed = kUses + 192;
 struct Uses {
   int id[kUses / 64];   // the experts of a lane's uses
 
-  __device__ void read(const int32_t* chosen, int count, int lane) {
+  template <class T>
+  __device__ void read(const T* chosen, int count, int lane) {
 #pragma unroll
     for (int n = 0; n < kUses / 64; ++n) {
       id[n] = -1;
@@ -464,8 +573,8 @@ struct Uses {
 };
 
 // act(x Wg^T) * (x Wu^T) of an expert's uses: 16 / S columns of each of which some wavefronts share the reduction.  The
-// result is stored as two values of the type, the rounded one and the rest, so that the product with Wd has it in nearly 32
-// bits: one part alone would make results 1.4 times as far from exact ones as their own rounding makes them.
+// result is handed on in f32: rounded to a type of 16 bits it would make results 1.4 times as far from exact ones as their own
+// rounding makes them, and f16 has neither its range nor, below 2^-14, its bits.
 // ROUTE: every workgroup routes by itself (kFused, kPicked logits at most), and the first one stores it, instead of a launch
 // before this one.
 // Every wavefront loads the next 128 bytes of its rows of both matrices, or 256 where 4 rows are all, while it multiplies those
@@ -473,7 +582,6 @@ struct Uses {
 // 5632 x 2048 from 433 us to 517.
 template <int TYPE, bool EIGHT, bool WHOLE, int S, int FR, bool ROUTE>
 __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_up(Moe a) {
-  using T = typename Elem<TYPE>::T;
   constexpr int kRows = 16 / S, kTokens = 16 / S * FR;
   __shared__ uint16_t lists[kWaves][kListed];
   __shared__ float sums[kWaves][2][kTokens][kRows + 1];
@@ -495,7 +603,7 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
     for (int at = 0; at < use; at += 64)
       if (__any(at + lane < use && chosen[min(at + lane, use)] == expert)) return;
   }
-  using P = Step<TYPE, EIGHT, WHOLE, WHOLE, S, 2, FR, 1>;
+  using P = Step<TYPE, EIGHT, WHOLE, WHOLE, S, 2, FR, false>;
   // (16 rows of at most 2^25 elements of a row's stride: 32 bits)
   const int row0 = min(j0, a.f - 1), lane_row = min(j0 + c / S, a.f - 1) - row0;
   const char* base[2];
@@ -527,20 +635,21 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
         x[f] = static_cast<const char*>(a.x) +
                ((first + lists[wave][min(at + f * kRows + c / S, have - 1)]) / a.top_k * a.ldx + P::own(lane)) * P::kSizeX;
       f32x4 acc[2][FR] = {};
+      typename P::Power power;
       int r0 = begin;
       if (begin + P::kAll <= a.d) {
         if (at != static_cast<int>(blockIdx.z) * kTokens) one.load_w(base, row, begin);
-        one.load_x(x, 0, begin);
+        one.load_x(x, begin);
         auto go = [&](const P& now, P& next) {   // whether there is a next one
           r0 += every;
           const bool more = r0 + P::kAll <= a.d;
-          if (more) next.load_w(base, row, r0), next.load_x(x, 0, r0);
-          now.multiply(base, row, x, acc);
+          if (more) next.load_w(base, row, r0), next.load_x(x, r0);
+          now.multiply(base, row, x, acc, power);
           return more;
         };
         while (go(one, two) && go(two, one)) {}
       }
-      if (r0 < a.d) one.rest(base, row, x, 0, r0, a.d, lane, acc);
+      if (r0 < a.d) one.rest(base, row, x, r0, a.d, lane, acc, power);
 #pragma unroll
       for (int f = 0; f < FR; ++f)
 #pragma unroll
@@ -558,24 +667,19 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
         const int r = t / (kRows * groups), group = t / kRows % groups, column = t % kRows;
         const int j = (blockIdx.x * groups + group) * kRows + column;
         if (at + r >= have || j >= a.f) continue;
-        float g[8] = {}, v = 0.0f;
+        float g = 0.0f, v = 0.0f;
 #pragma unroll
         for (int n = 0; n < kWaves; ++n) {
           const int from = group * sharing + min(n, sharing - 1);
-          g[0] += n < sharing ? sums[from][0][r][column] : 0.0f, v += n < sharing ? sums[from][1][r][column] : 0.0f;
+          g += n < sharing ? sums[from][0][r][column] : 0.0f, v += n < sharing ? sums[from][1][r][column] : 0.0f;
         }
         if constexpr (EIGHT) {
-          g[0] *= a.scale[0][int64_t(expert) * a.f + j];
+          g *= a.scale[0][int64_t(expert) * a.f + j];
           v *= a.scale[1][int64_t(expert) * a.f + j];
         }
-        act8<TYPE>(g, a.act);
-        v *= g[0];
-        T* const h = static_cast<T*>(a.h) + (first + lists[wave][at + r]) * a.ldh + j;
-        *h = T(v);
-        if constexpr (TYPE != kDenseF32) {
-          const float rest = v - float(T(v));
-          h[uses * a.ldh] = T(fabsf(rest) < __builtin_inff() ? rest : 0.0f);   // (of an infinity there is none)
-        }
+        v *= act_f(g, a.act);
+        // (a NaN whose upper half says so)
+        a.h[(first + lists[wave][at + r]) * a.ldh + j] = v == v ? v : __uint_as_float(0x7fc00000u);
       }
       __syncthreads();
     }
@@ -589,24 +693,21 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_u
 template <int TYPE, bool EIGHT, bool WHOLE, int S, int FI, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT, WHOLE>(TYPE == kDenseF32 ? 1 : 2))) void moe_down(Moe a) {
   using T = typename Elem<TYPE>::T;
-  constexpr int kParts = TYPE == kDenseF32 ? 1 : 2;
   constexpr int FR = 1, kRows = 16 / S, kCols = kRows * FI, kTokens = kRows * FR;
-  __shared__ uint16_t lists[WAVES][2][kDownRows], used[kUses];   // (a row uses an expert once)
+  __shared__ uint16_t lists[WAVES][2][kDownRows], used[kUses], ids[kUses];   // (a row uses an expert once)
   __shared__ uint32_t mask[kMostExperts / 32];
   __shared__ float sums[WAVES][kDownRows][kCols];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), q = lane >> 4, c = lane & 15;
   const int j0 = blockIdx.x * kCols;
   const int first_row = blockIdx.y * a.down_rows, rows = min(a.down_rows, a.m - first_row), count = rows * a.top_k;
-  const int64_t first = int64_t(first_row) * a.top_k, part = int64_t(a.m) * a.top_k * a.ldh * sizeof(T);
-  Uses u;
-  u.read(a.chosen + first, count, lane);
+  const int64_t first = int64_t(first_row) * a.top_k;
+  int32_t id = -1;   // (wavefronts from kUses / 64 on have none)
+  if (tid < count) ids[tid] = static_cast<uint16_t>(id = a.chosen[first + tid]);
   if (tid < kMostExperts / 32) mask[tid] = 0;
   for (int at = lane; at < rows * kCols; at += 64) sums[wave][at / kCols][at % kCols] = 0.0f;
   __syncthreads();
   // the experts that are used, in order
-#pragma unroll
-  for (int n = 0; n < kUses / 64; ++n)
-    if (n == wave && u.id[n] >= 0) atomicOr(&mask[u.id[n] >> 5], 1u << (u.id[n] & 31));
+  if (id >= 0) atomicOr(&mask[id >> 5], 1u << (id & 31));
   __syncthreads();
   for (int e = tid; e < a.experts; e += 64 * WAVES) {
     if (!(mask[e >> 5] >> (e & 31) & 1)) continue;
@@ -618,7 +719,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   for (int n = 0; n < (a.experts + 31) / 32; ++n) total += __popc(mask[n]);
   __syncthreads();
   const int chunks = (a.f + a.chunk - 1) / a.chunk;
-  using P = Step<TYPE, EIGHT, WHOLE, true, S, FI, FR, kParts>;   // (rows of h start at multiples of 16 bytes)
+  using P = Step<TYPE, EIGHT, WHOLE, true, S, FI, FR, true>;   // (rows of h start at multiples of 16 bytes)
   // Where a wavefront is: an item, its expert's uses from `at` on, and r0 of its reduction.
   struct Place {
     int item, expert, to, have, at, r0, which;
@@ -630,6 +731,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   auto begin_item = [&](Place& p) {
     p.expert = __builtin_amdgcn_readfirstlane(used[p.item / chunks]);
     p.which ^= 1;
+    Uses u;   // (held, its registers would be those of the loads)
+    u.read(ids, count, lane);
     p.have = u.list(p.expert, lists[wave][p.which], 0, 0, count, lane);
 #pragma unroll
     for (int i = 0; i < FI; ++i) {
@@ -645,13 +748,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
       p.use[f] = lists[wave][p.which][min(p.at + f * kRows + c / S, p.have - 1)];
-      p.h[f] = static_cast<const char*>(a.h) + ((first + p.use[f]) * a.ldh + P::own(lane)) * P::kSizeX;
+      p.h[f] = reinterpret_cast<const char*>(a.h + (first + p.use[f]) * a.ldh + P::own(lane));
     }
   };
   auto load = [&](P& s, const Place& p) {
-    if (p.r0 + P::kAll <= p.to) s.load_w(p.w, p.row, p.r0), s.load_x(p.h, part, p.r0);
+    if (p.r0 + P::kAll <= p.to) s.load_w(p.w, p.row, p.r0), s.load_x(p.h, p.r0);
   };
   f32x4 acc[FI][FR] = {};
+  typename P::Power power;
   auto finish = [&](const Place& p) {
 #pragma unroll
     for (int f = 0; f < FR; ++f) {
@@ -660,6 +764,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
       float* const mine = sums[wave][p.use[f] / a.top_k];
 #pragma unroll
       for (int i = 0; i < FI; ++i) {
+        const f32x4 whole = power.undo(acc[i][f], f);
         auto add = [&](int j, float s) {
           s *= share;
           if constexpr (EIGHT) s *= a.scale[2][int64_t(p.expert) * a.d + min(j0 + j, a.d - 1)];
@@ -667,14 +772,15 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
         };
         if constexpr (S == 1) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) add(i * 16 + 4 * q + e, acc[i][f][e]);
+          for (int e = 0; e < 4; ++e) add(i * 16 + 4 * q + e, whole[e]);
         } else {
-          const float s = segments(acc[i][f], lane);
+          const float s = segments(whole, lane);
           if ((c & 3) == 0) add(i * 4 + q, s);
         }
         acc[i][f] = f32x4{};
       }
     }
+    power.reset();
   };
   const int items = total * chunks;
   P one, two;
@@ -695,10 +801,16 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
       }
       if (more) begin_rows(then);
     }
-    if (more) load(other, then);
-    if (left > now.r0) s.multiply(now.w, now.row, now.h, acc);
+    if (more && then.r0 + P::kAll <= then.to && left > now.r0) {   // (a block of its own waits for what it multiplies, and no more)
+      other.load_w(then.w, then.row, then.r0), other.load_x(then.h, then.r0);
+      s.multiply(now.w, now.row, now.h, acc, power);
+      asm volatile("");
+    } else {
+      if (more) load(other, then);
+      if (left > now.r0) s.multiply(now.w, now.row, now.h, acc, power);
+    }
     if (last) {
-      if (left < now.to) s.rest(now.w, now.row, now.h, part, left, now.to, lane, acc);
+      if (left < now.to) s.rest(now.w, now.row, now.h, left, now.to, lane, acc, power);
       finish(now);
     }
     now = then;
@@ -725,15 +837,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
 // memory in f32, a row for each use, without their shares.
 template <int TYPE, bool WHOLE, int FR>
 __global__ __launch_bounds__(512, (waves_of<TYPE, false, WHOLE>(TYPE == kDenseF32 ? FR : 2 * FR))) void moe_down_each(Moe a) {
-  using T = typename Elem<TYPE>::T;
-  constexpr int kParts = TYPE == kDenseF32 ? 1 : 2, kTokens = 16 * FR, kCols = 32;
+  constexpr int kTokens = 16 * FR, kCols = 32;
   __shared__ uint16_t lists[kWaves][kListed];
   __shared__ float sums[kWaves][kTokens][kCols + 1];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4, c = lane & 15;
   const int sharing = a.down_waves, groups = kWaves / sharing, expert = blockIdx.y;
   const int j0 = (blockIdx.x * groups + wave / sharing) * kCols;
-  const int64_t uses = int64_t(a.m) * a.top_k, part = uses * a.ldh * sizeof(T);
-  using P = Step<TYPE, false, WHOLE, true, 1, 2, FR, kParts>;
+  const int64_t uses = int64_t(a.m) * a.top_k;
+  using P = Step<TYPE, false, WHOLE, true, 1, 2, FR, true>;
   const char* base[2];
   uint32_t row[2];
 #pragma unroll
@@ -761,28 +872,31 @@ __global__ __launch_bounds__(512, (waves_of<TYPE, false, WHOLE>(TYPE == kDenseF3
       const char* h[FR];
 #pragma unroll
       for (int f = 0; f < FR; ++f)
-        h[f] = static_cast<const char*>(a.h) + ((first + lists[wave][min(at + f * 16 + c, have - 1)]) * a.ldh + P::own(lane)) * P::kSizeX;
+        h[f] = reinterpret_cast<const char*>(a.h + (first + lists[wave][min(at + f * 16 + c, have - 1)]) * a.ldh + P::own(lane));
       f32x4 acc[2][FR] = {};
+      typename P::Power power;
       int r0 = begin;
       if (begin + P::kAll <= a.f) {
         if (at != static_cast<int>(blockIdx.z) * kTokens) one.load_w(base, row, begin);
-        one.load_x(h, part, begin);
+        one.load_x(h, begin);
         auto go = [&](const P& now, P& next) {   // whether there is a next one
           r0 += every;
           const bool more = r0 + P::kAll <= a.f;
-          if (more) next.load_w(base, row, r0), next.load_x(h, part, r0);
-          now.multiply(base, row, h, acc);
+          if (more) next.load_w(base, row, r0), next.load_x(h, r0);
+          now.multiply(base, row, h, acc, power);
           return more;
         };
         while (go(one, two) && go(two, one)) {}
       }
-      if (r0 < a.f) one.rest(base, row, h, part, r0, a.f, lane, acc);
+      if (r0 < a.f) one.rest(base, row, h, r0, a.f, lane, acc, power);
 #pragma unroll
       for (int f = 0; f < FR; ++f)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < 2; ++i) {
+          const f32x4 whole = power.undo(acc[i][f], f);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sums[wave][f * 16 + c][i * 16 + 4 * q + e] = acc[i][f][e];
+          for (int e = 0; e < 4; ++e) sums[wave][f * 16 + c][i * 16 + 4 * q + e] = whole[e];
+        }
       __syncthreads();
       for (int t = threadIdx.x; t < kTokens * kCols * groups; t += 512) {
         const int r = t / (kCols * groups), group = t / kCols % groups, column = t % kCols;

@@ -25,7 +25,7 @@ struct Moe {
   const void* router;
   const void* w[3];
   const float* scale[3];   // 8-bit matrices, or NULL
-  void* h;                 // [m * top_k][ldh]: act(gate) * up of each row's experts; [2] of that with 16 bits: what rounding left
+  float* h;                // [m * top_k][ldh]: act(gate) * up of each row's experts
   void* y;
   int32_t* chosen;         // [m][top_k]
   float* share;            // [m][top_k]

@@ -156,7 +156,7 @@ bool aligned(const emb_experts_t& w, size_t size) {
 }
 
 struct MoeSpace {
-  void* h;
+  float* h;
   int64_t ldh;
   int32_t* chosen;
   float* share;
@@ -259,7 +259,7 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
     s.partial = ar.take<float>(uses * a.d * 4);
   }
   if (s.splits > 1) s.partial = ar.take<float>(s.splits * a.m * a.d * 4);
-  s.h = ar.take<void>(uses * s.ldh * 4);   // (in f32, or as two values of 16 bits)
+  s.h = ar.take<float>(uses * s.ldh * 4);
   if (!s.chosen) s.chosen = ar.take<int32_t>(uses * 4);
   if (!s.share) s.share = ar.take<float>(uses * 4);
   return s;
