@@ -162,14 +162,26 @@ struct MoeSpace {
   float* share;
   float* partial;
   double* logits;
-  int32_t up_variant, up_waves, up_blocks, up_parts, fused;
-  int32_t down_variant, down_waves, down_blocks, down_parts, down_rows, splits, chunk;
 };
 
-MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
+MoeSpace moe_space(Arena& ar, const emb_moe_t& a, const MoeChoice& c) {
   const int64_t uses = a.m * a.top_k;
   MoeSpace s = {};
   s.ldh = (a.f + 7) / 8 * 8, s.chosen = a.chosen, s.share = a.share;
+  if (c.apart) s.logits = ar.take<double>(a.m * a.experts * 8);
+  if (c.down_variant == kMoeMany) s.partial = ar.take<float>(uses * a.d * 4);
+  else if (c.splits > 1) s.partial = ar.take<float>(c.splits * a.m * a.d * 4);
+  s.h = ar.take<float>(uses * s.ldh * 4);
+  if (!s.chosen) s.chosen = ar.take<int32_t>(uses * 4);
+  if (!s.share) s.share = ar.take<float>(uses * 4);
+  return s;
+}
+
+}  // namespace
+
+MoeChoice embx::moe_choose(const emb_moe_t& a) {
+  const int64_t uses = a.m * a.top_k;
+  MoeChoice s = {};
   const int64_t used = std::min<int64_t>(uses, a.experts);   // experts, at most
   const int64_t step = a.gate.scale ? 64 : 32;               // of the reduction: a matrix instruction, or two
   // The up projections: four rows of x at most go by columns of four to a wavefront (kMoeFew; us a call: one query, one expert
@@ -208,9 +220,8 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
   // so 61; 4 of 64 of 704 x 2048 29 and 23.7; 22 rows, 2 of 20 of 1792 x 1088 62.6 and 62.0; but 8 rows, 4 of 16 of 704 x 256 23.0
   // and 24.5), and what is left of the routing in every workgroup of the up projections up to kPicked (those of 256 63 us with
   // a launch for it; f32, two rows, 4 of 64 of 512 x 1024 24.4 and 25.9)
-  const bool apart = a.m <= 256 && a.experts > 16;
-  if (apart) s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kPicked;
-  if (apart) s.logits = ar.take<double>(a.m * a.experts * 8);
+  s.apart = a.m <= 256 && a.experts > 16;
+  if (s.apart) s.fused = s.up_variant != kMoeMany && a.m * a.experts <= kPicked;
   // The down projection: 32 columns a workgroup, or 4 (one query, two of eight experts of 2816 x 1024: 17.9 with 4 columns,
   // 19.6 with 32; eight queries 37.8 and 41.7, but five with 8-bit weights 32.9 and 31.8; one, 1024 x 4096 19.8 and 17.9; f32,
   // 8 rows, 4 of 16 of 704 x 256 24.3 and 32).
@@ -256,16 +267,9 @@ MoeSpace moe_space(Arena& ar, const emb_moe_t& a) {
     const int64_t tile = 16 * s.down_blocks, tiles_each = (uses / a.experts + 16 + tile - 1) / tile;
     s.down_parts = static_cast<int32_t>(std::max<int64_t>(1, std::min(512 / workgroups(s.down_waves), tiles_each)));
     s.splits = 1;
-    s.partial = ar.take<float>(uses * a.d * 4);
   }
-  if (s.splits > 1) s.partial = ar.take<float>(s.splits * a.m * a.d * 4);
-  s.h = ar.take<float>(uses * s.ldh * 4);
-  if (!s.chosen) s.chosen = ar.take<int32_t>(uses * 4);
-  if (!s.share) s.share = ar.take<float>(uses * 4);
   return s;
 }
-
-}  // namespace
 
 extern "C" {
 
@@ -334,7 +338,7 @@ emb_status_t emb_moe_workspace(const emb_moe_t* a, size_t* bytes) {
   if (!a || !bytes) return EMB_ERR_INVALID_ARGUMENT;
   EMBX_TRY(check_shape(*a));
   Arena ar{nullptr};
-  if (a->m > 0) moe_space(ar, *a);
+  if (a->m > 0) moe_space(ar, *a, moe_choose(*a));
   *bytes = ar.used;
   return EMB_OK;
 }
@@ -352,9 +356,11 @@ emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes
   EMBX_TRY(check_vector(a->share, a->share ? 1 : 0, 4));
   if (a->m == 0) return EMB_OK;
   Arena ar{static_cast<char*>(workspace)};
-  const MoeSpace s = moe_space(ar, *a);
+  const MoeChoice c = moe_choose(*a);
+  const MoeSpace s = moe_space(ar, *a, c);
   EMBX_TRY(check_workspace(workspace, workspace_bytes, ar.used));
   Moe g = {};
+  static_cast<MoeChoice&>(g) = c;
   g.x = a->x, g.ldx = a->ldx, g.router = a->router, g.ldr = a->ldr;
   int i = 0;
   for (const emb_experts_t* w : {&a->gate, &a->up, &a->down}) {
@@ -362,11 +368,7 @@ emb_status_t emb_moe(const emb_moe_t* a, void* workspace, size_t workspace_bytes
     ++i;
   }
   g.h = s.h, g.ldh = s.ldh, g.chosen = s.chosen, g.share = s.share;
-  g.up_variant = s.up_variant, g.up_blocks = s.up_blocks, g.down_variant = s.down_variant, g.up_waves = s.up_waves;
-  g.down_waves = s.down_waves, g.fused = s.fused, g.logits = s.logits;
-  g.down_parts = s.down_parts, g.down_blocks = s.down_blocks;
-  g.up_parts = s.up_parts, g.down_rows = s.down_rows;
-  g.partial = s.partial, g.splits = s.splits, g.chunk = s.chunk;
+  g.partial = s.partial, g.logits = s.logits;
   const size_t size = esize(a->dtype);
   g.whole = aligned(a->x, a->ldx, size) && aligned(a->router, a->ldr, size) && aligned(a->gate, size) && aligned(a->up, size) &&
             aligned(a->down, size);
