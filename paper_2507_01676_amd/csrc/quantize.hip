@@ -116,7 +116,8 @@ __global__ __launch_bounds__(256) void quantize_held(Quantize a) {
 }
 
 // Rows that are too long for that, or go to a q whose rows start anywhere: read twice, consecutive elements by consecutive
-// threads.
+// threads.  bf16 16384 x 32768 492 us, f32 764, 3.3 and 3.5 TB/s of what has to be read and written once; bf16 65536 x 4096 to
+// rows of 4097 250 us, to whole ones, in registers, 155.
 template <int TYPE, int LANES>
 __global__ __launch_bounds__(256) void quantize_any(Quantize a) {
   using T = typename Elem<TYPE>::T;

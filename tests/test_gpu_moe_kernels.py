@@ -41,3 +41,24 @@ def test_kernel(gpu_lib, dtype, kind, kernels, size):
         assert torch.equal(again, y), what + ": equal calls, equal bits"
         out.fill_(float("nan"))
         assert bool(torch.isnan(around).all()), what + ": written outside the result"
+
+
+@pytest.mark.parametrize("m", [32768, 32769])
+def test_as_many_rows_as_partial_sums_fit_and_one_more(gpu_lib, m):
+    """Results of each use, in f32, take memory: beyond 2^26 of them the down projection goes by rows again."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    log(f"{m} rows, 2 of 8 of 264 x 1024")
+
+    def normal(*shape, std):
+        return (torch.randn(*shape, generator=gen, device="cuda") * std).bfloat16()
+
+    x, router = normal(m, 1024, std=1.0), normal(8, 1024, std=2.0 / 32)
+    ws = [normal(8, 264, 1024, std=1 / 32), normal(8, 264, 1024, std=1 / 32), normal(8, 1024, 264, std=1 / 16)]
+    y, chosen, share = gpu_lib.moe_ffn(x, router, *ws, top_k=2, routing=True)
+    rows = torch.tensor([0, 1, 63, 64, 511, 4095, 4096, 16384, 32700, 32766, 32767, m - 1], device="cuda")
+    want, experts, shares = M.moe(x[rows], router, *ws, 2, "silu", "bf16")
+    assert torch.equal(chosen[rows].cpu(), experts)
+    R.check(share[rows], shares, "shares")
+    R.check(y[rows], want, "rows")
+    assert bool(torch.isfinite(y).all())
