@@ -18,8 +18,9 @@
  * scale 2^-126.  A row with an infinity or NaN has scale NaN and zeros, so that what is
  * computed from it is NaN and not a number that looks right.
  *
- * linear_int8: sums of the products are exact; the scales, bias, activation and residual are
- * applied in f32, and the result is rounded once.  x is 8-bit integers with their scales
+ * linear_int8: sums of the products are exact; the scales (the larger one last, so that no
+ * infinity comes between), bias, activation and residual are applied in f32, and the result is
+ * rounded once.  x is 8-bit integers with their scales
  * (x_scale), or, without x_scale, a matrix of the call's type whose rows the call quantizes
  * first, as emb_quantize does.  A scale may be any f32 value, NaN among them.
  *
@@ -40,8 +41,8 @@
  * A call's outputs and workspace must not overlap its inputs, except that linear_int8's y may
  * be the residual itself (same pointer and row stride).  Calls that share a workspace must
  * not overlap in time.  Nothing is kept between calls, and equal calls give equal bits.
- * The aligned 16 bytes, or 4, that hold a row's start or end may be read whole; what they hold
- * beside the row does not matter.
+ * The aligned 16 bytes, or 4, that hold a row's start or end may be read whole, and of 8-bit
+ * matrices what lies between two rows; what that holds does not matter.
  *
  * Errors (emb_status_t of embx.h): EMB_ERR_INVALID_ARGUMENT for a NULL or misaligned pointer,
  * a size below its least (m >= 0, the others >= 1), a row stride below its row, top_k above

@@ -399,8 +399,19 @@ struct Finish<kDenseI8, kForward> {
 
   __device__ void put(float* s, const Held& h, int which) const {
     const int64_t row = i + which * step;
+    // (a sum, below 2^31, times a row's scale is no infinity on the way if that is below 2^96; if not, a sum times a column's scale
+    // is none, or the result is one.  Asked of a wavefront's rows at once: one by one 2048 x 4096 x 256 took 15.9 us, so 15.6)
+    const bool large = !(fabsf(h.row) < 0x1p96f);
+    if (__any(large)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) s[e] = static_cast<float>(__float_as_int(s[e])) * h.row * scale[e] + bias[e];
+      for (int e = 0; e < 8; ++e) {
+        const float sum = static_cast<float>(__float_as_int(s[e]));
+        s[e] = sum * (large ? scale[e] : h.row) * (large ? h.row : scale[e]) + bias[e];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] = static_cast<float>(__float_as_int(s[e])) * h.row * scale[e] + bias[e];
+    }
     if (g.result == kDenseF32) act8<kDenseF32>(s, g.act);
     else act8<kDenseBF16>(s, g.act);
     if (g.res) {
