@@ -18,9 +18,9 @@
  * scale 2^-126.  A row with an infinity or NaN has scale NaN and zeros, so that what is
  * computed from it is NaN and not a number that looks right.
  *
- * linear_int8: sums of the products are exact; the scales (the larger one last, so that no
- * infinity comes between), bias, activation and residual are applied in f32, and the result is
- * rounded once.  x is 8-bit integers with their scales
+ * linear_int8: sums of the products are exact; the scales (in an order in which no infinity
+ * comes between), bias, activation and residual are applied in f32, and the result is rounded
+ * once.  x is 8-bit integers with their scales
  * (x_scale), or, without x_scale, a matrix of the call's type whose rows the call quantizes
  * first, as emb_quantize does.  A scale may be any f32 value, NaN among them.
  *

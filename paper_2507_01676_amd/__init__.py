@@ -435,8 +435,8 @@ def dedup_tile(idx, stream=None):
 
 
 # The dense layers and their serving forms are imported with the first use of one of their names: the lookup does not need
-# their binding (_dense.so, built for one torch).  (This file alone, loaded under another name beside the package, has no package to import from: it
-# has the lookup.)
+# their binding (_dense.so, built for one torch).  (This file alone, loaded under another name beside the package, has no
+# package to import from: it has the lookup.)
 _LATE = {**dict.fromkeys(("dense", "ACTIVATIONS", "gated_ffn", "gated_ffn_backward", "linear", "linear_backward"), "dense"),
          **dict.fromkeys(("serving", "linear_int8", "moe_ffn", "quantize_rows"), "serving")}
 

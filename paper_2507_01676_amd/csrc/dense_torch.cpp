@@ -1,6 +1,7 @@
 // The dense layers' calls and their serving forms' for Python: checks torch tensors, allocates results and workspace with
-// torch's allocator and calls include/embx_dense.h and embx_serving.h on the current stream.  Argument marshalling only.  It is compiled because a small call's time
-// is the host's: 4.4 us with it, of which a launch is 2.6, and 7.1 with the same checks in Python.
+// torch's allocator and calls include/embx_dense.h and embx_serving.h on the current stream.  Argument marshalling only.
+// It is compiled because a small call's time is the host's: 4.4 us with it, of which a launch is 2.6, and 7.1 with the same
+// checks in Python.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

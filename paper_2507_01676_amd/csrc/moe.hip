@@ -6,8 +6,8 @@
 // ("uses"), number row * top_k + place; a workgroup finds the uses of an expert by itself, so nothing is sorted or counted in
 // memory.
 //
-// What bounds it is reading the weights of the experts that are used, once: 64 rows of bf16, 4 of 32 experts of 5632 x 2048, 432
-// us a call, 2.2 GB at 5.1 TB/s (the up projections 272 us, 5.4 TB/s; down 145).  With few rows a launch is not long enough to
+// What bounds it is reading the weights of the experts that are used, once: 64 rows of bf16, 4 of 32 experts of 5632 x 2048, 426
+// us a call, 2.2 GB at 5.2 TB/s (the up projections 268 us, 5.5 TB/s; down 143).  With few rows a launch is not long enough to
 // get there (about 5 us each, of which the loads' and the routing's latency is most): one query, two of eight of 2816 x 1024,
 // 16.2 us, 35 MB; five with 8-bit weights 31.3.
 #include <hip/hip_runtime.h>
@@ -533,8 +533,8 @@ constexpr int waves_of(int fragments) {
   return fragments * (EIGHT ? 2 : 1) * (TYPE == kDenseF32 ? 2 : 1) + (WHOLE ? 0 : EIGHT ? 2 : 4) <= (TYPE == kDenseF32 || EIGHT ? 3 : 4) ? 4 : 2;
 }
 
-// Uses of an expert that a workgroup lists before it multiplies, so that it reads the weights once for them: as many as leave
-// room for two workgroups a CU.
+// Uses of an expert that a workgroup lists before it multiplies, as many as leave room for two workgroups a CU: its weights come
+// from memory once for them, and from a cache for each further 16 to 64 (as many as are multiplied at a time).
 constexpr int kListed = kUses + 192;
 
 // The uses of one expert among up to kUses of them, `first` .. `first + count - 1`: a wavefront lists them in LDS of its own,
@@ -579,7 +579,8 @@ struct Uses {
 // before this one.
 // Every wavefront loads the next 128 bytes of its rows of both matrices, or 256 where 4 rows are all, while it multiplies those
 // before: whole lines, and enough under way with the CU's other wavefronts.  64 bytes at a time instead took 64 rows, 4 of 32 of
-// 5632 x 2048 from 433 us to 517.
+// 5632 x 2048 from 433 us to 517.  (With 64 rows of x at a time, which come from 26 uses an expert on, it is 64 bytes, and so it
+// is in moe_down_each with 32: registers hold no more.)
 template <int TYPE, bool EIGHT, bool WHOLE, int S, int FR, bool ROUTE>
 __global__ __launch_bounds__(512, (waves_of<TYPE, EIGHT, WHOLE>(FR))) void moe_up(Moe a) {
   constexpr int kRows = 16 / S, kTokens = 16 / S * FR;
@@ -832,8 +833,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 16 ? 4 : (waves_of<TYPE, EIGHT
   }
 }
 
-// The same for many rows: the uses of one expert and 32 columns for some wavefronts, as in moe_up, so that its weights are read
-// once, and not once for every a.down_rows rows: 200 rows, 4 of 64 of 704 x 4096 302 us a call, by rows 445.  Results go to
+// The same for many rows: the uses of one expert and 32 columns for some wavefronts, as in moe_up, so that its weights come from
+// memory once, and not once for every a.down_rows rows: 200 rows, 4 of 64 of 704 x 4096 302 us a call, by rows 445.  Results go to
 // memory in f32, a row for each use, without their shares.
 template <int TYPE, bool WHOLE, int FR>
 __global__ __launch_bounds__(512, (waves_of<TYPE, false, WHOLE>(TYPE == kDenseF32 ? FR : 2 * FR))) void moe_down_each(Moe a) {
